@@ -442,6 +442,128 @@ FST_API int fst_compose3_fill(fst_ctx *ctx, const fst_graph3_out *C, void *strea
  * count and the fill), generated_backward -1. */
 FST_API int fst_compose3_stats(const fst_ctx *ctx, fst_stats *out);
 
+/* ---- Between a network and its graphs ----------------------------------
+ * What a recogniser computes on the other side of the arc weights: a gated
+ * recurrence over the frames, the weights of emission graphs by a linear
+ * layer and log-softmax, a cross entropy over a vocabulary of words, and the
+ * gradients of all three.
+ *
+ * Activations and weights are row-major matrices of one of three types,
+ * with any row stride; the matrices of a call share one type.  Sums,
+ * statistics of the softmax and states are float32 whatever the type;
+ * results are rounded to their type once.  Results do not depend on anything but the
+ * arguments (no atomic sums).  Calls are asynchronous on `stream` after a
+ * call of the same sizes has made the workspace; they read nothing back, so
+ * they can be captured into a HIP graph. */
+enum fst_type { FST_F32 = 0, FST_F16 = 1, FST_BF16 = 2 };
+
+/* Element (r, c) is data[r * stride + c] (device memory, caller-owned);
+ * stride >= cols, in elements; data aligned to an element. */
+typedef struct {
+  void *data;
+  int64_t rows, cols, stride;
+  int32_t type; /* enum fst_type */
+} fst_matrix;
+
+/* Ragged sequences through a gated linear recurrence: sequence s is rows
+ * [offset[s], offset[s+1]) of x and gate, channel by channel
+ *   f_t = sigmoid(gate_t),  h_t = f_t h_(t-1) + (1 - f_t) x_t,  y_t = h_t
+ * from h = state[s] (0 where state is NULL), the first row first, or the last
+ * row first if `reverse` is not 0.
+ *   offset[num_seqs + 1]  device; 0, non-decreasing, ending with x.rows.
+ *                         Other offsets give unspecified results, and rows
+ *                         of no sequence are left as they are; no access
+ *                         leaves the matrices.  A sequence may be empty.
+ *   state[num_seqs * x.cols]  device, float32, or NULL
+ * num_seqs is at most FST_RECURRENCE_MAX_SEQS. */
+typedef struct {
+  int32_t num_seqs;
+  const int32_t *offset;
+  int32_t reverse;
+  fst_matrix x, gate;
+  const float *state;
+} fst_recurrence;
+
+#define FST_RECURRENCE_MAX_SEQS (1 << 22)
+#define FST_RECURRENCE_SAVE_ROWS 64
+
+/* y (as x; may not overlap x or gate), last[num_seqs * x.cols] (float32,
+ * optional): the state after each sequence (state[s], or 0, after an empty
+ * one).  saved (float32, optional), for fst_recurrence_grads:
+ * (x.rows / FST_RECURRENCE_SAVE_ROWS + num_seqs) * x.cols values, the states
+ * entering every 64 steps of a sequence; rows of `saved` that stand for no
+ * step are left as they are. */
+FST_API int fst_recurrence_run(fst_ctx *ctx, const fst_recurrence *R, const fst_matrix *y,
+                               float *last, float *saved, void *stream);
+
+/* Gradients of a loss by x, gate and state, from its gradients by y (grad_y)
+ * and by `last` (grad_last, float32, NULL = 0), with `saved` of the run on the
+ * same R:
+ *   D_t = grad_y_t + f_(t+1) D_(t+1)   (and grad_last at the last step)
+ *   grad_x_t = (1 - f_t) D_t
+ *   grad_gate_t = D_t (h_(t-1) - x_t) f_t (1 - f_t)
+ *   grad_state = f_0 D_0 (grad_last for an empty sequence)
+ * grad_state (float32, num_seqs * x.cols) is optional.  No output may overlap
+ * an input or another output. */
+FST_API int fst_recurrence_grads(fst_ctx *ctx, const fst_recurrence *R, const float *saved,
+                                 const fst_matrix *grad_y, const float *grad_last,
+                                 const fst_matrix *grad_x, const fst_matrix *grad_gate,
+                                 float *grad_state, void *stream);
+
+/* One step of many streams: row i of x, gate and y is a stream whose state
+ * is row slot[i] of state_in and state_out (device, float32, num_slots *
+ * x.cols; slot NULL: row i, num_slots >= x.rows).  A slot outside [0,
+ * num_slots) marks an idle row: its y is 0 and no state is read or written.
+ * state_out may be state_in; slots of one call must differ. */
+FST_API int fst_recurrence_step(fst_ctx *ctx, const fst_matrix *x, const fst_matrix *gate,
+                                const float *state_in, float *state_out, const int32_t *slot,
+                                int32_t num_slots, const fst_matrix *y, void *stream);
+
+/* Heads take at most this many rows of x and of w (FST_ERR_TOO_LARGE). */
+#define FST_HEAD_MAX_ROWS (1 << 25)
+
+/* Weights of emission graphs: weight[n * C + c] = z[n][c] - log-sum over c'
+ * of exp(z[n][c']), z = x w^T, for the N rows of x (frames, of any number of
+ * utterances) and the C rows of w (tokens), C >= 1 unless N is 0.  weight
+ * (device, float32, N * C) is the weight array of the graph whose state n
+ * has the C arcs [n C, (n + 1) C), or of several such graphs in a row.  A
+ * row whose scores hold a NaN comes out NaN; scores of -inf weigh -inf. */
+FST_API int fst_emission_weights(fst_ctx *ctx, const fst_matrix *x, const fst_matrix *w,
+                                 float *weight, void *stream);
+
+/* Gradients of a loss by x and w (each optional, not both) from its gradient
+ * by the weights (float32, N * C; e.g. what fst_grad_scatter returns), with
+ * the weights of fst_emission_weights on the same x and w:
+ *   dz = grad - exp(weight) * (sum of grad over the row)
+ *   grad_x = dz w,  grad_w = dz^T x
+ * dz is rounded to the matrices' type for the two products (float16: scaled
+ * by a power of two first, so that the smallest keep their digits). */
+FST_API int fst_emission_grads(fst_ctx *ctx, const fst_matrix *x, const fst_matrix *w,
+                               const float *weight, const float *grad,
+                               const fst_matrix *grad_x, const fst_matrix *grad_w,
+                               void *stream);
+
+/* Cross entropy over the V rows of w (words): with z = x w^T and
+ * lse[n] = log-sum over v of exp(z[n][v]), loss[n] = lse[n] -
+ * z[n][target[n]], or 0 where target[n] is -1 (no word).  Any other target
+ * outside [0, V) gives a loss of NaN.  The scores z are not stored.
+ * target: device, N; loss, lse: device, float32, N.  V >= 1 unless N is 0. */
+FST_API int fst_cross_entropy(fst_ctx *ctx, const fst_matrix *x, const fst_matrix *w,
+                              const int32_t *target, float *loss, float *lse, void *stream);
+
+/* Gradients of the sum over n of grad[n] * loss[n] by x and w (each optional,
+ * not both), with lse of fst_cross_entropy on the same x, w and target
+ * (grad: device, float32, N, or NULL for 1):
+ *   dz = grad[n] (exp(z - lse[n]) - [v = target[n]])  (0 for no word)
+ *   grad_x = dz w,  grad_w = dz^T x
+ * z is computed again, for a piece of the vocabulary at a time whose dz (in the
+ * matrices' type, float16 scaled as above) takes 512 MiB of workspace at most
+ * (more only where 256 words take more). */
+FST_API int fst_cross_entropy_grads(fst_ctx *ctx, const fst_matrix *x, const fst_matrix *w,
+                                    const int32_t *target, const float *lse, const float *grad,
+                                    const fst_matrix *grad_x, const fst_matrix *grad_w,
+                                    void *stream);
+
 /* Static string for a status code. */
 FST_API const char *fst_strerror(int code);
 

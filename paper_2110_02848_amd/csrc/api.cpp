@@ -21,6 +21,7 @@
 #include <vector>
 
 #include "internal.h"
+#include "layers.h"
 
 using namespace fstc;
 
@@ -69,6 +70,8 @@ struct fst_ctx {
       s_mpos, s_sweep, s_chg, s_ioff, s_iarc;
   // batches: the union of the A graphs, item tables, segment sums
   DevBuf u_off, u_src, u_dst, u_il, u_ol, u_w, u_start, u_accept, u_items, seg;
+  // operators between a network and its graphs: one workspace a call
+  DevBuf layer;
   // three-input composition
   DevBuf t_scal, t_aPerm, t_aArc, t_aRec, t_bPerm, t_bArc, t_bRec, t_bLab, t_bW, t_dPerm,
       t_dArc, t_dRec, t_dLab, t_dW, t_bflags, t_lists, t_tab, t_F, t_chunks, t_arcs, t_inoff,
@@ -1931,6 +1934,78 @@ int fill_parts(fst_ctx *c, const fst_graph_out *C, hipStream_t s) {
 
 }  // namespace
 
+namespace {
+
+// ---- operators between a network and its graphs ----
+
+bool matrix_ok(const fst_matrix *m) {
+  if (!m || m->rows < 0 || m->cols < 0 || m->rows > INT32_MAX || m->cols > INT32_MAX) return false;
+  if (m->type != FST_F32 && m->type != FST_F16 && m->type != FST_BF16) return false;
+  if (m->rows == 0 || m->cols == 0) return true;
+  // (the last element's byte fits 63 bits)
+  if (m->stride < m->cols || m->stride > (1ll << 62) / 4 / m->rows) return false;
+  return m->data && (uintptr_t)m->data % type_bytes(m->type) == 0;
+}
+
+// Of the given sizes and type.
+bool matrix_is(const fst_matrix *m, const fst_matrix &like, int64_t rows, int64_t cols) {
+  return matrix_ok(m) && m->rows == rows && m->cols == cols && m->type == like.type;
+}
+
+Mat mat(const fst_matrix &m) { return Mat{m.data, m.rows, m.cols, m.stride, m.type}; }
+
+bool recurrence_ok(const fst_recurrence *R) {
+  return R && R->num_seqs >= 0 && R->num_seqs <= FST_RECURRENCE_MAX_SEQS && matrix_ok(&R->x) &&
+         matrix_is(&R->gate, R->x, R->x.rows, R->x.cols) && (R->num_seqs == 0 || R->offset) &&
+         (R->num_seqs > 0 || R->x.rows == 0);
+}
+
+RecArgs recurrence_args(const fst_recurrence *R) {
+  RecArgs a{};
+  a.x = R->x.data;
+  a.xs = R->x.stride;
+  a.u = R->gate.data;
+  a.us = R->gate.stride;
+  a.state = R->state;
+  a.off = R->offset;
+  a.N = R->x.rows;
+  a.n = R->num_seqs;
+  a.D = (int)R->x.cols;
+  return a;
+}
+
+int hip_status(hipError_t e) {
+  if (e == hipSuccess) return FST_OK;
+  (void)hipGetLastError();
+  return e == hipErrorInvalidValue ? FST_ERR_TOO_LARGE : FST_ERR_HIP;
+}
+
+// Runs `f(workspace, &bytes)` twice: for the bytes it needs, then with them.
+template <typename F>
+int with_workspace(fst_ctx *c, F &&f) {
+  size_t need = 0;
+  FST_TRY(hip_status(f(nullptr, &need)));
+  FST_TRY(with_room(c, [&]() { return ensure(c, c->layer, need); }));
+  return hip_status(f(c->layer.p, &need));
+}
+
+// x and w of a head: rows of the same width, one type, at least one row of w.
+bool head_ok(const fst_matrix *x, const fst_matrix *w) {
+  return matrix_ok(x) && matrix_ok(w) && w->cols == x->cols && w->type == x->type &&
+         (w->rows > 0 || x->rows == 0);
+}
+bool head_large(const fst_matrix *x, const fst_matrix *w) {
+  return x->rows > FST_HEAD_MAX_ROWS || w->rows > FST_HEAD_MAX_ROWS;
+}
+
+bool head_grads_ok(const fst_matrix *x, const fst_matrix *w, const fst_matrix *gx,
+                   const fst_matrix *gw) {
+  return head_ok(x, w) && (gx || gw) && (!gx || matrix_is(gx, *x, x->rows, x->cols)) &&
+         (!gw || matrix_is(gw, *x, w->rows, w->cols));
+}
+
+}  // namespace
+
 extern "C" {
 
 int fst_ctx_create(int device, fst_ctx **ctx) {
@@ -2026,7 +2101,7 @@ void fst_ctx_destroy(fst_ctx *c) {
                     &c->t_coacc,  &c->t_keys0,  &c->t_keys1, &c->t_slots0, &c->t_slots1,
                     &c->t_idof,   &c->t_units,  &c->t_ucnt,  &c->t_aLab,  &c->t_aW,
                     &c->t_heavy,  &c->t_aLut,   &c->t_bLut,  &c->t_dLut, &c->t_bChain,
-                    &c->t_segs,   &c->t_segof};
+                    &c->t_segs,   &c->t_segof, &c->layer};
   for (DevBuf *b : bufs) release(*b);
   for (ScoreBufs *sb : {&c->score_f, &c->score_b}) {
     for (DevBuf *b : {&sb->sc, &sb->rec, &sb->term, &sb->mkey, &sb->pend, &sb->q, &sb->h,
@@ -2453,6 +2528,140 @@ int fst_segment_logsum(fst_ctx *c, const double *val, const uint8_t *flag, int32
   // host memory
   HIP_TRY(hipStreamSynchronize(s));
   return FST_OK;
+}
+
+// ---- operators between a network and its graphs ----
+
+int fst_recurrence_run(fst_ctx *c, const fst_recurrence *R, const fst_matrix *y, float *last,
+                       float *saved, void *stream) {
+  if (!c || !recurrence_ok(R) || !matrix_is(y, R->x, R->x.rows, R->x.cols))
+    return FST_ERR_INVALID_ARG;
+  if (R->num_seqs == 0 || R->x.cols == 0) return FST_OK;
+  DeviceGuard g(c->device);
+  if (!g.ok) return FST_ERR_HIP;
+  RecArgs a = recurrence_args(R);
+  a.y = y->data;
+  a.ys = y->stride;
+  a.last = last;
+  a.saved = saved;
+  return hip_status(launch_recurrence(a, R->x.type, R->reverse != 0,
+                                      reinterpret_cast<hipStream_t>(stream)));
+}
+
+int fst_recurrence_grads(fst_ctx *c, const fst_recurrence *R, const float *saved,
+                         const fst_matrix *grad_y, const float *grad_last,
+                         const fst_matrix *grad_x, const fst_matrix *grad_gate,
+                         float *grad_state, void *stream) {
+  if (!c || !recurrence_ok(R)) return FST_ERR_INVALID_ARG;
+  for (const fst_matrix *m : {grad_y, grad_x, grad_gate})
+    if (!matrix_is(m, R->x, R->x.rows, R->x.cols)) return FST_ERR_INVALID_ARG;
+  if (R->num_seqs == 0 || R->x.cols == 0) return FST_OK;
+  if (R->x.rows > 0 && !saved) return FST_ERR_INVALID_ARG;
+  DeviceGuard g(c->device);
+  if (!g.ok) return FST_ERR_HIP;
+  RecArgs a = recurrence_args(R);
+  a.gy = grad_y->data;
+  a.gys = grad_y->stride;
+  a.gx = grad_x->data;
+  a.gxs = grad_x->stride;
+  a.gu = grad_gate->data;
+  a.gus = grad_gate->stride;
+  a.saved = const_cast<float *>(saved);
+  a.glast = grad_last;
+  a.gstate = grad_state;
+  return hip_status(launch_recurrence_grads(a, R->x.type, R->reverse != 0,
+                                            reinterpret_cast<hipStream_t>(stream)));
+}
+
+int fst_recurrence_step(fst_ctx *c, const fst_matrix *x, const fst_matrix *gate,
+                        const float *state_in, float *state_out, const int32_t *slot,
+                        int32_t num_slots, const fst_matrix *y, void *stream) {
+  if (!c || !matrix_ok(x) || !matrix_is(gate, *x, x->rows, x->cols) ||
+      !matrix_is(y, *x, x->rows, x->cols) || num_slots < 0)
+    return FST_ERR_INVALID_ARG;
+  if (!slot && num_slots < x->rows) return FST_ERR_INVALID_ARG;
+  if (x->rows == 0 || x->cols == 0) return FST_OK;
+  if (num_slots > 0 && (!state_in || !state_out)) return FST_ERR_INVALID_ARG;
+  DeviceGuard g(c->device);
+  if (!g.ok) return FST_ERR_HIP;
+  StepArgs a{};
+  a.x = x->data;
+  a.xs = x->stride;
+  a.u = gate->data;
+  a.us = gate->stride;
+  a.y = y->data;
+  a.ys = y->stride;
+  a.in = state_in;
+  a.out = state_out;
+  a.slot = slot;
+  a.slots = num_slots;
+  a.n = x->rows;
+  a.D = (int)x->cols;
+  return hip_status(launch_recurrence_step(a, x->type, reinterpret_cast<hipStream_t>(stream)));
+}
+
+int fst_emission_weights(fst_ctx *c, const fst_matrix *x, const fst_matrix *w, float *weight,
+                         void *stream) {
+  if (!c || !head_ok(x, w)) return FST_ERR_INVALID_ARG;
+  if (head_large(x, w)) return FST_ERR_TOO_LARGE;
+  if (x->rows == 0) return FST_OK;
+  if (!weight) return FST_ERR_INVALID_ARG;
+  DeviceGuard g(c->device);
+  if (!g.ok) return FST_ERR_HIP;
+  return with_workspace(c, [&](void *ws, size_t *need) {
+    return launch_emission(mat(*x), mat(*w), weight, ws, need,
+                           reinterpret_cast<hipStream_t>(stream));
+  });
+}
+
+int fst_emission_grads(fst_ctx *c, const fst_matrix *x, const fst_matrix *w, const float *weight,
+                       const float *grad, const fst_matrix *grad_x, const fst_matrix *grad_w,
+                       void *stream) {
+  if (!c || !head_grads_ok(x, w, grad_x, grad_w)) return FST_ERR_INVALID_ARG;
+  if (head_large(x, w)) return FST_ERR_TOO_LARGE;
+  if (x->rows > 0 && (!weight || !grad)) return FST_ERR_INVALID_ARG;
+  DeviceGuard g(c->device);
+  if (!g.ok) return FST_ERR_HIP;
+  Mat gx, gw;
+  if (grad_x) gx = mat(*grad_x);
+  if (grad_w) gw = mat(*grad_w);
+  return with_workspace(c, [&](void *ws, size_t *need) {
+    return launch_emission_grads(mat(*x), mat(*w), weight, grad, grad_x ? &gx : nullptr,
+                                 grad_w ? &gw : nullptr, ws, need,
+                                 reinterpret_cast<hipStream_t>(stream));
+  });
+}
+
+int fst_cross_entropy(fst_ctx *c, const fst_matrix *x, const fst_matrix *w, const int32_t *target,
+                      float *loss, float *lse, void *stream) {
+  if (!c || !head_ok(x, w)) return FST_ERR_INVALID_ARG;
+  if (head_large(x, w)) return FST_ERR_TOO_LARGE;
+  if (x->rows == 0) return FST_OK;
+  if (!target || !loss || !lse) return FST_ERR_INVALID_ARG;
+  DeviceGuard g(c->device);
+  if (!g.ok) return FST_ERR_HIP;
+  return with_workspace(c, [&](void *ws, size_t *need) {
+    return launch_loss(mat(*x), mat(*w), target, loss, lse, ws, need,
+                       reinterpret_cast<hipStream_t>(stream));
+  });
+}
+
+int fst_cross_entropy_grads(fst_ctx *c, const fst_matrix *x, const fst_matrix *w,
+                            const int32_t *target, const float *lse, const float *grad,
+                            const fst_matrix *grad_x, const fst_matrix *grad_w, void *stream) {
+  if (!c || !head_grads_ok(x, w, grad_x, grad_w)) return FST_ERR_INVALID_ARG;
+  if (head_large(x, w)) return FST_ERR_TOO_LARGE;
+  if (x->rows > 0 && (!target || !lse)) return FST_ERR_INVALID_ARG;
+  DeviceGuard g(c->device);
+  if (!g.ok) return FST_ERR_HIP;
+  Mat gx, gw;
+  if (grad_x) gx = mat(*grad_x);
+  if (grad_w) gw = mat(*grad_w);
+  return with_workspace(c, [&](void *ws, size_t *need) {
+    return launch_loss_grads(mat(*x), mat(*w), target, lse, grad, grad_x ? &gx : nullptr,
+                             grad_w ? &gw : nullptr, ws, need,
+                             reinterpret_cast<hipStream_t>(stream));
+  });
 }
 
 const char *fst_strerror(int code) {

@@ -1,0 +1,905 @@
+// Heads of a network: log-softmax of a linear layer as weights of emission
+// graphs (fst_emission_weights), cross entropy over a vocabulary
+// (fst_cross_entropy), and the gradients of both.
+//
+// All of them are products of matrices on the matrix cores: scores z = x w^T
+// (N x C over H), and from the gradient dS of the scores dx = dS w (N x H over
+// C) and dw = dS^T x (C x H over N).  One kernel computes them, with an
+// epilogue for each: a row's maximum and sum of exponentials, scores, dS, or a
+// sum.  Scores of a vocabulary never reach memory: the forward pass leaves
+// each tile's maxima and sums, and the gradient computes them again for a
+// piece of the vocabulary at a time, whose dS it keeps for its two products.
+#include <math.h>
+
+#include <type_traits>
+
+#include "layers.h"
+
+namespace fstc {
+
+namespace {
+
+typedef _Float16 f16;
+typedef __bf16 bf16;
+typedef __attribute__((ext_vector_type(4))) float float4v;
+typedef __attribute__((ext_vector_type(4))) int int4v;
+typedef __attribute__((ext_vector_type(8))) _Float16 half8;
+typedef __attribute__((ext_vector_type(8))) __bf16 bhalf8;
+typedef __attribute__((ext_vector_type(4))) short short4v;
+
+#define LDS_PTR(p) ((__attribute__((address_space(3))) void *)(p))
+#define GLB_PTR(p) ((const __attribute__((address_space(1))) void *)(p))
+
+constexpr int KBYTES = 128;  // bytes of a row of an operand's tile along the sum
+
+template <typename T>
+constexpr int k_step() { return KBYTES / (int)sizeof(T); }
+
+// ---------------------------------------------------------------------------
+// matrix core products of fragments
+// ---------------------------------------------------------------------------
+
+// A fragment: 16 rows by 64 bytes of the sum; lane l holds row l & 15, the
+// 16-byte group l >> 4.
+template <typename T>
+struct Frag {
+  int4v v;
+};
+
+__device__ __forceinline__ float4v mac(const Frag<bf16> &a, const Frag<bf16> &b, float4v c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bhalf8, a.v),
+                                                 __builtin_bit_cast(bhalf8, b.v), c, 0, 0, 0);
+}
+__device__ __forceinline__ float4v mac(const Frag<f16> &a, const Frag<f16> &b, float4v c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, a.v),
+                                                __builtin_bit_cast(half8, b.v), c, 0, 0, 0);
+}
+// (four steps of 4: step j sums over element j of the four groups)
+__device__ __forceinline__ float4v mac(const Frag<float> &a, const Frag<float> &b, float4v c) {
+  const float4v x = __builtin_bit_cast(float4v, a.v), y = __builtin_bit_cast(float4v, b.v);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(x[j], y[j], c, 0, 0, 0);
+  return c;
+}
+
+// ---------------------------------------------------------------------------
+// operands' tiles in LDS
+// ---------------------------------------------------------------------------
+
+// Row-wise operand: element (r, k) at p[r * ld + k].  The tile holds R rows
+// of 128 bytes; 16-byte group g of row r lies at group g ^ (r & 7), so that the
+// 16 lanes of a fragment's group, a row apart, read different banks.  Rows
+// past the last are read as the last (their results are not used); k has no
+// tail (rows are padded with zeros to whole steps).
+template <typename T, int R, int NWV>
+struct RowTile {
+  static constexpr int BYTES = R * KBYTES;
+  static constexpr int LOADS = BYTES / 1024 / NWV;  // of 64 lanes by 16 bytes, a wavefront
+  static_assert(LOADS >= 1 && LOADS * 1024 * NWV == BYTES, "whole loads");
+  const char *src[LOADS];
+
+  __device__ __forceinline__ void init(const void *p, long long ld, long long r0, long long rows,
+                                       int wave, int lane) {
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+      const int r = (wave * LOADS + i) * 8 + (lane >> 3);
+      long long g = r0 + r;
+      g = g < rows ? g : rows - 1;
+      src[i] = static_cast<const char *>(p) + g * ld * (long long)sizeof(T) +
+               (((lane & 7) ^ (r & 7)) << 4);
+    }
+  }
+  // the tile of step `t`, to `lds`
+  __device__ __forceinline__ void fetch(char *lds, long long t, long long, int wave) const {
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i)
+      __builtin_amdgcn_global_load_lds(GLB_PTR(src[i] + t * KBYTES),
+                                       LDS_PTR(lds + (wave * LOADS + i) * 1024), 16, 0, 0);
+  }
+  __device__ __forceinline__ Frag<T> frag(const char *lds, int row, int half, int lane) const {
+    const int r = row + (lane & 15), g = half * 4 + (lane >> 4);
+    return Frag<T>{*reinterpret_cast<const int4v *>(lds + r * KBYTES + ((g ^ (r & 7)) << 4))};
+  }
+};
+
+// Column-wise operand: element (r, k) at p[k * ld + r].  The tile holds the
+// step's k, each R elements of consecutive r; of 16-bit types, 32-byte block
+// b of k lies at block b ^ swizzle(k), so that the reads that transpose (16
+// lanes read four k of 16 rows) meet different banks.  Past the last k the
+// last one is read (the other operand is zero there), past the last row a
+// group inside the row.
+template <typename T, int R, int NWV>
+struct ColTile {
+  static constexpr int K = k_step<T>();
+  static constexpr int ROW = R * (int)sizeof(T);  // bytes of a k
+  static constexpr int BYTES = ROW * K;
+  static constexpr int LOADS = BYTES / 1024 / NWV;
+  static constexpr int GROUPS = ROW / 16;
+  static constexpr int BLOCKS = ROW / 32;
+  static_assert(LOADS >= 1 && LOADS * 1024 * NWV == BYTES, "whole loads");
+  const char *src;
+  long long ldb;
+  int kk[LOADS], ro[LOADS];  // k and byte in the row of each load
+
+  static __device__ __forceinline__ int swizzle(int k) {
+    return sizeof(T) == 2 ? ((k & 3) | ((k >> 1) & 4)) & (BLOCKS - 1) : 0;
+  }
+
+  __device__ __forceinline__ void init(const void *p, long long ld, long long r0, long long rows,
+                                       int wave, int lane) {
+    src = static_cast<const char *>(p);
+    ldb = ld * (long long)sizeof(T);
+    src += r0 * (long long)sizeof(T);
+    const long long room = (rows - r0) * (long long)sizeof(T) - 16;
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+      const int q = (wave * LOADS + i) * 64 + lane;
+      const int k = q / GROUPS, g = q % GROUPS;
+      const int o = (((g >> 1) ^ swizzle(k)) << 5) + ((g & 1) << 4);
+      kk[i] = k;
+      ro[i] = o <= room ? o : (int)room;
+    }
+  }
+  __device__ __forceinline__ void fetch(char *lds, long long t, long long depth,
+                                        int wave) const {
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+      long long k = t * K + kk[i];
+      k = k < depth ? k : depth - 1;
+      __builtin_amdgcn_global_load_lds(GLB_PTR(src + k * ldb + ro[i]),
+                                       LDS_PTR(lds + (wave * LOADS + i) * 1024), 16, 0, 0);
+    }
+  }
+  // Fragment of 16 rows: lane l wants k = half * 32 + (l >> 4) * 8 .. + 8 of
+  // row l & 15 (16-bit types).  A read that transposes gives lane i of 16 the
+  // i-th column of four k: lanes 4j .. 4j + 3 point at the j-th k.
+  __device__ __forceinline__ Frag<T> frag(const char *lds, int row, int half, int lane) const {
+    if constexpr (sizeof(T) == 2) {
+      const int k = half * 32 + (lane >> 4) * 8 + ((lane >> 2) & 3);
+      const int block = row / 16, in = (lane & 3) * 8;
+      int2 v[2];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const int q = k + 4 * j;
+        const char *at = lds + q * ROW + ((block ^ swizzle(q)) << 5) + in;
+        v[j] = __builtin_bit_cast(
+            int2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                      (__attribute__((address_space(3))) short4v *)(LDS_PTR(at))));
+      }
+      return Frag<T>{int4v{v[0].x, v[0].y, v[1].x, v[1].y}};
+    } else {
+      const int k = half * 16 + (lane >> 4) * 4;
+      int4v v;
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        v[j] = *reinterpret_cast<const int *>(lds + (k + j) * ROW + (row + (lane & 15)) * 4);
+      return Frag<T>{v};
+    }
+  }
+};
+
+// ---------------------------------------------------------------------------
+// the product
+// ---------------------------------------------------------------------------
+
+// out[m][n] = sum over k of A(m, k) B(n, k), m < M, n < N, k < K, by tiles of
+// BM x BN.
+struct Product {
+  Operand A, B;
+  long long M, N, K;
+  int tiles_m, tiles_n;
+  int splits;            // parts of the sum (grid z), `steps` K-steps each
+  long long steps;
+  // epilogues
+  long long n0, words;   // what column 0 stands for (a piece's first word), all words
+  void *out;             // scores, dS, sums or results
+  long long ldo;
+  float2 *part;          // [M, parts]: each tile's maximum and sum of a row
+  int parts;
+  const int32_t *target; // [M]
+  float *hit;            // [M]: the target's score
+  const float *lse;      // [M]
+  const float *grad;     // [M] or null (1)
+  const float *scale;    // power of two on dS (16-bit floats), or null (1)
+  long long Mp, Np;      // dS: rows and columns to write, zeros past M and N
+  int add;               // sums: add to what is there
+};
+
+enum Epilogue {
+  EPI_PART,    // maxima and sums of exponentials, targets' scores
+  EPI_SCORE,   // the same and the scores as float32
+  EPI_DS,      // gradient of the scores
+  EPI_SUM,     // float32 sums, one block of M x N a split
+  EPI_RESULT   // results in T, times 1 / scale
+};
+
+template <typename T>
+__device__ __forceinline__ void store4(T *p, float4v v, int valid) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    if (j < valid) p[j] = (T)v[j];
+}
+
+// Maximum that takes no infinity as a shift (exp(inf - inf) is no number).
+__device__ __forceinline__ float shift_of(float m) { return fabsf(m) == INFINITY ? 0.0f : m; }
+
+__device__ __forceinline__ void join(float &m, float &s, float m2, float s2) {
+  const float mm = fmaxf(m, m2), sh = shift_of(mm);
+  s = s * __expf(m - sh) + s2 * __expf(m2 - sh);
+  m = mm;
+}
+
+template <typename T, template <typename, int, int> class TA,
+          template <typename, int, int> class TB, int BM, int BN, int WM, int WN, int EPI>
+__global__ __launch_bounds__(WM *WN *WAVE) void k_product(Product g) {
+  constexpr int NWV = WM * WN, FM = BM / WM / 16, FN = BN / WN / 16;
+  using A = TA<T, BM, NWV>;
+  using B = TB<T, BN, NWV>;
+  __shared__ __align__(1024) char s_a[2][A::BYTES];
+  __shared__ __align__(1024) char s_b[2][B::BYTES];
+  const int lane = threadIdx.x & (WAVE - 1);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
+  const int wm = wave / WN, wn = wave % WN;
+  const int tm = blockIdx.x % g.tiles_m, tn = blockIdx.x / g.tiles_m;
+  const long long m0 = (long long)tm * BM, n0 = (long long)tn * BN;
+  const int split = blockIdx.z;
+
+  A ta;
+  B tb;
+  ta.init(g.A.p, g.A.ld, m0, g.A.rows, wave, lane);
+  tb.init(g.B.p, g.B.ld, n0, g.B.rows, wave, lane);
+  const long long all = (g.K + k_step<T>() - 1) / k_step<T>();
+  const long long first = split * g.steps;
+  const long long end = first + g.steps < all ? first + g.steps : all;
+
+  float4v acc[FM][FN];
+#pragma unroll
+  for (int i = 0; i < FM; ++i)
+#pragma unroll
+    for (int j = 0; j < FN; ++j) acc[i][j] = float4v{0, 0, 0, 0};
+
+  if (first < end) {
+    ta.fetch(s_a[0], first, g.A.depth, wave);
+    tb.fetch(s_b[0], first, g.B.depth, wave);
+  }
+  int cur = 0;
+  for (long long t = first; t < end; ++t, cur ^= 1) {
+    // step t has landed, and no one reads the other buffer
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    if (t + 1 < end) {
+      ta.fetch(s_a[cur ^ 1], t + 1, g.A.depth, wave);
+      tb.fetch(s_b[cur ^ 1], t + 1, g.B.depth, wave);
+    }
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      Frag<T> fa[FM], fb[FN];
+#pragma unroll
+      for (int i = 0; i < FM; ++i) fa[i] = ta.frag(s_a[cur], (wm * FM + i) * 16, half, lane);
+#pragma unroll
+      for (int j = 0; j < FN; ++j) fb[j] = tb.frag(s_b[cur], (wn * FN + j) * 16, half, lane);
+#pragma unroll
+      for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int j = 0; j < FN; ++j) acc[i][j] = mac(fb[j], fa[i], acc[i][j]);
+    }
+  }
+
+  // acc[i][j][r]: row m0 + (wm FM + i) 16 + (lane & 15), column n0 + (wn FN +
+  // j) 16 + (lane >> 4) 4 + r
+#pragma unroll
+  for (int i = 0; i < FM; ++i) {
+    const long long m = m0 + (wm * FM + i) * 16 + (lane & 15);
+    const bool in = m < g.M;
+    const long long nb = n0 + wn * FN * 16 + (lane >> 4) * 4;
+    if constexpr (EPI == EPI_PART || EPI == EPI_SCORE) {
+      float mx = -INFINITY;
+      const long long tgt = EPI == EPI_PART && in ? g.target[m] : -1;
+#pragma unroll
+      for (int j = 0; j < FN; ++j) {
+        const long long n = nb + j * 16;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          if (n + r < g.N) mx = fmaxf(mx, acc[i][j][r]);
+          if (EPI == EPI_PART && n + r == tgt && n + r < g.N) g.hit[m] = acc[i][j][r];
+        }
+        if (EPI == EPI_SCORE && in && n < g.N) {
+          const long long left = g.N - n;
+          store4(static_cast<float *>(g.out) + m * g.ldo + n, acc[i][j],
+                 left < 4 ? (int)left : 4);
+        }
+      }
+      const float sh = shift_of(mx);
+      float sum = 0.0f;
+#pragma unroll
+      for (int j = 0; j < FN; ++j)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          if (nb + j * 16 + r < g.N) sum += __expf(acc[i][j][r] - sh);
+      // the four lanes of a row
+#pragma unroll
+      for (int x = 16; x < 64; x <<= 1) {
+        const float m2 = __shfl_xor(mx, x), s2 = __shfl_xor(sum, x);
+        join(mx, sum, m2, s2);
+      }
+      if (in && lane < 16) g.part[m * g.parts + tn * WN + wn] = make_float2(mx, sum);
+    } else if constexpr (EPI == EPI_DS) {
+      const float lse = in ? g.lse[m] : 0.0f;
+      const long long tgt = in ? g.target[m] : -1;
+      float c = in && tgt != -1 ? (g.grad ? g.grad[m] : 1.0f) : 0.0f;
+      if (tgt < -1 || tgt >= g.words) c = NAN;  // no such word
+      if (g.scale) c *= *g.scale;
+#pragma unroll
+      for (int j = 0; j < FN; ++j) {
+        const long long n = nb + j * 16;
+        float4v v;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const float p = __expf(acc[i][j][r] - lse) - (g.n0 + n + r == tgt ? 1.0f : 0.0f);
+          v[r] = c != 0.0f && n + r < g.N ? c * p : 0.0f;
+        }
+        if (m < g.Mp && n < g.Np) store4(static_cast<T *>(g.out) + m * g.ldo + n, v, 4);
+      }
+    } else {
+      const float back = EPI == EPI_RESULT && g.scale ? 1.0f / *g.scale : 1.0f;
+#pragma unroll
+      for (int j = 0; j < FN; ++j) {
+        const long long n = nb + j * 16;
+        if (!in || n >= g.N) continue;
+        const int valid = g.N - n < 4 ? (int)(g.N - n) : 4;
+        if constexpr (EPI == EPI_SUM) {
+          float *p = static_cast<float *>(g.out) + (split * g.M + m) * g.ldo + n;
+          float4v v = acc[i][j];
+          if (g.add)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+              if (r < valid) v[r] += p[r];
+          store4(p, v, valid);
+        } else {
+          store4(static_cast<T *>(g.out) + m * g.ldo + n, acc[i][j] * back, valid);
+        }
+      }
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// rows and elements
+// ---------------------------------------------------------------------------
+
+// A copy with rows padded with zeros to `cols` elements.
+template <typename T>
+__global__ __launch_bounds__(NT) void k_pad(const T *__restrict__ p, long long ld, long long rows,
+                                            long long n, T *__restrict__ out, long long cols) {
+  for (long long r = blockIdx.y; r < rows; r += gridDim.y)
+    for (long long c = (long long)blockIdx.x * NT + threadIdx.x; c < cols;
+         c += (long long)gridDim.x * NT)
+      out[r * cols + c] = c < n ? p[r * ld + c] : (T)0.0f;
+}
+
+__device__ __forceinline__ float wave_sum_f(float v) {
+#pragma unroll
+  for (int x = 1; x < WAVE; x <<= 1) v += __shfl_xor(v, x);
+  return v;
+}
+
+// log of the sum of exponentials of a row from its tiles' maxima and sums.
+__device__ __forceinline__ float row_lse(const float2 *part, int parts, int lane) {
+  float m = -INFINITY, s = 0.0f;
+  for (int i = lane; i < parts; i += WAVE) {
+    const float2 v = part[i];
+    join(m, s, v.x, v.y);
+  }
+#pragma unroll
+  for (int x = 1; x < WAVE; x <<= 1) {
+    const float m2 = __shfl_xor(m, x), s2 = __shfl_xor(s, x);
+    join(m, s, m2, s2);
+  }
+  // (a row of infinities: the sum, or none of it, is what is left)
+  return shift_of(m) + logf(s);
+}
+
+__global__ __launch_bounds__(NT) void k_loss(const float2 *__restrict__ part, int parts,
+                                             long long rows, const int32_t *__restrict__ target,
+                                             long long words, const float *__restrict__ hit,
+                                             float *__restrict__ loss, float *__restrict__ lse) {
+  const int lane = threadIdx.x & (WAVE - 1);
+  const long long r = (long long)blockIdx.x * NWAVES + threadIdx.x / WAVE;
+  if (r >= rows) return;
+  const float l = row_lse(part + r * parts, parts, lane);
+  if (lane) return;
+  lse[r] = l;
+  const int32_t t = target[r];
+  loss[r] = t == -1 ? 0.0f : t < -1 || t >= words ? NAN : l - hit[r];
+}
+
+// Scores to log-probabilities, in place.
+__global__ __launch_bounds__(NT) void k_normalise(const float2 *__restrict__ part, int parts,
+                                                  long long rows, long long cols,
+                                                  float *__restrict__ z) {
+  const int lane = threadIdx.x & (WAVE - 1);
+  const long long r = (long long)blockIdx.x * NWAVES + threadIdx.x / WAVE;
+  if (r >= rows) return;
+  const float l = row_lse(part + r * parts, parts, lane);
+  float *p = z + r * cols;
+  for (long long c = lane; c < cols; c += WAVE) p[c] -= l;
+}
+
+// The power of two that brings the largest |gradient| to [2^13, 2^14): 16-bit
+// floats then hold dS down to 2^-38 of it, and no |dS| (at most twice the
+// largest) overflows.  1 where the largest is 0, infinite or no number.
+__device__ __forceinline__ float scale_of(uint32_t bits) {
+  const int e = (int)(bits >> 23);
+  if (e == 0 || e >= 255) return 1.0f;
+  const int k = 127 + 13 - (e - 127);
+  return __uint_as_float((uint32_t)(k < 1 ? 1 : k > 254 ? 254 : k) << 23);
+}
+
+__global__ void k_clear_max(uint32_t *mx) { *mx = 0; }
+__global__ void k_scale(const uint32_t *mx, float *scale) { *scale = scale_of(*mx); }
+
+__global__ __launch_bounds__(NT) void k_max_abs(const float *__restrict__ p,
+                                                const int32_t *__restrict__ target, long long n,
+                                                uint32_t *__restrict__ mx) {
+  float m = 0.0f;
+  for (long long i = (long long)blockIdx.x * NT + threadIdx.x; i < n;
+       i += (long long)gridDim.x * NT)
+    if (target[i] >= 0) m = fmaxf(m, fabsf(p[i]));
+#pragma unroll
+  for (int x = 1; x < WAVE; x <<= 1) m = fmaxf(m, __shfl_xor(m, x));
+  if (__lane_id() == 0) atomicMax(mx, __float_as_uint(m));
+}
+
+// Emissions: the sum of each row's gradient, and the largest of the sums and
+// the gradients (mx not null).
+__global__ __launch_bounds__(NT) void k_row_sums(const float *__restrict__ grad, long long rows,
+                                                 long long cols, uint32_t *__restrict__ mx) {
+  const int lane = threadIdx.x & (WAVE - 1);
+  float m = 0.0f;
+  for (long long r = (long long)blockIdx.x * NWAVES + threadIdx.x / WAVE; r < rows;
+       r += (long long)gridDim.x * NWAVES) {
+    float s = 0.0f;
+    for (long long c = lane; c < cols; c += WAVE) {
+      const float g = grad[r * cols + c];
+      s += g;
+      m = fmaxf(m, fabsf(g));
+    }
+    m = fmaxf(m, fabsf(wave_sum_f(s)));
+  }
+#pragma unroll
+  for (int x = 1; x < WAVE; x <<= 1) m = fmaxf(m, __shfl_xor(m, x));
+  if (lane == 0) atomicMax(mx, __float_as_uint(m));
+}
+
+// dS = grad - exp(weight) sum(grad), a wavefront a row, zeros up to Rp x Cp.
+template <typename T>
+__global__ __launch_bounds__(NT) void k_emission_ds(const float *__restrict__ weight,
+                                                    const float *__restrict__ grad,
+                                                    long long rows, long long cols,
+                                                    const float *__restrict__ scale,
+                                                    T *__restrict__ out, long long Rp,
+                                                    long long Cp) {
+  const int lane = threadIdx.x & (WAVE - 1);
+  const long long r = (long long)blockIdx.x * NWAVES + threadIdx.x / WAVE;
+  if (r >= Rp) return;
+  const float k = scale ? *scale : 1.0f;
+  float s = 0.0f;
+  if (r < rows)
+    for (long long c = lane; c < cols; c += WAVE) s += grad[r * cols + c];
+  s = wave_sum_f(s);
+  for (long long c = lane; c < Cp; c += WAVE) {
+    float v = 0.0f;
+    if (r < rows && c < cols)
+      v = k * (grad[r * cols + c] - __expf(weight[r * cols + c]) * s);
+    out[r * Cp + c] = (T)v;
+  }
+}
+
+// Sums of the splits, in their order, to results.
+template <typename T>
+__global__ __launch_bounds__(NT) void k_finish(const float *__restrict__ sums, int splits,
+                                               long long rows, long long cols,
+                                               const float *__restrict__ scale,
+                                               T *__restrict__ out, long long ldo) {
+  const float back = scale ? 1.0f / *scale : 1.0f;
+  const long long n = rows * cols;
+  for (long long i = (long long)blockIdx.x * NT + threadIdx.x; i < n;
+       i += (long long)gridDim.x * NT) {
+    float v = 0.0f;
+    for (int s = 0; s < splits; ++s) v += sums[s * n + i];
+    const long long r = i / cols;
+    out[r * ldo + (i - r * cols)] = (T)(v * back);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// plans
+// ---------------------------------------------------------------------------
+
+constexpr int CUS = 256;
+
+long long up(long long x, long long m) { return (x + m - 1) / m * m; }
+unsigned blocks_for(long long items, long long per, long long most = 1 << 16) {
+  const long long b = (items + per - 1) / per;
+  return (unsigned)(b < 1 ? 1 : b < most ? b : most);
+}
+
+// Workspace, laid out by running a plan once without memory.
+struct Bump {
+  char *base;
+  size_t at = 0;
+  template <typename U>
+  U *take(long long n) {
+    U *p = reinterpret_cast<U *>(base + at);
+    at += ((size_t)n * sizeof(U) + 255) & ~(size_t)255;
+    return base ? p : nullptr;
+  }
+};
+
+struct Tile {
+  int bm, bn, wn;
+};
+constexpr Tile TILES[3] = {{256, 256, 4}, {128, 128, 2}, {64, 64, 2}};
+
+// The largest tile that still gives most CUs one.
+int tile_for(long long M, long long N) {
+  for (int i = 0; i < 2; ++i)
+    if (((M + TILES[i].bm - 1) / TILES[i].bm) * ((N + TILES[i].bn - 1) / TILES[i].bn) >=
+        CUS * 3 / 4)
+      return i;
+  return 2;
+}
+
+template <typename T, template <typename, int, int> class TA,
+          template <typename, int, int> class TB, int EPI>
+hipError_t product(Product g, int tile, hipStream_t s) {
+  const Tile c = TILES[tile];
+  const long long tm = (g.M + c.bm - 1) / c.bm, tn = (g.N + c.bn - 1) / c.bn;
+  if (tm * tn * 512 >= (1ll << 32) || tm > INT32_MAX || tn > INT32_MAX) return hipErrorInvalidValue;
+  g.tiles_m = (int)tm;
+  g.tiles_n = (int)tn;
+  const dim3 grid((unsigned)(tm * tn), 1, (unsigned)g.splits);
+  if (tile == 0)
+    k_product<T, TA, TB, 256, 256, 2, 4, EPI><<<grid, 512, 0, s>>>(g);
+  else if (tile == 1)
+    k_product<T, TA, TB, 128, 128, 2, 2, EPI><<<grid, 256, 0, s>>>(g);
+  else
+    k_product<T, TA, TB, 64, 64, 2, 2, EPI><<<grid, 256, 0, s>>>(g);
+  return hipGetLastError();
+}
+
+#define TRY(e)                           \
+  do {                                   \
+    const hipError_t e_ = (e);           \
+    if (e_ != hipSuccess) return e_;     \
+  } while (0)
+
+// An operand whose rows are whole K-steps from aligned addresses, as it is or
+// copied so.
+template <typename T>
+struct Laid {
+  Operand o;
+  T *copy;
+  long long cols;
+  Operand columns() const { return {o.p, o.ld, cols, o.depth}; }  // read column by column
+};
+
+template <typename T>
+Laid<T> lay(const Mat &m, Bump &b) {
+  const long long cols = up(m.cols, k_step<T>());
+  if ((uintptr_t)m.data % 16 == 0 && m.stride * sizeof(T) % 16 == 0 && cols == m.cols)
+    return {{m.data, m.stride, m.rows, m.rows}, nullptr, cols};
+  T *p = b.take<T>(m.rows * cols);
+  return {{p, cols, m.rows, m.rows}, p, cols};
+}
+template <typename T>
+hipError_t fill(const Laid<T> &l, const Mat &m, hipStream_t s) {
+  if (l.o.p == m.data || !l.copy) return hipSuccess;
+  const dim3 grid(blocks_for(l.cols, NT), blocks_for(m.rows, 1, 32768));
+  k_pad<T><<<grid, NT, 0, s>>>(static_cast<const T *>(m.data), m.stride, m.rows, m.cols, l.copy,
+                               l.cols);
+  return hipGetLastError();
+}
+
+// out = A B^T with the sum split where the tiles alone are too few.
+template <typename T, template <typename, int, int> class TA,
+          template <typename, int, int> class TB>
+struct SplitProduct {
+  int tile, splits;
+  long long steps;
+  float *sums;
+
+  void plan(long long M, long long N, long long K, Bump &b) {
+    splits = 1;
+    steps = 1;
+    if (M == 0 || N == 0) return;
+    tile = tile_for(M, N);
+    const long long tiles =
+        ((M + TILES[tile].bm - 1) / TILES[tile].bm) * ((N + TILES[tile].bn - 1) / TILES[tile].bn);
+    const long long all = (K + k_step<T>() - 1) / k_step<T>();
+    long long want = tiles >= CUS ? 1 : 2 * CUS / tiles;
+    want = want < all / 4 ? want : all / 4;  // four steps a split at least
+    want = want < 1 ? 1 : want > 256 ? 256 : want;
+    steps = (all + want - 1) / want;
+    splits = (int)((all + steps - 1) / steps);
+    sums = splits > 1 ? b.take<float>(splits * M * N) : nullptr;
+  }
+  hipError_t run(Operand A, Operand B, long long M, long long N, long long K, const float *scale,
+                 const Mat &out, hipStream_t s) const {
+    if (M == 0 || N == 0) return hipSuccess;
+    Product g{};
+    g.A = A;
+    g.B = B;
+    g.M = M;
+    g.N = N;
+    g.K = K;
+    g.splits = splits;
+    g.steps = steps;
+    if (splits == 1) {
+      g.out = out.data;
+      g.ldo = out.stride;
+      g.scale = scale;
+      return product<T, TA, TB, EPI_RESULT>(g, tile, s);
+    }
+    g.out = sums;
+    g.ldo = N;
+    TRY((product<T, TA, TB, EPI_SUM>(g, tile, s)));
+    k_finish<T><<<blocks_for(M * N, NT), NT, 0, s>>>(sums, splits, M, N, scale,
+                                                   static_cast<T *>(out.data), out.stride);
+    return hipGetLastError();
+  }
+};
+
+template <typename T>
+hipError_t emission_as(const Mat &x, const Mat &w, float *weight, Bump &b, hipStream_t s) {
+  const long long N = x.rows, C = w.rows;
+  const Laid<T> lx = lay<T>(x, b), lw = lay<T>(w, b);
+  const int tile = tile_for(N, C);
+  const int parts = (int)((C + TILES[tile].bn - 1) / TILES[tile].bn) * TILES[tile].wn;
+  float2 *part = b.take<float2>(N * parts);
+  if (!b.base) return hipSuccess;
+  TRY(fill(lx, x, s));
+  TRY(fill(lw, w, s));
+  Product g{};
+  g.A = lx.o;
+  g.B = lw.o;
+  g.M = N;
+  g.N = C;
+  g.K = lx.cols;
+  g.splits = 1;
+  g.steps = INT64_MAX / 2;
+  g.out = weight;
+  g.ldo = C;
+  g.part = part;
+  g.parts = parts;
+  TRY((product<T, RowTile, RowTile, EPI_SCORE>(g, tile, s)));
+  k_normalise<<<(unsigned)((N + NWAVES - 1) / NWAVES), NT, 0, s>>>(part, parts, N, C, weight);
+  return hipGetLastError();
+}
+
+template <typename T>
+hipError_t emission_grads_as(const Mat &x, const Mat &w, const float *weight, const float *grad,
+                             const Mat *gx, const Mat *gw, Bump &b, hipStream_t s) {
+  const long long N = x.rows, C = w.rows, H = x.cols;
+  const long long Np = up(N, 64), Cp = up(C, 64);
+  if (N == 0) {  // nothing to sum over
+    if (b.base && gw && C * H)
+      k_finish<T><<<blocks_for(C * H, NT), NT, 0, s>>>(nullptr, 0, C, H, nullptr,
+                                                     static_cast<T *>(gw->data), gw->stride);
+    b.take<char>(1);
+    return hipGetLastError();
+  }
+  const Laid<T> lx = lay<T>(x, b), lw = lay<T>(w, b);
+  T *ds = b.take<T>(Np * Cp);
+  uint32_t *mx = b.take<uint32_t>(1);
+  float *scale = b.take<float>(1);
+  SplitProduct<T, RowTile, ColTile> px{};
+  SplitProduct<T, ColTile, ColTile> pw{};
+  if (gx) px.plan(N, H, Cp, b);
+  if (gw) pw.plan(C, H, Np, b);
+  if (!b.base) return hipSuccess;
+  if (gw) TRY(fill(lx, x, s));
+  if (gx) TRY(fill(lw, w, s));
+  const bool scaled = sizeof(T) == 2 && std::is_same<T, f16>::value;
+  if (scaled) {
+    k_clear_max<<<1, 1, 0, s>>>(mx);
+    k_row_sums<<<blocks_for(N, NWAVES, 2048), NT, 0, s>>>(grad, N, C, mx);
+    k_scale<<<1, 1, 0, s>>>(mx, scale);
+  } else {
+    scale = nullptr;
+  }
+  k_emission_ds<T><<<(unsigned)((Np + NWAVES - 1) / NWAVES), NT, 0, s>>>(weight, grad, N, C, scale,
+                                                                        ds, Np, Cp);
+  TRY(hipGetLastError());
+  if (gx) TRY(px.run({ds, Cp, N, N}, lw.columns(), N, H, C, scale, *gx, s));
+  if (gw) TRY(pw.run({ds, Cp, Cp, Np}, lx.columns(), C, H, N, scale, *gw, s));
+  return hipSuccess;
+}
+
+template <typename T>
+hipError_t loss_as(const Mat &x, const Mat &w, const int32_t *target, float *loss, float *lse,
+                   Bump &b, hipStream_t s) {
+  const long long N = x.rows, V = w.rows;
+  const Laid<T> lx = lay<T>(x, b), lw = lay<T>(w, b);
+  const int tile = tile_for(N, V);
+  const int parts = (int)((V + TILES[tile].bn - 1) / TILES[tile].bn) * TILES[tile].wn;
+  float2 *part = b.take<float2>(N * parts);
+  float *hit = b.take<float>(N);
+  if (!b.base) return hipSuccess;
+  TRY(fill(lx, x, s));
+  TRY(fill(lw, w, s));
+  Product g{};
+  g.A = lx.o;
+  g.B = lw.o;
+  g.M = N;
+  g.N = V;
+  g.K = lx.cols;
+  g.splits = 1;
+  g.steps = INT64_MAX / 2;
+  g.part = part;
+  g.parts = parts;
+  g.target = target;
+  g.hit = hit;
+  TRY((product<T, RowTile, RowTile, EPI_PART>(g, tile, s)));
+  k_loss<<<(unsigned)((N + NWAVES - 1) / NWAVES), NT, 0, s>>>(part, parts, N, target, V, hit, loss,
+                                                            lse);
+  return hipGetLastError();
+}
+
+// Bytes of dS that a piece of the vocabulary may take.
+constexpr long long PIECE_BYTES = 512ll << 20;
+
+template <typename T>
+hipError_t loss_grads_as(const Mat &x, const Mat &w, const int32_t *target, const float *lse,
+                         const float *grad, const Mat *gx, const Mat *gw, Bump &b,
+                         hipStream_t s) {
+  const long long N = x.rows, V = w.rows, H = x.cols, Np = up(N, 64);
+  if (N == 0) {  // nothing to sum over
+    if (b.base && gw && V * H)
+      k_finish<T><<<blocks_for(V * H, NT), NT, 0, s>>>(nullptr, 0, V, H, nullptr,
+                                                     static_cast<T *>(gw->data), gw->stride);
+    b.take<char>(1);
+    return hipGetLastError();
+  }
+  const Laid<T> lx = lay<T>(x, b), lw = lay<T>(w, b);
+  long long piece = PIECE_BYTES / (Np * (long long)sizeof(T)) / 256 * 256;
+  piece = piece < 256 ? 256 : piece;
+  const bool whole = piece >= V;
+  if (whole) piece = V;
+  const long long Pp = up(piece, 64);
+  T *ds = b.take<T>(Np * Pp);
+  uint32_t *mx = b.take<uint32_t>(1);
+  float *scale = b.take<float>(1);
+  SplitProduct<T, RowTile, ColTile> px{};
+  SplitProduct<T, ColTile, ColTile> pw{};
+  float *sums = nullptr;
+  if (gx && whole) px.plan(N, H, Pp, b);
+  if (gx && !whole) sums = b.take<float>(N * H);
+  const size_t mark = b.at;
+  size_t most = mark;
+  if (gw) {
+    for (long long v0 = 0; v0 < V; v0 += piece) {
+      b.at = mark;
+      pw.plan(V - v0 < piece ? V - v0 : piece, H, Np, b);
+      most = b.at > most ? b.at : most;
+    }
+  }
+  b.at = most;
+  if (!b.base) return hipSuccess;
+  TRY(fill(lx, x, s));
+  TRY(fill(lw, w, s));
+  if (std::is_same<T, f16>::value && grad) {
+    k_clear_max<<<1, 1, 0, s>>>(mx);
+    k_max_abs<<<blocks_for(N, NT, 256), NT, 0, s>>>(grad, target, N, mx);
+    k_scale<<<1, 1, 0, s>>>(mx, scale);
+  } else if (std::is_same<T, f16>::value) {
+    k_clear_max<<<1, 1, 0, s>>>(mx);
+    k_scale<<<1, 1, 0, s>>>(mx, scale);
+  } else {
+    scale = nullptr;
+  }
+  TRY(hipGetLastError());
+  for (long long v0 = 0; v0 < V; v0 += piece) {
+    const long long n = V - v0 < piece ? V - v0 : piece, np = up(n, 64);
+    const Operand wp{static_cast<const T *>(lw.o.p) + v0 * lw.o.ld, lw.o.ld, n, n};
+    const Operand wc{wp.p, wp.ld, lw.cols, n};
+    Product g{};
+    g.A = lx.o;
+    g.B = wp;
+    g.M = N;
+    g.N = n;
+    g.K = lx.cols;
+    g.splits = 1;
+    g.steps = INT64_MAX / 2;
+    g.n0 = v0;
+    g.words = V;
+    g.out = ds;
+    g.ldo = np;
+    g.target = target;
+    g.lse = lse;
+    g.grad = grad;
+    g.scale = scale;
+    g.Mp = Np;
+    g.Np = np;
+    TRY((product<T, RowTile, RowTile, EPI_DS>(g, tile_for(N, n), s)));
+    if (gx && whole) {
+      TRY(px.run({ds, np, N, N}, wc, N, H, n, scale, *gx, s));
+    } else if (gx) {
+      Product q{};
+      q.A = {ds, np, N, N};
+      q.B = wc;
+      q.M = N;
+      q.N = H;
+      q.K = n;
+      q.splits = 1;
+      q.steps = INT64_MAX / 2;
+      q.out = sums;
+      q.ldo = H;
+      q.add = v0 > 0;
+      TRY((product<T, RowTile, ColTile, EPI_SUM>(q, tile_for(N, H), s)));
+    }
+    if (gw) {
+      Mat out = *gw;
+      out.data = static_cast<T *>(out.data) + v0 * out.stride;
+      out.rows = n;
+      b.at = mark;
+      pw.plan(n, H, Np, b);
+      TRY(pw.run({ds, np, np, Np}, lx.columns(), n, H, N, scale, out, s));
+    }
+  }
+  if (sums) {
+    k_finish<T><<<blocks_for(N * H, NT), NT, 0, s>>>(sums, 1, N, H, scale,
+                                                   static_cast<T *>(gx->data), gx->stride);
+    TRY(hipGetLastError());
+  }
+  return hipSuccess;
+}
+
+}  // namespace
+
+#define BY_TYPE(type, call)                  \
+  switch (type) {                            \
+    case FST_F32: { typedef float T; e = call; break; }  \
+    case FST_F16: { typedef f16 T; e = call; break; }    \
+    default: { typedef bf16 T; e = call; break; }        \
+  }
+
+hipError_t launch_emission(const Mat &x, const Mat &w, float *weight, void *ws, size_t *need,
+                           hipStream_t s) {
+  Bump b{static_cast<char *>(ws)};
+  hipError_t e;
+  BY_TYPE(x.type, emission_as<T>(x, w, weight, b, s));
+  *need = b.at;
+  return e;
+}
+
+hipError_t launch_emission_grads(const Mat &x, const Mat &w, const float *weight,
+                                 const float *grad, const Mat *gx, const Mat *gw, void *ws,
+                                 size_t *need, hipStream_t s) {
+  Bump b{static_cast<char *>(ws)};
+  hipError_t e;
+  BY_TYPE(x.type, emission_grads_as<T>(x, w, weight, grad, gx, gw, b, s));
+  *need = b.at;
+  return e;
+}
+
+hipError_t launch_loss(const Mat &x, const Mat &w, const int32_t *target, float *loss, float *lse,
+                       void *ws, size_t *need, hipStream_t s) {
+  Bump b{static_cast<char *>(ws)};
+  hipError_t e;
+  BY_TYPE(x.type, loss_as<T>(x, w, target, loss, lse, b, s));
+  *need = b.at;
+  return e;
+}
+
+hipError_t launch_loss_grads(const Mat &x, const Mat &w, const int32_t *target, const float *lse,
+                             const float *grad, const Mat *gx, const Mat *gw, void *ws,
+                             size_t *need, hipStream_t s) {
+  Bump b{static_cast<char *>(ws)};
+  hipError_t e;
+  BY_TYPE(x.type, loss_grads_as<T>(x, w, target, lse, grad, gx, gw, b, s));
+  *need = b.at;
+  return e;
+}
+
+}  // namespace fstc

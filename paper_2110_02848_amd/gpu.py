@@ -41,6 +41,14 @@ FST_ORDER_FORWARD_FIRST = 0
 FST_ORDER_COACCESSIBLE_FIRST = 1
 FST_ORDER_CONCURRENT = 2
 
+FST_F32 = 0
+FST_F16 = 1
+FST_BF16 = 2
+
+FST_RECURRENCE_MAX_SEQS = 1 << 22
+FST_RECURRENCE_SAVE_ROWS = 64
+FST_HEAD_MAX_ROWS = 1 << 25
+
 PHASES = ("preprocess", "forward", "backward", "count", "fill")
 
 # kernels timed one by one (enum fst_kernel): a composition's, then a score's
@@ -77,6 +85,17 @@ class _GraphOut3(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in (
         "arc_offset", "src", "dst", "ilabel", "olabel", "weight", "start", "accept", "key_a",
         "key_b", "key_fab", "key_d", "key_f", "arc_a", "arc_b", "arc_d")]
+
+
+class _Matrix(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("rows", ctypes.c_int64), ("cols", ctypes.c_int64),
+                ("stride", ctypes.c_int64), ("type", ctypes.c_int32)]
+
+
+class _Recurrence(ctypes.Structure):
+    _fields_ = [("num_seqs", ctypes.c_int32), ("offset", ctypes.c_void_p),
+                ("reverse", ctypes.c_int32), ("x", _Matrix), ("gate", _Matrix),
+                ("state", ctypes.c_void_p)]
 
 
 class _Stats(ctypes.Structure):
@@ -159,6 +178,19 @@ def load():
     lib.fst_compose3_fill.restype = ctypes.c_int
     lib.fst_compose3_stats.argtypes = [ctypes.c_void_p, ctypes.POINTER(_Stats)]
     lib.fst_compose3_stats.restype = ctypes.c_int
+    P = ctypes.c_void_p
+    M = ctypes.POINTER(_Matrix)
+    R = ctypes.POINTER(_Recurrence)
+    for name, args in dict(
+            fst_recurrence_run=[P, R, M, P, P, P],
+            fst_recurrence_grads=[P, R, P, M, P, M, M, P, P],
+            fst_recurrence_step=[P, M, M, P, P, P, ctypes.c_int32, M, P],
+            fst_emission_weights=[P, M, M, P, P],
+            fst_emission_grads=[P, M, M, P, P, M, M, P],
+            fst_cross_entropy=[P, M, M, P, P, P, P],
+            fst_cross_entropy_grads=[P, M, M, P, P, P, M, M, P]).items():
+        getattr(lib, name).argtypes = args
+        getattr(lib, name).restype = ctypes.c_int
     lib.fst_strerror.argtypes = [ctypes.c_int]
     lib.fst_strerror.restype = ctypes.c_char_p
     _lib = lib
@@ -185,6 +217,34 @@ def _stream_handle(stream):
     import torch
     s = stream if stream is not None else torch.cuda.current_stream()
     return ctypes.c_void_p(s.cuda_stream)
+
+
+def _matrix_types():
+    import torch
+    return {torch.float32: FST_F32, torch.float16: FST_F16, torch.bfloat16: FST_BF16}
+
+
+def _matrix(t, name):
+    """View of a 2-D device tensor whose rows are contiguous."""
+    typ = _matrix_types().get(t.dtype)
+    if typ is None or t.dim() != 2 or not t.is_cuda:
+        raise ValueError(f"{name}: a 2-D device tensor of float32, float16 or bfloat16 is needed")
+    rows, cols = t.shape
+    step, inner = t.stride()
+    if cols > 1 and rows > 0 and inner != 1:
+        raise ValueError(f"{name}: the elements of a row must lie side by side")
+    if rows > 1 and cols > 0 and step < cols:
+        raise ValueError(f"{name}: rows overlap")
+    return _Matrix(t.data_ptr() if rows and cols else None, rows, cols, max(step, cols), typ)
+
+
+def _array(t, name, dtype, n):
+    """Pointer of a contiguous device tensor of n elements (None: NULL)."""
+    if t is None:
+        return ctypes.c_void_p(None)
+    if t.dtype != dtype or t.numel() != n or not t.is_cuda or not t.is_contiguous():
+        raise ValueError(f"{name}: a contiguous device tensor of {n} {dtype} is needed")
+    return ctypes.c_void_p(t.data_ptr() if n else None)
 
 
 GRAPH_DTYPES = dict(arc_offset=np.int32, src=np.int32, dst=np.int32, ilabel=np.int32,
@@ -470,6 +530,161 @@ class Composer:
         post = self.posterior(C, sc["alpha"], sc["beta"], sc["total"], scale, stream)
         return (self.grad_scatter(post, C["arc_a"], A_arcs, stream),
                 self.grad_scatter(post, C["arc_b"], B_arcs, stream))
+
+    # ---- between a network and its graphs ----
+
+    def _allocating(self, stream):
+        """Context in which new tensors belong to the stream of the call."""
+        import contextlib
+
+        import torch
+        return torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext()
+
+    def _uses(self, stream, *tensors):
+        """Tells the allocator that the stream of the call uses these."""
+        if stream is not None:
+            for t in tensors:
+                if t is not None and t.numel():
+                    t.record_stream(stream)
+
+    def recurrence(self, x, gate, offset, state=None, reverse=False, save=False, stream=None):
+        """Gated linear recurrence over the sequences offset[s] .. offset[s + 1]
+        of rows of x and gate ([N, D], offset int32 [n + 1]) from state
+        (float32 [n, D], None: 0): dict(y: as x, last: the states after each
+        sequence, saved: what ``recurrence_grads`` needs, with ``save``)."""
+        import torch
+        R, n = self._recurrence(x, gate, offset, state, reverse)
+        N, D = x.shape
+        with self._allocating(stream):
+            y = torch.empty(N, D, dtype=x.dtype, device=x.device)
+            last = torch.empty(n, D, dtype=torch.float32, device=x.device)
+            saved = torch.empty(N // FST_RECURRENCE_SAVE_ROWS + n, D, dtype=torch.float32,
+                                device=x.device) if save else None
+        self._uses(stream, x, gate, offset, state)
+        rc = self._lib.fst_recurrence_run(self._h, R, _matrix(y, "y"), _ptr(last), _ptr(saved),
+                                          _stream_handle(stream))
+        _check(rc, "fst_recurrence_run")
+        return dict(y=y, last=last, saved=saved)
+
+    def recurrence_grads(self, x, gate, offset, grad_y, saved, state=None, grad_last=None,
+                         reverse=False, stream=None):
+        """Gradients of a loss by x, gate and state from those by y and last
+        (``recurrence`` of the same arguments with ``save``): dict(x, gate:
+        as x, state: float32 [n, D])."""
+        import torch
+        R, n = self._recurrence(x, gate, offset, state, reverse)
+        N, D = x.shape
+        rows = N // FST_RECURRENCE_SAVE_ROWS + n
+        with self._allocating(stream):
+            gx = torch.empty(N, D, dtype=x.dtype, device=x.device)
+            gu = torch.empty(N, D, dtype=x.dtype, device=x.device)
+            gs = torch.empty(n, D, dtype=torch.float32, device=x.device)
+        self._uses(stream, x, gate, offset, grad_y, saved, state, grad_last)
+        rc = self._lib.fst_recurrence_grads(
+            self._h, R, _array(saved, "saved", torch.float32, rows * D),
+            _matrix(grad_y, "grad_y"), _array(grad_last, "grad_last", torch.float32, n * D),
+            _matrix(gx, "x"), _matrix(gu, "gate"), _ptr(gs), _stream_handle(stream))
+        _check(rc, "fst_recurrence_grads")
+        return dict(x=gx, gate=gu, state=gs)
+
+    def _recurrence(self, x, gate, offset, state, reverse):
+        import torch
+        n = int(offset.numel()) - 1
+        if n < 0:
+            raise ValueError("offset: at least one entry is needed")
+        R = _Recurrence(n, _array(offset, "offset", torch.int32, n + 1), int(bool(reverse)),
+                        _matrix(x, "x"), _matrix(gate, "gate"),
+                        _array(state, "state", torch.float32, n * x.shape[1]))
+        return R, n
+
+    def recurrence_step(self, x, gate, state, slot=None, out=None, stream=None):
+        """One step of the rows of x and gate ([n, D]): (y, new states).
+        state: float32 [n, D]; the new states go to ``out`` (may be state) or
+        a new tensor.  With slot (int32 [n]) state holds any number of rows,
+        row i's is slot[i] (an idle row's lies outside), and the new states
+        replace the old ones unless ``out`` is given."""
+        import torch
+        slots, D = int(state.shape[0]), int(x.shape[1])
+        with self._allocating(stream):
+            if out is None:
+                out = torch.empty_like(state) if slot is None else state
+            y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        self._uses(stream, x, gate, state, slot, out)
+        rc = self._lib.fst_recurrence_step(
+            self._h, _matrix(x, "x"), _matrix(gate, "gate"),
+            _array(state, "state", torch.float32, slots * D),
+            _array(out, "out", torch.float32, slots * D),
+            _array(slot, "slot", torch.int32, x.shape[0]), slots, _matrix(y, "y"),
+            _stream_handle(stream))
+        _check(rc, "fst_recurrence_step")
+        return y, out
+
+    def emission_weights(self, x, w, out=None, stream=None):
+        """Log-softmax of x w^T, float32 [N, C] (x [N, H], w [C, H]): the arc
+        weights of emission graphs.  ``out`` may be a graph's weight tensor."""
+        import torch
+        N, C = int(x.shape[0]), int(w.shape[0])
+        with self._allocating(stream):
+            if out is None:
+                out = torch.empty(N, C, dtype=torch.float32, device=x.device)
+        self._uses(stream, x, w, out)
+        rc = self._lib.fst_emission_weights(self._h, _matrix(x, "x"), _matrix(w, "w"),
+                                            _array(out, "out", torch.float32, N * C),
+                                            _stream_handle(stream))
+        _check(rc, "fst_emission_weights")
+        return out
+
+    def emission_grads(self, x, w, weight, grad, need_x=True, need_w=True, stream=None):
+        """Gradients by x and w (None where not needed) from the gradient by
+        the weights of ``emission_weights`` (grad: float32, N * C)."""
+        import torch
+        n = int(x.shape[0]) * int(w.shape[0])
+        gx, gw = self._head_grads(x, w, need_x, need_w, stream)
+        self._uses(stream, x, w, weight, grad)
+        rc = self._lib.fst_emission_grads(
+            self._h, _matrix(x, "x"), _matrix(w, "w"),
+            _array(weight, "weight", torch.float32, n), _array(grad, "grad", torch.float32, n),
+            _matrix(gx, "x") if need_x else None, _matrix(gw, "w") if need_w else None,
+            _stream_handle(stream))
+        _check(rc, "fst_emission_grads")
+        return gx, gw
+
+    def cross_entropy(self, x, w, target, stream=None):
+        """Cross entropy of x w^T (x [N, H], w [V, H]) against target (int32
+        [N], -1: no word): dict(loss, lse: float32 [N])."""
+        import torch
+        N = int(x.shape[0])
+        with self._allocating(stream):
+            loss = torch.empty(N, dtype=torch.float32, device=x.device)
+            lse = torch.empty(N, dtype=torch.float32, device=x.device)
+        self._uses(stream, x, w, target)
+        rc = self._lib.fst_cross_entropy(self._h, _matrix(x, "x"), _matrix(w, "w"),
+                                         _array(target, "target", torch.int32, N), _ptr(loss),
+                                         _ptr(lse), _stream_handle(stream))
+        _check(rc, "fst_cross_entropy")
+        return dict(loss=loss, lse=lse)
+
+    def cross_entropy_grads(self, x, w, target, lse, grad=None, need_x=True, need_w=True,
+                            stream=None):
+        """Gradients of sum(grad * loss) by x and w (None where not needed);
+        grad: float32 [N], None: 1."""
+        import torch
+        N = int(x.shape[0])
+        gx, gw = self._head_grads(x, w, need_x, need_w, stream)
+        self._uses(stream, x, w, target, lse, grad)
+        rc = self._lib.fst_cross_entropy_grads(
+            self._h, _matrix(x, "x"), _matrix(w, "w"),
+            _array(target, "target", torch.int32, N), _array(lse, "lse", torch.float32, N),
+            _array(grad, "grad", torch.float32, N), _matrix(gx, "x") if need_x else None,
+            _matrix(gw, "w") if need_w else None, _stream_handle(stream))
+        _check(rc, "fst_cross_entropy_grads")
+        return gx, gw
+
+    def _head_grads(self, x, w, need_x, need_w, stream):
+        import torch
+        with self._allocating(stream):
+            return (torch.empty(x.shape, dtype=x.dtype, device=x.device) if need_x else None,
+                    torch.empty(w.shape, dtype=w.dtype, device=w.device) if need_w else None)
 
     def score_kernel_times(self):
         """{kernel: (ms, launches)} of the last timed fst_score."""
