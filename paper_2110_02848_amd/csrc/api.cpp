@@ -1971,6 +1971,7 @@ RecArgs recurrence_args(const fst_recurrence *R) {
   a.N = R->x.rows;
   a.n = R->num_seqs;
   a.D = (int)R->x.cols;
+  a.reverse = R->reverse != 0;
   return a;
 }
 
@@ -2544,8 +2545,9 @@ int fst_recurrence_run(fst_ctx *c, const fst_recurrence *R, const fst_matrix *y,
   a.ys = y->stride;
   a.last = last;
   a.saved = saved;
-  return hip_status(launch_recurrence(a, R->x.type, R->reverse != 0,
-                                      reinterpret_cast<hipStream_t>(stream)));
+  return with_workspace(c, [&](void *ws, size_t *need) {
+    return launch_recurrence(a, R->x.type, ws, need, reinterpret_cast<hipStream_t>(stream));
+  });
 }
 
 int fst_recurrence_grads(fst_ctx *c, const fst_recurrence *R, const float *saved,
@@ -2569,8 +2571,9 @@ int fst_recurrence_grads(fst_ctx *c, const fst_recurrence *R, const float *saved
   a.saved = const_cast<float *>(saved);
   a.glast = grad_last;
   a.gstate = grad_state;
-  return hip_status(launch_recurrence_grads(a, R->x.type, R->reverse != 0,
-                                            reinterpret_cast<hipStream_t>(stream)));
+  return with_workspace(c, [&](void *ws, size_t *need) {
+    return launch_recurrence_grads(a, R->x.type, ws, need, reinterpret_cast<hipStream_t>(stream));
+  });
 }
 
 int fst_recurrence_step(fst_ctx *c, const fst_matrix *x, const fst_matrix *gate,

@@ -28,16 +28,17 @@ struct RecArgs {
   const float *glast;            // [n, D] or null
   float *gstate;                 // [n, D] or null
   const int32_t *off;            // [n + 1]
-  float2 *agg;                   // split form: (product, sum) of each tile, [tiles, D]
-  long long N;
-  int n, D;
+  float2 *agg;                   // split form: maps of the units, [N / unit + n, D]
+  long long N, unit;             // rows; steps of a unit, 0: not split
+  int n, D, reverse;
 };
 
 constexpr int REC_SAVE = 64;  // scan steps between saved states
 static_assert(REC_SAVE == FST_RECURRENCE_SAVE_ROWS, "the header's constant");
 
-hipError_t launch_recurrence(const RecArgs &a, int type, bool reverse, hipStream_t s);
-hipError_t launch_recurrence_grads(const RecArgs &a, int type, bool reverse, hipStream_t s);
+// Called twice, as the heads below: first without workspace for its bytes.
+hipError_t launch_recurrence(RecArgs a, int type, void *ws, size_t *need, hipStream_t s);
+hipError_t launch_recurrence_grads(RecArgs a, int type, void *ws, size_t *need, hipStream_t s);
 
 struct StepArgs {
   const void *x, *u;
