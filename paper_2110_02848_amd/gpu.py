@@ -219,32 +219,41 @@ def _stream_handle(stream):
     return ctypes.c_void_p(s.cuda_stream)
 
 
-def _matrix_types():
-    import torch
-    return {torch.float32: FST_F32, torch.float16: FST_F16, torch.bfloat16: FST_BF16}
+_types = {}  # torch type -> enum fst_type
 
 
 def _matrix(t, name):
     """View of a 2-D device tensor whose rows are contiguous."""
-    typ = _matrix_types().get(t.dtype)
+    if not _types:
+        import torch
+        _types.update({torch.float32: FST_F32, torch.float16: FST_F16,
+                       torch.bfloat16: FST_BF16})
+    typ = _types.get(t.dtype)
     if typ is None or t.dim() != 2 or not t.is_cuda:
         raise ValueError(f"{name}: a 2-D device tensor of float32, float16 or bfloat16 is needed")
     rows, cols = t.shape
     step, inner = t.stride()
-    if cols > 1 and rows > 0 and inner != 1:
+    if inner != 1 and cols > 1 and rows > 0:
         raise ValueError(f"{name}: the elements of a row must lie side by side")
-    if rows > 1 and cols > 0 and step < cols:
-        raise ValueError(f"{name}: rows overlap")
-    return _Matrix(t.data_ptr() if rows and cols else None, rows, cols, max(step, cols), typ)
+    if step < cols:
+        if rows > 1:
+            raise ValueError(f"{name}: rows overlap")
+        step = cols
+    return _Matrix(t.data_ptr() if rows and cols else None, rows, cols, step, typ)
 
 
 def _array(t, name, dtype, n):
-    """Pointer of a contiguous device tensor of n elements (None: NULL)."""
+    """Address of a contiguous device tensor of n elements (None: NULL)."""
     if t is None:
-        return ctypes.c_void_p(None)
+        return None
     if t.dtype != dtype or t.numel() != n or not t.is_cuda or not t.is_contiguous():
         raise ValueError(f"{name}: a contiguous device tensor of {n} {dtype} is needed")
-    return ctypes.c_void_p(t.data_ptr() if n else None)
+    return t.data_ptr() if n else None
+
+
+def _address(t):
+    """Address of a tensor made here (None, or nothing in it: NULL)."""
+    return t.data_ptr() if t is not None and t.numel() else None
 
 
 GRAPH_DTYPES = dict(arc_offset=np.int32, src=np.int32, dst=np.int32, ilabel=np.int32,
@@ -279,6 +288,8 @@ class Composer:
         _check(self._lib.fst_ctx_create(self.device, ctypes.byref(h)), "fst_ctx_create")
         self._h = h
         self.options = {}  # options set on this context (option -> value)
+        import torch
+        self._dev = torch.device("cuda", self.device)
 
     def close(self):
         if getattr(self, "_h", None):
@@ -533,12 +544,19 @@ class Composer:
 
     # ---- between a network and its graphs ----
 
-    def _allocating(self, stream):
-        """Context in which new tensors belong to the stream of the call."""
-        import contextlib
-
+    def _call_stream(self, stream):
+        if stream is not None:
+            return stream.cuda_stream
         import torch
-        return torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext()
+        return torch._C._cuda_getCurrentRawStream(self.device)
+
+    def _new(self, stream, shape, dtype):
+        """A tensor that belongs to the stream of the call."""
+        import torch
+        if stream is None:
+            return torch.empty(shape, dtype=dtype, device=self._dev)
+        with torch.cuda.stream(stream):
+            return torch.empty(shape, dtype=dtype, device=self._dev)
 
     def _uses(self, stream, *tensors):
         """Tells the allocator that the stream of the call uses these."""
@@ -555,14 +573,13 @@ class Composer:
         import torch
         R, n = self._recurrence(x, gate, offset, state, reverse)
         N, D = x.shape
-        with self._allocating(stream):
-            y = torch.empty(N, D, dtype=x.dtype, device=x.device)
-            last = torch.empty(n, D, dtype=torch.float32, device=x.device)
-            saved = torch.empty(N // FST_RECURRENCE_SAVE_ROWS + n, D, dtype=torch.float32,
-                                device=x.device) if save else None
+        y = self._new(stream, (N, D), x.dtype)
+        last = self._new(stream, (n, D), torch.float32)
+        saved = self._new(stream, (N // FST_RECURRENCE_SAVE_ROWS + n, D),
+                          torch.float32) if save else None
         self._uses(stream, x, gate, offset, state)
-        rc = self._lib.fst_recurrence_run(self._h, R, _matrix(y, "y"), _ptr(last), _ptr(saved),
-                                          _stream_handle(stream))
+        rc = self._lib.fst_recurrence_run(self._h, R, _matrix(y, "y"), _address(last),
+                                          _address(saved), self._call_stream(stream))
         _check(rc, "fst_recurrence_run")
         return dict(y=y, last=last, saved=saved)
 
@@ -575,15 +592,13 @@ class Composer:
         R, n = self._recurrence(x, gate, offset, state, reverse)
         N, D = x.shape
         rows = N // FST_RECURRENCE_SAVE_ROWS + n
-        with self._allocating(stream):
-            gx = torch.empty(N, D, dtype=x.dtype, device=x.device)
-            gu = torch.empty(N, D, dtype=x.dtype, device=x.device)
-            gs = torch.empty(n, D, dtype=torch.float32, device=x.device)
+        gx, gu = self._new(stream, (N, D), x.dtype), self._new(stream, (N, D), x.dtype)
+        gs = self._new(stream, (n, D), torch.float32)
         self._uses(stream, x, gate, offset, grad_y, saved, state, grad_last)
         rc = self._lib.fst_recurrence_grads(
             self._h, R, _array(saved, "saved", torch.float32, rows * D),
             _matrix(grad_y, "grad_y"), _array(grad_last, "grad_last", torch.float32, n * D),
-            _matrix(gx, "x"), _matrix(gu, "gate"), _ptr(gs), _stream_handle(stream))
+            _matrix(gx, "x"), _matrix(gu, "gate"), _address(gs), self._call_stream(stream))
         _check(rc, "fst_recurrence_grads")
         return dict(x=gx, gate=gu, state=gs)
 
@@ -605,17 +620,16 @@ class Composer:
         replace the old ones unless ``out`` is given."""
         import torch
         slots, D = int(state.shape[0]), int(x.shape[1])
-        with self._allocating(stream):
-            if out is None:
-                out = torch.empty_like(state) if slot is None else state
-            y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        if out is None:
+            out = self._new(stream, (slots, D), torch.float32) if slot is None else state
+        y = self._new(stream, x.shape, x.dtype)
         self._uses(stream, x, gate, state, slot, out)
         rc = self._lib.fst_recurrence_step(
             self._h, _matrix(x, "x"), _matrix(gate, "gate"),
             _array(state, "state", torch.float32, slots * D),
             _array(out, "out", torch.float32, slots * D),
             _array(slot, "slot", torch.int32, x.shape[0]), slots, _matrix(y, "y"),
-            _stream_handle(stream))
+            self._call_stream(stream))
         _check(rc, "fst_recurrence_step")
         return y, out
 
@@ -624,13 +638,12 @@ class Composer:
         weights of emission graphs.  ``out`` may be a graph's weight tensor."""
         import torch
         N, C = int(x.shape[0]), int(w.shape[0])
-        with self._allocating(stream):
-            if out is None:
-                out = torch.empty(N, C, dtype=torch.float32, device=x.device)
+        if out is None:
+            out = self._new(stream, (N, C), torch.float32)
         self._uses(stream, x, w, out)
         rc = self._lib.fst_emission_weights(self._h, _matrix(x, "x"), _matrix(w, "w"),
                                             _array(out, "out", torch.float32, N * C),
-                                            _stream_handle(stream))
+                                            self._call_stream(stream))
         _check(rc, "fst_emission_weights")
         return out
 
@@ -645,7 +658,7 @@ class Composer:
             self._h, _matrix(x, "x"), _matrix(w, "w"),
             _array(weight, "weight", torch.float32, n), _array(grad, "grad", torch.float32, n),
             _matrix(gx, "x") if need_x else None, _matrix(gw, "w") if need_w else None,
-            _stream_handle(stream))
+            self._call_stream(stream))
         _check(rc, "fst_emission_grads")
         return gx, gw
 
@@ -654,13 +667,13 @@ class Composer:
         [N], -1: no word): dict(loss, lse: float32 [N])."""
         import torch
         N = int(x.shape[0])
-        with self._allocating(stream):
-            loss = torch.empty(N, dtype=torch.float32, device=x.device)
-            lse = torch.empty(N, dtype=torch.float32, device=x.device)
+        loss = self._new(stream, (N,), torch.float32)
+        lse = self._new(stream, (N,), torch.float32)
         self._uses(stream, x, w, target)
         rc = self._lib.fst_cross_entropy(self._h, _matrix(x, "x"), _matrix(w, "w"),
-                                         _array(target, "target", torch.int32, N), _ptr(loss),
-                                         _ptr(lse), _stream_handle(stream))
+                                         _array(target, "target", torch.int32, N),
+                                         _address(loss), _address(lse),
+                                         self._call_stream(stream))
         _check(rc, "fst_cross_entropy")
         return dict(loss=loss, lse=lse)
 
@@ -676,15 +689,13 @@ class Composer:
             self._h, _matrix(x, "x"), _matrix(w, "w"),
             _array(target, "target", torch.int32, N), _array(lse, "lse", torch.float32, N),
             _array(grad, "grad", torch.float32, N), _matrix(gx, "x") if need_x else None,
-            _matrix(gw, "w") if need_w else None, _stream_handle(stream))
+            _matrix(gw, "w") if need_w else None, self._call_stream(stream))
         _check(rc, "fst_cross_entropy_grads")
         return gx, gw
 
     def _head_grads(self, x, w, need_x, need_w, stream):
-        import torch
-        with self._allocating(stream):
-            return (torch.empty(x.shape, dtype=x.dtype, device=x.device) if need_x else None,
-                    torch.empty(w.shape, dtype=w.dtype, device=w.device) if need_w else None)
+        return (self._new(stream, x.shape, x.dtype) if need_x else None,
+                self._new(stream, w.shape, w.dtype) if need_w else None)
 
     def score_kernel_times(self):
         """{kernel: (ms, launches)} of the last timed fst_score."""
