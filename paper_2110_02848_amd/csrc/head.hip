@@ -66,49 +66,82 @@ __device__ __forceinline__ float4v mac(const Frag<float> &a, const Frag<float> &
 // operands' tiles in LDS
 // ---------------------------------------------------------------------------
 
-// Row-wise operand: element (r, k) at p[r * ld + k].  The tile holds R rows
-// of 128 bytes; 16-byte group g of row r lies at group g ^ (r & 7), so that the
+// Loads of 64 lanes by 16 bytes go from memory to LDS without registers: lane
+// i's bytes land at `lds` + 16 i.  Written as instructions, because the
+// compiler would wait for all of them before the next read of LDS; whoever
+// reads waits with wait_loads and a barrier.
+__device__ __forceinline__ void load_lds(uint32_t lds, uint32_t offset, const char *base) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+               :
+               : "s"(lds), "v"(offset), "s"(base)
+               : "memory");
+}
+template <int N>
+__device__ __forceinline__ void wait_loads() {  // all but the last N
+  asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory");
+}
+__device__ __forceinline__ uint32_t lds_address(const char *p) {
+  return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char *)p;
+}
+
+// Where the rows of a tile part lie among the rows of the whole tile: runs of
+// RUN rows, one every EVERY rows from row FIRST on.
+template <int RUN_, int EVERY_>
+struct Rows {
+  static constexpr int RUN = RUN_;
+  static __device__ __forceinline__ int of(int first, int r) {
+    return first + r / RUN * EVERY_ + r % RUN;
+  }
+};
+
+// Row-wise operand: element (r, k) at p[r * ld + k].  A part holds R rows of
+// 128 bytes; 16-byte group g of row r lies at group g ^ (r & 7), so that the
 // 16 lanes of a fragment's group, a row apart, read different banks.  Rows
 // past the last are read as the last (their results are not used); k has no
 // tail (rows are padded with zeros to whole steps).
-template <typename T, int R, int NWV>
+template <typename T, int R, int NWV, typename ROWS>
 struct RowTile {
   static constexpr int BYTES = R * KBYTES;
-  static constexpr int LOADS = BYTES / 1024 / NWV;  // of 64 lanes by 16 bytes, a wavefront
+  static constexpr int LOADS = BYTES / 1024 / NWV;  // a wavefront
   static_assert(LOADS >= 1 && LOADS * 1024 * NWV == BYTES, "whole loads");
-  const char *src[LOADS];
+  uint32_t off[LOADS];
 
-  __device__ __forceinline__ void init(const void *p, long long ld, long long r0, long long rows,
-                                       int wave, int lane) {
+  // `first`: the part's first row in the tile; the tile's rows are r0 on
+  __device__ __forceinline__ void init(const Operand &o, long long r0, int first, int wave,
+                                       int lane) {
+    const long long left = o.rows - 1 - r0;  // (>= 0)
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) {
       const int r = (wave * LOADS + i) * 8 + (lane >> 3);
-      long long g = r0 + r;
-      g = g < rows ? g : rows - 1;
-      src[i] = static_cast<const char *>(p) + g * ld * (long long)sizeof(T) +
-               (((lane & 7) ^ (r & 7)) << 4);
+      int g = ROWS::of(first, r);
+      g = g <= left ? g : (int)left;
+      off[i] = (uint32_t)g * (uint32_t)(o.ld * sizeof(T)) + (((lane & 7) ^ (r & 7)) << 4);
     }
   }
-  // the tile of step `t`, to `lds`
-  __device__ __forceinline__ void fetch(char *lds, long long t, long long, int wave) const {
+  static __device__ __forceinline__ const char *base(const Operand &o, long long r0) {
+    return static_cast<const char *>(o.p) + r0 * o.ld * (long long)sizeof(T);
+  }
+  // the part of step `t`, to `lds`
+  __device__ __forceinline__ void fetch(uint32_t lds, const char *base, const Operand &,
+                                        long long t, int wave, int) const {
 #pragma unroll
     for (int i = 0; i < LOADS; ++i)
-      __builtin_amdgcn_global_load_lds(GLB_PTR(src[i] + t * KBYTES),
-                                       LDS_PTR(lds + (wave * LOADS + i) * 1024), 16, 0, 0);
+      load_lds(lds + (wave * LOADS + i) * 1024, off[i], base + t * KBYTES);
   }
-  __device__ __forceinline__ Frag<T> frag(const char *lds, int row, int half, int lane) const {
+  // the fragment of rows `row` on, for half of the step
+  static __device__ __forceinline__ Frag<T> frag(const char *lds, int row, int half, int lane) {
     const int r = row + (lane & 15), g = half * 4 + (lane >> 4);
     return Frag<T>{*reinterpret_cast<const int4v *>(lds + r * KBYTES + ((g ^ (r & 7)) << 4))};
   }
 };
 
-// Column-wise operand: element (r, k) at p[k * ld + r].  The tile holds the
+// Column-wise operand: element (r, k) at p[k * ld + r].  A part holds the
 // step's k, each R elements of consecutive r; of 16-bit types, 32-byte block
 // b of k lies at block b ^ swizzle(k), so that the reads that transpose (16
 // lanes read four k of 16 rows) meet different banks.  Past the last k the
 // last one is read (the other operand is zero there), past the last row a
 // group inside the row.
-template <typename T, int R, int NWV>
+template <typename T, int R, int NWV, typename ROWS>
 struct ColTile {
   static constexpr int K = k_step<T>();
   static constexpr int ROW = R * (int)sizeof(T);  // bytes of a k
@@ -117,43 +150,49 @@ struct ColTile {
   static constexpr int GROUPS = ROW / 16;
   static constexpr int BLOCKS = ROW / 32;
   static_assert(LOADS >= 1 && LOADS * 1024 * NWV == BYTES, "whole loads");
-  const char *src;
-  long long ldb;
-  int kk[LOADS], ro[LOADS];  // k and byte in the row of each load
+  static_assert(ROWS::RUN * sizeof(T) % 32 == 0, "whole blocks");
+  uint32_t off[LOADS];
 
   static __device__ __forceinline__ int swizzle(int k) {
     return sizeof(T) == 2 ? ((k & 3) | ((k >> 1) & 4)) & (BLOCKS - 1) : 0;
   }
+  static __device__ __forceinline__ int k_of(int i, int wave, int lane) {
+    return ((wave * LOADS + i) * 64 + lane) / GROUPS;
+  }
 
-  __device__ __forceinline__ void init(const void *p, long long ld, long long r0, long long rows,
-                                       int wave, int lane) {
-    src = static_cast<const char *>(p);
-    ldb = ld * (long long)sizeof(T);
-    src += r0 * (long long)sizeof(T);
-    const long long room = (rows - r0) * (long long)sizeof(T) - 16;
+  __device__ __forceinline__ void init(const Operand &o, long long r0, int first, int wave,
+                                       int lane) {
+    const long long room = (o.rows - r0) * (long long)sizeof(T) - 16;  // (>= 0)
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) {
-      const int q = (wave * LOADS + i) * 64 + lane;
-      const int k = q / GROUPS, g = q % GROUPS;
-      const int o = (((g >> 1) ^ swizzle(k)) << 5) + ((g & 1) << 4);
-      kk[i] = k;
-      ro[i] = o <= room ? o : (int)room;
+      const int k = k_of(i, wave, lane), g = lane % GROUPS;
+      const int b = (((g >> 1) ^ swizzle(k)) << 5) + ((g & 1) << 4);
+      int at = ROWS::of(first, b / (int)sizeof(T)) * (int)sizeof(T);
+      at = at <= room ? at : (int)room;
+      off[i] = (uint32_t)k * (uint32_t)(o.ld * sizeof(T)) + at;
     }
   }
-  __device__ __forceinline__ void fetch(char *lds, long long t, long long depth,
-                                        int wave) const {
+  static __device__ __forceinline__ const char *base(const Operand &o, long long r0) {
+    return static_cast<const char *>(o.p) + r0 * (long long)sizeof(T);
+  }
+  __device__ __forceinline__ void fetch(uint32_t lds, const char *base, const Operand &o,
+                                        long long t, int wave, int lane) const {
+    const long long left = o.depth - t * K;  // of this step's k
+    const char *p = base + t * K * o.ld * (long long)sizeof(T);
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) {
-      long long k = t * K + kk[i];
-      k = k < depth ? k : depth - 1;
-      __builtin_amdgcn_global_load_lds(GLB_PTR(src + k * ldb + ro[i]),
-                                       LDS_PTR(lds + (wave * LOADS + i) * 1024), 16, 0, 0);
+      uint32_t at = off[i];
+      if (left < K) {
+        const int k = k_of(i, wave, lane), last = (int)left - 1;
+        if (k > last) at -= (uint32_t)(k - last) * (uint32_t)(o.ld * sizeof(T));
+      }
+      load_lds(lds + (wave * LOADS + i) * 1024, at, p);
     }
   }
   // Fragment of 16 rows: lane l wants k = half * 32 + (l >> 4) * 8 .. + 8 of
   // row l & 15 (16-bit types).  A read that transposes gives lane i of 16 the
   // i-th column of four k: lanes 4j .. 4j + 3 point at the j-th k.
-  __device__ __forceinline__ Frag<T> frag(const char *lds, int row, int half, int lane) const {
+  static __device__ __forceinline__ Frag<T> frag(const char *lds, int row, int half, int lane) {
     if constexpr (sizeof(T) == 2) {
       const int k = half * 32 + (lane >> 4) * 8 + ((lane >> 2) & 3);
       const int block = row / 16, in = (lane & 3) * 8;
@@ -229,25 +268,57 @@ __device__ __forceinline__ void join(float &m, float &s, float m2, float s2) {
   m = mm;
 }
 
-template <typename T, template <typename, int, int> class TA,
-          template <typename, int, int> class TB, int BM, int BN, int WM, int WN, int EPI>
+// Tile (tm, tn) of workgroup `id`.  Workgroups go to the eight XCDs in turn,
+// and each has a second-level cache: an XCD gets a run of consecutive tiles,
+// eight rows of tiles deep, so that its workgroups share rows of both operands.
+__device__ __forceinline__ void tile_of(const Product &g, unsigned id, int &tm, int &tn) {
+  const unsigned all = (unsigned)g.tiles_m * (unsigned)g.tiles_n;
+  const unsigned x = id % 8, per = all / 8, more = all % 8;
+  const unsigned q = x * per + (x < more ? x : more) + id / 8;
+  constexpr unsigned DEEP = 8;
+  const unsigned band = q / (DEEP * g.tiles_n), first = band * DEEP;
+  const unsigned deep = g.tiles_m - first < DEEP ? g.tiles_m - first : DEEP;
+  const unsigned in = q - first * g.tiles_n;
+  tm = (int)(first + in % deep);
+  tn = (int)(in / deep);
+}
+
+enum Layout { ROWS_ROWS, ROWS_COLS, COLS_COLS };  // of A and B
+
+template <typename T, int LAYOUT, int R, int NWV, typename ROWS>
+using TileA = std::conditional_t<LAYOUT == COLS_COLS, ColTile<T, R, NWV, ROWS>,
+                                 RowTile<T, R, NWV, ROWS>>;
+template <typename T, int LAYOUT, int R, int NWV, typename ROWS>
+using TileB = std::conditional_t<LAYOUT == ROWS_ROWS, RowTile<T, R, NWV, ROWS>,
+                                 ColTile<T, R, NWV, ROWS>>;
+
+template <typename T, int WN, int FM, int FN, int EPI>
+__device__ __forceinline__ void epilogue(const Product &g, float4v (&acc)[FM][FN], long long m0,
+                                         long long n0, int tn, int wm, int wn, int split,
+                                         int lane);
+
+// Tiles of BM x BN where there are too few large ones: two buffers, the next
+// step's loads under way while one step's fragments are multiplied.
+template <typename T, int LAYOUT, int BM, int BN, int WM, int WN, int EPI>
 __global__ __launch_bounds__(WM *WN *WAVE) void k_product(Product g) {
   constexpr int NWV = WM * WN, FM = BM / WM / 16, FN = BN / WN / 16;
-  using A = TA<T, BM, NWV>;
-  using B = TB<T, BN, NWV>;
-  __shared__ __align__(1024) char s_a[2][A::BYTES];
-  __shared__ __align__(1024) char s_b[2][B::BYTES];
+  using A = TileA<T, LAYOUT, BM, NWV, Rows<BM, BM>>;
+  using B = TileB<T, LAYOUT, BN, NWV, Rows<BN, BN>>;
+  __shared__ __align__(1024) char s_lds[2][A::BYTES + B::BYTES];
   const int lane = threadIdx.x & (WAVE - 1);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
   const int wm = wave / WN, wn = wave % WN;
-  const int tm = blockIdx.x % g.tiles_m, tn = blockIdx.x / g.tiles_m;
+  int tm, tn;
+  tile_of(g, blockIdx.x, tm, tn);
   const long long m0 = (long long)tm * BM, n0 = (long long)tn * BN;
   const int split = blockIdx.z;
 
   A ta;
   B tb;
-  ta.init(g.A.p, g.A.ld, m0, g.A.rows, wave, lane);
-  tb.init(g.B.p, g.B.ld, n0, g.B.rows, wave, lane);
+  ta.init(g.A, m0, 0, wave, lane);
+  tb.init(g.B, n0, 0, wave, lane);
+  const char *pa = A::base(g.A, m0), *pb = B::base(g.B, n0);
+  const uint32_t lds = lds_address(s_lds[0]);
   const long long all = (g.K + k_step<T>() - 1) / k_step<T>();
   const long long first = split * g.steps;
   const long long end = first + g.steps < all ? first + g.steps : all;
@@ -259,32 +330,211 @@ __global__ __launch_bounds__(WM *WN *WAVE) void k_product(Product g) {
     for (int j = 0; j < FN; ++j) acc[i][j] = float4v{0, 0, 0, 0};
 
   if (first < end) {
-    ta.fetch(s_a[0], first, g.A.depth, wave);
-    tb.fetch(s_b[0], first, g.B.depth, wave);
+    ta.fetch(lds, pa, g.A, first, wave, lane);
+    tb.fetch(lds + A::BYTES, pb, g.B, first, wave, lane);
   }
-  int cur = 0;
+  uint32_t cur = 0;
   for (long long t = first; t < end; ++t, cur ^= 1) {
     // step t has landed, and no one reads the other buffer
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    wait_loads<0>();
     __syncthreads();
     if (t + 1 < end) {
-      ta.fetch(s_a[cur ^ 1], t + 1, g.A.depth, wave);
-      tb.fetch(s_b[cur ^ 1], t + 1, g.B.depth, wave);
+      const uint32_t to = lds + (cur ^ 1) * (A::BYTES + B::BYTES);
+      ta.fetch(to, pa, g.A, t + 1, wave, lane);
+      tb.fetch(to + A::BYTES, pb, g.B, t + 1, wave, lane);
     }
+    const char *sa = s_lds[cur], *sb = sa + A::BYTES;
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
       Frag<T> fa[FM], fb[FN];
 #pragma unroll
-      for (int i = 0; i < FM; ++i) fa[i] = ta.frag(s_a[cur], (wm * FM + i) * 16, half, lane);
+      for (int i = 0; i < FM; ++i) fa[i] = A::frag(sa, (wm * FM + i) * 16, half, lane);
 #pragma unroll
-      for (int j = 0; j < FN; ++j) fb[j] = tb.frag(s_b[cur], (wn * FN + j) * 16, half, lane);
+      for (int j = 0; j < FN; ++j) fb[j] = B::frag(sb, (wn * FN + j) * 16, half, lane);
 #pragma unroll
       for (int i = 0; i < FM; ++i)
 #pragma unroll
         for (int j = 0; j < FN; ++j) acc[i][j] = mac(fb[j], fa[i], acc[i][j]);
     }
   }
+  epilogue<T, WN, FM, FN, EPI>(g, acc, m0, n0, tn, wm, wn, split, lane);
+}
 
+__device__ __forceinline__ void meet() {
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("s_barrier" : : : "memory");
+  __builtin_amdgcn_sched_barrier(0);
+}
+
+// Tiles of 256 x 256, eight wavefronts as 2 x 4 of 128 x 64 results each.  A
+// step (64 of the sum, 32 in float32) has four phases, the quarters of a
+// wavefront's results: (A0, B0), (A0, B1), (A1, B1), (A1, B0), where A0, A1, B0,
+// B1 are the halves of its rows and columns, 24 fragments read a step.  A phase
+// is a time for reading and one for multiplying, with a barrier after each,
+// and the wavefronts of the lower half are one time behind: on every SIMD one
+// wavefront multiplies while the other reads, so the matrix cores always have
+// one to feed them.
+//
+// Each half is a part of LDS of its own (16 KiB, two buffers), loaded by all
+// wavefronts (two loads each) as soon as no one reads it any more: A0 and B0
+// are last read in a step's phase 0, B1 in phase 1, A1 in phase 2, by the lower
+// half one time later, done with another time later; so in phases 0 .. 3 of step t
+// go out the loads of B1 and A1 of step t + 1 and A0 and B0 of step t + 2.
+// What a phase reads has landed for all once each wavefront has waited for its
+// own loads and met the others: in phase 3 for the next A0 and B0, in phase 0
+// for B1, in phase 1 for A1, each time for all but the last eight loads.
+template <typename T, int LAYOUT>
+struct Large {
+  static constexpr int NWV = 8;
+  using A = TileA<T, LAYOUT, 128, NWV, Rows<64, 128>>;
+  using B = TileB<T, LAYOUT, 128, NWV, Rows<32, 64>>;
+  static constexpr int PART = A::BYTES;
+  static_assert(A::BYTES == B::BYTES && A::LOADS == 2 && B::LOADS == 2, "equal parts");
+
+  A ta[2];
+  B tb[2];
+  const char *pa, *pb;
+  const char *lds;
+  uint32_t at;
+  int lane, wave, wm, wn;
+  Frag<T> fa[4][2], fb[2][2][2];  // [fragment][half of the step]; fb: [half of the columns]
+
+  // buffer: A0, A1, B0, B1
+  static __device__ __forceinline__ int part(int buffer, int which) {
+    return (buffer * 4 + which) * PART;
+  }
+  template <int H>
+  __device__ __forceinline__ void load_a(const Product &g, long long t, int buffer) {
+    ta[H].fetch(at + part(buffer, H), pa, g.A, t, wave, lane);
+  }
+  template <int H>
+  __device__ __forceinline__ void load_b(const Product &g, long long t, int buffer) {
+    tb[H].fetch(at + part(buffer, 2 + H), pb, g.B, t, wave, lane);
+  }
+  template <int H>
+  __device__ __forceinline__ void read_a(int buffer) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+        fa[i][k] = A::frag(lds + part(buffer, H), wm * 64 + i * 16, k, lane);
+  }
+  template <int H>
+  __device__ __forceinline__ void read_b(int buffer) {
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+        fb[H][j][k] = B::frag(lds + part(buffer, 2 + H), wn * 32 + j * 16, k, lane);
+  }
+  template <int HA, int HB>
+  __device__ __forceinline__ void multiply(float4v (&acc)[8][4]) {
+    __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+          acc[HA * 4 + i][HB * 2 + j] = mac(fb[HB][j][k], fa[i][k], acc[HA * 4 + i][HB * 2 + j]);
+    __builtin_amdgcn_s_setprio(0);
+  }
+
+  // Step t of buffer `b`; LEFT: steps after it (2: two at least).
+  template <int LEFT>
+  __device__ __forceinline__ void step(const Product &g, long long t, int b,
+                                       float4v (&acc)[8][4]) {
+    read_a<0>(b);
+    read_b<0>(b);
+    if constexpr (LEFT > 0) load_b<1>(g, t + 1, b ^ 1);
+    wait_loads<(LEFT > 0) ? 8 : 2>();
+    meet();
+    multiply<0, 0>(acc);
+    meet();
+    read_b<1>(b);
+    if constexpr (LEFT > 0) load_a<1>(g, t + 1, b ^ 1);
+    wait_loads<(LEFT > 0) ? 8 : 0>();
+    meet();
+    multiply<0, 1>(acc);
+    meet();
+    read_a<1>(b);
+    if constexpr (LEFT > 1) load_a<0>(g, t + 2, b);
+    meet();
+    multiply<1, 1>(acc);
+    meet();
+    if constexpr (LEFT > 1) load_b<0>(g, t + 2, b);
+    if constexpr (LEFT > 0) wait_loads<(LEFT > 1) ? 8 : 4>();
+    meet();
+    multiply<1, 0>(acc);
+    meet();
+  }
+};
+
+template <typename T, int LAYOUT, int EPI>
+__global__ __launch_bounds__(512) void k_product_large(Product g) {
+  using L = Large<T, LAYOUT>;
+  __shared__ __align__(1024) char s_lds[8 * L::PART];
+  L l;
+  l.lane = threadIdx.x & (WAVE - 1);
+  l.wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
+  l.wm = l.wave / 4;
+  l.wn = l.wave % 4;
+  l.lds = s_lds;
+  l.at = lds_address(s_lds);
+  int tm, tn;
+  tile_of(g, blockIdx.x, tm, tn);
+  const long long m0 = (long long)tm * 256, n0 = (long long)tn * 256;
+  const int split = blockIdx.z;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    l.ta[h].init(g.A, m0, h * 64, l.wave, l.lane);
+    l.tb[h].init(g.B, n0, h * 32, l.wave, l.lane);
+  }
+  l.pa = L::A::base(g.A, m0);
+  l.pb = L::B::base(g.B, n0);
+  const long long all = (g.K + k_step<T>() - 1) / k_step<T>();
+  const long long first = split * g.steps;
+  const long long end = first + g.steps < all ? first + g.steps : all;
+
+  float4v acc[8][4];
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) acc[i][j] = float4v{0, 0, 0, 0};
+
+  if (first < end) {
+    const bool two = first + 1 < end;
+    l.template load_a<0>(g, first, 0);
+    l.template load_b<0>(g, first, 0);
+    l.template load_b<1>(g, first, 0);
+    l.template load_a<1>(g, first, 0);
+    if (two) {
+      l.template load_a<0>(g, first + 1, 1);
+      l.template load_b<0>(g, first + 1, 1);
+      wait_loads<8>();
+    } else {
+      wait_loads<4>();
+    }
+    meet();
+    if (l.wm == 1) meet();
+    int b = 0;
+    long long t = first;
+    for (; t + 2 < end; ++t, b ^= 1) l.template step<2>(g, t, b, acc);
+    if (two) {
+      l.template step<1>(g, t, b, acc);
+      ++t;
+      b ^= 1;
+    }
+    l.template step<0>(g, t, b, acc);
+    if (l.wm == 0) meet();
+  }
+  epilogue<T, 4, 8, 4, EPI>(g, acc, m0, n0, tn, l.wm, l.wn, split, l.lane);
+}
+
+template <typename T, int WN, int FM, int FN, int EPI>
+__device__ __forceinline__ void epilogue(const Product &g, float4v (&acc)[FM][FN], long long m0,
+                                         long long n0, int tn, int wm, int wn, int split,
+                                         int lane) {
   // acc[i][j][r]: row m0 + (wm FM + i) 16 + (lane & 15), column n0 + (wn FN +
   // j) 16 + (lane >> 4) 4 + r
 #pragma unroll
@@ -550,8 +800,7 @@ int tile_for(long long M, long long N) {
   return 2;
 }
 
-template <typename T, template <typename, int, int> class TA,
-          template <typename, int, int> class TB, int EPI>
+template <typename T, int LAYOUT, int EPI>
 hipError_t product(Product g, int tile, hipStream_t s) {
   const Tile c = TILES[tile];
   const long long tm = (g.M + c.bm - 1) / c.bm, tn = (g.N + c.bn - 1) / c.bn;
@@ -560,11 +809,11 @@ hipError_t product(Product g, int tile, hipStream_t s) {
   g.tiles_n = (int)tn;
   const dim3 grid((unsigned)(tm * tn), 1, (unsigned)g.splits);
   if (tile == 0)
-    k_product<T, TA, TB, 256, 256, 2, 4, EPI><<<grid, 512, 0, s>>>(g);
+    k_product_large<T, LAYOUT, EPI><<<grid, 512, 0, s>>>(g);
   else if (tile == 1)
-    k_product<T, TA, TB, 128, 128, 2, 2, EPI><<<grid, 256, 0, s>>>(g);
+    k_product<T, LAYOUT, 128, 128, 2, 2, EPI><<<grid, 256, 0, s>>>(g);
   else
-    k_product<T, TA, TB, 64, 64, 2, 2, EPI><<<grid, 256, 0, s>>>(g);
+    k_product<T, LAYOUT, 64, 64, 2, 2, EPI><<<grid, 256, 0, s>>>(g);
   return hipGetLastError();
 }
 
@@ -602,8 +851,7 @@ hipError_t fill(const Laid<T> &l, const Mat &m, hipStream_t s) {
 }
 
 // out = A B^T with the sum split where the tiles alone are too few.
-template <typename T, template <typename, int, int> class TA,
-          template <typename, int, int> class TB>
+template <typename T, int LAYOUT>
 struct SplitProduct {
   int tile, splits;
   long long steps;
@@ -639,11 +887,11 @@ struct SplitProduct {
       g.out = out.data;
       g.ldo = out.stride;
       g.scale = scale;
-      return product<T, TA, TB, EPI_RESULT>(g, tile, s);
+      return product<T, LAYOUT, EPI_RESULT>(g, tile, s);
     }
     g.out = sums;
     g.ldo = N;
-    TRY((product<T, TA, TB, EPI_SUM>(g, tile, s)));
+    TRY((product<T, LAYOUT, EPI_SUM>(g, tile, s)));
     k_finish<T><<<blocks_for(M * N, NT), NT, 0, s>>>(sums, splits, M, N, scale,
                                                    static_cast<T *>(out.data), out.stride);
     return hipGetLastError();
@@ -672,7 +920,7 @@ hipError_t emission_as(const Mat &x, const Mat &w, float *weight, Bump &b, hipSt
   g.ldo = C;
   g.part = part;
   g.parts = parts;
-  TRY((product<T, RowTile, RowTile, EPI_SCORE>(g, tile, s)));
+  TRY((product<T, ROWS_ROWS, EPI_SCORE>(g, tile, s)));
   k_normalise<<<(unsigned)((N + NWAVES - 1) / NWAVES), NT, 0, s>>>(part, parts, N, C, weight);
   return hipGetLastError();
 }
@@ -693,8 +941,8 @@ hipError_t emission_grads_as(const Mat &x, const Mat &w, const float *weight, co
   T *ds = b.take<T>(Np * Cp);
   uint32_t *mx = b.take<uint32_t>(1);
   float *scale = b.take<float>(1);
-  SplitProduct<T, RowTile, ColTile> px{};
-  SplitProduct<T, ColTile, ColTile> pw{};
+  SplitProduct<T, ROWS_COLS> px{};
+  SplitProduct<T, COLS_COLS> pw{};
   if (gx) px.plan(N, H, Cp, b);
   if (gw) pw.plan(C, H, Np, b);
   if (!b.base) return hipSuccess;
@@ -740,7 +988,7 @@ hipError_t loss_as(const Mat &x, const Mat &w, const int32_t *target, float *los
   g.parts = parts;
   g.target = target;
   g.hit = hit;
-  TRY((product<T, RowTile, RowTile, EPI_PART>(g, tile, s)));
+  TRY((product<T, ROWS_ROWS, EPI_PART>(g, tile, s)));
   k_loss<<<(unsigned)((N + NWAVES - 1) / NWAVES), NT, 0, s>>>(part, parts, N, target, V, hit, loss,
                                                             lse);
   return hipGetLastError();
@@ -770,8 +1018,8 @@ hipError_t loss_grads_as(const Mat &x, const Mat &w, const int32_t *target, cons
   T *ds = b.take<T>(Np * Pp);
   uint32_t *mx = b.take<uint32_t>(1);
   float *scale = b.take<float>(1);
-  SplitProduct<T, RowTile, ColTile> px{};
-  SplitProduct<T, ColTile, ColTile> pw{};
+  SplitProduct<T, ROWS_COLS> px{};
+  SplitProduct<T, COLS_COLS> pw{};
   float *sums = nullptr;
   if (gx && whole) px.plan(N, H, Pp, b);
   if (gx && !whole) sums = b.take<float>(N * H);
@@ -821,7 +1069,7 @@ hipError_t loss_grads_as(const Mat &x, const Mat &w, const int32_t *target, cons
     g.scale = scale;
     g.Mp = Np;
     g.Np = np;
-    TRY((product<T, RowTile, RowTile, EPI_DS>(g, tile_for(N, n), s)));
+    TRY((product<T, ROWS_ROWS, EPI_DS>(g, tile_for(N, n), s)));
     if (gx && whole) {
       TRY(px.run({ds, np, N, N}, wc, N, H, n, scale, *gx, s));
     } else if (gx) {
@@ -836,7 +1084,7 @@ hipError_t loss_grads_as(const Mat &x, const Mat &w, const int32_t *target, cons
       q.out = sums;
       q.ldo = H;
       q.add = v0 > 0;
-      TRY((product<T, RowTile, ColTile, EPI_SUM>(q, tile_for(N, H), s)));
+      TRY((product<T, ROWS_COLS, EPI_SUM>(q, tile_for(N, H), s)));
     }
     if (gw) {
       Mat out = *gw;
