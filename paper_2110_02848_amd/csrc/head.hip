@@ -73,7 +73,7 @@ __device__ __forceinline__ float4v mac(const Frag<float> &a, const Frag<float> &
 __device__ __forceinline__ void load_lds(uint32_t lds, uint32_t offset, const char *base) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
                :
-               : "s"(lds), "v"(offset), "s"(base)
+               : "s"(__builtin_amdgcn_readfirstlane(lds)), "v"(offset), "s"(base)
                : "memory");
 }
 template <int N>
@@ -122,11 +122,11 @@ struct RowTile {
     return static_cast<const char *>(o.p) + r0 * o.ld * (long long)sizeof(T);
   }
   // the part of step `t`, to `lds`
-  __device__ __forceinline__ void fetch(uint32_t lds, const char *base, const Operand &,
-                                        long long t, int wave, int) const {
+  __device__ __forceinline__ void fetch(uint32_t lds, const char *base, const Operand &, int t,
+                                        int wave, int) const {
+    const char *p = base + (long long)t * KBYTES;
 #pragma unroll
-    for (int i = 0; i < LOADS; ++i)
-      load_lds(lds + (wave * LOADS + i) * 1024, off[i], base + t * KBYTES);
+    for (int i = 0; i < LOADS; ++i) load_lds(lds + (wave * LOADS + i) * 1024, off[i], p);
   }
   // the fragment of rows `row` on, for half of the step
   static __device__ __forceinline__ Frag<T> frag(const char *lds, int row, int half, int lane) {
@@ -175,18 +175,20 @@ struct ColTile {
   static __device__ __forceinline__ const char *base(const Operand &o, long long r0) {
     return static_cast<const char *>(o.p) + r0 * (long long)sizeof(T);
   }
-  __device__ __forceinline__ void fetch(uint32_t lds, const char *base, const Operand &o,
-                                        long long t, int wave, int lane) const {
-    const long long left = o.depth - t * K;  // of this step's k
-    const char *p = base + t * K * o.ld * (long long)sizeof(T);
+  __device__ __forceinline__ void fetch(uint32_t lds, const char *base, const Operand &o, int t,
+                                        int wave, int lane) const {
+    const uint32_t ldb = (uint32_t)(o.ld * sizeof(T));
+    const char *p = base + (long long)t * ((long long)ldb * K);
+    if (t < (int)(o.depth / K)) {
 #pragma unroll
-    for (int i = 0; i < LOADS; ++i) {
-      uint32_t at = off[i];
-      if (left < K) {
-        const int k = k_of(i, wave, lane), last = (int)left - 1;
-        if (k > last) at -= (uint32_t)(k - last) * (uint32_t)(o.ld * sizeof(T));
+      for (int i = 0; i < LOADS; ++i) load_lds(lds + (wave * LOADS + i) * 1024, off[i], p);
+    } else {
+      const int last = (int)(o.depth % K) - 1;  // (a step has one k at least)
+#pragma unroll
+      for (int i = 0; i < LOADS; ++i) {
+        const int k = k_of(i, wave, lane);
+        load_lds(lds + (wave * LOADS + i) * 1024, off[i] - (k > last ? (k - last) * ldb : 0), p);
       }
-      load_lds(lds + (wave * LOADS + i) * 1024, at, p);
     }
   }
   // Fragment of 16 rows: lane l wants k = half * 32 + (l >> 4) * 8 .. + 8 of
@@ -227,8 +229,7 @@ struct Product {
   Operand A, B;
   long long M, N, K;
   int tiles_m, tiles_n;
-  int splits;            // parts of the sum (grid z), `steps` K-steps each
-  long long steps;
+  int splits, steps;     // parts of the sum (grid z), `steps` K-steps each
   // epilogues
   long long n0, words;   // what column 0 stands for (a piece's first word), all words
   void *out;             // scores, dS, sums or results
@@ -319,9 +320,9 @@ __global__ __launch_bounds__(WM *WN *WAVE) void k_product(Product g) {
   tb.init(g.B, n0, 0, wave, lane);
   const char *pa = A::base(g.A, m0), *pb = B::base(g.B, n0);
   const uint32_t lds = lds_address(s_lds[0]);
-  const long long all = (g.K + k_step<T>() - 1) / k_step<T>();
-  const long long first = split * g.steps;
-  const long long end = first + g.steps < all ? first + g.steps : all;
+  const int all = (int)((g.K + k_step<T>() - 1) / k_step<T>());
+  const int first = split * g.steps;
+  const int end = all - first < g.steps ? all : first + g.steps;
 
   float4v acc[FM][FN];
 #pragma unroll
@@ -334,7 +335,7 @@ __global__ __launch_bounds__(WM *WN *WAVE) void k_product(Product g) {
     tb.fetch(lds + A::BYTES, pb, g.B, first, wave, lane);
   }
   uint32_t cur = 0;
-  for (long long t = first; t < end; ++t, cur ^= 1) {
+  for (int t = first; t < end; ++t, cur ^= 1) {
     // step t has landed, and no one reads the other buffer
     wait_loads<0>();
     __syncthreads();
@@ -369,20 +370,19 @@ __device__ __forceinline__ void meet() {
 // Tiles of 256 x 256, eight wavefronts as 2 x 4 of 128 x 64 results each.  A
 // step (64 of the sum, 32 in float32) has four phases, the quarters of a
 // wavefront's results: (A0, B0), (A0, B1), (A1, B1), (A1, B0), where A0, A1, B0,
-// B1 are the halves of its rows and columns, 24 fragments read a step.  A phase
-// is a time for reading and one for multiplying, with a barrier after each,
-// and the wavefronts of the lower half are one time behind: on every SIMD one
-// wavefront multiplies while the other reads, so the matrix cores always have
-// one to feed them.
+// B1 are the halves of its rows and columns.  A phase is a time for reading and
+// one for multiplying, with a barrier after each, and the wavefronts of the
+// lower half are one time behind: on every SIMD one wavefront multiplies while
+// the other reads, so the matrix cores always have one to feed them.  Phases
+// 0 .. 3 read A0, B1, A1 and the next step's B0 (8, 4, 8, 4 fragments), the last
+// into the registers that B1 has left.
 //
 // Each half is a part of LDS of its own (16 KiB, two buffers), loaded by all
-// wavefronts (two loads each) as soon as no one reads it any more: A0 and B0
-// are last read in a step's phase 0, B1 in phase 1, A1 in phase 2, by the lower
-// half one time later, done with another time later; so in phases 0 .. 3 of step t
-// go out the loads of B1 and A1 of step t + 1 and A0 and B0 of step t + 2.
-// What a phase reads has landed for all once each wavefront has waited for its
-// own loads and met the others: in phase 3 for the next A0 and B0, in phase 0
-// for B1, in phase 1 for A1, each time for all but the last eight loads.
+// wavefronts (two loads each) once no one reads it any more, which is two phases
+// after the one that reads it: in phases 0 .. 3 of step t go out the loads of
+// A1 of step t + 1 and of B0, A0 and B1 of step t + 2.  What the next phase reads
+// has landed for all when each wavefront has waited for its own loads of it,
+// all but the last ten, and met the others: six phases for a load to arrive.
 template <typename T, int LAYOUT>
 struct Large {
   static constexpr int NWV = 8;
@@ -394,22 +394,24 @@ struct Large {
   A ta[2];
   B tb[2];
   const char *pa, *pb;
-  const char *lds;
+  const char *lds;  // A: buffer 0 (A0, A1), buffer 1; then B
   uint32_t at;
   int lane, wave, wm, wn;
   Frag<T> fa[4][2], fb[2][2][2];  // [fragment][half of the step]; fb: [half of the columns]
 
-  // buffer: A0, A1, B0, B1
-  static __device__ __forceinline__ int part(int buffer, int which) {
-    return (buffer * 4 + which) * PART;
+  static __device__ __forceinline__ int part_a(int buffer, int half) {
+    return (buffer * 2 + half) * PART;
+  }
+  static __device__ __forceinline__ int part_b(int buffer, int half) {
+    return (4 + buffer * 2 + half) * PART;
   }
   template <int H>
-  __device__ __forceinline__ void load_a(const Product &g, long long t, int buffer) {
-    ta[H].fetch(at + part(buffer, H), pa, g.A, t, wave, lane);
+  __device__ __forceinline__ void load_a(const Product &g, int t, int buffer) {
+    ta[H].fetch(at + part_a(buffer, H), pa, g.A, t, wave, lane);
   }
   template <int H>
-  __device__ __forceinline__ void load_b(const Product &g, long long t, int buffer) {
-    tb[H].fetch(at + part(buffer, 2 + H), pb, g.B, t, wave, lane);
+  __device__ __forceinline__ void load_b(const Product &g, int t, int buffer) {
+    tb[H].fetch(at + part_b(buffer, H), pb, g.B, t, wave, lane);
   }
   template <int H>
   __device__ __forceinline__ void read_a(int buffer) {
@@ -417,15 +419,16 @@ struct Large {
     for (int i = 0; i < 4; ++i)
 #pragma unroll
       for (int k = 0; k < 2; ++k)
-        fa[i][k] = A::frag(lds + part(buffer, H), wm * 64 + i * 16, k, lane);
+        fa[i][k] = A::frag(lds + part_a(buffer, H), wm * 64 + i * 16, k, lane);
   }
-  template <int H>
+  // columns' half H, to the registers of half TO
+  template <int H, int TO>
   __device__ __forceinline__ void read_b(int buffer) {
 #pragma unroll
     for (int j = 0; j < 2; ++j)
 #pragma unroll
       for (int k = 0; k < 2; ++k)
-        fb[H][j][k] = B::frag(lds + part(buffer, 2 + H), wn * 32 + j * 16, k, lane);
+        fb[TO][j][k] = B::frag(lds + part_b(buffer, H), wn * 32 + j * 16, k, lane);
   }
   template <int HA, int HB>
   __device__ __forceinline__ void multiply(float4v (&acc)[8][4]) {
@@ -440,33 +443,69 @@ struct Large {
     __builtin_amdgcn_s_setprio(0);
   }
 
-  // Step t of buffer `b`; LEFT: steps after it (2: two at least).
+  // Step t, in buffer b; LEFT: steps after it (2: two at least).
   template <int LEFT>
-  __device__ __forceinline__ void step(const Product &g, long long t, int b,
-                                       float4v (&acc)[8][4]) {
+  __device__ __forceinline__ void step(const Product &g, int t, int b, float4v (&acc)[8][4]) {
     read_a<0>(b);
-    read_b<0>(b);
-    if constexpr (LEFT > 0) load_b<1>(g, t + 1, b ^ 1);
-    wait_loads<(LEFT > 0) ? 8 : 2>();
+    if constexpr (LEFT > 0) load_a<1>(g, t + 1, b ^ 1);
+    wait_loads<(LEFT > 0) ? 10 : 2>();
     meet();
     multiply<0, 0>(acc);
     meet();
-    read_b<1>(b);
-    if constexpr (LEFT > 0) load_a<1>(g, t + 1, b ^ 1);
-    wait_loads<(LEFT > 0) ? 8 : 0>();
+    read_b<1, 1>(b);
+    if constexpr (LEFT > 1) load_b<0>(g, t + 2, b);
+    wait_loads<(LEFT > 1) ? 10 : (LEFT > 0) ? 8 : 0>();
     meet();
     multiply<0, 1>(acc);
     meet();
     read_a<1>(b);
     if constexpr (LEFT > 1) load_a<0>(g, t + 2, b);
+    if constexpr (LEFT > 0) wait_loads<(LEFT > 1) ? 10 : 6>();
     meet();
     multiply<1, 1>(acc);
     meet();
-    if constexpr (LEFT > 1) load_b<0>(g, t + 2, b);
-    if constexpr (LEFT > 0) wait_loads<(LEFT > 1) ? 8 : 4>();
+    if constexpr (LEFT > 0) read_b<0, 1>(b ^ 1);
+    if constexpr (LEFT > 1) load_b<1>(g, t + 2, b);
+    if constexpr (LEFT > 0) wait_loads<(LEFT > 1) ? 10 : 4>();
     meet();
     multiply<1, 0>(acc);
     meet();
+    if constexpr (LEFT > 0) {  // the next step's B0 to its place
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int k = 0; k < 2; ++k) fb[0][j][k] = fb[1][j][k];
+    }
+  }
+
+  // Steps first .. end - 1 (one at least).
+  __device__ __forceinline__ void run(const Product &g, int first, int end,
+                                      float4v (&acc)[8][4]) {
+    const bool two = first + 1 < end;
+    load_b<0>(g, first, 0);
+    load_a<0>(g, first, 0);
+    load_b<1>(g, first, 0);
+    load_a<1>(g, first, 0);
+    if (two) {
+      load_b<0>(g, first + 1, 1);
+      load_a<0>(g, first + 1, 1);
+      load_b<1>(g, first + 1, 1);
+      wait_loads<10>();
+    } else {
+      wait_loads<4>();
+    }
+    meet();
+    read_b<0, 0>(0);
+    if (wm == 1) meet();
+    int b = 0, t = first;
+    for (; t + 2 < end; ++t, b ^= 1) step<2>(g, t, b, acc);
+    if (two) {
+      step<1>(g, t, b, acc);
+      ++t;
+      b ^= 1;
+    }
+    step<0>(g, t, b, acc);
+    if (wm == 0) meet();
   }
 };
 
@@ -492,42 +531,16 @@ __global__ __launch_bounds__(512) void k_product_large(Product g) {
   }
   l.pa = L::A::base(g.A, m0);
   l.pb = L::B::base(g.B, n0);
-  const long long all = (g.K + k_step<T>() - 1) / k_step<T>();
-  const long long first = split * g.steps;
-  const long long end = first + g.steps < all ? first + g.steps : all;
+  const int all = (int)((g.K + k_step<T>() - 1) / k_step<T>());
+  const int first = split * g.steps;
+  const int end = all - first < g.steps ? all : first + g.steps;
 
   float4v acc[8][4];
 #pragma unroll
   for (int i = 0; i < 8; ++i)
 #pragma unroll
     for (int j = 0; j < 4; ++j) acc[i][j] = float4v{0, 0, 0, 0};
-
-  if (first < end) {
-    const bool two = first + 1 < end;
-    l.template load_a<0>(g, first, 0);
-    l.template load_b<0>(g, first, 0);
-    l.template load_b<1>(g, first, 0);
-    l.template load_a<1>(g, first, 0);
-    if (two) {
-      l.template load_a<0>(g, first + 1, 1);
-      l.template load_b<0>(g, first + 1, 1);
-      wait_loads<8>();
-    } else {
-      wait_loads<4>();
-    }
-    meet();
-    if (l.wm == 1) meet();
-    int b = 0;
-    long long t = first;
-    for (; t + 2 < end; ++t, b ^= 1) l.template step<2>(g, t, b, acc);
-    if (two) {
-      l.template step<1>(g, t, b, acc);
-      ++t;
-      b ^= 1;
-    }
-    l.template step<0>(g, t, b, acc);
-    if (l.wm == 0) meet();
-  }
+  if (first < end) l.run(g, first, end, acc);
   epilogue<T, 4, 8, 4, EPI>(g, acc, m0, n0, tn, l.wm, l.wn, split, l.lane);
 }
 
@@ -882,7 +895,7 @@ struct SplitProduct {
     g.N = N;
     g.K = K;
     g.splits = splits;
-    g.steps = steps;
+    g.steps = (int)steps;
     if (splits == 1) {
       g.out = out.data;
       g.ldo = out.stride;
@@ -915,7 +928,7 @@ hipError_t emission_as(const Mat &x, const Mat &w, float *weight, Bump &b, hipSt
   g.N = C;
   g.K = lx.cols;
   g.splits = 1;
-  g.steps = INT64_MAX / 2;
+  g.steps = INT32_MAX;
   g.out = weight;
   g.ldo = C;
   g.part = part;
@@ -983,7 +996,7 @@ hipError_t loss_as(const Mat &x, const Mat &w, const int32_t *target, float *los
   g.N = V;
   g.K = lx.cols;
   g.splits = 1;
-  g.steps = INT64_MAX / 2;
+  g.steps = INT32_MAX;
   g.part = part;
   g.parts = parts;
   g.target = target;
@@ -996,6 +1009,18 @@ hipError_t loss_as(const Mat &x, const Mat &w, const int32_t *target, float *los
 
 // Bytes of dS that a piece of the vocabulary may take.
 constexpr long long PIECE_BYTES = 512ll << 20;
+
+// Words of a piece of the vocabulary, `most` at most (or 256): all of them, or
+// rows of dw's tiles that fill the CUs a whole number of times (16,000 rows, 32,000
+// words, width 1024: pieces of 16,640 words leave dw 260 tiles, 0.90 ms; 16,384
+// leave 256, 0.50 ms).
+long long piece_of(long long V, long long H, long long most) {
+  if (most >= V) return V;
+  const long long across = (H + 255) / 256;
+  const long long fill = across < CUS ? CUS / across * 256 : 256;
+  const long long unit = most >= fill ? fill : 256;
+  return most < unit ? unit : most / unit * unit;
+}
 
 template <typename T>
 hipError_t loss_grads_as(const Mat &x, const Mat &w, const int32_t *target, const float *lse,
@@ -1010,10 +1035,8 @@ hipError_t loss_grads_as(const Mat &x, const Mat &w, const int32_t *target, cons
     return hipGetLastError();
   }
   const Laid<T> lx = lay<T>(x, b), lw = lay<T>(w, b);
-  long long piece = PIECE_BYTES / (Np * (long long)sizeof(T)) / 256 * 256;
-  piece = piece < 256 ? 256 : piece;
-  const bool whole = piece >= V;
-  if (whole) piece = V;
+  const long long piece = piece_of(V, H, PIECE_BYTES / (Np * (long long)sizeof(T)));
+  const bool whole = piece == V;
   const long long Pp = up(piece, 64);
   T *ds = b.take<T>(Np * Pp);
   uint32_t *mx = b.take<uint32_t>(1);
@@ -1058,7 +1081,7 @@ hipError_t loss_grads_as(const Mat &x, const Mat &w, const int32_t *target, cons
     g.N = n;
     g.K = lx.cols;
     g.splits = 1;
-    g.steps = INT64_MAX / 2;
+    g.steps = INT32_MAX;
     g.n0 = v0;
     g.words = V;
     g.out = ds;
@@ -1080,7 +1103,7 @@ hipError_t loss_grads_as(const Mat &x, const Mat &w, const int32_t *target, cons
       q.N = H;
       q.K = n;
       q.splits = 1;
-      q.steps = INT64_MAX / 2;
+      q.steps = INT32_MAX;
       q.out = sums;
       q.ldo = H;
       q.add = v0 > 0;

@@ -122,6 +122,23 @@ def test_cross_entropy(comp, N, V, H, typ):
     _loss(comp, N, V, H, typ)
 
 
+# large tiles in the scores (one to five steps of the sum), in grad_x and in
+# grad_w (sums over V and over N), with rows and columns past the last tile
+LARGE = [(3500, 3500, h) for h in (24, 100, 192, 256, 320)] + \
+    [(12500, v, 1000) for v in (40, 128, 190, 300)] + [(n, 12500, 1000) for n in (50, 65, 200, 257)]
+
+
+@pytest.mark.parametrize("typ", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("N,V,H", LARGE)
+def test_cross_entropy_large_tiles(comp, N, V, H, typ):
+    _loss(comp, N, V, H, typ)
+
+
+@pytest.mark.parametrize("typ", ["f32", "bf16"])
+def test_emission_large_tiles(comp, typ):
+    _emission(comp, 3500, 3500, 136, typ)
+
+
 @pytest.mark.parametrize("pad", [1, 4, 8])
 @pytest.mark.parametrize("typ", ["f32", "f16", "bf16"])
 def test_cross_entropy_strided(comp, typ, pad):
