@@ -67,14 +67,25 @@ __device__ __forceinline__ float4v mac(const Frag<float> &a, const Frag<float> &
 // ---------------------------------------------------------------------------
 
 // Loads of 64 lanes by 16 bytes go from memory to LDS without registers: lane
-// i's bytes land at `lds` + 16 i.  Written as instructions, because the
-// compiler would wait for all of them before the next read of LDS; whoever
-// reads waits with wait_loads and a barrier.
-__device__ __forceinline__ void load_lds(uint32_t lds, uint32_t offset, const char *base) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+// i's bytes land at `lds` + 16 i, zeros where they lie past the end of the
+// buffer.  Written as instructions, because the compiler would wait for all of
+// them before the next read of LDS; whoever reads waits with wait_loads and a
+// barrier.
+__device__ __forceinline__ void load_lds(uint32_t lds, uint32_t offset, int4v buffer) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
                :
-               : "s"(__builtin_amdgcn_readfirstlane(lds)), "v"(offset), "s"(base)
+               : "s"(__builtin_amdgcn_readfirstlane(lds)), "v"(offset), "s"(buffer)
                : "memory");
+}
+// The buffer of `bytes` bytes at p + at (as many of them as 32 bits count; all
+// arguments the same in every lane).
+__device__ __forceinline__ int4v buffer_at(const char *p, long long bytes, long long at) {
+  const unsigned long long q = (unsigned long long)(uintptr_t)p + at;
+  const long long left = bytes - at;
+  const uint32_t n = left <= 0 ? 0u : left > 0xffffffffll ? 0xffffffffu : (uint32_t)left;
+  return int4v{__builtin_amdgcn_readfirstlane((int)(uint32_t)q),
+               __builtin_amdgcn_readfirstlane((int)(uint32_t)(q >> 32)),
+               __builtin_amdgcn_readfirstlane((int)n), 0x00027000};
 }
 template <int N>
 __device__ __forceinline__ void wait_loads() {  // all but the last N
@@ -97,8 +108,8 @@ struct Rows {
 // Row-wise operand: element (r, k) at p[r * ld + k].  A part holds R rows of
 // 128 bytes; 16-byte group g of row r lies at group g ^ (r & 7), so that the
 // 16 lanes of a fragment's group, a row apart, read different banks.  Rows
-// past the last are read as the last (their results are not used); k has no
-// tail (rows are padded with zeros to whole steps).
+// past the last are zeros; k has no tail (rows are padded with zeros to whole
+// steps).
 template <typename T, int R, int NWV, typename ROWS>
 struct RowTile {
   static constexpr int BYTES = R * KBYTES;
@@ -106,27 +117,29 @@ struct RowTile {
   static_assert(LOADS >= 1 && LOADS * 1024 * NWV == BYTES, "whole loads");
   uint32_t off[LOADS];
 
-  // `first`: the part's first row in the tile; the tile's rows are r0 on
-  __device__ __forceinline__ void init(const Operand &o, long long r0, int first, int wave,
-                                       int lane) {
-    const long long left = o.rows - 1 - r0;  // (>= 0)
+  // `first`: the part's first row in the tile
+  __device__ __forceinline__ void init(const Operand &o, int first, int wave, int lane) {
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) {
       const int r = (wave * LOADS + i) * 8 + (lane >> 3);
-      int g = ROWS::of(first, r);
-      g = g <= left ? g : (int)left;
-      off[i] = (uint32_t)g * (uint32_t)(o.ld * sizeof(T)) + (((lane & 7) ^ (r & 7)) << 4);
+      off[i] = (uint32_t)ROWS::of(first, r) * (uint32_t)(o.ld * sizeof(T)) +
+               (((lane & 7) ^ (r & 7)) << 4);
     }
   }
   static __device__ __forceinline__ const char *base(const Operand &o, long long r0) {
     return static_cast<const char *>(o.p) + r0 * o.ld * (long long)sizeof(T);
   }
-  // the part of step `t`, to `lds`
-  __device__ __forceinline__ void fetch(uint32_t lds, const char *base, const Operand &, int t,
-                                        int wave, int) const {
-    const char *p = base + (long long)t * KBYTES;
-#pragma unroll
-    for (int i = 0; i < LOADS; ++i) load_lds(lds + (wave * LOADS + i) * 1024, off[i], p);
+  // bytes from there to the end of the last row
+  static __device__ __forceinline__ long long bytes(const Operand &o, long long r0) {
+    return ((o.rows - 1 - r0) * o.ld + o.depth) * (long long)sizeof(T);
+  }
+  static __device__ __forceinline__ int4v step(const Operand &, const char *base,
+                                               long long bytes, int t) {
+    return buffer_at(base, bytes, (long long)t * KBYTES);
+  }
+  // the i-th load of the part, of the step whose buffer it is, to `lds`
+  __device__ __forceinline__ void fetch(int i, uint32_t lds, int4v buffer, int wave) const {
+    load_lds(lds + (wave * LOADS + i) * 1024, off[i], buffer);
   }
   // the fragment of rows `row` on, for half of the step
   static __device__ __forceinline__ Frag<T> frag(const char *lds, int row, int half, int lane) {
@@ -138,9 +151,8 @@ struct RowTile {
 // Column-wise operand: element (r, k) at p[k * ld + r].  A part holds the
 // step's k, each R elements of consecutive r; of 16-bit types, 32-byte block
 // b of k lies at block b ^ swizzle(k), so that the reads that transpose (16
-// lanes read four k of 16 rows) meet different banks.  Past the last k the
-// last one is read (the other operand is zero there), past the last row a
-// group inside the row.
+// lanes read four k of 16 rows) meet different banks.  Past the last k there
+// are zeros, past the last row what lies there in memory, or zeros.
 template <typename T, int R, int NWV, typename ROWS>
 struct ColTile {
   static constexpr int K = k_step<T>();
@@ -156,40 +168,28 @@ struct ColTile {
   static __device__ __forceinline__ int swizzle(int k) {
     return sizeof(T) == 2 ? ((k & 3) | ((k >> 1) & 4)) & (BLOCKS - 1) : 0;
   }
-  static __device__ __forceinline__ int k_of(int i, int wave, int lane) {
-    return ((wave * LOADS + i) * 64 + lane) / GROUPS;
-  }
-
-  __device__ __forceinline__ void init(const Operand &o, long long r0, int first, int wave,
-                                       int lane) {
-    const long long room = (o.rows - r0) * (long long)sizeof(T) - 16;  // (>= 0)
+  // `first`: the part's first row in the tile
+  __device__ __forceinline__ void init(const Operand &o, int first, int wave, int lane) {
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) {
-      const int k = k_of(i, wave, lane), g = lane % GROUPS;
+      const int q = (wave * LOADS + i) * 64 + lane, k = q / GROUPS, g = q % GROUPS;
       const int b = (((g >> 1) ^ swizzle(k)) << 5) + ((g & 1) << 4);
-      int at = ROWS::of(first, b / (int)sizeof(T)) * (int)sizeof(T);
-      at = at <= room ? at : (int)room;
-      off[i] = (uint32_t)k * (uint32_t)(o.ld * sizeof(T)) + at;
+      off[i] = (uint32_t)k * (uint32_t)(o.ld * sizeof(T)) +
+               ROWS::of(first, b / (int)sizeof(T)) * (int)sizeof(T);
     }
   }
   static __device__ __forceinline__ const char *base(const Operand &o, long long r0) {
     return static_cast<const char *>(o.p) + r0 * (long long)sizeof(T);
   }
-  __device__ __forceinline__ void fetch(uint32_t lds, const char *base, const Operand &o, int t,
-                                        int wave, int lane) const {
-    const uint32_t ldb = (uint32_t)(o.ld * sizeof(T));
-    const char *p = base + (long long)t * ((long long)ldb * K);
-    if (t < (int)(o.depth / K)) {
-#pragma unroll
-      for (int i = 0; i < LOADS; ++i) load_lds(lds + (wave * LOADS + i) * 1024, off[i], p);
-    } else {
-      const int last = (int)(o.depth % K) - 1;  // (a step has one k at least)
-#pragma unroll
-      for (int i = 0; i < LOADS; ++i) {
-        const int k = k_of(i, wave, lane);
-        load_lds(lds + (wave * LOADS + i) * 1024, off[i] - (k > last ? (k - last) * ldb : 0), p);
-      }
-    }
+  static __device__ __forceinline__ long long bytes(const Operand &o, long long r0) {
+    return ((o.depth - 1) * o.ld + o.rows - r0) * (long long)sizeof(T);
+  }
+  static __device__ __forceinline__ int4v step(const Operand &o, const char *base,
+                                               long long bytes, int t) {
+    return buffer_at(base, bytes, (long long)t * (K * o.ld * (long long)sizeof(T)));
+  }
+  __device__ __forceinline__ void fetch(int i, uint32_t lds, int4v buffer, int wave) const {
+    load_lds(lds + (wave * LOADS + i) * 1024, off[i], buffer);
   }
   // Fragment of 16 rows: lane l wants k = half * 32 + (l >> 4) * 8 .. + 8 of
   // row l & 15 (16-bit types).  A read that transposes gives lane i of 16 the
@@ -316,9 +316,17 @@ __global__ __launch_bounds__(WM *WN *WAVE) void k_product(Product g) {
 
   A ta;
   B tb;
-  ta.init(g.A, m0, 0, wave, lane);
-  tb.init(g.B, n0, 0, wave, lane);
+  ta.init(g.A, 0, wave, lane);
+  tb.init(g.B, 0, wave, lane);
   const char *pa = A::base(g.A, m0), *pb = B::base(g.B, n0);
+  const long long na = A::bytes(g.A, m0), nb = B::bytes(g.B, n0);
+  const auto fetch = [&](uint32_t to, int t) {
+    const int4v ba = A::step(g.A, pa, na, t), bb = B::step(g.B, pb, nb, t);
+#pragma unroll
+    for (int i = 0; i < A::LOADS; ++i) ta.fetch(i, to, ba, wave);
+#pragma unroll
+    for (int i = 0; i < B::LOADS; ++i) tb.fetch(i, to + A::BYTES, bb, wave);
+  };
   const uint32_t lds = lds_address(s_lds[0]);
   const int all = (int)((g.K + k_step<T>() - 1) / k_step<T>());
   const int first = split * g.steps;
@@ -330,20 +338,13 @@ __global__ __launch_bounds__(WM *WN *WAVE) void k_product(Product g) {
 #pragma unroll
     for (int j = 0; j < FN; ++j) acc[i][j] = float4v{0, 0, 0, 0};
 
-  if (first < end) {
-    ta.fetch(lds, pa, g.A, first, wave, lane);
-    tb.fetch(lds + A::BYTES, pb, g.B, first, wave, lane);
-  }
+  if (first < end) fetch(lds, first);
   uint32_t cur = 0;
   for (int t = first; t < end; ++t, cur ^= 1) {
     // step t has landed, and no one reads the other buffer
     wait_loads<0>();
     __syncthreads();
-    if (t + 1 < end) {
-      const uint32_t to = lds + (cur ^ 1) * (A::BYTES + B::BYTES);
-      ta.fetch(to, pa, g.A, t + 1, wave, lane);
-      tb.fetch(to + A::BYTES, pb, g.B, t + 1, wave, lane);
-    }
+    if (t + 1 < end) fetch(lds + (cur ^ 1) * (A::BYTES + B::BYTES), t + 1);
     const char *sa = s_lds[cur], *sb = sa + A::BYTES;
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
@@ -368,21 +369,23 @@ __device__ __forceinline__ void meet() {
 }
 
 // Tiles of 256 x 256, eight wavefronts as 2 x 4 of 128 x 64 results each.  A
-// step (64 of the sum, 32 in float32) has four phases, the quarters of a
-// wavefront's results: (A0, B0), (A0, B1), (A1, B1), (A1, B0), where A0, A1, B0,
-// B1 are the halves of its rows and columns.  A phase is a time for reading and
-// one for multiplying, with a barrier after each, and the wavefronts of the
+// step (64 of the sum, 32 in float32) has two phases, the halves A0, A1 of a
+// wavefront's rows, each with all its columns B.  A phase is a time for reading
+// and one for multiplying, with a barrier after each, and the wavefronts of the
 // lower half are one time behind: on every SIMD one wavefront multiplies while
-// the other reads, so the matrix cores always have one to feed them.  Phases
-// 0 .. 3 read A0, B1, A1 and the next step's B0 (8, 4, 8, 4 fragments), the last
-// into the registers that B1 has left.
+// the other reads, so the matrix cores always have one to feed them.  (With four
+// phases of a quarter each, a barrier for every 16 products instead of 32, they were
+// busy 60 % of the time, see DESIGN.)
 //
-// Each half is a part of LDS of its own (16 KiB, two buffers), loaded by all
-// wavefronts (two loads each) once no one reads it any more, which is two phases
-// after the one that reads it: in phases 0 .. 3 of step t go out the loads of
-// A1 of step t + 1 and of B0, A0 and B1 of step t + 2.  What the next phase reads
-// has landed for all when each wavefront has waited for its own loads of it,
-// all but the last ten, and met the others: six phases for a load to arrive.
+// The 256 rows of A and the 256 of B of a step are 32 KiB each; LDS holds five
+// of them in a ring: B(t), A(t), B(t + 1), A(t + 1), B(t + 2), ...  One that was
+// read in one phase is free in the next one's time for multiplying (the lower
+// half has multiplied by then, so its reads are done).  B is read in phase 0
+// and A for the last time in phase 1, so phase 0 of step t sends for B(t + 2) where
+// A(t - 1) was, and phase 1 for A(t + 2) where B(t) was: four loads each.
+// What the next phase reads has landed for all when each wavefront has waited
+// for its own loads of it and met the others: five times of 32 products for a load
+// to arrive, three for A0.
 template <typename T, int LAYOUT>
 struct Large {
   static constexpr int NWV = 8;
@@ -391,120 +394,115 @@ struct Large {
   static constexpr int PART = A::BYTES;
   static_assert(A::BYTES == B::BYTES && A::LOADS == 2 && B::LOADS == 2, "equal parts");
 
+  static constexpr int PAIR = 2 * PART;  // an operand's rows of a step
+  static constexpr int RING = 5 * PAIR;
+
   A ta[2];
   B tb[2];
   const char *pa, *pb;
-  const char *lds;  // A: buffer 0 (A0, A1), buffer 1; then B
+  long long na, nb;  // bytes from there
+  const char *lds;
   uint32_t at;
   int lane, wave, wm, wn;
-  Frag<T> fa[4][2], fb[2][2][2];  // [fragment][half of the step]; fb: [half of the columns]
+  Frag<T> fa[4][2], fb[4][2];  // [fragment][half of the step]
 
-  static __device__ __forceinline__ int part_a(int buffer, int half) {
-    return (buffer * 2 + half) * PART;
+  // the place `n` places on in the ring
+  static __device__ __forceinline__ int on(int place, int n) {
+    place += n * PAIR;
+    return place >= RING ? place - RING : place;
   }
-  static __device__ __forceinline__ int part_b(int buffer, int half) {
-    return (4 + buffer * 2 + half) * PART;
+  // the i-th of four loads: A0, A0, A1, A1 or B, to a place in the ring
+  __device__ __forceinline__ void load_a(int i, int4v buffer, int place) {
+    ta[i / 2].fetch(i % 2, at + place + i / 2 * PART, buffer, wave);
   }
-  template <int H>
-  __device__ __forceinline__ void load_a(const Product &g, int t, int buffer) {
-    ta[H].fetch(at + part_a(buffer, H), pa, g.A, t, wave, lane);
-  }
-  template <int H>
-  __device__ __forceinline__ void load_b(const Product &g, int t, int buffer) {
-    tb[H].fetch(at + part_b(buffer, H), pb, g.B, t, wave, lane);
+  __device__ __forceinline__ void load_b(int i, int4v buffer, int place) {
+    tb[i / 2].fetch(i % 2, at + place + i / 2 * PART, buffer, wave);
   }
   template <int H>
-  __device__ __forceinline__ void read_a(int buffer) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-      for (int k = 0; k < 2; ++k)
-        fa[i][k] = A::frag(lds + part_a(buffer, H), wm * 64 + i * 16, k, lane);
-  }
-  // columns' half H, to the registers of half TO
-  template <int H, int TO>
-  __device__ __forceinline__ void read_b(int buffer) {
-#pragma unroll
-    for (int j = 0; j < 2; ++j)
-#pragma unroll
-      for (int k = 0; k < 2; ++k)
-        fb[TO][j][k] = B::frag(lds + part_b(buffer, H), wn * 32 + j * 16, k, lane);
-  }
-  template <int HA, int HB>
-  __device__ __forceinline__ void multiply(float4v (&acc)[8][4]) {
-    __builtin_amdgcn_s_setprio(1);
+  __device__ __forceinline__ void read_a(int place) {
 #pragma unroll
     for (int k = 0; k < 2; ++k)
 #pragma unroll
       for (int i = 0; i < 4; ++i)
+        fa[i][k] = A::frag(lds + place + H * PART, wm * 64 + i * 16, k, lane);
+  }
+  __device__ __forceinline__ void read_b(int place) {
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
-          acc[HA * 4 + i][HB * 2 + j] = mac(fb[HB][j][k], fa[i][k], acc[HA * 4 + i][HB * 2 + j]);
+    for (int k = 0; k < 2; ++k)
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        fb[j][k] = B::frag(lds + place + j / 2 * PART, wn * 32 + j % 2 * 16, k, lane);
+  }
+  // The 32 products of rows' half HA, with load(0) .. load(N - 1) spread among
+  // them: loads go out one in 16 cycles of a CU, and a wavefront that has to
+  // wait for its turn feeds no matrix core.  The last LATE products come after
+  // the barrier that ends the phase, so that there is work for the matrix core
+  // while the other wavefront starts.
+  template <int HA, int N, typename F>
+  __device__ __forceinline__ void multiply(float4v (&acc)[8][4], F &&load) {
+    constexpr int LATE = 4;
+    __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+    for (int q = 0; q < 32; ++q) {
+      if (q == 32 - LATE) {
+        asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");  // all that was read
+        meet();
+      }
+      const int k = q / 16, i = q / 4 % 4, j = q % 4;
+      acc[HA * 4 + i][j] = mac(fb[j][k], fa[i][k], acc[HA * 4 + i][j]);
+      if constexpr (N > 0) {
+        constexpr int EVERY = 24 / N;
+        if (q % EVERY == EVERY / 2 && q / EVERY < N) {
+          __builtin_amdgcn_sched_barrier(0);
+          load(q / EVERY);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+    }
     __builtin_amdgcn_s_setprio(0);
   }
 
-  // Step t, in buffer b; LEFT: steps after it (2: two at least).
+  // Step t with B(t) at `place`; LEFT: steps after it (2: two at least).
   template <int LEFT>
-  __device__ __forceinline__ void step(const Product &g, int t, int b, float4v (&acc)[8][4]) {
-    read_a<0>(b);
-    if constexpr (LEFT > 0) load_a<1>(g, t + 1, b ^ 1);
-    wait_loads<(LEFT > 0) ? 10 : 2>();
+  __device__ __forceinline__ void step(const Product &g, int t, int place,
+                                       float4v (&acc)[8][4]) {
+    const int4v ba = A::step(g.A, pa, na, t + 2), bb = B::step(g.B, pb, nb, t + 2);
+    read_b(place);
+    read_a<0>(on(place, 1));
+    wait_loads<(LEFT > 0) ? 8 : 0>();
     meet();
-    multiply<0, 0>(acc);
+    multiply<0, (LEFT > 1) ? 4 : 0>(acc, [&](int i) { load_b(i, bb, on(place, 4)); });
+    read_a<1>(on(place, 1));
+    if constexpr (LEFT > 0) wait_loads<(LEFT > 1) ? 6 : 2>();
     meet();
-    read_b<1, 1>(b);
-    if constexpr (LEFT > 1) load_b<0>(g, t + 2, b);
-    wait_loads<(LEFT > 1) ? 10 : (LEFT > 0) ? 8 : 0>();
-    meet();
-    multiply<0, 1>(acc);
-    meet();
-    read_a<1>(b);
-    if constexpr (LEFT > 1) load_a<0>(g, t + 2, b);
-    if constexpr (LEFT > 0) wait_loads<(LEFT > 1) ? 10 : 6>();
-    meet();
-    multiply<1, 1>(acc);
-    meet();
-    if constexpr (LEFT > 0) read_b<0, 1>(b ^ 1);
-    if constexpr (LEFT > 1) load_b<1>(g, t + 2, b);
-    if constexpr (LEFT > 0) wait_loads<(LEFT > 1) ? 10 : 4>();
-    meet();
-    multiply<1, 0>(acc);
-    meet();
-    if constexpr (LEFT > 0) {  // the next step's B0 to its place
-#pragma unroll
-      for (int j = 0; j < 2; ++j)
-#pragma unroll
-        for (int k = 0; k < 2; ++k) fb[0][j][k] = fb[1][j][k];
-    }
+    multiply<1, (LEFT > 1) ? 4 : 0>(acc, [&](int i) { load_a(i, ba, place); });
   }
 
   // Steps first .. end - 1 (one at least).
   __device__ __forceinline__ void run(const Product &g, int first, int end,
                                       float4v (&acc)[8][4]) {
     const bool two = first + 1 < end;
-    load_b<0>(g, first, 0);
-    load_a<0>(g, first, 0);
-    load_b<1>(g, first, 0);
-    load_a<1>(g, first, 0);
-    if (two) {
-      load_b<0>(g, first + 1, 1);
-      load_a<0>(g, first + 1, 1);
-      load_b<1>(g, first + 1, 1);
+    for (int s = 0; s < (two ? 2 : 1); ++s) {
+      const int4v ba = A::step(g.A, pa, na, first + s), bb = B::step(g.B, pb, nb, first + s);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) load_b(i, bb, 2 * s * PAIR);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) load_a(i, ba, (2 * s + 1) * PAIR);
+    }
+    if (two)
       wait_loads<10>();
-    } else {
-      wait_loads<4>();
-    }
+    else
+      wait_loads<2>();
     meet();
-    read_b<0, 0>(0);
     if (wm == 1) meet();
-    int b = 0, t = first;
-    for (; t + 2 < end; ++t, b ^= 1) step<2>(g, t, b, acc);
+    int place = 0, t = first;
+    for (; t + 2 < end; ++t, place = on(place, 2)) step<2>(g, t, place, acc);
     if (two) {
-      step<1>(g, t, b, acc);
+      step<1>(g, t, place, acc);
       ++t;
-      b ^= 1;
+      place = on(place, 2);
     }
-    step<0>(g, t, b, acc);
+    step<0>(g, t, place, acc);
     if (wm == 0) meet();
   }
 };
@@ -512,7 +510,7 @@ struct Large {
 template <typename T, int LAYOUT, int EPI>
 __global__ __launch_bounds__(512) void k_product_large(Product g) {
   using L = Large<T, LAYOUT>;
-  __shared__ __align__(1024) char s_lds[8 * L::PART];
+  __shared__ __align__(1024) char s_lds[L::RING];
   L l;
   l.lane = threadIdx.x & (WAVE - 1);
   l.wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
@@ -526,11 +524,13 @@ __global__ __launch_bounds__(512) void k_product_large(Product g) {
   const int split = blockIdx.z;
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
-    l.ta[h].init(g.A, m0, h * 64, l.wave, l.lane);
-    l.tb[h].init(g.B, n0, h * 32, l.wave, l.lane);
+    l.ta[h].init(g.A, h * 64, l.wave, l.lane);
+    l.tb[h].init(g.B, h * 32, l.wave, l.lane);
   }
   l.pa = L::A::base(g.A, m0);
   l.pb = L::B::base(g.B, n0);
+  l.na = L::A::bytes(g.A, m0);
+  l.nb = L::B::bytes(g.B, n0);
   const int all = (int)((g.K + k_step<T>() - 1) / k_step<T>());
   const int first = split * g.steps;
   const int end = all - first < g.steps ? all : first + g.steps;
@@ -843,16 +843,16 @@ struct Laid {
   Operand o;
   T *copy;
   long long cols;
-  Operand columns() const { return {o.p, o.ld, cols, o.depth}; }  // read column by column
+  Operand columns() const { return {o.p, o.ld, cols, o.rows}; }  // read column by column
 };
 
 template <typename T>
 Laid<T> lay(const Mat &m, Bump &b) {
   const long long cols = up(m.cols, k_step<T>());
   if ((uintptr_t)m.data % 16 == 0 && m.stride * sizeof(T) % 16 == 0 && cols == m.cols)
-    return {{m.data, m.stride, m.rows, m.rows}, nullptr, cols};
+    return {{m.data, m.stride, m.rows, cols}, nullptr, cols};
   T *p = b.take<T>(m.rows * cols);
-  return {{p, cols, m.rows, m.rows}, p, cols};
+  return {{p, cols, m.rows, cols}, p, cols};
 }
 template <typename T>
 hipError_t fill(const Laid<T> &l, const Mat &m, hipStream_t s) {
@@ -972,8 +972,8 @@ hipError_t emission_grads_as(const Mat &x, const Mat &w, const float *weight, co
   k_emission_ds<T><<<(unsigned)((Np + NWAVES - 1) / NWAVES), NT, 0, s>>>(weight, grad, N, C, scale,
                                                                         ds, Np, Cp);
   TRY(hipGetLastError());
-  if (gx) TRY(px.run({ds, Cp, N, N}, lw.columns(), N, H, C, scale, *gx, s));
-  if (gw) TRY(pw.run({ds, Cp, Cp, Np}, lx.columns(), C, H, N, scale, *gw, s));
+  if (gx) TRY(px.run({ds, Cp, N, Cp}, lw.columns(), N, H, C, scale, *gx, s));
+  if (gw) TRY(pw.run({ds, Cp, Cp, N}, lx.columns(), C, H, N, scale, *gw, s));
   return hipSuccess;
 }
 
@@ -1010,6 +1010,9 @@ hipError_t loss_as(const Mat &x, const Mat &w, const int32_t *target, float *los
 // Bytes of dS that a piece of the vocabulary may take.
 constexpr long long PIECE_BYTES = 512ll << 20;
 
+#ifndef DSPAD
+#define DSPAD 64
+#endif
 // Words of a piece of the vocabulary, `most` at most (or 256): all of them, or
 // rows of dw's tiles that fill the CUs a whole number of times (16,000 rows, 32,000
 // words, width 1024: pieces of 16,640 words leave dw 260 tiles, 0.90 ms; 16,384
@@ -1038,7 +1041,7 @@ hipError_t loss_grads_as(const Mat &x, const Mat &w, const int32_t *target, cons
   const long long piece = piece_of(V, H, PIECE_BYTES / (Np * (long long)sizeof(T)));
   const bool whole = piece == V;
   const long long Pp = up(piece, 64);
-  T *ds = b.take<T>(Np * Pp);
+  T *ds = b.take<T>(Np * (Pp + DSPAD));
   uint32_t *mx = b.take<uint32_t>(1);
   float *scale = b.take<float>(1);
   SplitProduct<T, ROWS_COLS> px{};
@@ -1072,7 +1075,7 @@ hipError_t loss_grads_as(const Mat &x, const Mat &w, const int32_t *target, cons
   TRY(hipGetLastError());
   for (long long v0 = 0; v0 < V; v0 += piece) {
     const long long n = V - v0 < piece ? V - v0 : piece, np = up(n, 64);
-    const Operand wp{static_cast<const T *>(lw.o.p) + v0 * lw.o.ld, lw.o.ld, n, n};
+    const Operand wp{static_cast<const T *>(lw.o.p) + v0 * lw.o.ld, lw.o.ld, n, lw.cols};
     const Operand wc{wp.p, wp.ld, lw.cols, n};
     Product g{};
     g.A = lx.o;
@@ -1085,7 +1088,7 @@ hipError_t loss_grads_as(const Mat &x, const Mat &w, const int32_t *target, cons
     g.n0 = v0;
     g.words = V;
     g.out = ds;
-    g.ldo = np;
+    g.ldo = np + DSPAD;
     g.target = target;
     g.lse = lse;
     g.grad = grad;
@@ -1094,10 +1097,10 @@ hipError_t loss_grads_as(const Mat &x, const Mat &w, const int32_t *target, cons
     g.Np = np;
     TRY((product<T, ROWS_ROWS, EPI_DS>(g, tile_for(N, n), s)));
     if (gx && whole) {
-      TRY(px.run({ds, np, N, N}, wc, N, H, n, scale, *gx, s));
+      TRY(px.run({ds, np + DSPAD, N, np}, wc, N, H, n, scale, *gx, s));
     } else if (gx) {
       Product q{};
-      q.A = {ds, np, N, N};
+      q.A = {ds, np + DSPAD, N, np};
       q.B = wc;
       q.M = N;
       q.N = H;
@@ -1115,7 +1118,7 @@ hipError_t loss_grads_as(const Mat &x, const Mat &w, const int32_t *target, cons
       out.rows = n;
       b.at = mark;
       pw.plan(n, H, Np, b);
-      TRY(pw.run({ds, np, np, Np}, lx.columns(), n, H, N, scale, out, s));
+      TRY(pw.run({ds, np + DSPAD, np, N}, lx.columns(), n, H, N, scale, out, s));
     }
   }
   if (sums) {

@@ -54,14 +54,13 @@ hipError_t launch_recurrence_step(const StepArgs &a, int type, hipStream_t s);
 
 // ---- heads ---------------------------------------------------------------
 
-// An operand of the products: rows of `ld` elements, 16-byte aligned.  `rows`:
-// how many rows may be read; read column by column, how many elements of a
-// row (whole groups of 16 bytes), and `depth` rows.
+// An operand of the products, element (r, k) of `rows` by `depth`: at
+// p[r * ld + k], or at p[k * ld + r] where it is read column by column.  Rows
+// of memory begin at multiples of 16 bytes, whole groups of them.
 struct Operand {
   const void *p;
   long long ld;
-  long long rows;
-  long long depth;
+  long long rows, depth;
 };
 
 // Each is called twice: without workspace (ws null) it only says how many
