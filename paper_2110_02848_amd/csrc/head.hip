@@ -104,6 +104,17 @@ struct Rows {
     return first + r / RUN * EVERY_ + r % RUN;
   }
 };
+// The rows of B so that a lane's results lie side by side: fragments FIRST on,
+// PER of a wavefront's FN, where row i of fragment j is the wavefront's row i / 4 *
+// 4 FN + 4 j + i % 4 (a lane of group i / 4 gets results i % 4 of every j).
+template <int FN, int PER>
+struct Spread {
+  static constexpr int RUN = 4;
+  static __device__ __forceinline__ int of(int first, int r) {
+    const int w = r / (PER * 16), j = first + r / 16 % PER, i = r % 16;
+    return w * FN * 16 + i / 4 * 4 * FN + 4 * j + i % 4;
+  }
+};
 
 // Row-wise operand: element (r, k) at p[r * ld + k].  A part holds R rows of
 // 128 bytes; 16-byte group g of row r lies at group g ^ (r & 7), so that the
@@ -234,15 +245,15 @@ struct Product {
   long long n0, words;   // what column 0 stands for (a piece's first word), all words
   void *out;             // scores, dS, sums or results
   long long ldo;
-  float2 *part;          // [M, parts]: each tile's maximum and sum of a row
-  int parts;
+  float2 *part;          // [parts, M]: maximum and sum of a row's scores in a part of a tile
   const int32_t *target; // [M]
   float *hit;            // [M]: the target's score
   const float *lse;      // [M]
   const float *grad;     // [M] or null (1)
   const float *scale;    // power of two on dS (16-bit floats), or null (1)
-  long long Mp, Np;      // dS: rows and columns to write, zeros past M and N
+  long long Np;          // dS: columns to write, zeros past N
   int add;               // sums: add to what is there
+  int wide;              // results: `out` and its rows are aligned to four
 };
 
 enum Epilogue {
@@ -252,13 +263,6 @@ enum Epilogue {
   EPI_SUM,     // float32 sums, one block of M x N a split
   EPI_RESULT   // results in T, times 1 / scale
 };
-
-template <typename T>
-__device__ __forceinline__ void store4(T *p, float4v v, int valid) {
-#pragma unroll
-  for (int j = 0; j < 4; ++j)
-    if (j < valid) p[j] = (T)v[j];
-}
 
 // Maximum that takes no infinity as a shift (exp(inf - inf) is no number).
 __device__ __forceinline__ float shift_of(float m) { return fabsf(m) == INFINITY ? 0.0f : m; }
@@ -289,11 +293,11 @@ enum Layout { ROWS_ROWS, ROWS_COLS, COLS_COLS };  // of A and B
 template <typename T, int LAYOUT, int R, int NWV, typename ROWS>
 using TileA = std::conditional_t<LAYOUT == COLS_COLS, ColTile<T, R, NWV, ROWS>,
                                  RowTile<T, R, NWV, ROWS>>;
-template <typename T, int LAYOUT, int R, int NWV, typename ROWS>
-using TileB = std::conditional_t<LAYOUT == ROWS_ROWS, RowTile<T, R, NWV, ROWS>,
+template <typename T, int LAYOUT, int R, int NWV, typename SPREAD, typename ROWS>
+using TileB = std::conditional_t<LAYOUT == ROWS_ROWS, RowTile<T, R, NWV, SPREAD>,
                                  ColTile<T, R, NWV, ROWS>>;
 
-template <typename T, int WN, int FM, int FN, int EPI>
+template <typename T, int LAYOUT, int WN, int FM, int FN, int EPI>
 __device__ __forceinline__ void epilogue(const Product &g, float4v (&acc)[FM][FN], long long m0,
                                          long long n0, int tn, int wm, int wn, int split,
                                          int lane);
@@ -304,7 +308,7 @@ template <typename T, int LAYOUT, int BM, int BN, int WM, int WN, int EPI>
 __global__ __launch_bounds__(WM *WN *WAVE) void k_product(Product g) {
   constexpr int NWV = WM * WN, FM = BM / WM / 16, FN = BN / WN / 16;
   using A = TileA<T, LAYOUT, BM, NWV, Rows<BM, BM>>;
-  using B = TileB<T, LAYOUT, BN, NWV, Rows<BN, BN>>;
+  using B = TileB<T, LAYOUT, BN, NWV, Spread<FN, FN>, Rows<BN, BN>>;
   __shared__ __align__(1024) char s_lds[2][A::BYTES + B::BYTES];
   const int lane = threadIdx.x & (WAVE - 1);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
@@ -359,7 +363,7 @@ __global__ __launch_bounds__(WM *WN *WAVE) void k_product(Product g) {
         for (int j = 0; j < FN; ++j) acc[i][j] = mac(fb[j], fa[i], acc[i][j]);
     }
   }
-  epilogue<T, WN, FM, FN, EPI>(g, acc, m0, n0, tn, wm, wn, split, lane);
+  epilogue<T, LAYOUT, WN, FM, FN, EPI>(g, acc, m0, n0, tn, wm, wn, split, lane);
 }
 
 __device__ __forceinline__ void meet() {
@@ -390,7 +394,7 @@ template <typename T, int LAYOUT>
 struct Large {
   static constexpr int NWV = 8;
   using A = TileA<T, LAYOUT, 128, NWV, Rows<64, 128>>;
-  using B = TileB<T, LAYOUT, 128, NWV, Rows<32, 64>>;
+  using B = TileB<T, LAYOUT, 128, NWV, Spread<4, 2>, Rows<32, 64>>;
   static constexpr int PART = A::BYTES;
   static_assert(A::BYTES == B::BYTES && A::LOADS == 2 && B::LOADS == 2, "equal parts");
 
@@ -525,7 +529,7 @@ __global__ __launch_bounds__(512) void k_product_large(Product g) {
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     l.ta[h].init(g.A, h * 64, l.wave, l.lane);
-    l.tb[h].init(g.B, h * 32, l.wave, l.lane);
+    l.tb[h].init(g.B, LAYOUT == ROWS_ROWS ? h * 2 : h * 32, l.wave, l.lane);
   }
   l.pa = L::A::base(g.A, m0);
   l.pb = L::B::base(g.B, n0);
@@ -541,85 +545,124 @@ __global__ __launch_bounds__(512) void k_product_large(Product g) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) acc[i][j] = float4v{0, 0, 0, 0};
   if (first < end) l.run(g, first, end, acc);
-  epilogue<T, 4, 8, 4, EPI>(g, acc, m0, n0, tn, l.wm, l.wn, split, l.lane);
+  epilogue<T, LAYOUT, 4, 8, 4, EPI>(g, acc, m0, n0, tn, l.wm, l.wn, split, l.lane);
 }
 
-template <typename T, int WN, int FM, int FN, int EPI>
+constexpr float LOG2E = 1.44269502162933349609375f;
+
+// exp(z - shift), of shift log2 e.
+__device__ __forceinline__ float exp_less(float z, float shift2) {
+  return __builtin_amdgcn_exp2f(fmaf(z, LOG2E, -shift2));
+}
+
+// acc[i][j][r] is row m0 + (wm FM + i) 16 + (lane & 15).  Its column is n0 + wn
+// 16 FN + (lane >> 4) 4 FN + 4 j + r where B is row-wise (the lane's results of a
+// row side by side), + 16 j + (lane >> 4) 4 + r where it is not.
+template <typename T, int LAYOUT, int WN, int FM, int FN, int EPI>
 __device__ __forceinline__ void epilogue(const Product &g, float4v (&acc)[FM][FN], long long m0,
                                          long long n0, int tn, int wm, int wn, int split,
                                          int lane) {
-  // acc[i][j][r]: row m0 + (wm FM + i) 16 + (lane & 15), column n0 + (wn FN +
-  // j) 16 + (lane >> 4) 4 + r
+  constexpr int L = 4 * FN;  // results of a lane in a row
+  const int group = lane >> 4;
+  if constexpr (EPI == EPI_PART || EPI == EPI_SCORE || EPI == EPI_DS) {
+    static_assert(LAYOUT == ROWS_ROWS, "a lane's results side by side");
+    const long long nb = n0 + wn * FN * 16 + group * L;
+    const bool full = n0 + wn * FN * 16 + FN * 16 <= g.N;
 #pragma unroll
-  for (int i = 0; i < FM; ++i) {
-    const long long m = m0 + (wm * FM + i) * 16 + (lane & 15);
-    const bool in = m < g.M;
-    const long long nb = n0 + wn * FN * 16 + (lane >> 4) * 4;
-    if constexpr (EPI == EPI_PART || EPI == EPI_SCORE) {
-      float mx = -INFINITY;
-      const long long tgt = EPI == EPI_PART && in ? g.target[m] : -1;
+    for (int i = 0; i < FM; ++i) {
+      const long long m = m0 + (wm * FM + i) * 16 + (lane & 15);
+      const bool in = m < g.M;
+      if constexpr (EPI == EPI_DS) {
+        const int32_t tgt = in ? g.target[m] : -1;
+        float c = in && tgt != -1 ? (g.grad ? g.grad[m] : 1.0f) : 0.0f;
+        if (tgt < -1 || tgt >= g.words) c = NAN;  // no such word
+        if (g.scale) c *= *g.scale;
+        const float lse2 = (in ? g.lse[m] : 0.0f) * LOG2E;
+        float v[L];
+#pragma unroll
+        for (int q = 0; q < L; ++q) v[q] = c * exp_less(acc[i][q / 4][q % 4], lse2);
+        const long long at = tgt - g.n0 - nb;
+        if (at >= 0 && at < L) {  // (one lane in many)
+#pragma unroll
+          for (int q = 0; q < L; ++q)
+            if (q == at) v[q] -= c;
+        }
+        if (__any(c == 0.0f)) {  // rows without a word: zeros, whatever their scores
+#pragma unroll
+          for (int q = 0; q < L; ++q)
+            if (c == 0.0f) v[q] = 0.0f;
+        }
+        if (!full) {
+#pragma unroll
+          for (int q = 0; q < L; ++q)
+            if (nb + q >= g.N) v[q] = 0.0f;
+        }
+        if (in && nb < g.Np) {
+          alignas(16) T o[L];
+#pragma unroll
+          for (int q = 0; q < L; ++q) o[q] = (T)v[q];
+          int4v *to = reinterpret_cast<int4v *>(static_cast<T *>(g.out) + m * g.ldo + nb);
+#pragma unroll
+          for (int q = 0; q < L * (int)sizeof(T) / 16; ++q)
+            to[q] = reinterpret_cast<const int4v *>(o)[q];
+        }
+      } else {
+        if constexpr (EPI == EPI_PART) {
+          const long long at = (in ? g.target[m] : -1) - nb;
+          if (at >= 0 && at < L && nb + at < g.N) {
+#pragma unroll
+            for (int q = 0; q < L; ++q)
+              if (q == at) g.hit[m] = acc[i][q / 4][q % 4];
+          }
+        } else if (in) {
+          float *to = static_cast<float *>(g.out) + m * g.ldo + nb;
+#pragma unroll
+          for (int q = 0; q < L; ++q)
+            if (full || nb + q < g.N) to[q] = acc[i][q / 4][q % 4];
+        }
+        if (!full) {  // what is not there weighs nothing
+#pragma unroll
+          for (int q = 0; q < L; ++q)
+            if (nb + q >= g.N) acc[i][q / 4][q % 4] = -INFINITY;
+        }
+        float mx = -INFINITY;
+#pragma unroll
+        for (int q = 0; q < L; ++q) mx = fmaxf(mx, acc[i][q / 4][q % 4]);
+        // the four lanes of a row
+        mx = fmaxf(mx, __shfl_xor(mx, 16));
+        mx = fmaxf(mx, __shfl_xor(mx, 32));
+        const float s2 = shift_of(mx) * LOG2E;
+        float sum = 0.0f;
+#pragma unroll
+        for (int q = 0; q < L; ++q) sum += exp_less(acc[i][q / 4][q % 4], s2);
+        sum += __shfl_xor(sum, 16);
+        sum += __shfl_xor(sum, 32);
+        if (in && lane < 16) g.part[(long long)(tn * WN + wn) * g.M + m] = make_float2(mx, sum);
+      }
+    }
+  } else {
+    const float back = EPI == EPI_RESULT && g.scale ? 1.0f / *g.scale : 1.0f;
+    typedef std::conditional_t<EPI == EPI_SUM, float, T> O;
+    typedef __attribute__((ext_vector_type(4))) O O4;
+#pragma unroll
+    for (int i = 0; i < FM; ++i) {
+      const long long m = m0 + (wm * FM + i) * 16 + (lane & 15);
+      if (m >= g.M) continue;
+      O *row = static_cast<O *>(g.out) + (EPI == EPI_SUM ? split * g.M + m : m) * g.ldo;
 #pragma unroll
       for (int j = 0; j < FN; ++j) {
-        const long long n = nb + j * 16;
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          if (n + r < g.N) mx = fmaxf(mx, acc[i][j][r]);
-          if (EPI == EPI_PART && n + r == tgt && n + r < g.N) g.hit[m] = acc[i][j][r];
-        }
-        if (EPI == EPI_SCORE && in && n < g.N) {
-          const long long left = g.N - n;
-          store4(static_cast<float *>(g.out) + m * g.ldo + n, acc[i][j],
-                 left < 4 ? (int)left : 4);
-        }
-      }
-      const float sh = shift_of(mx);
-      float sum = 0.0f;
-#pragma unroll
-      for (int j = 0; j < FN; ++j)
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-          if (nb + j * 16 + r < g.N) sum += __expf(acc[i][j][r] - sh);
-      // the four lanes of a row
-#pragma unroll
-      for (int x = 16; x < 64; x <<= 1) {
-        const float m2 = __shfl_xor(mx, x), s2 = __shfl_xor(sum, x);
-        join(mx, sum, m2, s2);
-      }
-      if (in && lane < 16) g.part[m * g.parts + tn * WN + wn] = make_float2(mx, sum);
-    } else if constexpr (EPI == EPI_DS) {
-      const float lse = in ? g.lse[m] : 0.0f;
-      const long long tgt = in ? g.target[m] : -1;
-      float c = in && tgt != -1 ? (g.grad ? g.grad[m] : 1.0f) : 0.0f;
-      if (tgt < -1 || tgt >= g.words) c = NAN;  // no such word
-      if (g.scale) c *= *g.scale;
-#pragma unroll
-      for (int j = 0; j < FN; ++j) {
-        const long long n = nb + j * 16;
-        float4v v;
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const float p = __expf(acc[i][j][r] - lse) - (g.n0 + n + r == tgt ? 1.0f : 0.0f);
-          v[r] = c != 0.0f && n + r < g.N ? c * p : 0.0f;
-        }
-        if (m < g.Mp && n < g.Np) store4(static_cast<T *>(g.out) + m * g.ldo + n, v, 4);
-      }
-    } else {
-      const float back = EPI == EPI_RESULT && g.scale ? 1.0f / *g.scale : 1.0f;
-#pragma unroll
-      for (int j = 0; j < FN; ++j) {
-        const long long n = nb + j * 16;
-        if (!in || n >= g.N) continue;
-        const int valid = g.N - n < 4 ? (int)(g.N - n) : 4;
-        if constexpr (EPI == EPI_SUM) {
-          float *p = static_cast<float *>(g.out) + (split * g.M + m) * g.ldo + n;
-          float4v v = acc[i][j];
-          if (g.add)
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-              if (r < valid) v[r] += p[r];
-          store4(p, v, valid);
+        const long long n = n0 + wn * FN * 16 +
+                            (LAYOUT == ROWS_ROWS ? group * L + j * 4 : j * 16 + group * 4);
+        if (n >= g.N) continue;
+        float4v v = acc[i][j] * back;
+        if (g.wide && n + 4 <= g.N) {
+          if (EPI == EPI_SUM && g.add) v += *reinterpret_cast<const float4v *>(row + n);
+          *reinterpret_cast<O4 *>(row + n) = O4{(O)v[0], (O)v[1], (O)v[2], (O)v[3]};
         } else {
-          store4(static_cast<T *>(g.out) + m * g.ldo + n, acc[i][j] * back, valid);
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            if (n + r < g.N)
+              row[n + r] = (O)(EPI == EPI_SUM && g.add ? v[r] + (float)row[n + r] : v[r]);
         }
       }
     }
@@ -646,31 +689,39 @@ __device__ __forceinline__ float wave_sum_f(float v) {
   return v;
 }
 
-// log of the sum of exponentials of a row from its tiles' maxima and sums.
-__device__ __forceinline__ float row_lse(const float2 *part, int parts, int lane) {
+// The log of the sum of exponentials of rows r0 .. r0 + 15 from their parts'
+// maxima and sums, by a workgroup of 16 threads a row, to s_lse.
+__device__ __forceinline__ void rows_lse(const float2 *__restrict__ part, int parts,
+                                         long long rows, long long r0, float *s_lse) {
+  __shared__ float2 s_part[NT];
+  const int row = threadIdx.x % 16, slice = threadIdx.x / 16;
   float m = -INFINITY, s = 0.0f;
-  for (int i = lane; i < parts; i += WAVE) {
-    const float2 v = part[i];
-    join(m, s, v.x, v.y);
+  if (r0 + row < rows) {
+#pragma unroll 4
+    for (int i = slice; i < parts; i += NT / 16) {
+      const float2 v = part[(long long)i * rows + r0 + row];
+      join(m, s, v.x, v.y);
+    }
   }
-#pragma unroll
-  for (int x = 1; x < WAVE; x <<= 1) {
-    const float m2 = __shfl_xor(m, x), s2 = __shfl_xor(s, x);
-    join(m, s, m2, s2);
+  s_part[threadIdx.x] = make_float2(m, s);
+  __syncthreads();
+  if (slice == 0) {
+    for (int i = 1; i < NT / 16; ++i) join(m, s, s_part[i * 16 + row].x, s_part[i * 16 + row].y);
+    // (a row of infinities: the sum, or none of it, is what is left)
+    s_lse[row] = shift_of(m) + logf(s);
   }
-  // (a row of infinities: the sum, or none of it, is what is left)
-  return shift_of(m) + logf(s);
+  __syncthreads();
 }
 
 __global__ __launch_bounds__(NT) void k_loss(const float2 *__restrict__ part, int parts,
                                              long long rows, const int32_t *__restrict__ target,
                                              long long words, const float *__restrict__ hit,
                                              float *__restrict__ loss, float *__restrict__ lse) {
-  const int lane = threadIdx.x & (WAVE - 1);
-  const long long r = (long long)blockIdx.x * NWAVES + threadIdx.x / WAVE;
-  if (r >= rows) return;
-  const float l = row_lse(part + r * parts, parts, lane);
-  if (lane) return;
+  __shared__ float s_lse[16];
+  const long long r0 = (long long)blockIdx.x * 16, r = r0 + threadIdx.x;
+  rows_lse(part, parts, rows, r0, s_lse);
+  if (threadIdx.x >= 16 || r >= rows) return;
+  const float l = s_lse[threadIdx.x];
   lse[r] = l;
   const int32_t t = target[r];
   loss[r] = t == -1 ? 0.0f : t < -1 || t >= words ? NAN : l - hit[r];
@@ -680,12 +731,12 @@ __global__ __launch_bounds__(NT) void k_loss(const float2 *__restrict__ part, in
 __global__ __launch_bounds__(NT) void k_normalise(const float2 *__restrict__ part, int parts,
                                                   long long rows, long long cols,
                                                   float *__restrict__ z) {
-  const int lane = threadIdx.x & (WAVE - 1);
-  const long long r = (long long)blockIdx.x * NWAVES + threadIdx.x / WAVE;
-  if (r >= rows) return;
-  const float l = row_lse(part + r * parts, parts, lane);
-  float *p = z + r * cols;
-  for (long long c = lane; c < cols; c += WAVE) p[c] -= l;
+  __shared__ float s_lse[16];
+  const long long r0 = (long long)blockIdx.x * 16;
+  rows_lse(part, parts, rows, r0, s_lse);
+  const int n = rows - r0 < 16 ? (int)(rows - r0) : 16;
+  for (int r = threadIdx.x / WAVE; r < n; r += NWAVES)
+    for (long long c = threadIdx.x % WAVE; c < cols; c += WAVE) z[(r0 + r) * cols + c] -= s_lse[r];
 }
 
 // The power of two that brings the largest |gradient| to [2^13, 2^14): 16-bit
@@ -899,11 +950,13 @@ struct SplitProduct {
     if (splits == 1) {
       g.out = out.data;
       g.ldo = out.stride;
+      g.wide = (uintptr_t)out.data % (4 * sizeof(T)) == 0 && out.stride % 4 == 0;
       g.scale = scale;
       return product<T, LAYOUT, EPI_RESULT>(g, tile, s);
     }
     g.out = sums;
     g.ldo = N;
+    g.wide = N % 4 == 0;
     TRY((product<T, LAYOUT, EPI_SUM>(g, tile, s)));
     k_finish<T><<<blocks_for(M * N, NT), NT, 0, s>>>(sums, splits, M, N, scale,
                                                    static_cast<T *>(out.data), out.stride);
@@ -917,7 +970,7 @@ hipError_t emission_as(const Mat &x, const Mat &w, float *weight, Bump &b, hipSt
   const Laid<T> lx = lay<T>(x, b), lw = lay<T>(w, b);
   const int tile = tile_for(N, C);
   const int parts = (int)((C + TILES[tile].bn - 1) / TILES[tile].bn) * TILES[tile].wn;
-  float2 *part = b.take<float2>(N * parts);
+  float2 *part = b.take<float2>((long long)N * parts);
   if (!b.base) return hipSuccess;
   TRY(fill(lx, x, s));
   TRY(fill(lw, w, s));
@@ -932,9 +985,8 @@ hipError_t emission_as(const Mat &x, const Mat &w, float *weight, Bump &b, hipSt
   g.out = weight;
   g.ldo = C;
   g.part = part;
-  g.parts = parts;
   TRY((product<T, ROWS_ROWS, EPI_SCORE>(g, tile, s)));
-  k_normalise<<<(unsigned)((N + NWAVES - 1) / NWAVES), NT, 0, s>>>(part, parts, N, C, weight);
+  k_normalise<<<(unsigned)((N + 15) / 16), NT, 0, s>>>(part, parts, N, C, weight);
   return hipGetLastError();
 }
 
@@ -984,7 +1036,7 @@ hipError_t loss_as(const Mat &x, const Mat &w, const int32_t *target, float *los
   const Laid<T> lx = lay<T>(x, b), lw = lay<T>(w, b);
   const int tile = tile_for(N, V);
   const int parts = (int)((V + TILES[tile].bn - 1) / TILES[tile].bn) * TILES[tile].wn;
-  float2 *part = b.take<float2>(N * parts);
+  float2 *part = b.take<float2>((long long)N * parts);
   float *hit = b.take<float>(N);
   if (!b.base) return hipSuccess;
   TRY(fill(lx, x, s));
@@ -998,11 +1050,10 @@ hipError_t loss_as(const Mat &x, const Mat &w, const int32_t *target, float *los
   g.splits = 1;
   g.steps = INT32_MAX;
   g.part = part;
-  g.parts = parts;
   g.target = target;
   g.hit = hit;
   TRY((product<T, ROWS_ROWS, EPI_PART>(g, tile, s)));
-  k_loss<<<(unsigned)((N + NWAVES - 1) / NWAVES), NT, 0, s>>>(part, parts, N, target, V, hit, loss,
+  k_loss<<<(unsigned)((N + 15) / 16), NT, 0, s>>>(part, parts, N, target, V, hit, loss,
                                                             lse);
   return hipGetLastError();
 }
@@ -1010,9 +1061,10 @@ hipError_t loss_as(const Mat &x, const Mat &w, const int32_t *target, float *los
 // Bytes of dS that a piece of the vocabulary may take.
 constexpr long long PIECE_BYTES = 512ll << 20;
 
-#ifndef DSPAD
-#define DSPAD 64
-#endif
+// Elements between rows of dS: with rows of a power of two bytes the product dx
+// takes 3 % longer, all of a wavefront's rows in the same channels.
+constexpr long long DS_GAP = 64;
+
 // Words of a piece of the vocabulary, `most` at most (or 256): all of them, or
 // rows of dw's tiles that fill the CUs a whole number of times (16,000 rows, 32,000
 // words, width 1024: pieces of 16,640 words leave dw 260 tiles, 0.90 ms; 16,384
@@ -1041,7 +1093,7 @@ hipError_t loss_grads_as(const Mat &x, const Mat &w, const int32_t *target, cons
   const long long piece = piece_of(V, H, PIECE_BYTES / (Np * (long long)sizeof(T)));
   const bool whole = piece == V;
   const long long Pp = up(piece, 64);
-  T *ds = b.take<T>(Np * (Pp + DSPAD));
+  T *ds = b.take<T>(N * (Pp + DS_GAP));
   uint32_t *mx = b.take<uint32_t>(1);
   float *scale = b.take<float>(1);
   SplitProduct<T, ROWS_COLS> px{};
@@ -1088,19 +1140,18 @@ hipError_t loss_grads_as(const Mat &x, const Mat &w, const int32_t *target, cons
     g.n0 = v0;
     g.words = V;
     g.out = ds;
-    g.ldo = np + DSPAD;
+    g.ldo = np + DS_GAP;
     g.target = target;
     g.lse = lse;
     g.grad = grad;
     g.scale = scale;
-    g.Mp = Np;
     g.Np = np;
     TRY((product<T, ROWS_ROWS, EPI_DS>(g, tile_for(N, n), s)));
     if (gx && whole) {
-      TRY(px.run({ds, np + DSPAD, N, np}, wc, N, H, n, scale, *gx, s));
+      TRY(px.run({ds, np + DS_GAP, N, np}, wc, N, H, n, scale, *gx, s));
     } else if (gx) {
       Product q{};
-      q.A = {ds, np + DSPAD, N, np};
+      q.A = {ds, np + DS_GAP, N, np};
       q.B = wc;
       q.M = N;
       q.N = H;
@@ -1109,6 +1160,7 @@ hipError_t loss_grads_as(const Mat &x, const Mat &w, const int32_t *target, cons
       q.steps = INT32_MAX;
       q.out = sums;
       q.ldo = H;
+      q.wide = H % 4 == 0;
       q.add = v0 > 0;
       TRY((product<T, ROWS_COLS, EPI_SUM>(q, tile_for(N, H), s)));
     }
@@ -1118,7 +1170,7 @@ hipError_t loss_grads_as(const Mat &x, const Mat &w, const int32_t *target, cons
       out.rows = n;
       b.at = mark;
       pw.plan(n, H, Np, b);
-      TRY(pw.run({ds, np + DSPAD, np, N}, lx.columns(), n, H, N, scale, out, s));
+      TRY(pw.run({ds, np + DS_GAP, np, N}, lx.columns(), n, H, N, scale, out, s));
     }
   }
   if (sums) {
