@@ -104,15 +104,19 @@ struct Rows {
     return first + r / RUN * EVERY_ + r % RUN;
   }
 };
-// The rows of B so that a lane's results lie side by side: fragments FIRST on,
-// PER of a wavefront's FN, where row i of fragment j is the wavefront's row i / 4 *
-// 4 FN + 4 j + i % 4 (a lane of group i / 4 gets results i % 4 of every j).
-template <int FN, int PER>
+// The rows of B so that a lane's results of a row lie side by side in groups of
+// E (16 bytes), and the groups of its four lanes side by side: of a lane group a,
+// the results r of its fragments j are q = 4 j + r, and column q / E 4 E + a E +
+// q % E.  FN fragments of a wavefront, PER of them from the FIRST on in this part.
+template <int E, int FN, int PER>
 struct Spread {
   static constexpr int RUN = 4;
+  static __device__ __forceinline__ int column(int group, int q) {
+    return q / E * 4 * E + group * E + q % E;
+  }
   static __device__ __forceinline__ int of(int first, int r) {
     const int w = r / (PER * 16), j = first + r / 16 % PER, i = r % 16;
-    return w * FN * 16 + i / 4 * 4 * FN + 4 * j + i % 4;
+    return w * FN * 16 + column(i / 4, 4 * j + i % 4);
   }
 };
 
@@ -308,7 +312,7 @@ template <typename T, int LAYOUT, int BM, int BN, int WM, int WN, int EPI>
 __global__ __launch_bounds__(WM *WN *WAVE) void k_product(Product g) {
   constexpr int NWV = WM * WN, FM = BM / WM / 16, FN = BN / WN / 16;
   using A = TileA<T, LAYOUT, BM, NWV, Rows<BM, BM>>;
-  using B = TileB<T, LAYOUT, BN, NWV, Spread<FN, FN>, Rows<BN, BN>>;
+  using B = TileB<T, LAYOUT, BN, NWV, Spread<16 / (int)sizeof(T), FN, FN>, Rows<BN, BN>>;
   __shared__ __align__(1024) char s_lds[2][A::BYTES + B::BYTES];
   const int lane = threadIdx.x & (WAVE - 1);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
@@ -394,7 +398,7 @@ template <typename T, int LAYOUT>
 struct Large {
   static constexpr int NWV = 8;
   using A = TileA<T, LAYOUT, 128, NWV, Rows<64, 128>>;
-  using B = TileB<T, LAYOUT, 128, NWV, Spread<4, 2>, Rows<32, 64>>;
+  using B = TileB<T, LAYOUT, 128, NWV, Spread<16 / (int)sizeof(T), 4, 2>, Rows<32, 64>>;
   static constexpr int PART = A::BYTES;
   static_assert(A::BYTES == B::BYTES && A::LOADS == 2 && B::LOADS == 2, "equal parts");
 
@@ -482,17 +486,26 @@ struct Large {
     multiply<1, (LEFT > 1) ? 4 : 0>(acc, [&](int i) { load_a(i, ba, place); });
   }
 
-  // Steps first .. end - 1 (one at least).
-  __device__ __forceinline__ void run(const Product &g, int first, int end,
-                                      float4v (&acc)[8][4]) {
-    const bool two = first + 1 < end;
-    for (int s = 0; s < (two ? 2 : 1); ++s) {
+  // Sends for the first two steps of a tile (of those there are).
+  __device__ __forceinline__ void begin(const Product &g, long long m0, long long n0, int first,
+                                        int end) {
+    pa = A::base(g.A, m0);
+    pb = B::base(g.B, n0);
+    na = A::bytes(g.A, m0);
+    nb = B::bytes(g.B, n0);
+    for (int s = 0; s < 2 && first + s < end; ++s) {
       const int4v ba = A::step(g.A, pa, na, first + s), bb = B::step(g.B, pb, nb, first + s);
 #pragma unroll
       for (int i = 0; i < 4; ++i) load_b(i, bb, 2 * s * PAIR);
 #pragma unroll
       for (int i = 0; i < 4; ++i) load_a(i, ba, (2 * s + 1) * PAIR);
     }
+  }
+
+  // Steps first .. end - 1 (one at least) of the tile that begin was called for.
+  __device__ __forceinline__ void run(const Product &g, int first, int end,
+                                      float4v (&acc)[8][4]) {
+    const bool two = first + 1 < end;
     if (two)
       wait_loads<10>();
     else
@@ -522,30 +535,35 @@ __global__ __launch_bounds__(512) void k_product_large(Product g) {
   l.wn = l.wave % 4;
   l.lds = s_lds;
   l.at = lds_address(s_lds);
-  int tm, tn;
-  tile_of(g, blockIdx.x, tm, tn);
-  const long long m0 = (long long)tm * 256, n0 = (long long)tn * 256;
   const int split = blockIdx.z;
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     l.ta[h].init(g.A, h * 64, l.wave, l.lane);
     l.tb[h].init(g.B, LAYOUT == ROWS_ROWS ? h * 2 : h * 32, l.wave, l.lane);
   }
-  l.pa = L::A::base(g.A, m0);
-  l.pb = L::B::base(g.B, n0);
-  l.na = L::A::bytes(g.A, m0);
-  l.nb = L::B::bytes(g.B, n0);
   const int all = (int)((g.K + k_step<T>() - 1) / k_step<T>());
   const int first = split * g.steps;
   const int end = all - first < g.steps ? all : first + g.steps;
+  const unsigned tiles = (unsigned)g.tiles_m * (unsigned)g.tiles_n;
 
-  float4v acc[8][4];
+  int tm, tn;
+  tile_of(g, blockIdx.x, tm, tn);
+  if (first < end) l.begin(g, tm * 256ll, tn * 256ll, first, end);
+  for (unsigned id = blockIdx.x; id < tiles; id += gridDim.x) {
+    float4v acc[8][4];
 #pragma unroll
-  for (int i = 0; i < 8; ++i)
+    for (int i = 0; i < 8; ++i)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) acc[i][j] = float4v{0, 0, 0, 0};
-  if (first < end) l.run(g, first, end, acc);
-  epilogue<T, LAYOUT, 4, 8, 4, EPI>(g, acc, m0, n0, tn, l.wm, l.wn, split, l.lane);
+      for (int j = 0; j < 4; ++j) acc[i][j] = float4v{0, 0, 0, 0};
+    if (first < end) l.run(g, first, end, acc);
+    const long long m0 = tm * 256ll, n0 = tn * 256ll;
+    const int at = tn;
+    if (id + gridDim.x < tiles) {  // the next tile's first loads, while this one is written
+      tile_of(g, id + gridDim.x, tm, tn);
+      if (first < end) l.begin(g, tm * 256ll, tn * 256ll, first, end);
+    }
+    epilogue<T, LAYOUT, 4, 8, 4, EPI>(g, acc, m0, n0, at, l.wm, l.wn, split, l.lane);
+  }
 }
 
 constexpr float LOG2E = 1.44269502162933349609375f;
@@ -555,9 +573,9 @@ __device__ __forceinline__ float exp_less(float z, float shift2) {
   return __builtin_amdgcn_exp2f(fmaf(z, LOG2E, -shift2));
 }
 
-// acc[i][j][r] is row m0 + (wm FM + i) 16 + (lane & 15).  Its column is n0 + wn
-// 16 FN + (lane >> 4) 4 FN + 4 j + r where B is row-wise (the lane's results of a
-// row side by side), + 16 j + (lane >> 4) 4 + r where it is not.
+// acc[i][j][r] is row m0 + (wm FM + i) 16 + (lane & 15).  Of the wavefront's
+// columns, n0 + wn 16 FN on, it is Spread's where B is row-wise, 16 j + (lane >>
+// 4) 4 + r where it is not.
 template <typename T, int LAYOUT, int WN, int FM, int FN, int EPI>
 __device__ __forceinline__ void epilogue(const Product &g, float4v (&acc)[FM][FN], long long m0,
                                          long long n0, int tn, int wm, int wn, int split,
@@ -566,8 +584,15 @@ __device__ __forceinline__ void epilogue(const Product &g, float4v (&acc)[FM][FN
   const int group = lane >> 4;
   if constexpr (EPI == EPI_PART || EPI == EPI_SCORE || EPI == EPI_DS) {
     static_assert(LAYOUT == ROWS_ROWS, "a lane's results side by side");
-    const long long nb = n0 + wn * FN * 16 + group * L;
-    const bool full = n0 + wn * FN * 16 + FN * 16 <= g.N;
+    constexpr int E = 16 / (int)sizeof(T);
+    const long long nb = n0 + wn * FN * 16;
+    const bool full = nb + FN * 16 <= g.N;
+    const auto col = [&](int q) { return Spread<E, FN, FN>::column(group, q); };
+    // which of the lane's results the row's target is, -1: none
+    const auto place = [&](long long word) {
+      const long long c = word - nb;
+      return c < 0 || c >= FN * 16 || c / E % 4 != group ? -1 : (int)(c / (4 * E) * E + c % E);
+    };
 #pragma unroll
     for (int i = 0; i < FM; ++i) {
       const long long m = m0 + (wm * FM + i) * 16 + (lane & 15);
@@ -581,8 +606,8 @@ __device__ __forceinline__ void epilogue(const Product &g, float4v (&acc)[FM][FN
         float v[L];
 #pragma unroll
         for (int q = 0; q < L; ++q) v[q] = c * exp_less(acc[i][q / 4][q % 4], lse2);
-        const long long at = tgt - g.n0 - nb;
-        if (at >= 0 && at < L) {  // (one lane in many)
+        const int at = place(tgt - g.n0);
+        if (at >= 0) {  // (one lane in many)
 #pragma unroll
           for (int q = 0; q < L; ++q)
             if (q == at) v[q] -= c;
@@ -595,21 +620,23 @@ __device__ __forceinline__ void epilogue(const Product &g, float4v (&acc)[FM][FN
         if (!full) {
 #pragma unroll
           for (int q = 0; q < L; ++q)
-            if (nb + q >= g.N) v[q] = 0.0f;
+            if (nb + col(q) >= g.N) v[q] = 0.0f;
         }
         if (in && nb < g.Np) {
           alignas(16) T o[L];
 #pragma unroll
           for (int q = 0; q < L; ++q) o[q] = (T)v[q];
-          int4v *to = reinterpret_cast<int4v *>(static_cast<T *>(g.out) + m * g.ldo + nb);
+          T *to = static_cast<T *>(g.out) + m * g.ldo + nb;
 #pragma unroll
-          for (int q = 0; q < L * (int)sizeof(T) / 16; ++q)
-            to[q] = reinterpret_cast<const int4v *>(o)[q];
+          for (int q = 0; q < L; q += E)
+            if (nb + col(q) < g.Np)
+              *reinterpret_cast<int4v *>(to + col(q)) = *reinterpret_cast<const int4v *>(o + q);
         }
       } else {
         if constexpr (EPI == EPI_PART) {
-          const long long at = (in ? g.target[m] : -1) - nb;
-          if (at >= 0 && at < L && nb + at < g.N) {
+          const int32_t tgt = in ? g.target[m] : -1;
+          const int at = tgt < g.N ? place(tgt) : -1;
+          if (at >= 0) {
 #pragma unroll
             for (int q = 0; q < L; ++q)
               if (q == at) g.hit[m] = acc[i][q / 4][q % 4];
@@ -618,12 +645,12 @@ __device__ __forceinline__ void epilogue(const Product &g, float4v (&acc)[FM][FN
           float *to = static_cast<float *>(g.out) + m * g.ldo + nb;
 #pragma unroll
           for (int q = 0; q < L; ++q)
-            if (full || nb + q < g.N) to[q] = acc[i][q / 4][q % 4];
+            if (full || nb + col(q) < g.N) to[col(q)] = acc[i][q / 4][q % 4];
         }
         if (!full) {  // what is not there weighs nothing
 #pragma unroll
           for (int q = 0; q < L; ++q)
-            if (nb + q >= g.N) acc[i][q / 4][q % 4] = -INFINITY;
+            if (nb + col(q) >= g.N) acc[i][q / 4][q % 4] = -INFINITY;
         }
         float mx = -INFINITY;
 #pragma unroll
@@ -652,7 +679,8 @@ __device__ __forceinline__ void epilogue(const Product &g, float4v (&acc)[FM][FN
 #pragma unroll
       for (int j = 0; j < FN; ++j) {
         const long long n = n0 + wn * FN * 16 +
-                            (LAYOUT == ROWS_ROWS ? group * L + j * 4 : j * 16 + group * 4);
+                            (LAYOUT == ROWS_ROWS ? Spread<16 / (int)sizeof(T), FN, FN>::column(group, 4 * j)
+                                                 : j * 16 + group * 4);
         if (n >= g.N) continue;
         float4v v = acc[i][j] * back;
         if (g.wide && n + 4 <= g.N) {
@@ -873,7 +901,8 @@ hipError_t product(Product g, int tile, hipStream_t s) {
   g.tiles_n = (int)tn;
   const dim3 grid((unsigned)(tm * tn), 1, (unsigned)g.splits);
   if (tile == 0)
-    k_product_large<T, LAYOUT, EPI><<<grid, 512, 0, s>>>(g);
+    k_product_large<T, LAYOUT, EPI>
+        <<<dim3((unsigned)(tm * tn < CUS ? tm * tn : CUS), 1, (unsigned)g.splits), 512, 0, s>>>(g);
   else if (tile == 1)
     k_product<T, LAYOUT, 128, 128, 2, 2, EPI><<<grid, 256, 0, s>>>(g);
   else
