@@ -257,6 +257,7 @@ struct Product {
   const float *scale;    // power of two on dS (16-bit floats), or null (1)
   long long Np;          // dS: columns to write, zeros past N
   int add;               // sums: add to what is there
+  const float *sums;     // [M, N] or null
   int wide;              // results: `out` and its rows are aligned to four
 };
 
@@ -265,7 +266,7 @@ enum Epilogue {
   EPI_SCORE,   // the same and the scores as float32
   EPI_DS,      // gradient of the scores
   EPI_SUM,     // float32 sums, one block of M x N a split
-  EPI_RESULT   // results in T, times 1 / scale
+  EPI_RESULT   // results in T, times 1 / scale, of this sum and earlier pieces' (`sums`)
 };
 
 // Maximum that takes no infinity as a shift (exp(inf - inf) is no number).
@@ -682,7 +683,13 @@ __device__ __forceinline__ void epilogue(const Product &g, float4v (&acc)[FM][FN
                             (LAYOUT == ROWS_ROWS ? Spread<16 / (int)sizeof(T), FN, FN>::column(group, 4 * j)
                                                  : j * 16 + group * 4);
         if (n >= g.N) continue;
-        float4v v = acc[i][j] * back;
+        float4v v = acc[i][j];
+        if (EPI == EPI_RESULT && g.sums) {
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            if (n + r < g.N) v[r] += g.sums[m * g.N + n + r];
+        }
+        v *= back;
         if (g.wide && n + 4 <= g.N) {
           if (EPI == EPI_SUM && g.add) v += *reinterpret_cast<const float4v *>(row + n);
           *reinterpret_cast<O4 *>(row + n) = O4{(O)v[0], (O)v[1], (O)v[2], (O)v[3]};
@@ -943,6 +950,12 @@ hipError_t fill(const Laid<T> &l, const Mat &m, hipStream_t s) {
   return hipGetLastError();
 }
 
+// Whether four results side by side may be written at once.
+template <typename T>
+int wide(const Mat &m) {
+  return (uintptr_t)m.data % (4 * sizeof(T)) == 0 && m.stride % 4 == 0;
+}
+
 // out = A B^T with the sum split where the tiles alone are too few.
 template <typename T, int LAYOUT>
 struct SplitProduct {
@@ -958,10 +971,17 @@ struct SplitProduct {
     const long long tiles =
         ((M + TILES[tile].bm - 1) / TILES[tile].bm) * ((N + TILES[tile].bn - 1) / TILES[tile].bn);
     const long long all = (K + k_step<T>() - 1) / k_step<T>();
-    long long want = tiles >= CUS ? 1 : 2 * CUS / tiles;
-    want = want < all / 4 ? want : all / 4;  // four steps a split at least
-    want = want < 1 ? 1 : want > 256 ? 256 : want;
-    steps = (all + want - 1) / want;
+    // What takes least, in steps: the rounds of all CUs, where a smaller tile
+    // leaves a CU room for more, and four steps more for what splitting adds
+    // (244 tiles of 256 x 256, 250 steps: one part 0.41 ms, two 0.44 and
+    // 0.05 to add them up).
+    const long long slots = tile == 0 ? CUS : 2 * CUS;
+    long long best = INT64_MAX;
+    for (long long p = 1; p <= 256 && (p == 1 || p <= all / 4); ++p) {
+      const long long per = (all + p - 1) / p;
+      const long long cost = (tiles * p + slots - 1) / slots * (per + 2) + (p > 1 ? 4 + p / 8 : 0);
+      if (cost < best) best = cost, steps = per;
+    }
     splits = (int)((all + steps - 1) / steps);
     sums = splits > 1 ? b.take<float>(splits * M * N) : nullptr;
   }
@@ -979,7 +999,7 @@ struct SplitProduct {
     if (splits == 1) {
       g.out = out.data;
       g.ldo = out.stride;
-      g.wide = (uintptr_t)out.data % (4 * sizeof(T)) == 0 && out.stride % 4 == 0;
+      g.wide = wide<T>(out);
       g.scale = scale;
       return product<T, LAYOUT, EPI_RESULT>(g, tile, s);
     }
@@ -1187,11 +1207,20 @@ hipError_t loss_grads_as(const Mat &x, const Mat &w, const int32_t *target, cons
       q.K = n;
       q.splits = 1;
       q.steps = INT32_MAX;
-      q.out = sums;
-      q.ldo = H;
-      q.wide = H % 4 == 0;
-      q.add = v0 > 0;
-      TRY((product<T, ROWS_COLS, EPI_SUM>(q, tile_for(N, H), s)));
+      if (v0 + n < V) {
+        q.out = sums;
+        q.ldo = H;
+        q.wide = H % 4 == 0;
+        q.add = v0 > 0;
+        TRY((product<T, ROWS_COLS, EPI_SUM>(q, tile_for(N, H), s)));
+      } else {
+        q.out = gx->data;
+        q.ldo = gx->stride;
+        q.wide = wide<T>(*gx);
+        q.scale = scale;
+        q.sums = sums;
+        TRY((product<T, ROWS_COLS, EPI_RESULT>(q, tile_for(N, H), s)));
+      }
     }
     if (gw) {
       Mat out = *gw;
@@ -1201,11 +1230,6 @@ hipError_t loss_grads_as(const Mat &x, const Mat &w, const int32_t *target, cons
       pw.plan(n, H, Np, b);
       TRY(pw.run({ds, np + DS_GAP, np, N}, lx.columns(), n, H, N, scale, out, s));
     }
-  }
-  if (sums) {
-    k_finish<T><<<blocks_for(N * H, NT), NT, 0, s>>>(sums, 1, N, H, scale,
-                                                   static_cast<T *>(gx->data), gx->stride);
-    TRY(hipGetLastError());
   }
   return hipSuccess;
 }

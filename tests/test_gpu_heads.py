@@ -124,7 +124,7 @@ def test_cross_entropy(comp, N, V, H, typ):
 
 # large tiles in the scores (one to five steps of the sum), in grad_x and in
 # grad_w (sums over V and over N), with rows and columns past the last tile
-LARGE = [(3500, 3500, h) for h in (24, 100, 192, 256, 320)] + \
+LARGE = [(3500, 3500, h) for h in (24, 100, 192, 256, 320)] + [(5000, 5200, 72)] + \
     [(12500, v, 1000) for v in (40, 128, 190, 300)] + [(n, 12500, 1000) for n in (50, 65, 200, 257)]
 
 
