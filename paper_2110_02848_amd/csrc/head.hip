@@ -257,13 +257,14 @@ struct Product {
   const float *scale;    // power of two on dS (16-bit floats), or null (1)
   long long Np;          // dS: columns to write, zeros past N
   int add;               // sums: add to what is there
-  const float *sums;     // [M, N] or null
+  const float *sums;     // [M, N rounded up to four] or null
   int wide;              // results: `out` and its rows are aligned to four
 };
 
 enum Epilogue {
   EPI_PART,    // maxima and sums of exponentials, targets' scores
   EPI_SCORE,   // the same and the scores as float32
+  EPI_LOG,     // log-probabilities, of tiles as wide as a row
   EPI_DS,      // gradient of the scores
   EPI_SUM,     // float32 sums, one block of M x N a split
   EPI_RESULT   // results in T, times 1 / scale, of this sum and earlier pieces' (`sums`)
@@ -276,6 +277,13 @@ __device__ __forceinline__ void join(float &m, float &s, float m2, float s2) {
   const float mm = fmaxf(m, m2), sh = shift_of(mm);
   s = s * __expf(m - sh) + s2 * __expf(m2 - sh);
   m = mm;
+}
+
+constexpr float LOG2E = 1.44269502162933349609375f;
+
+// exp(z - shift), of shift log2 e.
+__device__ __forceinline__ float exp_less(float z, float shift2) {
+  return __builtin_amdgcn_exp2f(fmaf(z, LOG2E, -shift2));
 }
 
 // Tile (tm, tn) of workgroup `id`.  Workgroups go to the eight XCDs in turn,
@@ -308,7 +316,9 @@ __device__ __forceinline__ void epilogue(const Product &g, float4v (&acc)[FM][FN
                                          int lane);
 
 // Tiles of BM x BN where there are too few large ones: two buffers, the next
-// step's loads under way while one step's fragments are multiplied.
+// step's loads under way while one step's fragments are multiplied; several
+// workgroups a CU fill each other's gaps (three or four buffers, which leave
+// room for fewer, took 5 to 60 % longer).
 template <typename T, int LAYOUT, int BM, int BN, int WM, int WN, int EPI>
 __global__ __launch_bounds__(WM *WN *WAVE) void k_product(Product g) {
   constexpr int NWV = WM * WN, FM = BM / WM / 16, FN = BN / WN / 16;
@@ -329,31 +339,31 @@ __global__ __launch_bounds__(WM *WN *WAVE) void k_product(Product g) {
   tb.init(g.B, 0, wave, lane);
   const char *pa = A::base(g.A, m0), *pb = B::base(g.B, n0);
   const long long na = A::bytes(g.A, m0), nb = B::bytes(g.B, n0);
-  const auto fetch = [&](uint32_t to, int t) {
+  const uint32_t lds = lds_address(s_lds[0]);
+  const int all = (int)((g.K + k_step<T>() - 1) / k_step<T>());
+  const int first = split * g.steps;
+  const int end = all - first < g.steps ? all : first + g.steps;
+  const auto fetch = [&](int buffer, int t) {
+    const uint32_t to = lds + buffer * (A::BYTES + B::BYTES);
     const int4v ba = A::step(g.A, pa, na, t), bb = B::step(g.B, pb, nb, t);
 #pragma unroll
     for (int i = 0; i < A::LOADS; ++i) ta.fetch(i, to, ba, wave);
 #pragma unroll
     for (int i = 0; i < B::LOADS; ++i) tb.fetch(i, to + A::BYTES, bb, wave);
   };
-  const uint32_t lds = lds_address(s_lds[0]);
-  const int all = (int)((g.K + k_step<T>() - 1) / k_step<T>());
-  const int first = split * g.steps;
-  const int end = all - first < g.steps ? all : first + g.steps;
 
   float4v acc[FM][FN];
 #pragma unroll
   for (int i = 0; i < FM; ++i)
 #pragma unroll
     for (int j = 0; j < FN; ++j) acc[i][j] = float4v{0, 0, 0, 0};
-
-  if (first < end) fetch(lds, first);
-  uint32_t cur = 0;
+  if (first < end) fetch(0, first);
+  int cur = 0;
   for (int t = first; t < end; ++t, cur ^= 1) {
     // step t has landed, and no one reads the other buffer
     wait_loads<0>();
     __syncthreads();
-    if (t + 1 < end) fetch(lds + (cur ^ 1) * (A::BYTES + B::BYTES), t + 1);
+    if (t + 1 < end) fetch(cur ^ 1, t + 1);
     const char *sa = s_lds[cur], *sb = sa + A::BYTES;
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
@@ -368,7 +378,41 @@ __global__ __launch_bounds__(WM *WN *WAVE) void k_product(Product g) {
         for (int j = 0; j < FN; ++j) acc[i][j] = mac(fb[j], fa[i], acc[i][j]);
     }
   }
-  epilogue<T, LAYOUT, WN, FM, FN, EPI>(g, acc, m0, n0, tn, wm, wn, split, lane);
+  if constexpr (EPI == EPI_LOG) {
+    // rows of log-probabilities, put together in LDS: the rows of a tile lie
+    // side by side in memory (ldo is N)
+    static_assert(LAYOUT == ROWS_ROWS && WN == 1 && FM == 1, "a wavefront has whole rows");
+    static_assert(BM * BN * 4 <= (int)sizeof(s_lds), "room for the tile");
+    constexpr int E = 16 / (int)sizeof(T), L = 4 * FN;
+    const int group = lane >> 4, cols = (int)g.N;
+    float mx = -INFINITY, sum = 0.0f;
+#pragma unroll
+    for (int q = 0; q < L; ++q) {
+      if (Spread<E, FN, FN>::column(group, q) >= cols) acc[0][q / 4][q % 4] = -INFINITY;
+      mx = fmaxf(mx, acc[0][q / 4][q % 4]);
+    }
+    mx = fmaxf(mx, __shfl_xor(mx, 16));
+    mx = fmaxf(mx, __shfl_xor(mx, 32));
+    const float sh = shift_of(mx);
+#pragma unroll
+    for (int q = 0; q < L; ++q) sum += exp_less(acc[0][q / 4][q % 4], sh * LOG2E);
+    sum += __shfl_xor(sum, 16);
+    sum += __shfl_xor(sum, 32);
+    const float lse = sh + logf(sum);
+    __syncthreads();  // no one reads operands any more
+    float *s = reinterpret_cast<float *>(s_lds);
+#pragma unroll
+    for (int q = 0; q < L; ++q) {
+      const int c = Spread<E, FN, FN>::column(group, q);
+      if (c < cols) s[(wm * 16 + (lane & 15)) * cols + c] = acc[0][q / 4][q % 4] - lse;
+    }
+    __syncthreads();
+    const int n = (int)(g.M - m0 < BM ? g.M - m0 : BM) * cols;
+    float *out = static_cast<float *>(g.out) + m0 * cols;
+    for (int i = threadIdx.x; i < n; i += NWV * WAVE) out[i] = s[i];
+  } else {
+    epilogue<T, LAYOUT, WN, FM, FN, EPI>(g, acc, m0, n0, tn, wm, wn, split, lane);
+  }
 }
 
 __device__ __forceinline__ void meet() {
@@ -567,13 +611,6 @@ __global__ __launch_bounds__(512) void k_product_large(Product g) {
   }
 }
 
-constexpr float LOG2E = 1.44269502162933349609375f;
-
-// exp(z - shift), of shift log2 e.
-__device__ __forceinline__ float exp_less(float z, float shift2) {
-  return __builtin_amdgcn_exp2f(fmaf(z, LOG2E, -shift2));
-}
-
 // acc[i][j][r] is row m0 + (wm FM + i) 16 + (lane & 15).  Of the wavefront's
 // columns, n0 + wn 16 FN on, it is Spread's where B is row-wise, 16 j + (lane >>
 // 4) 4 + r where it is not.
@@ -687,7 +724,7 @@ __device__ __forceinline__ void epilogue(const Product &g, float4v (&acc)[FM][FN
         if (EPI == EPI_RESULT && g.sums) {
 #pragma unroll
           for (int r = 0; r < 4; ++r)
-            if (n + r < g.N) v[r] += g.sums[m * g.N + n + r];
+            if (n + r < g.N) v[r] += g.sums[m * ((g.N + 3) / 4 * 4) + n + r];
         }
         v *= back;
         if (g.wide && n + 4 <= g.N) {
@@ -708,14 +745,28 @@ __device__ __forceinline__ void epilogue(const Product &g, float4v (&acc)[FM][FN
 // rows and elements
 // ---------------------------------------------------------------------------
 
-// A copy with rows padded with zeros to `cols` elements.
+// Copies of two matrices with rows padded with zeros to `cols` elements (whole
+// groups of 16 bytes, one a thread).
 template <typename T>
-__global__ __launch_bounds__(NT) void k_pad(const T *__restrict__ p, long long ld, long long rows,
-                                            long long n, T *__restrict__ out, long long cols) {
-  for (long long r = blockIdx.y; r < rows; r += gridDim.y)
-    for (long long c = (long long)blockIdx.x * NT + threadIdx.x; c < cols;
-         c += (long long)gridDim.x * NT)
-      out[r * cols + c] = c < n ? p[r * ld + c] : (T)0.0f;
+struct Pad {
+  const T *p;
+  long long ld, rows, n, cols;
+  T *out;
+};
+template <typename T>
+__global__ __launch_bounds__(NT) void k_pad(Pad<T> x, Pad<T> w) {
+  constexpr int E = 16 / (int)sizeof(T);
+  const long long nx = x.rows * (x.cols / E), nw = w.rows * (w.cols / E);
+  for (long long i = (long long)blockIdx.x * NT + threadIdx.x; i < nx + nw;
+       i += (long long)gridDim.x * NT) {
+    const Pad<T> &m = i < nx ? x : w;
+    const long long q = i < nx ? i : i - nx, groups = m.cols / E;
+    const long long r = q / groups, c = (q - r * groups) * E;
+    alignas(16) T v[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) v[e] = c + e < m.n ? m.p[r * m.ld + c + e] : (T)0.0f;
+    *reinterpret_cast<int4v *>(m.out + r * m.cols + c) = *reinterpret_cast<const int4v *>(v);
+  }
 }
 
 __device__ __forceinline__ float wave_sum_f(float v) {
@@ -724,38 +775,47 @@ __device__ __forceinline__ float wave_sum_f(float v) {
   return v;
 }
 
-// The log of the sum of exponentials of rows r0 .. r0 + 15 from their parts'
-// maxima and sums, by a workgroup of 16 threads a row, to s_lse.
+// The log of the sum of exponentials of rows r0 .. r0 + ROWS - 1 from their
+// parts' maxima and sums, by a workgroup, to s_lse.
+template <int ROWS>
 __device__ __forceinline__ void rows_lse(const float2 *__restrict__ part, int parts,
                                          long long rows, long long r0, float *s_lse) {
+  constexpr int SLICES = NT / ROWS;
   __shared__ float2 s_part[NT];
-  const int row = threadIdx.x % 16, slice = threadIdx.x / 16;
+  const int row = threadIdx.x % ROWS, slice = threadIdx.x / ROWS;
   float m = -INFINITY, s = 0.0f;
   if (r0 + row < rows) {
 #pragma unroll 4
-    for (int i = slice; i < parts; i += NT / 16) {
+    for (int i = slice; i < parts; i += SLICES) {
       const float2 v = part[(long long)i * rows + r0 + row];
       join(m, s, v.x, v.y);
     }
   }
+  // a wavefront's slices of a row, then the wavefronts'
+#pragma unroll
+  for (int x = ROWS; x < WAVE; x <<= 1) {
+    const float m2 = __shfl_xor(m, x), s2 = __shfl_xor(s, x);
+    join(m, s, m2, s2);
+  }
   s_part[threadIdx.x] = make_float2(m, s);
   __syncthreads();
   if (slice == 0) {
-    for (int i = 1; i < NT / 16; ++i) join(m, s, s_part[i * 16 + row].x, s_part[i * 16 + row].y);
+    for (int i = 1; i < NWAVES; ++i) join(m, s, s_part[i * WAVE + row].x, s_part[i * WAVE + row].y);
     // (a row of infinities: the sum, or none of it, is what is left)
     s_lse[row] = shift_of(m) + logf(s);
   }
   __syncthreads();
 }
 
+template <int ROWS>
 __global__ __launch_bounds__(NT) void k_loss(const float2 *__restrict__ part, int parts,
                                              long long rows, const int32_t *__restrict__ target,
                                              long long words, const float *__restrict__ hit,
                                              float *__restrict__ loss, float *__restrict__ lse) {
-  __shared__ float s_lse[16];
-  const long long r0 = (long long)blockIdx.x * 16, r = r0 + threadIdx.x;
-  rows_lse(part, parts, rows, r0, s_lse);
-  if (threadIdx.x >= 16 || r >= rows) return;
+  __shared__ float s_lse[ROWS];
+  const long long r0 = (long long)blockIdx.x * ROWS, r = r0 + threadIdx.x;
+  rows_lse<ROWS>(part, parts, rows, r0, s_lse);
+  if (threadIdx.x >= ROWS || r >= rows) return;
   const float l = s_lse[threadIdx.x];
   lse[r] = l;
   const int32_t t = target[r];
@@ -763,15 +823,16 @@ __global__ __launch_bounds__(NT) void k_loss(const float2 *__restrict__ part, in
 }
 
 // Scores to log-probabilities, in place.
+template <int ROWS>
 __global__ __launch_bounds__(NT) void k_normalise(const float2 *__restrict__ part, int parts,
                                                   long long rows, long long cols,
                                                   float *__restrict__ z) {
-  __shared__ float s_lse[16];
-  const long long r0 = (long long)blockIdx.x * 16;
-  rows_lse(part, parts, rows, r0, s_lse);
-  const int n = rows - r0 < 16 ? (int)(rows - r0) : 16;
-  for (int r = threadIdx.x / WAVE; r < n; r += NWAVES)
-    for (long long c = threadIdx.x % WAVE; c < cols; c += WAVE) z[(r0 + r) * cols + c] -= s_lse[r];
+  __shared__ float s_lse[ROWS];
+  const long long r0 = (long long)blockIdx.x * ROWS;
+  rows_lse<ROWS>(part, parts, rows, r0, s_lse);
+  const int n = rows - r0 < ROWS ? (int)(rows - r0) : ROWS;
+  for (int r = 0; r < n; ++r)
+    for (long long c = threadIdx.x; c < cols; c += NT) z[(r0 + r) * cols + c] -= s_lse[r];
 }
 
 // The power of two that brings the largest |gradient| to [2^13, 2^14): 16-bit
@@ -784,25 +845,36 @@ __device__ __forceinline__ float scale_of(uint32_t bits) {
   return __uint_as_float((uint32_t)(k < 1 ? 1 : k > 254 ? 254 : k) << 23);
 }
 
-__global__ void k_clear_max(uint32_t *mx) { *mx = 0; }
-__global__ void k_scale(const uint32_t *mx, float *scale) { *scale = scale_of(*mx); }
-
-__global__ __launch_bounds__(NT) void k_max_abs(const float *__restrict__ p,
-                                                const int32_t *__restrict__ target, long long n,
-                                                uint32_t *__restrict__ mx) {
-  float m = 0.0f;
-  for (long long i = (long long)blockIdx.x * NT + threadIdx.x; i < n;
-       i += (long long)gridDim.x * NT)
-    if (target[i] >= 0) m = fmaxf(m, fabsf(p[i]));
+__device__ __forceinline__ float block_max(float m) {
+  __shared__ float s_max[16];
 #pragma unroll
   for (int x = 1; x < WAVE; x <<= 1) m = fmaxf(m, __shfl_xor(m, x));
-  if (__lane_id() == 0) atomicMax(mx, __float_as_uint(m));
+  if (__lane_id() == 0) s_max[threadIdx.x / WAVE] = m;
+  __syncthreads();
+  m = 0.0f;
+  for (int i = 0; i < (int)(blockDim.x / WAVE); ++i) m = fmaxf(m, s_max[i]);
+  return m;
 }
 
-// Emissions: the sum of each row's gradient, and the largest of the sums and
-// the gradients (mx not null).
-__global__ __launch_bounds__(NT) void k_row_sums(const float *__restrict__ grad, long long rows,
-                                                 long long cols, uint32_t *__restrict__ mx) {
+// The largest |p[i]| of rows with a word (p null: 1): one workgroup, the power
+// of two for it; several, each its own (then once more over theirs).
+__global__ __launch_bounds__(1024) void k_scale(const float *__restrict__ p,
+                                                const int32_t *__restrict__ target, long long n,
+                                                float *__restrict__ out) {
+  float m = p ? 0.0f : 1.0f;
+  if (p)
+    for (long long i = (long long)blockIdx.x * 1024 + threadIdx.x; i < n;
+         i += (long long)gridDim.x * 1024)
+      if (!target || target[i] >= 0) m = fmaxf(m, fabsf(p[i]));
+  m = block_max(m);
+  if (threadIdx.x == 0) out[blockIdx.x] = gridDim.x > 1 ? m : scale_of(__float_as_uint(m));
+}
+
+// Emissions: for each workgroup the largest of its rows' gradients and of their
+// sums.
+__global__ __launch_bounds__(NT) void k_emission_max(const float *__restrict__ grad,
+                                                     long long rows, long long cols,
+                                                     float *__restrict__ out) {
   const int lane = threadIdx.x & (WAVE - 1);
   float m = 0.0f;
   for (long long r = (long long)blockIdx.x * NWAVES + threadIdx.x / WAVE; r < rows;
@@ -815,49 +887,68 @@ __global__ __launch_bounds__(NT) void k_row_sums(const float *__restrict__ grad,
     }
     m = fmaxf(m, fabsf(wave_sum_f(s)));
   }
-#pragma unroll
-  for (int x = 1; x < WAVE; x <<= 1) m = fmaxf(m, __shfl_xor(m, x));
-  if (lane == 0) atomicMax(mx, __float_as_uint(m));
+  m = block_max(m);
+  if (threadIdx.x == 0) out[blockIdx.x] = m;
 }
 
-// dS = grad - exp(weight) sum(grad), a wavefront a row, zeros up to Rp x Cp.
-template <typename T>
+// dS = grad - exp(weight) sum(grad), LANES lanes a row, zeros up to Cp columns.
+template <typename T, int LANES>
 __global__ __launch_bounds__(NT) void k_emission_ds(const float *__restrict__ weight,
                                                     const float *__restrict__ grad,
                                                     long long rows, long long cols,
                                                     const float *__restrict__ scale,
-                                                    T *__restrict__ out, long long Rp,
-                                                    long long Cp) {
-  const int lane = threadIdx.x & (WAVE - 1);
-  const long long r = (long long)blockIdx.x * NWAVES + threadIdx.x / WAVE;
-  if (r >= Rp) return;
+                                                    T *__restrict__ out, long long Cp) {
+  constexpr int E = 16 / (int)sizeof(T);
+  const int lane = threadIdx.x % LANES;
+  const long long r = (long long)blockIdx.x * (NT / LANES) + threadIdx.x / LANES;
+  if (r >= rows) return;  // (a row's lanes together)
   const float k = scale ? *scale : 1.0f;
+  const float *g = grad + r * cols, *w = weight + r * cols;
   float s = 0.0f;
-  if (r < rows)
-    for (long long c = lane; c < cols; c += WAVE) s += grad[r * cols + c];
-  s = wave_sum_f(s);
-  for (long long c = lane; c < Cp; c += WAVE) {
-    float v = 0.0f;
-    if (r < rows && c < cols)
-      v = k * (grad[r * cols + c] - __expf(weight[r * cols + c]) * s);
-    out[r * Cp + c] = (T)v;
+#pragma unroll 4
+  for (long long c = lane; c < cols; c += LANES) s += g[c];
+#pragma unroll
+  for (int x = 1; x < LANES; x <<= 1) s += __shfl_xor(s, x);
+  for (long long c = (long long)lane * E; c < Cp; c += LANES * E) {
+    alignas(16) T v[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+      v[e] = (T)(c + e < cols ? k * (g[c + e] - exp_less(w[c + e], 0.0f) * s) : 0.0f);
+    *reinterpret_cast<int4v *>(out + r * Cp + c) = *reinterpret_cast<const int4v *>(v);
   }
 }
 
-// Sums of the splits, in their order, to results.
+// Sums of the splits to results: 64 groups of four columns a workgroup, each
+// split by its four wavefronts in turn, added in a fixed order.  (Rows of
+// `sums` are padded to whole groups.)
 template <typename T>
 __global__ __launch_bounds__(NT) void k_finish(const float *__restrict__ sums, int splits,
                                                long long rows, long long cols,
                                                const float *__restrict__ scale,
                                                T *__restrict__ out, long long ldo) {
+  __shared__ float4v s_sum[NWAVES][WAVE];
+  const int lane = threadIdx.x & (WAVE - 1), w = threadIdx.x / WAVE;
   const float back = scale ? 1.0f / *scale : 1.0f;
-  const long long n = rows * cols;
-  for (long long i = (long long)blockIdx.x * NT + threadIdx.x; i < n;
-       i += (long long)gridDim.x * NT) {
-    float v = 0.0f;
-    for (int s = 0; s < splits; ++s) v += sums[s * n + i];
-    const long long r = i / cols;
-    out[r * ldo + (i - r * cols)] = (T)(v * back);
+  const long long groups = (cols + 3) / 4, all = rows * groups;
+  for (long long i0 = (long long)blockIdx.x * WAVE; i0 < all; i0 += (long long)gridDim.x * WAVE) {
+    const long long i = i0 + lane;
+    float4v v = {0, 0, 0, 0};
+    if (i < all) {
+#pragma unroll 8
+      for (int s = w; s < splits; s += NWAVES)
+        v += reinterpret_cast<const float4v *>(sums)[s * all + i];
+    }
+    s_sum[w][lane] = v;
+    __syncthreads();
+    if (w == 0 && i < all) {
+#pragma unroll
+      for (int q = 1; q < NWAVES; ++q) v += s_sum[q][lane];
+      const long long r = i / groups, c = (i - r * groups) * 4;
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (c + e < cols) out[r * ldo + c + e] = (T)(v[e] * back);
+    }
+    __syncthreads();
   }
 }
 
@@ -890,13 +981,47 @@ struct Tile {
 };
 constexpr Tile TILES[3] = {{256, 256, 4}, {128, 128, 2}, {64, 64, 2}};
 
-// The largest tile that still gives most CUs one.
-int tile_for(long long M, long long N) {
-  for (int i = 0; i < 2; ++i)
-    if (((M + TILES[i].bm - 1) / TILES[i].bm) * ((N + TILES[i].bn - 1) / TILES[i].bn) >=
-        CUS * 3 / 4)
-      return i;
-  return 2;
+// How a product is cut: the tile, and the parts of its sum.
+struct Cut {
+  int tile, splits, steps;
+};
+
+// The cut that takes least, by a model in microseconds fitted to products of
+// 0.5 to 35 Gflop (2000 x 4000 over 512, tiles of 256, 128 and 64: measured 19, 14
+// and 19; 1600 x 26,000 over 256: 42, 47, 55; 64 x 10,000 over 512: 17, 11 and 7;
+// 4096 x 4096 over 1024: 32, 44, 59).  A step of the largest tile takes a CU 1.54
+// (256 of the products at once); 512 of the next take 1.2, 0.85 where a CU has
+// one alone; of the smallest 256 take 0.22, one alone 0.5.  In float32 the matrix
+// cores take longer than that.  Splitting costs a launch and the sums' way to
+// memory and back.
+template <typename T>
+Cut cut_for(long long M, long long N, long long K, bool may_split) {
+  const long long all = (K + k_step<T>() - 1) / k_step<T>();
+  const bool wide = sizeof(T) == 4;
+  Cut best{0, 1, (int)(all < 1 ? 1 : all)};
+  double least = 1e30;
+  for (int tile = 0; tile < 3; ++tile) {
+    const double tiles = (double)((M + TILES[tile].bm - 1) / TILES[tile].bm) *
+                         (double)((N + TILES[tile].bn - 1) / TILES[tile].bn);
+    for (long long p = 1; p == 1 || (may_split && p <= 256 && p <= all / 2); p += 1 + p / 16) {
+      const double per = (double)((all + p - 1) / p), q = ceil(tiles * p / CUS);
+      double us;
+      if (tile == 0)
+        us = 1.5 + q * (per * (wide ? 7.0 : 1.54) + 5.5);
+      else if (tile == 1)
+        us = 4 + per * (q <= 1 ? (wide ? 1.75 : 0.85) : ceil(q / 2) * (wide ? 3.5 : 1.2));
+      else
+        us = 3.5 + per * (wide ? 0.44 * q : q <= 1 ? 0.5 : fmax(0.5, 0.218 * q));
+      if (p > 1) us += 3.5 + (double)p * M * N * 8 / 4e6;
+      if (us < least) {
+        least = us;
+        best = {tile, 1, (int)((all + p - 1) / p)};
+        best.splits = all ? (int)((all + best.steps - 1) / best.steps) : 1;
+        if (best.steps < 1) best.steps = 1;
+      }
+    }
+  }
+  return best;
 }
 
 template <typename T, int LAYOUT, int EPI>
@@ -941,12 +1066,17 @@ Laid<T> lay(const Mat &m, Bump &b) {
   T *p = b.take<T>(m.rows * cols);
   return {{p, cols, m.rows, cols}, p, cols};
 }
+// The copies there are, in one launch.
 template <typename T>
-hipError_t fill(const Laid<T> &l, const Mat &m, hipStream_t s) {
-  if (l.o.p == m.data || !l.copy) return hipSuccess;
-  const dim3 grid(blocks_for(l.cols, NT), blocks_for(m.rows, 1, 32768));
-  k_pad<T><<<grid, NT, 0, s>>>(static_cast<const T *>(m.data), m.stride, m.rows, m.cols, l.copy,
-                               l.cols);
+hipError_t fill(const Laid<T> *lx, const Mat &x, const Laid<T> *lw, const Mat &w, hipStream_t s) {
+  Pad<T> px{}, pw{};
+  if (lx && lx->copy)
+    px = {static_cast<const T *>(x.data), x.stride, x.rows, x.cols, lx->cols, lx->copy};
+  if (lw && lw->copy)
+    pw = {static_cast<const T *>(w.data), w.stride, w.rows, w.cols, lw->cols, lw->copy};
+  const long long groups = (px.rows * px.cols + pw.rows * pw.cols) / (16 / (int)sizeof(T));
+  if (!groups) return hipSuccess;
+  k_pad<T><<<blocks_for(groups, NT), NT, 0, s>>>(px, pw);
   return hipGetLastError();
 }
 
@@ -956,34 +1086,17 @@ int wide(const Mat &m) {
   return (uintptr_t)m.data % (4 * sizeof(T)) == 0 && m.stride % 4 == 0;
 }
 
-// out = A B^T with the sum split where the tiles alone are too few.
+// out = A B^T, its sum in parts where that takes less.
 template <typename T, int LAYOUT>
 struct SplitProduct {
-  int tile, splits;
-  long long steps;
+  Cut cut;
   float *sums;
 
   void plan(long long M, long long N, long long K, Bump &b) {
-    splits = 1;
-    steps = 1;
+    cut = {0, 1, 1};
     if (M == 0 || N == 0) return;
-    tile = tile_for(M, N);
-    const long long tiles =
-        ((M + TILES[tile].bm - 1) / TILES[tile].bm) * ((N + TILES[tile].bn - 1) / TILES[tile].bn);
-    const long long all = (K + k_step<T>() - 1) / k_step<T>();
-    // What takes least, in steps: the rounds of all CUs, where a smaller tile
-    // leaves a CU room for more, and four steps more for what splitting adds
-    // (244 tiles of 256 x 256, 250 steps: one part 0.41 ms, two 0.44 and
-    // 0.05 to add them up).
-    const long long slots = tile == 0 ? CUS : 2 * CUS;
-    long long best = INT64_MAX;
-    for (long long p = 1; p <= 256 && (p == 1 || p <= all / 4); ++p) {
-      const long long per = (all + p - 1) / p;
-      const long long cost = (tiles * p + slots - 1) / slots * (per + 2) + (p > 1 ? 4 + p / 8 : 0);
-      if (cost < best) best = cost, steps = per;
-    }
-    splits = (int)((all + steps - 1) / steps);
-    sums = splits > 1 ? b.take<float>(splits * M * N) : nullptr;
+    cut = cut_for<T>(M, N, K, true);
+    sums = cut.splits > 1 ? b.take<float>(cut.splits * M * up(N, 4)) : nullptr;
   }
   hipError_t run(Operand A, Operand B, long long M, long long N, long long K, const float *scale,
                  const Mat &out, hipStream_t s) const {
@@ -994,35 +1107,39 @@ struct SplitProduct {
     g.M = M;
     g.N = N;
     g.K = K;
-    g.splits = splits;
-    g.steps = (int)steps;
-    if (splits == 1) {
+    g.splits = cut.splits;
+    g.steps = cut.steps;
+    if (cut.splits == 1) {
       g.out = out.data;
       g.ldo = out.stride;
       g.wide = wide<T>(out);
       g.scale = scale;
-      return product<T, LAYOUT, EPI_RESULT>(g, tile, s);
+      return product<T, LAYOUT, EPI_RESULT>(g, cut.tile, s);
     }
     g.out = sums;
-    g.ldo = N;
-    g.wide = N % 4 == 0;
-    TRY((product<T, LAYOUT, EPI_SUM>(g, tile, s)));
-    k_finish<T><<<blocks_for(M * N, NT), NT, 0, s>>>(sums, splits, M, N, scale,
-                                                   static_cast<T *>(out.data), out.stride);
+    g.ldo = up(N, 4);
+    g.wide = 1;
+    TRY((product<T, LAYOUT, EPI_SUM>(g, cut.tile, s)));
+    k_finish<T><<<blocks_for(M * up(N, 4), 4 * WAVE), NT, 0, s>>>(
+        sums, cut.splits, M, N, scale, static_cast<T *>(out.data), out.stride);
     return hipGetLastError();
   }
 };
+
+// Rows that a workgroup of the kernels over rows takes: 16 where that leaves
+// enough workgroups (a row each otherwise: 165 rows of 869 columns 19 us by 16).
+bool many_rows(long long N) { return N >= 4096; }
 
 template <typename T>
 hipError_t emission_as(const Mat &x, const Mat &w, float *weight, Bump &b, hipStream_t s) {
   const long long N = x.rows, C = w.rows;
   const Laid<T> lx = lay<T>(x, b), lw = lay<T>(w, b);
-  const int tile = tile_for(N, C);
-  const int parts = (int)((C + TILES[tile].bn - 1) / TILES[tile].bn) * TILES[tile].wn;
-  float2 *part = b.take<float2>((long long)N * parts);
+  const bool whole = C <= 128;  // a tile takes whole rows
+  const Cut cut = cut_for<T>(N, C, lx.cols, false);
+  const int parts = (int)((C + TILES[cut.tile].bn - 1) / TILES[cut.tile].bn) * TILES[cut.tile].wn;
+  float2 *part = b.take<float2>(whole ? 1 : N * parts);
   if (!b.base) return hipSuccess;
-  TRY(fill(lx, x, s));
-  TRY(fill(lw, w, s));
+  TRY(fill(&lx, x, &lw, w, s));
   Product g{};
   g.A = lx.o;
   g.B = lw.o;
@@ -1033,9 +1150,21 @@ hipError_t emission_as(const Mat &x, const Mat &w, float *weight, Bump &b, hipSt
   g.steps = INT32_MAX;
   g.out = weight;
   g.ldo = C;
+  if (whole) {
+    g.tiles_m = (int)((N + 31) / 32);
+    g.tiles_n = 1;
+    if (C <= 64)
+      k_product<T, ROWS_ROWS, 32, 64, 2, 1, EPI_LOG><<<g.tiles_m, 2 * WAVE, 0, s>>>(g);
+    else
+      k_product<T, ROWS_ROWS, 32, 128, 2, 1, EPI_LOG><<<g.tiles_m, 2 * WAVE, 0, s>>>(g);
+    return hipGetLastError();
+  }
   g.part = part;
-  TRY((product<T, ROWS_ROWS, EPI_SCORE>(g, tile, s)));
-  k_normalise<<<(unsigned)((N + 15) / 16), NT, 0, s>>>(part, parts, N, C, weight);
+  TRY((product<T, ROWS_ROWS, EPI_SCORE>(g, cut.tile, s)));
+  if (many_rows(N))
+    k_normalise<16><<<(unsigned)((N + 15) / 16), NT, 0, s>>>(part, parts, N, C, weight);
+  else
+    k_normalise<1><<<(unsigned)N, NT, 0, s>>>(part, parts, N, C, weight);
   return hipGetLastError();
 }
 
@@ -1043,37 +1172,38 @@ template <typename T>
 hipError_t emission_grads_as(const Mat &x, const Mat &w, const float *weight, const float *grad,
                              const Mat *gx, const Mat *gw, Bump &b, hipStream_t s) {
   const long long N = x.rows, C = w.rows, H = x.cols;
-  const long long Np = up(N, 64), Cp = up(C, 64);
+  const long long Cp = up(C, 64);
   if (N == 0) {  // nothing to sum over
     if (b.base && gw && C * H)
-      k_finish<T><<<blocks_for(C * H, NT), NT, 0, s>>>(nullptr, 0, C, H, nullptr,
+      k_finish<T><<<blocks_for(C * up(H, 4), 4 * WAVE), NT, 0, s>>>(nullptr, 0, C, H, nullptr,
                                                      static_cast<T *>(gw->data), gw->stride);
     b.take<char>(1);
     return hipGetLastError();
   }
   const Laid<T> lx = lay<T>(x, b), lw = lay<T>(w, b);
-  T *ds = b.take<T>(Np * Cp);
-  uint32_t *mx = b.take<uint32_t>(1);
-  float *scale = b.take<float>(1);
+  T *ds = b.take<T>(N * Cp);
+  constexpr int GROUPS = 256;
+  float *most = b.take<float>(GROUPS), *scale = b.take<float>(1);
   SplitProduct<T, ROWS_COLS> px{};
   SplitProduct<T, COLS_COLS> pw{};
   if (gx) px.plan(N, H, Cp, b);
-  if (gw) pw.plan(C, H, Np, b);
+  if (gw) pw.plan(C, H, N, b);
   if (!b.base) return hipSuccess;
-  if (gw) TRY(fill(lx, x, s));
-  if (gx) TRY(fill(lw, w, s));
-  const bool scaled = sizeof(T) == 2 && std::is_same<T, f16>::value;
-  if (scaled) {
-    k_clear_max<<<1, 1, 0, s>>>(mx);
-    k_row_sums<<<blocks_for(N, NWAVES, 2048), NT, 0, s>>>(grad, N, C, mx);
-    k_scale<<<1, 1, 0, s>>>(mx, scale);
+  TRY(fill(gw ? &lx : nullptr, x, gx ? &lw : nullptr, w, s));
+  if (std::is_same<T, f16>::value) {
+    const unsigned n = blocks_for(N, NWAVES, GROUPS);
+    k_emission_max<<<n, NT, 0, s>>>(grad, N, C, most);
+    k_scale<<<1, 1024, 0, s>>>(most, nullptr, n, scale);
   } else {
     scale = nullptr;
   }
-  k_emission_ds<T><<<(unsigned)((Np + NWAVES - 1) / NWAVES), NT, 0, s>>>(weight, grad, N, C, scale,
-                                                                        ds, Np, Cp);
+  // (16 lanes a row where a row is short)
+  if (C <= 256)
+    k_emission_ds<T, 16><<<(unsigned)((N + 15) / 16), NT, 0, s>>>(weight, grad, N, C, scale, ds, Cp);
+  else
+    k_emission_ds<T, 64><<<(unsigned)((N + 3) / 4), NT, 0, s>>>(weight, grad, N, C, scale, ds, Cp);
   TRY(hipGetLastError());
-  if (gx) TRY(px.run({ds, Cp, N, Cp}, lw.columns(), N, H, C, scale, *gx, s));
+  if (gx) TRY(px.run({ds, Cp, N, Cp}, lw.columns(), N, H, Cp, scale, *gx, s));
   if (gw) TRY(pw.run({ds, Cp, Cp, N}, lx.columns(), C, H, N, scale, *gw, s));
   return hipSuccess;
 }
@@ -1083,13 +1213,12 @@ hipError_t loss_as(const Mat &x, const Mat &w, const int32_t *target, float *los
                    Bump &b, hipStream_t s) {
   const long long N = x.rows, V = w.rows;
   const Laid<T> lx = lay<T>(x, b), lw = lay<T>(w, b);
-  const int tile = tile_for(N, V);
+  const int tile = cut_for<T>(N, V, lx.cols, false).tile;
   const int parts = (int)((V + TILES[tile].bn - 1) / TILES[tile].bn) * TILES[tile].wn;
-  float2 *part = b.take<float2>((long long)N * parts);
+  float2 *part = b.take<float2>(N * parts);
   float *hit = b.take<float>(N);
   if (!b.base) return hipSuccess;
-  TRY(fill(lx, x, s));
-  TRY(fill(lw, w, s));
+  TRY(fill(&lx, x, &lw, w, s));
   Product g{};
   g.A = lx.o;
   g.B = lw.o;
@@ -1102,8 +1231,10 @@ hipError_t loss_as(const Mat &x, const Mat &w, const int32_t *target, float *los
   g.target = target;
   g.hit = hit;
   TRY((product<T, ROWS_ROWS, EPI_PART>(g, tile, s)));
-  k_loss<<<(unsigned)((N + 15) / 16), NT, 0, s>>>(part, parts, N, target, V, hit, loss,
-                                                            lse);
+  if (many_rows(N))
+    k_loss<16><<<(unsigned)((N + 15) / 16), NT, 0, s>>>(part, parts, N, target, V, hit, loss, lse);
+  else
+    k_loss<1><<<(unsigned)N, NT, 0, s>>>(part, parts, N, target, V, hit, loss, lse);
   return hipGetLastError();
 }
 
@@ -1130,50 +1261,47 @@ template <typename T>
 hipError_t loss_grads_as(const Mat &x, const Mat &w, const int32_t *target, const float *lse,
                          const float *grad, const Mat *gx, const Mat *gw, Bump &b,
                          hipStream_t s) {
-  const long long N = x.rows, V = w.rows, H = x.cols, Np = up(N, 64);
+  const long long N = x.rows, V = w.rows, H = x.cols;
   if (N == 0) {  // nothing to sum over
     if (b.base && gw && V * H)
-      k_finish<T><<<blocks_for(V * H, NT), NT, 0, s>>>(nullptr, 0, V, H, nullptr,
+      k_finish<T><<<blocks_for(V * up(H, 4), 4 * WAVE), NT, 0, s>>>(nullptr, 0, V, H, nullptr,
                                                      static_cast<T *>(gw->data), gw->stride);
     b.take<char>(1);
     return hipGetLastError();
   }
   const Laid<T> lx = lay<T>(x, b), lw = lay<T>(w, b);
-  const long long piece = piece_of(V, H, PIECE_BYTES / (Np * (long long)sizeof(T)));
+  const long long piece = piece_of(V, H, PIECE_BYTES / (N * (long long)sizeof(T)));
   const bool whole = piece == V;
   const long long Pp = up(piece, 64);
   T *ds = b.take<T>(N * (Pp + DS_GAP));
-  uint32_t *mx = b.take<uint32_t>(1);
-  float *scale = b.take<float>(1);
+  constexpr int GROUPS = 256;
+  float *most_g = b.take<float>(GROUPS), *scale = b.take<float>(1);
   SplitProduct<T, ROWS_COLS> px{};
   SplitProduct<T, COLS_COLS> pw{};
   float *sums = nullptr;
   if (gx && whole) px.plan(N, H, Pp, b);
-  if (gx && !whole) sums = b.take<float>(N * H);
+  if (gx && !whole) sums = b.take<float>(N * up(H, 4));
   const size_t mark = b.at;
   size_t most = mark;
   if (gw) {
     for (long long v0 = 0; v0 < V; v0 += piece) {
       b.at = mark;
-      pw.plan(V - v0 < piece ? V - v0 : piece, H, Np, b);
+      pw.plan(V - v0 < piece ? V - v0 : piece, H, N, b);
       most = b.at > most ? b.at : most;
     }
   }
   b.at = most;
   if (!b.base) return hipSuccess;
-  TRY(fill(lx, x, s));
-  TRY(fill(lw, w, s));
-  if (std::is_same<T, f16>::value && grad) {
-    k_clear_max<<<1, 1, 0, s>>>(mx);
-    k_max_abs<<<blocks_for(N, NT, 256), NT, 0, s>>>(grad, target, N, mx);
-    k_scale<<<1, 1, 0, s>>>(mx, scale);
-  } else if (std::is_same<T, f16>::value) {
-    k_clear_max<<<1, 1, 0, s>>>(mx);
-    k_scale<<<1, 1, 0, s>>>(mx, scale);
+  TRY(fill(&lx, x, &lw, w, s));
+  if (std::is_same<T, f16>::value) {
+    const bool one = !grad || N <= 65536;
+    if (!one) k_scale<<<GROUPS, 1024, 0, s>>>(grad, target, N, most_g);
+    k_scale<<<1, 1024, 0, s>>>(one ? grad : most_g, one ? target : nullptr, one ? N : GROUPS,
+                               scale);
+    TRY(hipGetLastError());
   } else {
     scale = nullptr;
   }
-  TRY(hipGetLastError());
   for (long long v0 = 0; v0 < V; v0 += piece) {
     const long long n = V - v0 < piece ? V - v0 : piece, np = up(n, 64);
     const Operand wp{static_cast<const T *>(lw.o.p) + v0 * lw.o.ld, lw.o.ld, n, lw.cols};
@@ -1195,31 +1323,31 @@ hipError_t loss_grads_as(const Mat &x, const Mat &w, const int32_t *target, cons
     g.grad = grad;
     g.scale = scale;
     g.Np = np;
-    TRY((product<T, ROWS_ROWS, EPI_DS>(g, tile_for(N, n), s)));
+    TRY((product<T, ROWS_ROWS, EPI_DS>(g, cut_for<T>(N, n, lx.cols, false).tile, s)));
     if (gx && whole) {
-      TRY(px.run({ds, np + DS_GAP, N, np}, wc, N, H, n, scale, *gx, s));
+      TRY(px.run({ds, np + DS_GAP, N, np}, wc, N, H, np, scale, *gx, s));
     } else if (gx) {
       Product q{};
       q.A = {ds, np + DS_GAP, N, np};
       q.B = wc;
       q.M = N;
       q.N = H;
-      q.K = n;
+      q.K = np;
       q.splits = 1;
       q.steps = INT32_MAX;
       if (v0 + n < V) {
         q.out = sums;
-        q.ldo = H;
-        q.wide = H % 4 == 0;
+        q.ldo = up(H, 4);
+        q.wide = 1;
         q.add = v0 > 0;
-        TRY((product<T, ROWS_COLS, EPI_SUM>(q, tile_for(N, H), s)));
+        TRY((product<T, ROWS_COLS, EPI_SUM>(q, cut_for<T>(N, H, np, false).tile, s)));
       } else {
         q.out = gx->data;
         q.ldo = gx->stride;
         q.wide = wide<T>(*gx);
         q.scale = scale;
         q.sums = sums;
-        TRY((product<T, ROWS_COLS, EPI_RESULT>(q, tile_for(N, H), s)));
+        TRY((product<T, ROWS_COLS, EPI_RESULT>(q, cut_for<T>(N, H, np, false).tile, s)));
       }
     }
     if (gw) {
@@ -1227,7 +1355,7 @@ hipError_t loss_grads_as(const Mat &x, const Mat &w, const int32_t *target, cons
       out.data = static_cast<T *>(out.data) + v0 * out.stride;
       out.rows = n;
       b.at = mark;
-      pw.plan(n, H, Np, b);
+      pw.plan(n, H, N, b);
       TRY(pw.run({ds, np + DS_GAP, np, N}, lx.columns(), n, H, N, scale, out, s));
     }
   }
