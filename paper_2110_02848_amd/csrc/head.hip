@@ -258,7 +258,7 @@ struct Product {
   long long Np;          // dS: columns to write, zeros past N
   int add;               // sums: add to what is there
   const float *sums;     // [M, N rounded up to four] or null
-  int wide;              // results: `out` and its rows are aligned to four
+  int wide;              // results: `out` and its rows are aligned to four (2: to 16 bytes)
 };
 
 enum Epilogue {
@@ -315,16 +315,17 @@ __device__ __forceinline__ void epilogue(const Product &g, float4v (&acc)[FM][FN
                                          long long n0, int tn, int wm, int wn, int split,
                                          int lane);
 
-// Tiles of BM x BN where there are too few large ones: two buffers, the next
-// step's loads under way while one step's fragments are multiplied; several
-// workgroups a CU fill each other's gaps (three or four buffers, which leave
-// room for fewer, took 5 to 60 % longer).
-template <typename T, int LAYOUT, int BM, int BN, int WM, int WN, int EPI>
+// Tiles of BM x BN where there are too few large ones: STAGES buffers, the loads
+// of the STAGES - 1 next steps under way while one step's fragments are
+// multiplied.  Two where several workgroups a CU fill each other's gaps (three
+// or four, which leave room for fewer, took 5 to 60 % longer); four for the
+// narrow tiles of emissions, whose steps are nothing but waiting for loads.
+template <typename T, int LAYOUT, int BM, int BN, int WM, int WN, int STAGES, int EPI>
 __global__ __launch_bounds__(WM *WN *WAVE) void k_product(Product g) {
   constexpr int NWV = WM * WN, FM = BM / WM / 16, FN = BN / WN / 16;
   using A = TileA<T, LAYOUT, BM, NWV, Rows<BM, BM>>;
   using B = TileB<T, LAYOUT, BN, NWV, Spread<16 / (int)sizeof(T), FN, FN>, Rows<BN, BN>>;
-  __shared__ __align__(1024) char s_lds[2][A::BYTES + B::BYTES];
+  __shared__ __align__(1024) char s_lds[STAGES][A::BYTES + B::BYTES];
   const int lane = threadIdx.x & (WAVE - 1);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
   const int wm = wave / WN, wn = wave % WN;
@@ -343,9 +344,11 @@ __global__ __launch_bounds__(WM *WN *WAVE) void k_product(Product g) {
   const int all = (int)((g.K + k_step<T>() - 1) / k_step<T>());
   const int first = split * g.steps;
   const int end = all - first < g.steps ? all : first + g.steps;
-  const auto fetch = [&](int buffer, int t) {
-    const uint32_t to = lds + buffer * (A::BYTES + B::BYTES);
-    const int4v ba = A::step(g.A, pa, na, t), bb = B::step(g.B, pb, nb, t);
+  // (past the end: of empty buffers, so that there are always as many loads)
+  const auto fetch = [&](int stage, int t) {
+    const uint32_t to = lds + stage * (A::BYTES + B::BYTES);
+    const int4v ba = A::step(g.A, pa, t < end ? na : 0, t);
+    const int4v bb = B::step(g.B, pb, t < end ? nb : 0, t);
 #pragma unroll
     for (int i = 0; i < A::LOADS; ++i) ta.fetch(i, to, ba, wave);
 #pragma unroll
@@ -357,14 +360,16 @@ __global__ __launch_bounds__(WM *WN *WAVE) void k_product(Product g) {
   for (int i = 0; i < FM; ++i)
 #pragma unroll
     for (int j = 0; j < FN; ++j) acc[i][j] = float4v{0, 0, 0, 0};
-  if (first < end) fetch(0, first);
+#pragma unroll
+  for (int s = 0; s < STAGES - 1; ++s) fetch(s, first + s);
   int cur = 0;
-  for (int t = first; t < end; ++t, cur ^= 1) {
-    // step t has landed, and no one reads the other buffer
-    wait_loads<0>();
+  for (int t = first; t < end; ++t) {
+    // step t has landed, and no one reads the buffer of the step before
+    wait_loads<(STAGES - 2) * (A::LOADS + B::LOADS)>();
     __syncthreads();
-    if (t + 1 < end) fetch(cur ^ 1, t + 1);
+    fetch(cur ? cur - 1 : STAGES - 1, t + STAGES - 1);
     const char *sa = s_lds[cur], *sb = sa + A::BYTES;
+    cur = cur == STAGES - 1 ? 0 : cur + 1;
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
       Frag<T> fa[FM], fb[FN];
@@ -378,6 +383,7 @@ __global__ __launch_bounds__(WM *WN *WAVE) void k_product(Product g) {
         for (int j = 0; j < FN; ++j) acc[i][j] = mac(fb[j], fa[i], acc[i][j]);
     }
   }
+  wait_loads<0>();  // (the empty ones, too: LDS is used for other things now, or by others)
   if constexpr (EPI == EPI_LOG) {
     // rows of log-probabilities, put together in LDS: the rows of a tile lie
     // side by side in memory (ldo is N)
@@ -410,6 +416,40 @@ __global__ __launch_bounds__(WM *WN *WAVE) void k_product(Product g) {
     const int n = (int)(g.M - m0 < BM ? g.M - m0 : BM) * cols;
     float *out = static_cast<float *>(g.out) + m0 * cols;
     for (int i = threadIdx.x; i < n; i += NWV * WAVE) out[i] = s[i];
+  } else if (EPI == EPI_RESULT && g.wide == 2 && !g.sums && n0 + BN <= g.N) {
+    // results by way of LDS, so that whole rows of the tile are written
+    constexpr int E = 16 / (int)sizeof(T), PITCH = BN + E, CHUNKS = BN / E;
+    constexpr int ROWS = (int)sizeof(s_lds) / (PITCH * (int)sizeof(T)) < BM ? BM / 2 : BM;
+    static_assert(ROWS * PITCH * (int)sizeof(T) <= (int)sizeof(s_lds), "room for the rows");
+    const float back = g.scale ? 1.0f / *g.scale : 1.0f;
+    T *s = reinterpret_cast<T *>(s_lds);
+#pragma unroll
+    for (int part = 0; part < BM / ROWS; ++part) {
+      __syncthreads();  // no one reads operands (the part before) any more
+#pragma unroll
+      for (int i = 0; i < FM; ++i) {
+        const int r = (wm * FM + i) * 16 + (lane & 15) - part * ROWS;
+        if (r >= 0 && r < ROWS) {
+#pragma unroll
+          for (int j = 0; j < FN; ++j) {
+            const int c = wn * FN * 16 + (LAYOUT == ROWS_ROWS
+                                              ? Spread<E, FN, FN>::column(lane >> 4, 4 * j)
+                                              : j * 16 + (lane >> 4) * 4);
+            typedef __attribute__((ext_vector_type(4))) T T4;
+            *reinterpret_cast<T4 *>(s + r * PITCH + c) =
+                T4{(T)(acc[i][j][0] * back), (T)(acc[i][j][1] * back), (T)(acc[i][j][2] * back),
+                   (T)(acc[i][j][3] * back)};
+          }
+        }
+      }
+      __syncthreads();
+      for (int q = threadIdx.x; q < ROWS * CHUNKS; q += NWV * WAVE) {
+        const long long m = m0 + part * ROWS + q / CHUNKS;
+        if (m < g.M)
+          *reinterpret_cast<int4v *>(static_cast<T *>(g.out) + m * g.ldo + n0 + q % CHUNKS * E) =
+              *reinterpret_cast<const int4v *>(s + q / CHUNKS * PITCH + q % CHUNKS * E);
+      }
+    }
   } else {
     epilogue<T, LAYOUT, WN, FM, FN, EPI>(g, acc, m0, n0, tn, wm, wn, split, lane);
   }
@@ -763,8 +803,13 @@ __global__ __launch_bounds__(NT) void k_pad(Pad<T> x, Pad<T> w) {
     const long long q = i < nx ? i : i - nx, groups = m.cols / E;
     const long long r = q / groups, c = (q - r * groups) * E;
     alignas(16) T v[E];
+    const T *p = m.p + r * m.ld + c;
+    if (c + E <= m.n) {
+      __builtin_memcpy(v, p, 16);  // (one load, wherever it lies)
+    } else {
 #pragma unroll
-    for (int e = 0; e < E; ++e) v[e] = c + e < m.n ? m.p[r * m.ld + c + e] : (T)0.0f;
+      for (int e = 0; e < E; ++e) v[e] = c + e < m.n ? p[e] : (T)0.0f;
+    }
     *reinterpret_cast<int4v *>(m.out + r * m.cols + c) = *reinterpret_cast<const int4v *>(v);
   }
 }
@@ -891,30 +936,71 @@ __global__ __launch_bounds__(NT) void k_emission_max(const float *__restrict__ g
   if (threadIdx.x == 0) out[blockIdx.x] = m;
 }
 
-// dS = grad - exp(weight) sum(grad), LANES lanes a row, zeros up to Cp columns.
-template <typename T, int LANES>
+// dS = grad - exp(weight) sum(grad), zeros up to Cp columns; a wavefront a row.
+template <typename T>
 __global__ __launch_bounds__(NT) void k_emission_ds(const float *__restrict__ weight,
                                                     const float *__restrict__ grad,
                                                     long long rows, long long cols,
                                                     const float *__restrict__ scale,
                                                     T *__restrict__ out, long long Cp) {
   constexpr int E = 16 / (int)sizeof(T);
-  const int lane = threadIdx.x % LANES;
-  const long long r = (long long)blockIdx.x * (NT / LANES) + threadIdx.x / LANES;
+  const int lane = threadIdx.x & (WAVE - 1);
+  const long long r = (long long)blockIdx.x * NWAVES + threadIdx.x / WAVE;
   if (r >= rows) return;  // (a row's lanes together)
   const float k = scale ? *scale : 1.0f;
   const float *g = grad + r * cols, *w = weight + r * cols;
   float s = 0.0f;
 #pragma unroll 4
-  for (long long c = lane; c < cols; c += LANES) s += g[c];
-#pragma unroll
-  for (int x = 1; x < LANES; x <<= 1) s += __shfl_xor(s, x);
-  for (long long c = (long long)lane * E; c < Cp; c += LANES * E) {
+  for (long long c = lane; c < cols; c += WAVE) s += g[c];
+  s = wave_sum_f(s);
+  for (long long c = (long long)lane * E; c < Cp; c += WAVE * E) {
     alignas(16) T v[E];
 #pragma unroll
     for (int e = 0; e < E; ++e)
       v[e] = (T)(c + e < cols ? k * (g[c + e] - exp_less(w[c + e], 0.0f) * s) : 0.0f);
     *reinterpret_cast<int4v *>(out + r * Cp + c) = *reinterpret_cast<const int4v *>(v);
+  }
+}
+
+// The same where rows are short (cols <= SHORT): 16 rows a workgroup, which lie
+// side by side, by way of LDS.
+constexpr int SHORT = 256;
+template <typename T>
+__global__ __launch_bounds__(NT) void k_emission_ds_short(const float *__restrict__ weight,
+                                                          const float *__restrict__ grad,
+                                                          long long rows, int cols,
+                                                          const float *__restrict__ scale,
+                                                          T *__restrict__ out, int Cp) {
+  constexpr int E = 16 / (int)sizeof(T);
+  __shared__ float s_w[16 * SHORT], s_g[16 * SHORT];
+  __shared__ float s_sum[16];
+  const long long r0 = (long long)blockIdx.x * 16;
+  const int n = (int)(rows - r0 < 16 ? rows - r0 : 16);
+  const float k = scale ? *scale : 1.0f;
+#pragma unroll 4
+  for (int i = threadIdx.x; i < n * cols; i += NT) {
+    s_w[i] = weight[r0 * cols + i];
+    s_g[i] = grad[r0 * cols + i];
+  }
+  __syncthreads();
+  const int row = threadIdx.x / 16;
+  float s = 0.0f;
+  if (row < n)
+    for (int c = threadIdx.x % 16; c < cols; c += 16) s += s_g[row * cols + c];
+#pragma unroll
+  for (int x = 1; x < 16; x <<= 1) s += __shfl_xor(s, x);
+  if (threadIdx.x % 16 == 0) s_sum[row] = s;
+  __syncthreads();
+  const int groups = Cp / E;
+  for (int i = threadIdx.x; i < n * groups; i += NT) {
+    const int r = i / groups, c = (i - r * groups) * E;
+    alignas(16) T v[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+      v[e] = (T)(c + e < cols ? k * (s_g[r * cols + c + e] -
+                                     exp_less(s_w[r * cols + c + e], 0.0f) * s_sum[r])
+                              : 0.0f);
+    *reinterpret_cast<int4v *>(out + (r0 + r) * Cp + c) = *reinterpret_cast<const int4v *>(v);
   }
 }
 
@@ -1036,9 +1122,9 @@ hipError_t product(Product g, int tile, hipStream_t s) {
     k_product_large<T, LAYOUT, EPI>
         <<<dim3((unsigned)(tm * tn < CUS ? tm * tn : CUS), 1, (unsigned)g.splits), 512, 0, s>>>(g);
   else if (tile == 1)
-    k_product<T, LAYOUT, 128, 128, 2, 2, EPI><<<grid, 256, 0, s>>>(g);
+    k_product<T, LAYOUT, 128, 128, 2, 2, 2, EPI><<<grid, 256, 0, s>>>(g);
   else
-    k_product<T, LAYOUT, 64, 64, 2, 2, EPI><<<grid, 256, 0, s>>>(g);
+    k_product<T, LAYOUT, 64, 64, 2, 2, 2, EPI><<<grid, 256, 0, s>>>(g);
   return hipGetLastError();
 }
 
@@ -1080,9 +1166,10 @@ hipError_t fill(const Laid<T> *lx, const Mat &x, const Laid<T> *lw, const Mat &w
   return hipGetLastError();
 }
 
-// Whether four results side by side may be written at once.
+// Whether four results side by side may be written at once, or (2) 16 bytes.
 template <typename T>
 int wide(const Mat &m) {
+  if ((uintptr_t)m.data % 16 == 0 && m.stride * sizeof(T) % 16 == 0) return 2;
   return (uintptr_t)m.data % (4 * sizeof(T)) == 0 && m.stride % 4 == 0;
 }
 
@@ -1154,9 +1241,9 @@ hipError_t emission_as(const Mat &x, const Mat &w, float *weight, Bump &b, hipSt
     g.tiles_m = (int)((N + 31) / 32);
     g.tiles_n = 1;
     if (C <= 64)
-      k_product<T, ROWS_ROWS, 32, 64, 2, 1, EPI_LOG><<<g.tiles_m, 2 * WAVE, 0, s>>>(g);
+      k_product<T, ROWS_ROWS, 32, 64, 2, 1, 4, EPI_LOG><<<g.tiles_m, 2 * WAVE, 0, s>>>(g);
     else
-      k_product<T, ROWS_ROWS, 32, 128, 2, 1, EPI_LOG><<<g.tiles_m, 2 * WAVE, 0, s>>>(g);
+      k_product<T, ROWS_ROWS, 32, 128, 2, 1, 4, EPI_LOG><<<g.tiles_m, 2 * WAVE, 0, s>>>(g);
     return hipGetLastError();
   }
   g.part = part;
@@ -1197,11 +1284,11 @@ hipError_t emission_grads_as(const Mat &x, const Mat &w, const float *weight, co
   } else {
     scale = nullptr;
   }
-  // (16 lanes a row where a row is short)
-  if (C <= 256)
-    k_emission_ds<T, 16><<<(unsigned)((N + 15) / 16), NT, 0, s>>>(weight, grad, N, C, scale, ds, Cp);
+  if (C <= SHORT)
+    k_emission_ds_short<T><<<(unsigned)((N + 15) / 16), NT, 0, s>>>(weight, grad, N, (int)C, scale,
+                                                                  ds, (int)Cp);
   else
-    k_emission_ds<T, 64><<<(unsigned)((N + 3) / 4), NT, 0, s>>>(weight, grad, N, C, scale, ds, Cp);
+    k_emission_ds<T><<<(unsigned)((N + 3) / 4), NT, 0, s>>>(weight, grad, N, C, scale, ds, Cp);
   TRY(hipGetLastError());
   if (gx) TRY(px.run({ds, Cp, N, Cp}, lw.columns(), N, H, Cp, scale, *gx, s));
   if (gw) TRY(pw.run({ds, Cp, Cp, N}, lx.columns(), C, H, N, scale, *gw, s));
