@@ -148,9 +148,10 @@ struct RowTile {
   static __device__ __forceinline__ long long bytes(const Operand &o, long long r0) {
     return ((o.rows - 1 - r0) * o.ld + o.depth) * (long long)sizeof(T);
   }
-  static __device__ __forceinline__ int4v step(const Operand &, const char *base,
+  static __device__ __forceinline__ int4v step(const Operand &o, const char *base,
                                                long long bytes, int t) {
-    return buffer_at(base, bytes, (long long)t * KBYTES);
+    const long long more = t >= o.wrap ? o.jump - (long long)o.wrap * KBYTES : 0;
+    return buffer_at(base, bytes, (long long)t * KBYTES + more);
   }
   // the i-th load of the part, of the step whose buffer it is, to `lds`
   __device__ __forceinline__ void fetch(int i, uint32_t lds, int4v buffer, int wave) const {
@@ -201,7 +202,8 @@ struct ColTile {
   }
   static __device__ __forceinline__ int4v step(const Operand &o, const char *base,
                                                long long bytes, int t) {
-    return buffer_at(base, bytes, (long long)t * (K * o.ld * (long long)sizeof(T)));
+    const long long every = K * o.ld * (long long)sizeof(T);
+    return buffer_at(base, bytes, t >= o.wrap ? (t - o.wrap) * every + o.jump : t * every);
   }
   __device__ __forceinline__ void fetch(int i, uint32_t lds, int4v buffer, int wave) const {
     load_lds(lds + (wave * LOADS + i) * 1024, off[i], buffer);
@@ -255,7 +257,8 @@ struct Product {
   const float *lse;      // [M]
   const float *grad;     // [M] or null (1)
   const float *scale;    // power of two on dS (16-bit floats), or null (1)
-  long long Np;          // dS: columns to write, zeros past N
+  long long Np, lo;      // dS: columns to write, zeros past N; what rounding lost goes
+                         // `lo` columns further on (0: it is dropped)
   int add;               // sums: add to what is there
   const float *sums;     // [M, N rounded up to four] or null
   int wide;              // results: `out` and its rows are aligned to four (2: to 16 bytes)
@@ -709,6 +712,15 @@ __device__ __forceinline__ void epilogue(const Product &g, float4v (&acc)[FM][FN
           for (int q = 0; q < L; q += E)
             if (nb + col(q) < g.Np)
               *reinterpret_cast<int4v *>(to + col(q)) = *reinterpret_cast<const int4v *>(o + q);
+          if (g.lo) {
+            to += g.lo;
+#pragma unroll
+            for (int q = 0; q < L; ++q) o[q] = (T)(v[q] - (float)o[q]);
+#pragma unroll
+            for (int q = 0; q < L; q += E)
+              if (nb + col(q) < g.Np)
+                *reinterpret_cast<int4v *>(to + col(q)) = *reinterpret_cast<const int4v *>(o + q);
+          }
         }
       } else {
         if constexpr (EPI == EPI_PART) {
@@ -936,13 +948,28 @@ __global__ __launch_bounds__(NT) void k_emission_max(const float *__restrict__ g
   if (threadIdx.x == 0) out[blockIdx.x] = m;
 }
 
+// 16 bytes of dS, and what rounding lost `lo` columns further on (0: dropped).
+template <typename T, int E>
+__device__ __forceinline__ void put_ds(T *to, const float (&d)[E], long long lo) {
+  alignas(16) T v[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) v[e] = (T)d[e];
+  *reinterpret_cast<int4v *>(to) = *reinterpret_cast<const int4v *>(v);
+  if (lo) {
+#pragma unroll
+    for (int e = 0; e < E; ++e) v[e] = (T)(d[e] - (float)v[e]);
+    *reinterpret_cast<int4v *>(to + lo) = *reinterpret_cast<const int4v *>(v);
+  }
+}
+
 // dS = grad - exp(weight) sum(grad), zeros up to Cp columns; a wavefront a row.
 template <typename T>
 __global__ __launch_bounds__(NT) void k_emission_ds(const float *__restrict__ weight,
                                                     const float *__restrict__ grad,
                                                     long long rows, long long cols,
                                                     const float *__restrict__ scale,
-                                                    T *__restrict__ out, long long Cp) {
+                                                    T *__restrict__ out, long long Cp,
+                                                    long long ld) {
   constexpr int E = 16 / (int)sizeof(T);
   const int lane = threadIdx.x & (WAVE - 1);
   const long long r = (long long)blockIdx.x * NWAVES + threadIdx.x / WAVE;
@@ -954,11 +981,11 @@ __global__ __launch_bounds__(NT) void k_emission_ds(const float *__restrict__ we
   for (long long c = lane; c < cols; c += WAVE) s += g[c];
   s = wave_sum_f(s);
   for (long long c = (long long)lane * E; c < Cp; c += WAVE * E) {
-    alignas(16) T v[E];
+    float d[E];
 #pragma unroll
     for (int e = 0; e < E; ++e)
-      v[e] = (T)(c + e < cols ? k * (g[c + e] - exp_less(w[c + e], 0.0f) * s) : 0.0f);
-    *reinterpret_cast<int4v *>(out + r * Cp + c) = *reinterpret_cast<const int4v *>(v);
+      d[e] = c + e < cols ? k * (g[c + e] - exp_less(w[c + e], 0.0f) * s) : 0.0f;
+    put_ds(out + r * ld + c, d, ld > Cp ? Cp : 0);
   }
 }
 
@@ -970,7 +997,7 @@ __global__ __launch_bounds__(NT) void k_emission_ds_short(const float *__restric
                                                           const float *__restrict__ grad,
                                                           long long rows, int cols,
                                                           const float *__restrict__ scale,
-                                                          T *__restrict__ out, int Cp) {
+                                                          T *__restrict__ out, int Cp, int ld) {
   constexpr int E = 16 / (int)sizeof(T);
   __shared__ float s_w[16 * SHORT], s_g[16 * SHORT];
   __shared__ float s_sum[16];
@@ -994,13 +1021,13 @@ __global__ __launch_bounds__(NT) void k_emission_ds_short(const float *__restric
   const int groups = Cp / E;
   for (int i = threadIdx.x; i < n * groups; i += NT) {
     const int r = i / groups, c = (i - r * groups) * E;
-    alignas(16) T v[E];
+    float d[E];
 #pragma unroll
     for (int e = 0; e < E; ++e)
-      v[e] = (T)(c + e < cols ? k * (s_g[r * cols + c + e] -
-                                     exp_less(s_w[r * cols + c + e], 0.0f) * s_sum[r])
-                              : 0.0f);
-    *reinterpret_cast<int4v *>(out + (r0 + r) * Cp + c) = *reinterpret_cast<const int4v *>(v);
+      d[e] = c + e < cols ? k * (s_g[r * cols + c + e] -
+                                 exp_less(s_w[r * cols + c + e], 0.0f) * s_sum[r])
+                          : 0.0f;
+    put_ds(out + (r0 + r) * ld + c, d, ld > Cp ? Cp : 0);
   }
 }
 
@@ -1213,9 +1240,58 @@ struct SplitProduct {
   }
 };
 
+// dS has the matrices' type, so that the matrix cores multiply it: in 16 bits it
+// is rounded.  Each element of a gradient then sums roundings of either sign,
+// which together come to about its own rounding.  Where the products are small
+// and a gradient sums few terms (one row's dx is its word's and little else), dS
+// is two numbers, the rounded one and the rest, and the sums run over both:
+// nothing is lost, for twice the products (up to 2^28 of them, 5 us more; 16,000
+// rows by 69 classes of width 512 would take 8 us more of 40).
+template <typename T>
+bool in_two(long long N, long long C, long long H) {
+  return sizeof(T) == 2 && (double)N * C * H <= (double)(1 << 28);
+}
+
+// The two products of dS, N x C with rows of `ld` (Cp columns, and again Cp of
+// rests if `two`): their operands.
+template <typename T>
+struct Gradients {
+  Operand dx_a, dx_b, dw_a, dw_b;
+  long long dx_k, dw_k;
+
+  Gradients(const T *ds, long long ld, long long N, long long Cp, bool two, Operand w, Operand x) {
+    const long long Ns = up(N, k_step<T>());
+    dx_a = {ds, ld, N, two ? 2 * Cp : Cp};
+    dx_b = w;
+    dw_a = {ds, ld, two ? 2 * Cp : Cp, N};
+    dw_b = x;
+    dx_k = Cp;
+    dw_k = N;
+    if (two) {
+      dx_b.wrap = (int)(Cp / k_step<T>());
+      dw_a.wrap = dw_b.wrap = (int)(Ns / k_step<T>());
+      dw_a.jump = Cp * (long long)sizeof(T);
+      dx_k = 2 * Cp;
+      dw_k = 2 * Ns;
+    }
+  }
+};
+
 // Rows that a workgroup of the kernels over rows takes: 16 where that leaves
 // enough workgroups (a row each otherwise: 165 rows of 869 columns 19 us by 16).
 bool many_rows(long long N) { return N >= 4096; }
+
+template <typename T, int BM, int WM>
+void log_rows(const Product &g, hipStream_t s) {
+  if (g.N <= 32)
+    k_product<T, ROWS_ROWS, BM, 32, WM, 1, 4, EPI_LOG><<<g.tiles_m, WM * WAVE, 0, s>>>(g);
+  else if (g.N <= 64)
+    k_product<T, ROWS_ROWS, BM, 64, WM, 1, 4, EPI_LOG><<<g.tiles_m, WM * WAVE, 0, s>>>(g);
+  else if (g.N <= 96)
+    k_product<T, ROWS_ROWS, BM, 96, WM, 1, 4, EPI_LOG><<<g.tiles_m, WM * WAVE, 0, s>>>(g);
+  else
+    k_product<T, ROWS_ROWS, BM, 128, WM, 1, 4, EPI_LOG><<<g.tiles_m, WM * WAVE, 0, s>>>(g);
+}
 
 template <typename T>
 hipError_t emission_as(const Mat &x, const Mat &w, float *weight, Bump &b, hipStream_t s) {
@@ -1238,12 +1314,15 @@ hipError_t emission_as(const Mat &x, const Mat &w, float *weight, Bump &b, hipSt
   g.out = weight;
   g.ldo = C;
   if (whole) {
-    g.tiles_m = (int)((N + 31) / 32);
     g.tiles_n = 1;
-    if (C <= 64)
-      k_product<T, ROWS_ROWS, 32, 64, 2, 1, 4, EPI_LOG><<<g.tiles_m, 2 * WAVE, 0, s>>>(g);
-    else
-      k_product<T, ROWS_ROWS, 32, 128, 2, 1, 4, EPI_LOG><<<g.tiles_m, 2 * WAVE, 0, s>>>(g);
+    // (rows of 64 a workgroup where they are enough: w is loaded half as often)
+    if (N >= 8192) {
+      g.tiles_m = (int)((N + 63) / 64);
+      log_rows<T, 64, 4>(g, s);
+    } else {
+      g.tiles_m = (int)((N + 31) / 32);
+      log_rows<T, 32, 2>(g, s);
+    }
     return hipGetLastError();
   }
   g.part = part;
@@ -1268,13 +1347,16 @@ hipError_t emission_grads_as(const Mat &x, const Mat &w, const float *weight, co
     return hipGetLastError();
   }
   const Laid<T> lx = lay<T>(x, b), lw = lay<T>(w, b);
-  T *ds = b.take<T>(N * Cp);
+  const bool two = in_two<T>(N, C, H);
+  const long long ld = two ? 2 * Cp : Cp;
+  T *ds = b.take<T>(N * ld);
   constexpr int GROUPS = 256;
   float *most = b.take<float>(GROUPS), *scale = b.take<float>(1);
+  const Gradients<T> p(ds, ld, N, Cp, two, lw.columns(), lx.columns());
   SplitProduct<T, ROWS_COLS> px{};
   SplitProduct<T, COLS_COLS> pw{};
-  if (gx) px.plan(N, H, Cp, b);
-  if (gw) pw.plan(C, H, N, b);
+  if (gx) px.plan(N, H, p.dx_k, b);
+  if (gw) pw.plan(C, H, p.dw_k, b);
   if (!b.base) return hipSuccess;
   TRY(fill(gw ? &lx : nullptr, x, gx ? &lw : nullptr, w, s));
   if (std::is_same<T, f16>::value) {
@@ -1286,12 +1368,12 @@ hipError_t emission_grads_as(const Mat &x, const Mat &w, const float *weight, co
   }
   if (C <= SHORT)
     k_emission_ds_short<T><<<(unsigned)((N + 15) / 16), NT, 0, s>>>(weight, grad, N, (int)C, scale,
-                                                                  ds, (int)Cp);
+                                                                  ds, (int)Cp, (int)ld);
   else
-    k_emission_ds<T><<<(unsigned)((N + 3) / 4), NT, 0, s>>>(weight, grad, N, C, scale, ds, Cp);
+    k_emission_ds<T><<<(unsigned)((N + 3) / 4), NT, 0, s>>>(weight, grad, N, C, scale, ds, Cp, ld);
   TRY(hipGetLastError());
-  if (gx) TRY(px.run({ds, Cp, N, Cp}, lw.columns(), N, H, Cp, scale, *gx, s));
-  if (gw) TRY(pw.run({ds, Cp, Cp, N}, lx.columns(), C, H, N, scale, *gw, s));
+  if (gx) TRY(px.run(p.dx_a, p.dx_b, N, H, p.dx_k, scale, *gx, s));
+  if (gw) TRY(pw.run(p.dw_a, p.dw_b, C, H, p.dw_k, scale, *gw, s));
   return hipSuccess;
 }
 
@@ -1358,22 +1440,29 @@ hipError_t loss_grads_as(const Mat &x, const Mat &w, const int32_t *target, cons
   }
   const Laid<T> lx = lay<T>(x, b), lw = lay<T>(w, b);
   const long long piece = piece_of(V, H, PIECE_BYTES / (N * (long long)sizeof(T)));
-  const bool whole = piece == V;
+  const bool whole = piece == V, two = whole && in_two<T>(N, V, H);
   const long long Pp = up(piece, 64);
-  T *ds = b.take<T>(N * (Pp + DS_GAP));
+  // a piece of `n` words from v0 on
+  const auto products = [&](const T *ds, long long v0, long long n) {
+    const long long np = up(n, 64);
+    const Operand wc{static_cast<const T *>(lw.o.p) + v0 * lw.o.ld, lw.o.ld, lw.cols, n};
+    return Gradients<T>(ds, (two ? 2 : 1) * np + DS_GAP, N, np, two, wc, lx.columns());
+  };
+  T *ds = b.take<T>(N * ((two ? 2 : 1) * Pp + DS_GAP));
   constexpr int GROUPS = 256;
   float *most_g = b.take<float>(GROUPS), *scale = b.take<float>(1);
   SplitProduct<T, ROWS_COLS> px{};
   SplitProduct<T, COLS_COLS> pw{};
   float *sums = nullptr;
-  if (gx && whole) px.plan(N, H, Pp, b);
+  if (gx && whole) px.plan(N, H, products(ds, 0, V).dx_k, b);
   if (gx && !whole) sums = b.take<float>(N * up(H, 4));
   const size_t mark = b.at;
   size_t most = mark;
   if (gw) {
     for (long long v0 = 0; v0 < V; v0 += piece) {
+      const long long n = V - v0 < piece ? V - v0 : piece;
       b.at = mark;
-      pw.plan(V - v0 < piece ? V - v0 : piece, H, N, b);
+      pw.plan(n, H, products(ds, v0, n).dw_k, b);
       most = b.at > most ? b.at : most;
     }
   }
@@ -1392,7 +1481,7 @@ hipError_t loss_grads_as(const Mat &x, const Mat &w, const int32_t *target, cons
   for (long long v0 = 0; v0 < V; v0 += piece) {
     const long long n = V - v0 < piece ? V - v0 : piece, np = up(n, 64);
     const Operand wp{static_cast<const T *>(lw.o.p) + v0 * lw.o.ld, lw.o.ld, n, lw.cols};
-    const Operand wc{wp.p, wp.ld, lw.cols, n};
+    const Gradients<T> p = products(ds, v0, n);
     Product g{};
     g.A = lx.o;
     g.B = wp;
@@ -1404,7 +1493,8 @@ hipError_t loss_grads_as(const Mat &x, const Mat &w, const int32_t *target, cons
     g.n0 = v0;
     g.words = V;
     g.out = ds;
-    g.ldo = np + DS_GAP;
+    g.ldo = p.dx_a.ld;
+    g.lo = two ? np : 0;
     g.target = target;
     g.lse = lse;
     g.grad = grad;
@@ -1412,11 +1502,11 @@ hipError_t loss_grads_as(const Mat &x, const Mat &w, const int32_t *target, cons
     g.Np = np;
     TRY((product<T, ROWS_ROWS, EPI_DS>(g, cut_for<T>(N, n, lx.cols, false).tile, s)));
     if (gx && whole) {
-      TRY(px.run({ds, np + DS_GAP, N, np}, wc, N, H, np, scale, *gx, s));
+      TRY(px.run(p.dx_a, p.dx_b, N, H, p.dx_k, scale, *gx, s));
     } else if (gx) {
       Product q{};
-      q.A = {ds, np + DS_GAP, N, np};
-      q.B = wc;
+      q.A = p.dx_a;
+      q.B = p.dx_b;
       q.M = N;
       q.N = H;
       q.K = np;
@@ -1442,8 +1532,8 @@ hipError_t loss_grads_as(const Mat &x, const Mat &w, const int32_t *target, cons
       out.data = static_cast<T *>(out.data) + v0 * out.stride;
       out.rows = n;
       b.at = mark;
-      pw.plan(n, H, N, b);
-      TRY(pw.run({ds, np + DS_GAP, np, N}, lx.columns(), n, H, N, scale, out, s));
+      pw.plan(n, H, p.dw_k, b);
+      TRY(pw.run(p.dw_a, p.dw_b, n, H, p.dw_k, scale, out, s));
     }
   }
   return hipSuccess;

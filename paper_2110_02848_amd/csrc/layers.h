@@ -56,11 +56,14 @@ hipError_t launch_recurrence_step(const StepArgs &a, int type, hipStream_t s);
 
 // An operand of the products, element (r, k) of `rows` by `depth`: at
 // p[r * ld + k], or at p[k * ld + r] where it is read column by column.  Rows
-// of memory begin at multiples of 16 bytes, whole groups of them.
+// of memory begin at multiples of 16 bytes, whole groups of them.  From step
+// `wrap` of the sum on, k starts over, `jump` bytes further on.
 struct Operand {
   const void *p;
   long long ld;
   long long rows, depth;
+  int wrap = INT32_MAX;
+  long long jump = 0;
 };
 
 // Each is called twice: without workspace (ws null) it only says how many
