@@ -137,7 +137,8 @@ struct DeviceGuard {
   bool ok = false;
   explicit DeviceGuard(int dev) {
     if (hipGetDevice(&prev) != hipSuccess) prev = -1;
-    ok = hipSetDevice(dev) == hipSuccess;
+    ok = prev == dev || hipSetDevice(dev) == hipSuccess;
+    if (prev == dev) prev = -1;  // nothing to go back to
   }
   ~DeviceGuard() {
     if (prev >= 0) (void)hipSetDevice(prev);

@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 
 import numpy as np
 
@@ -222,14 +223,16 @@ def _stream_handle(stream):
 _types = {}  # torch type -> enum fst_type
 
 
-def _matrix(t, name):
-    """View of a 2-D device tensor whose rows are contiguous."""
-    if not _types:
+def _view(t, name):
+    """(address, rows, cols, stride, type) of a 2-D device tensor whose rows are
+    contiguous."""
+    typ = _types.get(t.dtype)
+    if typ is None and not _types:
         import torch
         _types.update({torch.float32: FST_F32, torch.float16: FST_F16,
                        torch.bfloat16: FST_BF16})
-    typ = _types.get(t.dtype)
-    if typ is None or t.dim() != 2 or not t.is_cuda:
+        typ = _types.get(t.dtype)
+    if typ is None or not t.is_cuda or t.dim() != 2:
         raise ValueError(f"{name}: a 2-D device tensor of float32, float16 or bfloat16 is needed")
     rows, cols = t.shape
     step, inner = t.stride()
@@ -239,7 +242,39 @@ def _matrix(t, name):
         if rows > 1:
             raise ValueError(f"{name}: rows overlap")
         step = cols
-    return _Matrix(t.data_ptr() if rows and cols else None, rows, cols, step, typ)
+    return t.data_ptr() if rows and cols else 0, rows, cols, step, typ
+
+
+def _matrix(t, name):
+    return _Matrix(*_view(t, name))
+
+
+class _Marshal:
+    """The structures that the calls of a context pass, made once and filled for
+    each call (a context is one thread's)."""
+    _VIEW = struct.Struct("<Qqqqi")
+    _RECURRENCE = struct.Struct("<i4xQi4xQqqqi4xQqqqi4xQ")
+
+    def __init__(self):
+        self._m = [_Matrix() for _ in range(4)]
+        self._ref = [ctypes.byref(m) for m in self._m]
+        self._r = _Recurrence()
+
+    def matrix(self, i, t, name):
+        self._VIEW.pack_into(self._m[i], 0, *_view(t, name))
+        return self._ref[i]
+
+    def made(self, i, t, typ):
+        """The same of a tensor made for the call."""
+        rows, cols = t.shape
+        self._VIEW.pack_into(self._m[i], 0, t.data_ptr() if rows and cols else 0, rows, cols, cols,
+                             typ)
+        return self._ref[i]
+
+    def recurrence(self, n, offset, reverse, x, gate, state):
+        self._RECURRENCE.pack_into(self._r, 0, n, offset or 0, reverse, *_view(x, "x"),
+                                   *_view(gate, "gate"), state or 0)
+        return self._r
 
 
 def _array(t, name, dtype, n):
@@ -290,6 +325,9 @@ class Composer:
         self.options = {}  # options set on this context (option -> value)
         import torch
         self._dev = torch.device("cuda", self.device)
+        self._pass = _Marshal()
+        self._raw_stream = torch._C._cuda_getCurrentRawStream
+        self._empty = torch.empty
 
     def close(self):
         if getattr(self, "_h", None):
@@ -545,16 +583,13 @@ class Composer:
     # ---- between a network and its graphs ----
 
     def _call_stream(self, stream):
-        if stream is not None:
-            return stream.cuda_stream
-        import torch
-        return torch._C._cuda_getCurrentRawStream(self.device)
+        return self._raw_stream(self.device) if stream is None else stream.cuda_stream
 
     def _new(self, stream, shape, dtype):
         """A tensor that belongs to the stream of the call."""
-        import torch
         if stream is None:
-            return torch.empty(shape, dtype=dtype, device=self._dev)
+            return self._empty(shape, dtype=dtype, device=self._dev)
+        import torch
         with torch.cuda.stream(stream):
             return torch.empty(shape, dtype=dtype, device=self._dev)
 
@@ -578,7 +613,7 @@ class Composer:
         saved = self._new(stream, (N // FST_RECURRENCE_SAVE_ROWS + n, D),
                           torch.float32) if save else None
         self._uses(stream, x, gate, offset, state)
-        rc = self._lib.fst_recurrence_run(self._h, R, _matrix(y, "y"), _address(last),
+        rc = self._lib.fst_recurrence_run(self._h, R, self._pass.made(0, y, _types[y.dtype]), _address(last),
                                           _address(saved), self._call_stream(stream))
         _check(rc, "fst_recurrence_run")
         return dict(y=y, last=last, saved=saved)
@@ -597,8 +632,9 @@ class Composer:
         self._uses(stream, x, gate, offset, grad_y, saved, state, grad_last)
         rc = self._lib.fst_recurrence_grads(
             self._h, R, _array(saved, "saved", torch.float32, rows * D),
-            _matrix(grad_y, "grad_y"), _array(grad_last, "grad_last", torch.float32, n * D),
-            _matrix(gx, "x"), _matrix(gu, "gate"), _address(gs), self._call_stream(stream))
+            self._pass.matrix(0, grad_y, "grad_y"),
+            _array(grad_last, "grad_last", torch.float32, n * D), self._pass.made(1, gx, _types[x.dtype]),
+            self._pass.made(2, gu, _types[x.dtype]), _address(gs), self._call_stream(stream))
         _check(rc, "fst_recurrence_grads")
         return dict(x=gx, gate=gu, state=gs)
 
@@ -607,9 +643,9 @@ class Composer:
         n = int(offset.numel()) - 1
         if n < 0:
             raise ValueError("offset: at least one entry is needed")
-        R = _Recurrence(n, _array(offset, "offset", torch.int32, n + 1), int(bool(reverse)),
-                        _matrix(x, "x"), _matrix(gate, "gate"),
-                        _array(state, "state", torch.float32, n * x.shape[1]))
+        R = self._pass.recurrence(n, _array(offset, "offset", torch.int32, n + 1),
+                                  int(bool(reverse)), x, gate,
+                                  _array(state, "state", torch.float32, n * x.shape[-1]))
         return R, n
 
     def recurrence_step(self, x, gate, state, slot=None, out=None, stream=None):
@@ -619,17 +655,17 @@ class Composer:
         row i's is slot[i] (an idle row's lies outside), and the new states
         replace the old ones unless ``out`` is given."""
         import torch
-        slots, D = int(state.shape[0]), int(x.shape[1])
+        slots, D = state.shape[0], x.shape[-1]
         if out is None:
             out = self._new(stream, (slots, D), torch.float32) if slot is None else state
         y = self._new(stream, x.shape, x.dtype)
         self._uses(stream, x, gate, state, slot, out)
         rc = self._lib.fst_recurrence_step(
-            self._h, _matrix(x, "x"), _matrix(gate, "gate"),
+            self._h, self._pass.matrix(0, x, "x"), self._pass.matrix(1, gate, "gate"),
             _array(state, "state", torch.float32, slots * D),
             _array(out, "out", torch.float32, slots * D),
-            _array(slot, "slot", torch.int32, x.shape[0]), slots, _matrix(y, "y"),
-            self._call_stream(stream))
+            _array(slot, "slot", torch.int32, x.shape[0]), slots,
+            self._pass.made(2, y, _types[x.dtype]), self._call_stream(stream))
         _check(rc, "fst_recurrence_step")
         return y, out
 
@@ -641,7 +677,8 @@ class Composer:
         if out is None:
             out = self._new(stream, (N, C), torch.float32)
         self._uses(stream, x, w, out)
-        rc = self._lib.fst_emission_weights(self._h, _matrix(x, "x"), _matrix(w, "w"),
+        rc = self._lib.fst_emission_weights(self._h, self._pass.matrix(0, x, "x"),
+                                            self._pass.matrix(1, w, "w"),
                                             _array(out, "out", torch.float32, N * C),
                                             self._call_stream(stream))
         _check(rc, "fst_emission_weights")
@@ -655,10 +692,10 @@ class Composer:
         gx, gw = self._head_grads(x, w, need_x, need_w, stream)
         self._uses(stream, x, w, weight, grad)
         rc = self._lib.fst_emission_grads(
-            self._h, _matrix(x, "x"), _matrix(w, "w"),
+            self._h, self._pass.matrix(0, x, "x"), self._pass.matrix(1, w, "w"),
             _array(weight, "weight", torch.float32, n), _array(grad, "grad", torch.float32, n),
-            _matrix(gx, "x") if need_x else None, _matrix(gw, "w") if need_w else None,
-            self._call_stream(stream))
+            self._pass.made(2, gx, _types[x.dtype]) if need_x else None,
+            self._pass.made(3, gw, _types[w.dtype]) if need_w else None, self._call_stream(stream))
         _check(rc, "fst_emission_grads")
         return gx, gw
 
@@ -670,7 +707,8 @@ class Composer:
         loss = self._new(stream, (N,), torch.float32)
         lse = self._new(stream, (N,), torch.float32)
         self._uses(stream, x, w, target)
-        rc = self._lib.fst_cross_entropy(self._h, _matrix(x, "x"), _matrix(w, "w"),
+        rc = self._lib.fst_cross_entropy(self._h, self._pass.matrix(0, x, "x"),
+                                         self._pass.matrix(1, w, "w"),
                                          _array(target, "target", torch.int32, N),
                                          _address(loss), _address(lse),
                                          self._call_stream(stream))
@@ -686,10 +724,11 @@ class Composer:
         gx, gw = self._head_grads(x, w, need_x, need_w, stream)
         self._uses(stream, x, w, target, lse, grad)
         rc = self._lib.fst_cross_entropy_grads(
-            self._h, _matrix(x, "x"), _matrix(w, "w"),
+            self._h, self._pass.matrix(0, x, "x"), self._pass.matrix(1, w, "w"),
             _array(target, "target", torch.int32, N), _array(lse, "lse", torch.float32, N),
-            _array(grad, "grad", torch.float32, N), _matrix(gx, "x") if need_x else None,
-            _matrix(gw, "w") if need_w else None, self._call_stream(stream))
+            _array(grad, "grad", torch.float32, N),
+            self._pass.made(2, gx, _types[x.dtype]) if need_x else None,
+            self._pass.made(3, gw, _types[w.dtype]) if need_w else None, self._call_stream(stream))
         _check(rc, "fst_cross_entropy_grads")
         return gx, gw
 
