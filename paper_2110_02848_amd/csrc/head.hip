@@ -1100,11 +1100,12 @@ struct Cut {
 };
 
 // The cut that takes least, by a model in microseconds fitted to products of
-// 0.5 to 35 Gflop (2000 x 4000 over 512, tiles of 256, 128 and 64: measured 19, 14
-// and 19; 1600 x 26,000 over 256: 42, 47, 55; 64 x 10,000 over 512: 17, 11 and 7;
-// 4096 x 4096 over 1024: 32, 44, 59).  A step of the largest tile takes a CU 1.54
-// (256 of the products at once); 512 of the next take 1.2, 0.85 where a CU has
-// one alone; of the smallest 256 take 0.22, one alone 0.5.  In float32 the matrix
+// 0.5 to 35 Gflop (2000 x 4000 over 512, tiles of 256, 128 and 64: measured 19, 12
+// and 19; 1600 x 26,000 over 256: 42, 43, 55; 64 x 10,000 over 512: 17, 10 and 7;
+// 4096 x 4096 over 1024: 32, 38, 59).  A step of the largest tile takes a CU 1.54
+// (256 of the products at once); 512 of the next take 1, 0.7 where a CU has
+// one alone (eight wavefronts of 32 x 64: four of 64 x 64 take 1.2); of the
+// smallest 256 take 0.22, one alone 0.5.  In float32 the matrix
 // cores take longer than that.  Splitting costs a launch and the sums' way to
 // memory and back.
 template <typename T>
@@ -1119,12 +1120,15 @@ Cut cut_for(long long M, long long N, long long K, bool may_split) {
     for (long long p = 1; p == 1 || (may_split && p <= 256 && p <= all / 2); p += 1 + p / 16) {
       const double per = (double)((all + p - 1) / p), q = ceil(tiles * p / CUS);
       double us;
-      if (tile == 0)
+      if (tile == 0) {
         us = 1.5 + q * (per * (wide ? 7.0 : 1.54) + 5.5);
-      else if (tile == 1)
-        us = 4 + per * (q <= 1 ? (wide ? 1.75 : 0.85) : ceil(q / 2) * (wide ? 3.5 : 1.2));
-      else
-        us = 3.5 + per * (wide ? 0.44 * q : q <= 1 ? 0.5 : fmax(0.5, 0.218 * q));
+      } else if (tile == 1) {
+        const double pairs = floor(tiles * p / (2 * CUS)), rest = tiles * p - pairs * 2 * CUS;
+        us = 4 + per * (wide ? 3.5 : 1.0) *
+                     (pairs + (rest <= 0 ? 0 : rest > CUS ? 1 : wide ? 0.5 : 0.7));
+      } else {
+        us = 3.5 + per * (wide ? 0.5 * q : fmax(0.5, 0.218 * q));
+      }
       if (p > 1) us += 3.5 + (double)p * M * N * 8 / 4e6;
       if (us < least) {
         least = us;
@@ -1149,7 +1153,7 @@ hipError_t product(Product g, int tile, hipStream_t s) {
     k_product_large<T, LAYOUT, EPI>
         <<<dim3((unsigned)(tm * tn < CUS ? tm * tn : CUS), 1, (unsigned)g.splits), 512, 0, s>>>(g);
   else if (tile == 1)
-    k_product<T, LAYOUT, 128, 128, 2, 2, 2, EPI><<<grid, 256, 0, s>>>(g);
+    k_product<T, LAYOUT, 128, 128, 4, 2, 2, EPI><<<grid, 512, 0, s>>>(g);
   else
     k_product<T, LAYOUT, 64, 64, 2, 2, 2, EPI><<<grid, 256, 0, s>>>(g);
   return hipGetLastError();
