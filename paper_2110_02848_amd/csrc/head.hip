@@ -327,7 +327,9 @@ template <typename T, int LAYOUT, int BM, int BN, int WM, int WN, int STAGES, in
 __global__ __launch_bounds__(WM *WN *WAVE) void k_product(Product g) {
   constexpr int NWV = WM * WN, FM = BM / WM / 16, FN = BN / WN / 16;
   using A = TileA<T, LAYOUT, BM, NWV, Rows<BM, BM>>;
-  using B = TileB<T, LAYOUT, BN, NWV, Spread<16 / (int)sizeof(T), FN, FN>, Rows<BN, BN>>;
+  // (whole rows are put together in LDS: any order of their columns will do)
+  constexpr int SIDE = EPI == EPI_LOG ? 4 : 16 / (int)sizeof(T);
+  using B = TileB<T, LAYOUT, BN, NWV, Spread<SIDE, FN, FN>, Rows<BN, BN>>;
   __shared__ __align__(1024) char s_lds[STAGES][A::BYTES + B::BYTES];
   const int lane = threadIdx.x & (WAVE - 1);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
@@ -390,14 +392,18 @@ __global__ __launch_bounds__(WM *WN *WAVE) void k_product(Product g) {
   if constexpr (EPI == EPI_LOG) {
     // rows of log-probabilities, put together in LDS: the rows of a tile lie
     // side by side in memory (ldo is N)
-    static_assert(LAYOUT == ROWS_ROWS && WN == 1 && FM == 1, "a wavefront has whole rows");
+    static_assert(LAYOUT == ROWS_ROWS && FM == 1, "a wavefront has 16 rows");
     static_assert(BM * BN * 4 <= (int)sizeof(s_lds), "room for the tile");
-    constexpr int E = 16 / (int)sizeof(T), L = 4 * FN;
-    const int group = lane >> 4, cols = (int)g.N;
+    __shared__ float2 s_row[WN][BM];
+    constexpr int L = 4 * FN;
+    const int group = lane >> 4, cols = (int)g.N, row = wm * 16 + (lane & 15);
+    const auto column = [&](int q) {
+      return wn * FN * 16 + Spread<SIDE, FN, FN>::column(group, q);
+    };
     float mx = -INFINITY, sum = 0.0f;
 #pragma unroll
     for (int q = 0; q < L; ++q) {
-      if (Spread<E, FN, FN>::column(group, q) >= cols) acc[0][q / 4][q % 4] = -INFINITY;
+      if (column(q) >= cols) acc[0][q / 4][q % 4] = -INFINITY;
       mx = fmaxf(mx, acc[0][q / 4][q % 4]);
     }
     mx = fmaxf(mx, __shfl_xor(mx, 16));
@@ -407,13 +413,18 @@ __global__ __launch_bounds__(WM *WN *WAVE) void k_product(Product g) {
     for (int q = 0; q < L; ++q) sum += exp_less(acc[0][q / 4][q % 4], sh * LOG2E);
     sum += __shfl_xor(sum, 16);
     sum += __shfl_xor(sum, 32);
-    const float lse = sh + logf(sum);
-    __syncthreads();  // no one reads operands any more
+    if (lane < 16) s_row[wn][row] = make_float2(mx, sum);
+    __syncthreads();  // and no one reads operands any more
+    mx = s_row[0][row].x;
+    sum = s_row[0][row].y;
+#pragma unroll
+    for (int q = 1; q < WN; ++q) join(mx, sum, s_row[q][row].x, s_row[q][row].y);
+    const float lse = shift_of(mx) + logf(sum);
     float *s = reinterpret_cast<float *>(s_lds);
 #pragma unroll
     for (int q = 0; q < L; ++q) {
-      const int c = Spread<E, FN, FN>::column(group, q);
-      if (c < cols) s[(wm * 16 + (lane & 15)) * cols + c] = acc[0][q / 4][q % 4] - lse;
+      const int c = column(q);
+      if (c < cols) s[row * cols + c] = acc[0][q / 4][q % 4] - lse;
     }
     __syncthreads();
     const int n = (int)(g.M - m0 < BM ? g.M - m0 : BM) * cols;
@@ -1285,16 +1296,18 @@ struct Gradients {
 // enough workgroups (a row each otherwise: 165 rows of 869 columns 19 us by 16).
 bool many_rows(long long N) { return N >= 4096; }
 
-template <typename T, int BM, int WM>
+// Tiles of 32 rows, whole: four wavefronts of 16 rows and half the columns.
+template <typename T>
 void log_rows(const Product &g, hipStream_t s) {
+  const unsigned grid = (unsigned)g.tiles_m;
   if (g.N <= 32)
-    k_product<T, ROWS_ROWS, BM, 32, WM, 1, 4, EPI_LOG><<<g.tiles_m, WM * WAVE, 0, s>>>(g);
+    k_product<T, ROWS_ROWS, 32, 32, 2, 2, 4, EPI_LOG><<<grid, 4 * WAVE, 0, s>>>(g);
   else if (g.N <= 64)
-    k_product<T, ROWS_ROWS, BM, 64, WM, 1, 4, EPI_LOG><<<g.tiles_m, WM * WAVE, 0, s>>>(g);
+    k_product<T, ROWS_ROWS, 32, 64, 2, 2, 4, EPI_LOG><<<grid, 4 * WAVE, 0, s>>>(g);
   else if (g.N <= 96)
-    k_product<T, ROWS_ROWS, BM, 96, WM, 1, 4, EPI_LOG><<<g.tiles_m, WM * WAVE, 0, s>>>(g);
+    k_product<T, ROWS_ROWS, 32, 96, 2, 2, 4, EPI_LOG><<<grid, 4 * WAVE, 0, s>>>(g);
   else
-    k_product<T, ROWS_ROWS, BM, 128, WM, 1, 4, EPI_LOG><<<g.tiles_m, WM * WAVE, 0, s>>>(g);
+    k_product<T, ROWS_ROWS, 32, 128, 2, 2, 4, EPI_LOG><<<grid, 4 * WAVE, 0, s>>>(g);
 }
 
 template <typename T>
@@ -1318,15 +1331,9 @@ hipError_t emission_as(const Mat &x, const Mat &w, float *weight, Bump &b, hipSt
   g.out = weight;
   g.ldo = C;
   if (whole) {
+    g.tiles_m = (int)((N + 31) / 32);
     g.tiles_n = 1;
-    // (rows of 64 a workgroup where they are enough: w is loaded half as often)
-    if (N >= 8192) {
-      g.tiles_m = (int)((N + 63) / 64);
-      log_rows<T, 64, 4>(g, s);
-    } else {
-      g.tiles_m = (int)((N + 31) / 32);
-      log_rows<T, 32, 2>(g, s);
-    }
+    log_rows<T>(g, s);
     return hipGetLastError();
   }
   g.part = part;
