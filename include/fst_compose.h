@@ -519,8 +519,13 @@ FST_API int fst_recurrence_step(fst_ctx *ctx, const fst_matrix *x, const fst_mat
                                 const float *state_in, float *state_out, const int32_t *slot,
                                 int32_t num_slots, const fst_matrix *y, void *stream);
 
-/* Heads take at most this many rows of x and of w (FST_ERR_TOO_LARGE). */
+/* Heads take at most FST_HEAD_MAX_ROWS rows of x and of w, and
+ * FST_HEAD_MAX_COLS columns and classes of an emission (FST_ERR_TOO_LARGE).
+ * None of their outputs may overlap an input or another output.  Matrices
+ * whose rows do not begin at multiples of 16 bytes, or whose width is not a
+ * multiple of 64 (float32: 32), are copied into the workspace first. */
 #define FST_HEAD_MAX_ROWS (1 << 25)
+#define FST_HEAD_MAX_COLS (1 << 22)
 
 /* Weights of emission graphs: weight[n * C + c] = z[n][c] - log-sum over c'
  * of exp(z[n][c']), z = x w^T, for the N rows of x (frames, of any number of
@@ -536,8 +541,9 @@ FST_API int fst_emission_weights(fst_ctx *ctx, const fst_matrix *x, const fst_ma
  * the weights of fst_emission_weights on the same x and w:
  *   dz = grad - exp(weight) * (sum of grad over the row)
  *   grad_x = dz w,  grad_w = dz^T x
- * dz is rounded to the matrices' type for the two products (float16: scaled
- * by a power of two first, so that the smallest keep their digits). */
+ * For the two products dz is rounded to the matrices' type (float16: scaled by a
+ * power of two first, so that the smallest keep their digits); up to 2^28
+ * products N C H it is kept as two such numbers. */
 FST_API int fst_emission_grads(fst_ctx *ctx, const fst_matrix *x, const fst_matrix *w,
                                const float *weight, const float *grad,
                                const fst_matrix *grad_x, const fst_matrix *grad_w,
@@ -556,9 +562,10 @@ FST_API int fst_cross_entropy(fst_ctx *ctx, const fst_matrix *x, const fst_matri
  * (grad: device, float32, N, or NULL for 1):
  *   dz = grad[n] (exp(z - lse[n]) - [v = target[n]])  (0 for no word)
  *   grad_x = dz w,  grad_w = dz^T x
- * z is computed again, for a piece of the vocabulary at a time whose dz (in the
- * matrices' type, float16 scaled as above) takes 512 MiB of workspace at most
- * (more only where 256 words take more). */
+ * z is computed again, for a piece of the vocabulary at a time whose dz (rounded
+ * as above) takes 512 MiB of workspace at most (more only where 256 words take
+ * more).  A row without a word has dz = 0, whatever its scores; its x still
+ * meets that 0 in grad_w, so it has to be finite there. */
 FST_API int fst_cross_entropy_grads(fst_ctx *ctx, const fst_matrix *x, const fst_matrix *w,
                                     const int32_t *target, const float *lse, const float *grad,
                                     const fst_matrix *grad_x, const fst_matrix *grad_w,

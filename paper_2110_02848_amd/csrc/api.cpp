@@ -1997,7 +1997,10 @@ bool head_ok(const fst_matrix *x, const fst_matrix *w) {
          (w->rows > 0 || x->rows == 0);
 }
 bool head_large(const fst_matrix *x, const fst_matrix *w) {
-  return x->rows > FST_HEAD_MAX_ROWS || w->rows > FST_HEAD_MAX_ROWS;
+  return x->rows > FST_HEAD_MAX_ROWS || w->rows > FST_HEAD_MAX_ROWS || x->cols > FST_HEAD_MAX_COLS;
+}
+bool emission_large(const fst_matrix *x, const fst_matrix *w) {
+  return head_large(x, w) || w->rows > FST_HEAD_MAX_COLS;
 }
 
 bool head_grads_ok(const fst_matrix *x, const fst_matrix *w, const fst_matrix *gx,
@@ -2607,7 +2610,7 @@ int fst_recurrence_step(fst_ctx *c, const fst_matrix *x, const fst_matrix *gate,
 int fst_emission_weights(fst_ctx *c, const fst_matrix *x, const fst_matrix *w, float *weight,
                          void *stream) {
   if (!c || !head_ok(x, w)) return FST_ERR_INVALID_ARG;
-  if (head_large(x, w)) return FST_ERR_TOO_LARGE;
+  if (emission_large(x, w)) return FST_ERR_TOO_LARGE;
   if (x->rows == 0) return FST_OK;
   if (!weight) return FST_ERR_INVALID_ARG;
   DeviceGuard g(c->device);
@@ -2622,7 +2625,7 @@ int fst_emission_grads(fst_ctx *c, const fst_matrix *x, const fst_matrix *w, con
                        const float *grad, const fst_matrix *grad_x, const fst_matrix *grad_w,
                        void *stream) {
   if (!c || !head_grads_ok(x, w, grad_x, grad_w)) return FST_ERR_INVALID_ARG;
-  if (head_large(x, w)) return FST_ERR_TOO_LARGE;
+  if (emission_large(x, w)) return FST_ERR_TOO_LARGE;
   if (x->rows > 0 && (!weight || !grad)) return FST_ERR_INVALID_ARG;
   DeviceGuard g(c->device);
   if (!g.ok) return FST_ERR_HIP;

@@ -28,7 +28,6 @@ typedef __attribute__((ext_vector_type(8))) __bf16 bhalf8;
 typedef __attribute__((ext_vector_type(4))) short short4v;
 
 #define LDS_PTR(p) ((__attribute__((address_space(3))) void *)(p))
-#define GLB_PTR(p) ((const __attribute__((address_space(1))) void *)(p))
 
 constexpr int KBYTES = 128;  // bytes of a row of an operand's tile along the sum
 
@@ -481,8 +480,8 @@ __device__ __forceinline__ void meet() {
 // and one for multiplying, with a barrier after each, and the wavefronts of the
 // lower half are one time behind: on every SIMD one wavefront multiplies while
 // the other reads, so the matrix cores always have one to feed them.  (With four
-// phases of a quarter each, a barrier for every 16 products instead of 32, they were
-// busy 60 % of the time, see DESIGN.)
+// phases of a quarter each, a barrier for every 16 products instead of 32, a step
+// took 3430 cycles; it takes 3060, of which the products are 2048.)
 //
 // The 256 rows of A and the 256 of B of a step are 32 KiB each; LDS holds five
 // of them in a ring: B(t), A(t), B(t + 1), A(t + 1), B(t + 2), ...  One that was
@@ -493,6 +492,12 @@ __device__ __forceinline__ void meet() {
 // What the next phase reads has landed for all when each wavefront has waited
 // for its own loads of it and met the others: five times of 32 products for a load
 // to arrive, three for A0.
+//
+// What bounds it: waiting for loads, barriers and the card's power.  With 16,000
+// x 32,000 over 1024 (bf16): products over long sums (dx, dw) 1.25 Pflop/s, 1.37
+// in the first milliseconds, scores with their statistics 1.07, dS, whose 1 GB
+// is written meanwhile, 0.91; the products alone, without reads or loads, would
+// run at 2.0.
 template <typename T, int LAYOUT>
 struct Large {
   static constexpr int NWV = 8;
@@ -1116,9 +1121,9 @@ struct Cut {
 // 4096 x 4096 over 1024: 32, 38, 59).  A step of the largest tile takes a CU 1.54
 // (256 of the products at once); 512 of the next take 1, 0.7 where a CU has
 // one alone (eight wavefronts of 32 x 64: four of 64 x 64 take 1.2); of the
-// smallest 256 take 0.22, one alone 0.5.  In float32 the matrix
-// cores take longer than that.  Splitting costs a launch and the sums' way to
-// memory and back.
+// smallest 256 take 0.22, one alone 0.5.  In float32 the matrix cores take
+// longer than that.  Splitting costs a launch and the sums' way to memory and
+// back.
 template <typename T>
 Cut cut_for(long long M, long long N, long long K, bool may_split) {
   const long long all = (K + k_step<T>() - 1) / k_step<T>();
@@ -1128,7 +1133,8 @@ Cut cut_for(long long M, long long N, long long K, bool may_split) {
   for (int tile = 0; tile < 3; ++tile) {
     const double tiles = (double)((M + TILES[tile].bm - 1) / TILES[tile].bm) *
                          (double)((N + TILES[tile].bn - 1) / TILES[tile].bn);
-    for (long long p = 1; p == 1 || (may_split && p <= 256 && p <= all / 2); p += 1 + p / 16) {
+    for (long long p = 1; p == 1 || (may_split && p <= 256 && p <= all / 2); p += 1 + p / 4) {
+      if (p > 1 && tiles * p > 8 * CUS) break;  // enough for every CU
       const double per = (double)((all + p - 1) / p), q = ceil(tiles * p / CUS);
       double us;
       if (tile == 0) {
@@ -1176,6 +1182,13 @@ hipError_t product(Product g, int tile, hipStream_t s) {
     if (e_ != hipSuccess) return e_;     \
   } while (0)
 
+// Bytes between rows of an operand, at most: 255 of them fit 32 bits.  (Copies
+// and dS keep to it by FST_HEAD_MAX_COLS, dS with twice as many columns of 16
+// bits and DS_GAP.)
+constexpr long long ROW_BYTES = 1 << 24;
+static_assert(255 * (ROW_BYTES + 1024) < (1ll << 32) && FST_HEAD_MAX_COLS * 4ll <= ROW_BYTES,
+              "offsets in a tile");
+
 // An operand whose rows are whole K-steps from aligned addresses, as it is or
 // copied so.
 template <typename T>
@@ -1189,7 +1202,8 @@ struct Laid {
 template <typename T>
 Laid<T> lay(const Mat &m, Bump &b) {
   const long long cols = up(m.cols, k_step<T>());
-  if ((uintptr_t)m.data % 16 == 0 && m.stride * sizeof(T) % 16 == 0 && cols == m.cols)
+  if ((uintptr_t)m.data % 16 == 0 && m.stride * sizeof(T) % 16 == 0 && cols == m.cols &&
+      m.stride * (long long)sizeof(T) <= ROW_BYTES)
     return {{m.data, m.stride, m.rows, cols}, nullptr, cols};
   T *p = b.take<T>(m.rows * cols);
   return {{p, cols, m.rows, cols}, p, cols};
@@ -1450,7 +1464,9 @@ hipError_t loss_grads_as(const Mat &x, const Mat &w, const int32_t *target, cons
     return hipGetLastError();
   }
   const Laid<T> lx = lay<T>(x, b), lw = lay<T>(w, b);
-  const long long piece = piece_of(V, H, PIECE_BYTES / (N * (long long)sizeof(T)));
+  long long most_words = PIECE_BYTES / (N * (long long)sizeof(T));
+  if (most_words > FST_HEAD_MAX_COLS) most_words = FST_HEAD_MAX_COLS;
+  const long long piece = piece_of(V, H, most_words);
   const bool whole = piece == V, two = whole && in_two<T>(N, V, H);
   const long long Pp = up(piece, 64);
   // a piece of `n` words from v0 on

@@ -49,6 +49,7 @@ FST_BF16 = 2
 FST_RECURRENCE_MAX_SEQS = 1 << 22
 FST_RECURRENCE_SAVE_ROWS = 64
 FST_HEAD_MAX_ROWS = 1 << 25
+FST_HEAD_MAX_COLS = 1 << 22
 
 PHASES = ("preprocess", "forward", "backward", "count", "fill")
 

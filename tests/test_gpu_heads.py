@@ -464,3 +464,27 @@ def test_refusals(comp):
     assert lib.fst_cross_entropy_grads(comp._h, mx, mw, p(t), None, None, mx, mw, s) == bad
     big = gpu._Matrix(x.data_ptr(), gpu.FST_HEAD_MAX_ROWS + 1, 8, 8, gpu.FST_F32)
     assert lib.fst_emission_weights(comp._h, mx, big, p(f), s) == gpu.FST_ERR_TOO_LARGE
+    wide = gpu._Matrix(x.data_ptr(), 1, gpu.FST_HEAD_MAX_COLS + 1, gpu.FST_HEAD_MAX_COLS + 1,
+                       gpu.FST_F32)
+    assert lib.fst_emission_weights(comp._h, wide, wide, p(f), s) == gpu.FST_ERR_TOO_LARGE
+    assert lib.fst_cross_entropy(comp._h, wide, wide, p(t), p(f), p(f), s) == gpu.FST_ERR_TOO_LARGE
+    many = gpu._Matrix(w.data_ptr(), gpu.FST_HEAD_MAX_COLS + 1, 8, 8, gpu.FST_F32)
+    assert lib.fst_emission_weights(comp._h, mx, many, p(f), s) == gpu.FST_ERR_TOO_LARGE
+
+
+def test_rows_far_apart(comp):
+    """Rows 16 MiB and more apart (offsets in a tile past 32 bits) are copied;
+    the same numbers as of rows side by side."""
+    step = (1 << 22) + 64  # float32: 16 MiB and 256 bytes
+    room = torch.zeros(300 * step, device="cuda")
+    x = room.as_strided((300, 64), (step, 1))
+    x.copy_(torch.randn(300, 64, device="cuda"))
+    w = torch.randn(70, 64, device="cuda")
+    t = torch.arange(300, dtype=torch.int32, device="cuda") % 70
+    near = x.contiguous()
+    assert torch.equal(comp.emission_weights(x, w), comp.emission_weights(near, w))
+    a, b = comp.cross_entropy(x, w, t), comp.cross_entropy(near, w, t)
+    assert torch.equal(a["loss"], b["loss"])
+    for p, q in zip(comp.cross_entropy_grads(x, w, t, a["lse"]),
+                    comp.cross_entropy_grads(near, w, t, b["lse"])):
+        assert torch.equal(p, q)
