@@ -317,26 +317,30 @@ __device__ __forceinline__ void epilogue(const Product &g, float4v (&acc)[FM][FN
                                          long long n0, int tn, int wm, int wn, int split,
                                          int lane);
 
+template <int BM, int BN>
+constexpr int STAGE_BYTES = (BM + BN) * KBYTES;
+
 // Tiles of BM x BN where there are too few large ones: STAGES buffers, the loads
 // of the STAGES - 1 next steps under way while one step's fragments are
 // multiplied.  Two where several workgroups a CU fill each other's gaps (three
 // or four, which leave room for fewer, took 5 to 60 % longer); four for the
 // narrow tiles of emissions, whose steps are nothing but waiting for loads.
 template <typename T, int LAYOUT, int BM, int BN, int WM, int WN, int STAGES, int EPI>
-__global__ __launch_bounds__(WM *WN *WAVE) void k_product(Product g) {
+__device__ __forceinline__ void product_tile(const Product &g, unsigned id, int split,
+                                             char *s_lds) {
   constexpr int NWV = WM * WN, FM = BM / WM / 16, FN = BN / WN / 16;
   using A = TileA<T, LAYOUT, BM, NWV, Rows<BM, BM>>;
   // (whole rows are put together in LDS: any order of their columns will do)
   constexpr int SIDE = EPI == EPI_LOG ? 4 : 16 / (int)sizeof(T);
   using B = TileB<T, LAYOUT, BN, NWV, Spread<SIDE, FN, FN>, Rows<BN, BN>>;
-  __shared__ __align__(1024) char s_lds[STAGES][A::BYTES + B::BYTES];
+  constexpr int STAGE = A::BYTES + B::BYTES, ROOM = STAGES * STAGE;
+  static_assert(STAGE == STAGE_BYTES<BM, BN>, "LDS of a step");
   const int lane = threadIdx.x & (WAVE - 1);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
   const int wm = wave / WN, wn = wave % WN;
   int tm, tn;
-  tile_of(g, blockIdx.x, tm, tn);
+  tile_of(g, id, tm, tn);
   const long long m0 = (long long)tm * BM, n0 = (long long)tn * BN;
-  const int split = blockIdx.z;
 
   A ta;
   B tb;
@@ -344,13 +348,13 @@ __global__ __launch_bounds__(WM *WN *WAVE) void k_product(Product g) {
   tb.init(g.B, 0, wave, lane);
   const char *pa = A::base(g.A, m0), *pb = B::base(g.B, n0);
   const long long na = A::bytes(g.A, m0), nb = B::bytes(g.B, n0);
-  const uint32_t lds = lds_address(s_lds[0]);
+  const uint32_t lds = lds_address(s_lds);
   const int all = (int)((g.K + k_step<T>() - 1) / k_step<T>());
   const int first = split * g.steps;
   const int end = all - first < g.steps ? all : first + g.steps;
   // (past the end: of empty buffers, so that there are always as many loads)
   const auto fetch = [&](int stage, int t) {
-    const uint32_t to = lds + stage * (A::BYTES + B::BYTES);
+    const uint32_t to = lds + stage * STAGE;
     const int4v ba = A::step(g.A, pa, t < end ? na : 0, t);
     const int4v bb = B::step(g.B, pb, t < end ? nb : 0, t);
 #pragma unroll
@@ -372,7 +376,7 @@ __global__ __launch_bounds__(WM *WN *WAVE) void k_product(Product g) {
     wait_loads<(STAGES - 2) * (A::LOADS + B::LOADS)>();
     __syncthreads();
     fetch(cur ? cur - 1 : STAGES - 1, t + STAGES - 1);
-    const char *sa = s_lds[cur], *sb = sa + A::BYTES;
+    const char *sa = s_lds + cur * STAGE, *sb = sa + A::BYTES;
     cur = cur == STAGES - 1 ? 0 : cur + 1;
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
@@ -392,7 +396,7 @@ __global__ __launch_bounds__(WM *WN *WAVE) void k_product(Product g) {
     // rows of log-probabilities, put together in LDS: the rows of a tile lie
     // side by side in memory (ldo is N)
     static_assert(LAYOUT == ROWS_ROWS && FM == 1, "a wavefront has 16 rows");
-    static_assert(BM * BN * 4 <= (int)sizeof(s_lds), "room for the tile");
+    static_assert(BM * BN * 4 <= ROOM, "room for the tile");
     __shared__ float2 s_row[WN][BM];
     constexpr int L = 4 * FN;
     const int group = lane >> 4, cols = (int)g.N, row = wm * 16 + (lane & 15);
@@ -432,8 +436,8 @@ __global__ __launch_bounds__(WM *WN *WAVE) void k_product(Product g) {
   } else if (EPI == EPI_RESULT && g.wide == 2 && !g.sums && n0 + BN <= g.N) {
     // results by way of LDS, so that whole rows of the tile are written
     constexpr int E = 16 / (int)sizeof(T), PITCH = BN + E, CHUNKS = BN / E;
-    constexpr int ROWS = (int)sizeof(s_lds) / (PITCH * (int)sizeof(T)) < BM ? BM / 2 : BM;
-    static_assert(ROWS * PITCH * (int)sizeof(T) <= (int)sizeof(s_lds), "room for the rows");
+    constexpr int ROWS = ROOM / (PITCH * (int)sizeof(T)) < BM ? BM / 2 : BM;
+    static_assert(ROWS * PITCH * (int)sizeof(T) <= ROOM, "room for the rows");
     const float back = g.scale ? 1.0f / *g.scale : 1.0f;
     T *s = reinterpret_cast<T *>(s_lds);
 #pragma unroll
@@ -465,6 +469,26 @@ __global__ __launch_bounds__(WM *WN *WAVE) void k_product(Product g) {
     }
   } else {
     epilogue<T, LAYOUT, WN, FM, FN, EPI>(g, acc, m0, n0, tn, wm, wn, split, lane);
+  }
+}
+
+template <typename T, int LAYOUT, int BM, int BN, int WM, int WN, int STAGES, int EPI>
+__global__ __launch_bounds__(WM *WN *WAVE) void k_product(Product g) {
+  __shared__ __align__(1024) char s_lds[STAGES * STAGE_BYTES<BM, BN>];
+  product_tile<T, LAYOUT, BM, BN, WM, WN, STAGES, EPI>(g, blockIdx.x, blockIdx.z, s_lds);
+}
+
+// Both products of dS in one launch, dx's tiles first: where neither fills the
+// card, its workgroups find a CU at once (two of them share one).
+template <typename T, int BM, int BN, int WM, int WN, int EPIX, int EPIW>
+__global__ __launch_bounds__(WM *WN *WAVE) void k_products(Product dx, Product dw) {
+  __shared__ __align__(1024) char s_lds[2 * STAGE_BYTES<BM, BN>];
+  const unsigned nx = (unsigned)dx.tiles_m * dx.tiles_n, id = blockIdx.x;
+  if (id < nx * dx.splits) {
+    product_tile<T, ROWS_COLS, BM, BN, WM, WN, 2, EPIX>(dx, id % nx, id / nx, s_lds);
+  } else {
+    const unsigned nw = (unsigned)dw.tiles_m * dw.tiles_n, at = id - nx * dx.splits;
+    product_tile<T, COLS_COLS, BM, BN, WM, WN, 2, EPIW>(dw, at % nw, at / nw, s_lds);
   }
 }
 
@@ -1125,12 +1149,13 @@ struct Cut {
 // longer than that.  Splitting costs a launch and the sums' way to memory and
 // back.
 template <typename T>
-Cut cut_for(long long M, long long N, long long K, bool may_split) {
+Cut cut_for(long long M, long long N, long long K, bool may_split, int only = -1) {
   const long long all = (K + k_step<T>() - 1) / k_step<T>();
   const bool wide = sizeof(T) == 4;
   Cut best{0, 1, (int)(all < 1 ? 1 : all)};
   double least = 1e30;
   for (int tile = 0; tile < 3; ++tile) {
+    if (only >= 0 && tile != only) continue;
     const double tiles = (double)((M + TILES[tile].bm - 1) / TILES[tile].bm) *
                          (double)((N + TILES[tile].bn - 1) / TILES[tile].bn);
     for (long long p = 1; p == 1 || (may_split && p <= 256 && p <= all / 2); p += 1 + p / 4) {
@@ -1241,9 +1266,8 @@ struct SplitProduct {
     cut = cut_for<T>(M, N, K, true);
     sums = cut.splits > 1 ? b.take<float>(cut.splits * M * up(N, 4)) : nullptr;
   }
-  hipError_t run(Operand A, Operand B, long long M, long long N, long long K, const float *scale,
-                 const Mat &out, hipStream_t s) const {
-    if (M == 0 || N == 0) return hipSuccess;
+  Product of(Operand A, Operand B, long long M, long long N, long long K, const float *scale,
+             const Mat &out) const {
     Product g{};
     g.A = A;
     g.B = B;
@@ -1257,15 +1281,27 @@ struct SplitProduct {
       g.ldo = out.stride;
       g.wide = wide<T>(out);
       g.scale = scale;
-      return product<T, LAYOUT, EPI_RESULT>(g, cut.tile, s);
+      return g;
     }
     g.out = sums;
     g.ldo = up(N, 4);
     g.wide = 1;
-    TRY((product<T, LAYOUT, EPI_SUM>(g, cut.tile, s)));
-    k_finish<T><<<blocks_for(M * up(N, 4), 4 * WAVE), NT, 0, s>>>(
-        sums, cut.splits, M, N, scale, static_cast<T *>(out.data), out.stride);
+    return g;
+  }
+  hipError_t finish(long long M, long long N, const float *scale, const Mat &out,
+                    hipStream_t s) const {
+    if (cut.splits > 1)
+      k_finish<T><<<blocks_for(M * up(N, 4), 4 * WAVE), NT, 0, s>>>(
+          sums, cut.splits, M, N, scale, static_cast<T *>(out.data), out.stride);
     return hipGetLastError();
+  }
+  hipError_t run(Operand A, Operand B, long long M, long long N, long long K, const float *scale,
+                 const Mat &out, hipStream_t s) const {
+    if (M == 0 || N == 0) return hipSuccess;
+    const Product g = of(A, B, M, N, K, scale, out);
+    if (cut.splits == 1) return product<T, LAYOUT, EPI_RESULT>(g, cut.tile, s);
+    TRY((product<T, LAYOUT, EPI_SUM>(g, cut.tile, s)));
+    return finish(M, N, scale, out, s);
   }
 };
 
@@ -1303,6 +1339,58 @@ struct Gradients {
       dx_k = 2 * Cp;
       dw_k = 2 * Ns;
     }
+  }
+};
+
+template <typename T, int BM, int BN, int WM, int WN>
+void products(const Product &x, const Product &w, unsigned grid, hipStream_t s) {
+  if (x.splits > 1 && w.splits > 1)
+    k_products<T, BM, BN, WM, WN, EPI_SUM, EPI_SUM><<<grid, WM * WN * WAVE, 0, s>>>(x, w);
+  else if (x.splits > 1)
+    k_products<T, BM, BN, WM, WN, EPI_SUM, EPI_RESULT><<<grid, WM * WN * WAVE, 0, s>>>(x, w);
+  else if (w.splits > 1)
+    k_products<T, BM, BN, WM, WN, EPI_RESULT, EPI_SUM><<<grid, WM * WN * WAVE, 0, s>>>(x, w);
+  else
+    k_products<T, BM, BN, WM, WN, EPI_RESULT, EPI_RESULT><<<grid, WM * WN * WAVE, 0, s>>>(x, w);
+}
+
+// dx (N x H) and dw (C x H) from dS, those that there are.
+template <typename T>
+struct Both {
+  SplitProduct<T, ROWS_COLS> x;
+  SplitProduct<T, COLS_COLS> w;
+  bool one;  // launch
+
+  void plan(const Gradients<T> &p, bool gx, bool gw, long long N, long long C, long long H,
+            Bump &b) {
+    if (gx) x.plan(N, H, p.dx_k, b);
+    if (gw) w.plan(C, H, p.dw_k, b);
+    one = gx && gw && H && x.cut.tile && x.cut.tile == w.cut.tile;
+  }
+  hipError_t run(const Gradients<T> &p, const Mat *gx, const Mat *gw, long long N, long long C,
+                 long long H, const float *scale, hipStream_t s) const {
+    if (!one) {
+      if (gx) TRY(x.run(p.dx_a, p.dx_b, N, H, p.dx_k, scale, *gx, s));
+      if (gw) TRY(w.run(p.dw_a, p.dw_b, C, H, p.dw_k, scale, *gw, s));
+      return hipSuccess;
+    }
+    const Tile c = TILES[x.cut.tile];
+    Product dx = x.of(p.dx_a, p.dx_b, N, H, p.dx_k, scale, *gx);
+    Product dw = w.of(p.dw_a, p.dw_b, C, H, p.dw_k, scale, *gw);
+    long long grid = 0;
+    for (Product *g : {&dx, &dw}) {
+      g->tiles_m = (int)((g->M + c.bm - 1) / c.bm);
+      g->tiles_n = (int)((g->N + c.bn - 1) / c.bn);
+      grid += (long long)g->tiles_m * g->tiles_n * g->splits;
+    }
+    if (grid * 512 >= (1ll << 32)) return hipErrorInvalidValue;
+    if (x.cut.tile == 1)
+      products<T, 128, 128, 4, 2>(dx, dw, (unsigned)grid, s);
+    else
+      products<T, 64, 64, 2, 2>(dx, dw, (unsigned)grid, s);
+    TRY(hipGetLastError());
+    TRY(x.finish(N, H, scale, *gx, s));
+    return w.finish(C, H, scale, *gw, s);
   }
 };
 
@@ -1378,10 +1466,8 @@ hipError_t emission_grads_as(const Mat &x, const Mat &w, const float *weight, co
   constexpr int GROUPS = 256;
   float *most = b.take<float>(GROUPS), *scale = b.take<float>(1);
   const Gradients<T> p(ds, ld, N, Cp, two, lw.columns(), lx.columns());
-  SplitProduct<T, ROWS_COLS> px{};
-  SplitProduct<T, COLS_COLS> pw{};
-  if (gx) px.plan(N, H, p.dx_k, b);
-  if (gw) pw.plan(C, H, p.dw_k, b);
+  Both<T> both{};
+  both.plan(p, gx, gw, N, C, H, b);
   if (!b.base) return hipSuccess;
   TRY(fill(gw ? &lx : nullptr, x, gx ? &lw : nullptr, w, s));
   if (std::is_same<T, f16>::value) {
@@ -1397,9 +1483,7 @@ hipError_t emission_grads_as(const Mat &x, const Mat &w, const float *weight, co
   else
     k_emission_ds<T><<<(unsigned)((N + 3) / 4), NT, 0, s>>>(weight, grad, N, C, scale, ds, Cp, ld);
   TRY(hipGetLastError());
-  if (gx) TRY(px.run(p.dx_a, p.dx_b, N, H, p.dx_k, scale, *gx, s));
-  if (gw) TRY(pw.run(p.dw_a, p.dw_b, C, H, p.dw_k, scale, *gw, s));
-  return hipSuccess;
+  return both.run(p, gx, gw, N, C, H, scale, s);
 }
 
 template <typename T>
@@ -1478,14 +1562,14 @@ hipError_t loss_grads_as(const Mat &x, const Mat &w, const int32_t *target, cons
   T *ds = b.take<T>(N * ((two ? 2 : 1) * Pp + DS_GAP));
   constexpr int GROUPS = 256;
   float *most_g = b.take<float>(GROUPS), *scale = b.take<float>(1);
-  SplitProduct<T, ROWS_COLS> px{};
-  SplitProduct<T, COLS_COLS> pw{};
+  Both<T> both{};
+  SplitProduct<T, COLS_COLS> &pw = both.w;
   float *sums = nullptr;
-  if (gx && whole) px.plan(N, H, products(ds, 0, V).dx_k, b);
+  if (whole) both.plan(products(ds, 0, V), gx, gw, N, V, H, b);
   if (gx && !whole) sums = b.take<float>(N * up(H, 4));
   const size_t mark = b.at;
   size_t most = mark;
-  if (gw) {
+  if (gw && !whole) {
     for (long long v0 = 0; v0 < V; v0 += piece) {
       const long long n = V - v0 < piece ? V - v0 : piece;
       b.at = mark;
@@ -1528,9 +1612,8 @@ hipError_t loss_grads_as(const Mat &x, const Mat &w, const int32_t *target, cons
     g.scale = scale;
     g.Np = np;
     TRY((product<T, ROWS_ROWS, EPI_DS>(g, cut_for<T>(N, n, lx.cols, false).tile, s)));
-    if (gx && whole) {
-      TRY(px.run(p.dx_a, p.dx_b, N, H, p.dx_k, scale, *gx, s));
-    } else if (gx) {
+    if (whole) return both.run(p, gx, gw, N, V, H, scale, s);
+    if (gx) {
       Product q{};
       q.A = p.dx_a;
       q.B = p.dx_b;
