@@ -478,18 +478,21 @@ __global__ __launch_bounds__(WM *WN *WAVE) void k_product(Product g) {
   product_tile<T, LAYOUT, BM, BN, WM, WN, STAGES, EPI>(g, blockIdx.x, blockIdx.z, s_lds);
 }
 
-// Both products of dS in one launch, dx's tiles first: where neither fills the
-// card, its workgroups find a CU at once (two of them share one).
+// Both products of dS in one launch, the tiles with the longer sums first: where
+// neither fills the card, its workgroups find a CU at once (two of them share
+// one), and none is left to work alone at the end.
 template <typename T, int BM, int BN, int WM, int WN, int EPIX, int EPIW>
 __global__ __launch_bounds__(WM *WN *WAVE) void k_products(Product dx, Product dw) {
   __shared__ __align__(1024) char s_lds[2 * STAGE_BYTES<BM, BN>];
-  const unsigned nx = (unsigned)dx.tiles_m * dx.tiles_n, id = blockIdx.x;
-  if (id < nx * dx.splits) {
-    product_tile<T, ROWS_COLS, BM, BN, WM, WN, 2, EPIX>(dx, id % nx, id / nx, s_lds);
-  } else {
-    const unsigned nw = (unsigned)dw.tiles_m * dw.tiles_n, at = id - nx * dx.splits;
-    product_tile<T, COLS_COLS, BM, BN, WM, WN, 2, EPIW>(dw, at % nw, at / nw, s_lds);
-  }
+  const unsigned tx = (unsigned)dx.tiles_m * dx.tiles_n, nx = tx * dx.splits;
+  const unsigned tw = (unsigned)dw.tiles_m * dw.tiles_n, nw = tw * dw.splits;
+  const bool x_first = dx.steps >= dw.steps;
+  const unsigned first = x_first ? nx : nw, at = blockIdx.x;
+  const unsigned id = at < first ? at : at - first;
+  if ((at < first) == x_first)
+    product_tile<T, ROWS_COLS, BM, BN, WM, WN, 2, EPIX>(dx, id % tx, id / tx, s_lds);
+  else
+    product_tile<T, COLS_COLS, BM, BN, WM, WN, 2, EPIW>(dw, id % tw, id / tw, s_lds);
 }
 
 __device__ __forceinline__ void meet() {
@@ -1137,6 +1140,7 @@ constexpr Tile TILES[3] = {{256, 256, 4}, {128, 128, 2}, {64, 64, 2}};
 // How a product is cut: the tile, and the parts of its sum.
 struct Cut {
   int tile, splits, steps;
+  double us;
 };
 
 // The cut that takes least, by a model in microseconds fitted to products of
@@ -1152,7 +1156,7 @@ template <typename T>
 Cut cut_for(long long M, long long N, long long K, bool may_split, int only = -1) {
   const long long all = (K + k_step<T>() - 1) / k_step<T>();
   const bool wide = sizeof(T) == 4;
-  Cut best{0, 1, (int)(all < 1 ? 1 : all)};
+  Cut best{0, 1, (int)(all < 1 ? 1 : all), 0};
   double least = 1e30;
   for (int tile = 0; tile < 3; ++tile) {
     if (only >= 0 && tile != only) continue;
@@ -1174,7 +1178,7 @@ Cut cut_for(long long M, long long N, long long K, bool may_split, int only = -1
       if (p > 1) us += 3.5 + (double)p * M * N * 8 / 4e6;
       if (us < least) {
         least = us;
-        best = {tile, 1, (int)((all + p - 1) / p)};
+        best = {tile, 1, (int)((all + p - 1) / p), us};
         best.splits = all ? (int)((all + best.steps - 1) / best.steps) : 1;
         if (best.steps < 1) best.steps = 1;
       }
@@ -1261,9 +1265,12 @@ struct SplitProduct {
   float *sums;
 
   void plan(long long M, long long N, long long K, Bump &b) {
-    cut = {0, 1, 1};
+    cut = {0, 1, 1, 0};
     if (M == 0 || N == 0) return;
     cut = cut_for<T>(M, N, K, true);
+    room(M, N, b);
+  }
+  void room(long long M, long long N, Bump &b) {
     sums = cut.splits > 1 ? b.take<float>(cut.splits * M * up(N, 4)) : nullptr;
   }
   Product of(Operand A, Operand B, long long M, long long N, long long K, const float *scale,
@@ -1354,7 +1361,11 @@ void products(const Product &x, const Product &w, unsigned grid, hipStream_t s) 
     k_products<T, BM, BN, WM, WN, EPI_RESULT, EPI_RESULT><<<grid, WM * WN * WAVE, 0, s>>>(x, w);
 }
 
-// dx (N x H) and dw (C x H) from dS, those that there are.
+// dx (N x H) and dw (C x H) from dS, those that are wanted: cut the same way
+// whether or not the other one is.  In one launch unless one of them has the
+// largest tiles (2000 rows, 1000 columns, width 512: 34 us as two, 27 as one;
+// 16,000, 69, 512: 29 and 22); tiles of 128 if they would differ in 16 bits (64:
+// 27 us of the last), in float32 what the model says of both.
 template <typename T>
 struct Both {
   SplitProduct<T, ROWS_COLS> x;
@@ -1363,9 +1374,24 @@ struct Both {
 
   void plan(const Gradients<T> &p, bool gx, bool gw, long long N, long long C, long long H,
             Bump &b) {
-    if (gx) x.plan(N, H, p.dx_k, b);
-    if (gw) w.plan(C, H, p.dw_k, b);
-    one = gx && gw && H && x.cut.tile && x.cut.tile == w.cut.tile;
+    if (H == 0) return;
+    x.cut = cut_for<T>(N, H, p.dx_k, true);
+    w.cut = cut_for<T>(C, H, p.dw_k, true);
+    one = x.cut.tile && w.cut.tile;
+    if (one && x.cut.tile != w.cut.tile) {
+      double least = 1e30;
+      for (int tile = 1; tile <= (sizeof(T) == 2 ? 1 : 2); ++tile) {
+        const Cut cx = cut_for<T>(N, H, p.dx_k, true, tile);
+        const Cut cw = cut_for<T>(C, H, p.dw_k, true, tile);
+        if (cx.us + cw.us >= least) continue;
+        least = cx.us + cw.us;
+        x.cut = cx;
+        w.cut = cw;
+      }
+    }
+    one = one && gx && gw;
+    if (gx) x.room(N, H, b);
+    if (gw) w.room(C, H, b);
   }
   hipError_t run(const Gradients<T> &p, const Mat *gx, const Mat *gw, long long N, long long C,
                  long long H, const float *scale, hipStream_t s) const {
