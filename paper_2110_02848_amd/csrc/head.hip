@@ -849,11 +849,18 @@ struct Pad {
   T *out;
 };
 template <typename T>
-__global__ __launch_bounds__(NT) void k_pad(Pad<T> x, Pad<T> w) {
+struct Pads {
+  Pad<T> x, w;
+  long long groups() const { return (x.rows * x.cols + w.rows * w.cols) / (16 / (int)sizeof(T)); }
+};
+// (workgroup `block` of `blocks`)
+template <typename T>
+__device__ __forceinline__ void pad(const Pads<T> &pads, unsigned block, unsigned blocks) {
   constexpr int E = 16 / (int)sizeof(T);
+  const Pad<T> &x = pads.x, &w = pads.w;
   const long long nx = x.rows * (x.cols / E), nw = w.rows * (w.cols / E);
-  for (long long i = (long long)blockIdx.x * NT + threadIdx.x; i < nx + nw;
-       i += (long long)gridDim.x * NT) {
+  for (long long i = (long long)block * blockDim.x + threadIdx.x; i < nx + nw;
+       i += (long long)blocks * blockDim.x) {
     const Pad<T> &m = i < nx ? x : w;
     const long long q = i < nx ? i : i - nx, groups = m.cols / E;
     const long long r = q / groups, c = (q - r * groups) * E;
@@ -867,6 +874,10 @@ __global__ __launch_bounds__(NT) void k_pad(Pad<T> x, Pad<T> w) {
     }
     *reinterpret_cast<int4v *>(m.out + r * m.cols + c) = *reinterpret_cast<const int4v *>(v);
   }
+}
+template <typename T>
+__global__ __launch_bounds__(NT) void k_pad(Pads<T> pads) {
+  pad(pads, blockIdx.x, gridDim.x);
 }
 
 __device__ __forceinline__ float wave_sum_f(float v) {
@@ -1006,13 +1017,16 @@ __device__ __forceinline__ void put_ds(T *to, const float (&d)[E], long long lo)
 }
 
 // dS = grad - exp(weight) sum(grad), zeros up to Cp columns; a wavefront a row.
+// Workgroups past the first `blocks` make the copies (one launch less).
 template <typename T>
-__global__ __launch_bounds__(NT) void k_emission_ds(const float *__restrict__ weight,
+__global__ __launch_bounds__(NT) void k_emission_ds(Pads<T> pads, unsigned blocks,
+                                                    const float *__restrict__ weight,
                                                     const float *__restrict__ grad,
                                                     long long rows, long long cols,
                                                     const float *__restrict__ scale,
                                                     T *__restrict__ out, long long Cp,
                                                     long long ld) {
+  if (blockIdx.x >= blocks) return pad(pads, blockIdx.x - blocks, gridDim.x - blocks);
   constexpr int E = 16 / (int)sizeof(T);
   const int lane = threadIdx.x & (WAVE - 1);
   const long long r = (long long)blockIdx.x * NWAVES + threadIdx.x / WAVE;
@@ -1036,11 +1050,13 @@ __global__ __launch_bounds__(NT) void k_emission_ds(const float *__restrict__ we
 // side by side, by way of LDS.
 constexpr int SHORT = 256;
 template <typename T>
-__global__ __launch_bounds__(NT) void k_emission_ds_short(const float *__restrict__ weight,
+__global__ __launch_bounds__(NT) void k_emission_ds_short(Pads<T> pads, unsigned blocks,
+                                                          const float *__restrict__ weight,
                                                           const float *__restrict__ grad,
                                                           long long rows, int cols,
                                                           const float *__restrict__ scale,
                                                           T *__restrict__ out, int Cp, int ld) {
+  if (blockIdx.x >= blocks) return pad(pads, blockIdx.x - blocks, gridDim.x - blocks);
   constexpr int E = 16 / (int)sizeof(T);
   __shared__ float s_w[16 * SHORT], s_g[16 * SHORT];
   __shared__ float s_sum[16];
@@ -1078,21 +1094,31 @@ __global__ __launch_bounds__(NT) void k_emission_ds_short(const float *__restric
 // split by its four wavefronts in turn, added in a fixed order.  (Rows of
 // `sums` are padded to whole groups.)
 template <typename T>
-__global__ __launch_bounds__(NT) void k_finish(const float *__restrict__ sums, int splits,
-                                               long long rows, long long cols,
-                                               const float *__restrict__ scale,
-                                               T *__restrict__ out, long long ldo) {
+struct Finish {
+  const float *sums;
+  int splits;
+  long long rows, cols;
+  T *out;
+  long long ldo;
+  __host__ __device__ long long groups() const { return rows * ((cols + 3) / 4); }
+};
+// (of two products, or of one: b has no rows)
+template <typename T>
+__global__ __launch_bounds__(NT) void k_finish(Finish<T> a, Finish<T> b,
+                                               const float *__restrict__ scale) {
   __shared__ float4v s_sum[NWAVES][WAVE];
   const int lane = threadIdx.x & (WAVE - 1), w = threadIdx.x / WAVE;
   const float back = scale ? 1.0f / *scale : 1.0f;
-  const long long groups = (cols + 3) / 4, all = rows * groups;
-  for (long long i0 = (long long)blockIdx.x * WAVE; i0 < all; i0 += (long long)gridDim.x * WAVE) {
-    const long long i = i0 + lane;
+  const long long na = (a.groups() + WAVE - 1) / WAVE, nb = (b.groups() + WAVE - 1) / WAVE;
+  for (long long k = blockIdx.x; k < na + nb; k += gridDim.x) {
+    const Finish<T> &f = k < na ? a : b;
+    const long long i = (k < na ? k : k - na) * WAVE + lane, all = f.groups();
+    const long long groups = (f.cols + 3) / 4;
     float4v v = {0, 0, 0, 0};
     if (i < all) {
 #pragma unroll 8
-      for (int s = w; s < splits; s += NWAVES)
-        v += reinterpret_cast<const float4v *>(sums)[s * all + i];
+      for (int s = w; s < f.splits; s += NWAVES)
+        v += reinterpret_cast<const float4v *>(f.sums)[s * all + i];
     }
     s_sum[w][lane] = v;
     __syncthreads();
@@ -1102,7 +1128,7 @@ __global__ __launch_bounds__(NT) void k_finish(const float *__restrict__ sums, i
       const long long r = i / groups, c = (i - r * groups) * 4;
 #pragma unroll
       for (int e = 0; e < 4; ++e)
-        if (c + e < cols) out[r * ldo + c + e] = (T)(v[e] * back);
+        if (c + e < f.cols) f.out[r * f.ldo + c + e] = (T)(v[e] * back);
     }
     __syncthreads();
   }
@@ -1237,17 +1263,23 @@ Laid<T> lay(const Mat &m, Bump &b) {
   T *p = b.take<T>(m.rows * cols);
   return {{p, cols, m.rows, cols}, p, cols};
 }
-// The copies there are, in one launch.
+// The copies there are to make.
 template <typename T>
-hipError_t fill(const Laid<T> *lx, const Mat &x, const Laid<T> *lw, const Mat &w, hipStream_t s) {
-  Pad<T> px{}, pw{};
+Pads<T> copies(const Laid<T> *lx, const Mat &x, const Laid<T> *lw, const Mat &w) {
+  Pads<T> p{};
   if (lx && lx->copy)
-    px = {static_cast<const T *>(x.data), x.stride, x.rows, x.cols, lx->cols, lx->copy};
+    p.x = {static_cast<const T *>(x.data), x.stride, x.rows, x.cols, lx->cols, lx->copy};
   if (lw && lw->copy)
-    pw = {static_cast<const T *>(w.data), w.stride, w.rows, w.cols, lw->cols, lw->copy};
-  const long long groups = (px.rows * px.cols + pw.rows * pw.cols) / (16 / (int)sizeof(T));
-  if (!groups) return hipSuccess;
-  k_pad<T><<<blocks_for(groups, NT), NT, 0, s>>>(px, pw);
+    p.w = {static_cast<const T *>(w.data), w.stride, w.rows, w.cols, lw->cols, lw->copy};
+  return p;
+}
+template <typename T>
+unsigned pad_blocks(const Pads<T> &p) {
+  return p.groups() ? blocks_for(p.groups(), NT) : 0;
+}
+template <typename T>
+hipError_t fill(const Pads<T> &p, hipStream_t s) {
+  if (const unsigned n = pad_blocks(p)) k_pad<T><<<n, NT, 0, s>>>(p);
   return hipGetLastError();
 }
 
@@ -1256,6 +1288,19 @@ template <typename T>
 int wide(const Mat &m) {
   if ((uintptr_t)m.data % 16 == 0 && m.stride * sizeof(T) % 16 == 0) return 2;
   return (uintptr_t)m.data % (4 * sizeof(T)) == 0 && m.stride % 4 == 0;
+}
+
+template <typename T>
+hipError_t finish(const Finish<T> &a, const Finish<T> &b, const float *scale, hipStream_t s) {
+  const long long n = (a.groups() + WAVE - 1) / WAVE + (b.groups() + WAVE - 1) / WAVE;
+  if (n) k_finish<T><<<blocks_for(n, 1), NT, 0, s>>>(a, b, scale);
+  return hipGetLastError();
+}
+// Zeros: the sum of nothing.
+template <typename T>
+hipError_t clear(const Mat &out, hipStream_t s) {
+  return finish<T>({nullptr, 0, out.rows, out.cols, static_cast<T *>(out.data), out.stride}, {},
+                   nullptr, s);
 }
 
 // out = A B^T, its sum in parts where that takes less.
@@ -1295,12 +1340,9 @@ struct SplitProduct {
     g.wide = 1;
     return g;
   }
-  hipError_t finish(long long M, long long N, const float *scale, const Mat &out,
-                    hipStream_t s) const {
-    if (cut.splits > 1)
-      k_finish<T><<<blocks_for(M * up(N, 4), 4 * WAVE), NT, 0, s>>>(
-          sums, cut.splits, M, N, scale, static_cast<T *>(out.data), out.stride);
-    return hipGetLastError();
+  Finish<T> rest(const Mat &out) const {  // what is left to do: nothing where nothing was cut
+    return {sums, cut.splits, cut.splits > 1 ? out.rows : 0, out.cols, static_cast<T *>(out.data),
+            out.stride};
   }
   hipError_t run(Operand A, Operand B, long long M, long long N, long long K, const float *scale,
                  const Mat &out, hipStream_t s) const {
@@ -1308,7 +1350,7 @@ struct SplitProduct {
     const Product g = of(A, B, M, N, K, scale, out);
     if (cut.splits == 1) return product<T, LAYOUT, EPI_RESULT>(g, cut.tile, s);
     TRY((product<T, LAYOUT, EPI_SUM>(g, cut.tile, s)));
-    return finish(M, N, scale, out, s);
+    return finish(rest(out), {}, scale, s);
   }
 };
 
@@ -1415,8 +1457,7 @@ struct Both {
     else
       products<T, 64, 64, 2, 2>(dx, dw, (unsigned)grid, s);
     TRY(hipGetLastError());
-    TRY(x.finish(N, H, scale, *gx, s));
-    return w.finish(C, H, scale, *gw, s);
+    return finish(x.rest(*gx), w.rest(*gw), scale, s);
   }
 };
 
@@ -1447,7 +1488,7 @@ hipError_t emission_as(const Mat &x, const Mat &w, float *weight, Bump &b, hipSt
   const int parts = (int)((C + TILES[cut.tile].bn - 1) / TILES[cut.tile].bn) * TILES[cut.tile].wn;
   float2 *part = b.take<float2>(whole ? 1 : N * parts);
   if (!b.base) return hipSuccess;
-  TRY(fill(&lx, x, &lw, w, s));
+  TRY(fill(copies(&lx, x, &lw, w), s));
   Product g{};
   g.A = lx.o;
   g.B = lw.o;
@@ -1479,11 +1520,9 @@ hipError_t emission_grads_as(const Mat &x, const Mat &w, const float *weight, co
   const long long N = x.rows, C = w.rows, H = x.cols;
   const long long Cp = up(C, 64);
   if (N == 0) {  // nothing to sum over
-    if (b.base && gw && C * H)
-      k_finish<T><<<blocks_for(C * up(H, 4), 4 * WAVE), NT, 0, s>>>(nullptr, 0, C, H, nullptr,
-                                                     static_cast<T *>(gw->data), gw->stride);
+    if (b.base && gw) TRY(clear<T>(*gw, s));
     b.take<char>(1);
-    return hipGetLastError();
+    return hipSuccess;
   }
   const Laid<T> lx = lay<T>(x, b), lw = lay<T>(w, b);
   const bool two = in_two<T>(N, C, H);
@@ -1495,7 +1534,6 @@ hipError_t emission_grads_as(const Mat &x, const Mat &w, const float *weight, co
   Both<T> both{};
   both.plan(p, gx, gw, N, C, H, b);
   if (!b.base) return hipSuccess;
-  TRY(fill(gw ? &lx : nullptr, x, gx ? &lw : nullptr, w, s));
   if (std::is_same<T, f16>::value) {
     const unsigned n = blocks_for(N, NWAVES, GROUPS);
     k_emission_max<<<n, NT, 0, s>>>(grad, N, C, most);
@@ -1503,11 +1541,14 @@ hipError_t emission_grads_as(const Mat &x, const Mat &w, const float *weight, co
   } else {
     scale = nullptr;
   }
+  const Pads<T> pads = copies(gw ? &lx : nullptr, x, gx ? &lw : nullptr, w);
+  const unsigned n = (unsigned)(C <= SHORT ? (N + 15) / 16 : (N + 3) / 4);
   if (C <= SHORT)
-    k_emission_ds_short<T><<<(unsigned)((N + 15) / 16), NT, 0, s>>>(weight, grad, N, (int)C, scale,
-                                                                  ds, (int)Cp, (int)ld);
+    k_emission_ds_short<T><<<n + pad_blocks(pads), NT, 0, s>>>(pads, n, weight, grad, N, (int)C,
+                                                               scale, ds, (int)Cp, (int)ld);
   else
-    k_emission_ds<T><<<(unsigned)((N + 3) / 4), NT, 0, s>>>(weight, grad, N, C, scale, ds, Cp, ld);
+    k_emission_ds<T><<<n + pad_blocks(pads), NT, 0, s>>>(pads, n, weight, grad, N, C, scale, ds,
+                                                         Cp, ld);
   TRY(hipGetLastError());
   return both.run(p, gx, gw, N, C, H, scale, s);
 }
@@ -1522,7 +1563,7 @@ hipError_t loss_as(const Mat &x, const Mat &w, const int32_t *target, float *los
   float2 *part = b.take<float2>(N * parts);
   float *hit = b.take<float>(N);
   if (!b.base) return hipSuccess;
-  TRY(fill(&lx, x, &lw, w, s));
+  TRY(fill(copies(&lx, x, &lw, w), s));
   Product g{};
   g.A = lx.o;
   g.B = lw.o;
@@ -1567,11 +1608,9 @@ hipError_t loss_grads_as(const Mat &x, const Mat &w, const int32_t *target, cons
                          hipStream_t s) {
   const long long N = x.rows, V = w.rows, H = x.cols;
   if (N == 0) {  // nothing to sum over
-    if (b.base && gw && V * H)
-      k_finish<T><<<blocks_for(V * up(H, 4), 4 * WAVE), NT, 0, s>>>(nullptr, 0, V, H, nullptr,
-                                                     static_cast<T *>(gw->data), gw->stride);
+    if (b.base && gw) TRY(clear<T>(*gw, s));
     b.take<char>(1);
-    return hipGetLastError();
+    return hipSuccess;
   }
   const Laid<T> lx = lay<T>(x, b), lw = lay<T>(w, b);
   long long most_words = PIECE_BYTES / (N * (long long)sizeof(T));
@@ -1605,7 +1644,7 @@ hipError_t loss_grads_as(const Mat &x, const Mat &w, const int32_t *target, cons
   }
   b.at = most;
   if (!b.base) return hipSuccess;
-  TRY(fill(&lx, x, &lw, w, s));
+  TRY(fill(copies(&lx, x, &lw, w), s));
   if (std::is_same<T, f16>::value) {
     const bool one = !grad || N <= 65536;
     if (!one) k_scale<<<GROUPS, 1024, 0, s>>>(grad, target, N, most_g);
