@@ -270,11 +270,11 @@ __global__ __launch_bounds__(NW *WAVE) void k_rec_units(RecArgs a) {
 // ---------------------------------------------------------------------------
 
 // A workgroup walks its unit tile by tile: from each chunk's map and the state
-// before the tile every wavefront knows its first state.  Bound by memory with
-// a vector unit that is nearly as busy (64 sequences of up to 2000 x 1024 bf16:
-// 146 us, 4.1 TB/s of three streams; a large copy reaches 5.0), by the barrier
-// and the loads of each tile where there are few workgroups (6 sequences of
-// up to 211 x 333 float32: 11 us, 36 workgroups).
+// before the tile every wavefront knows its first state.  Bound by memory (64
+// sequences of up to 2000 x 1024 bf16, 1500 on average: 146 us, 4.1 TB/s of three
+// streams, although the shorter sequences' workgroups end first; a large copy
+// reaches 5.0), by the barrier and the loads of each tile where there are few
+// workgroups (6 sequences of up to 211 x 333 float32: 11 us, 36 workgroups).
 template <typename T, int V, int NW>
 __global__ __launch_bounds__(NW *WAVE) void k_rec_forward(RecArgs a) {
   __shared__ float2 s_map[2][NW][V][WAVE];
