@@ -329,6 +329,7 @@ class Composer:
         self._pass = _Marshal()
         self._raw_stream = torch._C._cuda_getCurrentRawStream
         self._empty = torch.empty
+        self._f32, self._i32 = torch.float32, torch.int32
 
     def close(self):
         if getattr(self, "_h", None):
@@ -606,13 +607,12 @@ class Composer:
         of rows of x and gate ([N, D], offset int32 [n + 1]) from state
         (float32 [n, D], None: 0): dict(y: as x, last: the states after each
         sequence, saved: what ``recurrence_grads`` needs, with ``save``)."""
-        import torch
         R, n = self._recurrence(x, gate, offset, state, reverse)
         N, D = x.shape
         y = self._new(stream, (N, D), x.dtype)
-        last = self._new(stream, (n, D), torch.float32)
+        last = self._new(stream, (n, D), self._f32)
         saved = self._new(stream, (N // FST_RECURRENCE_SAVE_ROWS + n, D),
-                          torch.float32) if save else None
+                          self._f32) if save else None
         self._uses(stream, x, gate, offset, state)
         rc = self._lib.fst_recurrence_run(self._h, R, self._pass.made(0, y, _types[y.dtype]), _address(last),
                                           _address(saved), self._call_stream(stream))
@@ -624,29 +624,27 @@ class Composer:
         """Gradients of a loss by x, gate and state from those by y and last
         (``recurrence`` of the same arguments with ``save``): dict(x, gate:
         as x, state: float32 [n, D])."""
-        import torch
         R, n = self._recurrence(x, gate, offset, state, reverse)
         N, D = x.shape
         rows = N // FST_RECURRENCE_SAVE_ROWS + n
         gx, gu = self._new(stream, (N, D), x.dtype), self._new(stream, (N, D), x.dtype)
-        gs = self._new(stream, (n, D), torch.float32)
+        gs = self._new(stream, (n, D), self._f32)
         self._uses(stream, x, gate, offset, grad_y, saved, state, grad_last)
         rc = self._lib.fst_recurrence_grads(
-            self._h, R, _array(saved, "saved", torch.float32, rows * D),
+            self._h, R, _array(saved, "saved", self._f32, rows * D),
             self._pass.matrix(0, grad_y, "grad_y"),
-            _array(grad_last, "grad_last", torch.float32, n * D), self._pass.made(1, gx, _types[x.dtype]),
+            _array(grad_last, "grad_last", self._f32, n * D), self._pass.made(1, gx, _types[x.dtype]),
             self._pass.made(2, gu, _types[x.dtype]), _address(gs), self._call_stream(stream))
         _check(rc, "fst_recurrence_grads")
         return dict(x=gx, gate=gu, state=gs)
 
     def _recurrence(self, x, gate, offset, state, reverse):
-        import torch
         n = int(offset.numel()) - 1
         if n < 0:
             raise ValueError("offset: at least one entry is needed")
-        R = self._pass.recurrence(n, _array(offset, "offset", torch.int32, n + 1),
+        R = self._pass.recurrence(n, _array(offset, "offset", self._i32, n + 1),
                                   int(bool(reverse)), x, gate,
-                                  _array(state, "state", torch.float32, n * x.shape[-1]))
+                                  _array(state, "state", self._f32, n * x.shape[-1]))
         return R, n
 
     def recurrence_step(self, x, gate, state, slot=None, out=None, stream=None):
@@ -655,17 +653,22 @@ class Composer:
         a new tensor.  With slot (int32 [n]) state holds any number of rows,
         row i's is slot[i] (an idle row's lies outside), and the new states
         replace the old ones unless ``out`` is given."""
-        import torch
-        slots, D = state.shape[0], x.shape[-1]
-        if out is None:
-            out = self._new(stream, (slots, D), torch.float32) if slot is None else state
-        y = self._new(stream, x.shape, x.dtype)
-        self._uses(stream, x, gate, state, slot, out)
+        shape = x.shape
+        slots, D = state.shape[0], shape[-1]
+        from_ = _array(state, "state", self._f32, slots * D)
+        if out is not None and out is not state:
+            to = _array(out, "out", self._f32, slots * D)
+        elif out is state or slot is not None:
+            out, to = state, from_
+        else:
+            out = self._new(stream, (slots, D), self._f32)
+            to = _address(out)
+        y = self._new(stream, shape, x.dtype)
+        if stream is not None:
+            self._uses(stream, x, gate, state, slot, out)
         rc = self._lib.fst_recurrence_step(
-            self._h, self._pass.matrix(0, x, "x"), self._pass.matrix(1, gate, "gate"),
-            _array(state, "state", torch.float32, slots * D),
-            _array(out, "out", torch.float32, slots * D),
-            _array(slot, "slot", torch.int32, x.shape[0]), slots,
+            self._h, self._pass.matrix(0, x, "x"), self._pass.matrix(1, gate, "gate"), from_, to,
+            _array(slot, "slot", self._i32, shape[0]), slots,
             self._pass.made(2, y, _types[x.dtype]), self._call_stream(stream))
         _check(rc, "fst_recurrence_step")
         return y, out
@@ -673,14 +676,15 @@ class Composer:
     def emission_weights(self, x, w, out=None, stream=None):
         """Log-softmax of x w^T, float32 [N, C] (x [N, H], w [C, H]): the arc
         weights of emission graphs.  ``out`` may be a graph's weight tensor."""
-        import torch
-        N, C = int(x.shape[0]), int(w.shape[0])
+        N, C = x.shape[0], w.shape[0]
         if out is None:
-            out = self._new(stream, (N, C), torch.float32)
+            out = self._new(stream, (N, C), self._f32)
+            to = _address(out)
+        else:
+            to = _array(out, "out", self._f32, N * C)
         self._uses(stream, x, w, out)
         rc = self._lib.fst_emission_weights(self._h, self._pass.matrix(0, x, "x"),
-                                            self._pass.matrix(1, w, "w"),
-                                            _array(out, "out", torch.float32, N * C),
+                                            self._pass.matrix(1, w, "w"), to,
                                             self._call_stream(stream))
         _check(rc, "fst_emission_weights")
         return out
@@ -688,13 +692,12 @@ class Composer:
     def emission_grads(self, x, w, weight, grad, need_x=True, need_w=True, stream=None):
         """Gradients by x and w (None where not needed) from the gradient by
         the weights of ``emission_weights`` (grad: float32, N * C)."""
-        import torch
         n = int(x.shape[0]) * int(w.shape[0])
         gx, gw = self._head_grads(x, w, need_x, need_w, stream)
         self._uses(stream, x, w, weight, grad)
         rc = self._lib.fst_emission_grads(
             self._h, self._pass.matrix(0, x, "x"), self._pass.matrix(1, w, "w"),
-            _array(weight, "weight", torch.float32, n), _array(grad, "grad", torch.float32, n),
+            _array(weight, "weight", self._f32, n), _array(grad, "grad", self._f32, n),
             self._pass.made(2, gx, _types[x.dtype]) if need_x else None,
             self._pass.made(3, gw, _types[w.dtype]) if need_w else None, self._call_stream(stream))
         _check(rc, "fst_emission_grads")
@@ -703,14 +706,13 @@ class Composer:
     def cross_entropy(self, x, w, target, stream=None):
         """Cross entropy of x w^T (x [N, H], w [V, H]) against target (int32
         [N], -1: no word): dict(loss, lse: float32 [N])."""
-        import torch
         N = int(x.shape[0])
-        loss = self._new(stream, (N,), torch.float32)
-        lse = self._new(stream, (N,), torch.float32)
+        loss = self._new(stream, (N,), self._f32)
+        lse = self._new(stream, (N,), self._f32)
         self._uses(stream, x, w, target)
         rc = self._lib.fst_cross_entropy(self._h, self._pass.matrix(0, x, "x"),
                                          self._pass.matrix(1, w, "w"),
-                                         _array(target, "target", torch.int32, N),
+                                         _array(target, "target", self._i32, N),
                                          _address(loss), _address(lse),
                                          self._call_stream(stream))
         _check(rc, "fst_cross_entropy")
@@ -720,14 +722,13 @@ class Composer:
                             stream=None):
         """Gradients of sum(grad * loss) by x and w (None where not needed);
         grad: float32 [N], None: 1."""
-        import torch
         N = int(x.shape[0])
         gx, gw = self._head_grads(x, w, need_x, need_w, stream)
         self._uses(stream, x, w, target, lse, grad)
         rc = self._lib.fst_cross_entropy_grads(
             self._h, self._pass.matrix(0, x, "x"), self._pass.matrix(1, w, "w"),
-            _array(target, "target", torch.int32, N), _array(lse, "lse", torch.float32, N),
-            _array(grad, "grad", torch.float32, N),
+            _array(target, "target", self._i32, N), _array(lse, "lse", self._f32, N),
+            _array(grad, "grad", self._f32, N),
             self._pass.made(2, gx, _types[x.dtype]) if need_x else None,
             self._pass.made(3, gw, _types[w.dtype]) if need_w else None, self._call_stream(stream))
         _check(rc, "fst_cross_entropy_grads")
