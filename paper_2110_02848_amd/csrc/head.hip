@@ -320,15 +320,15 @@ __device__ __forceinline__ void epilogue(const Product &g, float4v (&acc)[FM][FN
 template <int BM, int BN>
 constexpr int STAGE_BYTES = (BM + BN) * KBYTES;
 
-// Tiles of BM x BN where there are too few large ones: STAGES buffers, the loads
-// of the STAGES - 1 next steps under way while one step's fragments are
-// multiplied.  Two where several workgroups a CU fill each other's gaps (three
-// or four, which leave room for fewer, took 5 to 60 % longer); four for the
-// narrow tiles of emissions, whose steps are nothing but waiting for loads (16,000
-// x 69 over 512 bf16: 9 us for 21 MB; 1266 x 41 over 333 float32: 8).  Bound by
-// that waiting and by the rounds of tiles (1053 x 7919 over 509 f16: 18 us, 0.46
-// Pflop/s, matrix cores busy 15 % of the time; 558 tiles for 512 places).
-template <typename T, int LAYOUT, int BM, int BN, int WM, int WN, int STAGES, int EPI>
+// Tiles of BM x BN where there are too few large ones: two buffers, the loads of
+// the next step under way while one step's fragments are multiplied, and several
+// workgroups a CU that fill each other's gaps (three or four buffers, which leave
+// room for fewer, took 5 to 60 % longer: 64,000 x 120 over 512 bf16, tiles of 32 x
+// 128: 42 us with four, 27 with two).  Bound by the wait for loads and by the rounds
+// of tiles (1053 x 7919 over 509 f16: 18 us, 0.46 Pflop/s, matrix cores busy 15 % of
+// the time; 558 tiles for 512 places).  Whole rows of 16,000 x 69 over 512 bf16: 8 us
+// for 21 MB; of 1266 x 41 over 333 float32: 8.
+template <typename T, int LAYOUT, int BM, int BN, int WM, int WN, int EPI>
 __device__ __forceinline__ void product_tile(const Product &g, unsigned id, int split,
                                              char *s_lds) {
   constexpr int NWV = WM * WN, FM = BM / WM / 16, FN = BN / WN / 16;
@@ -336,7 +336,7 @@ __device__ __forceinline__ void product_tile(const Product &g, unsigned id, int 
   // (whole rows are put together in LDS: any order of their columns will do)
   constexpr int SIDE = EPI == EPI_LOG ? 4 : 16 / (int)sizeof(T);
   using B = TileB<T, LAYOUT, BN, NWV, Spread<SIDE, FN, FN>, Rows<BN, BN>>;
-  constexpr int STAGE = A::BYTES + B::BYTES, ROOM = STAGES * STAGE;
+  constexpr int STAGE = A::BYTES + B::BYTES, ROOM = 2 * STAGE;
   static_assert(STAGE == STAGE_BYTES<BM, BN>, "LDS of a step");
   const int lane = threadIdx.x & (WAVE - 1);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
@@ -371,16 +371,15 @@ __device__ __forceinline__ void product_tile(const Product &g, unsigned id, int 
   for (int i = 0; i < FM; ++i)
 #pragma unroll
     for (int j = 0; j < FN; ++j) acc[i][j] = float4v{0, 0, 0, 0};
-#pragma unroll
-  for (int s = 0; s < STAGES - 1; ++s) fetch(s, first + s);
+  fetch(0, first);
   int cur = 0;
   for (int t = first; t < end; ++t) {
     // step t has landed, and no one reads the buffer of the step before
-    wait_loads<(STAGES - 2) * (A::LOADS + B::LOADS)>();
+    wait_loads<0>();
     __syncthreads();
-    fetch(cur ? cur - 1 : STAGES - 1, t + STAGES - 1);
+    fetch(cur ^ 1, t + 1);
     const char *sa = s_lds + cur * STAGE, *sb = sa + A::BYTES;
-    cur = cur == STAGES - 1 ? 0 : cur + 1;
+    cur ^= 1;
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
       Frag<T> fa[FM], fb[FN];
@@ -475,10 +474,10 @@ __device__ __forceinline__ void product_tile(const Product &g, unsigned id, int 
   }
 }
 
-template <typename T, int LAYOUT, int BM, int BN, int WM, int WN, int STAGES, int EPI>
+template <typename T, int LAYOUT, int BM, int BN, int WM, int WN, int EPI>
 __global__ __launch_bounds__(WM *WN *WAVE) void k_product(Product g) {
-  __shared__ __align__(1024) char s_lds[STAGES * STAGE_BYTES<BM, BN>];
-  product_tile<T, LAYOUT, BM, BN, WM, WN, STAGES, EPI>(g, blockIdx.x, blockIdx.z, s_lds);
+  __shared__ __align__(1024) char s_lds[2 * STAGE_BYTES<BM, BN>];
+  product_tile<T, LAYOUT, BM, BN, WM, WN, EPI>(g, blockIdx.x, blockIdx.z, s_lds);
 }
 
 // Both products of dS in one launch, the tiles with the longer sums first: where
@@ -495,9 +494,9 @@ __global__ __launch_bounds__(WM *WN *WAVE) void k_products(Product dx, Product d
   const unsigned first = x_first ? nx : nw, at = blockIdx.x;
   const unsigned id = at < first ? at : at - first;
   if ((at < first) == x_first)
-    product_tile<T, ROWS_COLS, BM, BN, WM, WN, 2, EPIX>(dx, id % tx, id / tx, s_lds);
+    product_tile<T, ROWS_COLS, BM, BN, WM, WN, EPIX>(dx, id % tx, id / tx, s_lds);
   else
-    product_tile<T, COLS_COLS, BM, BN, WM, WN, 2, EPIW>(dw, id % tw, id / tw, s_lds);
+    product_tile<T, COLS_COLS, BM, BN, WM, WN, EPIW>(dw, id % tw, id / tw, s_lds);
 }
 
 __device__ __forceinline__ void meet() {
@@ -1232,9 +1231,9 @@ hipError_t product(Product g, int tile, hipStream_t s) {
     k_product_large<T, LAYOUT, EPI>
         <<<dim3((unsigned)(tm * tn < CUS ? tm * tn : CUS), 1, (unsigned)g.splits), 512, 0, s>>>(g);
   else if (tile == 1)
-    k_product<T, LAYOUT, 128, 128, 4, 2, 2, EPI><<<grid, 512, 0, s>>>(g);
+    k_product<T, LAYOUT, 128, 128, 4, 2, EPI><<<grid, 512, 0, s>>>(g);
   else
-    k_product<T, LAYOUT, 64, 64, 2, 2, 2, EPI><<<grid, 256, 0, s>>>(g);
+    k_product<T, LAYOUT, 64, 64, 2, 2, EPI><<<grid, 256, 0, s>>>(g);
   return hipGetLastError();
 }
 
@@ -1477,20 +1476,27 @@ template <typename T>
 void log_rows(const Product &g, hipStream_t s) {
   const unsigned grid = (unsigned)g.tiles_m;
   if (g.N <= 32)
-    k_product<T, ROWS_ROWS, 32, 32, 2, 2, 4, EPI_LOG><<<grid, 4 * WAVE, 0, s>>>(g);
+    k_product<T, ROWS_ROWS, 32, 32, 2, 2, EPI_LOG><<<grid, 4 * WAVE, 0, s>>>(g);
   else if (g.N <= 64)
-    k_product<T, ROWS_ROWS, 32, 64, 2, 2, 4, EPI_LOG><<<grid, 4 * WAVE, 0, s>>>(g);
+    k_product<T, ROWS_ROWS, 32, 64, 2, 2, EPI_LOG><<<grid, 4 * WAVE, 0, s>>>(g);
   else if (g.N <= 96)
-    k_product<T, ROWS_ROWS, 32, 96, 2, 2, 4, EPI_LOG><<<grid, 4 * WAVE, 0, s>>>(g);
+    k_product<T, ROWS_ROWS, 32, 96, 2, 2, EPI_LOG><<<grid, 4 * WAVE, 0, s>>>(g);
+  else if (g.N <= 128)
+    k_product<T, ROWS_ROWS, 32, 128, 2, 2, EPI_LOG><<<grid, 4 * WAVE, 0, s>>>(g);
+  else if (g.N <= 192)
+    k_product<T, ROWS_ROWS, 32, 192, 2, 2, EPI_LOG><<<grid, 4 * WAVE, 0, s>>>(g);
   else
-    k_product<T, ROWS_ROWS, 32, 128, 2, 2, 4, EPI_LOG><<<grid, 4 * WAVE, 0, s>>>(g);
+    k_product<T, ROWS_ROWS, 32, 256, 2, 2, EPI_LOG><<<grid, 4 * WAVE, 0, s>>>(g);
 }
 
 template <typename T>
 hipError_t emission_as(const Mat &x, const Mat &w, float *weight, Bump &b, hipStream_t s) {
   const long long N = x.rows, C = w.rows;
   const Laid<T> lx = lay<T>(x, b), lw = lay<T>(w, b);
-  const bool whole = C <= 128;  // a tile takes whole rows
+  // a tile takes whole rows; past 128 classes in float32 only where there is one
+  // for every CU (500 x 200 over 1024: 45 us whole, 28 by 64 and normalised after;
+  // 13,637 x 250 over 286: 39 and 47, in bf16 21 and 39)
+  const bool whole = C <= 128 || (C <= 256 && (sizeof(T) == 2 || N >= 32 * CUS));
   const Cut cut = cut_for<T>(N, C, lx.cols, false);
   const int parts = (int)((C + TILES[cut.tile].bn - 1) / TILES[cut.tile].bn) * TILES[cut.tile].wn;
   float2 *part = b.take<float2>(whole ? 1 : N * parts);

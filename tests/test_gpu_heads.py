@@ -488,3 +488,12 @@ def test_rows_far_apart(comp):
     for p, q in zip(comp.cross_entropy_grads(x, w, t, a["lse"]),
                     comp.cross_entropy_grads(near, w, t, b["lse"])):
         assert torch.equal(p, q)
+
+
+# whole rows of up to 256 classes, in float32 past 128 only of many rows
+@pytest.mark.parametrize("typ", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("N,C,H", [(1, 129, 64), (33, 192, 70), (70, 193, 128), (45, 256, 100),
+                                   (8191, 150, 40), (8193, 150, 40), (8200, 256, 64),
+                                   (8192, 193, 33), (40, 257, 64)])
+def test_emission_wide_rows(comp, N, C, H, typ):
+    _emission(comp, N, C, H, typ)
