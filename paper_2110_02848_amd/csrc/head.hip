@@ -326,7 +326,7 @@ constexpr int STAGE_BYTES = (BM + BN) * KBYTES;
 // room for fewer, took 5 to 60 % longer: 64,000 x 120 over 512 bf16, tiles of 32 x
 // 128: 42 us with four, 27 with two).  Bound by the wait for loads and by the rounds
 // of tiles (1053 x 7919 over 509 f16: 18 us, 0.46 Pflop/s, matrix cores busy 15 % of
-// the time; 558 tiles for 512 places).  Whole rows of 16,000 x 69 over 512 bf16: 8 us
+// the time; 558 tiles for 512 places).  Whole rows of 16,000 x 69 over 512 bf16: 9 us
 // for 21 MB; of 1266 x 41 over 333 float32: 8.
 template <typename T, int LAYOUT, int BM, int BN, int WM, int WN, int EPI>
 __device__ __forceinline__ void product_tile(const Product &g, unsigned id, int split,
@@ -816,7 +816,8 @@ __device__ __forceinline__ void epilogue(const Product &g, float4v (&acc)[FM][FN
 #pragma unroll
       for (int j = 0; j < FN; ++j) {
         const long long n = n0 + wn * FN * 16 +
-                            (LAYOUT == ROWS_ROWS ? Spread<16 / (int)sizeof(T), FN, FN>::column(group, 4 * j)
+                            (LAYOUT == ROWS_ROWS
+                                 ? Spread<16 / (int)sizeof(T), FN, FN>::column(group, 4 * j)
                                                  : j * 16 + group * 4);
         if (n >= g.N) continue;
         float4v v = acc[i][j];

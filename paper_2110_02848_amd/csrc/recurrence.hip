@@ -421,7 +421,8 @@ __global__ __launch_bounds__(NW *WAVE) void k_rec_backward(RecArgs a) {
         for (int k = 0; k < CHUNK; ++k)
           if (i + k >= u.hi)
 #pragma unroll
-            for (int c = 0; c < V; ++c) f[k][c] = 1.0f, g[k][c] = 0.0f, x[k][c] = 0.0f, D[k][c] = 0.0f;
+            for (int c = 0; c < V; ++c)
+              f[k][c] = 1.0f, g[k][c] = 0.0f, x[k][c] = 0.0f, D[k][c] = 0.0f;
       }
       if (i0 > u.lo) {
         fetch<T, V>(xr, a.x, a.xs, u, i - TILE, d);

@@ -614,8 +614,9 @@ class Composer:
         saved = self._new(stream, (N // FST_RECURRENCE_SAVE_ROWS + n, D),
                           self._f32) if save else None
         self._uses(stream, x, gate, offset, state)
-        rc = self._lib.fst_recurrence_run(self._h, R, self._pass.made(0, y, _types[y.dtype]), _address(last),
-                                          _address(saved), self._call_stream(stream))
+        rc = self._lib.fst_recurrence_run(self._h, R, self._pass.made(0, y, _types[y.dtype]),
+                                          _address(last), _address(saved),
+                                          self._call_stream(stream))
         _check(rc, "fst_recurrence_run")
         return dict(y=y, last=last, saved=saved)
 
@@ -633,8 +634,8 @@ class Composer:
         rc = self._lib.fst_recurrence_grads(
             self._h, R, _array(saved, "saved", self._f32, rows * D),
             self._pass.matrix(0, grad_y, "grad_y"),
-            _array(grad_last, "grad_last", self._f32, n * D), self._pass.made(1, gx, _types[x.dtype]),
-            self._pass.made(2, gu, _types[x.dtype]), _address(gs), self._call_stream(stream))
+            _array(grad_last, "grad_last", self._f32, n * D),
+            self._pass.made(1, gx, _types[x.dtype]), self._pass.made(2, gu, _types[x.dtype]), _address(gs), self._call_stream(stream))
         _check(rc, "fst_recurrence_grads")
         return dict(x=gx, gate=gu, state=gs)
 
