@@ -818,7 +818,7 @@ __device__ __forceinline__ void epilogue(const Product &g, float4v (&acc)[FM][FN
         const long long n = n0 + wn * FN * 16 +
                             (LAYOUT == ROWS_ROWS
                                  ? Spread<16 / (int)sizeof(T), FN, FN>::column(group, 4 * j)
-                                                 : j * 16 + group * 4);
+                                 : j * 16 + group * 4);
         if (n >= g.N) continue;
         float4v v = acc[i][j];
         if (EPI == EPI_RESULT && g.sums) {

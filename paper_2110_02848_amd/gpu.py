@@ -635,7 +635,8 @@ class Composer:
             self._h, R, _array(saved, "saved", self._f32, rows * D),
             self._pass.matrix(0, grad_y, "grad_y"),
             _array(grad_last, "grad_last", self._f32, n * D),
-            self._pass.made(1, gx, _types[x.dtype]), self._pass.made(2, gu, _types[x.dtype]), _address(gs), self._call_stream(stream))
+            self._pass.made(1, gx, _types[x.dtype]), self._pass.made(2, gu, _types[x.dtype]),
+            _address(gs), self._call_stream(stream))
         _check(rc, "fst_recurrence_grads")
         return dict(x=gx, gate=gu, state=gs)
 
