@@ -355,3 +355,74 @@ def test_refusals(comp):
     R2 = gpu._Recurrence(gpu.FST_RECURRENCE_MAX_SEQS + 1, R.offset, 0, R.x, R.gate, None)
     assert lib.fst_recurrence_run(comp._h, R2, M(x, "y"), None, None, s) == \
         gpu.FST_ERR_INVALID_ARG
+
+
+def _no_numbers(*tensors):
+    return [torch.isnan(t.float()).cpu() for t in tensors]
+
+
+@pytest.mark.parametrize("rev", [False, True])
+@pytest.mark.parametrize("where", ["x", "gate", "state"])
+@pytest.mark.parametrize("lens,D", [([70, 0, 133], 66), ([700], 64), ([9] * 255 + [100], 128)])
+@pytest.mark.parametrize("typ", ["f32", "f16", "bf16"])
+def test_what_is_no_number_goes_on(comp, typ, lens, D, where, rev):
+    """A NaN in x, gate or state comes out wherever the formulas carry it, and
+    nowhere else: whole sequences, one cut into units, two channels a lane."""
+    x, gate, gy, state, glast = _inputs(13, lens, D, typ)
+    off = _offsets(lens)
+    offset = torch.tensor(off, dtype=torch.int32, device="cuda")
+
+    def run():
+        r = comp.recurrence(x, gate, offset, state=state, reverse=rev, save=True)
+        g = comp.recurrence_grads(x, gate, offset, gy, r["saved"], state=state, grad_last=glast,
+                                  reverse=rev)
+        return [r["y"], r["last"], g["x"], g["gate"], g["state"]]
+    good = run()
+    t, r = dict(x=x, gate=gate, state=state)[where], 0 if where == "state" else 41
+    t[r, 7] = t[r, 62] = float("nan")
+    got = run()
+    X, G, GY, S, GL = [v.cpu().double() for v in (x, gate, gy, state, glast)]
+    want = _no_numbers(*ref.recurrence(X, G, off, S, rev),
+                       *ref.recurrence_grads(X, G, off, S, GY, GL, rev))
+    for a, b, m in zip(got, good, want):
+        assert m.any() or where != "gate"
+        assert torch.equal(_no_numbers(a)[0], m)
+        assert torch.equal(a.cpu()[~m], b.cpu()[~m])
+
+
+@pytest.mark.parametrize("D", [8, 7])
+@pytest.mark.parametrize("where", ["x", "gate", "state"])
+@pytest.mark.parametrize("typ", ["f32", "f16", "bf16"])
+def test_step_of_what_is_no_number(comp, typ, where, D):
+    x, gate, _, _, _ = _inputs(4, [5], D, typ)
+    state = torch.randn(5, D, device="cuda")
+    y0, s0 = comp.recurrence_step(x, gate, state)
+    dict(x=x, gate=gate, state=state)[where][2, 3] = float("nan")
+    y, s = comp.recurrence_step(x, gate, state)
+    m = torch.zeros(5, D, dtype=torch.bool)
+    m[2, 3] = True
+    for a, b in ((y, y0), (s, s0)):
+        assert torch.equal(_no_numbers(a)[0], m)
+        assert torch.equal(a.cpu()[~m], b.cpu()[~m])
+
+
+@pytest.mark.parametrize("typ", ["f16", "bf16"])
+def test_gates_at_their_ends_in_16_bits(comp, typ):
+    dt = ref.TYPES[typ]
+    big = torch.tensor([float("inf"), 200.0, -200.0, float("-inf")], device="cuda").to(dt)
+    x = torch.randn(40, 4, device="cuda").to(dt)
+    gate = big.expand(40, 4).contiguous()
+    state = torch.randn(1, 4, device="cuda")
+    off = torch.tensor([0, 40], dtype=torch.int32, device="cuda")
+    r = comp.recurrence(x, gate, off, state=state, save=True)
+    assert torch.equal(r["last"][:, :2], state[:, :2])
+    assert torch.equal(r["y"][:, :2], state[:, :2].to(dt).expand(40, 2))
+    assert torch.equal(r["y"][:, 2:], x[:, 2:]) and torch.equal(r["last"][0, 2:], x[-1, 2:].float())
+    g = comp.recurrence_grads(x, gate, off, torch.ones_like(x), r["saved"], state=state)
+    assert torch.isfinite(g["x"]).all() and torch.isfinite(g["gate"]).all()
+    assert torch.equal(g["state"][:, :2], torch.full((1, 2), 40.0, device="cuda"))
+    # (what keeps nothing keeps 2^-126 at most)
+    assert (g["state"][:, 2:].abs() <= 2.0 ** -126).all()
+    y, new = comp.recurrence_step(x[:1], gate[:1], state)
+    assert torch.equal(new[:, :2], state[:, :2]) and torch.equal(new[:, 2:], x[:1, 2:].float())
+    assert torch.equal(y, new.to(dt))
