@@ -514,7 +514,8 @@ FST_API int fst_recurrence_grads(fst_ctx *ctx, const fst_recurrence *R, const fl
  * is row slot[i] of state_in and state_out (device, float32, num_slots *
  * x.cols; slot NULL: row i, num_slots >= x.rows).  A slot outside [0,
  * num_slots) marks an idle row: its y is 0 and no state is read or written.
- * state_out may be state_in; slots of one call must differ. */
+ * Rows of state_out that no row of x names are left as they are.  state_out
+ * may be state_in; slots of one call must differ. */
 FST_API int fst_recurrence_step(fst_ctx *ctx, const fst_matrix *x, const fst_matrix *gate,
                                 const float *state_in, float *state_out, const int32_t *slot,
                                 int32_t num_slots, const fst_matrix *y, void *stream);

@@ -595,6 +595,14 @@ class Composer:
         with torch.cuda.stream(stream):
             return torch.empty(shape, dtype=dtype, device=self._dev)
 
+    def _copy(self, stream, to, from_):
+        if stream is None:
+            to.copy_(from_)
+            return
+        import torch
+        with torch.cuda.stream(stream):
+            to.copy_(from_)
+
     def _uses(self, stream, *tensors):
         """Tells the allocator that the stream of the call uses these."""
         if stream is not None:
@@ -651,10 +659,11 @@ class Composer:
 
     def recurrence_step(self, x, gate, state, slot=None, out=None, stream=None):
         """One step of the rows of x and gate ([n, D]): (y, new states).
-        state: float32 [n, D]; the new states go to ``out`` (may be state) or
-        a new tensor.  With slot (int32 [n]) state holds any number of rows,
-        row i's is slot[i] (an idle row's lies outside), and the new states
-        replace the old ones unless ``out`` is given."""
+        state: float32 [n, D], or more rows, which stay as they are; the new
+        states go to ``out`` (may be state) or a new tensor.  With slot (int32
+        [n]) state holds any number of rows, row i's is slot[i] (an idle row's
+        lies outside), and the new states replace the old ones unless ``out``
+        is given.  Rows of ``out`` that no row of x names are not written."""
         shape = x.shape
         slots, D = state.shape[0], shape[-1]
         from_ = _array(state, "state", self._f32, slots * D)
@@ -665,6 +674,8 @@ class Composer:
         else:
             out = self._new(stream, (slots, D), self._f32)
             to = _address(out)
+            if slots > shape[0]:  # states that this step leaves alone
+                self._copy(stream, out[shape[0]:], state.view(slots, D)[shape[0]:])
         y = self._new(stream, shape, x.dtype)
         if stream is not None:
             self._uses(stream, x, gate, state, slot, out)

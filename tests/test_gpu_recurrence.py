@@ -426,3 +426,34 @@ def test_gates_at_their_ends_in_16_bits(comp, typ):
     y, new = comp.recurrence_step(x[:1], gate[:1], state)
     assert torch.equal(new[:, :2], state[:, :2]) and torch.equal(new[:, 2:], x[:1, 2:].float())
     assert torch.equal(y, new.to(dt))
+
+
+@pytest.mark.parametrize("other", [False, True])
+def test_step_with_states_to_spare(comp, other):
+    """More states than rows: those that no row names keep their values in the
+    new tensor, and `out` keeps its own."""
+    D = 40
+    x, gate, _, _, _ = _inputs(2, [5], D, "f16")
+    pool = torch.randn(9, D, device="cuda")
+    s = torch.cuda.Stream() if other else None
+    torch.cuda.synchronize()
+    y1, want = comp.recurrence_step(x, gate, pool[:5].contiguous())
+    torch.full((9, D), 7.0, device="cuda")  # (what a new tensor may hold)
+    torch.cuda.synchronize()
+    before = pool.clone()
+    y, new = comp.recurrence_step(x, gate, pool, stream=s)
+    torch.cuda.synchronize()
+    assert torch.equal(y, y1) and torch.equal(new[:5], want) and torch.equal(new[5:], pool[5:])
+    assert new.shape == pool.shape and torch.equal(pool, before)
+    none, same = comp.recurrence_step(x[:0], gate[:0], pool, stream=s)
+    torch.cuda.synchronize()
+    assert none.shape == (0, D) and torch.equal(same, pool)
+    for slot in (None, torch.tensor([8, 0, -1, 9, 3], dtype=torch.int32, device="cuda")):
+        out = torch.full((9, D), 7.0, device="cuda")
+        torch.cuda.synchronize()
+        _, got = comp.recurrence_step(x, gate, pool, slot=slot, out=out, stream=s)
+        torch.cuda.synchronize()
+        rows = [0, 1, 2, 3, 4] if slot is None else [8, 0, 3]
+        assert got is out and torch.equal(pool, before)
+        assert (out[[i for i in range(9) if i not in rows]] == 7).all()
+        assert not (out[rows] == 7).any()
