@@ -1423,7 +1423,6 @@ struct Both {
 
   void plan(const Gradients<T> &p, bool gx, bool gw, long long N, long long C, long long H,
             Bump &b) {
-    if (H == 0) return;
     x.cut = cut_for<T>(N, H, p.dx_k, true);
     w.cut = cut_for<T>(C, H, p.dw_k, true);
     one = x.cut.tile && w.cut.tile;
@@ -1533,7 +1532,7 @@ hipError_t emission_grads_as(const Mat &x, const Mat &w, const float *weight, co
                              const Mat *gx, const Mat *gw, Bump &b, hipStream_t s) {
   const long long N = x.rows, C = w.rows, H = x.cols;
   const long long Cp = up(C, 64);
-  if (N == 0) {  // nothing to sum over
+  if (N == 0 || H == 0) {  // nothing to sum over, or nothing to write
     if (b.base && gw) TRY(clear<T>(*gw, s));
     b.take<char>(1);
     return hipSuccess;
@@ -1621,7 +1620,7 @@ hipError_t loss_grads_as(const Mat &x, const Mat &w, const int32_t *target, cons
                          const float *grad, const Mat *gx, const Mat *gw, Bump &b,
                          hipStream_t s) {
   const long long N = x.rows, V = w.rows, H = x.cols;
-  if (N == 0) {  // nothing to sum over
+  if (N == 0 || H == 0) {  // nothing to sum over, or nothing to write
     if (b.base && gw) TRY(clear<T>(*gw, s));
     b.take<char>(1);
     return hipSuccess;

@@ -497,3 +497,23 @@ def test_rows_far_apart(comp):
                                    (8192, 193, 33), (40, 257, 64)])
 def test_emission_wide_rows(comp, N, C, H, typ):
     _emission(comp, N, C, H, typ)
+
+
+@pytest.mark.parametrize("typ,N,V", [("f32", 5, 8), ("bf16", 3, 700), ("f32", 4096, 70001),
+                                     ("f16", 8192, 40000), ("bf16", 8192, 40000)])
+def test_no_columns(comp, typ, N, V):
+    """Nothing to score by, in one piece of the vocabulary and in several."""
+    print(f"[no columns] N={N} V={V} {typ}", flush=True)
+    dt = ref.TYPES[typ]
+    x, w = torch.empty(N, 0, dtype=dt, device="cuda"), torch.empty(V, 0, dtype=dt, device="cuda")
+    t = torch.arange(N, dtype=torch.int32, device="cuda") % V
+    t[1] = -1
+    r = comp.cross_entropy(x, w, t)
+    want = torch.full((N,), math.log(V), device="cuda")
+    torch.testing.assert_close(r["lse"], want, rtol=1e-6, atol=0)
+    want[1] = 0
+    torch.testing.assert_close(r["loss"], want, rtol=1e-6, atol=0)
+    gx, gw = comp.cross_entropy_grads(x, w, t, r["lse"])
+    assert gx.shape == (N, 0) and gw.shape == (V, 0)
+    assert comp.cross_entropy_grads(x, w, t, r["lse"], need_w=False)[0].shape == (N, 0)
+    assert comp.cross_entropy_grads(x, w, t, r["lse"], need_x=False)[1].shape == (V, 0)
