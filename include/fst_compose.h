@@ -454,7 +454,11 @@ FST_API int fst_compose3_stats(const fst_ctx *ctx, fst_stats *out);
  * results are rounded to their type once.  Results do not depend on anything but the
  * arguments (no atomic sums).  Calls are asynchronous on `stream` after a
  * call of the same sizes has made the workspace; they read nothing back, so
- * they can be captured into a HIP graph. */
+ * they can be captured into a HIP graph.  The workspace that a captured call
+ * uses stays allocated until the context is destroyed, beside a larger one
+ * that other calls may need (FST_OPT_MAX_WORKSPACE counts both): a graph may
+ * be replayed as long as the context lives.  A replay uses the workspace as a
+ * call does, so replays and calls of one context have to follow one another. */
 enum fst_type { FST_F32 = 0, FST_F16 = 1, FST_BF16 = 2 };
 
 /* Element (r, c) is data[r * stride + c] (device memory, caller-owned);

@@ -70,8 +70,12 @@ struct fst_ctx {
       s_mpos, s_sweep, s_chg, s_ioff, s_iarc;
   // batches: the union of the A graphs, item tables, segment sums
   DevBuf u_off, u_src, u_dst, u_il, u_ol, u_w, u_start, u_accept, u_items, seg;
-  // operators between a network and its graphs: one workspace a call
+  // operators between a network and its graphs: one workspace for a call.  One
+  // that a captured call uses stays where it is until the context goes, as the
+  // graph holds its address: what outgrows it is another one.
   DevBuf layer;
+  bool layer_kept = false;        // a captured call uses `layer`
+  std::vector<DevBuf> old_layers;  // ones that captured calls use, outgrown
   // three-input composition
   DevBuf t_scal, t_aPerm, t_aArc, t_aRec, t_bPerm, t_bArc, t_bRec, t_bLab, t_bW, t_dPerm,
       t_dArc, t_dRec, t_dLab, t_dW, t_bflags, t_lists, t_tab, t_F, t_chunks, t_arcs, t_inoff,
@@ -1982,12 +1986,57 @@ int hip_status(hipError_t e) {
   return e == hipErrorInvalidValue ? FST_ERR_TOO_LARGE : FST_ERR_HIP;
 }
 
+// Whether `s` is being captured into a graph.
+bool captured(hipStream_t s) {
+  hipStreamCaptureStatus st = hipStreamCaptureStatusNone;
+  if (hipStreamIsCapturing(s, &st) == hipSuccess) return st != hipStreamCaptureStatusNone;
+  (void)hipGetLastError();
+  return false;
+}
+
+// Memory may be allocated while the thread's streams are captured.
+struct RelaxedCapture {
+  hipStreamCaptureMode mode = hipStreamCaptureModeRelaxed;
+  bool on;
+  explicit RelaxedCapture(bool capture) : on(capture) {
+    if (on) on = hipThreadExchangeStreamCaptureMode(&mode) == hipSuccess;
+  }
+  ~RelaxedCapture() {
+    if (on) (void)hipThreadExchangeStreamCaptureMode(&mode);
+  }
+};
+
+// A workspace of `bytes` for a call that is being captured, or one that
+// outgrows a captured call's: the old one stays.
+int another_layer(fst_ctx *c, size_t bytes, bool capture) {
+  RelaxedCapture relaxed(capture);
+  DevBuf b;
+  try {
+    c->old_layers.reserve(c->old_layers.size() + 1);
+  } catch (const std::bad_alloc &) {
+    return FST_ERR_NOMEM;
+  }
+  FST_TRY(ensure(c, b, bytes));
+  if (c->layer.p) c->old_layers.push_back(c->layer);
+  c->layer = b;
+  c->layer_kept = false;
+  return FST_OK;
+}
+
 // Runs `f(workspace, &bytes)` twice: for the bytes it needs, then with them.
 template <typename F>
-int with_workspace(fst_ctx *c, F &&f) {
+int with_workspace(fst_ctx *c, hipStream_t s, F &&f) {
   size_t need = 0;
   FST_TRY(hip_status(f(nullptr, &need)));
-  FST_TRY(with_room(c, [&]() { return ensure(c, c->layer, need); }));
+  const bool capture = captured(s);
+  if (c->layer.cap < round_up(need ? need : 1) && (capture || c->layer_kept)) {
+    // (nothing can be waited for, and so freed, during a capture)
+    const auto more = [&]() { return another_layer(c, need, capture); };
+    FST_TRY(capture ? more() : with_room(c, more));
+  } else {
+    FST_TRY(with_room(c, [&]() { return ensure(c, c->layer, need); }));
+  }
+  c->layer_kept = c->layer_kept || (capture && need);
   return hip_status(f(c->layer.p, &need));
 }
 
@@ -2108,6 +2157,7 @@ void fst_ctx_destroy(fst_ctx *c) {
                     &c->t_heavy,  &c->t_aLut,   &c->t_bLut,  &c->t_dLut, &c->t_bChain,
                     &c->t_segs,   &c->t_segof, &c->layer};
   for (DevBuf *b : bufs) release(*b);
+  for (DevBuf &b : c->old_layers) release(b);
   for (ScoreBufs *sb : {&c->score_f, &c->score_b}) {
     for (DevBuf *b : {&sb->sc, &sb->rec, &sb->term, &sb->mkey, &sb->pend, &sb->q, &sb->h,
                       &sb->hoff})
@@ -2549,7 +2599,7 @@ int fst_recurrence_run(fst_ctx *c, const fst_recurrence *R, const fst_matrix *y,
   a.ys = y->stride;
   a.last = last;
   a.saved = saved;
-  return with_workspace(c, [&](void *ws, size_t *need) {
+  return with_workspace(c, reinterpret_cast<hipStream_t>(stream), [&](void *ws, size_t *need) {
     return launch_recurrence(a, R->x.type, ws, need, reinterpret_cast<hipStream_t>(stream));
   });
 }
@@ -2575,7 +2625,7 @@ int fst_recurrence_grads(fst_ctx *c, const fst_recurrence *R, const float *saved
   a.saved = const_cast<float *>(saved);
   a.glast = grad_last;
   a.gstate = grad_state;
-  return with_workspace(c, [&](void *ws, size_t *need) {
+  return with_workspace(c, reinterpret_cast<hipStream_t>(stream), [&](void *ws, size_t *need) {
     return launch_recurrence_grads(a, R->x.type, ws, need, reinterpret_cast<hipStream_t>(stream));
   });
 }
@@ -2615,7 +2665,7 @@ int fst_emission_weights(fst_ctx *c, const fst_matrix *x, const fst_matrix *w, f
   if (!weight) return FST_ERR_INVALID_ARG;
   DeviceGuard g(c->device);
   if (!g.ok) return FST_ERR_HIP;
-  return with_workspace(c, [&](void *ws, size_t *need) {
+  return with_workspace(c, reinterpret_cast<hipStream_t>(stream), [&](void *ws, size_t *need) {
     return launch_emission(mat(*x), mat(*w), weight, ws, need,
                            reinterpret_cast<hipStream_t>(stream));
   });
@@ -2632,7 +2682,7 @@ int fst_emission_grads(fst_ctx *c, const fst_matrix *x, const fst_matrix *w, con
   Mat gx, gw;
   if (grad_x) gx = mat(*grad_x);
   if (grad_w) gw = mat(*grad_w);
-  return with_workspace(c, [&](void *ws, size_t *need) {
+  return with_workspace(c, reinterpret_cast<hipStream_t>(stream), [&](void *ws, size_t *need) {
     return launch_emission_grads(mat(*x), mat(*w), weight, grad, grad_x ? &gx : nullptr,
                                  grad_w ? &gw : nullptr, ws, need,
                                  reinterpret_cast<hipStream_t>(stream));
@@ -2647,7 +2697,7 @@ int fst_cross_entropy(fst_ctx *c, const fst_matrix *x, const fst_matrix *w, cons
   if (!target || !loss || !lse) return FST_ERR_INVALID_ARG;
   DeviceGuard g(c->device);
   if (!g.ok) return FST_ERR_HIP;
-  return with_workspace(c, [&](void *ws, size_t *need) {
+  return with_workspace(c, reinterpret_cast<hipStream_t>(stream), [&](void *ws, size_t *need) {
     return launch_loss(mat(*x), mat(*w), target, loss, lse, ws, need,
                        reinterpret_cast<hipStream_t>(stream));
   });
@@ -2664,7 +2714,7 @@ int fst_cross_entropy_grads(fst_ctx *c, const fst_matrix *x, const fst_matrix *w
   Mat gx, gw;
   if (grad_x) gx = mat(*grad_x);
   if (grad_w) gw = mat(*grad_w);
-  return with_workspace(c, [&](void *ws, size_t *need) {
+  return with_workspace(c, reinterpret_cast<hipStream_t>(stream), [&](void *ws, size_t *need) {
     return launch_loss_grads(mat(*x), mat(*w), target, lse, grad, grad_x ? &gx : nullptr,
                              grad_w ? &gw : nullptr, ws, need,
                              reinterpret_cast<hipStream_t>(stream));

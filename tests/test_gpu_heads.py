@@ -517,3 +517,58 @@ def test_no_columns(comp, typ, N, V):
     assert gx.shape == (N, 0) and gw.shape == (V, 0)
     assert comp.cross_entropy_grads(x, w, t, r["lse"], need_w=False)[0].shape == (N, 0)
     assert comp.cross_entropy_grads(x, w, t, r["lse"], need_x=False)[1].shape == (V, 0)
+
+
+def test_graphs_and_larger_calls():
+    """Graphs captured on a context go on as they are when later calls, and
+    later captures, need more workspace; a first call may be captured."""
+    from paper_2110_02848_amd import gpu
+    c = gpu.Composer(0)
+    gen = torch.Generator().manual_seed(6)
+
+    def program(N, V, H, frames, typ):
+        g, x, w = _head(N + V, N, V, H, typ)
+        target, up = _targets(g, N, V), torch.randn(N, V, generator=g).cuda()
+        # (long enough to be cut into units, whose maps are workspace)
+        f, gate = _mat(g, frames, 64, typ), _mat(g, frames, 64, typ)
+        off = torch.tensor([0, frames], dtype=torch.int32, device="cuda")
+
+        def step():
+            r = c.cross_entropy(x, w, target)
+            a = c.cross_entropy_grads(x, w, target, r["lse"])
+            e = c.emission_weights(x, w)
+            b = c.emission_grads(x, w, e, up)
+            q = c.recurrence(f, gate, off, save=True)
+            d = c.recurrence_grads(f, gate, off, f, q["saved"])
+            return [r["loss"], r["lse"], *a, e, *b, q["y"], q["last"], d["x"], d["gate"]]
+
+        def change():
+            x.copy_(torch.randn(N, H, generator=gen).to(x.dtype))
+            f.copy_(torch.randn(frames, 64, generator=gen).to(f.dtype))
+        return step, change
+
+    graphs = []
+    for k, (N, V, H, frames) in enumerate([(100, 300, 70, 600), (700, 900, 72, 3000),
+                                           (2000, 3000, 80, 9000)]):
+        step, change = program(N, V, H, frames, ("bf16", "f16", "f32")[k])
+        if k:  # (the first one: nothing has run on the context)
+            step()
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            outs = step()
+        graphs.append((graph, step, change, outs))
+        # memory that a freed workspace would be found in again
+        fill = [torch.full((n << 18,), float("nan"), device="cuda") for n in (1, 2, 4, 8, 16, 32)]
+        for again in range(2):
+            for g, s, ch, o in graphs:
+                ch()
+                want = [t.clone() for t in s()]
+                torch.cuda.synchronize()
+                g.replay()
+                torch.cuda.synchronize()
+                for a, b in zip(o, want):
+                    assert torch.equal(a, b), (k, again)
+        assert all(torch.isnan(t).all() for t in fill)
+        del fill
+    c.close()
