@@ -569,8 +569,9 @@ FST_API int fst_cross_entropy(fst_ctx *ctx, const fst_matrix *x, const fst_matri
  *   grad_x = dz w,  grad_w = dz^T x
  * z is computed again, for a piece of the vocabulary at a time whose dz (rounded
  * as above) takes 512 MiB of workspace at most (more only where 256 words take
- * more).  A row without a word has dz = 0, whatever its scores; its x still
- * meets that 0 in grad_w, so it has to be finite there. */
+ * more).  The pieces depend on the sizes alone: a cap of the workspace that has
+ * no room for one refuses the call.  A row without a word has dz = 0, whatever
+ * its scores; its x still meets that 0 in grad_w, so it has to be finite there. */
 FST_API int fst_cross_entropy_grads(fst_ctx *ctx, const fst_matrix *x, const fst_matrix *w,
                                     const int32_t *target, const float *lse, const float *grad,
                                     const fst_matrix *grad_x, const fst_matrix *grad_w,

@@ -204,13 +204,39 @@ int release_all(fst_ctx *c, std::initializer_list<DevBuf *> bufs, bool *held) {
   return FST_OK;
 }
 
-// What only a two-input search needs: no fill reads it.
+// What the heads and the recurrence leave behind, unless a graph uses it.
+int release_layer(fst_ctx *c, bool *held) {
+  *held = false;
+  return c->layer_kept ? FST_OK : release_all(c, {&c->layer}, held);
+}
+
+// What only a two-input search needs (no fill reads it), and what no call needs
+// any more.
 int release_search(fst_ctx *c, bool *held) {
-  return release_all(
+  bool layer = false;
+  FST_TRY(release_layer(c, &layer));
+  FST_TRY(release_all(
       c, {&c->k0, &c->k1, &c->v0, &c->v1, &c->sort_tmp, &c->lists, &c->vis, &c->coacc,
           &c->fcnt, &c->lin, &c->heavy, &c->hoff, &c->heavy2, &c->hoff2, &c->aInOff,
           &c->aInPerm, &c->aInArc, &c->aInRec, &c->aInLut, &c->bInOff, &c->bInPerm, &c->bInArc,
-          &c->bInRec, &c->bInLut, &c->bOutChain, &c->bInChain}, held);
+          &c->bInRec, &c->bInLut, &c->bOutChain, &c->bInChain}, held));
+  *held = *held || layer;
+  return FST_OK;
+}
+
+// What scores, posteriors and scatters leave behind.
+int release_scores(fst_ctx *c, bool *held) {
+  bool f = false, b = false;
+  for (ScoreBufs *sb : {&c->score_f, &c->score_b})
+    FST_TRY(release_all(c, {&sb->sc, &sb->rec, &sb->term, &sb->mkey, &sb->pend, &sb->q, &sb->h,
+                            &sb->hoff}, sb == &c->score_f ? &f : &b));
+  FST_TRY(release_all(
+      c, {&c->s_sc, &c->s_owner, &c->s_extra, &c->s_inref, &c->s_mbeg, &c->s_mlen, &c->s_mcur,
+          &c->s_marc, &c->s_val, &c->s_acc, &c->s_pg, &c->s_pidx, &c->s_bcnt, &c->s_bscan,
+          &c->s_btotal, &c->s_mpos, &c->s_sweep, &c->s_chg, &c->s_ioff, &c->s_iarc, &c->seg},
+      held));
+  *held = *held || f || b;
+  return FST_OK;
 }
 
 // A call that finds no room (f() returns FST_ERR_NOMEM) runs once more without
@@ -1207,13 +1233,15 @@ int run_impl(fst_ctx *c, const fst_graph *A, const fst_graph *B, hipStream_t s, 
       continue;
     }
     if (rc == FST_ERR_NOMEM) {
+      bool held;
+      FST_TRY(release_layer(c, &held));
+      if (held) continue;  // as it was
       if (!linear) {
         too_large = cap;
         if (too_small ? cap - too_small <= too_small / 4 : cap <= 1024) return rc;
         cap_try = too_small ? (too_small + cap) / 2 : cap / 4;
       }
       try_linear = false;
-      bool held;
       FST_TRY(release_all(c, {&c->lin, &c->fq, &c->bq, &c->heavy, &c->hoff, &c->heavy2, &c->hoff2},
                           &held));
       continue;
@@ -2029,12 +2057,20 @@ int with_workspace(fst_ctx *c, hipStream_t s, F &&f) {
   size_t need = 0;
   FST_TRY(hip_status(f(nullptr, &need)));
   const bool capture = captured(s);
-  if (c->layer.cap < round_up(need ? need : 1) && (capture || c->layer_kept)) {
-    // (nothing can be waited for, and so freed, during a capture)
-    const auto more = [&]() { return another_layer(c, need, capture); };
-    FST_TRY(capture ? more() : with_room(c, more));
+  const bool another = (capture || c->layer_kept) && c->layer.cap < round_up(need ? need : 1);
+  const auto room = [&]() {
+    return another ? another_layer(c, need, capture) : ensure(c, c->layer, need);
+  };
+  if (capture) {  // (nothing can be waited for, and so freed)
+    FST_TRY(room());
   } else {
-    FST_TRY(with_room(c, [&]() { return ensure(c, c->layer, need); }));
+    int rc = with_room(c, room);
+    if (rc == FST_ERR_NOMEM) {
+      bool held = false;
+      FST_TRY(release_scores(c, &held));
+      if (held) rc = room();
+    }
+    FST_TRY(rc);
   }
   c->layer_kept = c->layer_kept || (capture && need);
   return hip_status(f(c->layer.p, &need));

@@ -572,3 +572,147 @@ def test_graphs_and_larger_calls():
         assert all(torch.isnan(t).all() for t in fill)
         del fill
     c.close()
+
+
+# ---- workspace caps before and after calls of other kinds ----
+
+def _within(call, cap, before=None):
+    """The call's results in a context of this cap, after `before` without
+    one; None where it finds no room."""
+    from paper_2110_02848_amd import gpu
+    c = gpu.Composer(0)
+    try:
+        if before:
+            before(c)
+        c.set_option(gpu.FST_OPT_MAX_WORKSPACE, cap)
+        out = call(c)
+        torch.cuda.synchronize()
+        return [t.clone() for t in out]
+    except gpu.FstError as e:
+        assert e.code == gpu.FST_ERR_NOMEM
+        return None
+    finally:
+        c.close()
+
+
+def _least(call):
+    lo, hi = 1 << 12, 1 << 27
+    while hi - lo > 1 << 14:
+        mid = (lo + hi) // 2
+        lo, hi = (mid, hi) if _within(call, mid) is None else (lo, mid)
+    return hi
+
+
+def _entropy_grads(N, V, H):
+    g, x, w = _head(1, N, V, H, "f32")
+    t = _targets(g, N, V)
+
+    def call(c):
+        r = c.cross_entropy(x, w, t)
+        return list(c.cross_entropy_grads(x, w, t, r["lse"]))
+    return call
+
+
+def _graph_call(kind):
+    import numpy as np
+    from paper_2110_02848_amd import gpu, synth
+    rng = np.random.default_rng(21)
+
+    def rand(V):
+        return gpu.to_device(synth.random_fst(rng, V, 4, 5, 0.1, 0.3, start=range(9)))
+    if kind in ("compose", "chain", "linear"):
+        lex = synth.lexicon(rng, 60, 4, 1, 4)[0]
+        A, B = {"compose": lambda: (rand(200), rand(200)),
+                "chain": lambda: (gpu.to_device(synth.random_fst(rng, 150, 5, 4, 0.1, 0.2)),
+                                  gpu.to_device(lex)),
+                "linear": lambda: (gpu.to_device(synth.emissions(rng, 250, 4)[0]),
+                                   gpu.to_device(lex))}[kind]()
+
+        def call(c):
+            C = c.compose(A, B)
+            return [C[k] for k in ("arc_offset", "dst", "ilabel", "weight", "arc_a", "arc_b")]
+    elif kind == "compose3":
+        A, B, D = rand(40), rand(40), rand(30)
+
+        def call(c):
+            C = c.compose3(A, B, D)
+            return [C[k] for k in ("arc_offset", "dst", "ilabel", "weight")]
+    elif kind == "score":
+        G = gpu.to_device(synth.random_dag(3, 4000))
+
+        def call(c):
+            s = c.score(G)
+            return [s["alpha"], s["beta"], s["total"]]
+    elif kind == "cyclic":
+        G = gpu.to_device(synth.random_cyclic(3, 2000, degree=4, mass=0.5))
+
+        def call(c):
+            s = c.score_cyclic(G)
+            return [s["alpha"], s["beta"], s["total"]]
+    else:
+        val = torch.randn(50000, device="cuda")
+        idx = (torch.arange(50000, device="cuda", dtype=torch.int32) * 7) % 9001
+
+        def call(c):
+            return [c.grad_scatter(val, idx, 9001)]
+    return call
+
+
+@pytest.mark.parametrize("kind", ["compose", "chain", "linear", "compose3", "score", "cyclic",
+                                  "scatter"])
+def test_room_of_other_calls_after_a_head(kind):
+    """Under the cap that a call fits in a fresh context it also fits one whose
+    workspace a head has grown, with the same results."""
+    call, head = _graph_call(kind), _entropy_grads(4096, 16384, 64)
+    # (half as much again: how many keys a chain search hands on varies by run)
+    cap = _least(call) * 3 // 2
+    assert cap < 4096 * 16384 * 4  # (less than the head leaves behind)
+    want, got = _within(call, cap), _within(call, cap, head)
+    assert want is not None and got is not None
+    for a, b in zip(want, got):
+        assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("kind", ["score", "cyclic", "scatter"])
+def test_room_of_a_head_after_scores(kind):
+    call = _entropy_grads(64, 100, 64)
+    cap, before = _least(call), _graph_call(kind)
+    for a, b in zip(_within(call, cap), _within(call, cap, before)):
+        assert torch.equal(a, b)
+
+
+def test_graph_after_a_call_without_room():
+    """What a graph uses stays, also where a composition finds no room."""
+    from paper_2110_02848_amd import gpu
+    call = _graph_call("compose")
+    cap = _least(call) * 3 // 2
+    c = gpu.Composer(0)
+    g, x, w = _head(2, 300, 400, 96, "bf16")
+    target = _targets(g, 300, 400)
+
+    def step():
+        r = c.cross_entropy(x, w, target)
+        return [r["loss"], *c.cross_entropy_grads(x, w, target, r["lse"])]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        outs = step()
+    want = _within(call, 0)
+    for limit in (1 << 16, cap + (8 << 20), 0):
+        c.set_option(gpu.FST_OPT_MAX_WORKSPACE, limit)
+        try:
+            for a, b in zip(call(c), want):
+                assert limit != 1 << 16 and torch.equal(a, b)
+        except gpu.FstError as e:
+            assert e.code == gpu.FST_ERR_NOMEM and limit == 1 << 16
+        fill = torch.full((1 << 24,), float("nan"), device="cuda")
+        x.copy_(torch.randn(300, 96, generator=g).to(x.dtype))
+        c.set_option(gpu.FST_OPT_MAX_WORKSPACE, 0)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in outs]
+        for a, b in zip(got, step()):
+            assert torch.equal(a, b)
+        assert torch.isnan(fill).all()
+    torch.cuda.synchronize()
+    c.close()
