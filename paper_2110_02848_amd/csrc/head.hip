@@ -69,13 +69,17 @@ __device__ __forceinline__ float4v mac(const Frag<float> &a, const Frag<float> &
 // i's bytes land at `lds` + 16 i, zeros where they lie past the end of the
 // buffer.  Written as instructions, because the compiler would wait for all of
 // them before the next read of LDS; whoever reads waits with wait_loads and a
-// barrier.
+// barrier.  (m0 is the compiler's own: it warns where it is named, and only
+// naming it keeps its uses of m0 clear of this one.)
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
 __device__ __forceinline__ void load_lds(uint32_t lds, uint32_t offset, int4v buffer) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
                :
                : "s"(__builtin_amdgcn_readfirstlane(lds)), "v"(offset), "s"(buffer)
-               : "memory");
+               : "memory", "m0");
 }
+#pragma clang diagnostic pop
 // The buffer of `bytes` bytes at p + at (as many of them as 32 bits count; all
 // arguments the same in every lane).
 __device__ __forceinline__ int4v buffer_at(const char *p, long long bytes, long long at) {
