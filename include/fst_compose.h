@@ -479,7 +479,8 @@ typedef struct {
  *                         of no sequence are left as they are; no access
  *                         leaves the matrices.  A sequence may be empty.
  *   state[num_seqs * x.cols]  device, float32, or NULL
- * num_seqs is at most FST_RECURRENCE_MAX_SEQS. */
+ * num_seqs is at most FST_RECURRENCE_MAX_SEQS; past 65,535 x 64 columns calls
+ * give FST_ERR_TOO_LARGE (16-bit rows read two columns at a time: twice that). */
 typedef struct {
   int32_t num_seqs;
   const int32_t *offset;

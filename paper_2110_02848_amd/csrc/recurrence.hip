@@ -543,17 +543,19 @@ bool packs(int D, size_t e, std::initializer_list<long long> strides,
 
 constexpr int NW = 8;  // wavefronts of a workgroup
 
+// Workgroups side by side, of 64 lanes' channels each; a launch takes MAX_ACROSS.
+constexpr long long MAX_ACROSS = 65535;
+long long across(const RecArgs &a, int v) { return (a.D + v * WAVE - 1ll) / (v * WAVE); }
+
 template <typename T, int V>
 void forward_as(const RecArgs &a, hipStream_t s) {
-  const dim3 grid((unsigned)(a.unit ? a.N / a.unit + a.n : a.n),
-                  (unsigned)((a.D + V * WAVE - 1) / (V * WAVE)));
+  const dim3 grid((unsigned)(a.unit ? a.N / a.unit + a.n : a.n), (unsigned)across(a, V));
   if (a.unit) k_rec_units<T, V, NW, false><<<grid, NW * WAVE, 0, s>>>(a);
   k_rec_forward<T, V, NW><<<grid, NW * WAVE, 0, s>>>(a);
 }
 template <typename T, int V>
 void backward_as(const RecArgs &a, hipStream_t s) {
-  const dim3 grid((unsigned)(a.unit ? a.N / a.unit + a.n : a.n),
-                  (unsigned)((a.D + V * WAVE - 1) / (V * WAVE)));
+  const dim3 grid((unsigned)(a.unit ? a.N / a.unit + a.n : a.n), (unsigned)across(a, V));
   if (a.unit) k_rec_units<T, V, NW, true><<<grid, NW * WAVE, 0, s>>>(a);
   k_rec_backward<T, V, NW><<<grid, NW * WAVE, 0, s>>>(a);
 }
@@ -589,6 +591,7 @@ hipError_t launch_recurrence(RecArgs a, int type, void *ws, size_t *need, hipStr
   const Layout l = layout(a, type != FST_F32 &&
                                  packs<2>(a.D, 2, {a.xs, a.us, a.ys}, {a.x, a.u, a.y}));
   const bool two = l.v == 2;
+  if (across(a, l.v) > MAX_ACROSS) return hipErrorInvalidValue;
   a.unit = l.unit;
   *need = a.unit ? (size_t)(a.N / a.unit + a.n) * a.D * sizeof(float2) : 0;
   if (!ws) return hipSuccess;
@@ -607,6 +610,7 @@ hipError_t launch_recurrence_grads(RecArgs a, int type, void *ws, size_t *need, 
   const Layout l = layout(a, type != FST_F32 && packs<2>(a.D, 2, {a.xs, a.us, a.gys, a.gxs, a.gus},
                                                          {a.x, a.u, a.gy, a.gx, a.gu}));
   const bool two = l.v == 2;
+  if (across(a, l.v) > MAX_ACROSS) return hipErrorInvalidValue;
   a.unit = l.unit;
   *need = a.unit ? (size_t)(a.N / a.unit + a.n) * a.D * sizeof(float2) : 0;
   if (!ws) return hipSuccess;

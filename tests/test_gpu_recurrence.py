@@ -457,3 +457,24 @@ def test_step_with_states_to_spare(comp, other):
         assert got is out and torch.equal(pool, before)
         assert (out[[i for i in range(9) if i not in rows]] == 7).all()
         assert not (out[rows] == 7).any()
+
+
+def test_widest_rows(comp):
+    """As many columns as a launch takes, and one more."""
+    from paper_2110_02848_amd import gpu
+    D = 65535 * 64
+    x, gate = torch.randn(2, D, device="cuda"), torch.randn(2, D, device="cuda")
+    off = torch.tensor([0, 2], dtype=torch.int32, device="cuda")
+    r = comp.recurrence(x, gate, off, save=True)
+    f = torch.sigmoid(gate.double())
+    want = f[1] * (1 - f[0]) * x[0].double() + (1 - f[1]) * x[1].double()
+    assert float((r["last"][0].double() - want).abs().max()) <= 4 * C * U * float(x.abs().max())
+    g = comp.recurrence_grads(x, gate, off, x, r["saved"])
+    assert torch.isfinite(g["gate"]).all()
+    x, gate = torch.zeros(2, D + 1, device="cuda"), torch.zeros(2, D + 1, device="cuda")
+    saved = torch.zeros(1, D + 1, device="cuda")
+    for call in (lambda: comp.recurrence(x, gate, off),
+                 lambda: comp.recurrence_grads(x, gate, off, x, saved)):
+        with pytest.raises(gpu.FstError) as e:
+            call()
+        assert e.value.code == gpu.FST_ERR_TOO_LARGE
