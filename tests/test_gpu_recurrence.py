@@ -478,3 +478,34 @@ def test_widest_rows(comp):
         with pytest.raises(gpu.FstError) as e:
             call()
         assert e.value.code == gpu.FST_ERR_TOO_LARGE
+
+
+@pytest.mark.parametrize("rev", [False, True])
+@pytest.mark.parametrize("lens,D", [([130, 0, 65, 64] + [i % 13 for i in range(252)], 128),
+                                    ([70] + [1 + i % 9 for i in range(130)], 258)])
+@pytest.mark.parametrize("typ", ["f16", "bf16"])
+def test_two_channels_a_lane(comp, typ, lens, D, rev):
+    """Batches of many sequences in 16 bits: each one workgroup's for every 128
+    channels."""
+    x, gate, gy, state, glast = _inputs(D, lens, D, typ)
+    _check(comp, x, gate, gy, _offsets(lens), state, glast, rev)
+
+
+@pytest.mark.parametrize("rev", [False, True])
+@pytest.mark.parametrize("typ", ["f32", "f16", "bf16"])
+def test_long_units(comp, typ, rev):
+    """10,100 steps of 1024 channels in units of 128 (two channels a lane) or
+    256: several chunks of steps for each wavefront of a unit, an empty sequence
+    between, ends inside a unit and inside a chunk."""
+    lens = [6001, 0, 4099]
+    x, gate, gy, state, glast = _inputs(17, lens, 1024, typ)
+    _check(comp, x, gate, gy, _offsets(lens), state, glast, rev)
+
+
+@pytest.mark.parametrize("rev", [False, True])
+@pytest.mark.parametrize("typ", ["f16", "bf16"])
+def test_units_of_one_channel(comp, typ, rev):
+    """Rows that begin anywhere, long, in 16 bits: one channel a lane."""
+    lens = [900, 0, 1500]
+    x, gate, gy, state, glast = _inputs(19, lens, 67, typ, pad=1)
+    _check(comp, x, gate, gy, _offsets(lens), state, glast, rev)
