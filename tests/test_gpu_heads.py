@@ -716,3 +716,86 @@ def test_graph_after_a_call_without_room():
         assert torch.isnan(fill).all()
     torch.cuda.synchronize()
     c.close()
+
+
+@pytest.mark.parametrize("typ", ["f16", "bf16"])
+def test_many_pieces_in_16_bits(comp, typ):
+    """Three pieces of a vocabulary (dS of 8192 rows takes 512 MiB for 32,768
+    words): the bounds of test_many_pieces, with dS rounded (h an element) and
+    the result's own rounding."""
+    N, V, H = 8192, 70001, 16
+    print(f"[pieces] N={N} V={V} H={H} {typ}", flush=True)
+    dt = ref.TYPES[typ]
+    h, tiny = ref.HALF_ULP[dt], 2.0 ** -37 if typ == "f16" else 0.0
+    g, x, w = _head(5, N, V, H, typ)
+    target = _targets(g, N, V)
+    r = comp.cross_entropy(x, w, target)
+    gx, gw = comp.cross_entropy_grads(x, w, target, r["lse"])
+    X, W = x.double(), w.double()
+    lse = torch.empty(N, dtype=torch.float64, device="cuda")
+    want_x, want_w = torch.zeros_like(X), torch.empty_like(W)
+    size_x, size_w = torch.zeros_like(X), torch.empty_like(W)
+    some = target >= 0
+    for i in range(0, N, 512):
+        lse[i:i + 512] = torch.logsumexp(torch.mm(X[i:i + 512], W.t().contiguous()), 1)
+    for v in range(0, V, 5000):
+        Wv = W[v:v + 5000]
+        p = torch.exp(torch.mm(X, Wv.t().contiguous()) - lse[:, None])
+        here = some & (target >= v) & (target < v + 5000)
+        rows = torch.nonzero(here)[:, 0]
+        p[rows, target[rows].long() - v] -= 1
+        p[~some] = 0
+        want_x += torch.mm(p, Wv)
+        size_x += torch.mm(p.abs(), Wv.abs())
+        want_w[v:v + 5000] = torch.mm(p.t().contiguous(), X)
+        size_w[v:v + 5000] = torch.mm(p.abs().t().contiguous(), X.abs())
+    e = 1200 * U
+    torch.testing.assert_close(r["lse"].double(), lse, rtol=0, atol=2 * e)
+    for got, want, size, n, other in ((gx, want_x, size_x, V, W), (gw, want_w, size_w, N, X)):
+        bound = (e + 2 * n * U + 1.01 * h) * size + tiny * other.abs().sum(0) + \
+            1.01 * h * want.abs() + ref.TINY[dt]
+        assert ((got.double() - want).abs() <= bound).all()
+        err = (got.double() - want).norm()
+        assert err <= h * want.norm() + ref.TINY[dt] * math.sqrt(want.numel()), float(err)
+    ox, _ = comp.cross_entropy_grads(x, w, target, r["lse"], need_w=False)
+    _, ow = comp.cross_entropy_grads(x, w, target, r["lse"], need_x=False)
+    assert torch.equal(ox, gx) and torch.equal(ow, gw)
+
+
+@pytest.mark.parametrize("typ,C", [("f16", 30), ("bf16", 30), ("f32", 300), ("f16", 300),
+                                   ("bf16", 300)])
+def test_infinite_and_missing_scores_of_each_type(comp, typ, C):
+    """As above in 16 bits, in whole rows and past them, with the gradients of
+    the sound rows."""
+    dt = ref.TYPES[typ]
+    x = torch.randn(20, 64, device="cuda").to(dt)
+    w = torch.randn(C, 64, device="cuda").to(dt)
+    w[:, 0] = w[:, 0].abs() + 1
+    t = torch.arange(20, dtype=torch.int32, device="cuda")
+    up = torch.randn(20, C, device="cuda")
+    x2 = x.clone()
+    x2[3, 5] = float("nan")
+    x2[4] = 0
+    x2[4, 0] = float("-inf")
+    keep = [i for i in range(20) if i not in (3, 4)]
+
+    def run(a):
+        e, r = comp.emission_weights(a, w), comp.cross_entropy(a, w, t)
+        return [e, r["loss"], r["lse"], comp.emission_grads(a, w, e, up)[0],
+                comp.cross_entropy_grads(a, w, t, r["lse"])[0]]
+    good, got = run(x), run(x2)
+    for a, b in zip(got, good):
+        assert torch.equal(a[keep], b[keep]) and torch.isfinite(b).all()
+        assert torch.isnan(a[3]).all()
+    assert got[2][4] == float("-inf")
+    # scores of -inf among others weigh nothing
+    w3 = w.clone()
+    w3[7] = 0
+    w3[7, 1] = float("-inf")
+    x3 = x.clone()
+    x3[:, 1] = x3[:, 1].abs() + 0.5
+    want = torch.log_softmax(torch.mm(x3.cpu().double(), w3.cpu().double().t().contiguous()), 1)
+    weight = comp.emission_weights(x3, w3)
+    assert (weight[:, 7] == float("-inf")).all()
+    others = [i for i in range(C) if i != 7]
+    assert torch.allclose(weight.cpu().double()[:, others], want[:, others], atol=1e-4)
