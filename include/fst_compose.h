@@ -526,7 +526,8 @@ FST_API int fst_recurrence_step(fst_ctx *ctx, const fst_matrix *x, const fst_mat
                                 int32_t num_slots, const fst_matrix *y, void *stream);
 
 /* Heads take at most FST_HEAD_MAX_ROWS rows of x and of w, and
- * FST_HEAD_MAX_COLS columns and classes of an emission (FST_ERR_TOO_LARGE).
+ * FST_HEAD_MAX_COLS columns and classes of an emission (FST_ERR_TOO_LARGE, which
+ * 2^37 scores and more in one call may give as well: a launch's limit).
  * None of their outputs may overlap an input or another output.  Matrices
  * whose rows do not begin at multiples of 16 bytes, or whose width is not a
  * multiple of 64 (float32: 32), are copied into the workspace first. */
@@ -548,8 +549,10 @@ FST_API int fst_emission_weights(fst_ctx *ctx, const fst_matrix *x, const fst_ma
  *   dz = grad - exp(weight) * (sum of grad over the row)
  *   grad_x = dz w,  grad_w = dz^T x
  * For the two products dz is rounded to the matrices' type (float16: scaled by a
- * power of two first, so that the smallest keep their digits); up to 2^28
- * products N C H it is kept as two such numbers. */
+ * power of two first, so that the smallest keep their digits): a gradient is off
+ * by half a spacing of the type, at most, of the sizes of the terms that it sums.
+ * Up to 2^28 products N C H dz is kept as two such numbers, which lose next to
+ * nothing. */
 FST_API int fst_emission_grads(fst_ctx *ctx, const fst_matrix *x, const fst_matrix *w,
                                const float *weight, const float *grad,
                                const fst_matrix *grad_x, const fst_matrix *grad_w,

@@ -569,7 +569,10 @@ void backward_as(const RecArgs &a, hipStream_t s) {
 // 256 steps leave the card idle: split into units over about 768 workgroups,
 // whose maps are found in a pass of their own, they read their inputs twice
 // (40,000 x 512: 49 us forward, unsplit 1,028; 4 of 2000 x 512: 17.6 and 56; 16
-// of 1000: 31 both ways; 32 of 500: 32 and 18.5, unsplit).
+// of 1000: 31 both ways; 32 of 500: 32 and 18.5, unsplit).  The lengths lie on the
+// device, so their average decides: one of 40,000 x 512 among 16 sequences is cut (53
+// us), among 64 it is not and takes as long as alone in one piece (1.27 ms with 63 of
+// 100 steps beside it).
 struct Layout {
   int v;
   long long unit;

@@ -583,6 +583,8 @@ class Composer:
                 self.grad_scatter(post, C["arc_b"], B_arcs, stream))
 
     # ---- between a network and its graphs ----
+    # Gradients are calls of their own: results carry no autograd history, whether
+    # or not an argument requires a gradient.
 
     def _call_stream(self, stream):
         return self._raw_stream(self.device) if stream is None else stream.cuda_stream
