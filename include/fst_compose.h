@@ -492,9 +492,10 @@ typedef struct {
 #define FST_RECURRENCE_MAX_SEQS (1 << 22)
 #define FST_RECURRENCE_SAVE_ROWS 64
 
-/* y (as x; may not overlap x or gate), last[num_seqs * x.cols] (float32,
- * optional): the state after each sequence (state[s], or 0, after an empty
- * one).  saved (float32, optional), for fst_recurrence_grads:
+/* y (as x), last[num_seqs * x.cols] (float32, optional): the state after each
+ * sequence (state[s], or 0, after an empty one).  No output may overlap an input
+ * (`last` not `state` either: a long sequence is read by several workgroups) or
+ * another output.  saved (float32, optional), for fst_recurrence_grads:
  * (x.rows / FST_RECURRENCE_SAVE_ROWS + num_seqs) * x.cols values, the states
  * entering every 64 steps of a sequence; rows of `saved` that stand for no
  * step are left as they are. */
