@@ -444,9 +444,10 @@ FST_API int fst_compose3_stats(const fst_ctx *ctx, fst_stats *out);
 
 /* ---- Between a network and its graphs ----------------------------------
  * What a recogniser computes on the other side of the arc weights: a gated
- * recurrence over the frames, the weights of emission graphs by a linear
- * layer and log-softmax, a cross entropy over a vocabulary of words, and the
- * gradients of all three.
+ * recurrence over the frames, attention to earlier frames (norms and rotation
+ * of queries and keys, linear attention with decays, attention to a window),
+ * the weights of emission graphs by a linear layer and log-softmax, a cross
+ * entropy over a vocabulary of words, and the gradients of all of these.
  *
  * Activations and weights are row-major matrices of one of three types,
  * with any row stride; the matrices of a call share one type.  Sums,
@@ -525,6 +526,161 @@ FST_API int fst_recurrence_grads(fst_ctx *ctx, const fst_recurrence *R, const fl
 FST_API int fst_recurrence_step(fst_ctx *ctx, const fst_matrix *x, const fst_matrix *gate,
                                 const float *state_in, float *state_out, const int32_t *slot,
                                 int32_t num_slots, const fst_matrix *y, void *stream);
+
+/* ---- Attention over frames ---------------------------------------------
+ * Queries, keys and values are matrices whose row t holds a frame's heads side
+ * by side, each of the same number of columns; matrices may be parts of wider
+ * ones (one product's queries, keys and values side by side).  Sequences are
+ * the rows [offset[s], offset[s+1]), offsets as in fst_recurrence.  No output
+ * may overlap an input or another output, but for the caches of
+ * fst_window_attention_step and state_out of fst_linear_attention_step.
+ * No results, gradients or states of rows depend on rows that they do not see:
+ * where those hold infinities or NaN, sums that these would make no number of are
+ * taken again without them (slowly, and rounded in another order).  Infinities and
+ * NaN in rows that they do see make no number of them, as the formulas do. */
+#define FST_NORM_MAX_WIDTH 512      /* columns of a head of fst_head_norms     */
+#define FST_ATTENTION_MAX_WIDTH 128 /* of the attentions (FST_ERR_TOO_LARGE),  */
+                                    /* which take at most 65,535 heads, 32,767 */
+                                    /* of more than 64 columns                 */
+
+/* Queries and keys normalised head by head, scaled, and rotated by position.
+ * For each head x of a row, of `width` columns, with one of the two weights
+ * (float32, width; queries' and keys' own):
+ *   z = x / sqrt(mean of x^2 + eps) * weight
+ * then the first 2 * num_freq columns are num_freq pairs, each turned by the
+ * angle pos[row] * freq[i]:  (a, b) -> (a cos - b sin, b cos + a sin).  Pair i is
+ * columns i and num_freq + i, or, with `pairs` not 0, columns 2 i and 2 i + 1.
+ * Angles are taken in 64 bits: any position keeps float32's precision.
+ *   q, k      q.cols and k.cols are multiples of width; k may be without columns
+ *   freq      device, float32, num_freq <= width / 2; NULL if num_freq is 0
+ *   pos       device, q.rows; NULL if num_freq is 0
+ * eps is finite and not negative. */
+typedef struct {
+  fst_matrix q, k;
+  int32_t width;
+  const float *q_weight, *k_weight;
+  const float *freq;
+  int32_t num_freq;
+  const int32_t *pos;
+  int32_t pairs;
+  float eps;
+} fst_head_norms;
+
+/* y_q, y_k: as q and k. */
+FST_API int fst_head_norms_run(fst_ctx *ctx, const fst_head_norms *A, const fst_matrix *y_q,
+                               const fst_matrix *y_k, void *stream);
+
+/* Gradients of a loss by q, k (grad_q, grad_k: as q and k) and the weights
+ * (float32, width, each optional) from those by y_q and y_k (grad_yq, grad_yk). */
+FST_API int fst_head_norms_grads(fst_ctx *ctx, const fst_head_norms *A,
+                                 const fst_matrix *grad_yq, const fst_matrix *grad_yk,
+                                 const fst_matrix *grad_q, const fst_matrix *grad_k,
+                                 float *grad_q_weight, float *grad_k_weight, void *stream);
+
+/* Linear attention with a decay for each head: with K = q.cols / heads and
+ * V = v.cols / heads columns of a head, head by head
+ *   S_t = e^(log_decay) S_(t-1) + k_t v_t^T,   y_t = scale S_t^T q_t
+ * from S = state[s] (num_seqs * heads * K * V float32 values, row-major; 0 where
+ * state is NULL), the first row of a sequence first, or the last if `reverse` is
+ * not 0.  log_decay (device, float32, heads) holds constants of the layer: no
+ * gradient is taken by them.  They are meant to be <= 0; -inf keeps nothing.
+ * With 16-bit matrices each score q_t . k_j of rows up to 63 apart, times its decay,
+ * and each number of the state that meets q is rounded to the matrices' type
+ * (float16: scaled by a power of two first) before it is multiplied; states
+ * themselves and `last` are float32 sums. */
+typedef struct {
+  int32_t num_seqs;
+  const int32_t *offset;
+  int32_t reverse;
+  int32_t heads;
+  const float *log_decay;
+  float scale;
+  fst_matrix q, k, v;
+  const float *state;
+} fst_linear_attention;
+
+/* y: as v.  last (float32, as state, optional): the state after each sequence
+ * (state[s], or 0, after an empty one). */
+FST_API int fst_linear_attention_run(fst_ctx *ctx, const fst_linear_attention *A,
+                                     const fst_matrix *y, float *last, void *stream);
+
+/* Gradients of a loss by q, k, v (as these) and state (float32, optional) from
+ * those by y (grad_y) and `last` (grad_last, NULL = 0).  With D_t the gradient by
+ * S_t, from the last row back:
+ *   D_t = scale q_t dy_t^T + e^(log_decay) D_(t+1)   (and grad_last at the last row)
+ *   dq_t = scale S_t dy_t,  dk_t = D_t v_t,  dv_t = D_t^T k_t,
+ *   grad_state = e^(log_decay) D_0   (grad_last for an empty sequence) */
+FST_API int fst_linear_attention_grads(fst_ctx *ctx, const fst_linear_attention *A,
+                                       const fst_matrix *grad_y, const float *grad_last,
+                                       const fst_matrix *grad_q, const fst_matrix *grad_k,
+                                       const fst_matrix *grad_v, float *grad_state,
+                                       void *stream);
+
+/* One step of many streams: row i of q, k, v and y is a stream whose state is
+ * slot[i] of state_in and state_out (num_slots of heads * K * V values; slot and
+ * num_slots as in fst_recurrence_step).  state_out may be state_in. */
+FST_API int fst_linear_attention_step(fst_ctx *ctx, const fst_matrix *q, const fst_matrix *k,
+                                      const fst_matrix *v, int32_t heads, const float *log_decay,
+                                      float scale, const float *state_in, float *state_out,
+                                      const int32_t *slot, int32_t num_slots,
+                                      const fst_matrix *y, void *stream);
+
+/* Attention to a window and a sequence's first frames: frame t sees frame s <= t
+ * of its sequence if t - s < window or s < sinks, and with z = scale q_t . k_s
+ *   lse_t = log sum over s of e^z,   y_t = sum over s of e^(z - lse_t) v_s.
+ * q has `heads` heads, k and v have kv_heads, each shared by heads / kv_heads
+ * consecutive heads of q; all heads have the same number of columns.  window >= 1
+ * (one as long as the sequences: all earlier frames), sinks >= 0, their sum at
+ * most 2^31 - 1.  With 16-bit matrices e^(z - maximum) and the gradient of z are
+ * rounded to the matrices' type (float16: the gradient scaled by a power of two
+ * first) before they are multiplied. */
+typedef struct {
+  int32_t num_seqs;
+  const int32_t *offset;
+  int32_t heads, kv_heads;
+  int32_t window, sinks;
+  float scale;
+  fst_matrix q, k, v;
+} fst_window_attention;
+
+/* y: as q; lse: float32, q.rows * heads. */
+FST_API int fst_window_attention_run(fst_ctx *ctx, const fst_window_attention *A,
+                                     const fst_matrix *y, float *lse, void *stream);
+
+/* Gradients of a loss by q, k and v (as these) from that by y (grad_y), with y
+ * and lse of the run on the same A. */
+FST_API int fst_window_attention_grads(fst_ctx *ctx, const fst_window_attention *A,
+                                       const fst_matrix *y, const float *lse,
+                                       const fst_matrix *grad_y, const fst_matrix *grad_q,
+                                       const fst_matrix *grad_k, const fst_matrix *grad_v,
+                                       void *stream);
+
+/* One step of many streams.  A stream's keys and values lie in the rows
+ * [slot * L, (slot + 1) * L) of k_cache and v_cache, L = sinks + window: the frame
+ * of position p in row p of these if p < sinks, else in row sinks + (p - sinks) %
+ * window.  Row i of q, k and v is the frame of position pos[i] of stream slot[i]
+ * (slot NULL: stream i): its k and v are written to the caches, and y is its
+ * attention to what the caches then hold, the frames of positions 0 .. pos[i] that
+ * it sees.  k_cache and v_cache have num_slots * L rows.  A slot outside
+ * [0, num_slots) or a negative position marks an idle row: its y is 0, no cache is
+ * read or written.  Slots of one call must differ. */
+FST_API int fst_window_attention_step(fst_ctx *ctx, const fst_matrix *q, const fst_matrix *k,
+                                      const fst_matrix *v, int32_t heads, int32_t kv_heads,
+                                      int32_t window, int32_t sinks, float scale,
+                                      const int32_t *pos, const int32_t *slot,
+                                      int32_t num_slots, const fst_matrix *k_cache,
+                                      const fst_matrix *v_cache, const fst_matrix *y,
+                                      void *stream);
+
+/* Fills the caches of fst_window_attention_step with whole sequences, that of
+ * sequence s in stream slot[s] (NULL: s; outside [0, num_slots): left out), so that
+ * the next frame's position is its length.  Rows that no frame belongs in are left
+ * as they are.  k and v have the caches' columns; window and sinks are theirs. */
+FST_API int fst_window_attention_fill(fst_ctx *ctx, int32_t num_seqs, const int32_t *offset,
+                                      const fst_matrix *k, const fst_matrix *v, int32_t window,
+                                      int32_t sinks, const int32_t *slot, int32_t num_slots,
+                                      const fst_matrix *k_cache, const fst_matrix *v_cache,
+                                      void *stream);
 
 /* Heads take at most FST_HEAD_MAX_ROWS rows of x and of w, and
  * FST_HEAD_MAX_COLS columns and classes of an emission (FST_ERR_TOO_LARGE, which

@@ -16,7 +16,7 @@ CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(HERE, "libfstcompose.so")
 SOURCES = ["primitives.hip", "compose.hip", "compose3.hip", "score.hip", "recurrence.hip",
-           "head.hip", "api.cpp"]
+           "head.hip", "norms.hip", "linear.hip", "window.hip", "api.cpp"]
 ARCH = "gfx950"
 
 

@@ -16,6 +16,7 @@
 #include <stdlib.h>
 #include <string.h>
 
+#include <cmath>
 #include <initializer_list>
 #include <new>
 #include <vector>
@@ -2008,6 +2009,106 @@ RecArgs recurrence_args(const fst_recurrence *R) {
   return a;
 }
 
+bool sequences_ok(int32_t num_seqs, const int32_t *offset, int64_t rows) {
+  return num_seqs >= 0 && num_seqs <= FST_RECURRENCE_MAX_SEQS && (num_seqs == 0 || offset) &&
+         (num_seqs > 0 || rows == 0);
+}
+
+// Two matrices of one type and number of rows.
+bool rows_match(const fst_matrix &a, const fst_matrix &b) {
+  return matrix_ok(&a) && matrix_ok(&b) && a.rows == b.rows && a.type == b.type;
+}
+
+bool head_norms_ok(const fst_head_norms *A) {
+  if (!A || !rows_match(A->q, A->k) || A->width < 1 || A->num_freq < 0) return false;
+  if (A->q.cols % A->width || A->k.cols % A->width || A->num_freq > A->width / 2) return false;
+  if (!(A->eps >= 0.0f) || !(A->eps < INFINITY)) return false;
+  if (A->num_freq > 0 && (!A->freq || (A->q.rows > 0 && !A->pos))) return false;
+  return (A->q.cols == 0 || A->q_weight) && (A->k.cols == 0 || A->k_weight);
+}
+NormArgs norm_args(const fst_head_norms *A) {
+  NormArgs a{};
+  a.side[0].x = A->q.data, a.side[0].xs = A->q.stride, a.side[0].w = A->q_weight;
+  a.side[1].x = A->k.data, a.side[1].xs = A->k.stride, a.side[1].w = A->k_weight;
+  a.side[0].heads = (int)(A->q.cols / A->width);
+  a.side[1].heads = (int)(A->k.cols / A->width);
+  a.freq = A->freq;
+  a.pos = A->pos;
+  a.N = A->q.rows;
+  a.D = A->width;
+  a.P = A->num_freq;
+  a.pairs = A->pairs != 0;
+  a.eps = A->eps;
+  return a;
+}
+
+// Heads of q, k and v: whole ones, those of q and k equally wide.
+bool linear_heads_ok(const fst_matrix &q, const fst_matrix &k, const fst_matrix &v,
+                     int32_t heads) {
+  return rows_match(q, k) && rows_match(q, v) && heads >= 1 && k.cols == q.cols &&
+         q.cols % heads == 0 && v.cols % heads == 0;
+}
+bool linear_ok(const fst_linear_attention *A) {
+  return A && linear_heads_ok(A->q, A->k, A->v, A->heads) &&
+         sequences_ok(A->num_seqs, A->offset, A->q.rows) && A->log_decay &&
+         std::isfinite(A->scale);
+}
+bool attention_wide(int64_t cols, int32_t heads) {
+  return cols / heads > FST_ATTENTION_MAX_WIDTH;
+}
+LinCall linear_call(const fst_linear_attention *A) {
+  LinCall c{};
+  c.q = A->q.data, c.qs = A->q.stride;
+  c.k = A->k.data, c.ks = A->k.stride;
+  c.v = A->v.data, c.vs = A->v.stride;
+  c.state = A->state;
+  c.off = A->offset;
+  c.log_decay = A->log_decay;
+  c.N = A->q.rows;
+  c.n = A->num_seqs;
+  c.H = A->heads;
+  c.K = (int)(A->q.cols / A->heads);
+  c.V = (int)(A->v.cols / A->heads);
+  c.reverse = A->reverse != 0;
+  c.scale = A->scale;
+  return c;
+}
+
+bool window_ok(int32_t window, int32_t sinks) {
+  return window >= 1 && sinks >= 0 && sinks <= INT32_MAX - window;
+}
+bool window_heads_ok(const fst_matrix &q, const fst_matrix &k, const fst_matrix &v,
+                     int32_t heads, int32_t kv_heads) {
+  return rows_match(q, k) && rows_match(q, v) && heads >= 1 && kv_heads >= 1 &&
+         heads % kv_heads == 0 && k.cols == v.cols && q.cols % heads == 0 &&
+         k.cols % kv_heads == 0 && q.cols / heads == k.cols / kv_heads;
+}
+bool window_attention_ok(const fst_window_attention *A) {
+  return A && window_heads_ok(A->q, A->k, A->v, A->heads, A->kv_heads) &&
+         sequences_ok(A->num_seqs, A->offset, A->q.rows) && window_ok(A->window, A->sinks) &&
+         std::isfinite(A->scale);
+}
+WinArgs window_args(const fst_window_attention *A) {
+  WinArgs a{};
+  a.q = A->q.data, a.qs = A->q.stride;
+  a.k = A->k.data, a.ks = A->k.stride;
+  a.v = A->v.data, a.vs = A->v.stride;
+  a.off = A->offset;
+  a.N = A->q.rows;
+  a.n = A->num_seqs;
+  a.H = A->heads;
+  a.G = A->kv_heads;
+  a.D = (int)(A->q.cols / A->heads);
+  a.window = A->window;
+  a.sinks = A->sinks;
+  a.scale = A->scale;
+  return a;
+}
+// A cache of num_slots streams, of the columns and type of `like`.
+bool cache_ok(const fst_matrix *m, const fst_matrix &like, int32_t num_slots, int64_t L) {
+  return matrix_ok(m) && m->cols == like.cols && m->type == like.type && m->rows == num_slots * L;
+}
+
 int hip_status(hipError_t e) {
   if (e == hipSuccess) return FST_OK;
   (void)hipGetLastError();
@@ -2691,6 +2792,231 @@ int fst_recurrence_step(fst_ctx *c, const fst_matrix *x, const fst_matrix *gate,
   a.n = x->rows;
   a.D = (int)x->cols;
   return hip_status(launch_recurrence_step(a, x->type, reinterpret_cast<hipStream_t>(stream)));
+}
+
+int fst_head_norms_run(fst_ctx *c, const fst_head_norms *A, const fst_matrix *y_q,
+                       const fst_matrix *y_k, void *stream) {
+  if (!c || !head_norms_ok(A) || !matrix_is(y_q, A->q, A->q.rows, A->q.cols) ||
+      !matrix_is(y_k, A->q, A->k.rows, A->k.cols))
+    return FST_ERR_INVALID_ARG;
+  if (A->width > FST_NORM_MAX_WIDTH) return FST_ERR_TOO_LARGE;
+  if (A->q.rows == 0 || A->q.cols + A->k.cols == 0) return FST_OK;
+  DeviceGuard g(c->device);
+  if (!g.ok) return FST_ERR_HIP;
+  NormArgs a = norm_args(A);
+  a.side[0].y = y_q->data, a.side[0].ys = y_q->stride;
+  a.side[1].y = y_k->data, a.side[1].ys = y_k->stride;
+  return hip_status(launch_norms(a, A->q.type, reinterpret_cast<hipStream_t>(stream)));
+}
+
+int fst_head_norms_grads(fst_ctx *c, const fst_head_norms *A, const fst_matrix *grad_yq,
+                         const fst_matrix *grad_yk, const fst_matrix *grad_q,
+                         const fst_matrix *grad_k, float *grad_q_weight, float *grad_k_weight,
+                         void *stream) {
+  if (!c || !head_norms_ok(A)) return FST_ERR_INVALID_ARG;
+  for (const fst_matrix *m : {grad_yq, grad_q})
+    if (!matrix_is(m, A->q, A->q.rows, A->q.cols)) return FST_ERR_INVALID_ARG;
+  for (const fst_matrix *m : {grad_yk, grad_k})
+    if (!matrix_is(m, A->q, A->k.rows, A->k.cols)) return FST_ERR_INVALID_ARG;
+  if (A->width > FST_NORM_MAX_WIDTH) return FST_ERR_TOO_LARGE;
+  DeviceGuard g(c->device);
+  if (!g.ok) return FST_ERR_HIP;
+  NormArgs a = norm_args(A);
+  a.side[0].g = grad_yq->data, a.side[0].gs = grad_yq->stride;
+  a.side[1].g = grad_yk->data, a.side[1].gs = grad_yk->stride;
+  a.side[0].y = grad_q->data, a.side[0].ys = grad_q->stride;
+  a.side[1].y = grad_k->data, a.side[1].ys = grad_k->stride;
+  a.side[0].gw = grad_q_weight;
+  a.side[1].gw = grad_k_weight;
+  return with_workspace(c, reinterpret_cast<hipStream_t>(stream), [&](void *ws, size_t *need) {
+    return launch_norms_grads(a, A->q.type, ws, need, reinterpret_cast<hipStream_t>(stream));
+  });
+}
+
+int fst_linear_attention_run(fst_ctx *c, const fst_linear_attention *A, const fst_matrix *y,
+                             float *last, void *stream) {
+  if (!c || !linear_ok(A) || !matrix_is(y, A->q, A->v.rows, A->v.cols))
+    return FST_ERR_INVALID_ARG;
+  if (attention_wide(A->q.cols, A->heads) || attention_wide(A->v.cols, A->heads))
+    return FST_ERR_TOO_LARGE;
+  if (A->num_seqs == 0 || A->v.cols == 0) return FST_OK;
+  DeviceGuard g(c->device);
+  if (!g.ok) return FST_ERR_HIP;
+  LinCall l = linear_call(A);
+  l.y = y->data, l.ys = y->stride;
+  l.last = last;
+  return with_workspace(c, reinterpret_cast<hipStream_t>(stream), [&](void *ws, size_t *need) {
+    return launch_linear(l, A->q.type, ws, need, reinterpret_cast<hipStream_t>(stream));
+  });
+}
+
+int fst_linear_attention_grads(fst_ctx *c, const fst_linear_attention *A,
+                               const fst_matrix *grad_y, const float *grad_last,
+                               const fst_matrix *grad_q, const fst_matrix *grad_k,
+                               const fst_matrix *grad_v, float *grad_state, void *stream) {
+  if (!c || !linear_ok(A)) return FST_ERR_INVALID_ARG;
+  for (const fst_matrix *m : {grad_q, grad_k})
+    if (!matrix_is(m, A->q, A->q.rows, A->q.cols)) return FST_ERR_INVALID_ARG;
+  for (const fst_matrix *m : {grad_y, grad_v})
+    if (!matrix_is(m, A->q, A->v.rows, A->v.cols)) return FST_ERR_INVALID_ARG;
+  if (attention_wide(A->q.cols, A->heads) || attention_wide(A->v.cols, A->heads))
+    return FST_ERR_TOO_LARGE;
+  if (A->num_seqs == 0 || A->q.cols + A->v.cols == 0) return FST_OK;
+  DeviceGuard g(c->device);
+  if (!g.ok) return FST_ERR_HIP;
+  LinCall l = linear_call(A);
+  l.y = grad_y->data, l.ys = grad_y->stride;
+  l.gq = grad_q->data, l.gqs = grad_q->stride;
+  l.gk = grad_k->data, l.gks = grad_k->stride;
+  l.gv = grad_v->data, l.gvs = grad_v->stride;
+  l.glast = grad_last;
+  l.gstate = grad_state;
+  return with_workspace(c, reinterpret_cast<hipStream_t>(stream), [&](void *ws, size_t *need) {
+    return launch_linear_grads(l, A->q.type, ws, need, reinterpret_cast<hipStream_t>(stream));
+  });
+}
+
+int fst_linear_attention_step(fst_ctx *c, const fst_matrix *q, const fst_matrix *k,
+                              const fst_matrix *v, int32_t heads, const float *log_decay,
+                              float scale, const float *state_in, float *state_out,
+                              const int32_t *slot, int32_t num_slots, const fst_matrix *y,
+                              void *stream) {
+  if (!c || !q || !k || !v || !linear_heads_ok(*q, *k, *v, heads) || !log_decay ||
+      !std::isfinite(scale) || !matrix_is(y, *q, v->rows, v->cols) || num_slots < 0)
+    return FST_ERR_INVALID_ARG;
+  if (!slot && num_slots < q->rows) return FST_ERR_INVALID_ARG;
+  if (attention_wide(q->cols, heads) || attention_wide(v->cols, heads)) return FST_ERR_TOO_LARGE;
+  if (q->rows == 0 || v->cols == 0) return FST_OK;
+  if (num_slots > 0 && q->cols > 0 && (!state_in || !state_out)) return FST_ERR_INVALID_ARG;
+  DeviceGuard g(c->device);
+  if (!g.ok) return FST_ERR_HIP;
+  LinStepArgs a{};
+  a.q = q->data, a.qs = q->stride;
+  a.k = k->data, a.ks = k->stride;
+  a.v = v->data, a.vs = v->stride;
+  a.y = y->data, a.ys = y->stride;
+  a.log_decay = log_decay;
+  a.in = state_in;
+  a.out = state_out;
+  a.slot = slot;
+  a.slots = num_slots;
+  a.n = q->rows;
+  a.H = heads;
+  a.A = (int)(q->cols / heads);
+  a.B = (int)(v->cols / heads);
+  a.scale = scale;
+  return hip_status(launch_linear_step(a, q->type, reinterpret_cast<hipStream_t>(stream)));
+}
+
+int fst_window_attention_run(fst_ctx *c, const fst_window_attention *A, const fst_matrix *y,
+                             float *lse, void *stream) {
+  if (!c || !window_attention_ok(A) || !matrix_is(y, A->q, A->q.rows, A->q.cols))
+    return FST_ERR_INVALID_ARG;
+  if (attention_wide(A->q.cols, A->heads)) return FST_ERR_TOO_LARGE;
+  if (A->q.rows > 0 && !lse) return FST_ERR_INVALID_ARG;
+  if (A->q.rows == 0) return FST_OK;
+  DeviceGuard g(c->device);
+  if (!g.ok) return FST_ERR_HIP;
+  WinArgs a = window_args(A);
+  a.o = y->data, a.os = y->stride;
+  a.lse = lse;
+  return hip_status(launch_window(a, A->q.type, reinterpret_cast<hipStream_t>(stream)));
+}
+
+int fst_window_attention_grads(fst_ctx *c, const fst_window_attention *A, const fst_matrix *y,
+                               const float *lse, const fst_matrix *grad_y,
+                               const fst_matrix *grad_q, const fst_matrix *grad_k,
+                               const fst_matrix *grad_v, void *stream) {
+  if (!c || !window_attention_ok(A)) return FST_ERR_INVALID_ARG;
+  for (const fst_matrix *m : {y, grad_y, grad_q})
+    if (!matrix_is(m, A->q, A->q.rows, A->q.cols)) return FST_ERR_INVALID_ARG;
+  for (const fst_matrix *m : {grad_k, grad_v})
+    if (!matrix_is(m, A->q, A->k.rows, A->k.cols)) return FST_ERR_INVALID_ARG;
+  if (attention_wide(A->q.cols, A->heads)) return FST_ERR_TOO_LARGE;
+  if (A->q.rows > 0 && !lse) return FST_ERR_INVALID_ARG;
+  if (A->q.rows == 0 || A->q.cols == 0) return FST_OK;
+  DeviceGuard g(c->device);
+  if (!g.ok) return FST_ERR_HIP;
+  WinArgs a = window_args(A);
+  a.y = y->data, a.ys = y->stride;
+  a.gy = grad_y->data, a.gys = grad_y->stride;
+  a.gq = grad_q->data, a.gqs = grad_q->stride;
+  a.gk = grad_k->data, a.gks = grad_k->stride;
+  a.gv = grad_v->data, a.gvs = grad_v->stride;
+  a.lse = const_cast<float *>(lse);
+  return with_workspace(c, reinterpret_cast<hipStream_t>(stream), [&](void *ws, size_t *need) {
+    return launch_window_grads(a, A->q.type, ws, need, reinterpret_cast<hipStream_t>(stream));
+  });
+}
+
+int fst_window_attention_step(fst_ctx *c, const fst_matrix *q, const fst_matrix *k,
+                              const fst_matrix *v, int32_t heads, int32_t kv_heads,
+                              int32_t window, int32_t sinks, float scale, const int32_t *pos,
+                              const int32_t *slot, int32_t num_slots, const fst_matrix *k_cache,
+                              const fst_matrix *v_cache, const fst_matrix *y, void *stream) {
+  if (!c || !q || !k || !v || !window_heads_ok(*q, *k, *v, heads, kv_heads) ||
+      !window_ok(window, sinks) || !std::isfinite(scale) || num_slots < 0 ||
+      !matrix_is(y, *q, q->rows, q->cols))
+    return FST_ERR_INVALID_ARG;
+  const int64_t L = (int64_t)window + sinks;
+  if (!cache_ok(k_cache, *k, num_slots, L) || !cache_ok(v_cache, *v, num_slots, L) ||
+      (!slot && num_slots < q->rows) || (q->rows > 0 && !pos))
+    return FST_ERR_INVALID_ARG;
+  if (attention_wide(q->cols, heads)) return FST_ERR_TOO_LARGE;
+  if (q->rows == 0 || q->cols == 0) return FST_OK;
+  DeviceGuard g(c->device);
+  if (!g.ok) return FST_ERR_HIP;
+  WinStepArgs a{};
+  a.q = q->data, a.qs = q->stride;
+  a.k = k->data, a.ks = k->stride;
+  a.v = v->data, a.vs = v->stride;
+  a.y = y->data, a.ys = y->stride;
+  a.kc = k_cache->data, a.kcs = k_cache->stride;
+  a.vc = v_cache->data, a.vcs = v_cache->stride;
+  a.pos = pos;
+  a.slot = slot;
+  a.slots = num_slots;
+  a.n = q->rows;
+  a.H = heads;
+  a.G = kv_heads;
+  a.D = (int)(q->cols / heads);
+  a.window = window;
+  a.sinks = sinks;
+  a.scale = scale;
+  return with_workspace(c, reinterpret_cast<hipStream_t>(stream), [&](void *ws, size_t *need) {
+    return launch_window_step(a, q->type, ws, need, reinterpret_cast<hipStream_t>(stream));
+  });
+}
+
+int fst_window_attention_fill(fst_ctx *c, int32_t num_seqs, const int32_t *offset,
+                              const fst_matrix *k, const fst_matrix *v, int32_t window,
+                              int32_t sinks, const int32_t *slot, int32_t num_slots,
+                              const fst_matrix *k_cache, const fst_matrix *v_cache,
+                              void *stream) {
+  if (!c || !k || !v || !rows_match(*k, *v) || k->cols != v->cols ||
+      !sequences_ok(num_seqs, offset, k->rows) || !window_ok(window, sinks) || num_slots < 0)
+    return FST_ERR_INVALID_ARG;
+  const int64_t L = (int64_t)window + sinks;
+  if (!cache_ok(k_cache, *k, num_slots, L) || !cache_ok(v_cache, *v, num_slots, L) ||
+      (!slot && num_slots < num_seqs))
+    return FST_ERR_INVALID_ARG;
+  if (num_seqs == 0 || k->cols == 0 || k->rows == 0) return FST_OK;
+  DeviceGuard g(c->device);
+  if (!g.ok) return FST_ERR_HIP;
+  WinFillArgs a{};
+  a.k = k->data, a.ks = k->stride;
+  a.v = v->data, a.vs = v->stride;
+  a.kc = k_cache->data, a.kcs = k_cache->stride;
+  a.vc = v_cache->data, a.vcs = v_cache->stride;
+  a.off = offset;
+  a.slot = slot;
+  a.N = k->rows;
+  a.n = num_seqs;
+  a.width = (int)k->cols;
+  a.window = window;
+  a.sinks = sinks;
+  a.slots = num_slots;
+  return hip_status(launch_window_fill(a, k->type, reinterpret_cast<hipStream_t>(stream)));
 }
 
 int fst_emission_weights(fst_ctx *c, const fst_matrix *x, const fst_matrix *w, float *weight,

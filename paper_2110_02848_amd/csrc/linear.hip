@@ -1,0 +1,586 @@
+// Linear attention with a decay for each head (fst_linear_attention_run, its
+// gradients and its single step).
+//
+//   S_t = e^g S_(t-1) + k_t v_t^T,  y_t = scale S_t^T q_t
+//
+// CHUNK rows at a time that is three products on the matrix cores: with S
+// the state before the chunk, its rows i, j counted from 0,
+//   y_i = scale (sum over j <= i of e^(g (i - j)) (q_i . k_j) v_j + e^(g (i + 1)) S^T q_i)
+//   S  <- e^(g CHUNK) S + sum over j of e^(g (CHUNK - 1 - j)) k_j v_j^T.
+// No power of the decay is divided by another, so none overflows however fast a
+// head forgets.  The gradients are the same operation (dy = the gradient of y):
+//   dq: (dy, v, k) in place of (q, k, v), from the transposed state;
+//   dk: (v, dy, q) and dv: (k, q, dy) from the last row to the first, from the
+//       gradient of the last state, which decays after a row instead of before
+//       it; what is left of it is the gradient of the first.
+#include <initializer_list>
+
+#include "sequences.h"
+#include "tiles.h"
+
+namespace fstc {
+
+using namespace tile;
+
+namespace {
+
+constexpr int CHUNK = 64;   // rows that are multiplied at once, 16 of them by a wavefront
+constexpr int SLICE = 64;   // columns of v that a workgroup takes
+constexpr int LNT = 256;    // threads of it
+constexpr int LNW = LNT / WAVE;
+static_assert(CHUNK == 16 * LNW && SLICE == 64, "a wavefront has 16 rows and four tiles of v");
+
+// e^(g n) for 0 <= n <= CHUNK, from 64 bits: chunk after chunk multiplies them.
+// (A head that keeps nothing has g = -inf, and e^(0 g) = 1 all the same.)
+__device__ __forceinline__ double power_of(float g, int n) {
+  const double d = g < -1e4f ? -1e4 : (double)g;
+  return exp(d * n);
+}
+
+// Whether all of a wavefront's results are numbers.
+__device__ __forceinline__ bool finite(const float4v (&x)[4]) {
+  float z = 0.0f;
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) z = fmaf(x[j][r], 0.0f, z);
+  return __all(z == 0.0f);
+}
+
+// Row i against the rows up to it alone, term by term.  The product also takes
+// the later rows of v, times 0, which makes no number of an infinity or a NaN
+// that row i does not see: where a result is none, the sums are taken again.
+struct Fours {
+  float4v x[4];
+};
+template <typename T, int PA>
+__device__ __noinline__ Fours exact_rows(const T *s_q, const T *s_k, const T *s_v,
+                                         const float *s_pow, int i, int A, int lg, float scale) {
+  Fours o{};
+  for (int row = 0; row <= i; ++row) {
+    float p = 0.0f;
+    for (int c = 0; c < A; ++c)
+      p = fmaf((float)s_q[i * LD<T, PA> + c], (float)s_k[row * LD<T, PA> + c], p);
+    p *= s_pow[i - row] * scale;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        o.x[j][r] = fmaf(p, (float)s_v[row * LD<T, SLICE> + 16 * j + 4 * lg + r], o.x[j][r]);
+  }
+  return o;
+}
+
+// FULL: rows' results; otherwise a unit's own contribution to the state, written
+// where the state entering the unit will be.
+//
+// Four wavefronts, 16 rows of the chunk each: scores as (k rows) x (q columns),
+// so that they become an operand of the product with v where they are; the state
+// in registers, a quarter of its rows a wavefront, and rounded to T in LDS as
+// (v rows) x (k columns) for the product with q.
+//
+// Roundings to 16 bits: scores and the state that meets q, once each.  The decayed k
+// that go into the state are as many numbers as hold them: states are float32
+// results.  float16: all three are scaled by a power of two from the
+// chunk's largest numbers, so that they neither overflow nor lose their digits.
+template <typename T, int PA, bool WIDE, bool FULL>
+__global__ __launch_bounds__(LNT) void k_linear(LinArgs a) {
+  static_assert(PA % 64 == 0, "whole tiles for four wavefronts");
+  constexpr int MT = PA / 64;  // tiles of 16 rows of the state, a wavefront
+  constexpr bool SCALED = std::is_same<T, f16>::value;
+  // numbers of T that a decayed k takes: 24 bits of it
+  constexpr int TERMS = std::is_same<T, bf16>::value ? 3 : std::is_same<T, f16>::value ? 2 : 1;
+  __shared__ __attribute__((aligned(16))) T s_q[FULL ? CHUNK * LD<T, PA> : 8];
+  __shared__ __attribute__((aligned(16))) T s_k[CHUNK * LD<T, PA>];
+  __shared__ __attribute__((aligned(16))) T s_v[CHUNK * LD<T, SLICE>];
+  __shared__ __attribute__((aligned(16))) T s_s[FULL ? SLICE * LD<T, PA> : 8];
+  __shared__ float s_pow[CHUNK + 1];
+  __shared__ float s_max[LNW][4];
+
+  const LinJob &job = a.job[blockIdx.z];
+  const int lane = threadIdx.x & (WAVE - 1), l16 = lane & 15, lg = lane >> 4;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
+  const int h = blockIdx.y / a.slices, b0 = blockIdx.y % a.slices * SLICE;
+  const int A = job.A, B = job.B, left = B - b0;
+  Unit u;
+  if (left <= 0 || !unit_of(a.off, a.n, a.N, a.unit, job.reverse, blockIdx.x, u)) return;
+
+  const float g = a.log_decay[h];
+  if (threadIdx.x <= CHUNK) s_pow[threadIdx.x] = (float)power_of(g, threadIdx.x);
+
+  // the state: rows (w MT + m) 16 + 4 lg + r, columns 16 j + l16
+  float4v S[MT][4];
+  const long long AB = (long long)A * B;
+  const int row0 = w * MT * 16 + 4 * lg;
+  float *unit_state =
+      a.unit ? job.units + ((long long)blockIdx.x * a.H + h) * AB : nullptr;
+  const float *from = !FULL ? nullptr
+                            : a.unit ? unit_state
+                                     : job.state ? job.state + ((long long)u.s * a.H + h) * AB
+                                                 : nullptr;
+#pragma unroll
+  for (int m = 0; m < MT; ++m)
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int ra = row0 + 16 * m + r, cb = 16 * j + l16;
+        S[m][j][r] = from && ra < A && cb < left
+                         ? from[(long long)ra * job.sa + (long long)(b0 + cb) * job.sb]
+                         : 0.0f;
+      }
+  float bound = 0.0f;  // SCALED: on the state's magnitudes
+  if constexpr (SCALED && FULL) {
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const float x = fabsf(S[m][j][r]);
+          bound = x < INFINITY ? fmaxf(bound, x) : bound;
+        }
+    bound = wave_max(bound);
+    if (lane == 0) s_max[w][3] = bound;
+  }
+  __syncthreads();
+  if constexpr (SCALED && FULL)
+    bound = fmaxf(fmaxf(s_max[0][3], s_max[1][3]), fmaxf(s_max[2][3], s_max[3][3]));
+
+  // powers that every chunk uses: of row i = 16 w + l16 against rows j = 16 t +
+  // 4 lg + r (0 where j is later), of row i against the state, of rows j to the
+  // chunk's end
+  const int i = 16 * w + l16, end = job.back ? 0 : 1;
+  float dec[4][4], wk[2][8];
+#pragma unroll
+  for (int t = 0; t < 4; ++t)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int d = i - (16 * t + 4 * lg + r);
+      dec[t][r] = d >= 0 ? s_pow[d] : 0.0f;
+    }
+#pragma unroll
+  for (int t = 0; t < 2; ++t)
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      wk[t][e] = s_pow[CHUNK - end - (32 * t + (e >> 2) * 16 + 4 * lg + (e & 3))];
+  const float over = s_pow[i + end];
+  // e^(g CHUNK) as two numbers
+  const double all = power_of(g, CHUNK);
+  float keep = (float)all, keep_lo = (float)(all - (double)keep);
+  if (!(fabsf(keep) < INFINITY)) keep_lo = 0.0f;
+  const float most = fmaxf(1.0f, keep);
+
+  const T *q = static_cast<const T *>(job.q) + (long long)h * A;
+  const T *k = static_cast<const T *>(job.k) + (long long)h * A;
+  const T *v = static_cast<const T *>(job.v) + (long long)h * B + b0;
+  Stage<T, PA, CHUNK, LNT, WIDE> rq, rk;
+  Stage<T, SLICE, CHUNK, LNT, WIDE> rv;
+  const auto fetch = [&](long long i0) {
+    const long long first = u.first + i0 * u.step;
+    const int count = (int)(u.hi - i0 < CHUNK ? u.hi - i0 : CHUNK);
+    if constexpr (FULL) rq.fetch(q, job.qs, A, first, u.step, count);
+    rk.fetch(k, job.ks, A, first, u.step, count);
+    rv.fetch(v, job.vs, left, first, u.step, count);
+  };
+  if (u.lo < u.hi) fetch(u.lo);
+  for (long long i0 = u.lo; i0 < u.hi; i0 += CHUNK) {
+    const int count = (int)(u.hi - i0 < CHUNK ? u.hi - i0 : CHUNK);
+    const bool more = i0 + CHUNK < u.hi;
+    float s_scale = 1.0f;
+    if constexpr (SCALED && FULL) s_scale = power_below(bound, 15);
+    if constexpr (FULL) {
+      rq.store(s_q);
+#pragma unroll
+      for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          store_four<T, true>(s_s + (16 * j + l16) * LD<T, PA>, row0 + 16 * m, PA,
+                              S[m][j] * s_scale);
+    }
+    rk.store(s_k);
+    rv.store(s_v);
+    if constexpr (SCALED) {
+      const float mk = wave_max(rk.largest()), mv = wave_max(rv.largest());
+      const float mq = FULL ? wave_max(rq.largest()) : 0.0f;
+      if (lane == 0) s_max[w][0] = mq, s_max[w][1] = mk, s_max[w][2] = mv;
+    }
+    __syncthreads();
+    if (more) fetch(i0 + CHUNK);
+
+    float p_scale = 1.0f, k_scale = 1.0f;
+    if constexpr (SCALED) {
+      float top[3];
+#pragma unroll
+      for (int c = 0; c < 3; ++c)
+        top[c] = fmaxf(fmaxf(s_max[0][c], s_max[1][c]), fmaxf(s_max[2][c], s_max[3][c]));
+      p_scale = power_below(most * (float)A * top[0] * top[1], 15);
+      k_scale = power_below(most * fabsf(job.sk) * top[1], 12);
+      bound = fmaf(keep, bound, most * fabsf(job.sk) * CHUNK * top[1] * top[2]);
+    }
+    if constexpr (FULL) {
+      float4v past[4] = {}, now[4] = {};
+      Frag<T> qf[PA / 32];
+#pragma unroll
+      for (int s = 0; s < PA / 32; ++s) qf[s] = rows<T, PA>(s_q, 16 * w, 32 * s, lane);
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int s = 0; s < PA / 32; ++s)
+          past[j] = mac(rows<T, PA>(s_s, 16 * j, 32 * s, lane), qf[s], past[j]);
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        if (2 * t > w) continue;
+        float4v x[2] = {};
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          if (2 * t + c > w) continue;
+#pragma unroll
+          for (int s = 0; s < PA / 32; ++s)
+            x[c] = mac(rows<T, PA>(s_k, 32 * t + 16 * c, 32 * s, lane), qf[s], x[c]);
+          // (later rows by a choice: what they hold may be no number)
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            x[c][r] = 32 * t + 16 * c + 4 * lg + r <= i
+                          ? x[c][r] * dec[2 * t + c][r] * p_scale
+                          : 0.0f;
+        }
+        const Frag<T> p = pack<T>(x[0], x[1]);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          now[j] = mac(columns<T, SLICE>(s_v, 32 * t, 16 * j, lane), p, now[j]);
+      }
+      if (!finite(now)) {
+        const Fours o = exact_rows<T, PA>(s_q, s_k, s_v, s_pow, i, A, lg, p_scale);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            now[j][r] = fabsf(now[j][r]) < INFINITY ? now[j][r] : o.x[j][r];
+      }
+      if (i < count) {
+        T *o = static_cast<T *>(job.o) + (u.first + (i0 + i) * u.step) * job.os +
+               (long long)h * B + b0;
+        const float f = job.ss * over / s_scale, f2 = job.so / p_scale;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          store_four<T, WIDE>(o, 16 * j + 4 * lg, left, past[j] * f + now[j] * f2);
+      }
+    }
+    if (more || !FULL || (job.last && u.hi == u.len)) {
+      float4v add[MT][4] = {};
+      const bool whole = count == CHUNK;
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        Frag<T> vf[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) vf[j] = columns<T, SLICE>(s_v, 32 * t, 16 * j, lane);
+        float f[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const int d = count - (32 * t + (e >> 2) * 16 + 4 * lg + (e & 3));
+          f[e] = (whole ? wk[t][e] : d > 0 ? s_pow[d - end] : 0.0f) * (job.sk * k_scale);
+        }
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+          float x[8], y[8];
+          unpack(columns<T, PA>(s_k, 32 * t, (w * MT + m) * 16, lane), x);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) x[e] *= f[e];
+          Frag<T> hi = pack<T>(x);
+          // (made once: what is left of x goes by the very numbers that are
+          // multiplied, where the compiler might round x for each in its own way)
+          if constexpr (TERMS > 1) asm("" : "+v"(hi.v[0]));
+#pragma unroll
+          for (int j = 0; j < 4; ++j) add[m][j] = mac(hi, vf[j], add[m][j]);
+#pragma unroll
+          for (int c = 1; c < TERMS; ++c) {
+            unpack(hi, y);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] -= y[e];
+            hi = pack<T>(x);
+            asm("" : "+v"(hi.v[0]));
+#pragma unroll
+            for (int j = 0; j < 4; ++j) add[m][j] = mac(hi, vf[j], add[m][j]);
+          }
+        }
+      }
+      float kh = keep, kl = keep_lo;
+      if (!whole) kh = s_pow[count], kl = 0.0f;
+      const float back = 1.0f / k_scale;
+#pragma unroll
+      for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            S[m][j][r] = fmaf(kh, S[m][j][r], fmaf(kl, S[m][j][r], add[m][j][r] * back));
+    }
+    __syncthreads();
+  }
+  float *to = !FULL ? unit_state
+                    : job.last && u.hi == u.len ? job.last + ((long long)u.s * a.H + h) * AB
+                                                : nullptr;
+  if (!to) return;
+#pragma unroll
+  for (int m = 0; m < MT; ++m)
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int ra = row0 + 16 * m + r, cb = 16 * j + l16;
+        if (ra < A && cb < left)
+          to[(long long)ra * job.sa + (long long)(b0 + cb) * job.sb] = S[m][j][r];
+      }
+}
+
+// From the units' own contributions to the states entering them, in place: a
+// thread takes an element of a head's state through a sequence's units.
+__global__ __launch_bounds__(NT) void k_linear_scan(LinArgs a) {
+  const LinJob &job = a.job[blockIdx.z];
+  const long long AB = (long long)job.A * job.B, all = AB * a.H;
+  const long long e = (long long)blockIdx.x * NT + threadIdx.x;
+  const int s = blockIdx.y;
+  if (e >= all) return;
+  const long long b = clamped(a.off[s], 0, a.N);
+  const long long len = clamped(a.off[s + 1], b, a.N) - b;
+  const int h = (int)(e / AB);
+  const float g = a.log_decay[h];
+  const double d = g < -1e4f ? -1e4 : (double)g, whole = exp(d * (double)a.unit);
+  const float kh = (float)whole;
+  const float kl = fabsf(kh) < INFINITY ? (float)(whole - (double)kh) : 0.0f;
+  float S = job.state ? job.state[s * all + e] : 0.0f;
+  float *p = job.units + rows_before(b, s, a.unit) * all + e;
+  const long long n = len > 0 ? (len + a.unit - 1) / a.unit : 1;
+  constexpr int AHEAD = 8;
+  for (long long i = 0; i < n; i += AHEAD) {
+    float x[AHEAD];
+#pragma unroll
+    for (int c = 0; c < AHEAD; ++c) x[c] = i + c < n ? p[(i + c) * all] : 0.0f;
+#pragma unroll
+    for (int c = 0; c < AHEAD; ++c) {
+      if (i + c >= n) break;
+      p[(i + c) * all] = S;
+      S = fmaf(kh, S, fmaf(kl, S, x[c]));
+    }
+  }
+}
+
+// One step: a workgroup takes a row's head, each thread V columns of every
+// `groups`-th row of the state.  Bound by memory: the state is read and written
+// once.
+template <typename T, int V>
+__global__ __launch_bounds__(LNT) void k_linear_step(LinStepArgs a) {
+  __shared__ float s_q[FST_ATTENTION_MAX_WIDTH], s_k[FST_ATTENTION_MAX_WIDTH];
+  __shared__ float s_y[LNT][V];
+  const long long i = blockIdx.x;
+  const int h = blockIdx.y, tid = threadIdx.x, A = a.A, B = a.B;
+  T *y = static_cast<T *>(a.y) + i * a.ys + (long long)h * B;
+  const long long slot = a.slot ? (long long)a.slot[i] : i;
+  if (slot < 0 || slot >= a.slots) {  // an idle row
+    for (int b = tid; b < B; b += LNT) y[b] = (T)0.0f;
+    return;
+  }
+  if (tid < A) {
+    s_q[tid] = (float)static_cast<const T *>(a.q)[i * a.qs + (long long)h * A + tid];
+    s_k[tid] = (float)static_cast<const T *>(a.k)[i * a.ks + (long long)h * A + tid];
+  }
+  const int cols = (B + V - 1) / V;
+  int across = 1;
+  while (across < cols) across *= 2;
+  const int groups = LNT / across, c = tid % across, gr = tid / across;
+  const float keep = (float)power_of(a.log_decay[h], 1);
+  struct alignas(4 * V) Pack { float v[V]; };
+  const long long base = (slot * a.H + h) * (long long)A * B;
+  const bool on = c < cols;
+  float vv[V], sum[V];
+#pragma unroll
+  for (int e = 0; e < V; ++e) {
+    vv[e] = on ? (float)static_cast<const T *>(a.v)[i * a.vs + (long long)h * B + c * V + e] : 0.0f;
+    sum[e] = 0.0f;
+  }
+  __syncthreads();
+  if (on) {
+#pragma unroll 4
+    for (int ra = gr; ra < A; ra += groups) {
+      Pack p = *reinterpret_cast<const Pack *>(a.in + base + (long long)ra * B + c * V);
+      const float kk = s_k[ra], qq = s_q[ra];
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        p.v[e] = fmaf(keep, p.v[e], kk * vv[e]);
+        sum[e] = fmaf(qq, p.v[e], sum[e]);
+      }
+      *reinterpret_cast<Pack *>(a.out + base + (long long)ra * B + c * V) = p;
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < V; ++e) s_y[tid][e] = sum[e];
+  for (int half = groups / 2; half; half /= 2) {
+    __syncthreads();
+    if (gr < half)
+#pragma unroll
+      for (int e = 0; e < V; ++e) s_y[tid][e] += s_y[tid + half * across][e];
+  }
+  if (gr == 0 && on)
+#pragma unroll
+    for (int e = 0; e < V; ++e) y[c * V + e] = (T)(a.scale * s_y[tid][e]);
+}
+
+unsigned units_of(const LinArgs &a) { return (unsigned)(a.unit ? a.N / a.unit + a.n : a.n); }
+
+template <typename T, int PA, bool WIDE, bool FULL>
+void launch_as(const LinArgs &a, int jobs, hipStream_t s) {
+  k_linear<T, PA, WIDE, FULL><<<dim3(units_of(a), a.H * a.slices, jobs), LNT, 0, s>>>(a);
+}
+template <typename T, bool FULL>
+void launch_jobs(const LinArgs &a, int jobs, int A, bool wide, hipStream_t s) {
+  if (A <= 64)
+    wide ? launch_as<T, 64, true, FULL>(a, jobs, s) : launch_as<T, 64, false, FULL>(a, jobs, s);
+  else
+    wide ? launch_as<T, 128, true, FULL>(a, jobs, s) : launch_as<T, 128, false, FULL>(a, jobs, s);
+}
+
+// Jobs [lo, hi) of `all`, which have one width of q and k (or widths up to 64).
+template <bool FULL>
+void launch_range(LinArgs a, const LinJob *all, int lo, int hi, int type, bool wide,
+                  hipStream_t s) {
+  int B = 0;
+  for (int i = lo; i < hi; ++i) {
+    a.job[i - lo] = all[i];
+    B = all[i].B > B ? all[i].B : B;
+  }
+  a.slices = (B + SLICE - 1) / SLICE;
+  if (type == FST_F32)
+    launch_jobs<float, FULL>(a, hi - lo, all[lo].A, wide, s);
+  else if (type == FST_F16)
+    launch_jobs<f16, FULL>(a, hi - lo, all[lo].A, wide, s);
+  else
+    launch_jobs<bf16, FULL>(a, hi - lo, all[lo].A, wide, s);
+}
+
+// Whether every row of a head, of each tensor, begins at a multiple of 16 bytes
+// and is whole groups of them.
+bool wide_rows(const LinCall &c, size_t e, std::initializer_list<long long> strides,
+               std::initializer_list<const void *> data) {
+  if (c.K * e % 16 || c.V * e % 16) return false;
+  for (long long t : strides)
+    if (t * e % 16) return false;
+  for (const void *p : data)
+    if (reinterpret_cast<uintptr_t>(p) % 16) return false;
+  return true;
+}
+
+// Steps of a unit, 0: sequences are not cut.
+long long unit_steps(const LinCall &c, int jobs) {
+  const long long groups = (long long)c.H * ((c.V + SLICE - 1) / SLICE);
+  if (c.n * groups * jobs >= 256 || c.N / c.n <= 256) return 0;
+  const long long steps = c.N * groups / 768;
+  return steps <= CHUNK ? CHUNK : (steps + CHUNK - 1) / CHUNK * CHUNK;
+}
+
+LinArgs linear_args(const LinCall &c, long long unit) {
+  LinArgs a{};
+  a.off = c.off;
+  a.log_decay = c.log_decay;
+  a.N = c.N;
+  a.unit = unit;
+  a.n = c.n;
+  a.H = c.H;
+  return a;
+}
+
+// Units' states of `jobs` jobs, and the scan that makes entering states of them.
+void launch_states(const LinArgs &a, const LinJob *all, int jobs, int type, bool wide,
+                   hipStream_t s) {
+  launch_range<false>(a, all, 0, jobs, type, wide, s);
+  LinArgs b = a;
+  for (int i = 0; i < jobs; ++i) b.job[i] = all[i];
+  const long long e = (long long)a.H * all[0].A * all[0].B;
+  k_linear_scan<<<dim3((unsigned)((e + NT - 1) / NT), a.n, jobs), NT, 0, s>>>(b);
+}
+
+constexpr long long MAX_ACROSS = 65535;  // of a grid's second dimension
+
+bool too_wide(const LinCall &c) {
+  const int most = c.K > c.V ? c.K : c.V;
+  return (long long)c.H * ((most + SLICE - 1) / SLICE) > MAX_ACROSS;
+}
+
+}  // namespace
+
+// (also without workspace: then `need` is all that is set)
+hipError_t launch_linear(const LinCall &c, int type, void *ws, size_t *need, hipStream_t s) {
+  if (too_wide(c)) return hipErrorInvalidValue;
+  const size_t e = type_bytes(type);
+  const long long unit = unit_steps(c, 1);
+  *need = unit ? (size_t)(c.N / unit + c.n) * c.H * c.K * c.V * sizeof(float) : 0;
+  if (!ws) return hipSuccess;
+  const LinArgs a = linear_args(c, unit);
+  const bool wide = wide_rows(c, e, {c.qs, c.ks, c.vs, c.ys}, {c.q, c.k, c.v, c.y});
+  const LinJob job = {c.q, c.k, c.v, c.y, c.qs, c.ks, c.vs, c.ys, c.K, c.V, c.state, c.last,
+                      c.V, 1, static_cast<float *>(ws), c.scale, c.scale, 1.0f, c.reverse, 0};
+  if (unit) launch_states(a, &job, 1, type, wide, s);
+  launch_range<true>(a, &job, 0, 1, type, wide, s);
+  return hipGetLastError();
+}
+
+hipError_t launch_linear_grads(const LinCall &c, int type, void *ws, size_t *need,
+                               hipStream_t s) {
+  if (too_wide(c)) return hipErrorInvalidValue;
+  const size_t e = type_bytes(type);
+  const long long unit = unit_steps(c, 3);
+  const size_t states = unit ? (size_t)(c.N / unit + c.n) * c.H * c.K * c.V : 0;
+  *need = 2 * states * sizeof(float);
+  if (!ws) return hipSuccess;
+  const LinArgs a = linear_args(c, unit);
+  const bool wide = wide_rows(c, e, {c.qs, c.ks, c.vs, c.ys, c.gqs, c.gks, c.gvs},
+                              {c.q, c.k, c.v, c.y, c.gq, c.gk, c.gv});
+  float *fwd = static_cast<float *>(ws), *bwd = fwd + states;
+  const int back = !c.reverse;
+  if (unit) {
+    const LinJob sums[2] = {
+        {nullptr, c.k, c.v, nullptr, 0, c.ks, c.vs, 0, c.K, c.V, c.state, nullptr, c.V, 1, fwd,
+         0.0f, 0.0f, 1.0f, c.reverse, 0},
+        {nullptr, c.q, c.y, nullptr, 0, c.qs, c.ys, 0, c.K, c.V, c.glast, nullptr, c.V, 1, bwd,
+         0.0f, 0.0f, c.scale, back, 1}};
+    launch_states(a, sums, 2, type, wide, s);
+  }
+  const LinJob jobs[3] = {
+      {c.y, c.v, c.k, c.gq, c.ys, c.vs, c.ks, c.gqs, c.V, c.K, c.state, nullptr, 1, c.V, fwd,
+       c.scale, c.scale, 1.0f, c.reverse, 0},
+      {c.v, c.y, c.q, c.gk, c.vs, c.ys, c.qs, c.gks, c.V, c.K, c.glast, nullptr, 1, c.V, bwd,
+       c.scale, 1.0f, c.scale, back, 1},
+      {c.k, c.q, c.y, c.gv, c.ks, c.qs, c.ys, c.gvs, c.K, c.V, c.glast, c.gstate, c.V, 1, bwd,
+       c.scale, 1.0f, c.scale, back, 1}};
+  if ((c.K <= 64) == (c.V <= 64)) {
+    launch_range<true>(a, jobs, 0, 3, type, wide, s);
+  } else {
+    launch_range<true>(a, jobs, 0, 2, type, wide, s);
+    launch_range<true>(a, jobs, 2, 3, type, wide, s);
+  }
+  return hipGetLastError();
+}
+
+template <typename T>
+static void linear_step_as(const LinStepArgs &a, bool four, hipStream_t s) {
+  const dim3 grid((unsigned)a.n, a.H);
+  if (four)
+    k_linear_step<T, 4><<<grid, LNT, 0, s>>>(a);
+  else
+    k_linear_step<T, 1><<<grid, LNT, 0, s>>>(a);
+}
+
+hipError_t launch_linear_step(const LinStepArgs &a, int type, hipStream_t s) {
+  if (a.H > MAX_ACROSS) return hipErrorInvalidValue;
+  const bool four = a.B % 4 == 0 && reinterpret_cast<uintptr_t>(a.in) % 16 == 0 &&
+                    reinterpret_cast<uintptr_t>(a.out) % 16 == 0;
+  if (type == FST_F32)
+    linear_step_as<float>(a, four, s);
+  else if (type == FST_F16)
+    linear_step_as<f16>(a, four, s);
+  else
+    linear_step_as<bf16>(a, four, s);
+  return hipGetLastError();
+}
+
+}  // namespace fstc

@@ -15,6 +15,7 @@
 #include <initializer_list>
 
 #include "layers.h"
+#include "sequences.h"
 
 namespace fstc {
 
@@ -84,55 +85,8 @@ __device__ __forceinline__ void gate(bf16 u, float &keep, float &add) {
   gate16((float)u, keep, add);
 }
 
-// What a workgroup works on: steps [lo, hi) of a sequence of `len` rows from
-// row b, the first step's row `first` and each next one `step` rows on.
-struct Unit {
-  int s;
-  long long b, len, lo, hi;
-  long long first, step;
-};
-
-__device__ __forceinline__ long long clamped(long long v, long long lo, long long hi) {
-  return v < lo ? lo : v > hi ? hi : v;
-}
-
-// First of the rows that sequence s, from row b, has in an array with a row
-// for every `per` steps of a sequence: ceil(len / per) rows fit before the
-// next sequence's, as floor(b / per) + s grows by at least that.
-__device__ __forceinline__ long long rows_before(long long b, int s, long long per) {
-  return b / per + s;
-}
-
-// The unit of workgroup k: a whole sequence, or (a.unit steps each) the
-// sequence that owns row k of an array with a row for every unit.  All of it
-// lies inside [0, N) whatever the offsets hold.  False: there is none.
 __device__ __forceinline__ bool unit_of(const RecArgs &a, long long k, Unit &u) {
-  int s = (int)k;
-  if (a.unit) {
-    int lo = 0, hi = a.n - 1;  // the last s with rows_before <= k
-    while (lo < hi) {
-      const int mid = lo + (hi - lo + 1) / 2;
-      if (rows_before(clamped(a.off[mid], 0, a.N), mid, a.unit) <= k)
-        lo = mid;
-      else
-        hi = mid - 1;
-    }
-    s = lo;
-  }
-  u.s = s;
-  u.b = clamped(a.off[s], 0, a.N);
-  u.len = clamped(a.off[s + 1], u.b, a.N) - u.b;
-  u.lo = 0;
-  u.hi = u.len;
-  if (a.unit) {
-    const long long j = k - rows_before(u.b, s, a.unit);
-    u.lo = j * a.unit;
-    if (j < 0 || (j > 0 && u.lo >= u.len)) return false;
-    u.hi = u.lo + a.unit < u.len ? u.lo + a.unit : u.len;
-  }
-  u.step = a.reverse ? -1 : 1;
-  u.first = a.reverse ? u.b + u.len - 1 : u.b;
-  return true;
+  return unit_of(a.off, a.n, a.N, a.unit, a.reverse, k, u);
 }
 
 // Rows of a chunk's steps: i counts from the sequence's start, and steps past

@@ -1,0 +1,218 @@
+// Tiles of matrices in LDS and the fragments of them that the matrix cores
+// multiply (linear.hip, window.hip).
+//
+// A product of 16 x 16 results takes 32 of the sum a step: of either operand
+// lane l holds row l & 15 and eight numbers of the sum; of the results column
+// l & 15 and rows 4 (l >> 4) + 0..3.  Which eight of the 32 a lane holds is
+// free as long as both operands agree.  Here there are two orders: `rows`
+// reads, along the rows of a tile, 8 (l >> 4) + 0..7; `columns` reads, down
+// its columns, 4 (l >> 4) + 0..3 and 16 + 4 (l >> 4) + 0..3.  The second is
+// how the results of two products above one another lie, so that these become
+// an operand of the next product in the registers that they are in.
+#pragma once
+
+#include <type_traits>
+
+#include "layers.h"
+
+namespace fstc {
+namespace tile {
+
+typedef _Float16 f16;
+typedef __bf16 bf16;
+typedef __attribute__((ext_vector_type(4))) float float4v;
+typedef __attribute__((ext_vector_type(4))) int int4v;
+typedef __attribute__((ext_vector_type(2))) int int2v;
+typedef __attribute__((ext_vector_type(8))) _Float16 half8;
+typedef __attribute__((ext_vector_type(8))) __bf16 bhalf8;
+typedef __attribute__((ext_vector_type(4))) short short4v;
+
+template <typename T>
+constexpr int PER = 16 / (int)sizeof(T);  // numbers in 16 bytes
+
+// Eight numbers of a lane.
+template <typename T>
+struct Frag {
+  int4v v[sizeof(T) / 2];
+};
+
+__device__ __forceinline__ float4v mac(const Frag<bf16> &a, const Frag<bf16> &b, float4v c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bhalf8, a.v[0]),
+                                                 __builtin_bit_cast(bhalf8, b.v[0]), c, 0, 0, 0);
+}
+__device__ __forceinline__ float4v mac(const Frag<f16> &a, const Frag<f16> &b, float4v c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, a.v[0]),
+                                                __builtin_bit_cast(half8, b.v[0]), c, 0, 0, 0);
+}
+// (eight steps of 4: step j sums over element j of the four lane groups)
+__device__ __forceinline__ float4v mac(const Frag<float> &a, const Frag<float> &b, float4v c) {
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const float4v x = __builtin_bit_cast(float4v, a.v[i]), y = __builtin_bit_cast(float4v, b.v[i]);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(x[j], y[j], c, 0, 0, 0);
+  }
+  return c;
+}
+
+// The eight numbers as they are held, and back.
+template <typename T>
+__device__ __forceinline__ void unpack(const Frag<T> &f, float (&x)[8]) {
+  struct alignas(16) { T v[8]; } e;
+  __builtin_memcpy(&e, &f, sizeof(e));
+#pragma unroll
+  for (int i = 0; i < 8; ++i) x[i] = (float)e.v[i];
+}
+template <typename T>
+__device__ __forceinline__ Frag<T> pack(const float (&x)[8]) {
+  struct alignas(16) { T v[8]; } e;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) e.v[i] = (T)x[i];
+  Frag<T> f;
+  __builtin_memcpy(&f, &e, sizeof(e));
+  return f;
+}
+// Results of two products, rows r.. and 16 + r.., as an operand.
+template <typename T>
+__device__ __forceinline__ Frag<T> pack(const float4v &a, const float4v &b) {
+  const float x[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+  return pack<T>(x);
+}
+
+// Rows of P numbers, 16 bytes between them, so that the reads of 16 lanes a
+// row apart meet different banks.
+template <typename T, int P>
+constexpr int LD = P + PER<T>;
+template <typename T, int P, int R>
+constexpr int BYTES = LD<T, P> * R * (int)sizeof(T);
+
+// Rows `row` .. + 15, numbers `k` .. + 31 of each.
+template <typename T, int P>
+__device__ __forceinline__ Frag<T> rows(const T *t, int row, int k, int lane) {
+  const T *p = t + (row + (lane & 15)) * LD<T, P> + k + (lane >> 4) * 8;
+  Frag<T> f;
+#pragma unroll
+  for (int i = 0; i < (int)sizeof(T) / 2; ++i)
+    f.v[i] = *reinterpret_cast<const int4v *>(p + i * PER<T>);
+  return f;
+}
+
+// Columns `col` .. + 15, rows `row` .. + 31 of each.  (A read that transposes
+// gives lane i of 16 the i-th column of four rows: lanes 4 j .. 4 j + 3 point
+// at the j-th.)
+template <typename T, int P>
+__device__ __forceinline__ Frag<T> columns(const T *t, int row, int col, int lane) {
+  Frag<T> f;
+  if constexpr (sizeof(T) == 2) {
+    const T *p = t + (row + (lane >> 4) * 4 + ((lane >> 2) & 3)) * LD<T, P> + col + (lane & 3) * 4;
+    int2v v[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      v[i] = __builtin_bit_cast(
+          int2v, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                     (__attribute__((address_space(3))) short4v *)(p + i * 16 * LD<T, P>)));
+    f.v[0] = int4v{v[0].x, v[0].y, v[1].x, v[1].y};
+  } else {
+    const T *p = t + (row + (lane >> 4) * 4) * LD<T, P> + col + (lane & 15);
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        f.v[i][j] = __builtin_bit_cast(int, (float)p[(i * 16 + j) * LD<T, P>]);
+  }
+  return f;
+}
+
+// 16 bytes from number c on of a row of `width`, zeros past its end; WIDE: the
+// width is a multiple of them and the row begins at one.
+template <typename T, bool WIDE>
+__device__ __forceinline__ int4v load_group(const T *row, int c, int width, bool there) {
+  int4v v{0, 0, 0, 0};
+  if constexpr (WIDE) {
+    if (there && c < width) v = *reinterpret_cast<const int4v *>(row + c);
+  } else {
+    struct alignas(16) { T v[PER<T>]; } e;
+    __builtin_memcpy(&e, &v, 16);
+    if (there) {
+#pragma unroll
+      for (int i = 0; i < PER<T>; ++i)
+        if (c + i < width) e.v[i] = row[c + i];
+    }
+    __builtin_memcpy(&v, &e, 16);
+  }
+  return v;
+}
+
+// A tile of R rows of P numbers on its way from memory to LDS, by NTH threads.
+template <typename T, int P, int R, int NTH, bool WIDE>
+struct Stage {
+  static constexpr int GROUPS = P / PER<T>;  // of a row
+  static constexpr int LOADS = R * GROUPS / NTH;
+  static_assert(LOADS >= 1 && LOADS * NTH == R * GROUPS, "whole loads");
+  int4v v[LOADS];
+
+  // row i of the tile is row first + i * step of the matrix, if i < count
+  __device__ __forceinline__ void fetch(const T *p, long long stride, int width, long long first,
+                                        long long step, int count) {
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+      const int q = i * NTH + (int)threadIdx.x, r = q / GROUPS, c = q % GROUPS * PER<T>;
+      v[i] = load_group<T, WIDE>(p + (first + r * step) * stride, c, width, r < count);
+    }
+  }
+  __device__ __forceinline__ void store(T *t) const {
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+      const int q = i * NTH + (int)threadIdx.x, r = q / GROUPS, c = q % GROUPS * PER<T>;
+      *reinterpret_cast<int4v *>(t + r * LD<T, P> + c) = v[i];
+    }
+  }
+  // the largest finite magnitude in it
+  __device__ __forceinline__ float largest() const {
+    float m = 0.0f;
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+      struct alignas(16) { T v[PER<T>]; } e;
+      __builtin_memcpy(&e, &v[i], 16);
+#pragma unroll
+      for (int j = 0; j < PER<T>; ++j) {
+        const float x = fabsf((float)e.v[j]);
+        m = x < INFINITY ? fmaxf(m, x) : m;
+      }
+    }
+    return m;
+  }
+};
+
+// Four results side by side, from column c on of a row of `width`.
+template <typename T, bool WIDE>
+__device__ __forceinline__ void store_four(T *row, int c, int width, const float4v &x) {
+  if constexpr (WIDE) {
+    struct alignas(4 * sizeof(T)) { T v[4]; } e;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) e.v[i] = (T)x[i];
+    if (c < width) *reinterpret_cast<decltype(e) *>(row + c) = e;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (c + i < width) row[c + i] = (T)x[i];
+  }
+}
+
+__device__ __forceinline__ float wave_max(float m) {
+#pragma unroll
+  for (int o = 32; o; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, WAVE));
+  return m;
+}
+
+// The power of two that takes numbers up to `most` below 2^top (1 where most is
+// 0 or no number).
+__device__ __forceinline__ float power_below(float most, int top) {
+  if (!(most > 0.0f) || !(most < INFINITY)) return 1.0f;
+  int e = top - 1 - ilogbf(most);
+  e = e < -120 ? -120 : e > 120 ? 120 : e;
+  return ldexpf(1.0f, e);
+}
+
+}  // namespace tile
+}  // namespace fstc

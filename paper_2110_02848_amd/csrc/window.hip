@@ -1,0 +1,1159 @@
+// Attention to a window of frames and a sequence's first ones
+// (fst_window_attention_run, its gradients, its single step and the filling of
+// its caches).
+//
+// Frame t of a sequence sees frame s <= t if t - s < window or s < sinks:
+//   z = scale q_t . k_s,  y_t = sum of e^(z - lse_t) v_s,  lse_t = log sum of e^z
+// in one pass over the frames that a block of queries sees, with the running
+// maximum and sum of the softmax.  Scores are products of (k rows) x (q columns),
+// whose results are an operand of the product with v in the registers that they
+// are in, and whose statistics are a lane's own.  Exponentials are powers of 2.
+//
+// Back, with P = e^(z - lse) and delta_t = y_t . dy_t:
+//   dS = P (dy v^T - delta),  dq = scale dS k,  dk = scale dS^T q,  dv = P^T dy
+// from scores that are computed again: one kernel by queries (dq), one by keys (dk,
+// dv), so that every sum has one owner and one order.  First frames are seen by
+// all later queries: what lies outside the window is summed by units of
+// queries first (k_window_sinks), and the owner of the keys adds the units.
+#include <initializer_list>
+
+#include "sequences.h"
+#include "tiles.h"
+
+namespace fstc {
+
+using namespace tile;
+
+namespace {
+
+constexpr int WNT = 256;             // threads
+constexpr int WNW = WNT / WAVE;
+constexpr int KEYS = 64;             // of a tile of keys
+constexpr int QT = 2;                // tiles of 16 queries (or keys) of a wavefront
+constexpr int BLOCK = 16 * QT * WNW; // queries, or keys, of a workgroup
+constexpr int FEW = 64;              // frames
+constexpr float LOG2 = 0.69314718055994530942f, LOG2E = 1.44269502162933349609375f;
+
+__device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
+
+template <int N, int M>
+__device__ __forceinline__ bool finite(const float4v (&x)[N][M]) {
+  float z = 0.0f;
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+#pragma unroll
+    for (int j = 0; j < M; ++j)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) z = fmaf(x[i][j][r], 0.0f, z);
+  return __all(z == 0.0f);
+}
+
+// a's numbers, and b's in the place of those that are none.
+__device__ __forceinline__ float4v either(float4v a, const float4v &b) {
+#pragma unroll
+  for (int r = 0; r < 4; ++r) a[r] = fabsf(a[r]) < INFINITY ? a[r] : b[r];
+  return a;
+}
+
+// Sum of a[i] b[i], i < D.
+template <typename T>
+__device__ __forceinline__ float dot(const T *a, const T *b, int D) {
+  float x = 0.0f;
+  for (int i = 0; i < D; ++i) x = fmaf((float)a[i], (float)b[i], x);
+  return x;
+}
+
+// Whether query t sees no frame but itself: then dS is 0 and no difference of two
+// sums.
+__device__ __forceinline__ bool sees_one(long long t, int window, int sinks) {
+  return t == 0 || (window == 1 && sinks == 0);
+}
+
+// The frames that queries [lo, hi) of a sequence see: sinks [0, sinks), before
+// the window of any of them, then [first, hi).
+struct Seen {
+  long long first;
+  int sinks, sink_tiles, tiles;
+};
+__device__ __forceinline__ Seen seen_by(long long lo, long long hi, int window, int sinks) {
+  Seen s;
+  s.first = lo - window + 1 > 0 ? lo - window + 1 : 0;
+  s.sinks = (int)(sinks < s.first ? sinks : s.first);
+  s.sink_tiles = (s.sinks + KEYS - 1) / KEYS;
+  s.tiles = s.sink_tiles + (int)((hi - s.first + KEYS - 1) / KEYS);
+  return s;
+}
+
+// ---------------------------------------------------------------------------
+// forward
+// ---------------------------------------------------------------------------
+
+// A query row against the frames that it sees alone, term by term, for four columns
+// from d0 on.  The products also take the others' v, times 0, which makes no number
+// of an infinity or a NaN that the query does not see: where a result is none, it
+// is taken again.  The same below for the gradients.
+template <typename T>
+__device__ __noinline__ float4v exact_row(const T *q, const T *k, long long ks, const T *v,
+                                          long long vs, int D, long long t, int window,
+                                          int sinks, float c, float m, int d0) {
+  float4v x{};
+  for (long long s = 0; s <= t; ++s) {
+    if (t - s >= window && s >= sinks) {
+      s = t - window;
+      continue;
+    }
+    const float p = exp2_of(dot(q, k + s * ks, D) * c - m);
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+      if (d0 + r < D) x[r] = fmaf(p, (float)v[s * vs + d0 + r], x[r]);
+  }
+  return x;
+}
+
+template <typename T, int P, bool WIDE>
+__global__ __launch_bounds__(WNT) void k_window(WinArgs a) {
+  __shared__ __attribute__((aligned(16))) T s_k[KEYS * LD<T, P>];
+  __shared__ __attribute__((aligned(16))) T s_v[KEYS * LD<T, P>];
+  constexpr int DT = P / 16, DS = P / 32;
+  const int lane = threadIdx.x & (WAVE - 1), l16 = lane & 15, lg = lane >> 4;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
+  const int h = blockIdx.y, g = h / (a.H / a.G), D = a.D;
+  Unit u;
+  if (!unit_of(a.off, a.n, a.N, BLOCK, false, blockIdx.x, u) || u.lo >= u.hi) return;
+
+  const T *q = static_cast<const T *>(a.q) + u.b * a.qs + (long long)h * D;
+  const T *k = static_cast<const T *>(a.k) + u.b * a.ks + (long long)g * D;
+  const T *v = static_cast<const T *>(a.v) + u.b * a.vs + (long long)g * D;
+  const long long tw = u.lo + w * 16 * QT;  // the wavefront's first query
+  Frag<T> qf[QT][DS];
+#pragma unroll
+  for (int i = 0; i < QT; ++i) {
+    const long long t = tw + 16 * i + l16;
+#pragma unroll
+    for (int s = 0; s < DS; ++s)
+#pragma unroll
+      for (int e = 0; e < (int)sizeof(T) / 2; ++e)
+        qf[i][s].v[e] =
+            load_group<T, WIDE>(q + t * a.qs, 32 * s + 8 * lg + e * PER<T>, D, t < u.hi);
+  }
+  const float c = a.scale * LOG2E;
+  float m[QT], l[QT];
+  float4v o[DT][QT] = {};
+#pragma unroll
+  for (int i = 0; i < QT; ++i) m[i] = -INFINITY, l[i] = 0.0f;
+
+  const Seen sn = seen_by(u.lo, u.hi, a.window, a.sinks);
+  Stage<T, P, KEYS, WNT, WIDE> rk, rv;
+  const auto fetch = [&](int tile) {
+    const bool sink = tile < sn.sink_tiles;
+    const long long s0 = sink ? (long long)tile * KEYS
+                              : sn.first + (long long)(tile - sn.sink_tiles) * KEYS;
+    const long long end = sink ? sn.sinks : u.hi;
+    const int count = (int)(end - s0 < KEYS ? end - s0 : KEYS);
+    rk.fetch(k, a.ks, D, s0, 1, count);
+    rv.fetch(v, a.vs, D, s0, 1, count);
+  };
+  fetch(0);
+  for (int tile = 0; tile < sn.tiles; ++tile) {
+    __syncthreads();
+    rk.store(s_k);
+    rv.store(s_v);
+    __syncthreads();
+    if (tile + 1 < sn.tiles) fetch(tile + 1);
+    const bool sink = tile < sn.sink_tiles;
+    const long long s0 = sink ? (long long)tile * KEYS
+                              : sn.first + (long long)(tile - sn.sink_tiles) * KEYS;
+    // none of the wavefront's queries sees the tile; all see all of it
+    if (!sink && (s0 > tw + 16 * QT - 1 || (tw - (s0 + KEYS - 1) >= a.window && s0 >= a.sinks)))
+      continue;
+    const bool whole = sink ? s0 + KEYS <= sn.sinks
+                            : s0 + KEYS - 1 <= tw && tw + 16 * QT - 1 - s0 < a.window;
+    float4v x[4][QT] = {};
+#pragma unroll
+    for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+      for (int s = 0; s < DS; ++s) {
+        const Frag<T> f = rows<T, P>(s_k, 16 * kt, 32 * s, lane);
+#pragma unroll
+        for (int i = 0; i < QT; ++i) x[kt][i] = mac(f, qf[i][s], x[kt][i]);
+      }
+#pragma unroll
+    for (int i = 0; i < QT; ++i) {
+      float top = -INFINITY;
+#pragma unroll
+      for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          x[kt][i][r] *= c;
+          if (!whole) {
+            const long long t = tw + 16 * i + l16, s = s0 + 16 * kt + 4 * lg + r;
+            const bool sees = sink ? s < sn.sinks
+                                   : s <= t && (t - s < a.window || s < a.sinks);
+            if (!sees) x[kt][i][r] = -INFINITY;
+          }
+          top = fmaxf(top, x[kt][i][r]);
+        }
+      top = fmaxf(top, __shfl_xor(top, 16, WAVE));
+      top = fmaxf(top, __shfl_xor(top, 32, WAVE));
+      const float next = fmaxf(m[i], top);
+      const float shift = next == -INFINITY ? 0.0f : next;
+      const float less = exp2_of(m[i] - shift);
+      m[i] = next;
+      l[i] *= less;
+#pragma unroll
+      for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          x[kt][i][r] = exp2_of(x[kt][i][r] - shift);
+          l[i] += x[kt][i][r];
+        }
+#pragma unroll
+      for (int d = 0; d < DT; ++d) o[d][i] *= less;
+    }
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      Frag<T> p[QT];
+#pragma unroll
+      for (int i = 0; i < QT; ++i) p[i] = pack<T>(x[2 * t][i], x[2 * t + 1][i]);
+#pragma unroll
+      for (int d = 0; d < DT; ++d) {
+        const Frag<T> f = columns<T, P>(s_v, 32 * t, 16 * d, lane);
+#pragma unroll
+        for (int i = 0; i < QT; ++i) o[d][i] = mac(f, p[i], o[d][i]);
+      }
+    }
+  }
+  if (!finite(o)) {
+#pragma unroll
+    for (int i = 0; i < QT; ++i) {
+      const long long t = tw + 16 * i + l16;
+      if (t >= u.hi) continue;
+#pragma unroll
+      for (int d = 0; d < DT; ++d)
+        if (16 * d + 4 * lg < D)
+          o[d][i] = either(
+              o[d][i], exact_row<T>(q + t * a.qs, k, a.ks, v, a.vs, D, t, a.window, a.sinks, c,
+                                    m[i] == -INFINITY ? 0.0f : m[i], 16 * d + 4 * lg));
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < QT; ++i) {
+    l[i] += __shfl_xor(l[i], 16, WAVE);
+    l[i] += __shfl_xor(l[i], 32, WAVE);
+    const long long t = tw + 16 * i + l16;
+    if (t >= u.hi) continue;
+    const float f = 1.0f / l[i];
+    T *y = static_cast<T *>(a.o) + (u.b + t) * a.os + (long long)h * D;
+#pragma unroll
+    for (int d = 0; d < DT; ++d) store_four<T, WIDE>(y, 16 * d + 4 * lg, D, o[d][i] * f);
+    if (lg == 0) a.lse[(u.b + t) * a.H + h] = (m[i] + log2f(l[i])) * LOG2;
+  }
+}
+
+// ---------------------------------------------------------------------------
+// gradients
+// ---------------------------------------------------------------------------
+
+// delta = y . dy of each row and head, 16 lanes each; float16: the largest
+// lengths of rows of dy and v, whose product bounds dS.
+template <typename T>
+__global__ __launch_bounds__(WNT) void k_window_delta(WinArgs a) {
+  const long long all = a.N * a.H;
+  const int l16 = threadIdx.x & 15;
+  float top = 0.0f, topv = 0.0f;
+  for (long long i = ((long long)blockIdx.x * WNT + threadIdx.x) / 16; i < all;
+       i += (long long)gridDim.x * (WNT / 16)) {
+    const long long row = i / a.H;
+    const int h = (int)(i % a.H);
+    const T *y = static_cast<const T *>(a.y) + row * a.ys + (long long)h * a.D;
+    const T *gy = static_cast<const T *>(a.gy) + row * a.gys + (long long)h * a.D;
+    float s = 0.0f, n = 0.0f, nv = 0.0f;
+    for (int d = l16; d < a.D; d += 16) {
+      const float g = (float)gy[d];
+      s = fmaf((float)y[d], g, s);
+      n = fmaf(g, g, n);
+    }
+    if (a.most && h < a.G) {
+      const T *v = static_cast<const T *>(a.v) + row * a.vs + (long long)h * a.D;
+      for (int d = l16; d < a.D; d += 16) nv = fmaf((float)v[d], (float)v[d], nv);
+    }
+#pragma unroll
+    for (int o = 8; o; o >>= 1) {
+      s += __shfl_xor(s, o, WAVE);
+      n += __shfl_xor(n, o, WAVE);
+      nv += __shfl_xor(nv, o, WAVE);
+    }
+    if (l16 == 0) a.delta[i] = s;
+    top = n < INFINITY ? fmaxf(top, n) : top;
+    topv = nv < INFINITY ? fmaxf(topv, nv) : topv;
+  }
+  if (!a.most) return;
+  top = wave_max(top), topv = wave_max(topv);
+  // (a maximum of non-negative floats, as integers: any order gives the same)
+  if ((threadIdx.x & (WAVE - 1)) == 0) {
+    atomicMax(a.most, __float_as_uint(sqrtf(top)));
+    atomicMax(a.most + 1, __float_as_uint(sqrtf(topv)));
+  }
+}
+__global__ void k_window_zero(uint32_t *p) { p[threadIdx.x] = 0; }
+
+// float16: the power of two that dS is scaled by.
+template <typename T>
+__device__ __forceinline__ float ds_scale(const WinArgs &a) {
+  if constexpr (std::is_same<T, f16>::value)
+    return power_below(2.0f * __uint_as_float(a.most[0]) * __uint_as_float(a.most[1]), 15);
+  return 1.0f;
+}
+
+template <typename T>
+__device__ __noinline__ float4v exact_dq(const T *q, const T *gy, const T *k, long long ks,
+                                         const T *v, long long vs, int D, long long t,
+                                         int window, int sinks, float c, float lse, float delta,
+                                         float up, int d0) {
+  float4v x{};
+  for (long long s = 0; s <= t; ++s) {
+    if (t - s >= window && s >= sinks) {
+      s = t - window;
+      continue;
+    }
+    const float e = exp2_of(fmaf(dot(q, k + s * ks, D), c, -lse));
+    const float d = e * (dot(gy, v + s * vs, D) - delta) * up;
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+      if (d0 + r < D) x[r] = fmaf(d, (float)k[s * ks + d0 + r], x[r]);
+  }
+  return x;
+}
+
+// What queries [t0, t1) of a head that see key s add to the gradients by it; or (run
+// > 0) the wave-th 32 in each run of them, those that are a window past it.
+struct TwoFours {
+  float4v k, v;
+};
+template <typename T>
+__device__ __noinline__ TwoFours exact_dkv(const T *q, long long qs, const T *gy, long long gys,
+                                           const float *lse, const float *delta, int H, int D,
+                                           const T *k, const T *v, long long s, long long t0,
+                                           long long t1, int run, int wave, int window,
+                                           int sinks, float c, float up, int d0) {
+  TwoFours x{};
+  for (long long t = t0; t < t1; ++t) {
+    if (run && ((t - t0) % run / 32 != wave || t - s < window)) continue;
+    const T *qt = q + t * qs, *gt = gy + t * gys;
+    const float e = exp2_of(fmaf(dot(qt, k, D), c, -lse[t * H] * LOG2E));
+    const float d =
+        sees_one(t, window, sinks) ? 0.0f : e * (dot(gt, v, D) - delta[t * H]) * up;
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+      if (d0 + r < D) {
+        x.k[r] = fmaf(d, (float)qt[d0 + r], x.k[r]);
+        x.v[r] = fmaf(e, (float)gt[d0 + r], x.v[r]);
+      }
+  }
+  return x;
+}
+
+// Gradients by queries.  delta from y as it was rounded is off by half a spacing of
+// y, which is next to nothing beside dS of many frames but as much as the rounding
+// of dS beside few: queries of a sequence's first block, and of windows up to FEW
+// frames, have it summed again from P and dy v^T, before their dS.
+template <typename T, int P, bool WIDE>
+__global__ __launch_bounds__(WNT) void k_window_dq(WinArgs a) {
+  __shared__ __attribute__((aligned(16))) T s_k[KEYS * LD<T, P>];
+  __shared__ __attribute__((aligned(16))) T s_v[KEYS * LD<T, P>];
+  constexpr int DT = P / 16, DS = P / 32;
+  const int lane = threadIdx.x & (WAVE - 1), l16 = lane & 15, lg = lane >> 4;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
+  const int h = blockIdx.y, g = h / (a.H / a.G), D = a.D;
+  Unit u;
+  if (!unit_of(a.off, a.n, a.N, BLOCK, false, blockIdx.x, u) || u.lo >= u.hi) return;
+
+  const T *q = static_cast<const T *>(a.q) + u.b * a.qs + (long long)h * D;
+  const T *gy = static_cast<const T *>(a.gy) + u.b * a.gys + (long long)h * D;
+  const T *k = static_cast<const T *>(a.k) + u.b * a.ks + (long long)g * D;
+  const T *v = static_cast<const T *>(a.v) + u.b * a.vs + (long long)g * D;
+  const long long tw = u.lo + w * 16 * QT;
+  Frag<T> qf[QT][DS], gf[QT][DS];
+  float lse[QT], delta[QT];
+#pragma unroll
+  for (int i = 0; i < QT; ++i) {
+    const long long t = tw + 16 * i + l16;
+    const bool there = t < u.hi;
+#pragma unroll
+    for (int s = 0; s < DS; ++s)
+#pragma unroll
+      for (int e = 0; e < (int)sizeof(T) / 2; ++e) {
+        const int at = 32 * s + 8 * lg + e * PER<T>;
+        qf[i][s].v[e] = load_group<T, WIDE>(q + t * a.qs, at, D, there);
+        gf[i][s].v[e] = load_group<T, WIDE>(gy + t * a.gys, at, D, there);
+      }
+    lse[i] = there && !sees_one(t, a.window, a.sinks) ? a.lse[(u.b + t) * a.H + h] * LOG2E
+                                                      : INFINITY;
+    delta[i] = there ? a.delta[(u.b + t) * a.H + h] : 0.0f;
+  }
+  const float c = a.scale * LOG2E, up = ds_scale<T>(a);
+  float4v o[DT][QT] = {};
+  const Seen sn = seen_by(u.lo, u.hi, a.window, a.sinks);
+  Stage<T, P, KEYS, WNT, WIDE> rk, rv;
+  const auto fetch = [&](int tile) {
+    const bool sink = tile < sn.sink_tiles;
+    const long long s0 = sink ? (long long)tile * KEYS
+                              : sn.first + (long long)(tile - sn.sink_tiles) * KEYS;
+    const long long end = sink ? sn.sinks : u.hi;
+    const int count = (int)(end - s0 < KEYS ? end - s0 : KEYS);
+    rk.fetch(k, a.ks, D, s0, 1, count);
+    rv.fetch(v, a.vs, D, s0, 1, count);
+  };
+  // sweep 0 sums delta, sweep 1 dq
+  const bool few = sizeof(T) == 2 && (u.lo == 0 || a.window + a.sinks <= FEW);
+  float sum[QT] = {};
+  const int steps = few ? 2 * sn.tiles : sn.tiles;
+  fetch(0);
+  for (int step = 0; step < steps; ++step) {
+    const bool sums = few && step < sn.tiles;
+    const int tile = few && !sums ? step - sn.tiles : step;
+    if (few && step == sn.tiles) {
+#pragma unroll
+      for (int i = 0; i < QT; ++i) {
+        sum[i] += __shfl_xor(sum[i], 16, WAVE);
+        sum[i] += __shfl_xor(sum[i], 32, WAVE);
+        delta[i] = sum[i];
+        const long long t = tw + 16 * i + l16;
+        if (lg == 0 && t < u.hi) a.delta[(u.b + t) * a.H + h] = sum[i];
+      }
+    }
+    __syncthreads();
+    rk.store(s_k);
+    rv.store(s_v);
+    __syncthreads();
+    if (step + 1 < steps) fetch(tile + 1 < sn.tiles ? tile + 1 : 0);
+    const bool sink = tile < sn.sink_tiles;
+    const long long s0 = sink ? (long long)tile * KEYS
+                              : sn.first + (long long)(tile - sn.sink_tiles) * KEYS;
+    if (!sink && (s0 > tw + 16 * QT - 1 || (tw - (s0 + KEYS - 1) >= a.window && s0 >= a.sinks)))
+      continue;
+    const bool whole = sink ? s0 + KEYS <= sn.sinks
+                            : s0 + KEYS - 1 <= tw && tw + 16 * QT - 1 - s0 < a.window;
+#pragma unroll
+    for (int t2 = 0; t2 < 2; ++t2) {
+      float4v x[2][QT] = {}, y[2][QT] = {};
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int s = 0; s < DS; ++s) {
+          const Frag<T> f = rows<T, P>(s_k, 32 * t2 + 16 * b, 32 * s, lane);
+          const Frag<T> f2 = rows<T, P>(s_v, 32 * t2 + 16 * b, 32 * s, lane);
+#pragma unroll
+          for (int i = 0; i < QT; ++i) {
+            x[b][i] = mac(f, qf[i][s], x[b][i]);
+            y[b][i] = mac(f2, gf[i][s], y[b][i]);
+          }
+        }
+      Frag<T> p[QT];
+#pragma unroll
+      for (int i = 0; i < QT; ++i) {
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const float e = exp2_of(fmaf(x[b][i][r], c, -lse[i]));
+            float d = sums ? e * y[b][i][r] : e * (y[b][i][r] - delta[i]) * up;
+            if (!whole) {
+              const long long t = tw + 16 * i + l16, s = s0 + 32 * t2 + 16 * b + 4 * lg + r;
+              const bool sees = sink ? s < sn.sinks
+                                     : s <= t && (t - s < a.window || s < a.sinks);
+              d = sees ? d : 0.0f;
+            }
+            x[b][i][r] = d;
+            sum[i] += d;
+          }
+        p[i] = pack<T>(x[0][i], x[1][i]);
+      }
+      if (sums) continue;
+#pragma unroll
+      for (int d = 0; d < DT; ++d) {
+        const Frag<T> f = columns<T, P>(s_k, 32 * t2, 16 * d, lane);
+#pragma unroll
+        for (int i = 0; i < QT; ++i) o[d][i] = mac(f, p[i], o[d][i]);
+      }
+    }
+  }
+  if (!finite(o)) {
+#pragma unroll
+    for (int i = 0; i < QT; ++i) {
+      const long long t = tw + 16 * i + l16;
+      if (t >= u.hi) continue;
+#pragma unroll
+      for (int d = 0; d < DT; ++d)
+        if (16 * d + 4 * lg < D)
+          o[d][i] = either(
+              o[d][i], exact_dq<T>(q + t * a.qs, gy + t * a.gys, k, a.ks, v, a.vs, D, t, a.window,
+                                   a.sinks, c, lse[i], delta[i], up, 16 * d + 4 * lg));
+    }
+  }
+  const float f = a.scale / up;
+#pragma unroll
+  for (int i = 0; i < QT; ++i) {
+    const long long t = tw + 16 * i + l16;
+    if (t >= u.hi) continue;
+    T *gq = static_cast<T *>(a.gq) + (u.b + t) * a.gqs + (long long)h * D;
+#pragma unroll
+    for (int d = 0; d < DT; ++d) store_four<T, WIDE>(gq, 16 * d + 4 * lg, D, o[d][i] * f);
+  }
+}
+
+// Gradients by keys and values: a workgroup has BLOCK keys of a key head, walks
+// the queries that see them through the window, head after head of its group,
+// and adds what the sinks' units found.
+template <typename T, int P, bool WIDE>
+__global__ __launch_bounds__(WNT) void k_window_dkv(WinArgs a) {
+  __shared__ __attribute__((aligned(16))) T s_q[KEYS * LD<T, P>];
+  __shared__ __attribute__((aligned(16))) T s_g[KEYS * LD<T, P>];
+  __shared__ __attribute__((aligned(16))) float s_lse[KEYS], s_delta[KEYS];
+  constexpr int DT = P / 16, DS = P / 32;
+  const int lane = threadIdx.x & (WAVE - 1), l16 = lane & 15, lg = lane >> 4;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
+  const int g = blockIdx.y, E = a.H / a.G, D = a.D;
+  Unit u;
+  if (!unit_of(a.off, a.n, a.N, BLOCK, false, blockIdx.x, u) || u.lo >= u.hi) return;
+
+  const T *k = static_cast<const T *>(a.k) + u.b * a.ks + (long long)g * D;
+  const T *v = static_cast<const T *>(a.v) + u.b * a.vs + (long long)g * D;
+  const long long sw = u.lo + w * 16 * QT;  // the wavefront's first key
+  Frag<T> kf[QT][DS], vf[QT][DS];
+#pragma unroll
+  for (int i = 0; i < QT; ++i) {
+    const long long s = sw + 16 * i + l16;
+#pragma unroll
+    for (int t = 0; t < DS; ++t)
+#pragma unroll
+      for (int e = 0; e < (int)sizeof(T) / 2; ++e) {
+        const int at = 32 * t + 8 * lg + e * PER<T>;
+        kf[i][t].v[e] = load_group<T, WIDE>(k + s * a.ks, at, D, s < u.hi);
+        vf[i][t].v[e] = load_group<T, WIDE>(v + s * a.vs, at, D, s < u.hi);
+      }
+  }
+  const float c = a.scale * LOG2E, up = ds_scale<T>(a);
+  float4v ok[DT][QT] = {}, ov[DT][QT] = {};
+  const long long end = u.hi - 1 + a.window < u.len ? u.hi - 1 + a.window : u.len;
+  const int tiles = (int)((end - u.lo + KEYS - 1) / KEYS), all = tiles * E;
+  Stage<T, P, KEYS, WNT, WIDE> rq, rg;
+  float r_lse = 0.0f, r_delta = 0.0f;
+  const auto fetch = [&](int j) {
+    const int h = g * E + j / tiles;
+    const long long t0 = u.lo + (long long)(j % tiles) * KEYS;
+    const int count = (int)(end - t0 < KEYS ? end - t0 : KEYS);
+    rq.fetch(static_cast<const T *>(a.q) + u.b * a.qs + (long long)h * D, a.qs, D, t0, 1, count);
+    rg.fetch(static_cast<const T *>(a.gy) + u.b * a.gys + (long long)h * D, a.gys, D, t0, 1,
+             count);
+    if (threadIdx.x < KEYS) {
+      const bool there = (int)threadIdx.x < count;
+      const long long at = (u.b + t0 + threadIdx.x) * a.H + h;
+      r_lse = there ? a.lse[at] * LOG2E : INFINITY;
+      r_delta = there ? a.delta[at] : 0.0f;
+    }
+  };
+  fetch(0);
+  for (int j = 0; j < all; ++j) {
+    __syncthreads();
+    rq.store(s_q);
+    rg.store(s_g);
+    if (threadIdx.x < KEYS) s_lse[threadIdx.x] = r_lse, s_delta[threadIdx.x] = r_delta;
+    __syncthreads();
+    if (j + 1 < all) fetch(j + 1);
+    const long long t0 = u.lo + (long long)(j % tiles) * KEYS;
+    if (t0 + KEYS - 1 < sw || t0 - (sw + 16 * QT - 1) >= a.window) continue;
+    const bool whole = t0 >= sw + 16 * QT - 1 && t0 + KEYS - 1 - sw < a.window;
+#pragma unroll
+    for (int t2 = 0; t2 < 2; ++t2) {
+      float4v x[2][QT] = {}, y[2][QT] = {};
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int s = 0; s < DS; ++s) {
+          const Frag<T> f = rows<T, P>(s_q, 32 * t2 + 16 * b, 32 * s, lane);
+          const Frag<T> f2 = rows<T, P>(s_g, 32 * t2 + 16 * b, 32 * s, lane);
+#pragma unroll
+          for (int i = 0; i < QT; ++i) {
+            x[b][i] = mac(f, kf[i][s], x[b][i]);
+            y[b][i] = mac(f2, vf[i][s], y[b][i]);
+          }
+        }
+      Frag<T> p[QT], ds[QT];
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        const int at = 32 * t2 + 16 * b + 4 * lg;
+        const float4v lse = *reinterpret_cast<const float4v *>(s_lse + at);
+        const float4v delta = *reinterpret_cast<const float4v *>(s_delta + at);
+#pragma unroll
+        for (int i = 0; i < QT; ++i)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            float e = exp2_of(fmaf(x[b][i][r], c, -lse[r]));
+            float d = e * (y[b][i][r] - delta[r]) * up;
+            if (!whole) {
+              const long long t = t0 + at + r, s = sw + 16 * i + l16;
+              const bool sees = s <= t && t - s < a.window && t < end;
+              e = sees ? e : 0.0f;
+              d = sees && !sees_one(t, a.window, a.sinks) ? d : 0.0f;
+            }
+            x[b][i][r] = e;
+            y[b][i][r] = d;
+          }
+      }
+#pragma unroll
+      for (int i = 0; i < QT; ++i) {
+        p[i] = pack<T>(x[0][i], x[1][i]);
+        ds[i] = pack<T>(y[0][i], y[1][i]);
+      }
+#pragma unroll
+      for (int d = 0; d < DT; ++d) {
+        const Frag<T> f = columns<T, P>(s_g, 32 * t2, 16 * d, lane);
+        const Frag<T> f2 = columns<T, P>(s_q, 32 * t2, 16 * d, lane);
+#pragma unroll
+        for (int i = 0; i < QT; ++i) {
+          ov[d][i] = mac(f, p[i], ov[d][i]);
+          ok[d][i] = mac(f2, ds[i], ok[d][i]);
+        }
+      }
+    }
+  }
+  if (!finite(ok) || !finite(ov)) {
+#pragma unroll
+    for (int i = 0; i < QT; ++i) {
+      const long long s = sw + 16 * i + l16;
+      if (s >= u.hi) continue;
+      const long long t1 = s + a.window < u.len ? s + a.window : u.len;
+#pragma unroll
+      for (int d = 0; d < DT; ++d) {
+        if (16 * d + 4 * lg >= D) continue;
+        float4v xk{}, xv{};
+        for (int h = g * E; h < g * E + E; ++h) {
+          const T *qh = static_cast<const T *>(a.q) + u.b * a.qs + (long long)h * D;
+          const T *gh = static_cast<const T *>(a.gy) + u.b * a.gys + (long long)h * D;
+          const TwoFours x = exact_dkv<T>(
+              qh, a.qs, gh, a.gys, a.lse + u.b * a.H + h, a.delta + u.b * a.H + h, a.H, D,
+              k + s * a.ks, v + s * a.vs, s, s, t1, 0, 0, a.window, a.sinks, c, up,
+              16 * d + 4 * lg);
+          xk += x.k;
+          xv += x.v;
+        }
+        ok[d][i] = either(ok[d][i], xk);
+        ov[d][i] = either(ov[d][i], xv);
+      }
+    }
+  }
+  const float f = a.scale / up;
+#pragma unroll
+  for (int i = 0; i < QT; ++i) {
+    const long long s = sw + 16 * i + l16;
+    if (s >= u.hi) continue;
+#pragma unroll
+    for (int d = 0; d < DT; ++d) ok[d][i] *= f;
+    if (s < a.sinks && u.len > a.window) {
+      // units of queries that see it from outside the window, in their order
+      const long long first = rows_before(u.b, u.s, a.unit);
+      const long long n = (u.len + a.unit - 1) / a.unit;
+      for (long long j = a.window / a.unit; j < n; ++j) {
+        const float *p = a.part + (((first + j) * a.G + g) * a.sinks + s) * 2 * P;
+#pragma unroll
+        for (int d = 0; d < DT; ++d) {
+          ok[d][i] += *reinterpret_cast<const float4v *>(p + 16 * d + 4 * lg);
+          ov[d][i] += *reinterpret_cast<const float4v *>(p + P + 16 * d + 4 * lg);
+        }
+      }
+    }
+    T *gk = static_cast<T *>(a.gk) + (u.b + s) * a.gks + (long long)g * D;
+    T *gv = static_cast<T *>(a.gv) + (u.b + s) * a.gvs + (long long)g * D;
+#pragma unroll
+    for (int d = 0; d < DT; ++d) {
+      store_four<T, WIDE>(gk, 16 * d + 4 * lg, D, ok[d][i]);
+      store_four<T, WIDE>(gv, 16 * d + 4 * lg, D, ov[d][i]);
+    }
+  }
+}
+
+// What a unit of queries adds to the gradients of 16 first frames that it sees
+// from outside its window: 32 queries a wavefront at a time, the wavefronts'
+// sums joined in LDS.  Rows of `part` of units without such a query are not
+// written, nor read.
+template <typename T, int P, bool WIDE>
+__global__ __launch_bounds__(WNT) void k_window_sinks(WinArgs a) {
+  constexpr int Q = 32 * WNW, DT = P / 16, DS = P / 32;
+  extern __shared__ __attribute__((aligned(16))) char s_dyn[];
+  T *s_q = reinterpret_cast<T *>(s_dyn), *s_g = s_q + Q * LD<T, P>;
+  float *s_lse = reinterpret_cast<float *>(s_g + Q * LD<T, P>), *s_delta = s_lse + Q;
+  const int lane = threadIdx.x & (WAVE - 1), l16 = lane & 15, lg = lane >> 4;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
+  const int g = blockIdx.y, E = a.H / a.G, D = a.D;
+  const long long s = (long long)blockIdx.z * 16 + l16;  // the lane's key
+  Unit u;
+  if (!unit_of(a.off, a.n, a.N, a.unit, false, blockIdx.x, u) || u.hi <= a.window) return;
+
+  const T *k = static_cast<const T *>(a.k) + u.b * a.ks + (long long)g * D;
+  const T *v = static_cast<const T *>(a.v) + u.b * a.vs + (long long)g * D;
+  const bool mine = s < a.sinks && s < u.len;
+  Frag<T> kf[DS], vf[DS];
+#pragma unroll
+  for (int t = 0; t < DS; ++t)
+#pragma unroll
+    for (int e = 0; e < (int)sizeof(T) / 2; ++e) {
+      const int at = 32 * t + 8 * lg + e * PER<T>;
+      kf[t].v[e] = load_group<T, WIDE>(k + s * a.ks, at, D, mine);
+      vf[t].v[e] = load_group<T, WIDE>(v + s * a.vs, at, D, mine);
+    }
+  const float c = a.scale * LOG2E, up = ds_scale<T>(a);
+  float4v ok[DT] = {}, ov[DT] = {};
+  const long long lo = u.lo > a.window ? u.lo : a.window;
+  const int tiles = (int)((u.hi - lo + Q - 1) / Q), all = tiles * E;
+  Stage<T, P, Q, WNT, WIDE> rq, rg;
+  float r_lse = 0.0f, r_delta = 0.0f;
+  const auto fetch = [&](int j) {
+    const int h = g * E + j / tiles;
+    const long long t0 = lo + (long long)(j % tiles) * Q;
+    const int count = (int)(u.hi - t0 < Q ? u.hi - t0 : Q);
+    rq.fetch(static_cast<const T *>(a.q) + u.b * a.qs + (long long)h * D, a.qs, D, t0, 1, count);
+    rg.fetch(static_cast<const T *>(a.gy) + u.b * a.gys + (long long)h * D, a.gys, D, t0, 1,
+             count);
+    if (threadIdx.x < Q) {
+      const bool there = (int)threadIdx.x < count;
+      const long long at = (u.b + t0 + threadIdx.x) * a.H + h;
+      r_lse = there ? a.lse[at] * LOG2E : INFINITY;
+      r_delta = there ? a.delta[at] : 0.0f;
+    }
+  };
+  fetch(0);
+  for (int j = 0; j < all; ++j) {
+    __syncthreads();
+    rq.store(s_q);
+    rg.store(s_g);
+    if (threadIdx.x < Q) s_lse[threadIdx.x] = r_lse, s_delta[threadIdx.x] = r_delta;
+    __syncthreads();
+    if (j + 1 < all) fetch(j + 1);
+    const long long t0 = lo + (long long)(j % tiles) * Q;
+    float4v x[2] = {}, y[2] = {};
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      const int at = 32 * w + 16 * b;
+#pragma unroll
+      for (int t = 0; t < DS; ++t) {
+        x[b] = mac(rows<T, P>(s_q, at, 32 * t, lane), kf[t], x[b]);
+        y[b] = mac(rows<T, P>(s_g, at, 32 * t, lane), vf[t], y[b]);
+      }
+      const float4v lse = *reinterpret_cast<const float4v *>(s_lse + at + 4 * lg);
+      const float4v delta = *reinterpret_cast<const float4v *>(s_delta + at + 4 * lg);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const long long t = t0 + at + 4 * lg + r;
+        const bool sees = mine && t - s >= a.window && t < u.hi;
+        const float e = exp2_of(fmaf(x[b][r], c, -lse[r]));
+        const float d = e * (y[b][r] - delta[r]) * up;
+        x[b][r] = sees ? e : 0.0f;
+        y[b][r] = sees ? d : 0.0f;
+      }
+    }
+    const Frag<T> p = pack<T>(x[0], x[1]), ds = pack<T>(y[0], y[1]);
+#pragma unroll
+    for (int d = 0; d < DT; ++d) {
+      ov[d] = mac(columns<T, P>(s_g, 32 * w, 16 * d, lane), p, ov[d]);
+      ok[d] = mac(columns<T, P>(s_q, 32 * w, 16 * d, lane), ds, ok[d]);
+    }
+  }
+  float z = 0.0f;
+#pragma unroll
+  for (int d = 0; d < DT; ++d)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) z = fmaf(ok[d][r], 0.0f, fmaf(ov[d][r], 0.0f, z));
+  if (!__all(z == 0.0f) && mine) {
+#pragma unroll
+    for (int d = 0; d < DT; ++d) {
+      if (16 * d + 4 * lg >= D) continue;
+      float4v xk{}, xv{};
+      for (int h = g * E; h < g * E + E; ++h) {
+        const T *qh = static_cast<const T *>(a.q) + u.b * a.qs + (long long)h * D;
+        const T *gh = static_cast<const T *>(a.gy) + u.b * a.gys + (long long)h * D;
+        const TwoFours x = exact_dkv<T>(
+            qh, a.qs, gh, a.gys, a.lse + u.b * a.H + h, a.delta + u.b * a.H + h, a.H, D,
+            k + s * a.ks, v + s * a.vs, s, lo, u.hi, Q, w, a.window, a.sinks, c, up,
+            16 * d + 4 * lg);
+        xk += x.k;
+        xv += x.v;
+      }
+      ok[d] = either(ok[d], xk);
+      ov[d] = either(ov[d], xv);
+    }
+  }
+  // (the sums take as much of LDS as the tiles of a 16-bit type)
+  float *s_sum = reinterpret_cast<float *>(s_dyn);
+  static_assert(WNW * 16 * P * 4 <= 2 * Q * LD<T, P> * (int)sizeof(T), "room for the sums");
+  const float f = a.scale / up;
+#pragma unroll
+  for (int o = 0; o < 2; ++o) {
+    __syncthreads();
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+      *reinterpret_cast<float4v *>(s_sum + (w * 16 + l16) * P + 16 * d + 4 * lg) =
+          o ? ov[d] : ok[d];
+    __syncthreads();
+    for (int i = threadIdx.x; i < 16 * P; i += WNT) {
+      float v = 0.0f;
+#pragma unroll
+      for (int q = 0; q < WNW; ++q) v += s_sum[q * 16 * P + i];
+      const long long key = (long long)blockIdx.z * 16 + i / P;
+      if (key < a.sinks)
+        a.part[((((long long)blockIdx.x * a.G + g) * a.sinks + key) * 2 + o) * P + i % P] =
+            o ? v : v * f;
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// one step
+// ---------------------------------------------------------------------------
+
+// Row of a cache where the frame of position p lies.
+__device__ __forceinline__ int ring(int p, int window, int sinks) {
+  return p < sinks ? p : sinks + (p - sinks) % window;
+}
+
+// 16 query heads of a key head (its group, or a part of it) of a row against a
+// part of its cache, 32 frames a wavefront at a time: k straight from memory as
+// an operand, v through LDS of the wavefront's own.  The row's own frame comes
+// from k and v, and the first part writes it to the cache, where no one reads it.
+template <typename T, int P, bool WIDE>
+__global__ __launch_bounds__(WNT) void k_window_step(WinStepArgs a) {
+  constexpr int DT = P / 16, DS = P / 32, GROUPS = P / PER<T>, LOADS = 32 * GROUPS / WAVE;
+  __shared__ __attribute__((aligned(16))) T s_v[WNW][32 * LD<T, P>];
+  __shared__ float s_m[WNW][16], s_l[WNW][16];
+  static_assert(WNW * BYTES<T, P, 32> >= WNW / 2 * 16 * P * 4, "room for half of the results");
+  const int lane = threadIdx.x & (WAVE - 1), l16 = lane & 15, lg = lane >> 4;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
+  const int E = a.H / a.G, parts = (E + 15) / 16, D = a.D;
+  const int g = blockIdx.y / parts, e0 = blockIdx.y % parts * 16;
+  const int heads = E - e0 < 16 ? E - e0 : 16;  // of this workgroup
+  const long long i = blockIdx.x;
+  const int h0 = g * E + e0;
+  const long long slot = a.slot ? (long long)a.slot[i] : i;
+  const int pos = a.pos[i];
+  const bool idle = slot < 0 || slot >= a.slots || pos < 0;
+  T *y = static_cast<T *>(a.y) + i * a.ys + (long long)h0 * D;
+  if (idle) {
+    if (blockIdx.z == 0)
+      for (int d = threadIdx.x; d < heads * D; d += WNT) y[d] = (T)0.0f;
+    return;
+  }
+  const int L = a.sinks + a.window, own = ring(pos, a.window, a.sinks);
+  const int count = pos < L ? pos + 1 : L;
+  T *kc = static_cast<T *>(a.kc) + slot * L * a.kcs + (long long)g * D;
+  T *vc = static_cast<T *>(a.vc) + slot * L * a.vcs + (long long)g * D;
+  const T *kn = static_cast<const T *>(a.k) + i * a.ks + (long long)g * D;
+  const T *vn = static_cast<const T *>(a.v) + i * a.vs + (long long)g * D;
+  if (blockIdx.z == 0 && e0 == 0)
+    for (int d = threadIdx.x; d < D; d += WNT) {
+      kc[own * a.kcs + d] = kn[d];
+      vc[own * a.vcs + d] = vn[d];
+    }
+  // the part's frames, whole tiles of all wavefronts
+  const int tiles = (count + 31) / 32, share = (tiles + a.splits - 1) / a.splits;
+  const int first = blockIdx.z * share, last = first + share < tiles ? first + share : tiles;
+
+  Frag<T> qf[DS];
+  const T *q = static_cast<const T *>(a.q) + i * a.qs + (long long)(h0 + l16) * D;
+#pragma unroll
+  for (int s = 0; s < DS; ++s)
+#pragma unroll
+    for (int e = 0; e < (int)sizeof(T) / 2; ++e)
+      qf[s].v[e] = load_group<T, WIDE>(q, 32 * s + 8 * lg + e * PER<T>, D, l16 < heads);
+  const float c = a.scale * LOG2E;
+  float m = -INFINITY, l = 0.0f;
+  float4v o[DT] = {};
+  for (int tile = first + w; tile < last; tile += WNW) {
+    const int c0 = tile * 32;
+    int4v vr[LOADS];
+#pragma unroll
+    for (int e = 0; e < LOADS; ++e) {
+      const int at = e * WAVE + lane, r = c0 + at / GROUPS;
+      vr[e] = load_group<T, WIDE>(r == own ? vn : vc + (long long)r * a.vcs,
+                                  at % GROUPS * PER<T>, D, r < count);
+    }
+    float4v x[2] = {};
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      const int r = c0 + 16 * b + l16;
+      const T *p = r == own ? kn : kc + (long long)r * a.kcs;
+#pragma unroll
+      for (int s = 0; s < DS; ++s) {
+        Frag<T> f;
+#pragma unroll
+        for (int e = 0; e < (int)sizeof(T) / 2; ++e)
+          f.v[e] = load_group<T, WIDE>(p, 32 * s + 8 * lg + e * PER<T>, D, r < count);
+        x[b] = mac(f, qf[s], x[b]);
+      }
+    }
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int e = 0; e < LOADS; ++e) {
+      const int at = e * WAVE + lane;
+      *reinterpret_cast<int4v *>(&s_v[w][at / GROUPS * LD<T, P> + at % GROUPS * PER<T>]) = vr[e];
+    }
+    __builtin_amdgcn_wave_barrier();
+    float top = -INFINITY;
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        x[b][r] = c0 + 16 * b + 4 * lg + r < count ? x[b][r] * c : -INFINITY;
+        top = fmaxf(top, x[b][r]);
+      }
+    top = fmaxf(top, __shfl_xor(top, 16, WAVE));
+    top = fmaxf(top, __shfl_xor(top, 32, WAVE));
+    const float next = fmaxf(m, top), shift = next == -INFINITY ? 0.0f : next;
+    const float less = exp2_of(m - shift);
+    m = next;
+    l *= less;
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        x[b][r] = exp2_of(x[b][r] - shift);
+        l += x[b][r];
+      }
+    const Frag<T> p = pack<T>(x[0], x[1]);
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+      o[d] = mac(columns<T, P>(s_v[w], 0, 16 * d, lane), p, o[d] * less);
+  }
+  l += __shfl_xor(l, 16, WAVE);
+  l += __shfl_xor(l, 32, WAVE);
+  if (lg == 0) s_m[w][l16] = m, s_l[w][l16] = l;
+  __syncthreads();
+  // the wavefronts' results joined: each scaled to the largest maximum, then summed
+  float most = -INFINITY, sum = 0.0f;
+#pragma unroll
+  for (int v = 0; v < WNW; ++v) most = fmaxf(most, s_m[v][l16]);
+  const float shift = most == -INFINITY ? 0.0f : most;
+#pragma unroll
+  for (int v = 0; v < WNW; ++v) sum += s_l[v][l16] * exp2_of(s_m[v][l16] - shift);
+  const float less = exp2_of(m - shift);
+  float *s_o = reinterpret_cast<float *>(&s_v[0][0]);  // [half of the waves][16][P]
+#pragma unroll
+  for (int half = WNW / 2; half; half /= 2) {
+    __syncthreads();
+    if (w >= half && w < 2 * half)
+#pragma unroll
+      for (int d = 0; d < DT; ++d)
+        *reinterpret_cast<float4v *>(s_o + ((w - half) * 16 + l16) * P + 16 * d + 4 * lg) =
+            half == WNW / 2 ? o[d] * less : o[d];
+    __syncthreads();
+    if (w < half)
+#pragma unroll
+      for (int d = 0; d < DT; ++d)
+        o[d] = (half == WNW / 2 ? o[d] * less : o[d]) +
+               *reinterpret_cast<float4v *>(s_o + (w * 16 + l16) * P + 16 * d + 4 * lg);
+  }
+  if (w || l16 >= heads) return;
+  if (a.splits == 1) {
+    const float f = 1.0f / sum;
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+      store_four<T, WIDE>(y + (long long)l16 * D, 16 * d + 4 * lg, D, o[d] * f);
+    return;
+  }
+  float *part = a.part + ((i * a.H + h0 + l16) * a.splits + blockIdx.z) * (P + 4);
+#pragma unroll
+  for (int d = 0; d < DT; ++d)
+    *reinterpret_cast<float4v *>(part + 4 + 16 * d + 4 * lg) = o[d];
+  if (lg == 0) part[0] = most, part[1] = sum;
+}
+
+// Joins the parts of a row's head.
+template <typename T, int P>
+__global__ __launch_bounds__(P) void k_window_join(WinStepArgs a) {
+  const long long i = blockIdx.x;
+  const int h = blockIdx.y, d = threadIdx.x;
+  const long long slot = a.slot ? (long long)a.slot[i] : i;
+  if (slot < 0 || slot >= a.slots || a.pos[i] < 0 || d >= a.D) return;
+  const float *part = a.part + (i * a.H + h) * (long long)a.splits * (P + 4);
+  float m = -INFINITY;
+  for (int s = 0; s < a.splits; ++s) m = fmaxf(m, part[s * (P + 4)]);
+  const float shift = m == -INFINITY ? 0.0f : m;
+  float l = 0.0f, x = 0.0f;
+  for (int s = 0; s < a.splits; ++s) {
+    const float *p = part + s * (P + 4);
+    const float f = exp2_of(p[0] - shift);
+    l = fmaf(f, p[1], l);
+    x = fmaf(f, p[4 + d], x);
+  }
+  static_cast<T *>(a.y)[i * a.ys + (long long)h * a.D + d] = (T)(x / l);
+}
+
+// Rows of the caches from the frames of whole sequences: entry c holds the last
+// frame that the ring puts there.
+template <typename T>
+__global__ __launch_bounds__(WNT) void k_window_fill(WinFillArgs a) {
+  const int s = a.first + blockIdx.y, L = a.sinks + a.window;
+  const long long slot = a.slot ? (long long)a.slot[s] : s;
+  if (slot < 0 || slot >= a.slots) return;
+  const long long b = clamped(a.off[s], 0, a.N), len = clamped(a.off[s + 1], b, a.N) - b;
+  for (long long e = blockIdx.x; e < L && e < len; e += gridDim.x) {
+    const long long t = e < a.sinks ? e : e + (len - 1 - e) / a.window * a.window;
+    const T *k = static_cast<const T *>(a.k) + (b + t) * a.ks;
+    const T *v = static_cast<const T *>(a.v) + (b + t) * a.vs;
+    T *kc = static_cast<T *>(a.kc) + (slot * L + e) * a.kcs;
+    T *vc = static_cast<T *>(a.vc) + (slot * L + e) * a.vcs;
+    for (int d = threadIdx.x; d < a.width; d += WNT) kc[d] = k[d], vc[d] = v[d];
+  }
+}
+
+// ---------------------------------------------------------------------------
+// launches
+// ---------------------------------------------------------------------------
+
+// Whether every head's row of each tensor begins at a multiple of 16 bytes and is
+// whole groups of them.
+bool wide_rows(size_t e, int D, std::initializer_list<long long> strides,
+               std::initializer_list<const void *> data) {
+  if (D * e % 16) return false;
+  for (long long t : strides)
+    if (t * e % 16) return false;
+  for (const void *p : data)
+    if (reinterpret_cast<uintptr_t>(p) % 16) return false;
+  return true;
+}
+
+dim3 blocks(const WinArgs &a, long long per, int across) {
+  return dim3((unsigned)(a.N / per + a.n), across);
+}
+
+template <typename T, int P, bool WIDE>
+hipError_t forward_as(const WinArgs &a, hipStream_t s) {
+  k_window<T, P, WIDE><<<blocks(a, BLOCK, a.H), WNT, 0, s>>>(a);
+  return hipGetLastError();
+}
+
+template <typename T, int P, bool WIDE>
+hipError_t sinks_as(const WinArgs &a, hipStream_t s) {
+  constexpr int Q = 32 * WNW;
+  constexpr int lds = 2 * BYTES<T, P, Q> + 2 * Q * (int)sizeof(float);
+  static_assert(lds <= 160 * 1024, "LDS of a CU");
+  dim3 grid = blocks(a, a.unit, a.G);
+  grid.z = (a.sinks + 15) / 16;
+  if (grid.z > 65535) return hipErrorInvalidValue;
+  const hipError_t e =
+      hipFuncSetAttribute(reinterpret_cast<const void *>(k_window_sinks<T, P, WIDE>),
+                          hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+  if (e != hipSuccess) return e;
+  k_window_sinks<T, P, WIDE><<<grid, WNT, lds, s>>>(a);
+  return hipGetLastError();
+}
+
+template <typename T, int P, bool WIDE>
+hipError_t backward_as(const WinArgs &a, hipStream_t s) {
+  if (a.most) k_window_zero<<<1, 2, 0, s>>>(a.most);
+  const long long rows = (a.N * a.H + WNT / 16 - 1) / (WNT / 16);
+  k_window_delta<T><<<(unsigned)(rows < 4096 ? rows : 4096), WNT, 0, s>>>(a);
+  k_window_dq<T, P, WIDE><<<blocks(a, BLOCK, a.H), WNT, 0, s>>>(a);
+  if (a.part) {
+    const hipError_t e = sinks_as<T, P, WIDE>(a, s);
+    if (e != hipSuccess) return e;
+  }
+  k_window_dkv<T, P, WIDE><<<blocks(a, BLOCK, a.G), WNT, 0, s>>>(a);
+  return hipGetLastError();
+}
+
+template <typename T, int P, bool WIDE>
+hipError_t step_as(const WinStepArgs &a, hipStream_t s) {
+  const int E = a.H / a.G;
+  k_window_step<T, P, WIDE>
+      <<<dim3((unsigned)a.n, a.G * ((E + 15) / 16), a.splits), WNT, 0, s>>>(a);
+  if (a.splits > 1) k_window_join<T, P><<<dim3((unsigned)a.n, a.H), P, 0, s>>>(a);
+  return hipGetLastError();
+}
+
+// f<T, P, WIDE>() of a type, a width and an alignment.
+#define FOR_FORM(f, ...)                                                                     \
+  (type == FST_F32   ? D <= 64 ? wide ? f<float, 64, true>(__VA_ARGS__)                      \
+                                      : f<float, 64, false>(__VA_ARGS__)                     \
+                               : wide ? f<float, 128, true>(__VA_ARGS__)                     \
+                                      : f<float, 128, false>(__VA_ARGS__)                    \
+   : type == FST_F16 ? D <= 64 ? wide ? f<f16, 64, true>(__VA_ARGS__)                        \
+                                      : f<f16, 64, false>(__VA_ARGS__)                       \
+                               : wide ? f<f16, 128, true>(__VA_ARGS__)                       \
+                                      : f<f16, 128, false>(__VA_ARGS__)                      \
+                     : D <= 64 ? wide ? f<bf16, 64, true>(__VA_ARGS__)                       \
+                                      : f<bf16, 64, false>(__VA_ARGS__)                      \
+                               : wide ? f<bf16, 128, true>(__VA_ARGS__)                      \
+                                      : f<bf16, 128, false>(__VA_ARGS__))
+
+int padded(int D) { return D <= 64 ? 64 : 128; }
+
+constexpr int MAX_ACROSS = 65535;  // of a grid's second and third dimension
+
+}  // namespace
+
+hipError_t launch_window(const WinArgs &a, int type, hipStream_t s) {
+  if (a.H > MAX_ACROSS) return hipErrorInvalidValue;
+  const int D = a.D;
+  const bool wide = wide_rows(type_bytes(type), D, {a.qs, a.ks, a.vs, a.os}, {a.q, a.k, a.v, a.o});
+  return FOR_FORM(forward_as, a, s);
+}
+
+// (also without workspace: then `need` is all that is set)
+hipError_t launch_window_grads(WinArgs a, int type, void *ws, size_t *need, hipStream_t s) {
+  if (a.H > MAX_ACROSS) return hipErrorInvalidValue;
+  const int D = a.D;
+  const size_t delta = ((size_t)a.N * a.H + 3) / 4 * 4;
+  // (a sequence has to be longer than the window for its first frames to be seen
+  // from outside it)
+  const bool sinks = a.sinks > 0 && a.N > a.window;
+  a.unit = 512;
+  const size_t part =
+      sinks ? (size_t)(a.N / a.unit + a.n) * a.G * a.sinks * 2 * padded(D) : 0;
+  *need = (4 + delta + part) * sizeof(float);
+  if (!ws) return hipSuccess;
+  float *p = static_cast<float *>(ws);
+  a.most = type == FST_F16 ? reinterpret_cast<uint32_t *>(p) : nullptr;
+  a.delta = p + 4;
+  a.part = sinks ? p + 4 + delta : nullptr;
+  const bool wide = wide_rows(type_bytes(type), D, {a.qs, a.ks, a.vs, a.gys, a.gqs, a.gks, a.gvs},
+                              {a.q, a.k, a.v, a.gy, a.gq, a.gk, a.gv});
+  return FOR_FORM(backward_as, a, s);
+}
+
+hipError_t launch_window_step(WinStepArgs a, int type, void *ws, size_t *need, hipStream_t s) {
+  const int D = a.D, E = a.H / a.G;
+  const long long groups = (long long)a.G * ((E + 15) / 16);
+  if (groups > MAX_ACROSS || a.H > MAX_ACROSS) return hipErrorInvalidValue;
+  // enough workgroups for the card, none with less than a tile a wavefront
+  const long long most = ((long long)a.sinks + a.window + 32 * WNW - 1) / (32 * WNW);
+  long long splits = (512 + a.n * groups - 1) / (a.n * groups);
+  splits = splits < most ? splits : most;
+  a.splits = (int)(splits < 64 ? splits : 64);
+  *need = a.splits > 1
+              ? (size_t)a.n * a.H * a.splits * (padded(D) + 4) * sizeof(float)
+              : 0;
+  if (!ws) return hipSuccess;
+  a.part = static_cast<float *>(ws);
+  const bool wide = wide_rows(type_bytes(type), D, {a.qs, a.ks, a.vs, a.ys, a.kcs, a.vcs},
+                              {a.q, a.k, a.v, a.y, a.kc, a.vc});
+  return FOR_FORM(step_as, a, s);
+}
+
+hipError_t launch_window_fill(const WinFillArgs &a, int type, hipStream_t s) {
+  const long long L = (long long)a.sinks + a.window;
+  for (int s0 = 0; s0 < a.n; s0 += MAX_ACROSS) {
+    WinFillArgs b = a;
+    b.first = s0;
+    const int n = a.n - s0 < MAX_ACROSS ? a.n - s0 : MAX_ACROSS;
+    const dim3 grid((unsigned)(L < 1024 ? L : 1024), n);
+    if (type == FST_F32)
+      k_window_fill<float><<<grid, WNT, 0, s>>>(b);
+    else if (type == FST_F16)
+      k_window_fill<f16><<<grid, WNT, 0, s>>>(b);
+    else
+      k_window_fill<bf16><<<grid, WNT, 0, s>>>(b);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace fstc

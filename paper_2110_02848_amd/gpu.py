@@ -50,6 +50,8 @@ FST_RECURRENCE_MAX_SEQS = 1 << 22
 FST_RECURRENCE_SAVE_ROWS = 64
 FST_HEAD_MAX_ROWS = 1 << 25
 FST_HEAD_MAX_COLS = 1 << 22
+FST_NORM_MAX_WIDTH = 512
+FST_ATTENTION_MAX_WIDTH = 128
 
 PHASES = ("preprocess", "forward", "backward", "count", "fill")
 
@@ -98,6 +100,27 @@ class _Recurrence(ctypes.Structure):
     _fields_ = [("num_seqs", ctypes.c_int32), ("offset", ctypes.c_void_p),
                 ("reverse", ctypes.c_int32), ("x", _Matrix), ("gate", _Matrix),
                 ("state", ctypes.c_void_p)]
+
+
+class _HeadNorms(ctypes.Structure):
+    _fields_ = [("q", _Matrix), ("k", _Matrix), ("width", ctypes.c_int32),
+                ("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p),
+                ("freq", ctypes.c_void_p), ("num_freq", ctypes.c_int32),
+                ("pos", ctypes.c_void_p), ("pairs", ctypes.c_int32), ("eps", ctypes.c_float)]
+
+
+class _LinearAttention(ctypes.Structure):
+    _fields_ = [("num_seqs", ctypes.c_int32), ("offset", ctypes.c_void_p),
+                ("reverse", ctypes.c_int32), ("heads", ctypes.c_int32),
+                ("log_decay", ctypes.c_void_p), ("scale", ctypes.c_float),
+                ("q", _Matrix), ("k", _Matrix), ("v", _Matrix), ("state", ctypes.c_void_p)]
+
+
+class _WindowAttention(ctypes.Structure):
+    _fields_ = [("num_seqs", ctypes.c_int32), ("offset", ctypes.c_void_p),
+                ("heads", ctypes.c_int32), ("kv_heads", ctypes.c_int32),
+                ("window", ctypes.c_int32), ("sinks", ctypes.c_int32),
+                ("scale", ctypes.c_float), ("q", _Matrix), ("k", _Matrix), ("v", _Matrix)]
 
 
 class _Stats(ctypes.Structure):
@@ -183,7 +206,18 @@ def load():
     P = ctypes.c_void_p
     M = ctypes.POINTER(_Matrix)
     R = ctypes.POINTER(_Recurrence)
+    A, L, W = (ctypes.POINTER(t) for t in (_HeadNorms, _LinearAttention, _WindowAttention))
+    I, F = ctypes.c_int32, ctypes.c_float
     for name, args in dict(
+            fst_head_norms_run=[P, A, M, M, P],
+            fst_head_norms_grads=[P, A, M, M, M, M, P, P, P],
+            fst_linear_attention_run=[P, L, M, P, P],
+            fst_linear_attention_grads=[P, L, M, P, M, M, M, P, P],
+            fst_linear_attention_step=[P, M, M, M, I, P, F, P, P, P, I, M, P],
+            fst_window_attention_run=[P, W, M, P, P],
+            fst_window_attention_grads=[P, W, M, P, M, M, M, M, P],
+            fst_window_attention_step=[P, M, M, M, I, I, I, I, F, P, P, I, M, M, M, P],
+            fst_window_attention_fill=[P, I, P, M, M, I, I, P, I, M, M, P],
             fst_recurrence_run=[P, R, M, P, P, P],
             fst_recurrence_grads=[P, R, P, M, P, M, M, P, P],
             fst_recurrence_step=[P, M, M, P, P, P, ctypes.c_int32, M, P],
@@ -255,11 +289,30 @@ class _Marshal:
     each call (a context is one thread's)."""
     _VIEW = struct.Struct("<Qqqqi")
     _RECURRENCE = struct.Struct("<i4xQi4xQqqqi4xQqqqi4xQ")
+    _NORMS = struct.Struct("<Qqqqi4xQqqqi4xi4xQQQi4xQif")
+    _LINEAR = struct.Struct("<i4xQiiQf4xQqqqi4xQqqqi4xQqqqi4xQ")
+    _WINDOW = struct.Struct("<i4xQiiiif4xQqqqi4xQqqqi4xQqqqi4x")
 
     def __init__(self):
-        self._m = [_Matrix() for _ in range(4)]
+        self._m = [_Matrix() for _ in range(6)]
         self._ref = [ctypes.byref(m) for m in self._m]
         self._r = _Recurrence()
+        self._a, self._l, self._w = _HeadNorms(), _LinearAttention(), _WindowAttention()
+
+    def norms(self, q, k, width, q_weight, k_weight, freq, num_freq, pos, pairs, eps):
+        self._NORMS.pack_into(self._a, 0, *_view(q, "q"), *_view(k, "k"), width, q_weight or 0,
+                              k_weight or 0, freq or 0, num_freq, pos or 0, pairs, eps)
+        return self._a
+
+    def linear(self, n, offset, reverse, heads, log_decay, scale, q, k, v, state):
+        self._LINEAR.pack_into(self._l, 0, n, offset or 0, reverse, heads, log_decay or 0, scale,
+                               *_view(q, "q"), *_view(k, "k"), *_view(v, "v"), state or 0)
+        return self._l
+
+    def window(self, n, offset, heads, kv_heads, window, sinks, scale, q, k, v):
+        self._WINDOW.pack_into(self._w, 0, n, offset or 0, heads, kv_heads, window, sinks, scale,
+                               *_view(q, "q"), *_view(k, "k"), *_view(v, "v"))
+        return self._w
 
     def matrix(self, i, t, name):
         self._VIEW.pack_into(self._m[i], 0, *_view(t, name))
@@ -290,6 +343,13 @@ def _array(t, name, dtype, n):
 def _address(t):
     """Address of a tensor made here (None, or nothing in it: NULL)."""
     return t.data_ptr() if t is not None and t.numel() else None
+
+
+def _int32(v, name):
+    v = int(v)
+    if not -(1 << 31) <= v < 1 << 31:
+        raise ValueError(f"{name}: {v} does not fit 32 bits")
+    return v
 
 
 GRAPH_DTYPES = dict(arc_offset=np.int32, src=np.int32, dst=np.int32, ilabel=np.int32,
@@ -687,6 +747,234 @@ class Composer:
             self._pass.made(2, y, _types[x.dtype]), self._call_stream(stream))
         _check(rc, "fst_recurrence_step")
         return y, out
+
+    # ---- attention over frames ----
+
+    def head_norms(self, q, k, q_weight, k_weight, freq=None, pos=None, eps=1e-6, pairs=False,
+                   stream=None):
+        """Queries and keys ([N, heads * D]; k and k_weight may be None)
+        normalised head by head, times their weights (float32 [D]), the first
+        2 P columns of each head turned by the angles pos * freq (pos int32
+        [N], freq float32 [P]): (q, k) as they were given.  Pair i of the
+        columns is i and P + i, or with ``pairs`` 2 i and 2 i + 1."""
+        A, k = self._head_norms(q, k, q_weight, k_weight, freq, pos, eps, pairs)
+        yq, yk = self._new(stream, q.shape, q.dtype), self._new(stream, k.shape, q.dtype)
+        self._uses(stream, q, k, q_weight, k_weight, freq, pos)
+        rc = self._lib.fst_head_norms_run(
+            self._h, A, self._pass.made(0, yq, _types[q.dtype]),
+            self._pass.made(1, yk, _types[q.dtype]), self._call_stream(stream))
+        _check(rc, "fst_head_norms_run")
+        return yq, None if k_weight is None else yk
+
+    def head_norms_grads(self, q, k, q_weight, k_weight, freq, pos, grad_q, grad_k, eps=1e-6,
+                         pairs=False, stream=None):
+        """Gradients of a loss by q, k and the weights from those by the
+        results of ``head_norms`` of the same arguments: dict(q, k: as these,
+        q_weight, k_weight: float32 [D]); k's are None where k is."""
+        one = k is None
+        A, k = self._head_norms(q, k, q_weight, k_weight, freq, pos, eps, pairs)
+        if one:
+            grad_k = k
+        gq, gk = self._new(stream, q.shape, q.dtype), self._new(stream, k.shape, q.dtype)
+        gqw = self._new(stream, q_weight.shape, self._f32)
+        gkw = None if one else self._new(stream, k_weight.shape, self._f32)
+        self._uses(stream, q, k, q_weight, k_weight, freq, pos, grad_q, grad_k)
+        rc = self._lib.fst_head_norms_grads(
+            self._h, A, self._pass.matrix(0, grad_q, "grad_q"),
+            self._pass.matrix(1, grad_k, "grad_k"), self._pass.made(2, gq, _types[q.dtype]),
+            self._pass.made(3, gk, _types[q.dtype]), _address(gqw), _address(gkw),
+            self._call_stream(stream))
+        _check(rc, "fst_head_norms_grads")
+        return dict(q=gq, k=None if one else gk, q_weight=gqw, k_weight=gkw)
+
+    def _head_norms(self, q, k, q_weight, k_weight, freq, pos, eps, pairs):
+        if (k is None) != (k_weight is None):
+            raise ValueError("k, k_weight: both or neither")
+        if k is None:
+            k = q[:, :0]
+        P = 0 if freq is None else freq.numel()
+        if P and pos is None:
+            raise ValueError("pos: rotations need positions")
+        D = q_weight.numel()
+        A = self._pass.norms(q, k, D, _array(q_weight, "q_weight", self._f32, D),
+                             _array(k_weight, "k_weight", self._f32, D),
+                             _array(freq, "freq", self._f32, P), P,
+                             _array(pos, "pos", self._i32, q.shape[0]) if P else None,
+                             int(bool(pairs)), float(eps))
+        return A, k
+
+    def linear_attention(self, q, k, v, log_decay, offset, state=None, scale=None, reverse=False,
+                         stream=None):
+        """Linear attention of the sequences offset[s] .. offset[s + 1] of rows
+        of q, k ([N, H * K]) and v ([N, H * V]; offset int32 [n + 1]) with
+        decays exp(log_decay) (float32 [H]) from state (float32 [n, H, K, V],
+        None: 0): dict(y: as v, last: the states after each sequence).  scale:
+        K ** -0.5 if None."""
+        A, n, (H, K, V) = self._linear(q, k, v, log_decay, offset, state, scale, reverse)
+        y = self._new(stream, v.shape, q.dtype)
+        last = self._new(stream, (n, H, K, V), self._f32)
+        self._uses(stream, q, k, v, log_decay, offset, state)
+        rc = self._lib.fst_linear_attention_run(self._h, A,
+                                                self._pass.made(0, y, _types[q.dtype]),
+                                                _address(last), self._call_stream(stream))
+        _check(rc, "fst_linear_attention_run")
+        return dict(y=y, last=last)
+
+    def linear_attention_grads(self, q, k, v, log_decay, offset, grad_y, state=None,
+                               grad_last=None, scale=None, reverse=False, stream=None):
+        """Gradients of a loss by q, k, v and state from those by y and last
+        (``linear_attention`` of the same arguments): dict(q, k, v: as these,
+        state: float32 [n, H, K, V]).  The decays are constants."""
+        A, n, (H, K, V) = self._linear(q, k, v, log_decay, offset, state, scale, reverse)
+        gq, gk, gv = (self._new(stream, t.shape, q.dtype) for t in (q, k, v))
+        gs = self._new(stream, (n, H, K, V), self._f32)
+        self._uses(stream, q, k, v, log_decay, offset, grad_y, state, grad_last)
+        typ = _types[q.dtype]
+        rc = self._lib.fst_linear_attention_grads(
+            self._h, A, self._pass.matrix(0, grad_y, "grad_y"),
+            _array(grad_last, "grad_last", self._f32, n * H * K * V), self._pass.made(1, gq, typ),
+            self._pass.made(2, gk, typ), self._pass.made(3, gv, typ), _address(gs),
+            self._call_stream(stream))
+        _check(rc, "fst_linear_attention_grads")
+        return dict(q=gq, k=gk, v=gv, state=gs)
+
+    def _linear_heads(self, q, v, log_decay):
+        """(heads, a head's columns of q, of v)."""
+        H = log_decay.numel()
+        if q.dim() != 2 or v.dim() != 2 or not H or q.shape[1] % H or v.shape[1] % H:
+            raise ValueError("q, v: columns for each entry of log_decay are needed")
+        return H, q.shape[1] // H, v.shape[1] // H
+
+    def _linear(self, q, k, v, log_decay, offset, state, scale, reverse):
+        n = int(offset.numel()) - 1
+        if n < 0:
+            raise ValueError("offset: at least one entry is needed")
+        H, K, V = self._linear_heads(q, v, log_decay)
+        A = self._pass.linear(n, _array(offset, "offset", self._i32, n + 1), int(bool(reverse)),
+                              H, _array(log_decay, "log_decay", self._f32, H),
+                              max(K, 1) ** -0.5 if scale is None else float(scale), q, k, v,
+                              _array(state, "state", self._f32, n * H * K * V))
+        return A, n, (H, K, V)
+
+    def linear_attention_step(self, q, k, v, log_decay, state, slot=None, out=None, scale=None,
+                              stream=None):
+        """One step of the rows of q, k and v: (y, new states).  state: float32
+        [n, H, K, V], or more; slot and ``out`` as in ``recurrence_step``."""
+        H, K, V = self._linear_heads(q, v, log_decay)
+        slots, rows = state.shape[0], q.shape[0]
+        from_ = _array(state, "state", self._f32, slots * H * K * V)
+        if out is not None and out is not state:
+            to = _array(out, "out", self._f32, slots * H * K * V)
+        elif out is state or slot is not None:
+            out, to = state, from_
+        else:
+            out = self._new(stream, (slots, H, K, V), self._f32)
+            to = _address(out)
+            if slots > rows:  # states that this step leaves alone
+                self._copy(stream, out[rows:], state.view(slots, H, K, V)[rows:])
+        y = self._new(stream, v.shape, q.dtype)
+        self._uses(stream, q, k, v, log_decay, state, slot, out)
+        m = self._pass
+        rc = self._lib.fst_linear_attention_step(
+            self._h, m.matrix(0, q, "q"), m.matrix(1, k, "k"), m.matrix(2, v, "v"), H,
+            _array(log_decay, "log_decay", self._f32, H),
+            max(K, 1) ** -0.5 if scale is None else float(scale), from_, to,
+            _array(slot, "slot", self._i32, rows), slots, m.made(3, y, _types[q.dtype]),
+            self._call_stream(stream))
+        _check(rc, "fst_linear_attention_step")
+        return y, out
+
+    def window_attention(self, q, k, v, offset, heads, kv_heads=None, window=1 << 30, sinks=0,
+                         scale=None, stream=None):
+        """Attention of the rows of q ([N, heads * D]) to those of k and v ([N,
+        kv_heads * D], kv_heads: heads if None) in the same sequence (rows
+        offset[s] .. offset[s + 1], offset int32 [n + 1]) that are no later,
+        and less than ``window`` rows before them or among the sequence's first
+        ``sinks``: dict(y: as q, lse: float32 [N, heads], the scores'
+        log-sums).  scale: D ** -0.5 if None."""
+        A, heads = self._window(q, k, v, offset, heads, kv_heads, window, sinks, scale)
+        y = self._new(stream, q.shape, q.dtype)
+        lse = self._new(stream, (q.shape[0], heads), self._f32)
+        self._uses(stream, q, k, v, offset)
+        rc = self._lib.fst_window_attention_run(self._h, A,
+                                                self._pass.made(0, y, _types[q.dtype]),
+                                                _address(lse), self._call_stream(stream))
+        _check(rc, "fst_window_attention_run")
+        return dict(y=y, lse=lse)
+
+    def window_attention_grads(self, q, k, v, offset, y, lse, grad_y, heads, kv_heads=None,
+                               window=1 << 30, sinks=0, scale=None, stream=None):
+        """Gradients of a loss by q, k and v from that by y, with y and lse of
+        ``window_attention`` of the same arguments: dict(q, k, v)."""
+        A, heads = self._window(q, k, v, offset, heads, kv_heads, window, sinks, scale)
+        gq, gk, gv = (self._new(stream, t.shape, q.dtype) for t in (q, k, v))
+        self._uses(stream, q, k, v, offset, y, lse, grad_y)
+        typ, m = _types[q.dtype], self._pass
+        rc = self._lib.fst_window_attention_grads(
+            self._h, A, m.matrix(0, y, "y"), _array(lse, "lse", self._f32, q.shape[0] * heads),
+            m.matrix(1, grad_y, "grad_y"), m.made(2, gq, typ), m.made(3, gk, typ),
+            m.made(4, gv, typ), self._call_stream(stream))
+        _check(rc, "fst_window_attention_grads")
+        return dict(q=gq, k=gk, v=gv)
+
+    @staticmethod
+    def _window_shape(q, heads, kv_heads, window, sinks, scale):
+        heads = _int32(heads, "heads")
+        kv_heads = heads if kv_heads is None else _int32(kv_heads, "kv_heads")
+        if heads < 1 or q.dim() != 2 or q.shape[1] % heads:
+            raise ValueError("heads: the columns of q are no multiple")
+        if scale is None:
+            scale = max(q.shape[1] // heads, 1) ** -0.5
+        return heads, kv_heads, _int32(window, "window"), _int32(sinks, "sinks"), float(scale)
+
+    def _window(self, q, k, v, offset, heads, kv_heads, window, sinks, scale):
+        n = int(offset.numel()) - 1
+        if n < 0:
+            raise ValueError("offset: at least one entry is needed")
+        how = self._window_shape(q, heads, kv_heads, window, sinks, scale)
+        return self._pass.window(n, _array(offset, "offset", self._i32, n + 1), *how, q, k,
+                                 v), how[0]
+
+    def window_attention_step(self, q, k, v, pos, k_cache, v_cache, heads, kv_heads=None,
+                              window=1, sinks=0, slot=None, scale=None, stream=None):
+        """One step of many streams: row i of q, k and v is the frame of
+        position pos[i] (int32 [n]; negative: an idle row) of the stream whose
+        keys and values lie in the sinks + window rows from slot[i] * (sinks +
+        window) on (slot int32 [n], None: i) of k_cache and v_cache ([slots *
+        (sinks + window), kv_heads * D]).  Writes k and v there and returns y."""
+        how = self._window_shape(q, heads, kv_heads, window, sinks, scale)
+        rows, L = q.shape[0], how[2] + how[3]
+        slots = k_cache.shape[0] // L if L > 0 else 0
+        y = self._new(stream, q.shape, q.dtype)
+        self._uses(stream, q, k, v, pos, k_cache, v_cache, slot)
+        m = self._pass
+        rc = self._lib.fst_window_attention_step(
+            self._h, m.matrix(0, q, "q"), m.matrix(1, k, "k"), m.matrix(2, v, "v"), *how,
+            _array(pos, "pos", self._i32, rows), _array(slot, "slot", self._i32, rows), slots,
+            m.matrix(3, k_cache, "k_cache"), m.matrix(4, v_cache, "v_cache"),
+            m.made(5, y, _types[q.dtype]), self._call_stream(stream))
+        _check(rc, "fst_window_attention_step")
+        return y
+
+    def window_attention_fill(self, k, v, offset, k_cache, v_cache, window, sinks=0, slot=None,
+                              stream=None):
+        """Fills the caches of ``window_attention_step`` with whole sequences
+        (k, v, offset as in ``window_attention``), that of sequence s in stream
+        slot[s] (int32 [n], None: s)."""
+        n = int(offset.numel()) - 1
+        if n < 0:
+            raise ValueError("offset: at least one entry is needed")
+        window, sinks = _int32(window, "window"), _int32(sinks, "sinks")
+        L = window + sinks
+        slots = k_cache.shape[0] // L if L > 0 else 0
+        self._uses(stream, k, v, offset, k_cache, v_cache, slot)
+        m = self._pass
+        rc = self._lib.fst_window_attention_fill(
+            self._h, n, _array(offset, "offset", self._i32, n + 1), m.matrix(0, k, "k"),
+            m.matrix(1, v, "v"), window, sinks, _array(slot, "slot", self._i32, n), slots,
+            m.matrix(2, k_cache, "k_cache"), m.matrix(3, v_cache, "v_cache"),
+            self._call_stream(stream))
+        _check(rc, "fst_window_attention_fill")
 
     def emission_weights(self, x, w, out=None, stream=None):
         """Log-softmax of x w^T, float32 [N, C] (x [N, H], w [C, H]): the arc
