@@ -25,10 +25,9 @@ using namespace tile;
 namespace {
 
 constexpr int CHUNK = 64;   // rows that are multiplied at once, 16 of them by a wavefront
-constexpr int SLICE = 64;   // columns of v that a workgroup takes
-constexpr int LNT = 256;    // threads of it
-constexpr int LNW = LNT / WAVE;
-static_assert(CHUNK == 16 * LNW && SLICE == 64, "a wavefront has 16 rows and four tiles of v");
+constexpr int SLICE = 64;   // columns of v that four wavefronts take
+constexpr int LNT = 256;    // threads of a step
+static_assert(CHUNK == 16 * 4 && SLICE == 64, "a wavefront has 16 rows and four tiles of v");
 
 // e^(g n) for 0 <= n <= CHUNK, from 64 bits: chunk after chunk multiplies them.
 // (A head that keeps nothing has g = -inf, and e^(0 g) = 1 all the same.)
@@ -53,7 +52,7 @@ __device__ __forceinline__ bool finite(const float4v (&x)[4]) {
 struct Fours {
   float4v x[4];
 };
-template <typename T, int PA>
+template <typename T, int PA, int PB>
 __device__ __noinline__ Fours exact_rows(const T *s_q, const T *s_k, const T *s_v,
                                          const float *s_pow, int i, int A, int lg, float scale) {
   Fours o{};
@@ -66,15 +65,25 @@ __device__ __noinline__ Fours exact_rows(const T *s_q, const T *s_k, const T *s_
     for (int j = 0; j < 4; ++j)
 #pragma unroll
       for (int r = 0; r < 4; ++r)
-        o.x[j][r] = fmaf(p, (float)s_v[row * LD<T, SLICE> + 16 * j + 4 * lg + r], o.x[j][r]);
+        o.x[j][r] = fmaf(p, (float)s_v[row * LD<T, PB> + 16 * j + 4 * lg + r], o.x[j][r]);
   }
   return o;
+}
+
+// Over the wavefronts.
+template <int NW>
+__device__ __forceinline__ float largest(const float (&m)[NW][4], int c) {
+  float x = m[0][c];
+#pragma unroll
+  for (int w = 1; w < NW; ++w) x = fmaxf(x, m[w][c]);
+  return x;
 }
 
 // FULL: rows' results; otherwise a unit's own contribution to the state, written
 // where the state entering the unit will be.
 //
-// Four wavefronts, 16 rows of the chunk each: scores as (k rows) x (q columns),
+// Four wavefronts, 16 rows of the chunk each, for every 64 columns of v (CG such
+// groups of wavefronts share the tiles of q and k): scores as (k rows) x (q columns),
 // so that they become an operand of the product with v where they are; the state
 // in registers, a quarter of its rows a wavefront, and rounded to T in LDS as
 // (v rows) x (k columns) for the product with q.
@@ -83,35 +92,45 @@ __device__ __noinline__ Fours exact_rows(const T *s_q, const T *s_k, const T *s_
 // that go into the state are as many numbers as hold them: states are float32
 // results.  float16: all three are scaled by a power of two from the
 // chunk's largest numbers, so that they neither overflow nor lose their digits.
-template <typename T, int PA, bool WIDE, bool FULL>
-__global__ __launch_bounds__(LNT) void k_linear(LinArgs a) {
+template <typename T, int PA, int CG, bool WIDE, bool FULL>
+__global__ __launch_bounds__(256 * CG, CG == 2 ? 2 : sizeof(T) == 2 && PA == 64 ? 3 : 1) void k_linear(LinArgs a) {
   static_assert(PA % 64 == 0, "whole tiles for four wavefronts");
+  constexpr int NTH = 256 * CG, NW = 4 * CG, PB = SLICE * CG;
   constexpr int MT = PA / 64;  // tiles of 16 rows of the state, a wavefront
   constexpr bool SCALED = std::is_same<T, f16>::value;
-  // numbers of T that a decayed k takes: 24 bits of it
+  // numbers of T that hold 24 bits of a decayed k
   constexpr int TERMS = std::is_same<T, bf16>::value ? 3 : std::is_same<T, f16>::value ? 2 : 1;
-  __shared__ __attribute__((aligned(16))) T s_q[FULL ? CHUNK * LD<T, PA> : 8];
-  __shared__ __attribute__((aligned(16))) T s_k[CHUNK * LD<T, PA>];
-  __shared__ __attribute__((aligned(16))) T s_v[CHUNK * LD<T, SLICE>];
-  __shared__ __attribute__((aligned(16))) T s_s[FULL ? SLICE * LD<T, PA> : 8];
+  extern __shared__ __attribute__((aligned(16))) char s_dyn[];
+  T *s_k = reinterpret_cast<T *>(s_dyn);       // [CHUNK][PA]
+  T *s_v = s_k + CHUNK * LD<T, PA>;            // [CHUNK][PB]
+  T *s_q = s_v + CHUNK * LD<T, PB>;            // FULL: [CHUNK][PA]
+  T *s_s = s_q + CHUNK * LD<T, PA>;            // FULL: [PB][PA]
   __shared__ float s_pow[CHUNK + 1];
-  __shared__ float s_max[LNW][4];
+  __shared__ __attribute__((aligned(16))) float s_end[CHUNK];  // rows' powers to the end
+  __shared__ float s_max[NW][4];
 
   const LinJob &job = a.job[blockIdx.z];
   const int lane = threadIdx.x & (WAVE - 1), l16 = lane & 15, lg = lane >> 4;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
-  const int h = blockIdx.y / a.slices, b0 = blockIdx.y % a.slices * SLICE;
+  const int wr = w & 3, c0 = CG == 1 ? 0 : (w >> 2) * SLICE;  // its rows and columns
+  const int h = blockIdx.y / a.slices, b0 = blockIdx.y % a.slices * PB;
   const int A = job.A, B = job.B, left = B - b0;
   Unit u;
   if (left <= 0 || !unit_of(a.off, a.n, a.N, a.unit, job.reverse, blockIdx.x, u)) return;
 
   const float g = a.log_decay[h];
-  if (threadIdx.x <= CHUNK) s_pow[threadIdx.x] = (float)power_of(g, threadIdx.x);
+  const int end = job.back ? 0 : 1;
+  if (threadIdx.x <= CHUNK) {
+    const float p = (float)power_of(g, threadIdx.x);
+    const int j = CHUNK - end - (int)threadIdx.x;  // the row that it takes to the end
+    s_pow[threadIdx.x] = p;
+    if (j >= 0 && j < CHUNK) s_end[j] = p;
+  }
 
-  // the state: rows (w MT + m) 16 + 4 lg + r, columns 16 j + l16
+  // the state: rows (wr MT + m) 16 + 4 lg + r, columns c0 + 16 j + l16
   float4v S[MT][4];
   const long long AB = (long long)A * B;
-  const int row0 = w * MT * 16 + 4 * lg;
+  const int row0 = wr * MT * 16 + 4 * lg;
   float *unit_state =
       a.unit ? job.units + ((long long)blockIdx.x * a.H + h) * AB : nullptr;
   const float *from = !FULL ? nullptr
@@ -124,7 +143,7 @@ __global__ __launch_bounds__(LNT) void k_linear(LinArgs a) {
     for (int j = 0; j < 4; ++j)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        const int ra = row0 + 16 * m + r, cb = 16 * j + l16;
+        const int ra = row0 + 16 * m + r, cb = c0 + 16 * j + l16;
         S[m][j][r] = from && ra < A && cb < left
                          ? from[(long long)ra * job.sa + (long long)(b0 + cb) * job.sb]
                          : 0.0f;
@@ -145,13 +164,12 @@ __global__ __launch_bounds__(LNT) void k_linear(LinArgs a) {
   }
   __syncthreads();
   if constexpr (SCALED && FULL)
-    bound = fmaxf(fmaxf(s_max[0][3], s_max[1][3]), fmaxf(s_max[2][3], s_max[3][3]));
+    bound = largest(s_max, 3);
 
-  // powers that every chunk uses: of row i = 16 w + l16 against rows j = 16 t +
-  // 4 lg + r (0 where j is later), of row i against the state, of rows j to the
-  // chunk's end
-  const int i = 16 * w + l16, end = job.back ? 0 : 1;
-  float dec[4][4], wk[2][8];
+  // powers that every chunk uses: of row i = 16 wr + l16 against rows j = 16 t +
+  // 4 lg + r (0 where j is later) and against the state
+  const int i = 16 * wr + l16;
+  float dec[4][4];
 #pragma unroll
   for (int t = 0; t < 4; ++t)
 #pragma unroll
@@ -159,11 +177,6 @@ __global__ __launch_bounds__(LNT) void k_linear(LinArgs a) {
       const int d = i - (16 * t + 4 * lg + r);
       dec[t][r] = d >= 0 ? s_pow[d] : 0.0f;
     }
-#pragma unroll
-  for (int t = 0; t < 2; ++t)
-#pragma unroll
-    for (int e = 0; e < 8; ++e)
-      wk[t][e] = s_pow[CHUNK - end - (32 * t + (e >> 2) * 16 + 4 * lg + (e & 3))];
   const float over = s_pow[i + end];
   // e^(g CHUNK) as two numbers
   const double all = power_of(g, CHUNK);
@@ -174,8 +187,8 @@ __global__ __launch_bounds__(LNT) void k_linear(LinArgs a) {
   const T *q = static_cast<const T *>(job.q) + (long long)h * A;
   const T *k = static_cast<const T *>(job.k) + (long long)h * A;
   const T *v = static_cast<const T *>(job.v) + (long long)h * B + b0;
-  Stage<T, PA, CHUNK, LNT, WIDE> rq, rk;
-  Stage<T, SLICE, CHUNK, LNT, WIDE> rv;
+  Stage<T, PA, CHUNK, NTH, WIDE> rq, rk;
+  Stage<T, PB, CHUNK, NTH, WIDE> rv;
   const auto fetch = [&](long long i0) {
     const long long first = u.first + i0 * u.step;
     const int count = (int)(u.hi - i0 < CHUNK ? u.hi - i0 : CHUNK);
@@ -195,7 +208,7 @@ __global__ __launch_bounds__(LNT) void k_linear(LinArgs a) {
       for (int m = 0; m < MT; ++m)
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-          store_four<T, true>(s_s + (16 * j + l16) * LD<T, PA>, row0 + 16 * m, PA,
+          store_four<T, true>(s_s + (c0 + 16 * j + l16) * LD<T, PA>, row0 + 16 * m, PA,
                               S[m][j] * s_scale);
     }
     rk.store(s_k);
@@ -212,29 +225,28 @@ __global__ __launch_bounds__(LNT) void k_linear(LinArgs a) {
     if constexpr (SCALED) {
       float top[3];
 #pragma unroll
-      for (int c = 0; c < 3; ++c)
-        top[c] = fmaxf(fmaxf(s_max[0][c], s_max[1][c]), fmaxf(s_max[2][c], s_max[3][c]));
+      for (int c = 0; c < 3; ++c) top[c] = largest(s_max, c);
       p_scale = power_below(most * (float)A * top[0] * top[1], 15);
-      k_scale = power_below(most * fabsf(job.sk) * top[1], 12);
+      k_scale = fminf(power_below(most * fabsf(job.sk) * top[1], 12), 0x1p60f);
       bound = fmaf(keep, bound, most * fabsf(job.sk) * CHUNK * top[1] * top[2]);
     }
     if constexpr (FULL) {
       float4v past[4] = {}, now[4] = {};
       Frag<T> qf[PA / 32];
 #pragma unroll
-      for (int s = 0; s < PA / 32; ++s) qf[s] = rows<T, PA>(s_q, 16 * w, 32 * s, lane);
+      for (int s = 0; s < PA / 32; ++s) qf[s] = rows<T, PA>(s_q, 16 * wr, 32 * s, lane);
 #pragma unroll
       for (int j = 0; j < 4; ++j)
 #pragma unroll
         for (int s = 0; s < PA / 32; ++s)
-          past[j] = mac(rows<T, PA>(s_s, 16 * j, 32 * s, lane), qf[s], past[j]);
+          past[j] = mac(rows<T, PA>(s_s, c0 + 16 * j, 32 * s, lane), qf[s], past[j]);
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
-        if (2 * t > w) continue;
+        if (2 * t > wr) continue;
         float4v x[2] = {};
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
-          if (2 * t + c > w) continue;
+          if (2 * t + c > wr) continue;
 #pragma unroll
           for (int s = 0; s < PA / 32; ++s)
             x[c] = mac(rows<T, PA>(s_k, 32 * t + 16 * c, 32 * s, lane), qf[s], x[c]);
@@ -248,10 +260,10 @@ __global__ __launch_bounds__(LNT) void k_linear(LinArgs a) {
         const Frag<T> p = pack<T>(x[0], x[1]);
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-          now[j] = mac(columns<T, SLICE>(s_v, 32 * t, 16 * j, lane), p, now[j]);
+          now[j] = mac(columns<T, PB>(s_v, 32 * t, c0 + 16 * j, lane), p, now[j]);
       }
       if (!finite(now)) {
-        const Fours o = exact_rows<T, PA>(s_q, s_k, s_v, s_pow, i, A, lg, p_scale);
+        const Fours o = exact_rows<T, PA, PB>(s_q, s_k, s_v + c0, s_pow, i, A, lg, p_scale);
 #pragma unroll
         for (int j = 0; j < 4; ++j)
 #pragma unroll
@@ -264,57 +276,71 @@ __global__ __launch_bounds__(LNT) void k_linear(LinArgs a) {
         const float f = job.ss * over / s_scale, f2 = job.so / p_scale;
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-          store_four<T, WIDE>(o, 16 * j + 4 * lg, left, past[j] * f + now[j] * f2);
+          store_four<T, WIDE>(o, c0 + 16 * j + 4 * lg, left, past[j] * f + now[j] * f2);
       }
     }
     if (more || !FULL || (job.last && u.hi == u.len)) {
-      float4v add[MT][4] = {};
       const bool whole = count == CHUNK;
-#pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        Frag<T> vf[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) vf[j] = columns<T, SLICE>(s_v, 32 * t, 16 * j, lane);
-        float f[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const int d = count - (32 * t + (e >> 2) * 16 + 4 * lg + (e & 3));
-          f[e] = (whole ? wk[t][e] : d > 0 ? s_pow[d - end] : 0.0f) * (job.sk * k_scale);
-        }
-#pragma unroll
-        for (int m = 0; m < MT; ++m) {
-          float x[8], y[8];
-          unpack(columns<T, PA>(s_k, 32 * t, (w * MT + m) * 16, lane), x);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) x[e] *= f[e];
-          Frag<T> hi = pack<T>(x);
-          // (made once: what is left of x goes by the very numbers that are
-          // multiplied, where the compiler might round x for each in its own way)
-          if constexpr (TERMS > 1) asm("" : "+v"(hi.v[0]));
-#pragma unroll
-          for (int j = 0; j < 4; ++j) add[m][j] = mac(hi, vf[j], add[m][j]);
-#pragma unroll
-          for (int c = 1; c < TERMS; ++c) {
-            unpack(hi, y);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] -= y[e];
-            hi = pack<T>(x);
-            asm("" : "+v"(hi.v[0]));
-#pragma unroll
-            for (int j = 0; j < 4; ++j) add[m][j] = mac(hi, vf[j], add[m][j]);
-          }
-        }
-      }
-      float kh = keep, kl = keep_lo;
-      if (!whole) kh = s_pow[count], kl = 0.0f;
-      const float back = 1.0f / k_scale;
+      const float kh = whole ? keep : s_pow[count], kl = whole ? keep_lo : 0.0f;
 #pragma unroll
       for (int m = 0; m < MT; ++m)
 #pragma unroll
         for (int j = 0; j < 4; ++j)
 #pragma unroll
           for (int r = 0; r < 4; ++r)
-            S[m][j][r] = fmaf(kh, S[m][j][r], fmaf(kl, S[m][j][r], add[m][j][r] * back));
+            S[m][j][r] = fmaf(kh, S[m][j][r], kl * S[m][j][r]) * k_scale;
+      const float f0 = job.sk * k_scale;
+      // (what a decayed k lost to two numbers matters to `last` alone)
+      const int terms = !FULL || job.last ? TERMS : TERMS < 2 ? TERMS : 2;
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        Frag<T> vf[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) vf[j] = columns<T, PB>(s_v, 32 * t, c0 + 16 * j, lane);
+        float f[8];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const int j = 32 * t + 16 * e + 4 * lg;
+          float4v x;
+          if (whole) {
+            x = *reinterpret_cast<const float4v *>(s_end + j);
+          } else {
+#pragma unroll
+            for (int r = 0; r < 4; ++r) x[r] = j + r < count ? s_end[CHUNK - count + j + r] : 0.0f;
+          }
+#pragma unroll
+          for (int r = 0; r < 4; ++r) f[4 * e + r] = x[r] * f0;
+        }
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+          float x[8], y[8];
+          unpack(columns<T, PA>(s_k, 32 * t, (wr * MT + m) * 16, lane), x);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) x[e] *= f[e];
+#pragma unroll
+          for (int c = 0; c < TERMS; ++c) {
+            if (c >= terms) continue;
+            Frag<T> part = pack<T>(x);
+            // (made once: what is left of x goes by the very numbers that are
+            // multiplied, where the compiler might round x for each in its own way)
+            if constexpr (TERMS > 1) asm("" : "+v"(part.v[0]));
+#pragma unroll
+            for (int j = 0; j < 4; ++j) S[m][j] = mac(part, vf[j], S[m][j]);
+            if (c + 1 < TERMS) {
+              unpack(part, y);
+#pragma unroll
+              for (int e = 0; e < 8; ++e) x[e] -= y[e];
+            }
+          }
+        }
+      }
+      if constexpr (SCALED) {
+        const float back = 1.0f / k_scale;
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) S[m][j] *= back;
+      }
     }
     __syncthreads();
   }
@@ -328,7 +354,7 @@ __global__ __launch_bounds__(LNT) void k_linear(LinArgs a) {
     for (int j = 0; j < 4; ++j)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        const int ra = row0 + 16 * m + r, cb = 16 * j + l16;
+        const int ra = row0 + 16 * m + r, cb = c0 + 16 * j + l16;
         if (ra < A && cb < left)
           to[(long long)ra * job.sa + (long long)(b0 + cb) * job.sb] = S[m][j][r];
       }
@@ -352,7 +378,7 @@ __global__ __launch_bounds__(NT) void k_linear_scan(LinArgs a) {
   float S = job.state ? job.state[s * all + e] : 0.0f;
   float *p = job.units + rows_before(b, s, a.unit) * all + e;
   const long long n = len > 0 ? (len + a.unit - 1) / a.unit : 1;
-  constexpr int AHEAD = 8;
+  constexpr int AHEAD = 32;
   for (long long i = 0; i < n; i += AHEAD) {
     float x[AHEAD];
 #pragma unroll
@@ -428,34 +454,55 @@ __global__ __launch_bounds__(LNT) void k_linear_step(LinStepArgs a) {
 
 unsigned units_of(const LinArgs &a) { return (unsigned)(a.unit ? a.N / a.unit + a.n : a.n); }
 
+template <typename T, int PA, int CG, bool WIDE, bool FULL>
+hipError_t launch_as(const LinArgs &a, int jobs, hipStream_t s) {
+  constexpr int PB = SLICE * CG;
+  constexpr int lds = BYTES<T, PA, CHUNK> + BYTES<T, PB, CHUNK> +
+                      (FULL ? BYTES<T, PA, CHUNK> + BYTES<T, PA, PB> : 0);
+  static_assert(lds <= 150 * 1024, "LDS of a CU");
+  if (lds > 64 * 1024) {
+    const hipError_t e =
+        hipFuncSetAttribute(reinterpret_cast<const void *>(k_linear<T, PA, CG, WIDE, FULL>),
+                            hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+    if (e != hipSuccess) return e;
+  }
+  k_linear<T, PA, CG, WIDE, FULL>
+      <<<dim3(units_of(a), a.H * a.slices, jobs), 256 * CG, lds, s>>>(a);
+  return hipGetLastError();
+}
 template <typename T, int PA, bool WIDE, bool FULL>
-void launch_as(const LinArgs &a, int jobs, hipStream_t s) {
-  k_linear<T, PA, WIDE, FULL><<<dim3(units_of(a), a.H * a.slices, jobs), LNT, 0, s>>>(a);
+hipError_t launch_by_columns(const LinArgs &a, int jobs, int B, hipStream_t s) {
+  // (float32 tiles of 128 by 128 would not fit)
+  if constexpr (sizeof(T) == 2) {
+    if (B > SLICE) return launch_as<T, PA, 2, WIDE, FULL>(a, jobs, s);
+  }
+  return launch_as<T, PA, 1, WIDE, FULL>(a, jobs, s);
 }
 template <typename T, bool FULL>
-void launch_jobs(const LinArgs &a, int jobs, int A, bool wide, hipStream_t s) {
+hipError_t launch_jobs(const LinArgs &a, int jobs, int A, int B, bool wide, hipStream_t s) {
   if (A <= 64)
-    wide ? launch_as<T, 64, true, FULL>(a, jobs, s) : launch_as<T, 64, false, FULL>(a, jobs, s);
-  else
-    wide ? launch_as<T, 128, true, FULL>(a, jobs, s) : launch_as<T, 128, false, FULL>(a, jobs, s);
+    return wide ? launch_by_columns<T, 64, true, FULL>(a, jobs, B, s)
+                : launch_by_columns<T, 64, false, FULL>(a, jobs, B, s);
+  return wide ? launch_by_columns<T, 128, true, FULL>(a, jobs, B, s)
+              : launch_by_columns<T, 128, false, FULL>(a, jobs, B, s);
 }
+
+// Columns of v of a workgroup.
+int slice_of(int type, int B) { return type != FST_F32 && B > SLICE ? 2 * SLICE : SLICE; }
 
 // Jobs [lo, hi) of `all`, which have one width of q and k (or widths up to 64).
 template <bool FULL>
-void launch_range(LinArgs a, const LinJob *all, int lo, int hi, int type, bool wide,
-                  hipStream_t s) {
+hipError_t launch_range(LinArgs a, const LinJob *all, int lo, int hi, int type, bool wide,
+                        hipStream_t s) {
   int B = 0;
   for (int i = lo; i < hi; ++i) {
     a.job[i - lo] = all[i];
     B = all[i].B > B ? all[i].B : B;
   }
-  a.slices = (B + SLICE - 1) / SLICE;
-  if (type == FST_F32)
-    launch_jobs<float, FULL>(a, hi - lo, all[lo].A, wide, s);
-  else if (type == FST_F16)
-    launch_jobs<f16, FULL>(a, hi - lo, all[lo].A, wide, s);
-  else
-    launch_jobs<bf16, FULL>(a, hi - lo, all[lo].A, wide, s);
+  a.slices = (B + slice_of(type, B) - 1) / slice_of(type, B);
+  if (type == FST_F32) return launch_jobs<float, FULL>(a, hi - lo, all[lo].A, B, wide, s);
+  if (type == FST_F16) return launch_jobs<f16, FULL>(a, hi - lo, all[lo].A, B, wide, s);
+  return launch_jobs<bf16, FULL>(a, hi - lo, all[lo].A, B, wide, s);
 }
 
 // Whether every row of a head, of each tensor, begins at a multiple of 16 bytes
@@ -471,8 +518,9 @@ bool wide_rows(const LinCall &c, size_t e, std::initializer_list<long long> stri
 }
 
 // Steps of a unit, 0: sequences are not cut.
-long long unit_steps(const LinCall &c, int jobs) {
-  const long long groups = (long long)c.H * ((c.V + SLICE - 1) / SLICE);
+long long unit_steps(const LinCall &c, int type, int jobs) {
+  const int slice = slice_of(type, c.V);
+  const long long groups = (long long)c.H * ((c.V + slice - 1) / slice);
   if (c.n * groups * jobs >= 256 || c.N / c.n <= 256) return 0;
   const long long steps = c.N * groups / 768;
   return steps <= CHUNK ? CHUNK : (steps + CHUNK - 1) / CHUNK * CHUNK;
@@ -490,13 +538,15 @@ LinArgs linear_args(const LinCall &c, long long unit) {
 }
 
 // Units' states of `jobs` jobs, and the scan that makes entering states of them.
-void launch_states(const LinArgs &a, const LinJob *all, int jobs, int type, bool wide,
-                   hipStream_t s) {
-  launch_range<false>(a, all, 0, jobs, type, wide, s);
+hipError_t launch_states(const LinArgs &a, const LinJob *all, int jobs, int type, bool wide,
+                         hipStream_t s) {
+  const hipError_t e = launch_range<false>(a, all, 0, jobs, type, wide, s);
+  if (e != hipSuccess) return e;
   LinArgs b = a;
   for (int i = 0; i < jobs; ++i) b.job[i] = all[i];
-  const long long e = (long long)a.H * all[0].A * all[0].B;
-  k_linear_scan<<<dim3((unsigned)((e + NT - 1) / NT), a.n, jobs), NT, 0, s>>>(b);
+  const long long n = (long long)a.H * all[0].A * all[0].B;
+  k_linear_scan<<<dim3((unsigned)((n + NT - 1) / NT), a.n, jobs), NT, 0, s>>>(b);
+  return hipGetLastError();
 }
 
 constexpr long long MAX_ACROSS = 65535;  // of a grid's second dimension
@@ -512,23 +562,25 @@ bool too_wide(const LinCall &c) {
 hipError_t launch_linear(const LinCall &c, int type, void *ws, size_t *need, hipStream_t s) {
   if (too_wide(c)) return hipErrorInvalidValue;
   const size_t e = type_bytes(type);
-  const long long unit = unit_steps(c, 1);
+  const long long unit = unit_steps(c, type, 1);
   *need = unit ? (size_t)(c.N / unit + c.n) * c.H * c.K * c.V * sizeof(float) : 0;
   if (!ws) return hipSuccess;
   const LinArgs a = linear_args(c, unit);
   const bool wide = wide_rows(c, e, {c.qs, c.ks, c.vs, c.ys}, {c.q, c.k, c.v, c.y});
   const LinJob job = {c.q, c.k, c.v, c.y, c.qs, c.ks, c.vs, c.ys, c.K, c.V, c.state, c.last,
                       c.V, 1, static_cast<float *>(ws), c.scale, c.scale, 1.0f, c.reverse, 0};
-  if (unit) launch_states(a, &job, 1, type, wide, s);
-  launch_range<true>(a, &job, 0, 1, type, wide, s);
-  return hipGetLastError();
+  if (unit) {
+    const hipError_t err = launch_states(a, &job, 1, type, wide, s);
+    if (err != hipSuccess) return err;
+  }
+  return launch_range<true>(a, &job, 0, 1, type, wide, s);
 }
 
 hipError_t launch_linear_grads(const LinCall &c, int type, void *ws, size_t *need,
                                hipStream_t s) {
   if (too_wide(c)) return hipErrorInvalidValue;
   const size_t e = type_bytes(type);
-  const long long unit = unit_steps(c, 3);
+  const long long unit = unit_steps(c, type, 3);
   const size_t states = unit ? (size_t)(c.N / unit + c.n) * c.H * c.K * c.V : 0;
   *need = 2 * states * sizeof(float);
   if (!ws) return hipSuccess;
@@ -543,7 +595,8 @@ hipError_t launch_linear_grads(const LinCall &c, int type, void *ws, size_t *nee
          0.0f, 0.0f, 1.0f, c.reverse, 0},
         {nullptr, c.q, c.y, nullptr, 0, c.qs, c.ys, 0, c.K, c.V, c.glast, nullptr, c.V, 1, bwd,
          0.0f, 0.0f, c.scale, back, 1}};
-    launch_states(a, sums, 2, type, wide, s);
+    const hipError_t err = launch_states(a, sums, 2, type, wide, s);
+    if (err != hipSuccess) return err;
   }
   const LinJob jobs[3] = {
       {c.y, c.v, c.k, c.gq, c.ys, c.vs, c.ks, c.gqs, c.V, c.K, c.state, nullptr, 1, c.V, fwd,
@@ -552,13 +605,9 @@ hipError_t launch_linear_grads(const LinCall &c, int type, void *ws, size_t *nee
        c.scale, 1.0f, c.scale, back, 1},
       {c.k, c.q, c.y, c.gv, c.ks, c.qs, c.ys, c.gvs, c.K, c.V, c.glast, c.gstate, c.V, 1, bwd,
        c.scale, 1.0f, c.scale, back, 1}};
-  if ((c.K <= 64) == (c.V <= 64)) {
-    launch_range<true>(a, jobs, 0, 3, type, wide, s);
-  } else {
-    launch_range<true>(a, jobs, 0, 2, type, wide, s);
-    launch_range<true>(a, jobs, 2, 3, type, wide, s);
-  }
-  return hipGetLastError();
+  if ((c.K <= 64) == (c.V <= 64)) return launch_range<true>(a, jobs, 0, 3, type, wide, s);
+  const hipError_t err = launch_range<true>(a, jobs, 0, 2, type, wide, s);
+  return err != hipSuccess ? err : launch_range<true>(a, jobs, 2, 3, type, wide, s);
 }
 
 template <typename T>
