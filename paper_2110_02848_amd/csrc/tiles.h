@@ -184,6 +184,140 @@ struct Stage {
   }
 };
 
+// Tiles whose rows lie side by side, without room between them: 16-byte group g of
+// row r lies at group g ^ swizzle(r), so that a read of 16 rows, and one that
+// transposes four, meet different banks.  They come from memory straight to LDS.
+template <typename T, int P>
+struct Packed {
+  static constexpr int GROUPS = P / PER<T>, ROW = P * (int)sizeof(T);
+
+  static __device__ __forceinline__ int swizzle(int r) {
+    return GROUPS == 8 ? ((r >> 1 & 3) << 1) | (r >> 3 & 1) : ((r & 7) << 1) | (r >> 3 & 1);
+  }
+  static __device__ __forceinline__ const char *at(const char *t, int r, int g) {
+    return t + r * ROW + ((g ^ swizzle(r)) << 4);
+  }
+  // as rows() and columns() above
+  static __device__ __forceinline__ Frag<T> rows(const char *t, int row, int k, int lane) {
+    const int r = row + (lane & 15), g = k / PER<T> + (lane >> 4) * (8 / PER<T>);
+    Frag<T> f;
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T) / 2; ++i)
+      f.v[i] = *reinterpret_cast<const int4v *>(at(t, r, g + i));
+    return f;
+  }
+  static __device__ __forceinline__ Frag<T> columns(const char *t, int row, int col, int lane) {
+    Frag<T> f;
+    if constexpr (sizeof(T) == 2) {
+      int2v v[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int r = row + 16 * i + (lane >> 4) * 4 + (lane >> 2 & 3);
+        const char *p = at(t, r, col / 8 + (lane >> 1 & 1)) + (lane & 1) * 8;
+        v[i] = __builtin_bit_cast(
+            int2v, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                       (__attribute__((address_space(3))) short4v *)p));
+      }
+      f.v[0] = int4v{v[0].x, v[0].y, v[1].x, v[1].y};
+    } else {
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int r = row + 16 * i + (lane >> 4) * 4 + j, c = col + (lane & 15);
+          f.v[i][j] = *reinterpret_cast<const int *>(at(t, r, c / 4) + c % 4 * 4);
+        }
+    }
+    return f;
+  }
+};
+
+// Loads of 64 lanes by 16 bytes from memory to LDS without registers: lane i's
+// bytes land at `lds` + 16 i, zeros where they lie past the end of the buffer.
+// Written as instructions, because the compiler would wait for all of them before
+// the next read of LDS; whoever reads waits with wait_loads and a barrier.  (m0 is
+// the compiler's own: it warns where it is named, and only naming it keeps its uses
+// of m0 clear of this one.)
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+__device__ __forceinline__ void load_lds(uint32_t lds, uint32_t offset, int4v buffer) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+               :
+               : "s"(__builtin_amdgcn_readfirstlane(lds)), "v"(offset), "s"(buffer)
+               : "memory", "m0");
+}
+#pragma clang diagnostic pop
+__device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(0)" : : : "memory"); }
+
+// Bytes that 32-bit offsets into a tile of rows reach, at most.
+constexpr long long MAX_TILE_BYTES = 1ll << 31;
+
+// A packed tile of R rows on its way from memory, by NTH threads; WIDE: straight to
+// LDS (rows whole 16-byte groups, and the tile's rows within MAX_TILE_BYTES),
+// otherwise through registers, element by element.
+template <typename T, int P, int R, int NTH, bool WIDE>
+struct Carry {
+  static constexpr int GROUPS = P / PER<T>;
+  static constexpr int LOADS = R * GROUPS / NTH;
+  static_assert(LOADS >= 1 && LOADS * NTH == R * GROUPS, "whole loads");
+  uint32_t off[WIDE ? LOADS : 1];
+  int4v v[WIDE ? 1 : LOADS];
+
+  // (row, group of it) of load i: lanes write 1,024 bytes in their order
+  static __device__ __forceinline__ int row_of(int i) {
+    return ((threadIdx.x / WAVE * LOADS + i) * WAVE + threadIdx.x % WAVE) / GROUPS;
+  }
+  static __device__ __forceinline__ int group_of(int i) {
+    const int q = (threadIdx.x / WAVE * LOADS + i) * WAVE + threadIdx.x % WAVE;
+    return q % GROUPS ^ Packed<T, P>::swizzle(row_of(i));
+  }
+  __device__ __forceinline__ void init(long long stride, int width) {
+    if constexpr (WIDE) {
+#pragma unroll
+      for (int i = 0; i < LOADS; ++i) {
+        const int c = group_of(i) * PER<T>;
+        // (past any buffer where the row has ended)
+        off[i] = c < width ? (uint32_t)((row_of(i) * stride + c) * (long long)sizeof(T))
+                           : (uint32_t)MAX_TILE_BYTES;
+      }
+    }
+  }
+  // rows first .. first + count of a matrix (all arguments the same in every lane)
+  __device__ __forceinline__ void fetch(const T *p, long long stride, int width, long long first,
+                                        int count, char *to) {
+    if constexpr (WIDE) {
+      const unsigned long long q = (unsigned long long)(uintptr_t)(p + first * stride);
+      const uint32_t n =
+          count > 0 ? (uint32_t)(((count - 1) * stride + width) * (long long)sizeof(T)) : 0u;
+      const int4v buffer{__builtin_amdgcn_readfirstlane((int)(uint32_t)q),
+                         __builtin_amdgcn_readfirstlane((int)(uint32_t)(q >> 32)),
+                         __builtin_amdgcn_readfirstlane((int)n), 0x00027000};
+      const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)to +
+                           threadIdx.x / WAVE * LOADS * 1024;
+#pragma unroll
+      for (int i = 0; i < LOADS; ++i) load_lds(lds + i * 1024, off[i], buffer);
+    } else {
+#pragma unroll
+      for (int i = 0; i < LOADS; ++i) {
+        const int r = row_of(i);
+        v[i] = load_group<T, false>(p + (first + r) * stride, group_of(i) * PER<T>, width,
+                                    r < count);
+      }
+    }
+  }
+  // what fetch() began, in LDS; before the barrier behind which it is read
+  __device__ __forceinline__ void finish(char *to) const {
+    if constexpr (WIDE) {
+      wait_loads();
+    } else {
+#pragma unroll
+      for (int i = 0; i < LOADS; ++i)
+        *reinterpret_cast<int4v *>(
+            to + ((threadIdx.x / WAVE * LOADS + i) * WAVE + threadIdx.x % WAVE) * 16) = v[i];
+    }
+  }
+};
+
 // Four results side by side, from column c on of a row of `width`.
 template <typename T, bool WIDE>
 __device__ __forceinline__ void store_four(T *row, int c, int width, const float4v &x) {

@@ -34,6 +34,12 @@ constexpr int BLOCK = 16 * QT * WNW; // queries, or keys, of a workgroup
 constexpr int FEW = 64;              // frames
 constexpr float LOG2 = 0.69314718055994530942f, LOG2E = 1.44269502162933349609375f;
 
+// Wavefronts of a SIMD, at least, of the kernels below.  Two have half of its
+// registers each, all of them ones that the vector units can add and multiply in;
+// float32's operands take twice the room.
+template <typename T>
+constexpr int MIN_WAVES = sizeof(T) == 2 ? 2 : 1;
+
 __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
 
 template <int N, int M>
@@ -110,11 +116,15 @@ __device__ __noinline__ float4v exact_row(const T *q, const T *k, long long ks, 
   return x;
 }
 
+// Tiles of 64 keys come to two pairs of buffers in turn, the next one's loads under
+// way while one is multiplied.  m is the maximum that exponents are taken from: it
+// follows a row's maximum only once that is past it by LATE (powers of 2), so that
+// most tiles leave the sums as they are; p stays below 2^LATE.
 template <typename T, int P, bool WIDE>
-__global__ __launch_bounds__(WNT) void k_window(WinArgs a) {
-  __shared__ __attribute__((aligned(16))) T s_k[KEYS * LD<T, P>];
-  __shared__ __attribute__((aligned(16))) T s_v[KEYS * LD<T, P>];
-  constexpr int DT = P / 16, DS = P / 32;
+__global__ __launch_bounds__(WNT, MIN_WAVES<T>) void k_window(WinArgs a) {
+  constexpr int DT = P / 16, DS = P / 32, TILE = KEYS * P * (int)sizeof(T);
+  constexpr float LATE = 8.0f;
+  extern __shared__ __attribute__((aligned(16))) char s_dyn[];  // [2][k, v][TILE]
   const int lane = threadIdx.x & (WAVE - 1), l16 = lane & 15, lg = lane >> 4;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
   const int h = blockIdx.y, g = h / (a.H / a.G), D = a.D;
@@ -124,7 +134,25 @@ __global__ __launch_bounds__(WNT) void k_window(WinArgs a) {
   const T *q = static_cast<const T *>(a.q) + u.b * a.qs + (long long)h * D;
   const T *k = static_cast<const T *>(a.k) + u.b * a.ks + (long long)g * D;
   const T *v = static_cast<const T *>(a.v) + u.b * a.vs + (long long)g * D;
+  const Seen sn = seen_by(u.lo, u.hi, a.window, a.sinks);
+  Carry<T, P, KEYS, WNT, WIDE> ck, cv;
+  ck.init(a.ks, D);
+  cv.init(a.vs, D);
+  const auto start = [&](int tile) {
+    return tile < sn.sink_tiles ? (long long)tile * KEYS
+                                : sn.first + (long long)(tile - sn.sink_tiles) * KEYS;
+  };
+  const auto fetch = [&](int tile, char *to) {
+    const long long s0 = start(tile), end = tile < sn.sink_tiles ? sn.sinks : u.hi;
+    const int count = (int)(end - s0 < KEYS ? end - s0 : KEYS);
+    ck.fetch(k, a.ks, D, s0, count, to);
+    cv.fetch(v, a.vs, D, s0, count, to + TILE);
+  };
+  fetch(0, s_dyn);
   const long long tw = u.lo + w * 16 * QT;  // the wavefront's first query
+  // (exponents are taken of sizes: a negative scale turns q's signs)
+  const uint32_t sign = a.scale < 0.0f ? sizeof(T) == 2 ? 0x80008000u : 0x80000000u : 0u;
+  const float c = fmaxf(fabsf(a.scale) * LOG2E, 0x1p-120f);
   Frag<T> qf[QT][DS];
 #pragma unroll
   for (int i = 0; i < QT; ++i) {
@@ -134,93 +162,114 @@ __global__ __launch_bounds__(WNT) void k_window(WinArgs a) {
 #pragma unroll
       for (int e = 0; e < (int)sizeof(T) / 2; ++e)
         qf[i][s].v[e] =
-            load_group<T, WIDE>(q + t * a.qs, 32 * s + 8 * lg + e * PER<T>, D, t < u.hi);
+            load_group<T, WIDE>(q + t * a.qs, 32 * s + 8 * lg + e * PER<T>, D, t < u.hi) ^
+            (int)sign;
   }
-  const float c = a.scale * LOG2E;
-  float m[QT], l[QT];
+  float m[QT], l[QT];  // (m in units of scores)
   float4v o[DT][QT] = {};
 #pragma unroll
   for (int i = 0; i < QT; ++i) m[i] = -INFINITY, l[i] = 0.0f;
 
-  const Seen sn = seen_by(u.lo, u.hi, a.window, a.sinks);
-  Stage<T, P, KEYS, WNT, WIDE> rk, rv;
-  const auto fetch = [&](int tile) {
-    const bool sink = tile < sn.sink_tiles;
-    const long long s0 = sink ? (long long)tile * KEYS
-                              : sn.first + (long long)(tile - sn.sink_tiles) * KEYS;
-    const long long end = sink ? sn.sinks : u.hi;
-    const int count = (int)(end - s0 < KEYS ? end - s0 : KEYS);
-    rk.fetch(k, a.ks, D, s0, 1, count);
-    rv.fetch(v, a.vs, D, s0, 1, count);
-  };
-  fetch(0);
   for (int tile = 0; tile < sn.tiles; ++tile) {
-    __syncthreads();
-    rk.store(s_k);
-    rv.store(s_v);
-    __syncthreads();
-    if (tile + 1 < sn.tiles) fetch(tile + 1);
-    const bool sink = tile < sn.sink_tiles;
-    const long long s0 = sink ? (long long)tile * KEYS
-                              : sn.first + (long long)(tile - sn.sink_tiles) * KEYS;
-    // none of the wavefront's queries sees the tile; all see all of it
-    if (!sink && (s0 > tw + 16 * QT - 1 || (tw - (s0 + KEYS - 1) >= a.window && s0 >= a.sinks)))
-      continue;
-    const bool whole = sink ? s0 + KEYS <= sn.sinks
-                            : s0 + KEYS - 1 <= tw && tw + 16 * QT - 1 - s0 < a.window;
-    float4v x[4][QT] = {};
-#pragma unroll
-    for (int kt = 0; kt < 4; ++kt)
-#pragma unroll
-      for (int s = 0; s < DS; ++s) {
-        const Frag<T> f = rows<T, P>(s_k, 16 * kt, 32 * s, lane);
-#pragma unroll
-        for (int i = 0; i < QT; ++i) x[kt][i] = mac(f, qf[i][s], x[kt][i]);
-      }
-#pragma unroll
-    for (int i = 0; i < QT; ++i) {
-      float top = -INFINITY;
-#pragma unroll
-      for (int kt = 0; kt < 4; ++kt)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          x[kt][i][r] *= c;
-          if (!whole) {
-            const long long t = tw + 16 * i + l16, s = s0 + 16 * kt + 4 * lg + r;
-            const bool sees = sink ? s < sn.sinks
-                                   : s <= t && (t - s < a.window || s < a.sinks);
-            if (!sees) x[kt][i][r] = -INFINITY;
-          }
-          top = fmaxf(top, x[kt][i][r]);
-        }
-      top = fmaxf(top, __shfl_xor(top, 16, WAVE));
-      top = fmaxf(top, __shfl_xor(top, 32, WAVE));
-      const float next = fmaxf(m[i], top);
-      const float shift = next == -INFINITY ? 0.0f : next;
-      const float less = exp2_of(m[i] - shift);
-      m[i] = next;
-      l[i] *= less;
-#pragma unroll
-      for (int kt = 0; kt < 4; ++kt)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          x[kt][i][r] = exp2_of(x[kt][i][r] - shift);
-          l[i] += x[kt][i][r];
-        }
-#pragma unroll
-      for (int d = 0; d < DT; ++d) o[d][i] *= less;
+    char *s_k = s_dyn + (tile & 1) * 2 * TILE, *s_v = s_k + TILE;
+    char *s_next = s_dyn + (~tile & 1) * 2 * TILE;
+    if (tile == 0 || WIDE) {
+      ck.finish(s_k);
+      cv.finish(s_v);
     }
+    __syncthreads();
+    const bool more = tile + 1 < sn.tiles;
+    if (more) fetch(tile + 1, s_next);
+    const bool sink = tile < sn.sink_tiles;
+    const long long s0 = start(tile);
+    // unless none of the wavefront's queries sees the tile
+    if (sink ||
+        !(s0 > tw + 16 * QT - 1 || (tw - (s0 + KEYS - 1) >= a.window && s0 >= a.sinks))) {
+      // whether all see all of it
+      const bool whole = sink ? s0 + KEYS <= sn.sinks
+                              : s0 + KEYS - 1 <= tw && tw + 16 * QT - 1 - s0 < a.window;
+      float4v x[4][QT] = {};
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      Frag<T> p[QT];
+      for (int kt = 0; kt < 4; ++kt)
 #pragma unroll
-      for (int i = 0; i < QT; ++i) p[i] = pack<T>(x[2 * t][i], x[2 * t + 1][i]);
+        for (int s = 0; s < DS; ++s) {
+          const Frag<T> f = Packed<T, P>::rows(s_k, 16 * kt, 32 * s, lane);
 #pragma unroll
-      for (int d = 0; d < DT; ++d) {
-        const Frag<T> f = columns<T, P>(s_v, 32 * t, 16 * d, lane);
+          for (int i = 0; i < QT; ++i) x[kt][i] = mac(f, qf[i][s], x[kt][i]);
+        }
+      if (!whole) {
 #pragma unroll
-        for (int i = 0; i < QT; ++i) o[d][i] = mac(f, p[i], o[d][i]);
+        for (int i = 0; i < QT; ++i) {
+          // (of a lane's keys s0 + 16 kt + 4 lg + r: those up to `last`, from
+          // `from` on or up to `sinks`, all within 32 bits of s0)
+          const long long t = tw + 16 * i + l16 - s0 - 4 * lg;
+          const long long far = t - a.window + 1, sinks = (sink ? sn.sinks : a.sinks) - s0 - 4 * lg;
+          const int last = sink ? KEYS : (int)(t < KEYS ? t : KEYS);
+          const int from = sink ? KEYS : (int)(far < -KEYS ? -KEYS : far > KEYS ? KEYS : far);
+          const int upto = (int)(sinks < -KEYS ? -KEYS : sinks > KEYS ? KEYS : sinks);
+#pragma unroll
+          for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              const int at = 16 * kt + r;
+              if (at > last || (at < from && at >= upto)) x[kt][i][r] = -INFINITY;
+            }
+        }
       }
+      float shift[QT];
+      bool late = false;
+#pragma unroll
+      for (int i = 0; i < QT; ++i) {
+        float top = fmaxf(fmaxf(x[0][i][0], x[0][i][1]), x[0][i][2]);
+        top = fmaxf(top, x[0][i][3]);
+#pragma unroll
+        for (int kt = 1; kt < 4; ++kt) {
+          top = fmaxf(fmaxf(top, x[kt][i][0]), x[kt][i][1]);
+          top = fmaxf(fmaxf(top, x[kt][i][2]), x[kt][i][3]);
+        }
+        top = fmaxf(top, __shfl_xor(top, 16, WAVE));
+        top = fmaxf(top, __shfl_xor(top, 32, WAVE));
+        shift[i] = fmaxf(m[i], top);
+        late = late || !((shift[i] - m[i]) * c <= LATE);
+      }
+      if (__any(late)) {
+#pragma unroll
+        for (int i = 0; i < QT; ++i) {
+          // (while a row has seen nothing, m is -infinity and the sums are 0)
+          const float less = shift[i] == -INFINITY ? 1.0f : exp2_of((m[i] - shift[i]) * c);
+          m[i] = shift[i];
+          l[i] *= less;
+#pragma unroll
+          for (int d = 0; d < DT; ++d) o[d][i] *= less;
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < QT; ++i) {
+        const float mc = m[i] == -INFINITY ? 0.0f : m[i] * c;
+#pragma unroll
+        for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            x[kt][i][r] = exp2_of(fmaf(x[kt][i][r], c, -mc));
+            l[i] += x[kt][i][r];
+          }
+      }
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        Frag<T> p[QT];
+#pragma unroll
+        for (int i = 0; i < QT; ++i) p[i] = pack<T>(x[2 * t][i], x[2 * t + 1][i]);
+#pragma unroll
+        for (int d = 0; d < DT; ++d) {
+          const Frag<T> f = Packed<T, P>::columns(s_v, 32 * t, 16 * d, lane);
+#pragma unroll
+          for (int i = 0; i < QT; ++i) o[d][i] = mac(f, p[i], o[d][i]);
+        }
+      }
+    }
+    if (!WIDE && more) {
+      ck.finish(s_next);
+      cv.finish(s_next + TILE);
     }
   }
   if (!finite(o)) {
@@ -232,8 +281,9 @@ __global__ __launch_bounds__(WNT) void k_window(WinArgs a) {
       for (int d = 0; d < DT; ++d)
         if (16 * d + 4 * lg < D)
           o[d][i] = either(
-              o[d][i], exact_row<T>(q + t * a.qs, k, a.ks, v, a.vs, D, t, a.window, a.sinks, c,
-                                    m[i] == -INFINITY ? 0.0f : m[i], 16 * d + 4 * lg));
+              o[d][i], exact_row<T>(q + t * a.qs, k, a.ks, v, a.vs, D, t, a.window, a.sinks,
+                                    a.scale < 0.0f ? -c : c,
+                                    m[i] == -INFINITY ? 0.0f : m[i] * c, 16 * d + 4 * lg));
     }
   }
 #pragma unroll
@@ -246,7 +296,7 @@ __global__ __launch_bounds__(WNT) void k_window(WinArgs a) {
     T *y = static_cast<T *>(a.o) + (u.b + t) * a.os + (long long)h * D;
 #pragma unroll
     for (int d = 0; d < DT; ++d) store_four<T, WIDE>(y, 16 * d + 4 * lg, D, o[d][i] * f);
-    if (lg == 0) a.lse[(u.b + t) * a.H + h] = (m[i] + log2f(l[i])) * LOG2;
+    if (lg == 0) a.lse[(u.b + t) * a.H + h] = fmaf(m[i], c, log2f(l[i])) * LOG2;
   }
 }
 
@@ -358,10 +408,9 @@ __device__ __noinline__ TwoFours exact_dkv(const T *q, long long qs, const T *gy
 // of dS beside few: queries of a sequence's first block, and of windows up to FEW
 // frames, have it summed again from P and dy v^T, before their dS.
 template <typename T, int P, bool WIDE>
-__global__ __launch_bounds__(WNT) void k_window_dq(WinArgs a) {
-  __shared__ __attribute__((aligned(16))) T s_k[KEYS * LD<T, P>];
-  __shared__ __attribute__((aligned(16))) T s_v[KEYS * LD<T, P>];
-  constexpr int DT = P / 16, DS = P / 32;
+__global__ __launch_bounds__(WNT, MIN_WAVES<T>) void k_window_dq(WinArgs a) {
+  constexpr int DT = P / 16, DS = P / 32, TILE = KEYS * P * (int)sizeof(T);
+  extern __shared__ __attribute__((aligned(16))) char s_dyn[];  // [2][k, v][TILE]
   const int lane = threadIdx.x & (WAVE - 1), l16 = lane & 15, lg = lane >> 4;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
   const int h = blockIdx.y, g = h / (a.H / a.G), D = a.D;
@@ -372,6 +421,21 @@ __global__ __launch_bounds__(WNT) void k_window_dq(WinArgs a) {
   const T *gy = static_cast<const T *>(a.gy) + u.b * a.gys + (long long)h * D;
   const T *k = static_cast<const T *>(a.k) + u.b * a.ks + (long long)g * D;
   const T *v = static_cast<const T *>(a.v) + u.b * a.vs + (long long)g * D;
+  const Seen sn = seen_by(u.lo, u.hi, a.window, a.sinks);
+  Carry<T, P, KEYS, WNT, WIDE> ck, cv;
+  ck.init(a.ks, D);
+  cv.init(a.vs, D);
+  const auto start = [&](int tile) {
+    return tile < sn.sink_tiles ? (long long)tile * KEYS
+                                : sn.first + (long long)(tile - sn.sink_tiles) * KEYS;
+  };
+  const auto fetch = [&](int tile, char *to) {
+    const long long s0 = start(tile), end = tile < sn.sink_tiles ? sn.sinks : u.hi;
+    const int count = (int)(end - s0 < KEYS ? end - s0 : KEYS);
+    ck.fetch(k, a.ks, D, s0, count, to);
+    cv.fetch(v, a.vs, D, s0, count, to + TILE);
+  };
+  fetch(0, s_dyn);
   const long long tw = u.lo + w * 16 * QT;
   Frag<T> qf[QT][DS], gf[QT][DS];
   float lse[QT], delta[QT];
@@ -393,22 +457,10 @@ __global__ __launch_bounds__(WNT) void k_window_dq(WinArgs a) {
   }
   const float c = a.scale * LOG2E, up = ds_scale<T>(a);
   float4v o[DT][QT] = {};
-  const Seen sn = seen_by(u.lo, u.hi, a.window, a.sinks);
-  Stage<T, P, KEYS, WNT, WIDE> rk, rv;
-  const auto fetch = [&](int tile) {
-    const bool sink = tile < sn.sink_tiles;
-    const long long s0 = sink ? (long long)tile * KEYS
-                              : sn.first + (long long)(tile - sn.sink_tiles) * KEYS;
-    const long long end = sink ? sn.sinks : u.hi;
-    const int count = (int)(end - s0 < KEYS ? end - s0 : KEYS);
-    rk.fetch(k, a.ks, D, s0, 1, count);
-    rv.fetch(v, a.vs, D, s0, 1, count);
-  };
   // sweep 0 sums delta, sweep 1 dq
   const bool few = sizeof(T) == 2 && (u.lo == 0 || a.window + a.sinks <= FEW);
   float sum[QT] = {};
   const int steps = few ? 2 * sn.tiles : sn.tiles;
-  fetch(0);
   for (int step = 0; step < steps; ++step) {
     const bool sums = few && step < sn.tiles;
     const int tile = few && !sums ? step - sn.tiles : step;
@@ -422,27 +474,30 @@ __global__ __launch_bounds__(WNT) void k_window_dq(WinArgs a) {
         if (lg == 0 && t < u.hi) a.delta[(u.b + t) * a.H + h] = sum[i];
       }
     }
+    char *s_k = s_dyn + (step & 1) * 2 * TILE, *s_v = s_k + TILE;
+    char *s_next = s_dyn + (~step & 1) * 2 * TILE;
+    if (step == 0 || WIDE) {
+      ck.finish(s_k);
+      cv.finish(s_v);
+    }
     __syncthreads();
-    rk.store(s_k);
-    rv.store(s_v);
-    __syncthreads();
-    if (step + 1 < steps) fetch(tile + 1 < sn.tiles ? tile + 1 : 0);
-    const bool sink = tile < sn.sink_tiles;
-    const long long s0 = sink ? (long long)tile * KEYS
-                              : sn.first + (long long)(tile - sn.sink_tiles) * KEYS;
-    if (!sink && (s0 > tw + 16 * QT - 1 || (tw - (s0 + KEYS - 1) >= a.window && s0 >= a.sinks)))
-      continue;
+    const bool more = step + 1 < steps, sink = tile < sn.sink_tiles;
+    if (more) fetch(tile + 1 < sn.tiles ? tile + 1 : 0, s_next);
+    const long long s0 = start(tile);
+    const bool none = !sink && (s0 > tw + 16 * QT - 1 ||
+                                (tw - (s0 + KEYS - 1) >= a.window && s0 >= a.sinks));
     const bool whole = sink ? s0 + KEYS <= sn.sinks
                             : s0 + KEYS - 1 <= tw && tw + 16 * QT - 1 - s0 < a.window;
 #pragma unroll
     for (int t2 = 0; t2 < 2; ++t2) {
+      if (none) continue;
       float4v x[2][QT] = {}, y[2][QT] = {};
 #pragma unroll
       for (int b = 0; b < 2; ++b)
 #pragma unroll
         for (int s = 0; s < DS; ++s) {
-          const Frag<T> f = rows<T, P>(s_k, 32 * t2 + 16 * b, 32 * s, lane);
-          const Frag<T> f2 = rows<T, P>(s_v, 32 * t2 + 16 * b, 32 * s, lane);
+          const Frag<T> f = Packed<T, P>::rows(s_k, 32 * t2 + 16 * b, 32 * s, lane);
+          const Frag<T> f2 = Packed<T, P>::rows(s_v, 32 * t2 + 16 * b, 32 * s, lane);
 #pragma unroll
           for (int i = 0; i < QT; ++i) {
             x[b][i] = mac(f, qf[i][s], x[b][i]);
@@ -472,10 +527,14 @@ __global__ __launch_bounds__(WNT) void k_window_dq(WinArgs a) {
       if (sums) continue;
 #pragma unroll
       for (int d = 0; d < DT; ++d) {
-        const Frag<T> f = columns<T, P>(s_k, 32 * t2, 16 * d, lane);
+        const Frag<T> f = Packed<T, P>::columns(s_k, 32 * t2, 16 * d, lane);
 #pragma unroll
         for (int i = 0; i < QT; ++i) o[d][i] = mac(f, p[i], o[d][i]);
       }
+    }
+    if (!WIDE && more) {
+      ck.finish(s_next);
+      cv.finish(s_next + TILE);
     }
   }
   if (!finite(o)) {
@@ -506,11 +565,10 @@ __global__ __launch_bounds__(WNT) void k_window_dq(WinArgs a) {
 // the queries that see them through the window, head after head of its group,
 // and adds what the sinks' units found.
 template <typename T, int P, bool WIDE>
-__global__ __launch_bounds__(WNT) void k_window_dkv(WinArgs a) {
-  __shared__ __attribute__((aligned(16))) T s_q[KEYS * LD<T, P>];
-  __shared__ __attribute__((aligned(16))) T s_g[KEYS * LD<T, P>];
-  __shared__ __attribute__((aligned(16))) float s_lse[KEYS], s_delta[KEYS];
-  constexpr int DT = P / 16, DS = P / 32;
+__global__ __launch_bounds__(WNT, P == 64 ? MIN_WAVES<T> : 1) void k_window_dkv(WinArgs a) {
+  constexpr int DT = P / 16, DS = P / 32, TILE = KEYS * P * (int)sizeof(T);
+  extern __shared__ __attribute__((aligned(16))) char s_dyn[];  // [2][q, dy][TILE]
+  __shared__ __attribute__((aligned(16))) float s_row[2][2][KEYS];  // lse, delta
   const int lane = threadIdx.x & (WAVE - 1), l16 = lane & 15, lg = lane >> 4;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
   const int g = blockIdx.y, E = a.H / a.G, D = a.D;
@@ -537,15 +595,16 @@ __global__ __launch_bounds__(WNT) void k_window_dkv(WinArgs a) {
   float4v ok[DT][QT] = {}, ov[DT][QT] = {};
   const long long end = u.hi - 1 + a.window < u.len ? u.hi - 1 + a.window : u.len;
   const int tiles = (int)((end - u.lo + KEYS - 1) / KEYS), all = tiles * E;
-  Stage<T, P, KEYS, WNT, WIDE> rq, rg;
+  Carry<T, P, KEYS, WNT, WIDE> cq, cg;
+  cq.init(a.qs, D);
+  cg.init(a.gys, D);
   float r_lse = 0.0f, r_delta = 0.0f;
-  const auto fetch = [&](int j) {
-    const int h = g * E + j / tiles;
-    const long long t0 = u.lo + (long long)(j % tiles) * KEYS;
+  const auto fetch = [&](int h, int tile, char *to) {
+    const long long t0 = u.lo + (long long)tile * KEYS;
     const int count = (int)(end - t0 < KEYS ? end - t0 : KEYS);
-    rq.fetch(static_cast<const T *>(a.q) + u.b * a.qs + (long long)h * D, a.qs, D, t0, 1, count);
-    rg.fetch(static_cast<const T *>(a.gy) + u.b * a.gys + (long long)h * D, a.gys, D, t0, 1,
-             count);
+    cq.fetch(static_cast<const T *>(a.q) + u.b * a.qs + (long long)h * D, a.qs, D, t0, count, to);
+    cg.fetch(static_cast<const T *>(a.gy) + u.b * a.gys + (long long)h * D, a.gys, D, t0, count,
+             to + TILE);
     if (threadIdx.x < KEYS) {
       const bool there = (int)threadIdx.x < count;
       const long long at = (u.b + t0 + threadIdx.x) * a.H + h;
@@ -553,26 +612,37 @@ __global__ __launch_bounds__(WNT) void k_window_dkv(WinArgs a) {
       r_delta = there ? a.delta[at] : 0.0f;
     }
   };
-  fetch(0);
+  const auto finish = [&](int j) {
+    cq.finish(s_dyn + (j & 1) * 2 * TILE);
+    cg.finish(s_dyn + (j & 1) * 2 * TILE + TILE);
+    if (threadIdx.x < KEYS) {
+      s_row[j & 1][0][threadIdx.x] = r_lse;
+      s_row[j & 1][1][threadIdx.x] = r_delta;
+    }
+  };
+  int h = g * E, tile = 0;
+  fetch(h, 0, s_dyn);
+  finish(0);
   for (int j = 0; j < all; ++j) {
+    const char *s_q = s_dyn + (j & 1) * 2 * TILE, *s_g = s_q + TILE;
+    const float *s_lse = s_row[j & 1][0], *s_delta = s_row[j & 1][1];
     __syncthreads();
-    rq.store(s_q);
-    rg.store(s_g);
-    if (threadIdx.x < KEYS) s_lse[threadIdx.x] = r_lse, s_delta[threadIdx.x] = r_delta;
-    __syncthreads();
-    if (j + 1 < all) fetch(j + 1);
-    const long long t0 = u.lo + (long long)(j % tiles) * KEYS;
-    if (t0 + KEYS - 1 < sw || t0 - (sw + 16 * QT - 1) >= a.window) continue;
+    const long long t0 = u.lo + (long long)tile * KEYS;
+    const bool more = j + 1 < all;
+    if (++tile == tiles) tile = 0, ++h;
+    if (more) fetch(h, tile, s_dyn + (~j & 1) * 2 * TILE);
+    const bool none = t0 + KEYS - 1 < sw || t0 - (sw + 16 * QT - 1) >= a.window;
     const bool whole = t0 >= sw + 16 * QT - 1 && t0 + KEYS - 1 - sw < a.window;
 #pragma unroll
     for (int t2 = 0; t2 < 2; ++t2) {
+      if (none) continue;
       float4v x[2][QT] = {}, y[2][QT] = {};
 #pragma unroll
       for (int b = 0; b < 2; ++b)
 #pragma unroll
         for (int s = 0; s < DS; ++s) {
-          const Frag<T> f = rows<T, P>(s_q, 32 * t2 + 16 * b, 32 * s, lane);
-          const Frag<T> f2 = rows<T, P>(s_g, 32 * t2 + 16 * b, 32 * s, lane);
+          const Frag<T> f = Packed<T, P>::rows(s_q, 32 * t2 + 16 * b, 32 * s, lane);
+          const Frag<T> f2 = Packed<T, P>::rows(s_g, 32 * t2 + 16 * b, 32 * s, lane);
 #pragma unroll
           for (int i = 0; i < QT; ++i) {
             x[b][i] = mac(f, kf[i][s], x[b][i]);
@@ -608,8 +678,8 @@ __global__ __launch_bounds__(WNT) void k_window_dkv(WinArgs a) {
       }
 #pragma unroll
       for (int d = 0; d < DT; ++d) {
-        const Frag<T> f = columns<T, P>(s_g, 32 * t2, 16 * d, lane);
-        const Frag<T> f2 = columns<T, P>(s_q, 32 * t2, 16 * d, lane);
+        const Frag<T> f = Packed<T, P>::columns(s_g, 32 * t2, 16 * d, lane);
+        const Frag<T> f2 = Packed<T, P>::columns(s_q, 32 * t2, 16 * d, lane);
 #pragma unroll
         for (int i = 0; i < QT; ++i) {
           ov[d][i] = mac(f, p[i], ov[d][i]);
@@ -617,6 +687,7 @@ __global__ __launch_bounds__(WNT) void k_window_dkv(WinArgs a) {
         }
       }
     }
+    if (more) finish(j + 1);
   }
   if (!finite(ok) || !finite(ov)) {
 #pragma unroll
@@ -678,7 +749,7 @@ __global__ __launch_bounds__(WNT) void k_window_dkv(WinArgs a) {
 // sums joined in LDS.  Rows of `part` of units without such a query are not
 // written, nor read.
 template <typename T, int P, bool WIDE>
-__global__ __launch_bounds__(WNT) void k_window_sinks(WinArgs a) {
+__global__ __launch_bounds__(WNT, MIN_WAVES<T>) void k_window_sinks(WinArgs a) {
   constexpr int Q = 32 * WNW, DT = P / 16, DS = P / 32;
   extern __shared__ __attribute__((aligned(16))) char s_dyn[];
   T *s_q = reinterpret_cast<T *>(s_dyn), *s_g = s_q + Q * LD<T, P>;
@@ -1010,12 +1081,12 @@ __global__ __launch_bounds__(WNT) void k_window_fill(WinFillArgs a) {
 // ---------------------------------------------------------------------------
 
 // Whether every head's row of each tensor begins at a multiple of 16 bytes and is
-// whole groups of them.
+// whole groups of them, and tiles are within reach.
 bool wide_rows(size_t e, int D, std::initializer_list<long long> strides,
                std::initializer_list<const void *> data) {
   if (D * e % 16) return false;
   for (long long t : strides)
-    if (t * e % 16) return false;
+    if (t * e % 16 || (t * KEYS + D) * (long long)e > MAX_TILE_BYTES) return false;
   for (const void *p : data)
     if (reinterpret_cast<uintptr_t>(p) % 16) return false;
   return true;
@@ -1025,10 +1096,26 @@ dim3 blocks(const WinArgs &a, long long per, int across) {
   return dim3((unsigned)(a.N / per + a.n), across);
 }
 
+// LDS of the walks over tiles of 64 rows: two pairs of them.
+template <typename T, int P>
+constexpr int WALK = 4 * KEYS * P * (int)sizeof(T);
+
+hipError_t allow_lds(const void *kernel, int lds) {
+  if (lds <= 64 * 1024) return hipSuccess;
+  return hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+}
+template <typename T, int P>
+hipError_t walk(void (*kernel)(WinArgs), int across, const WinArgs &a, hipStream_t s) {
+  static_assert(WALK<T, P> <= 150 * 1024, "LDS of a CU");
+  const hipError_t e = allow_lds(reinterpret_cast<const void *>(kernel), WALK<T, P>);
+  if (e != hipSuccess) return e;
+  kernel<<<blocks(a, BLOCK, across), WNT, WALK<T, P>, s>>>(a);
+  return hipGetLastError();
+}
+
 template <typename T, int P, bool WIDE>
 hipError_t forward_as(const WinArgs &a, hipStream_t s) {
-  k_window<T, P, WIDE><<<blocks(a, BLOCK, a.H), WNT, 0, s>>>(a);
-  return hipGetLastError();
+  return walk<T, P>(k_window<T, P, WIDE>, a.H, a, s);
 }
 
 template <typename T, int P, bool WIDE>
@@ -1039,9 +1126,7 @@ hipError_t sinks_as(const WinArgs &a, hipStream_t s) {
   dim3 grid = blocks(a, a.unit, a.G);
   grid.z = (a.sinks + 15) / 16;
   if (grid.z > 65535) return hipErrorInvalidValue;
-  const hipError_t e =
-      hipFuncSetAttribute(reinterpret_cast<const void *>(k_window_sinks<T, P, WIDE>),
-                          hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+  const hipError_t e = allow_lds(reinterpret_cast<const void *>(k_window_sinks<T, P, WIDE>), lds);
   if (e != hipSuccess) return e;
   k_window_sinks<T, P, WIDE><<<grid, WNT, lds, s>>>(a);
   return hipGetLastError();
@@ -1052,13 +1137,10 @@ hipError_t backward_as(const WinArgs &a, hipStream_t s) {
   if (a.most) k_window_zero<<<1, 2, 0, s>>>(a.most);
   const long long rows = (a.N * a.H + WNT / 16 - 1) / (WNT / 16);
   k_window_delta<T><<<(unsigned)(rows < 4096 ? rows : 4096), WNT, 0, s>>>(a);
-  k_window_dq<T, P, WIDE><<<blocks(a, BLOCK, a.H), WNT, 0, s>>>(a);
-  if (a.part) {
-    const hipError_t e = sinks_as<T, P, WIDE>(a, s);
-    if (e != hipSuccess) return e;
-  }
-  k_window_dkv<T, P, WIDE><<<blocks(a, BLOCK, a.G), WNT, 0, s>>>(a);
-  return hipGetLastError();
+  hipError_t e = walk<T, P>(k_window_dq<T, P, WIDE>, a.H, a, s);
+  if (e == hipSuccess && a.part) e = sinks_as<T, P, WIDE>(a, s);
+  if (e == hipSuccess) e = walk<T, P>(k_window_dkv<T, P, WIDE>, a.G, a, s);
+  return e;
 }
 
 template <typename T, int P, bool WIDE>
