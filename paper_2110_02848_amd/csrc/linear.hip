@@ -46,28 +46,33 @@ __device__ __forceinline__ bool finite(const float4v (&x)[4]) {
   return __all(z == 0.0f);
 }
 
-// Row i against the rows up to it alone, term by term.  The product also takes
-// the later rows of v, times 0, which makes no number of an infinity or a NaN
-// that row i does not see: where a result is none, the sums are taken again.
-struct Fours {
-  float4v x[4];
-};
+// Row i against the state and the rows up to it alone, term by term, for 16 columns
+// of v of which lane group lg has four at a time.  The product also takes the later
+// rows of v, times 0, which makes no number of an infinity or a NaN that row i does
+// not see: where a result (in memory, at o) is none, it is taken again.
 template <typename T, int PA, int PB>
-__device__ __noinline__ Fours exact_rows(const T *s_q, const T *s_k, const T *s_v,
-                                         const float *s_pow, int i, int A, int lg, float scale) {
-  Fours o{};
-  for (int row = 0; row <= i; ++row) {
-    float p = 0.0f;
-    for (int c = 0; c < A; ++c)
-      p = fmaf((float)s_q[i * LD<T, PA> + c], (float)s_k[row * LD<T, PA> + c], p);
-    p *= s_pow[i - row] * scale;
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
+__device__ __noinline__ void exact_rows(T *o, int left, const T *s_q, const T *s_k, const T *s_v,
+                                        const T *s_s, const float *s_pow, int i, int A, int lg,
+                                        float f_past, float f_now) {
+  for (int c = 4 * lg; c < SLICE; c += 16) {
+    if (!none_of_four(o, c, left)) continue;
+    float4v past{}, now{};
+    for (int d = 0; d < A; ++d)
 #pragma unroll
       for (int r = 0; r < 4; ++r)
-        o.x[j][r] = fmaf(p, (float)s_v[row * LD<T, PB> + 16 * j + 4 * lg + r], o.x[j][r]);
+        past[r] = fmaf((float)s_q[i * LD<T, PA> + d], (float)s_s[(c + r) * LD<T, PA> + d],
+                       past[r]);
+    for (int row = 0; row <= i; ++row) {
+      float p = 0.0f;
+      for (int d = 0; d < A; ++d)
+        p = fmaf((float)s_q[i * LD<T, PA> + d], (float)s_k[row * LD<T, PA> + d], p);
+      p *= s_pow[i - row];
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        now[r] = fmaf(p, (float)s_v[row * LD<T, PB> + c + r], now[r]);
+    }
+    mend_four(o, c, left, past * f_past + now * f_now);
   }
-  return o;
 }
 
 // Over the wavefronts.
@@ -262,14 +267,7 @@ __global__ __launch_bounds__(256 * CG, CG == 2 ? 2 : sizeof(T) == 2 && PA == 64 
         for (int j = 0; j < 4; ++j)
           now[j] = mac(columns<T, PB>(s_v, 32 * t, c0 + 16 * j, lane), p, now[j]);
       }
-      if (!finite(now)) {
-        const Fours o = exact_rows<T, PA, PB>(s_q, s_k, s_v + c0, s_pow, i, A, lg, p_scale);
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-#pragma unroll
-          for (int r = 0; r < 4; ++r)
-            now[j][r] = fabsf(now[j][r]) < INFINITY ? now[j][r] : o.x[j][r];
-      }
+      const bool fine = finite(now);
       if (i < count) {
         T *o = static_cast<T *>(job.o) + (u.first + (i0 + i) * u.step) * job.os +
                (long long)h * B + b0;
@@ -277,6 +275,9 @@ __global__ __launch_bounds__(256 * CG, CG == 2 ? 2 : sizeof(T) == 2 && PA == 64 
 #pragma unroll
         for (int j = 0; j < 4; ++j)
           store_four<T, WIDE>(o, c0 + 16 * j + 4 * lg, left, past[j] * f + now[j] * f2);
+        if (!fine)
+          exact_rows<T, PA, PB>(o + c0, left - c0, s_q, s_k, s_v + c0, s_s + c0 * LD<T, PA>, s_pow,
+                                i, A, lg, f, job.so);
       }
     }
     if (more || !FULL || (job.last && u.hi == u.len)) {

@@ -333,6 +333,23 @@ __device__ __forceinline__ void store_four(T *row, int c, int width, const float
   }
 }
 
+// Of the same four, as they were written: whether one is no number, and x in the
+// place of those that are none.
+template <typename T>
+__device__ __forceinline__ bool none_of_four(const T *row, int c, int width) {
+  bool bad = false;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (c + i < width) bad = bad || !(fabsf((float)row[c + i]) < INFINITY);
+  return bad;
+}
+template <typename T>
+__device__ __forceinline__ void mend_four(T *row, int c, int width, const float4v &x) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (c + i < width && !(fabsf((float)row[c + i]) < INFINITY)) row[c + i] = (T)x[i];
+}
+
 __device__ __forceinline__ float wave_max(float m) {
 #pragma unroll
   for (int o = 32; o; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, WAVE));

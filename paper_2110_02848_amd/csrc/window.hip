@@ -29,6 +29,7 @@ namespace {
 constexpr int WNT = 256;             // threads
 constexpr int WNW = WNT / WAVE;
 constexpr int KEYS = 64;             // of a tile of keys
+constexpr int QUERIES = 32;          // of a tile of queries
 constexpr int QT = 2;                // tiles of 16 queries (or keys) of a wavefront
 constexpr int BLOCK = 16 * QT * WNW; // queries, or keys, of a workgroup
 constexpr int FEW = 64;              // frames
@@ -52,13 +53,6 @@ __device__ __forceinline__ bool finite(const float4v (&x)[N][M]) {
 #pragma unroll
       for (int r = 0; r < 4; ++r) z = fmaf(x[i][j][r], 0.0f, z);
   return __all(z == 0.0f);
-}
-
-// a's numbers, and b's in the place of those that are none.
-__device__ __forceinline__ float4v either(float4v a, const float4v &b) {
-#pragma unroll
-  for (int r = 0; r < 4; ++r) a[r] = fabsf(a[r]) < INFINITY ? a[r] : b[r];
-  return a;
 }
 
 // Sum of a[i] b[i], i < D.
@@ -97,7 +91,9 @@ __device__ __forceinline__ Seen seen_by(long long lo, long long hi, int window, 
 // A query row against the frames that it sees alone, term by term, for four columns
 // from d0 on.  The products also take the others' v, times 0, which makes no number
 // of an infinity or a NaN that the query does not see: where a result is none, it
-// is taken again.  The same below for the gradients.
+// is taken again.  The same below for the gradients.  (Behind the results' stores:
+// registers that had to hold results across these calls would be missing in the
+// products.)
 template <typename T>
 __device__ __noinline__ float4v exact_row(const T *q, const T *k, long long ks, const T *v,
                                           long long vs, int D, long long t, int window,
@@ -272,20 +268,7 @@ __global__ __launch_bounds__(WNT, MIN_WAVES<T>) void k_window(WinArgs a) {
       cv.finish(s_next + TILE);
     }
   }
-  if (!finite(o)) {
-#pragma unroll
-    for (int i = 0; i < QT; ++i) {
-      const long long t = tw + 16 * i + l16;
-      if (t >= u.hi) continue;
-#pragma unroll
-      for (int d = 0; d < DT; ++d)
-        if (16 * d + 4 * lg < D)
-          o[d][i] = either(
-              o[d][i], exact_row<T>(q + t * a.qs, k, a.ks, v, a.vs, D, t, a.window, a.sinks,
-                                    a.scale < 0.0f ? -c : c,
-                                    m[i] == -INFINITY ? 0.0f : m[i] * c, 16 * d + 4 * lg));
-    }
-  }
+  const bool fine = finite(o);
 #pragma unroll
   for (int i = 0; i < QT; ++i) {
     l[i] += __shfl_xor(l[i], 16, WAVE);
@@ -297,6 +280,19 @@ __global__ __launch_bounds__(WNT, MIN_WAVES<T>) void k_window(WinArgs a) {
 #pragma unroll
     for (int d = 0; d < DT; ++d) store_four<T, WIDE>(y, 16 * d + 4 * lg, D, o[d][i] * f);
     if (lg == 0) a.lse[(u.b + t) * a.H + h] = fmaf(m[i], c, log2f(l[i])) * LOG2;
+  }
+  if (fine) return;
+#pragma unroll
+  for (int i = 0; i < QT; ++i) {
+    const long long t = tw + 16 * i + l16;
+    if (t >= u.hi) continue;
+    T *y = static_cast<T *>(a.o) + (u.b + t) * a.os + (long long)h * D;
+    for (int d = 4 * lg; d < D; d += 16)
+      if (none_of_four(y, d, D))
+        mend_four(y, d, D,
+                  exact_row<T>(q + t * a.qs, k, a.ks, v, a.vs, D, t, a.window, a.sinks,
+                               a.scale < 0.0f ? -c : c, m[i] == -INFINITY ? 0.0f : m[i] * c, d) *
+                      (1.0f / l[i]));
   }
 }
 
@@ -537,19 +533,7 @@ __global__ __launch_bounds__(WNT, MIN_WAVES<T>) void k_window_dq(WinArgs a) {
       cv.finish(s_next + TILE);
     }
   }
-  if (!finite(o)) {
-#pragma unroll
-    for (int i = 0; i < QT; ++i) {
-      const long long t = tw + 16 * i + l16;
-      if (t >= u.hi) continue;
-#pragma unroll
-      for (int d = 0; d < DT; ++d)
-        if (16 * d + 4 * lg < D)
-          o[d][i] = either(
-              o[d][i], exact_dq<T>(q + t * a.qs, gy + t * a.gys, k, a.ks, v, a.vs, D, t, a.window,
-                                   a.sinks, c, lse[i], delta[i], up, 16 * d + 4 * lg));
-    }
-  }
+  const bool fine = finite(o);
   const float f = a.scale / up;
 #pragma unroll
   for (int i = 0; i < QT; ++i) {
@@ -559,16 +543,29 @@ __global__ __launch_bounds__(WNT, MIN_WAVES<T>) void k_window_dq(WinArgs a) {
 #pragma unroll
     for (int d = 0; d < DT; ++d) store_four<T, WIDE>(gq, 16 * d + 4 * lg, D, o[d][i] * f);
   }
+  if (fine) return;
+#pragma unroll
+  for (int i = 0; i < QT; ++i) {
+    const long long t = tw + 16 * i + l16;
+    if (t >= u.hi) continue;
+    T *gq = static_cast<T *>(a.gq) + (u.b + t) * a.gqs + (long long)h * D;
+    for (int d = 4 * lg; d < D; d += 16)
+      if (none_of_four(gq, d, D))
+        mend_four(gq, d, D,
+                  exact_dq<T>(q + t * a.qs, gy + t * a.gys, k, a.ks, v, a.vs, D, t, a.window,
+                              a.sinks, c, lse[i], delta[i], up, d) * f);
+  }
 }
 
 // Gradients by keys and values: a workgroup has BLOCK keys of a key head, walks
 // the queries that see them through the window, head after head of its group,
 // and adds what the sinks' units found.
 template <typename T, int P, bool WIDE>
-__global__ __launch_bounds__(WNT, P == 64 ? MIN_WAVES<T> : 1) void k_window_dkv(WinArgs a) {
-  constexpr int DT = P / 16, DS = P / 32, TILE = KEYS * P * (int)sizeof(T);
-  extern __shared__ __attribute__((aligned(16))) char s_dyn[];  // [2][q, dy][TILE]
-  __shared__ __attribute__((aligned(16))) float s_row[2][2][KEYS];  // lse, delta
+__global__ __launch_bounds__(WNT, MIN_WAVES<T>) void k_window_dkv(WinArgs a) {
+  constexpr int DT = P / 16, DS = P / 32, TILE = QUERIES * P * (int)sizeof(T);
+  extern __shared__ __attribute__((aligned(16))) char s_dyn[];  // [2][q, dy][TILE], v
+  __shared__ __attribute__((aligned(16))) float s_row[2][2][QUERIES];  // lse, delta
+  char *s_v = s_dyn + 4 * TILE;
   const int lane = threadIdx.x & (WAVE - 1), l16 = lane & 15, lg = lane >> 4;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
   const int g = blockIdx.y, E = a.H / a.G, D = a.D;
@@ -578,7 +575,10 @@ __global__ __launch_bounds__(WNT, P == 64 ? MIN_WAVES<T> : 1) void k_window_dkv(
   const T *k = static_cast<const T *>(a.k) + u.b * a.ks + (long long)g * D;
   const T *v = static_cast<const T *>(a.v) + u.b * a.vs + (long long)g * D;
   const long long sw = u.lo + w * 16 * QT;  // the wavefront's first key
-  Frag<T> kf[QT][DS], vf[QT][DS];
+  Carry<T, P, BLOCK, WNT, WIDE> cv;
+  cv.init(a.vs, D);
+  cv.fetch(v, a.vs, D, u.lo, (int)(u.hi - u.lo), s_v);
+  Frag<T> kf[QT][DS];
 #pragma unroll
   for (int i = 0; i < QT; ++i) {
     const long long s = sw + 16 * i + l16;
@@ -588,24 +588,24 @@ __global__ __launch_bounds__(WNT, P == 64 ? MIN_WAVES<T> : 1) void k_window_dkv(
       for (int e = 0; e < (int)sizeof(T) / 2; ++e) {
         const int at = 32 * t + 8 * lg + e * PER<T>;
         kf[i][t].v[e] = load_group<T, WIDE>(k + s * a.ks, at, D, s < u.hi);
-        vf[i][t].v[e] = load_group<T, WIDE>(v + s * a.vs, at, D, s < u.hi);
       }
   }
+  cv.finish(s_v);
   const float c = a.scale * LOG2E, up = ds_scale<T>(a);
   float4v ok[DT][QT] = {}, ov[DT][QT] = {};
   const long long end = u.hi - 1 + a.window < u.len ? u.hi - 1 + a.window : u.len;
-  const int tiles = (int)((end - u.lo + KEYS - 1) / KEYS), all = tiles * E;
-  Carry<T, P, KEYS, WNT, WIDE> cq, cg;
+  const int tiles = (int)((end - u.lo + QUERIES - 1) / QUERIES), all = tiles * E;
+  Carry<T, P, QUERIES, WNT, WIDE> cq, cg;
   cq.init(a.qs, D);
   cg.init(a.gys, D);
   float r_lse = 0.0f, r_delta = 0.0f;
   const auto fetch = [&](int h, int tile, char *to) {
-    const long long t0 = u.lo + (long long)tile * KEYS;
-    const int count = (int)(end - t0 < KEYS ? end - t0 : KEYS);
+    const long long t0 = u.lo + (long long)tile * QUERIES;
+    const int count = (int)(end - t0 < QUERIES ? end - t0 : QUERIES);
     cq.fetch(static_cast<const T *>(a.q) + u.b * a.qs + (long long)h * D, a.qs, D, t0, count, to);
     cg.fetch(static_cast<const T *>(a.gy) + u.b * a.gys + (long long)h * D, a.gys, D, t0, count,
              to + TILE);
-    if (threadIdx.x < KEYS) {
+    if (threadIdx.x < QUERIES) {
       const bool there = (int)threadIdx.x < count;
       const long long at = (u.b + t0 + threadIdx.x) * a.H + h;
       r_lse = there ? a.lse[at] * LOG2E : INFINITY;
@@ -615,7 +615,7 @@ __global__ __launch_bounds__(WNT, P == 64 ? MIN_WAVES<T> : 1) void k_window_dkv(
   const auto finish = [&](int j) {
     cq.finish(s_dyn + (j & 1) * 2 * TILE);
     cg.finish(s_dyn + (j & 1) * 2 * TILE + TILE);
-    if (threadIdx.x < KEYS) {
+    if (threadIdx.x < QUERIES) {
       s_row[j & 1][0][threadIdx.x] = r_lse;
       s_row[j & 1][1][threadIdx.x] = r_delta;
     }
@@ -627,32 +627,34 @@ __global__ __launch_bounds__(WNT, P == 64 ? MIN_WAVES<T> : 1) void k_window_dkv(
     const char *s_q = s_dyn + (j & 1) * 2 * TILE, *s_g = s_q + TILE;
     const float *s_lse = s_row[j & 1][0], *s_delta = s_row[j & 1][1];
     __syncthreads();
-    const long long t0 = u.lo + (long long)tile * KEYS;
+    const long long t0 = u.lo + (long long)tile * QUERIES;
     const bool more = j + 1 < all;
     if (++tile == tiles) tile = 0, ++h;
     if (more) fetch(h, tile, s_dyn + (~j & 1) * 2 * TILE);
-    const bool none = t0 + KEYS - 1 < sw || t0 - (sw + 16 * QT - 1) >= a.window;
-    const bool whole = t0 >= sw + 16 * QT - 1 && t0 + KEYS - 1 - sw < a.window;
-#pragma unroll
-    for (int t2 = 0; t2 < 2; ++t2) {
-      if (none) continue;
+    const bool none = t0 + QUERIES - 1 < sw || t0 - (sw + 16 * QT - 1) >= a.window;
+    const bool whole = t0 >= sw + 16 * QT - 1 && t0 + QUERIES - 1 - sw < a.window;
+    if (!none) {
       float4v x[2][QT] = {}, y[2][QT] = {};
 #pragma unroll
-      for (int b = 0; b < 2; ++b)
+      for (int s = 0; s < DS; ++s) {
+        Frag<T> vf[QT];
 #pragma unroll
-        for (int s = 0; s < DS; ++s) {
-          const Frag<T> f = Packed<T, P>::rows(s_q, 32 * t2 + 16 * b, 32 * s, lane);
-          const Frag<T> f2 = Packed<T, P>::rows(s_g, 32 * t2 + 16 * b, 32 * s, lane);
+        for (int i = 0; i < QT; ++i)
+          vf[i] = Packed<T, P>::rows(s_v, (w * QT + i) * 16, 32 * s, lane);
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+          const Frag<T> f = Packed<T, P>::rows(s_q, 16 * b, 32 * s, lane);
+          const Frag<T> f2 = Packed<T, P>::rows(s_g, 16 * b, 32 * s, lane);
 #pragma unroll
           for (int i = 0; i < QT; ++i) {
             x[b][i] = mac(f, kf[i][s], x[b][i]);
-            y[b][i] = mac(f2, vf[i][s], y[b][i]);
+            y[b][i] = mac(f2, vf[i], y[b][i]);
           }
         }
-      Frag<T> p[QT], ds[QT];
+      }
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
-        const int at = 32 * t2 + 16 * b + 4 * lg;
+        const int at = 16 * b + 4 * lg;
         const float4v lse = *reinterpret_cast<const float4v *>(s_lse + at);
         const float4v delta = *reinterpret_cast<const float4v *>(s_delta + at);
 #pragma unroll
@@ -671,6 +673,7 @@ __global__ __launch_bounds__(WNT, P == 64 ? MIN_WAVES<T> : 1) void k_window_dkv(
             y[b][i][r] = d;
           }
       }
+      Frag<T> p[QT], ds[QT];
 #pragma unroll
       for (int i = 0; i < QT; ++i) {
         p[i] = pack<T>(x[0][i], x[1][i]);
@@ -678,8 +681,8 @@ __global__ __launch_bounds__(WNT, P == 64 ? MIN_WAVES<T> : 1) void k_window_dkv(
       }
 #pragma unroll
       for (int d = 0; d < DT; ++d) {
-        const Frag<T> f = Packed<T, P>::columns(s_g, 32 * t2, 16 * d, lane);
-        const Frag<T> f2 = Packed<T, P>::columns(s_q, 32 * t2, 16 * d, lane);
+        const Frag<T> f = Packed<T, P>::columns(s_g, 0, 16 * d, lane);
+        const Frag<T> f2 = Packed<T, P>::columns(s_q, 0, 16 * d, lane);
 #pragma unroll
         for (int i = 0; i < QT; ++i) {
           ov[d][i] = mac(f, p[i], ov[d][i]);
@@ -689,57 +692,58 @@ __global__ __launch_bounds__(WNT, P == 64 ? MIN_WAVES<T> : 1) void k_window_dkv(
     }
     if (more) finish(j + 1);
   }
-  if (!finite(ok) || !finite(ov)) {
-#pragma unroll
-    for (int i = 0; i < QT; ++i) {
-      const long long s = sw + 16 * i + l16;
-      if (s >= u.hi) continue;
-      const long long t1 = s + a.window < u.len ? s + a.window : u.len;
-#pragma unroll
-      for (int d = 0; d < DT; ++d) {
-        if (16 * d + 4 * lg >= D) continue;
-        float4v xk{}, xv{};
-        for (int h = g * E; h < g * E + E; ++h) {
-          const T *qh = static_cast<const T *>(a.q) + u.b * a.qs + (long long)h * D;
-          const T *gh = static_cast<const T *>(a.gy) + u.b * a.gys + (long long)h * D;
-          const TwoFours x = exact_dkv<T>(
-              qh, a.qs, gh, a.gys, a.lse + u.b * a.H + h, a.delta + u.b * a.H + h, a.H, D,
-              k + s * a.ks, v + s * a.vs, s, s, t1, 0, 0, a.window, a.sinks, c, up,
-              16 * d + 4 * lg);
-          xk += x.k;
-          xv += x.v;
-        }
-        ok[d][i] = either(ok[d][i], xk);
-        ov[d][i] = either(ov[d][i], xv);
-      }
-    }
-  }
+  const bool fine = finite(ok) && finite(ov);
   const float f = a.scale / up;
+  // what units of queries found that see a first frame from outside the window, in
+  // their order
+  const long long units = rows_before(u.b, u.s, a.unit);
+  const auto from_units = [&](long long s, int d, float4v &xk, float4v &xv) {
+    if (s >= a.sinks || u.len <= a.window) return;
+    const long long n = (u.len + a.unit - 1) / a.unit;
+    for (long long j = a.window / a.unit; j < n; ++j) {
+      const float *p = a.part + (((units + j) * a.G + g) * a.sinks + s) * 2 * P + d;
+      xk += *reinterpret_cast<const float4v *>(p);
+      xv += *reinterpret_cast<const float4v *>(p + P);
+    }
+  };
 #pragma unroll
   for (int i = 0; i < QT; ++i) {
     const long long s = sw + 16 * i + l16;
     if (s >= u.hi) continue;
-#pragma unroll
-    for (int d = 0; d < DT; ++d) ok[d][i] *= f;
-    if (s < a.sinks && u.len > a.window) {
-      // units of queries that see it from outside the window, in their order
-      const long long first = rows_before(u.b, u.s, a.unit);
-      const long long n = (u.len + a.unit - 1) / a.unit;
-      for (long long j = a.window / a.unit; j < n; ++j) {
-        const float *p = a.part + (((first + j) * a.G + g) * a.sinks + s) * 2 * P;
-#pragma unroll
-        for (int d = 0; d < DT; ++d) {
-          ok[d][i] += *reinterpret_cast<const float4v *>(p + 16 * d + 4 * lg);
-          ov[d][i] += *reinterpret_cast<const float4v *>(p + P + 16 * d + 4 * lg);
-        }
-      }
-    }
     T *gk = static_cast<T *>(a.gk) + (u.b + s) * a.gks + (long long)g * D;
     T *gv = static_cast<T *>(a.gv) + (u.b + s) * a.gvs + (long long)g * D;
 #pragma unroll
     for (int d = 0; d < DT; ++d) {
+      ok[d][i] *= f;
+      from_units(s, 16 * d + 4 * lg, ok[d][i], ov[d][i]);
       store_four<T, WIDE>(gk, 16 * d + 4 * lg, D, ok[d][i]);
       store_four<T, WIDE>(gv, 16 * d + 4 * lg, D, ov[d][i]);
+    }
+  }
+  if (fine) return;
+#pragma unroll 1
+  for (int i = 0; i < QT; ++i) {
+    const long long s = sw + 16 * i + l16;
+    if (s >= u.hi) continue;
+    T *gk = static_cast<T *>(a.gk) + (u.b + s) * a.gks + (long long)g * D;
+    T *gv = static_cast<T *>(a.gv) + (u.b + s) * a.gvs + (long long)g * D;
+    const long long t1 = s + a.window < u.len ? s + a.window : u.len;
+    for (int d = 4 * lg; d < D; d += 16) {
+      if (!none_of_four(gk, d, D) && !none_of_four(gv, d, D)) continue;
+      float4v xk{}, xv{};
+      for (int hh = g * E; hh < g * E + E; ++hh) {
+        const T *qh = static_cast<const T *>(a.q) + u.b * a.qs + (long long)hh * D;
+        const T *gh = static_cast<const T *>(a.gy) + u.b * a.gys + (long long)hh * D;
+        const TwoFours x = exact_dkv<T>(
+            qh, a.qs, gh, a.gys, a.lse + u.b * a.H + hh, a.delta + u.b * a.H + hh, a.H, D,
+            k + s * a.ks, v + s * a.vs, s, s, t1, 0, 0, a.window, a.sinks, c, up, d);
+        xk += x.k;
+        xv += x.v;
+      }
+      xk *= f;
+      from_units(s, d, xk, xv);
+      mend_four(gk, d, D, xk);
+      mend_four(gv, d, D, xv);
     }
   }
 }
@@ -850,8 +854,11 @@ __global__ __launch_bounds__(WNT, MIN_WAVES<T>) void k_window_sinks(WinArgs a) {
         xk += x.k;
         xv += x.v;
       }
-      ok[d] = either(ok[d], xk);
-      ov[d] = either(ov[d], xv);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        ok[d][r] = fabsf(ok[d][r]) < INFINITY ? ok[d][r] : xk[r];
+        ov[d][r] = fabsf(ov[d][r]) < INFINITY ? ov[d][r] : xv[r];
+      }
     }
   }
   // (the sums take as much of LDS as the tiles of a 16-bit type)
@@ -1086,7 +1093,7 @@ bool wide_rows(size_t e, int D, std::initializer_list<long long> strides,
                std::initializer_list<const void *> data) {
   if (D * e % 16) return false;
   for (long long t : strides)
-    if (t * e % 16 || (t * KEYS + D) * (long long)e > MAX_TILE_BYTES) return false;
+    if (t * e % 16 || (t * BLOCK + D) * (long long)e > MAX_TILE_BYTES) return false;
   for (const void *p : data)
     if (reinterpret_cast<uintptr_t>(p) % 16) return false;
   return true;
@@ -1104,18 +1111,22 @@ hipError_t allow_lds(const void *kernel, int lds) {
   if (lds <= 64 * 1024) return hipSuccess;
   return hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
 }
+// and of the walk over queries: two pairs of 32 rows, and a block of v.
 template <typename T, int P>
-hipError_t walk(void (*kernel)(WinArgs), int across, const WinArgs &a, hipStream_t s) {
-  static_assert(WALK<T, P> <= 150 * 1024, "LDS of a CU");
-  const hipError_t e = allow_lds(reinterpret_cast<const void *>(kernel), WALK<T, P>);
+constexpr int WALK_KEYS = (4 * QUERIES + BLOCK) * P * (int)sizeof(T);
+
+hipError_t walk(void (*kernel)(WinArgs), int lds, int across, const WinArgs &a, hipStream_t s) {
+  const hipError_t e = allow_lds(reinterpret_cast<const void *>(kernel), lds);
   if (e != hipSuccess) return e;
-  kernel<<<blocks(a, BLOCK, across), WNT, WALK<T, P>, s>>>(a);
+  kernel<<<blocks(a, BLOCK, across), WNT, lds, s>>>(a);
   return hipGetLastError();
 }
+static_assert(WALK<float, 128> <= 150 * 1024 && WALK_KEYS<float, 128> <= 150 * 1024,
+              "LDS of a CU");
 
 template <typename T, int P, bool WIDE>
 hipError_t forward_as(const WinArgs &a, hipStream_t s) {
-  return walk<T, P>(k_window<T, P, WIDE>, a.H, a, s);
+  return walk(k_window<T, P, WIDE>, WALK<T, P>, a.H, a, s);
 }
 
 template <typename T, int P, bool WIDE>
@@ -1137,9 +1148,9 @@ hipError_t backward_as(const WinArgs &a, hipStream_t s) {
   if (a.most) k_window_zero<<<1, 2, 0, s>>>(a.most);
   const long long rows = (a.N * a.H + WNT / 16 - 1) / (WNT / 16);
   k_window_delta<T><<<(unsigned)(rows < 4096 ? rows : 4096), WNT, 0, s>>>(a);
-  hipError_t e = walk<T, P>(k_window_dq<T, P, WIDE>, a.H, a, s);
+  hipError_t e = walk(k_window_dq<T, P, WIDE>, WALK<T, P>, a.H, a, s);
   if (e == hipSuccess && a.part) e = sinks_as<T, P, WIDE>(a, s);
-  if (e == hipSuccess) e = walk<T, P>(k_window_dkv<T, P, WIDE>, a.G, a, s);
+  if (e == hipSuccess) e = walk(k_window_dkv<T, P, WIDE>, WALK_KEYS<T, P>, a.G, a, s);
   return e;
 }
 
