@@ -631,7 +631,8 @@ FST_API int fst_linear_attention_step(fst_ctx *ctx, const fst_matrix *q, const f
  * q has `heads` heads, k and v have kv_heads, each shared by heads / kv_heads
  * consecutive heads of q; all heads have the same number of columns.  window >= 1
  * (one as long as the sequences: all earlier frames), sinks >= 0, their sum at
- * most 2^31 - 1.  With 16-bit matrices e^(z - maximum) and the gradient of z are
+ * most 2^31 - 1; blocks of 128 rows and sequences together more than 2^23 give
+ * FST_ERR_TOO_LARGE.  With 16-bit matrices e^(z - maximum) and the gradient of z are
  * rounded to the matrices' type (float16: the gradient scaled by a power of two
  * first) before they are multiplied. */
 typedef struct {

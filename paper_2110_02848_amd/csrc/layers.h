@@ -173,8 +173,9 @@ struct WinArgs {
   // workspace of the gradients
   float *delta;                     // [N, H]
   uint32_t *most;                   // float16: largest lengths of rows of gy and v
-  float *part;                      // sinks: units' sums for gk and gv
-  long long unit;                   // queries of one of these
+  float *own, *part;                // sums for gk and gv of cut sequences' first frames:
+                                    // their blocks' own, and units' (or null)
+  long long unit;                   // queries of a unit
 };
 hipError_t launch_window(const WinArgs &a, int type, hipStream_t s);
 hipError_t launch_window_grads(WinArgs a, int type, void *ws, size_t *need, hipStream_t s);

@@ -11,10 +11,11 @@
 //
 // Back, with P = e^(z - lse) and delta_t = y_t . dy_t:
 //   dS = P (dy v^T - delta),  dq = scale dS k,  dk = scale dS^T q,  dv = P^T dy
-// from scores that are computed again: one kernel by queries (dq), one by keys (dk,
-// dv), so that every sum has one owner and one order.  First frames are seen by
-// all later queries: what lies outside the window is summed by units of
-// queries first (k_window_sinks), and the owner of the keys adds the units.
+// from scores that are computed again, once by queries (dq) and once by keys (dk, dv),
+// so that every sum has one owner and one order.  First frames are seen by all
+// later queries: in long sequences, units of queries sum what lies outside the
+// window, and k_window_first adds the units.  All three are workgroups of one launch,
+// the long ones first, so that none waits for another's last.
 #include <initializer_list>
 
 #include "sequences.h"
@@ -399,20 +400,14 @@ __device__ __noinline__ TwoFours exact_dkv(const T *q, long long qs, const T *gy
   return x;
 }
 
-// Gradients by queries.  delta from y as it was rounded is off by half a spacing of
-// y, which is next to nothing beside dS of many frames but as much as the rounding
-// of dS beside few: queries of a sequence's first block, and of windows up to FEW
-// frames, have it summed again from P and dy v^T, before their dS.
-template <typename T, int P, bool WIDE>
-__global__ __launch_bounds__(WNT, MIN_WAVES<T>) void k_window_dq(WinArgs a) {
+// Gradients by queries; SUMS: only their delta, from P and dy v^T.
+template <typename T, int P, bool WIDE, bool SUMS>
+__device__ __forceinline__ void dq_block(const WinArgs &a, const Unit &u, int h, char *s_dyn) {
+  // s_dyn: [2][k, v][TILE]
   constexpr int DT = P / 16, DS = P / 32, TILE = KEYS * P * (int)sizeof(T);
-  extern __shared__ __attribute__((aligned(16))) char s_dyn[];  // [2][k, v][TILE]
   const int lane = threadIdx.x & (WAVE - 1), l16 = lane & 15, lg = lane >> 4;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
-  const int h = blockIdx.y, g = h / (a.H / a.G), D = a.D;
-  Unit u;
-  if (!unit_of(a.off, a.n, a.N, BLOCK, false, blockIdx.x, u) || u.lo >= u.hi) return;
-
+  const int g = h / (a.H / a.G), D = a.D;
   const T *q = static_cast<const T *>(a.q) + u.b * a.qs + (long long)h * D;
   const T *gy = static_cast<const T *>(a.gy) + u.b * a.gys + (long long)h * D;
   const T *k = static_cast<const T *>(a.k) + u.b * a.ks + (long long)g * D;
@@ -453,32 +448,17 @@ __global__ __launch_bounds__(WNT, MIN_WAVES<T>) void k_window_dq(WinArgs a) {
   }
   const float c = a.scale * LOG2E, up = ds_scale<T>(a);
   float4v o[DT][QT] = {};
-  // sweep 0 sums delta, sweep 1 dq
-  const bool few = sizeof(T) == 2 && (u.lo == 0 || a.window + a.sinks <= FEW);
   float sum[QT] = {};
-  const int steps = few ? 2 * sn.tiles : sn.tiles;
-  for (int step = 0; step < steps; ++step) {
-    const bool sums = few && step < sn.tiles;
-    const int tile = few && !sums ? step - sn.tiles : step;
-    if (few && step == sn.tiles) {
-#pragma unroll
-      for (int i = 0; i < QT; ++i) {
-        sum[i] += __shfl_xor(sum[i], 16, WAVE);
-        sum[i] += __shfl_xor(sum[i], 32, WAVE);
-        delta[i] = sum[i];
-        const long long t = tw + 16 * i + l16;
-        if (lg == 0 && t < u.hi) a.delta[(u.b + t) * a.H + h] = sum[i];
-      }
-    }
-    char *s_k = s_dyn + (step & 1) * 2 * TILE, *s_v = s_k + TILE;
-    char *s_next = s_dyn + (~step & 1) * 2 * TILE;
-    if (step == 0 || WIDE) {
+  for (int tile = 0; tile < sn.tiles; ++tile) {
+    char *s_k = s_dyn + (tile & 1) * 2 * TILE, *s_v = s_k + TILE;
+    char *s_next = s_dyn + (~tile & 1) * 2 * TILE;
+    if (tile == 0 || WIDE) {
       ck.finish(s_k);
       cv.finish(s_v);
     }
     __syncthreads();
-    const bool more = step + 1 < steps, sink = tile < sn.sink_tiles;
-    if (more) fetch(tile + 1 < sn.tiles ? tile + 1 : 0, s_next);
+    const bool more = tile + 1 < sn.tiles, sink = tile < sn.sink_tiles;
+    if (more) fetch(tile + 1, s_next);
     const long long s0 = start(tile);
     const bool none = !sink && (s0 > tw + 16 * QT - 1 ||
                                 (tw - (s0 + KEYS - 1) >= a.window && s0 >= a.sinks));
@@ -508,7 +488,7 @@ __global__ __launch_bounds__(WNT, MIN_WAVES<T>) void k_window_dq(WinArgs a) {
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
             const float e = exp2_of(fmaf(x[b][i][r], c, -lse[i]));
-            float d = sums ? e * y[b][i][r] : e * (y[b][i][r] - delta[i]) * up;
+            float d = SUMS ? e * y[b][i][r] : e * (y[b][i][r] - delta[i]) * up;
             if (!whole) {
               const long long t = tw + 16 * i + l16, s = s0 + 32 * t2 + 16 * b + 4 * lg + r;
               const bool sees = sink ? s < sn.sinks
@@ -516,11 +496,11 @@ __global__ __launch_bounds__(WNT, MIN_WAVES<T>) void k_window_dq(WinArgs a) {
               d = sees ? d : 0.0f;
             }
             x[b][i][r] = d;
-            sum[i] += d;
+            if constexpr (SUMS) sum[i] += d;
           }
         p[i] = pack<T>(x[0][i], x[1][i]);
       }
-      if (sums) continue;
+      if constexpr (SUMS) continue;
 #pragma unroll
       for (int d = 0; d < DT; ++d) {
         const Frag<T> f = Packed<T, P>::columns(s_k, 32 * t2, 16 * d, lane);
@@ -532,6 +512,16 @@ __global__ __launch_bounds__(WNT, MIN_WAVES<T>) void k_window_dq(WinArgs a) {
       ck.finish(s_next);
       cv.finish(s_next + TILE);
     }
+  }
+  if constexpr (SUMS) {
+#pragma unroll
+    for (int i = 0; i < QT; ++i) {
+      sum[i] += __shfl_xor(sum[i], 16, WAVE);
+      sum[i] += __shfl_xor(sum[i], 32, WAVE);
+      const long long t = tw + 16 * i + l16;
+      if (lg == 0 && t < u.hi) a.delta[(u.b + t) * a.H + h] = sum[i];
+    }
+    return;
   }
   const bool fine = finite(o);
   const float f = a.scale / up;
@@ -557,21 +547,36 @@ __global__ __launch_bounds__(WNT, MIN_WAVES<T>) void k_window_dq(WinArgs a) {
   }
 }
 
-// Gradients by keys and values: a workgroup has BLOCK keys of a key head, walks
-// the queries that see them through the window, head after head of its group,
-// and adds what the sinks' units found.
+// Whether the queries outside the window of a sequence's first frames are cut into
+// units: where there are more than one of them.
+__device__ __forceinline__ bool in_units(const WinArgs &a, const Unit &u) {
+  return a.sinks > 0 && u.len > a.window && u.len > a.unit;
+}
+// Sums [2][P] for a first frame of such a sequence: its block's own, and unit j's.
+// Such sequences are longer than a unit, so floor(b / unit) differs, and floor(2 b /
+// unit) by as much as they have units.
+__device__ __forceinline__ float *own_part(const WinArgs &a, const Unit &u, int g, int s, int P) {
+  return a.own + ((u.b / a.unit * a.G + g) * a.sinks + s) * 2 * P;
+}
+__device__ __forceinline__ float *unit_part(const WinArgs &a, const Unit &u, long long j, int g,
+                                            int s, int P) {
+  return a.part + (((2 * u.b / a.unit + j) * a.G + g) * a.sinks + s) * 2 * P;
+}
+
+// Gradients by keys and values: a workgroup has BLOCK keys of a key head and walks
+// the queries that see them, head after head of its group.
 template <typename T, int P, bool WIDE>
-__global__ __launch_bounds__(WNT, MIN_WAVES<T>) void k_window_dkv(WinArgs a) {
+__device__ __forceinline__ void dkv_block(const WinArgs &a, const Unit &u, int g, char *s_dyn) {
+  // s_dyn: [2][q, dy][TILE], v, lse and delta [2][2][QUERIES]
   constexpr int DT = P / 16, DS = P / 32, TILE = QUERIES * P * (int)sizeof(T);
-  extern __shared__ __attribute__((aligned(16))) char s_dyn[];  // [2][q, dy][TILE], v
-  __shared__ __attribute__((aligned(16))) float s_row[2][2][QUERIES];  // lse, delta
   char *s_v = s_dyn + 4 * TILE;
+  float *s_row = reinterpret_cast<float *>(s_v + BLOCK * P * (int)sizeof(T));
   const int lane = threadIdx.x & (WAVE - 1), l16 = lane & 15, lg = lane >> 4;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
-  const int g = blockIdx.y, E = a.H / a.G, D = a.D;
-  Unit u;
-  if (!unit_of(a.off, a.n, a.N, BLOCK, false, blockIdx.x, u) || u.lo >= u.hi) return;
-
+  const int E = a.H / a.G, D = a.D;
+  // first frames among the keys: their queries outside the window are units', or
+  // (short sequences) walked here too
+  const bool split = in_units(a, u), onward = u.lo < a.sinks && !split;
   const T *k = static_cast<const T *>(a.k) + u.b * a.ks + (long long)g * D;
   const T *v = static_cast<const T *>(a.v) + u.b * a.vs + (long long)g * D;
   const long long sw = u.lo + w * 16 * QT;  // the wavefront's first key
@@ -593,7 +598,8 @@ __global__ __launch_bounds__(WNT, MIN_WAVES<T>) void k_window_dkv(WinArgs a) {
   cv.finish(s_v);
   const float c = a.scale * LOG2E, up = ds_scale<T>(a);
   float4v ok[DT][QT] = {}, ov[DT][QT] = {};
-  const long long end = u.hi - 1 + a.window < u.len ? u.hi - 1 + a.window : u.len;
+  const long long end =
+      u.hi - 1 + a.window < u.len && !onward ? u.hi - 1 + a.window : u.len;
   const int tiles = (int)((end - u.lo + QUERIES - 1) / QUERIES), all = tiles * E;
   Carry<T, P, QUERIES, WNT, WIDE> cq, cg;
   cq.init(a.qs, D);
@@ -616,8 +622,8 @@ __global__ __launch_bounds__(WNT, MIN_WAVES<T>) void k_window_dkv(WinArgs a) {
     cq.finish(s_dyn + (j & 1) * 2 * TILE);
     cg.finish(s_dyn + (j & 1) * 2 * TILE + TILE);
     if (threadIdx.x < QUERIES) {
-      s_row[j & 1][0][threadIdx.x] = r_lse;
-      s_row[j & 1][1][threadIdx.x] = r_delta;
+      s_row[(j & 1) * 2 * QUERIES + threadIdx.x] = r_lse;
+      s_row[((j & 1) * 2 + 1) * QUERIES + threadIdx.x] = r_delta;
     }
   };
   int h = g * E, tile = 0;
@@ -625,13 +631,14 @@ __global__ __launch_bounds__(WNT, MIN_WAVES<T>) void k_window_dkv(WinArgs a) {
   finish(0);
   for (int j = 0; j < all; ++j) {
     const char *s_q = s_dyn + (j & 1) * 2 * TILE, *s_g = s_q + TILE;
-    const float *s_lse = s_row[j & 1][0], *s_delta = s_row[j & 1][1];
+    const float *s_lse = s_row + (j & 1) * 2 * QUERIES, *s_delta = s_lse + QUERIES;
     __syncthreads();
     const long long t0 = u.lo + (long long)tile * QUERIES;
     const bool more = j + 1 < all;
     if (++tile == tiles) tile = 0, ++h;
     if (more) fetch(h, tile, s_dyn + (~j & 1) * 2 * TILE);
-    const bool none = t0 + QUERIES - 1 < sw || t0 - (sw + 16 * QT - 1) >= a.window;
+    const bool none = t0 + QUERIES - 1 < sw || (t0 - (sw + 16 * QT - 1) >= a.window &&
+                                                !(onward && sw < a.sinks));
     const bool whole = t0 >= sw + 16 * QT - 1 && t0 + QUERIES - 1 - sw < a.window;
     if (!none) {
       float4v x[2][QT] = {}, y[2][QT] = {};
@@ -665,7 +672,8 @@ __global__ __launch_bounds__(WNT, MIN_WAVES<T>) void k_window_dkv(WinArgs a) {
             float d = e * (y[b][i][r] - delta[r]) * up;
             if (!whole) {
               const long long t = t0 + at + r, s = sw + 16 * i + l16;
-              const bool sees = s <= t && t - s < a.window && t < end;
+              const bool sees =
+                  s <= t && t < end && (t - s < a.window || (onward && s < a.sinks));
               e = sees ? e : 0.0f;
               d = sees && !sees_one(t, a.window, a.sinks) ? d : 0.0f;
             }
@@ -694,30 +702,23 @@ __global__ __launch_bounds__(WNT, MIN_WAVES<T>) void k_window_dkv(WinArgs a) {
   }
   const bool fine = finite(ok) && finite(ov);
   const float f = a.scale / up;
-  // what units of queries found that see a first frame from outside the window, in
-  // their order
-  const long long units = rows_before(u.b, u.s, a.unit);
-  const auto from_units = [&](long long s, int d, float4v &xk, float4v &xv) {
-    if (s >= a.sinks || u.len <= a.window) return;
-    const long long n = (u.len + a.unit - 1) / a.unit;
-    for (long long j = a.window / a.unit; j < n; ++j) {
-      const float *p = a.part + (((units + j) * a.G + g) * a.sinks + s) * 2 * P + d;
-      xk += *reinterpret_cast<const float4v *>(p);
-      xv += *reinterpret_cast<const float4v *>(p + P);
-    }
-  };
 #pragma unroll
   for (int i = 0; i < QT; ++i) {
     const long long s = sw + 16 * i + l16;
     if (s >= u.hi) continue;
     T *gk = static_cast<T *>(a.gk) + (u.b + s) * a.gks + (long long)g * D;
     T *gv = static_cast<T *>(a.gv) + (u.b + s) * a.gvs + (long long)g * D;
+    float *own = split && s < a.sinks ? own_part(a, u, g, (int)s, P) : nullptr;
 #pragma unroll
     for (int d = 0; d < DT; ++d) {
       ok[d][i] *= f;
-      from_units(s, 16 * d + 4 * lg, ok[d][i], ov[d][i]);
-      store_four<T, WIDE>(gk, 16 * d + 4 * lg, D, ok[d][i]);
-      store_four<T, WIDE>(gv, 16 * d + 4 * lg, D, ov[d][i]);
+      if (own) {
+        *reinterpret_cast<float4v *>(own + 16 * d + 4 * lg) = ok[d][i];
+        *reinterpret_cast<float4v *>(own + P + 16 * d + 4 * lg) = ov[d][i];
+      } else {
+        store_four<T, WIDE>(gk, 16 * d + 4 * lg, D, ok[d][i]);
+        store_four<T, WIDE>(gv, 16 * d + 4 * lg, D, ov[d][i]);
+      }
     }
   }
   if (fine) return;
@@ -727,9 +728,13 @@ __global__ __launch_bounds__(WNT, MIN_WAVES<T>) void k_window_dkv(WinArgs a) {
     if (s >= u.hi) continue;
     T *gk = static_cast<T *>(a.gk) + (u.b + s) * a.gks + (long long)g * D;
     T *gv = static_cast<T *>(a.gv) + (u.b + s) * a.gvs + (long long)g * D;
-    const long long t1 = s + a.window < u.len ? s + a.window : u.len;
+    float *own = split && s < a.sinks ? own_part(a, u, g, (int)s, P) : nullptr;
+    const long long t1 =
+        s + a.window < u.len && !(onward && s < a.sinks) ? s + a.window : u.len;
     for (int d = 4 * lg; d < D; d += 16) {
-      if (!none_of_four(gk, d, D) && !none_of_four(gv, d, D)) continue;
+      if (own ? !none_of_four(own, d, D) && !none_of_four(own + P, d, D)
+              : !none_of_four(gk, d, D) && !none_of_four(gv, d, D))
+        continue;
       float4v xk{}, xv{};
       for (int hh = g * E; hh < g * E + E; ++hh) {
         const T *qh = static_cast<const T *>(a.q) + u.b * a.qs + (long long)hh * D;
@@ -740,10 +745,13 @@ __global__ __launch_bounds__(WNT, MIN_WAVES<T>) void k_window_dkv(WinArgs a) {
         xk += x.k;
         xv += x.v;
       }
-      xk *= f;
-      from_units(s, d, xk, xv);
-      mend_four(gk, d, D, xk);
-      mend_four(gv, d, D, xv);
+      if (own) {
+        mend_four(own, d, D, xk * f);
+        mend_four(own + P, d, D, xv);
+      } else {
+        mend_four(gk, d, D, xk * f);
+        mend_four(gv, d, D, xv);
+      }
     }
   }
 }
@@ -753,17 +761,16 @@ __global__ __launch_bounds__(WNT, MIN_WAVES<T>) void k_window_dkv(WinArgs a) {
 // sums joined in LDS.  Rows of `part` of units without such a query are not
 // written, nor read.
 template <typename T, int P, bool WIDE>
-__global__ __launch_bounds__(WNT, MIN_WAVES<T>) void k_window_sinks(WinArgs a) {
+__device__ __forceinline__ void sinks_block(const WinArgs &a, const Unit &u, int g, int first,
+                                            char *s_dyn) {
   constexpr int Q = 32 * WNW, DT = P / 16, DS = P / 32;
-  extern __shared__ __attribute__((aligned(16))) char s_dyn[];
   T *s_q = reinterpret_cast<T *>(s_dyn), *s_g = s_q + Q * LD<T, P>;
   float *s_lse = reinterpret_cast<float *>(s_g + Q * LD<T, P>), *s_delta = s_lse + Q;
   const int lane = threadIdx.x & (WAVE - 1), l16 = lane & 15, lg = lane >> 4;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
-  const int g = blockIdx.y, E = a.H / a.G, D = a.D;
-  const long long s = (long long)blockIdx.z * 16 + l16;  // the lane's key
-  Unit u;
-  if (!unit_of(a.off, a.n, a.N, a.unit, false, blockIdx.x, u) || u.hi <= a.window) return;
+  const int E = a.H / a.G, D = a.D;
+  const long long s = first + l16;  // the lane's key
+  if (!in_units(a, u) || u.hi <= a.window) return;
 
   const T *k = static_cast<const T *>(a.k) + u.b * a.ks + (long long)g * D;
   const T *v = static_cast<const T *>(a.v) + u.b * a.vs + (long long)g * D;
@@ -877,11 +884,71 @@ __global__ __launch_bounds__(WNT, MIN_WAVES<T>) void k_window_sinks(WinArgs a) {
       float v = 0.0f;
 #pragma unroll
       for (int q = 0; q < WNW; ++q) v += s_sum[q * 16 * P + i];
-      const long long key = (long long)blockIdx.z * 16 + i / P;
+      const int key = first + i / P;
       if (key < a.sinks)
-        a.part[((((long long)blockIdx.x * a.G + g) * a.sinks + key) * 2 + o) * P + i % P] =
+        unit_part(a, u, u.lo / a.unit, g, key, P)[o * P + i % P] =
             o ? v : v * f;
     }
+  }
+}
+
+// Workgroups of all three: blocks of keys, blocks of queries, units for the first
+// frames.
+template <typename T, int P, bool WIDE>
+__global__ __launch_bounds__(WNT, MIN_WAVES<T>) void k_window_back(WinArgs a) {
+  extern __shared__ __attribute__((aligned(16))) char s_dyn[];
+  const long long blocks = a.N / BLOCK + a.n;
+  long long id = (long long)blockIdx.y * gridDim.x + blockIdx.x;
+  Unit u;
+  if (id < blocks * a.G) {
+    if (unit_of(a.off, a.n, a.N, BLOCK, false, id % blocks, u) && u.lo < u.hi)
+      dkv_block<T, P, WIDE>(a, u, (int)(id / blocks), s_dyn);
+    return;
+  }
+  id -= blocks * a.G;
+  if (id < blocks * a.H) {
+    if (unit_of(a.off, a.n, a.N, BLOCK, false, id % blocks, u) && u.lo < u.hi)
+      dq_block<T, P, WIDE, false>(a, u, (int)(id / blocks), s_dyn);
+    return;
+  }
+  id -= blocks * a.H;
+  const long long units = a.N / a.unit + a.n, part = id / units;
+  if (part < (long long)a.G * ((a.sinks + 15) / 16) &&
+      unit_of(a.off, a.n, a.N, a.unit, false, id % units, u) && u.lo < u.hi)
+    sinks_block<T, P, WIDE>(a, u, (int)(part % a.G), (int)(part / a.G) * 16, s_dyn);
+}
+
+// delta from y as it was rounded is off by half a spacing of y, which is next to
+// nothing beside dS of many frames but as much as the rounding of dS beside few:
+// queries of a sequence's first block, and of windows up to FEW frames, have it
+// summed again from P and dy v^T.
+template <typename T, int P, bool WIDE>
+__global__ __launch_bounds__(WNT, MIN_WAVES<T>) void k_window_sums(WinArgs a, int every) {
+  extern __shared__ __attribute__((aligned(16))) char s_dyn[];
+  Unit u;
+  if (!unit_of(a.off, a.n, a.N, every ? BLOCK : 0, false, blockIdx.x, u)) return;
+  if (u.hi > u.lo + BLOCK) u.hi = u.lo + BLOCK;
+  if (u.lo < u.hi) dq_block<T, P, WIDE, true>(a, u, blockIdx.y, s_dyn);
+}
+
+// Gradients of first frames whose sums lie in parts: their own, then the units'.
+template <typename T, int P>
+__global__ __launch_bounds__(P) void k_window_first(WinArgs a) {
+  Unit u;
+  if (!unit_of(a.off, a.n, a.N, 0, false, blockIdx.x, u) || !in_units(a, u)) return;
+  const int d = threadIdx.x, g = blockIdx.y;
+  if (d >= a.D) return;
+  const long long n = (u.len + a.unit - 1) / a.unit;
+  for (int s = blockIdx.z; s < a.sinks && s < u.len; s += gridDim.z) {
+    const float *own = own_part(a, u, g, s, P);
+    float k = own[d], v = own[P + d];
+    for (long long j = a.window / a.unit; j < n; ++j) {
+      const float *p = unit_part(a, u, j, g, s, P);
+      k += p[d];
+      v += p[P + d];
+    }
+    static_cast<T *>(a.gk)[(u.b + s) * a.gks + (long long)g * a.D + d] = (T)k;
+    static_cast<T *>(a.gv)[(u.b + s) * a.gvs + (long long)g * a.D + d] = (T)v;
   }
 }
 
@@ -1099,59 +1166,65 @@ bool wide_rows(size_t e, int D, std::initializer_list<long long> strides,
   return true;
 }
 
-dim3 blocks(const WinArgs &a, long long per, int across) {
-  return dim3((unsigned)(a.N / per + a.n), across);
-}
-
-// LDS of the walks over tiles of 64 rows: two pairs of them.
+// LDS of a walk over keys: two pairs of tiles; over queries: two pairs of smaller
+// ones, a block of v, their rows' numbers; of a unit's queries.
 template <typename T, int P>
 constexpr int WALK = 4 * KEYS * P * (int)sizeof(T);
+template <typename T, int P>
+constexpr int WALK_BACK = (4 * QUERIES + BLOCK) * P * (int)sizeof(T) + 4 * QUERIES * 4;
+template <typename T, int P>
+constexpr int WALK_UNIT = 2 * BYTES<T, P, 32 * WNW> + 2 * 32 * WNW * 4;
+static_assert(WALK<float, 128> <= 160 * 1024 && WALK_BACK<float, 128> <= 160 * 1024 &&
+                  WALK_UNIT<float, 128> <= 160 * 1024,
+              "LDS of a CU");
 
 hipError_t allow_lds(const void *kernel, int lds) {
   if (lds <= 64 * 1024) return hipSuccess;
   return hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
 }
-// and of the walk over queries: two pairs of 32 rows, and a block of v.
-template <typename T, int P>
-constexpr int WALK_KEYS = (4 * QUERIES + BLOCK) * P * (int)sizeof(T);
 
-hipError_t walk(void (*kernel)(WinArgs), int lds, int across, const WinArgs &a, hipStream_t s) {
-  const hipError_t e = allow_lds(reinterpret_cast<const void *>(kernel), lds);
-  if (e != hipSuccess) return e;
-  kernel<<<blocks(a, BLOCK, across), WNT, lds, s>>>(a);
-  return hipGetLastError();
-}
-static_assert(WALK<float, 128> <= 150 * 1024 && WALK_KEYS<float, 128> <= 150 * 1024,
-              "LDS of a CU");
+constexpr int MAX_ACROSS = 65535;           // of a grid's second and third dimension
+constexpr long long MAX_BLOCKS = 1 << 23;   // and of its first
 
 template <typename T, int P, bool WIDE>
 hipError_t forward_as(const WinArgs &a, hipStream_t s) {
-  return walk(k_window<T, P, WIDE>, WALK<T, P>, a.H, a, s);
-}
-
-template <typename T, int P, bool WIDE>
-hipError_t sinks_as(const WinArgs &a, hipStream_t s) {
-  constexpr int Q = 32 * WNW;
-  constexpr int lds = 2 * BYTES<T, P, Q> + 2 * Q * (int)sizeof(float);
-  static_assert(lds <= 160 * 1024, "LDS of a CU");
-  dim3 grid = blocks(a, a.unit, a.G);
-  grid.z = (a.sinks + 15) / 16;
-  if (grid.z > 65535) return hipErrorInvalidValue;
-  const hipError_t e = allow_lds(reinterpret_cast<const void *>(k_window_sinks<T, P, WIDE>), lds);
+  constexpr int lds = WALK<T, P>;
+  if (a.N / BLOCK + a.n > MAX_BLOCKS) return hipErrorInvalidValue;
+  const hipError_t e = allow_lds(reinterpret_cast<const void *>(k_window<T, P, WIDE>), lds);
   if (e != hipSuccess) return e;
-  k_window_sinks<T, P, WIDE><<<grid, WNT, lds, s>>>(a);
+  k_window<T, P, WIDE><<<dim3((unsigned)(a.N / BLOCK + a.n), a.H), WNT, lds, s>>>(a);
   return hipGetLastError();
 }
 
 template <typename T, int P, bool WIDE>
 hipError_t backward_as(const WinArgs &a, hipStream_t s) {
+  const long long blocks = a.N / BLOCK + a.n;
   if (a.most) k_window_zero<<<1, 2, 0, s>>>(a.most);
   const long long rows = (a.N * a.H + WNT / 16 - 1) / (WNT / 16);
   k_window_delta<T><<<(unsigned)(rows < 4096 ? rows : 4096), WNT, 0, s>>>(a);
-  hipError_t e = walk(k_window_dq<T, P, WIDE>, WALK<T, P>, a.H, a, s);
-  if (e == hipSuccess && a.part) e = sinks_as<T, P, WIDE>(a, s);
-  if (e == hipSuccess) e = walk(k_window_dkv<T, P, WIDE>, WALK_KEYS<T, P>, a.G, a, s);
-  return e;
+  if constexpr (sizeof(T) == 2) {
+    constexpr int lds = WALK<T, P>;
+    const hipError_t e =
+        allow_lds(reinterpret_cast<const void *>(k_window_sums<T, P, WIDE>), lds);
+    if (e != hipSuccess) return e;
+    const int every = a.window + a.sinks <= FEW;
+    k_window_sums<T, P, WIDE>
+        <<<dim3((unsigned)(every ? blocks : a.n), a.H), WNT, lds, s>>>(a, every);
+  }
+  const long long pieces = a.part ? (a.N / a.unit + a.n) * a.G * ((a.sinks + 15) / 16) : 0;
+  const long long all = blocks * (a.G + a.H) + pieces;
+  const long long across = all < MAX_BLOCKS ? all : MAX_BLOCKS;
+  if (blocks > MAX_BLOCKS || all > across * MAX_ACROSS) return hipErrorInvalidValue;
+  constexpr int keys = WALK<T, P> > WALK_BACK<T, P> ? WALK<T, P> : WALK_BACK<T, P>;
+  const int lds = pieces && WALK_UNIT<T, P> > keys ? WALK_UNIT<T, P> : keys;
+  const hipError_t e = allow_lds(reinterpret_cast<const void *>(k_window_back<T, P, WIDE>), lds);
+  if (e != hipSuccess) return e;
+  k_window_back<T, P, WIDE>
+      <<<dim3((unsigned)across, (unsigned)((all + across - 1) / across)), WNT, lds, s>>>(a);
+  if (a.part)
+    k_window_first<T, P>
+        <<<dim3(a.n, a.G, a.sinks < 1024 ? a.sinks : 1024), P, 0, s>>>(a);
+  return hipGetLastError();
 }
 
 template <typename T, int P, bool WIDE>
@@ -1180,8 +1253,6 @@ hipError_t step_as(const WinStepArgs &a, hipStream_t s) {
 
 int padded(int D) { return D <= 64 ? 64 : 128; }
 
-constexpr int MAX_ACROSS = 65535;  // of a grid's second and third dimension
-
 }  // namespace
 
 hipError_t launch_window(const WinArgs &a, int type, hipStream_t s) {
@@ -1196,18 +1267,19 @@ hipError_t launch_window_grads(WinArgs a, int type, void *ws, size_t *need, hipS
   if (a.H > MAX_ACROSS) return hipErrorInvalidValue;
   const int D = a.D;
   const size_t delta = ((size_t)a.N * a.H + 3) / 4 * 4;
-  // (a sequence has to be longer than the window for its first frames to be seen
-  // from outside it)
-  const bool sinks = a.sinks > 0 && a.N > a.window;
+  // (a sequence has to be longer than the window, and than a unit, for the queries of
+  // its first frames to be cut)
   a.unit = 512;
-  const size_t part =
-      sinks ? (size_t)(a.N / a.unit + a.n) * a.G * a.sinks * 2 * padded(D) : 0;
-  *need = (4 + delta + part) * sizeof(float);
+  const bool cut = a.sinks > 0 && a.N > a.window && a.N > a.unit;
+  const size_t first = cut ? (size_t)a.G * a.sinks * 2 * padded(D) : 0;
+  const size_t own = (a.N / a.unit + 1) * first, part = (2 * a.N / a.unit + 1) * first;
+  *need = (4 + delta + own + part) * sizeof(float);
   if (!ws) return hipSuccess;
   float *p = static_cast<float *>(ws);
   a.most = type == FST_F16 ? reinterpret_cast<uint32_t *>(p) : nullptr;
   a.delta = p + 4;
-  a.part = sinks ? p + 4 + delta : nullptr;
+  a.own = p + 4 + delta;
+  a.part = cut ? a.own + own : nullptr;
   const bool wide = wide_rows(type_bytes(type), D, {a.qs, a.ks, a.vs, a.gys, a.gqs, a.gks, a.gvs},
                               {a.q, a.k, a.v, a.gy, a.gq, a.gk, a.gv});
   return FOR_FORM(backward_as, a, s);
