@@ -540,8 +540,8 @@ FST_API int fst_recurrence_step(fst_ctx *ctx, const fst_matrix *x, const fst_mat
  * NaN in rows that they do see make no number of them, as the formulas do. */
 #define FST_NORM_MAX_WIDTH 512      /* columns of a head of fst_head_norms     */
 #define FST_ATTENTION_MAX_WIDTH 128 /* of the attentions (FST_ERR_TOO_LARGE),  */
-                                    /* which take at most 65,535 heads, 32,767 */
-                                    /* of more than 64 columns                 */
+                                    /* which take at most 16,383 heads, and    */
+                                    /* rows up to 2^22 numbers apart           */
 
 /* Queries and keys normalised head by head, scaled, and rotated by position.
  * For each head x of a row, of `width` columns, with one of the two weights

@@ -25,9 +25,13 @@ using namespace tile;
 namespace {
 
 constexpr int CHUNK = 64;   // rows that are multiplied at once, 16 of them by a wavefront
-constexpr int SLICE = 64;   // columns of v that four wavefronts take
+// Columns of v that four wavefronts take.  float32's products take eight times as
+// long, and half the columns leave them twice the workgroups (6 x 211 x 5 heads of 41
+// and 57, with gradients: 71 us with 64).
+template <typename T>
+constexpr int SLICE_OF = sizeof(T) == 2 ? 64 : 32;
 constexpr int LNT = 256;    // threads of a step
-static_assert(CHUNK == 16 * 4 && SLICE == 64, "a wavefront has 16 rows and four tiles of v");
+static_assert(CHUNK == 16 * 4, "a wavefront has 16 rows");
 
 // e^(g n) for 0 <= n <= CHUNK, from 64 bits: chunk after chunk multiplies them.
 // (A head that keeps nothing has g = -inf, and e^(0 g) = 1 all the same.)
@@ -37,10 +41,11 @@ __device__ __forceinline__ double power_of(float g, int n) {
 }
 
 // Whether all of a wavefront's results are numbers.
-__device__ __forceinline__ bool finite(const float4v (&x)[4]) {
+template <int N>
+__device__ __forceinline__ bool finite(const float4v (&x)[N]) {
   float z = 0.0f;
 #pragma unroll
-  for (int j = 0; j < 4; ++j)
+  for (int j = 0; j < N; ++j)
 #pragma unroll
     for (int r = 0; r < 4; ++r) z = fmaf(x[j][r], 0.0f, z);
   return __all(z == 0.0f);
@@ -54,7 +59,7 @@ template <typename T, int PA, int PB>
 __device__ __noinline__ void exact_rows(T *o, int left, const T *s_q, const T *s_k, const T *s_v,
                                         const T *s_s, const float *s_pow, int i, int A, int lg,
                                         float f_past, float f_now) {
-  for (int c = 4 * lg; c < SLICE; c += 16) {
+  for (int c = 4 * lg; c < SLICE_OF<T>; c += 16) {
     if (!none_of_four(o, c, left)) continue;
     float4v past{}, now{};
     for (int d = 0; d < A; ++d)
@@ -100,7 +105,7 @@ __device__ __forceinline__ float largest(const float (&m)[NW][4], int c) {
 template <typename T, int PA, int CG, bool WIDE, bool FULL>
 __global__ __launch_bounds__(256 * CG, CG == 2 ? 2 : sizeof(T) == 2 && PA == 64 ? 3 : 1) void k_linear(LinArgs a) {
   static_assert(PA % 64 == 0, "whole tiles for four wavefronts");
-  constexpr int NTH = 256 * CG, NW = 4 * CG, PB = SLICE * CG;
+  constexpr int NTH = 256 * CG, NW = 4 * CG, SLICE = SLICE_OF<T>, NJ = SLICE / 16, PB = SLICE * CG;
   constexpr int MT = PA / 64;  // tiles of 16 rows of the state, a wavefront
   constexpr bool SCALED = std::is_same<T, f16>::value;
   // numbers of T that hold 24 bits of a decayed k
@@ -133,7 +138,7 @@ __global__ __launch_bounds__(256 * CG, CG == 2 ? 2 : sizeof(T) == 2 && PA == 64 
   }
 
   // the state: rows (wr MT + m) 16 + 4 lg + r, columns c0 + 16 j + l16
-  float4v S[MT][4];
+  float4v S[MT][NJ];
   const long long AB = (long long)A * B;
   const int row0 = wr * MT * 16 + 4 * lg;
   float *unit_state =
@@ -145,7 +150,7 @@ __global__ __launch_bounds__(256 * CG, CG == 2 ? 2 : sizeof(T) == 2 && PA == 64 
 #pragma unroll
   for (int m = 0; m < MT; ++m)
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
+    for (int j = 0; j < NJ; ++j)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         const int ra = row0 + 16 * m + r, cb = c0 + 16 * j + l16;
@@ -158,7 +163,7 @@ __global__ __launch_bounds__(256 * CG, CG == 2 ? 2 : sizeof(T) == 2 && PA == 64 
 #pragma unroll
     for (int m = 0; m < MT; ++m)
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
+      for (int j = 0; j < NJ; ++j)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           const float x = fabsf(S[m][j][r]);
@@ -212,7 +217,7 @@ __global__ __launch_bounds__(256 * CG, CG == 2 ? 2 : sizeof(T) == 2 && PA == 64 
 #pragma unroll
       for (int m = 0; m < MT; ++m)
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
+        for (int j = 0; j < NJ; ++j)
           store_four<T, true>(s_s + (c0 + 16 * j + l16) * LD<T, PA>, row0 + 16 * m, PA,
                               S[m][j] * s_scale);
     }
@@ -236,12 +241,12 @@ __global__ __launch_bounds__(256 * CG, CG == 2 ? 2 : sizeof(T) == 2 && PA == 64 
       bound = fmaf(keep, bound, most * fabsf(job.sk) * CHUNK * top[1] * top[2]);
     }
     if constexpr (FULL) {
-      float4v past[4] = {}, now[4] = {};
+      float4v past[NJ] = {}, now[NJ] = {};
       Frag<T> qf[PA / 32];
 #pragma unroll
       for (int s = 0; s < PA / 32; ++s) qf[s] = rows<T, PA>(s_q, 16 * wr, 32 * s, lane);
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
+      for (int j = 0; j < NJ; ++j)
 #pragma unroll
         for (int s = 0; s < PA / 32; ++s)
           past[j] = mac(rows<T, PA>(s_s, c0 + 16 * j, 32 * s, lane), qf[s], past[j]);
@@ -264,7 +269,7 @@ __global__ __launch_bounds__(256 * CG, CG == 2 ? 2 : sizeof(T) == 2 && PA == 64 
         }
         const Frag<T> p = pack<T>(x[0], x[1]);
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
+        for (int j = 0; j < NJ; ++j)
           now[j] = mac(columns<T, PB>(s_v, 32 * t, c0 + 16 * j, lane), p, now[j]);
       }
       const bool fine = finite(now);
@@ -273,7 +278,7 @@ __global__ __launch_bounds__(256 * CG, CG == 2 ? 2 : sizeof(T) == 2 && PA == 64 
                (long long)h * B + b0;
         const float f = job.ss * over / s_scale, f2 = job.so / p_scale;
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
+        for (int j = 0; j < NJ; ++j)
           store_four<T, WIDE>(o, c0 + 16 * j + 4 * lg, left, past[j] * f + now[j] * f2);
         if (!fine)
           exact_rows<T, PA, PB>(o + c0, left - c0, s_q, s_k, s_v + c0, s_s + c0 * LD<T, PA>, s_pow,
@@ -286,7 +291,7 @@ __global__ __launch_bounds__(256 * CG, CG == 2 ? 2 : sizeof(T) == 2 && PA == 64 
 #pragma unroll
       for (int m = 0; m < MT; ++m)
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
+        for (int j = 0; j < NJ; ++j)
 #pragma unroll
           for (int r = 0; r < 4; ++r)
             S[m][j][r] = fmaf(kh, S[m][j][r], kl * S[m][j][r]) * k_scale;
@@ -295,9 +300,9 @@ __global__ __launch_bounds__(256 * CG, CG == 2 ? 2 : sizeof(T) == 2 && PA == 64 
       const int terms = !FULL || job.last ? TERMS : TERMS < 2 ? TERMS : 2;
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
-        Frag<T> vf[4];
+        Frag<T> vf[NJ];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) vf[j] = columns<T, PB>(s_v, 32 * t, c0 + 16 * j, lane);
+        for (int j = 0; j < NJ; ++j) vf[j] = columns<T, PB>(s_v, 32 * t, c0 + 16 * j, lane);
         float f[8];
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
@@ -326,7 +331,7 @@ __global__ __launch_bounds__(256 * CG, CG == 2 ? 2 : sizeof(T) == 2 && PA == 64 
             // multiplied, where the compiler might round x for each in its own way)
             if constexpr (TERMS > 1) asm("" : "+v"(part.v[0]));
 #pragma unroll
-            for (int j = 0; j < 4; ++j) S[m][j] = mac(part, vf[j], S[m][j]);
+            for (int j = 0; j < NJ; ++j) S[m][j] = mac(part, vf[j], S[m][j]);
             if (c + 1 < TERMS) {
               unpack(part, y);
 #pragma unroll
@@ -340,7 +345,7 @@ __global__ __launch_bounds__(256 * CG, CG == 2 ? 2 : sizeof(T) == 2 && PA == 64 
 #pragma unroll
         for (int m = 0; m < MT; ++m)
 #pragma unroll
-          for (int j = 0; j < 4; ++j) S[m][j] *= back;
+          for (int j = 0; j < NJ; ++j) S[m][j] *= back;
       }
     }
     __syncthreads();
@@ -352,7 +357,7 @@ __global__ __launch_bounds__(256 * CG, CG == 2 ? 2 : sizeof(T) == 2 && PA == 64 
 #pragma unroll
   for (int m = 0; m < MT; ++m)
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
+    for (int j = 0; j < NJ; ++j)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         const int ra = row0 + 16 * m + r, cb = c0 + 16 * j + l16;
@@ -457,7 +462,7 @@ unsigned units_of(const LinArgs &a) { return (unsigned)(a.unit ? a.N / a.unit + 
 
 template <typename T, int PA, int CG, bool WIDE, bool FULL>
 hipError_t launch_as(const LinArgs &a, int jobs, hipStream_t s) {
-  constexpr int PB = SLICE * CG;
+  constexpr int PB = SLICE_OF<T> * CG;
   constexpr int lds = BYTES<T, PA, CHUNK> + BYTES<T, PB, CHUNK> +
                       (FULL ? BYTES<T, PA, CHUNK> + BYTES<T, PA, PB> : 0);
   static_assert(lds <= 150 * 1024, "LDS of a CU");
@@ -473,9 +478,8 @@ hipError_t launch_as(const LinArgs &a, int jobs, hipStream_t s) {
 }
 template <typename T, int PA, bool WIDE, bool FULL>
 hipError_t launch_by_columns(const LinArgs &a, int jobs, int B, hipStream_t s) {
-  // (float32 tiles of 128 by 128 would not fit)
   if constexpr (sizeof(T) == 2) {
-    if (B > SLICE) return launch_as<T, PA, 2, WIDE, FULL>(a, jobs, s);
+    if (B > SLICE_OF<T>) return launch_as<T, PA, 2, WIDE, FULL>(a, jobs, s);
   }
   return launch_as<T, PA, 1, WIDE, FULL>(a, jobs, s);
 }
@@ -489,7 +493,10 @@ hipError_t launch_jobs(const LinArgs &a, int jobs, int A, int B, bool wide, hipS
 }
 
 // Columns of v of a workgroup.
-int slice_of(int type, int B) { return type != FST_F32 && B > SLICE ? 2 * SLICE : SLICE; }
+int slice_of(int type, int B) {
+  if (type == FST_F32) return SLICE_OF<float>;
+  return B > SLICE_OF<bf16> ? 2 * SLICE_OF<bf16> : SLICE_OF<bf16>;
+}
 
 // Jobs [lo, hi) of `all`, which have one width of q and k (or widths up to 64).
 template <bool FULL>
@@ -552,16 +559,18 @@ hipError_t launch_states(const LinArgs &a, const LinJob *all, int jobs, int type
 
 constexpr long long MAX_ACROSS = 65535;  // of a grid's second dimension
 
-bool too_wide(const LinCall &c) {
+bool too_large(const LinCall &c) {
   const int most = c.K > c.V ? c.K : c.V;
-  return (long long)c.H * ((most + SLICE - 1) / SLICE) > MAX_ACROSS;
+  for (long long t : {c.qs, c.ks, c.vs})
+    if (t > MAX_STRIDE) return true;
+  return (long long)c.H * ((most + SLICE_OF<float> - 1) / SLICE_OF<float>) > MAX_ACROSS;
 }
 
 }  // namespace
 
 // (also without workspace: then `need` is all that is set)
 hipError_t launch_linear(const LinCall &c, int type, void *ws, size_t *need, hipStream_t s) {
-  if (too_wide(c)) return hipErrorInvalidValue;
+  if (too_large(c)) return hipErrorInvalidValue;
   const size_t e = type_bytes(type);
   const long long unit = unit_steps(c, type, 1);
   *need = unit ? (size_t)(c.N / unit + c.n) * c.H * c.K * c.V * sizeof(float) : 0;
@@ -579,7 +588,7 @@ hipError_t launch_linear(const LinCall &c, int type, void *ws, size_t *need, hip
 
 hipError_t launch_linear_grads(const LinCall &c, int type, void *ws, size_t *need,
                                hipStream_t s) {
-  if (too_wide(c)) return hipErrorInvalidValue;
+  if (too_large(c) || c.ys > MAX_STRIDE) return hipErrorInvalidValue;
   const size_t e = type_bytes(type);
   const long long unit = unit_steps(c, type, 3);
   const size_t states = unit ? (size_t)(c.N / unit + c.n) * c.H * c.K * c.V : 0;

@@ -123,27 +123,45 @@ __device__ __forceinline__ Frag<T> columns(const T *t, int row, int col, int lan
   return f;
 }
 
-// 16 bytes from number c on of a row of `width`, zeros past its end; WIDE: the
-// width is a multiple of them and the row begins at one.
+// 16 bytes from number c on of a row of `width`, zeros past its end or where the row
+// is not there; WIDE: the width is a multiple of them and the row begins at one.
+// Otherwise every number is read by itself, all of them at once: one that is not
+// there reads the first of `safe` instead.
 template <typename T, bool WIDE>
-__device__ __forceinline__ int4v load_group(const T *row, int c, int width, bool there) {
+__device__ __forceinline__ int4v load_group(const T *row, int c, int width, bool there,
+                                            const T *safe) {
   int4v v{0, 0, 0, 0};
   if constexpr (WIDE) {
     if (there && c < width) v = *reinterpret_cast<const int4v *>(row + c);
   } else {
     struct alignas(16) { T v[PER<T>]; } e;
-    __builtin_memcpy(&e, &v, 16);
-    if (there) {
 #pragma unroll
-      for (int i = 0; i < PER<T>; ++i)
-        if (c + i < width) e.v[i] = row[c + i];
-    }
+    for (int i = 0; i < PER<T>; ++i) e.v[i] = *(there && c + i < width ? row + c + i : safe);
+#pragma unroll
+    for (int i = 0; i < PER<T>; ++i) e.v[i] = there && c + i < width ? e.v[i] : (T)0.0f;
     __builtin_memcpy(&v, &e, 16);
   }
   return v;
 }
 
-// A tile of R rows of P numbers on its way from memory to LDS, by NTH threads.
+// The number at a byte offset of a buffer, 0 past its end.
+template <typename T>
+__device__ __forceinline__ T load_number(__amdgpu_buffer_rsrc_t buffer, int at) {
+  if constexpr (sizeof(T) == 2)
+    return __builtin_bit_cast(
+        T, (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(buffer, at, 0, 0));
+  else
+    return __builtin_bit_cast(T, __builtin_amdgcn_raw_buffer_load_b32(buffer, at, 0, 0));
+}
+
+// Row strides up to MAX_STRIDE keep 32-bit byte offsets within a tile of up to 128
+// rows below PAST_END, an offset that is past any tile's end.
+constexpr long long MAX_STRIDE = 1ll << 22;
+constexpr int PAST_END = INT32_MIN;  // (as a number without a sign)
+
+// A tile of R rows of P numbers on its way from memory to LDS, by NTH threads: by 16
+// bytes (WIDE) or number by number, through a buffer, which gives zeros past its
+// end without a branch.
 template <typename T, int P, int R, int NTH, bool WIDE>
 struct Stage {
   static constexpr int GROUPS = P / PER<T>;  // of a row
@@ -151,13 +169,31 @@ struct Stage {
   static_assert(LOADS >= 1 && LOADS * NTH == R * GROUPS, "whole loads");
   int4v v[LOADS];
 
-  // row i of the tile is row first + i * step of the matrix, if i < count
+  // row i of the tile is row first + i * step of the matrix (step 1 or -1), if i <
+  // count (1 or more)
   __device__ __forceinline__ void fetch(const T *p, long long stride, int width, long long first,
                                         long long step, int count) {
+    const long long low = step < 0 ? first - (count - 1) : first;
+    const __amdgpu_buffer_rsrc_t buffer = __builtin_amdgcn_make_buffer_rsrc(
+        const_cast<T *>(p + low * stride), 0,
+        (int)(((count - 1) * stride + width) * (long long)sizeof(T)), 0x00027000);
+    const int row = (int)(stride * (long long)sizeof(T));
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) {
       const int q = i * NTH + (int)threadIdx.x, r = q / GROUPS, c = q % GROUPS * PER<T>;
-      v[i] = load_group<T, WIDE>(p + (first + r * step) * stride, c, width, r < count);
+      // (before the first row: past the end, as a number without a sign)
+      const int at = (step < 0 ? count - 1 - r : r) * row + c * (int)sizeof(T);
+      if constexpr (WIDE) {
+        v[i] = __builtin_bit_cast(int4v, __builtin_amdgcn_raw_buffer_load_b128(
+                                             buffer, c < width ? at : PAST_END, 0, 0));
+      } else {
+        struct alignas(16) { T v[PER<T>]; } e;
+#pragma unroll
+        for (int j = 0; j < PER<T>; ++j)
+          e.v[j] =
+              load_number<T>(buffer, c + j < width ? at + j * (int)sizeof(T) : PAST_END);
+        __builtin_memcpy(&v[i], &e, 16);
+      }
     }
   }
   __device__ __forceinline__ void store(T *t) const {
@@ -249,18 +285,14 @@ __device__ __forceinline__ void load_lds(uint32_t lds, uint32_t offset, int4v bu
 #pragma clang diagnostic pop
 __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(0)" : : : "memory"); }
 
-// Bytes that 32-bit offsets into a tile of rows reach, at most.
-constexpr long long MAX_TILE_BYTES = 1ll << 31;
-
 // A packed tile of R rows on its way from memory, by NTH threads; WIDE: straight to
-// LDS (rows whole 16-byte groups, and the tile's rows within MAX_TILE_BYTES),
-// otherwise through registers, element by element.
+// LDS, otherwise through registers, number by number.
 template <typename T, int P, int R, int NTH, bool WIDE>
 struct Carry {
   static constexpr int GROUPS = P / PER<T>;
   static constexpr int LOADS = R * GROUPS / NTH;
   static_assert(LOADS >= 1 && LOADS * NTH == R * GROUPS, "whole loads");
-  uint32_t off[WIDE ? LOADS : 1];
+  int off[LOADS];
   int4v v[WIDE ? 1 : LOADS];
 
   // (row, group of it) of load i: lanes write 1,024 bytes in their order
@@ -272,36 +304,37 @@ struct Carry {
     return q % GROUPS ^ Packed<T, P>::swizzle(row_of(i));
   }
   __device__ __forceinline__ void init(long long stride, int width) {
-    if constexpr (WIDE) {
 #pragma unroll
-      for (int i = 0; i < LOADS; ++i) {
-        const int c = group_of(i) * PER<T>;
-        // (past any buffer where the row has ended)
-        off[i] = c < width ? (uint32_t)((row_of(i) * stride + c) * (long long)sizeof(T))
-                           : (uint32_t)MAX_TILE_BYTES;
-      }
+    for (int i = 0; i < LOADS; ++i) {
+      const int c = group_of(i) * PER<T>;
+      off[i] = c < width ? (int)((row_of(i) * stride + c) * (long long)sizeof(T)) : PAST_END;
     }
   }
   // rows first .. first + count of a matrix (all arguments the same in every lane)
   __device__ __forceinline__ void fetch(const T *p, long long stride, int width, long long first,
                                         int count, char *to) {
+    const uint32_t n =
+        count > 0 ? (uint32_t)(((count - 1) * stride + width) * (long long)sizeof(T)) : 0u;
     if constexpr (WIDE) {
       const unsigned long long q = (unsigned long long)(uintptr_t)(p + first * stride);
-      const uint32_t n =
-          count > 0 ? (uint32_t)(((count - 1) * stride + width) * (long long)sizeof(T)) : 0u;
       const int4v buffer{__builtin_amdgcn_readfirstlane((int)(uint32_t)q),
                          __builtin_amdgcn_readfirstlane((int)(uint32_t)(q >> 32)),
                          __builtin_amdgcn_readfirstlane((int)n), 0x00027000};
       const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)to +
                            threadIdx.x / WAVE * LOADS * 1024;
 #pragma unroll
-      for (int i = 0; i < LOADS; ++i) load_lds(lds + i * 1024, off[i], buffer);
+      for (int i = 0; i < LOADS; ++i) load_lds(lds + i * 1024, (uint32_t)off[i], buffer);
     } else {
+      const __amdgpu_buffer_rsrc_t buffer = __builtin_amdgcn_make_buffer_rsrc(
+          const_cast<T *>(p + first * stride), 0, (int)n, 0x00027000);
 #pragma unroll
       for (int i = 0; i < LOADS; ++i) {
-        const int r = row_of(i);
-        v[i] = load_group<T, false>(p + (first + r) * stride, group_of(i) * PER<T>, width,
-                                    r < count);
+        const int c = group_of(i) * PER<T>;
+        struct alignas(16) { T v[PER<T>]; } e;
+#pragma unroll
+        for (int j = 0; j < PER<T>; ++j)
+          e.v[j] = load_number<T>(buffer, c + j < width ? off[i] + j * (int)sizeof(T) : PAST_END);
+        __builtin_memcpy(&v[i], &e, 16);
       }
     }
   }

@@ -31,8 +31,13 @@ constexpr int WNT = 256;             // threads
 constexpr int WNW = WNT / WAVE;
 constexpr int KEYS = 64;             // of a tile of keys
 constexpr int QUERIES = 32;          // of a tile of queries
-constexpr int QT = 2;                // tiles of 16 queries (or keys) of a wavefront
-constexpr int BLOCK = 16 * QT * WNW; // queries, or keys, of a workgroup
+// Tiles of 16 queries (or keys) of a wavefront.  Two read half as much of LDS for a
+// product; float32's products take eight times as long, and one leaves it more
+// workgroups (6 x 211 x 6 heads of 43, gradients: 146 us with two).
+template <typename T>
+constexpr int QT_OF = sizeof(T) == 2 ? 2 : 1;
+template <typename T>
+constexpr int BLOCK_OF = 16 * QT_OF<T> * WNW;  // queries, or keys, of a workgroup
 constexpr int FEW = 64;              // frames
 constexpr float LOG2 = 0.69314718055994530942f, LOG2E = 1.44269502162933349609375f;
 
@@ -119,14 +124,14 @@ __device__ __noinline__ float4v exact_row(const T *q, const T *k, long long ks, 
 // most tiles leave the sums as they are; p stays below 2^LATE.
 template <typename T, int P, bool WIDE>
 __global__ __launch_bounds__(WNT, MIN_WAVES<T>) void k_window(WinArgs a) {
-  constexpr int DT = P / 16, DS = P / 32, TILE = KEYS * P * (int)sizeof(T);
+  constexpr int QT = QT_OF<T>, DT = P / 16, DS = P / 32, TILE = KEYS * P * (int)sizeof(T);
   constexpr float LATE = 8.0f;
   extern __shared__ __attribute__((aligned(16))) char s_dyn[];  // [2][k, v][TILE]
   const int lane = threadIdx.x & (WAVE - 1), l16 = lane & 15, lg = lane >> 4;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
   const int h = blockIdx.y, g = h / (a.H / a.G), D = a.D;
   Unit u;
-  if (!unit_of(a.off, a.n, a.N, BLOCK, false, blockIdx.x, u) || u.lo >= u.hi) return;
+  if (!unit_of(a.off, a.n, a.N, BLOCK_OF<T>, false, blockIdx.x, u) || u.lo >= u.hi) return;
 
   const T *q = static_cast<const T *>(a.q) + u.b * a.qs + (long long)h * D;
   const T *k = static_cast<const T *>(a.k) + u.b * a.ks + (long long)g * D;
@@ -159,7 +164,7 @@ __global__ __launch_bounds__(WNT, MIN_WAVES<T>) void k_window(WinArgs a) {
 #pragma unroll
       for (int e = 0; e < (int)sizeof(T) / 2; ++e)
         qf[i][s].v[e] =
-            load_group<T, WIDE>(q + t * a.qs, 32 * s + 8 * lg + e * PER<T>, D, t < u.hi) ^
+            load_group<T, WIDE>(q + t * a.qs, 32 * s + 8 * lg + e * PER<T>, D, t < u.hi, q) ^
             (int)sign;
   }
   float m[QT], l[QT];  // (m in units of scores)
@@ -404,7 +409,7 @@ __device__ __noinline__ TwoFours exact_dkv(const T *q, long long qs, const T *gy
 template <typename T, int P, bool WIDE, bool SUMS>
 __device__ __forceinline__ void dq_block(const WinArgs &a, const Unit &u, int h, char *s_dyn) {
   // s_dyn: [2][k, v][TILE]
-  constexpr int DT = P / 16, DS = P / 32, TILE = KEYS * P * (int)sizeof(T);
+  constexpr int QT = QT_OF<T>, DT = P / 16, DS = P / 32, TILE = KEYS * P * (int)sizeof(T);
   const int lane = threadIdx.x & (WAVE - 1), l16 = lane & 15, lg = lane >> 4;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
   const int g = h / (a.H / a.G), D = a.D;
@@ -439,8 +444,8 @@ __device__ __forceinline__ void dq_block(const WinArgs &a, const Unit &u, int h,
 #pragma unroll
       for (int e = 0; e < (int)sizeof(T) / 2; ++e) {
         const int at = 32 * s + 8 * lg + e * PER<T>;
-        qf[i][s].v[e] = load_group<T, WIDE>(q + t * a.qs, at, D, there);
-        gf[i][s].v[e] = load_group<T, WIDE>(gy + t * a.gys, at, D, there);
+        qf[i][s].v[e] = load_group<T, WIDE>(q + t * a.qs, at, D, there, q);
+        gf[i][s].v[e] = load_group<T, WIDE>(gy + t * a.gys, at, D, there, gy);
       }
     lse[i] = there && !sees_one(t, a.window, a.sinks) ? a.lse[(u.b + t) * a.H + h] * LOG2E
                                                       : INFINITY;
@@ -568,7 +573,8 @@ __device__ __forceinline__ float *unit_part(const WinArgs &a, const Unit &u, lon
 template <typename T, int P, bool WIDE>
 __device__ __forceinline__ void dkv_block(const WinArgs &a, const Unit &u, int g, char *s_dyn) {
   // s_dyn: [2][q, dy][TILE], v, lse and delta [2][2][QUERIES]
-  constexpr int DT = P / 16, DS = P / 32, TILE = QUERIES * P * (int)sizeof(T);
+  constexpr int QT = QT_OF<T>, BLOCK = BLOCK_OF<T>, DT = P / 16, DS = P / 32;
+  constexpr int TILE = QUERIES * P * (int)sizeof(T);
   char *s_v = s_dyn + 4 * TILE;
   float *s_row = reinterpret_cast<float *>(s_v + BLOCK * P * (int)sizeof(T));
   const int lane = threadIdx.x & (WAVE - 1), l16 = lane & 15, lg = lane >> 4;
@@ -592,7 +598,7 @@ __device__ __forceinline__ void dkv_block(const WinArgs &a, const Unit &u, int g
 #pragma unroll
       for (int e = 0; e < (int)sizeof(T) / 2; ++e) {
         const int at = 32 * t + 8 * lg + e * PER<T>;
-        kf[i][t].v[e] = load_group<T, WIDE>(k + s * a.ks, at, D, s < u.hi);
+        kf[i][t].v[e] = load_group<T, WIDE>(k + s * a.ks, at, D, s < u.hi, k);
       }
   }
   cv.finish(s_v);
@@ -781,8 +787,8 @@ __device__ __forceinline__ void sinks_block(const WinArgs &a, const Unit &u, int
 #pragma unroll
     for (int e = 0; e < (int)sizeof(T) / 2; ++e) {
       const int at = 32 * t + 8 * lg + e * PER<T>;
-      kf[t].v[e] = load_group<T, WIDE>(k + s * a.ks, at, D, mine);
-      vf[t].v[e] = load_group<T, WIDE>(v + s * a.vs, at, D, mine);
+      kf[t].v[e] = load_group<T, WIDE>(k + s * a.ks, at, D, mine, k);
+      vf[t].v[e] = load_group<T, WIDE>(v + s * a.vs, at, D, mine, v);
     }
   const float c = a.scale * LOG2E, up = ds_scale<T>(a);
   float4v ok[DT] = {}, ov[DT] = {};
@@ -897,6 +903,7 @@ __device__ __forceinline__ void sinks_block(const WinArgs &a, const Unit &u, int
 template <typename T, int P, bool WIDE>
 __global__ __launch_bounds__(WNT, MIN_WAVES<T>) void k_window_back(WinArgs a) {
   extern __shared__ __attribute__((aligned(16))) char s_dyn[];
+  constexpr int BLOCK = BLOCK_OF<T>;
   const long long blocks = a.N / BLOCK + a.n;
   long long id = (long long)blockIdx.y * gridDim.x + blockIdx.x;
   Unit u;
@@ -924,6 +931,7 @@ __global__ __launch_bounds__(WNT, MIN_WAVES<T>) void k_window_back(WinArgs a) {
 // summed again from P and dy v^T.
 template <typename T, int P, bool WIDE>
 __global__ __launch_bounds__(WNT, MIN_WAVES<T>) void k_window_sums(WinArgs a, int every) {
+  constexpr int BLOCK = BLOCK_OF<T>;
   extern __shared__ __attribute__((aligned(16))) char s_dyn[];
   Unit u;
   if (!unit_of(a.off, a.n, a.N, every ? BLOCK : 0, false, blockIdx.x, u)) return;
@@ -1008,33 +1016,48 @@ __global__ __launch_bounds__(WNT) void k_window_step(WinStepArgs a) {
   for (int s = 0; s < DS; ++s)
 #pragma unroll
     for (int e = 0; e < (int)sizeof(T) / 2; ++e)
-      qf[s].v[e] = load_group<T, WIDE>(q, 32 * s + 8 * lg + e * PER<T>, D, l16 < heads);
+      qf[s].v[e] = load_group<T, WIDE>(q, 32 * s + 8 * lg + e * PER<T>, D, l16 < heads, kn);
   const float c = a.scale * LOG2E;
   float m = -INFINITY, l = 0.0f;
   float4v o[DT] = {};
-  for (int tile = first + w; tile < last; tile += WNW) {
-    const int c0 = tile * 32;
-    int4v vr[LOADS];
-#pragma unroll
-    for (int e = 0; e < LOADS; ++e) {
-      const int at = e * WAVE + lane, r = c0 + at / GROUPS;
-      vr[e] = load_group<T, WIDE>(r == own ? vn : vc + (long long)r * a.vcs,
-                                  at % GROUPS * PER<T>, D, r < count);
-    }
-    float4v x[2] = {};
+  // a tile's keys, as operands, and values: the next one's are read as soon as this
+  // one's are used
+  Frag<T> kr[2][DS];
+  int4v vr[LOADS];
+  const auto read_keys = [&](int c0) {
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
       const int r = c0 + 16 * b + l16;
       const T *p = r == own ? kn : kc + (long long)r * a.kcs;
 #pragma unroll
-      for (int s = 0; s < DS; ++s) {
-        Frag<T> f;
+      for (int s = 0; s < DS; ++s)
 #pragma unroll
         for (int e = 0; e < (int)sizeof(T) / 2; ++e)
-          f.v[e] = load_group<T, WIDE>(p, 32 * s + 8 * lg + e * PER<T>, D, r < count);
-        x[b] = mac(f, qf[s], x[b]);
-      }
+          kr[b][s].v[e] =
+              load_group<T, WIDE>(p, 32 * s + 8 * lg + e * PER<T>, D, r < count, kn);
     }
+  };
+  const auto read_values = [&](int c0) {
+#pragma unroll
+    for (int e = 0; e < LOADS; ++e) {
+      const int at = e * WAVE + lane, r = c0 + at / GROUPS;
+      vr[e] = load_group<T, WIDE>(r == own ? vn : vc + (long long)r * a.vcs,
+                                  at % GROUPS * PER<T>, D, r < count, vn);
+    }
+  };
+  if (first + w < last) {
+    read_keys((first + w) * 32);
+    read_values((first + w) * 32);
+  }
+  for (int tile = first + w; tile < last; tile += WNW) {
+    const int c0 = tile * 32, next0 = c0 + 32 * WNW;
+    const bool more = tile + WNW < last;
+    float4v x[2] = {};
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int s = 0; s < DS; ++s) x[b] = mac(kr[b][s], qf[s], x[b]);
+    if (more) read_keys(next0);
     __builtin_amdgcn_wave_barrier();
 #pragma unroll
     for (int e = 0; e < LOADS; ++e) {
@@ -1042,6 +1065,7 @@ __global__ __launch_bounds__(WNT) void k_window_step(WinStepArgs a) {
       *reinterpret_cast<int4v *>(&s_v[w][at / GROUPS * LD<T, P> + at % GROUPS * PER<T>]) = vr[e];
     }
     __builtin_amdgcn_wave_barrier();
+    if (more) read_values(next0);
     float top = -INFINITY;
 #pragma unroll
     for (int b = 0; b < 2; ++b)
@@ -1155,12 +1179,12 @@ __global__ __launch_bounds__(WNT) void k_window_fill(WinFillArgs a) {
 // ---------------------------------------------------------------------------
 
 // Whether every head's row of each tensor begins at a multiple of 16 bytes and is
-// whole groups of them, and tiles are within reach.
+// whole groups of them.
 bool wide_rows(size_t e, int D, std::initializer_list<long long> strides,
                std::initializer_list<const void *> data) {
   if (D * e % 16) return false;
   for (long long t : strides)
-    if (t * e % 16 || (t * BLOCK + D) * (long long)e > MAX_TILE_BYTES) return false;
+    if (t * e % 16) return false;
   for (const void *p : data)
     if (reinterpret_cast<uintptr_t>(p) % 16) return false;
   return true;
@@ -1171,7 +1195,7 @@ bool wide_rows(size_t e, int D, std::initializer_list<long long> strides,
 template <typename T, int P>
 constexpr int WALK = 4 * KEYS * P * (int)sizeof(T);
 template <typename T, int P>
-constexpr int WALK_BACK = (4 * QUERIES + BLOCK) * P * (int)sizeof(T) + 4 * QUERIES * 4;
+constexpr int WALK_BACK = (4 * QUERIES + BLOCK_OF<T>) * P * (int)sizeof(T) + 4 * QUERIES * 4;
 template <typename T, int P>
 constexpr int WALK_UNIT = 2 * BYTES<T, P, 32 * WNW> + 2 * 32 * WNW * 4;
 static_assert(WALK<float, 128> <= 160 * 1024 && WALK_BACK<float, 128> <= 160 * 1024 &&
@@ -1189,6 +1213,7 @@ constexpr long long MAX_BLOCKS = 1 << 23;   // and of its first
 template <typename T, int P, bool WIDE>
 hipError_t forward_as(const WinArgs &a, hipStream_t s) {
   constexpr int lds = WALK<T, P>;
+  constexpr int BLOCK = BLOCK_OF<T>;
   if (a.N / BLOCK + a.n > MAX_BLOCKS) return hipErrorInvalidValue;
   const hipError_t e = allow_lds(reinterpret_cast<const void *>(k_window<T, P, WIDE>), lds);
   if (e != hipSuccess) return e;
@@ -1198,7 +1223,7 @@ hipError_t forward_as(const WinArgs &a, hipStream_t s) {
 
 template <typename T, int P, bool WIDE>
 hipError_t backward_as(const WinArgs &a, hipStream_t s) {
-  const long long blocks = a.N / BLOCK + a.n;
+  const long long blocks = a.N / BLOCK_OF<T> + a.n;
   if (a.most) k_window_zero<<<1, 2, 0, s>>>(a.most);
   const long long rows = (a.N * a.H + WNT / 16 - 1) / (WNT / 16);
   k_window_delta<T><<<(unsigned)(rows < 4096 ? rows : 4096), WNT, 0, s>>>(a);
@@ -1256,7 +1281,7 @@ int padded(int D) { return D <= 64 ? 64 : 128; }
 }  // namespace
 
 hipError_t launch_window(const WinArgs &a, int type, hipStream_t s) {
-  if (a.H > MAX_ACROSS) return hipErrorInvalidValue;
+  if (a.H > MAX_ACROSS || a.ks > MAX_STRIDE || a.vs > MAX_STRIDE) return hipErrorInvalidValue;
   const int D = a.D;
   const bool wide = wide_rows(type_bytes(type), D, {a.qs, a.ks, a.vs, a.os}, {a.q, a.k, a.v, a.o});
   return FOR_FORM(forward_as, a, s);
@@ -1265,11 +1290,14 @@ hipError_t launch_window(const WinArgs &a, int type, hipStream_t s) {
 // (also without workspace: then `need` is all that is set)
 hipError_t launch_window_grads(WinArgs a, int type, void *ws, size_t *need, hipStream_t s) {
   if (a.H > MAX_ACROSS) return hipErrorInvalidValue;
+  for (long long t : {a.qs, a.ks, a.vs, a.gys})
+    if (t > MAX_STRIDE) return hipErrorInvalidValue;
   const int D = a.D;
   const size_t delta = ((size_t)a.N * a.H + 3) / 4 * 4;
   // (a sequence has to be longer than the window, and than a unit, for the queries of
-  // its first frames to be cut)
-  a.unit = 512;
+  // its first frames to be cut; units give small calls 256 workgroups)
+  const long long unit = a.N * a.G / 256 / 128 * 128;
+  a.unit = unit < 128 ? 128 : unit > 512 ? 512 : unit;
   const bool cut = a.sinks > 0 && a.N > a.window && a.N > a.unit;
   const size_t first = cut ? (size_t)a.G * a.sinks * 2 * padded(D) : 0;
   const size_t own = (a.N / a.unit + 1) * first, part = (2 * a.N / a.unit + 1) * first;
@@ -1289,10 +1317,13 @@ hipError_t launch_window_step(WinStepArgs a, int type, void *ws, size_t *need, h
   const int D = a.D, E = a.H / a.G;
   const long long groups = (long long)a.G * ((E + 15) / 16);
   if (groups > MAX_ACROSS || a.H > MAX_ACROSS) return hipErrorInvalidValue;
-  // enough workgroups for the card, none with less than a tile a wavefront
-  const long long most = ((long long)a.sinks + a.window + 32 * WNW - 1) / (32 * WNW);
+  // enough workgroups for the card, none with less than three tiles a wavefront: the
+  // parts' join is a launch of its own (8 query and 2 key heads of 64, bf16, replayed:
+  // one stream of 256 frames 7.6 us with parts of one tile, 6.3 in one piece; of 2,000
+  // 14.5 with 16 parts, 11 with 4)
+  const long long most = ((long long)a.sinks + a.window) / (96 * WNW);
   long long splits = (512 + a.n * groups - 1) / (a.n * groups);
-  splits = splits < most ? splits : most;
+  splits = splits < most ? splits : most > 1 ? most : 1;
   a.splits = (int)(splits < 64 ? splits : 64);
   *need = a.splits > 1
               ? (size_t)a.n * a.H * a.splits * (padded(D) + 4) * sizeof(float)
