@@ -383,6 +383,34 @@ __device__ __forceinline__ void mend_four(T *row, int c, int width, const float4
     if (c + i < width && !(fabsf((float)row[c + i]) < INFINITY)) row[c + i] = (T)x[i];
 }
 
+// Maximum, and sum, over the four lanes that hold a column of results (16 apart): a
+// swap of rows of 16 lanes between two copies leaves a lane both its own and its
+// partner's, then one of halves does.
+__device__ __forceinline__ float2 swap16(float x) {
+  const uint32_t b = __builtin_bit_cast(uint32_t, x);
+  const auto r = __builtin_amdgcn_permlane16_swap(b, b, false, false);
+  return make_float2(__builtin_bit_cast(float, (uint32_t)r[0]),
+                     __builtin_bit_cast(float, (uint32_t)r[1]));
+}
+__device__ __forceinline__ float2 swap32(float x) {
+  const uint32_t b = __builtin_bit_cast(uint32_t, x);
+  const auto r = __builtin_amdgcn_permlane32_swap(b, b, false, false);
+  return make_float2(__builtin_bit_cast(float, (uint32_t)r[0]),
+                     __builtin_bit_cast(float, (uint32_t)r[1]));
+}
+__device__ __forceinline__ float column_max(float x) {
+  float2 p = swap16(x);
+  x = fmaxf(p.x, p.y);
+  p = swap32(x);
+  return fmaxf(p.x, p.y);
+}
+__device__ __forceinline__ float column_sum(float x) {
+  float2 p = swap16(x);
+  x = p.x + p.y;
+  p = swap32(x);
+  return p.x + p.y;
+}
+
 __device__ __forceinline__ float wave_max(float m) {
 #pragma unroll
   for (int o = 32; o; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, WAVE));

@@ -90,6 +90,28 @@ __device__ __forceinline__ Seen seen_by(long long lo, long long hi, int window, 
   return s;
 }
 
+// Of a tile of keys from s0 on, which of a lane's (s0 + 4 lg + at, at = 16 kt + r)
+// query t sees: at <= last, and at >= from or at < upto.  A tile that no query has
+// the near, or the far, end of its frames in needs no such choice.
+struct Edge {
+  int last, from, upto;
+  bool near, far;
+};
+__device__ __forceinline__ int within_tile(long long x) {
+  return (int)(x < -KEYS ? -KEYS : x > KEYS ? KEYS : x);
+}
+__device__ __forceinline__ Edge edge_of(const WinArgs &a, const Seen &sn, bool sink, long long s0,
+                                        long long t, int lg) {
+  Edge e;
+  const long long at0 = s0 + 4 * lg;
+  e.last = sink ? KEYS : within_tile(t - at0);
+  e.from = sink ? KEYS : within_tile(t - a.window + 1 - at0);
+  e.upto = within_tile((sink ? sn.sinks : a.sinks) - at0);
+  e.near = __any(e.last < KEYS);
+  e.far = __any(e.from > 0);
+  return e;
+}
+
 // ---------------------------------------------------------------------------
 // forward
 // ---------------------------------------------------------------------------
@@ -202,20 +224,22 @@ __global__ __launch_bounds__(WNT, MIN_WAVES<T>) void k_window(WinArgs a) {
       if (!whole) {
 #pragma unroll
         for (int i = 0; i < QT; ++i) {
-          // (of a lane's keys s0 + 16 kt + 4 lg + r: those up to `last`, from
-          // `from` on or up to `sinks`, all within 32 bits of s0)
-          const long long t = tw + 16 * i + l16 - s0 - 4 * lg;
-          const long long far = t - a.window + 1, sinks = (sink ? sn.sinks : a.sinks) - s0 - 4 * lg;
-          const int last = sink ? KEYS : (int)(t < KEYS ? t : KEYS);
-          const int from = sink ? KEYS : (int)(far < -KEYS ? -KEYS : far > KEYS ? KEYS : far);
-          const int upto = (int)(sinks < -KEYS ? -KEYS : sinks > KEYS ? KEYS : sinks);
+          const Edge e = edge_of(a, sn, sink, s0, tw + 16 * i + l16, lg);
+          if (e.near) {
 #pragma unroll
-          for (int kt = 0; kt < 4; ++kt)
+            for (int kt = 0; kt < 4; ++kt)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-              const int at = 16 * kt + r;
-              if (at > last || (at < from && at >= upto)) x[kt][i][r] = -INFINITY;
-            }
+              for (int r = 0; r < 4; ++r)
+                x[kt][i][r] = 16 * kt + r <= e.last ? x[kt][i][r] : -INFINITY;
+          }
+          if (e.far) {
+#pragma unroll
+            for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+              for (int r = 0; r < 4; ++r)
+                x[kt][i][r] = ((16 * kt + r >= e.from) | (16 * kt + r < e.upto)) ? x[kt][i][r]
+                                                                              : -INFINITY;
+          }
         }
       }
       float shift[QT];
@@ -229,8 +253,7 @@ __global__ __launch_bounds__(WNT, MIN_WAVES<T>) void k_window(WinArgs a) {
           top = fmaxf(fmaxf(top, x[kt][i][0]), x[kt][i][1]);
           top = fmaxf(fmaxf(top, x[kt][i][2]), x[kt][i][3]);
         }
-        top = fmaxf(top, __shfl_xor(top, 16, WAVE));
-        top = fmaxf(top, __shfl_xor(top, 32, WAVE));
+        top = column_max(top);
         shift[i] = fmaxf(m[i], top);
         late = late || !((shift[i] - m[i]) * c <= LATE);
       }
@@ -277,8 +300,7 @@ __global__ __launch_bounds__(WNT, MIN_WAVES<T>) void k_window(WinArgs a) {
   const bool fine = finite(o);
 #pragma unroll
   for (int i = 0; i < QT; ++i) {
-    l[i] += __shfl_xor(l[i], 16, WAVE);
-    l[i] += __shfl_xor(l[i], 32, WAVE);
+    l[i] = column_sum(l[i]);
     const long long t = tw + 16 * i + l16;
     if (t >= u.hi) continue;
     const float f = 1.0f / l[i];
@@ -493,16 +515,25 @@ __device__ __forceinline__ void dq_block(const WinArgs &a, const Unit &u, int h,
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
             const float e = exp2_of(fmaf(x[b][i][r], c, -lse[i]));
-            float d = SUMS ? e * y[b][i][r] : e * (y[b][i][r] - delta[i]) * up;
-            if (!whole) {
-              const long long t = tw + 16 * i + l16, s = s0 + 32 * t2 + 16 * b + 4 * lg + r;
-              const bool sees = sink ? s < sn.sinks
-                                     : s <= t && (t - s < a.window || s < a.sinks);
-              d = sees ? d : 0.0f;
-            }
-            x[b][i][r] = d;
-            if constexpr (SUMS) sum[i] += d;
+            x[b][i][r] = SUMS ? e * y[b][i][r] : e * (y[b][i][r] - delta[i]) * up;
           }
+        if (!whole) {
+          const Edge e = edge_of(a, sn, sink, s0 + 32 * t2, tw + 16 * i + l16, lg);
+#pragma unroll
+          for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              const int at = 16 * b + r;
+              const bool sees = (at <= e.last) & ((at >= e.from) | (at < e.upto));
+              x[b][i][r] = sees ? x[b][i][r] : 0.0f;
+            }
+        }
+        if constexpr (SUMS) {
+#pragma unroll
+          for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) sum[i] += x[b][i][r];
+        }
         p[i] = pack<T>(x[0][i], x[1][i]);
       }
       if constexpr (SUMS) continue;
@@ -521,8 +552,7 @@ __device__ __forceinline__ void dq_block(const WinArgs &a, const Unit &u, int h,
   if constexpr (SUMS) {
 #pragma unroll
     for (int i = 0; i < QT; ++i) {
-      sum[i] += __shfl_xor(sum[i], 16, WAVE);
-      sum[i] += __shfl_xor(sum[i], 32, WAVE);
+      sum[i] = column_sum(sum[i]);
       const long long t = tw + 16 * i + l16;
       if (lg == 0 && t < u.hi) a.delta[(u.b + t) * a.H + h] = sum[i];
     }
@@ -674,18 +704,31 @@ __device__ __forceinline__ void dkv_block(const WinArgs &a, const Unit &u, int g
         for (int i = 0; i < QT; ++i)
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
-            float e = exp2_of(fmaf(x[b][i][r], c, -lse[r]));
-            float d = e * (y[b][i][r] - delta[r]) * up;
-            if (!whole) {
-              const long long t = t0 + at + r, s = sw + 16 * i + l16;
-              const bool sees =
-                  s <= t && t < end && (t - s < a.window || (onward && s < a.sinks));
-              e = sees ? e : 0.0f;
-              d = sees && !sees_one(t, a.window, a.sinks) ? d : 0.0f;
-            }
+            const float e = exp2_of(fmaf(x[b][i][r], c, -lse[r]));
             x[b][i][r] = e;
-            y[b][i][r] = d;
+            y[b][i][r] = e * (y[b][i][r] - delta[r]) * up;
           }
+      }
+      if (!whole) {
+#pragma unroll
+        for (int i = 0; i < QT; ++i) {
+          // of a lane's queries t0 + 4 lg + at: those from the key on, up to `end` and
+          // to the end of the window
+          const long long s = sw + 16 * i + l16, at0 = t0 + 4 * lg;
+          const long long past = onward && s < a.sinks ? end : s + a.window;
+          const int from = within_tile(s - at0);
+          const int upto = within_tile((past < end ? past : end) - at0);
+          const int first = a.window == 1 && a.sinks == 0 ? KEYS : within_tile(-at0);
+#pragma unroll
+          for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              const int at = 16 * b + r;
+              const bool sees = (at >= from) & (at < upto);
+              x[b][i][r] = sees ? x[b][i][r] : 0.0f;
+              y[b][i][r] = (sees & (at > first)) ? y[b][i][r] : 0.0f;
+            }
+        }
       }
       Frag<T> p[QT], ds[QT];
 #pragma unroll
@@ -1074,8 +1117,7 @@ __global__ __launch_bounds__(WNT) void k_window_step(WinStepArgs a) {
         x[b][r] = c0 + 16 * b + 4 * lg + r < count ? x[b][r] * c : -INFINITY;
         top = fmaxf(top, x[b][r]);
       }
-    top = fmaxf(top, __shfl_xor(top, 16, WAVE));
-    top = fmaxf(top, __shfl_xor(top, 32, WAVE));
+    top = column_max(top);
     const float next = fmaxf(m, top), shift = next == -INFINITY ? 0.0f : next;
     const float less = exp2_of(m - shift);
     m = next;
@@ -1092,8 +1134,7 @@ __global__ __launch_bounds__(WNT) void k_window_step(WinStepArgs a) {
     for (int d = 0; d < DT; ++d)
       o[d] = mac(columns<T, P>(s_v[w], 0, 16 * d, lane), p, o[d] * less);
   }
-  l += __shfl_xor(l, 16, WAVE);
-  l += __shfl_xor(l, 32, WAVE);
+  l = column_sum(l);
   if (lg == 0) s_m[w][l16] = m, s_l[w][l16] = l;
   __syncthreads();
   // the wavefronts' results joined: each scaled to the largest maximum, then summed
