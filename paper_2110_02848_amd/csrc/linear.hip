@@ -366,35 +366,54 @@ __global__ __launch_bounds__(256 * CG, CG == 2 ? 2 : sizeof(T) == 2 && PA == 64 
       }
 }
 
-// From the units' own contributions to the states entering them, in place: a
-// thread takes an element of a head's state through a sequence's units.
+// From the units' own contributions to the states entering them, in place: a lane
+// takes an element of a head's state, its workgroup's wavefronts a part of a
+// sequence's units each.  What each part makes of a zero state meets in LDS; a part's
+// units stay in registers, unless there are more than AHEAD of them.  Bound by two
+// trips to memory (90 units of 8 x 64 x 64: 6 us, one wavefront for all units 10).
 __global__ __launch_bounds__(NT) void k_linear_scan(LinArgs a) {
+  constexpr int AHEAD = 32;
+  __shared__ float s_sum[NWAVES][WAVE];
   const LinJob &job = a.job[blockIdx.z];
-  const long long AB = (long long)job.A * job.B, all = AB * a.H;
-  const long long e = (long long)blockIdx.x * NT + threadIdx.x;
+  const int AB = job.A * job.B, all = AB * a.H;
+  const int lane = threadIdx.x & (WAVE - 1);
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
+  const int at = blockIdx.x * WAVE + lane, e = at < all ? at : all - 1;
   const int s = blockIdx.y;
-  if (e >= all) return;
   const long long b = clamped(a.off[s], 0, a.N);
   const long long len = clamped(a.off[s + 1], b, a.N) - b;
-  const int h = (int)(e / AB);
-  const float g = a.log_decay[h];
-  const double d = g < -1e4f ? -1e4 : (double)g, whole = exp(d * (double)a.unit);
+  const long long n = len > 0 ? over_steps(len - 1, a.unit) + 1 : 1;
+  const long long share = (n + NWAVES - 1) / NWAVES, u0 = w * share;
+  const long long u1 = u0 + share < n ? u0 + share : n;
+  float *p = job.units + rows_before(b, s, a.unit) * all + e;
+  float x[AHEAD];
+#pragma unroll
+  for (int c = 0; c < AHEAD; ++c) x[c] = u0 + c < u1 ? p[(u0 + c) * all] : 0.0f;
+  const float g = a.log_decay[e / AB];
+  const double d = (g < -1e4f ? -1e4 : (double)g) * (double)a.unit, whole = exp(d);
   const float kh = (float)whole;
   const float kl = fabsf(kh) < INFINITY ? (float)(whole - (double)kh) : 0.0f;
-  float S = job.state ? job.state[s * all + e] : 0.0f;
-  float *p = job.units + rows_before(b, s, a.unit) * all + e;
-  const long long n = len > 0 ? (len + a.unit - 1) / a.unit : 1;
-  constexpr int AHEAD = 32;
-  for (long long i = 0; i < n; i += AHEAD) {
-    float x[AHEAD];
+  float sum = 0.0f;
 #pragma unroll
-    for (int c = 0; c < AHEAD; ++c) x[c] = i + c < n ? p[(i + c) * all] : 0.0f;
+  for (int c = 0; c < AHEAD; ++c)
+    if (u0 + c < u1) sum = fmaf(kh, sum, fmaf(kl, sum, x[c]));
+  for (long long u = u0 + AHEAD; u < u1; ++u) sum = fmaf(kh, sum, fmaf(kl, sum, p[u * all]));
+  s_sum[w][lane] = sum;
+  __syncthreads();
+  float S = job.state ? job.state[(long long)s * all + e] : 0.0f;
+  const float over = w ? (float)exp(d * (double)share) : 1.0f;
+  for (int q = 0; q < w; ++q) S = fmaf(over, S, s_sum[q][lane]);
+  if (at >= all) return;
 #pragma unroll
-    for (int c = 0; c < AHEAD; ++c) {
-      if (i + c >= n) break;
-      p[(i + c) * all] = S;
+  for (int c = 0; c < AHEAD; ++c)
+    if (u0 + c < u1) {
+      p[(u0 + c) * all] = S;
       S = fmaf(kh, S, fmaf(kl, S, x[c]));
     }
+  for (long long u = u0 + AHEAD; u < u1; ++u) {
+    const float y = p[u * all];
+    p[u * all] = S;
+    S = fmaf(kh, S, fmaf(kl, S, y));
   }
 }
 
@@ -553,7 +572,7 @@ hipError_t launch_states(const LinArgs &a, const LinJob *all, int jobs, int type
   LinArgs b = a;
   for (int i = 0; i < jobs; ++i) b.job[i] = all[i];
   const long long n = (long long)a.H * all[0].A * all[0].B;
-  k_linear_scan<<<dim3((unsigned)((n + NT - 1) / NT), a.n, jobs), NT, 0, s>>>(b);
+  k_linear_scan<<<dim3((unsigned)((n + WAVE - 1) / WAVE), a.n, jobs), NT, 0, s>>>(b);
   return hipGetLastError();
 }
 

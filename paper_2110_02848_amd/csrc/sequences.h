@@ -18,11 +18,16 @@ __device__ __forceinline__ long long clamped(long long v, long long lo, long lon
   return v < lo ? lo : v > hi ? hi : v;
 }
 
+// x / per of a row x (rows fit 31 bits): a division of 64 bits takes a microsecond.
+__device__ __forceinline__ long long over_steps(long long x, long long per) {
+  return per > INT32_MAX ? 0 : (long long)((uint32_t)x / (uint32_t)per);
+}
+
 // First of the rows that sequence s, from row b, has in an array with a row
 // for every `per` steps of a sequence: ceil(len / per) rows fit before the
 // next sequence's, as floor(b / per) + s grows by at least that.
 __device__ __forceinline__ long long rows_before(long long b, int s, long long per) {
-  return b / per + s;
+  return over_steps(b, per) + s;
 }
 
 // The unit of workgroup k among n sequences of N rows: a whole sequence, or
@@ -57,6 +62,16 @@ __device__ __forceinline__ bool unit_of(const int32_t *off, int n, long long N, 
   u.step = reverse ? -1 : 1;
   u.first = reverse ? u.b + u.len - 1 : u.b;
   return true;
+}
+
+// Which of `all` pieces of work workgroup `id` takes.  Workgroups go to the eight XCDs
+// in turn, and each has a second-level cache: an XCD gets a run of consecutive
+// pieces, which read much the same rows.
+__device__ __forceinline__ long long piece_of(long long id, long long all) {
+  const int x = (int)(id % 8);
+  const long long per = all / 8;
+  const int more = (int)(all % 8);
+  return x * per + (x < more ? x : more) + id / 8;
 }
 
 }  // namespace fstc

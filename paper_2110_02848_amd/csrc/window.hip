@@ -98,7 +98,11 @@ struct Edge {
   bool near, far;
 };
 __device__ __forceinline__ int within_tile(long long x) {
-  return (int)(x < -KEYS ? -KEYS : x > KEYS ? KEYS : x);
+  int y = (int)(x < -KEYS ? -KEYS : x > KEYS ? KEYS : x);
+  // (as it is: comparisons with it would be made with x, in 64 bits, and the choices
+  // for tiles at an edge for all of them)
+  asm volatile("" : "+v"(y));
+  return y;
 }
 __device__ __forceinline__ Edge edge_of(const WinArgs &a, const Seen &sn, bool sink, long long s0,
                                         long long t, int lg) {
@@ -151,9 +155,11 @@ __global__ __launch_bounds__(WNT, MIN_WAVES<T>) void k_window(WinArgs a) {
   extern __shared__ __attribute__((aligned(16))) char s_dyn[];  // [2][k, v][TILE]
   const int lane = threadIdx.x & (WAVE - 1), l16 = lane & 15, lg = lane >> 4;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
-  const int h = blockIdx.y, g = h / (a.H / a.G), D = a.D;
+  const long long piece = piece_of((long long)blockIdx.y * gridDim.x + blockIdx.x,
+                                   (long long)gridDim.x * gridDim.y);
+  const int h = (int)(piece / gridDim.x), g = h / (a.H / a.G), D = a.D;
   Unit u;
-  if (!unit_of(a.off, a.n, a.N, BLOCK_OF<T>, false, blockIdx.x, u) || u.lo >= u.hi) return;
+  if (!unit_of(a.off, a.n, a.N, BLOCK_OF<T>, false, piece % gridDim.x, u) || u.lo >= u.hi) return;
 
   const T *q = static_cast<const T *>(a.q) + u.b * a.qs + (long long)h * D;
   const T *k = static_cast<const T *>(a.k) + u.b * a.ks + (long long)g * D;
@@ -951,12 +957,14 @@ __global__ __launch_bounds__(WNT, MIN_WAVES<T>) void k_window_back(WinArgs a) {
   long long id = (long long)blockIdx.y * gridDim.x + blockIdx.x;
   Unit u;
   if (id < blocks * a.G) {
+    id = piece_of(id, blocks * a.G);
     if (unit_of(a.off, a.n, a.N, BLOCK, false, id % blocks, u) && u.lo < u.hi)
       dkv_block<T, P, WIDE>(a, u, (int)(id / blocks), s_dyn);
     return;
   }
   id -= blocks * a.G;
   if (id < blocks * a.H) {
+    id = piece_of(id, blocks * a.H);
     if (unit_of(a.off, a.n, a.N, BLOCK, false, id % blocks, u) && u.lo < u.hi)
       dq_block<T, P, WIDE, false>(a, u, (int)(id / blocks), s_dyn);
     return;
