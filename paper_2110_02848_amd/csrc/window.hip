@@ -334,36 +334,44 @@ __global__ __launch_bounds__(WNT, MIN_WAVES<T>) void k_window(WinArgs a) {
 // gradients
 // ---------------------------------------------------------------------------
 
-// delta = y . dy of each row and head, 16 lanes each; float16: the largest
-// lengths of rows of dy and v, whose product bounds dS.
-template <typename T>
+// delta = y . dy of each row and head, a lane for 16 bytes of it; float16: the largest
+// lengths of rows of dy and v, whose product bounds dS.  Bound by memory.
+template <typename T, int P, bool WIDE>
 __global__ __launch_bounds__(WNT) void k_window_delta(WinArgs a) {
+  constexpr int LANES = P / PER<T>, EACH = WNT / LANES;
   const long long all = a.N * a.H;
-  const int l16 = threadIdx.x & 15;
+  const int c = threadIdx.x % LANES * PER<T>;
+  struct alignas(16) Group { T v[PER<T>]; };
+  const auto read = [&](const void *p, long long at) {
+    const T *row = static_cast<const T *>(p) + at;
+    return __builtin_bit_cast(Group, load_group<T, WIDE>(row, c, a.D, true, row));
+  };
   float top = 0.0f, topv = 0.0f;
-  for (long long i = ((long long)blockIdx.x * WNT + threadIdx.x) / 16; i < all;
-       i += (long long)gridDim.x * (WNT / 16)) {
-    const long long row = i / a.H;
-    const int h = (int)(i % a.H);
-    const T *y = static_cast<const T *>(a.y) + row * a.ys + (long long)h * a.D;
-    const T *gy = static_cast<const T *>(a.gy) + row * a.gys + (long long)h * a.D;
+  for (long long i = (long long)blockIdx.x * EACH + threadIdx.x / LANES; i < all;
+       i += (long long)gridDim.x * EACH) {
+    const long long row = (uint64_t)i / (uint32_t)a.H;
+    const int h = (int)(i - row * a.H);
+    const Group y = read(a.y, row * a.ys + (long long)h * a.D);
+    const Group gy = read(a.gy, row * a.gys + (long long)h * a.D);
+    Group v{};
+    if (a.most && h < a.G) v = read(a.v, row * a.vs + (long long)h * a.D);
     float s = 0.0f, n = 0.0f, nv = 0.0f;
-    for (int d = l16; d < a.D; d += 16) {
-      const float g = (float)gy[d];
-      s = fmaf((float)y[d], g, s);
+#pragma unroll
+    for (int j = 0; j < PER<T>; ++j) {
+      const float g = (float)gy.v[j];
+      s = fmaf((float)y.v[j], g, s);
       n = fmaf(g, g, n);
-    }
-    if (a.most && h < a.G) {
-      const T *v = static_cast<const T *>(a.v) + row * a.vs + (long long)h * a.D;
-      for (int d = l16; d < a.D; d += 16) nv = fmaf((float)v[d], (float)v[d], nv);
+      nv = fmaf((float)v.v[j], (float)v.v[j], nv);
     }
 #pragma unroll
-    for (int o = 8; o; o >>= 1) {
+    for (int o = LANES / 2; o; o >>= 1) {
       s += __shfl_xor(s, o, WAVE);
-      n += __shfl_xor(n, o, WAVE);
-      nv += __shfl_xor(nv, o, WAVE);
+      if (a.most) {
+        n += __shfl_xor(n, o, WAVE);
+        nv += __shfl_xor(nv, o, WAVE);
+      }
     }
-    if (l16 == 0) a.delta[i] = s;
+    if (c == 0) a.delta[i] = s;
     top = n < INFINITY ? fmaxf(top, n) : top;
     topv = nv < INFINITY ? fmaxf(topv, nv) : topv;
   }
@@ -1274,8 +1282,9 @@ template <typename T, int P, bool WIDE>
 hipError_t backward_as(const WinArgs &a, hipStream_t s) {
   const long long blocks = a.N / BLOCK_OF<T> + a.n;
   if (a.most) k_window_zero<<<1, 2, 0, s>>>(a.most);
-  const long long rows = (a.N * a.H + WNT / 16 - 1) / (WNT / 16);
-  k_window_delta<T><<<(unsigned)(rows < 4096 ? rows : 4096), WNT, 0, s>>>(a);
+  constexpr int each = WNT / (P / PER<T>);
+  const long long rows = (a.N * a.H + each - 1) / each;
+  k_window_delta<T, P, WIDE><<<(unsigned)(rows < 8192 ? rows : 8192), WNT, 0, s>>>(a);
   if constexpr (sizeof(T) == 2) {
     constexpr int lds = WALK<T, P>;
     const hipError_t e =
@@ -1357,8 +1366,8 @@ hipError_t launch_window_grads(WinArgs a, int type, void *ws, size_t *need, hipS
   a.delta = p + 4;
   a.own = p + 4 + delta;
   a.part = cut ? a.own + own : nullptr;
-  const bool wide = wide_rows(type_bytes(type), D, {a.qs, a.ks, a.vs, a.gys, a.gqs, a.gks, a.gvs},
-                              {a.q, a.k, a.v, a.gy, a.gq, a.gk, a.gv});
+  const bool wide = wide_rows(type_bytes(type), D, {a.qs, a.ks, a.vs, a.ys, a.gys, a.gqs, a.gks, a.gvs},
+                              {a.q, a.k, a.v, a.y, a.gy, a.gq, a.gk, a.gv});
   return FOR_FORM(backward_as, a, s);
 }
 

@@ -388,7 +388,8 @@ class Composer:
         self._dev = torch.device("cuda", self.device)
         self._pass = _Marshal()
         self._raw_stream = torch._C._cuda_getCurrentRawStream
-        self._empty = torch.empty
+        self._empty, self._empty_like = torch.empty, torch.empty_like
+        self._contiguous = torch.contiguous_format
         self._f32, self._i32 = torch.float32, torch.int32
 
     def close(self):
@@ -657,6 +658,13 @@ class Composer:
         with torch.cuda.stream(stream):
             return torch.empty(shape, dtype=dtype, device=self._dev)
 
+    def _like(self, stream, t):
+        """A tensor of t's shape and type that belongs to the stream of the call
+        (half the time of naming them)."""
+        if stream is None:
+            return self._empty_like(t, memory_format=self._contiguous)
+        return self._new(stream, t.shape, t.dtype)
+
     def _copy(self, stream, to, from_):
         if stream is None:
             to.copy_(from_)
@@ -758,7 +766,7 @@ class Composer:
         [N], freq float32 [P]): (q, k) as they were given.  Pair i of the
         columns is i and P + i, or with ``pairs`` 2 i and 2 i + 1."""
         A, k = self._head_norms(q, k, q_weight, k_weight, freq, pos, eps, pairs)
-        yq, yk = self._new(stream, q.shape, q.dtype), self._new(stream, k.shape, q.dtype)
+        yq, yk = self._like(stream, q), self._like(stream, k)
         self._uses(stream, q, k, q_weight, k_weight, freq, pos)
         rc = self._lib.fst_head_norms_run(
             self._h, A, self._pass.made(0, yq, _types[q.dtype]),
@@ -775,9 +783,9 @@ class Composer:
         A, k = self._head_norms(q, k, q_weight, k_weight, freq, pos, eps, pairs)
         if one:
             grad_k = k
-        gq, gk = self._new(stream, q.shape, q.dtype), self._new(stream, k.shape, q.dtype)
-        gqw = self._new(stream, q_weight.shape, self._f32)
-        gkw = None if one else self._new(stream, k_weight.shape, self._f32)
+        gq, gk = self._like(stream, q), self._like(stream, k)
+        gqw = self._like(stream, q_weight)
+        gkw = None if one else self._like(stream, k_weight)
         self._uses(stream, q, k, q_weight, k_weight, freq, pos, grad_q, grad_k)
         rc = self._lib.fst_head_norms_grads(
             self._h, A, self._pass.matrix(0, grad_q, "grad_q"),
@@ -811,7 +819,7 @@ class Composer:
         None: 0): dict(y: as v, last: the states after each sequence).  scale:
         K ** -0.5 if None."""
         A, n, (H, K, V) = self._linear(q, k, v, log_decay, offset, state, scale, reverse)
-        y = self._new(stream, v.shape, q.dtype)
+        y = self._like(stream, v)
         last = self._new(stream, (n, H, K, V), self._f32)
         self._uses(stream, q, k, v, log_decay, offset, state)
         rc = self._lib.fst_linear_attention_run(self._h, A,
@@ -826,7 +834,7 @@ class Composer:
         (``linear_attention`` of the same arguments): dict(q, k, v: as these,
         state: float32 [n, H, K, V]).  The decays are constants."""
         A, n, (H, K, V) = self._linear(q, k, v, log_decay, offset, state, scale, reverse)
-        gq, gk, gv = (self._new(stream, t.shape, q.dtype) for t in (q, k, v))
+        gq, gk, gv = self._like(stream, q), self._like(stream, k), self._like(stream, v)
         gs = self._new(stream, (n, H, K, V), self._f32)
         self._uses(stream, q, k, v, log_decay, offset, grad_y, state, grad_last)
         typ = _types[q.dtype]
@@ -872,7 +880,7 @@ class Composer:
             to = _address(out)
             if slots > rows:  # states that this step leaves alone
                 self._copy(stream, out[rows:], state.view(slots, H, K, V)[rows:])
-        y = self._new(stream, v.shape, q.dtype)
+        y = self._like(stream, v)
         self._uses(stream, q, k, v, log_decay, state, slot, out)
         m = self._pass
         rc = self._lib.fst_linear_attention_step(
@@ -893,7 +901,7 @@ class Composer:
         ``sinks``: dict(y: as q, lse: float32 [N, heads], the scores'
         log-sums).  scale: D ** -0.5 if None."""
         A, heads = self._window(q, k, v, offset, heads, kv_heads, window, sinks, scale)
-        y = self._new(stream, q.shape, q.dtype)
+        y = self._like(stream, q)
         lse = self._new(stream, (q.shape[0], heads), self._f32)
         self._uses(stream, q, k, v, offset)
         rc = self._lib.fst_window_attention_run(self._h, A,
@@ -907,7 +915,7 @@ class Composer:
         """Gradients of a loss by q, k and v from that by y, with y and lse of
         ``window_attention`` of the same arguments: dict(q, k, v)."""
         A, heads = self._window(q, k, v, offset, heads, kv_heads, window, sinks, scale)
-        gq, gk, gv = (self._new(stream, t.shape, q.dtype) for t in (q, k, v))
+        gq, gk, gv = self._like(stream, q), self._like(stream, k), self._like(stream, v)
         self._uses(stream, q, k, v, offset, y, lse, grad_y)
         typ, m = _types[q.dtype], self._pass
         rc = self._lib.fst_window_attention_grads(
@@ -945,7 +953,7 @@ class Composer:
         how = self._window_shape(q, heads, kv_heads, window, sinks, scale)
         rows, L = q.shape[0], how[2] + how[3]
         slots = k_cache.shape[0] // L if L > 0 else 0
-        y = self._new(stream, q.shape, q.dtype)
+        y = self._like(stream, q)
         self._uses(stream, q, k, v, pos, k_cache, v_cache, slot)
         m = self._pass
         rc = self._lib.fst_window_attention_step(
