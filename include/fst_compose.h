@@ -539,9 +539,10 @@ FST_API int fst_recurrence_step(fst_ctx *ctx, const fst_matrix *x, const fst_mat
  * taken again without them (slowly, and rounded in another order).  Infinities and
  * NaN in rows that they do see make no number of them, as the formulas do. */
 #define FST_NORM_MAX_WIDTH 512      /* columns of a head of fst_head_norms     */
-#define FST_ATTENTION_MAX_WIDTH 128 /* of the attentions (FST_ERR_TOO_LARGE),  */
-                                    /* which take at most 16,383 heads, and    */
-                                    /* rows up to 2^22 numbers apart           */
+#define FST_ATTENTION_MAX_WIDTH 128 /* of the attentions (FST_ERR_TOO_LARGE,   */
+                                    /* which more than 16,383 heads, rows more */
+                                    /* than 2^22 numbers apart and steps of    */
+                                    /* more than 2^23 rows may give as well)   */
 
 /* Queries and keys normalised head by head, scaled, and rotated by position.
  * For each head x of a row, of `width` columns, with one of the two weights

@@ -2014,6 +2014,9 @@ bool sequences_ok(int32_t num_seqs, const int32_t *offset, int64_t rows) {
          (num_seqs > 0 || rows == 0);
 }
 
+// The distance between rows, also where there is one and any may be given.
+long long pitch(const fst_matrix &m) { return m.rows > 1 ? m.stride : m.cols; }
+
 // Two matrices of one type and number of rows.
 bool rows_match(const fst_matrix &a, const fst_matrix &b) {
   return matrix_ok(&a) && matrix_ok(&b) && a.rows == b.rows && a.type == b.type;
@@ -2028,8 +2031,8 @@ bool head_norms_ok(const fst_head_norms *A) {
 }
 NormArgs norm_args(const fst_head_norms *A) {
   NormArgs a{};
-  a.side[0].x = A->q.data, a.side[0].xs = A->q.stride, a.side[0].w = A->q_weight;
-  a.side[1].x = A->k.data, a.side[1].xs = A->k.stride, a.side[1].w = A->k_weight;
+  a.side[0].x = A->q.data, a.side[0].xs = pitch(A->q), a.side[0].w = A->q_weight;
+  a.side[1].x = A->k.data, a.side[1].xs = pitch(A->k), a.side[1].w = A->k_weight;
   a.side[0].heads = (int)(A->q.cols / A->width);
   a.side[1].heads = (int)(A->k.cols / A->width);
   a.freq = A->freq;
@@ -2058,9 +2061,9 @@ bool attention_wide(int64_t cols, int32_t heads) {
 }
 LinCall linear_call(const fst_linear_attention *A) {
   LinCall c{};
-  c.q = A->q.data, c.qs = A->q.stride;
-  c.k = A->k.data, c.ks = A->k.stride;
-  c.v = A->v.data, c.vs = A->v.stride;
+  c.q = A->q.data, c.qs = pitch(A->q);
+  c.k = A->k.data, c.ks = pitch(A->k);
+  c.v = A->v.data, c.vs = pitch(A->v);
   c.state = A->state;
   c.off = A->offset;
   c.log_decay = A->log_decay;
@@ -2090,9 +2093,9 @@ bool window_attention_ok(const fst_window_attention *A) {
 }
 WinArgs window_args(const fst_window_attention *A) {
   WinArgs a{};
-  a.q = A->q.data, a.qs = A->q.stride;
-  a.k = A->k.data, a.ks = A->k.stride;
-  a.v = A->v.data, a.vs = A->v.stride;
+  a.q = A->q.data, a.qs = pitch(A->q);
+  a.k = A->k.data, a.ks = pitch(A->k);
+  a.v = A->v.data, a.vs = pitch(A->v);
   a.off = A->offset;
   a.N = A->q.rows;
   a.n = A->num_seqs;
@@ -2804,8 +2807,8 @@ int fst_head_norms_run(fst_ctx *c, const fst_head_norms *A, const fst_matrix *y_
   DeviceGuard g(c->device);
   if (!g.ok) return FST_ERR_HIP;
   NormArgs a = norm_args(A);
-  a.side[0].y = y_q->data, a.side[0].ys = y_q->stride;
-  a.side[1].y = y_k->data, a.side[1].ys = y_k->stride;
+  a.side[0].y = y_q->data, a.side[0].ys = pitch(*y_q);
+  a.side[1].y = y_k->data, a.side[1].ys = pitch(*y_k);
   return hip_status(launch_norms(a, A->q.type, reinterpret_cast<hipStream_t>(stream)));
 }
 
@@ -2822,10 +2825,10 @@ int fst_head_norms_grads(fst_ctx *c, const fst_head_norms *A, const fst_matrix *
   DeviceGuard g(c->device);
   if (!g.ok) return FST_ERR_HIP;
   NormArgs a = norm_args(A);
-  a.side[0].g = grad_yq->data, a.side[0].gs = grad_yq->stride;
-  a.side[1].g = grad_yk->data, a.side[1].gs = grad_yk->stride;
-  a.side[0].y = grad_q->data, a.side[0].ys = grad_q->stride;
-  a.side[1].y = grad_k->data, a.side[1].ys = grad_k->stride;
+  a.side[0].g = grad_yq->data, a.side[0].gs = pitch(*grad_yq);
+  a.side[1].g = grad_yk->data, a.side[1].gs = pitch(*grad_yk);
+  a.side[0].y = grad_q->data, a.side[0].ys = pitch(*grad_q);
+  a.side[1].y = grad_k->data, a.side[1].ys = pitch(*grad_k);
   a.side[0].gw = grad_q_weight;
   a.side[1].gw = grad_k_weight;
   return with_workspace(c, reinterpret_cast<hipStream_t>(stream), [&](void *ws, size_t *need) {
@@ -2843,7 +2846,7 @@ int fst_linear_attention_run(fst_ctx *c, const fst_linear_attention *A, const fs
   DeviceGuard g(c->device);
   if (!g.ok) return FST_ERR_HIP;
   LinCall l = linear_call(A);
-  l.y = y->data, l.ys = y->stride;
+  l.y = y->data, l.ys = pitch(*y);
   l.last = last;
   return with_workspace(c, reinterpret_cast<hipStream_t>(stream), [&](void *ws, size_t *need) {
     return launch_linear(l, A->q.type, ws, need, reinterpret_cast<hipStream_t>(stream));
@@ -2865,10 +2868,10 @@ int fst_linear_attention_grads(fst_ctx *c, const fst_linear_attention *A,
   DeviceGuard g(c->device);
   if (!g.ok) return FST_ERR_HIP;
   LinCall l = linear_call(A);
-  l.y = grad_y->data, l.ys = grad_y->stride;
-  l.gq = grad_q->data, l.gqs = grad_q->stride;
-  l.gk = grad_k->data, l.gks = grad_k->stride;
-  l.gv = grad_v->data, l.gvs = grad_v->stride;
+  l.y = grad_y->data, l.ys = pitch(*grad_y);
+  l.gq = grad_q->data, l.gqs = pitch(*grad_q);
+  l.gk = grad_k->data, l.gks = pitch(*grad_k);
+  l.gv = grad_v->data, l.gvs = pitch(*grad_v);
   l.glast = grad_last;
   l.gstate = grad_state;
   return with_workspace(c, reinterpret_cast<hipStream_t>(stream), [&](void *ws, size_t *need) {
@@ -2891,10 +2894,10 @@ int fst_linear_attention_step(fst_ctx *c, const fst_matrix *q, const fst_matrix 
   DeviceGuard g(c->device);
   if (!g.ok) return FST_ERR_HIP;
   LinStepArgs a{};
-  a.q = q->data, a.qs = q->stride;
-  a.k = k->data, a.ks = k->stride;
-  a.v = v->data, a.vs = v->stride;
-  a.y = y->data, a.ys = y->stride;
+  a.q = q->data, a.qs = pitch(*q);
+  a.k = k->data, a.ks = pitch(*k);
+  a.v = v->data, a.vs = pitch(*v);
+  a.y = y->data, a.ys = pitch(*y);
   a.log_decay = log_decay;
   a.in = state_in;
   a.out = state_out;
@@ -2918,7 +2921,7 @@ int fst_window_attention_run(fst_ctx *c, const fst_window_attention *A, const fs
   DeviceGuard g(c->device);
   if (!g.ok) return FST_ERR_HIP;
   WinArgs a = window_args(A);
-  a.o = y->data, a.os = y->stride;
+  a.o = y->data, a.os = pitch(*y);
   a.lse = lse;
   return hip_status(launch_window(a, A->q.type, reinterpret_cast<hipStream_t>(stream)));
 }
@@ -2938,11 +2941,11 @@ int fst_window_attention_grads(fst_ctx *c, const fst_window_attention *A, const 
   DeviceGuard g(c->device);
   if (!g.ok) return FST_ERR_HIP;
   WinArgs a = window_args(A);
-  a.y = y->data, a.ys = y->stride;
-  a.gy = grad_y->data, a.gys = grad_y->stride;
-  a.gq = grad_q->data, a.gqs = grad_q->stride;
-  a.gk = grad_k->data, a.gks = grad_k->stride;
-  a.gv = grad_v->data, a.gvs = grad_v->stride;
+  a.y = y->data, a.ys = pitch(*y);
+  a.gy = grad_y->data, a.gys = pitch(*grad_y);
+  a.gq = grad_q->data, a.gqs = pitch(*grad_q);
+  a.gk = grad_k->data, a.gks = pitch(*grad_k);
+  a.gv = grad_v->data, a.gvs = pitch(*grad_v);
   a.lse = const_cast<float *>(lse);
   return with_workspace(c, reinterpret_cast<hipStream_t>(stream), [&](void *ws, size_t *need) {
     return launch_window_grads(a, A->q.type, ws, need, reinterpret_cast<hipStream_t>(stream));
@@ -2967,12 +2970,12 @@ int fst_window_attention_step(fst_ctx *c, const fst_matrix *q, const fst_matrix 
   DeviceGuard g(c->device);
   if (!g.ok) return FST_ERR_HIP;
   WinStepArgs a{};
-  a.q = q->data, a.qs = q->stride;
-  a.k = k->data, a.ks = k->stride;
-  a.v = v->data, a.vs = v->stride;
-  a.y = y->data, a.ys = y->stride;
-  a.kc = k_cache->data, a.kcs = k_cache->stride;
-  a.vc = v_cache->data, a.vcs = v_cache->stride;
+  a.q = q->data, a.qs = pitch(*q);
+  a.k = k->data, a.ks = pitch(*k);
+  a.v = v->data, a.vs = pitch(*v);
+  a.y = y->data, a.ys = pitch(*y);
+  a.kc = k_cache->data, a.kcs = pitch(*k_cache);
+  a.vc = v_cache->data, a.vcs = pitch(*v_cache);
   a.pos = pos;
   a.slot = slot;
   a.slots = num_slots;
@@ -3004,10 +3007,10 @@ int fst_window_attention_fill(fst_ctx *c, int32_t num_seqs, const int32_t *offse
   DeviceGuard g(c->device);
   if (!g.ok) return FST_ERR_HIP;
   WinFillArgs a{};
-  a.k = k->data, a.ks = k->stride;
-  a.v = v->data, a.vs = v->stride;
-  a.kc = k_cache->data, a.kcs = k_cache->stride;
-  a.vc = v_cache->data, a.vcs = v_cache->stride;
+  a.k = k->data, a.ks = pitch(*k);
+  a.v = v->data, a.vs = pitch(*v);
+  a.kc = k_cache->data, a.kcs = pitch(*k_cache);
+  a.vc = v_cache->data, a.vcs = pitch(*v_cache);
   a.off = offset;
   a.slot = slot;
   a.N = k->rows;

@@ -67,7 +67,8 @@ __device__ __noinline__ void exact_rows(T *o, int left, const T *s_q, const T *s
       for (int r = 0; r < 4; ++r)
         past[r] = fmaf((float)s_q[i * LD<T, PA> + d], (float)s_s[(c + r) * LD<T, PA> + d],
                        past[r]);
-    for (int row = 0; row <= i; ++row) {
+    // (four NaN stay such)
+    for (int row = 0; row <= i && !all_nan(past * f_past + now); ++row) {
       float p = 0.0f;
       for (int d = 0; d < A; ++d)
         p = fmaf((float)s_q[i * LD<T, PA> + d], (float)s_k[row * LD<T, PA> + d], p);
@@ -549,7 +550,7 @@ long long unit_steps(const LinCall &c, int type, int jobs) {
   const int slice = slice_of(type, c.V);
   const long long groups = (long long)c.H * ((c.V + slice - 1) / slice);
   if (c.n * groups * jobs >= 256 || c.N / c.n <= 256) return 0;
-  const long long steps = c.N * groups / 768;
+  const long long steps = c.N * groups / 512;
   return steps <= CHUNK ? CHUNK : (steps + CHUNK - 1) / CHUNK * CHUNK;
 }
 
@@ -576,7 +577,8 @@ hipError_t launch_states(const LinArgs &a, const LinJob *all, int jobs, int type
   return hipGetLastError();
 }
 
-constexpr long long MAX_ACROSS = 65535;  // of a grid's second dimension
+constexpr long long MAX_ACROSS = 65535;    // of a grid's second dimension
+constexpr long long MAX_ROWS = 1 << 23;    // of a step
 
 bool too_large(const LinCall &c) {
   const int most = c.K > c.V ? c.K : c.V;
@@ -649,7 +651,7 @@ static void linear_step_as(const LinStepArgs &a, bool four, hipStream_t s) {
 }
 
 hipError_t launch_linear_step(const LinStepArgs &a, int type, hipStream_t s) {
-  if (a.H > MAX_ACROSS) return hipErrorInvalidValue;
+  if (a.H > MAX_ACROSS || a.n > MAX_ROWS) return hipErrorInvalidValue;
   const bool four = a.B % 4 == 0 && reinterpret_cast<uintptr_t>(a.in) % 16 == 0 &&
                     reinterpret_cast<uintptr_t>(a.out) % 16 == 0;
   if (type == FST_F32)

@@ -366,6 +366,10 @@ __device__ __forceinline__ void store_four(T *row, int c, int width, const float
   }
 }
 
+__device__ __forceinline__ bool all_nan(const float4v &x) {
+  return x[0] != x[0] && x[1] != x[1] && x[2] != x[2] && x[3] != x[3];
+}
+
 // Of the same four, as they were written: whether one is no number, and x in the
 // place of those that are none.
 template <typename T>

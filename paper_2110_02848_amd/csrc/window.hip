@@ -39,6 +39,7 @@ constexpr int QT_OF = sizeof(T) == 2 ? 2 : 1;
 template <typename T>
 constexpr int BLOCK_OF = 16 * QT_OF<T> * WNW;  // queries, or keys, of a workgroup
 constexpr int FEW = 64;              // frames
+constexpr int MAX_CUT = 256;         // first frames whose queries are cut into units
 constexpr float LOG2 = 0.69314718055994530942f, LOG2E = 1.44269502162933349609375f;
 
 // Wavefronts of a SIMD, at least, of the kernels below.  Two have half of its
@@ -139,7 +140,8 @@ __device__ __noinline__ float4v exact_row(const T *q, const T *k, long long ks, 
     const float p = exp2_of(dot(q, k + s * ks, D) * c - m);
 #pragma unroll
     for (int r = 0; r < 4; ++r)
-      if (d0 + r < D) x[r] = fmaf(p, (float)v[s * vs + d0 + r], x[r]);
+      x[r] = fmaf(p, d0 + r < D ? (float)v[s * vs + d0 + r] : p, x[r]);
+    if (all_nan(x)) break;  // (and so they stay)
   }
   return x;
 }
@@ -408,7 +410,8 @@ __device__ __noinline__ float4v exact_dq(const T *q, const T *gy, const T *k, lo
     const float d = e * (dot(gy, v + s * vs, D) - delta) * up;
 #pragma unroll
     for (int r = 0; r < 4; ++r)
-      if (d0 + r < D) x[r] = fmaf(d, (float)k[s * ks + d0 + r], x[r]);
+      x[r] = fmaf(d, d0 + r < D ? (float)k[s * ks + d0 + r] : d, x[r]);
+    if (all_nan(x)) break;
   }
   return x;
 }
@@ -432,11 +435,11 @@ __device__ __noinline__ TwoFours exact_dkv(const T *q, long long qs, const T *gy
     const float d =
         sees_one(t, window, sinks) ? 0.0f : e * (dot(gt, v, D) - delta[t * H]) * up;
 #pragma unroll
-    for (int r = 0; r < 4; ++r)
-      if (d0 + r < D) {
-        x.k[r] = fmaf(d, (float)qt[d0 + r], x.k[r]);
-        x.v[r] = fmaf(e, (float)gt[d0 + r], x.v[r]);
-      }
+    for (int r = 0; r < 4; ++r) {
+      x.k[r] = fmaf(d, d0 + r < D ? (float)qt[d0 + r] : d, x.k[r]);
+      x.v[r] = fmaf(e, d0 + r < D ? (float)gt[d0 + r] : e, x.v[r]);
+    }
+    if (all_nan(x.k) && all_nan(x.v)) break;
   }
   return x;
 }
@@ -599,7 +602,7 @@ __device__ __forceinline__ void dq_block(const WinArgs &a, const Unit &u, int h,
 // Whether the queries outside the window of a sequence's first frames are cut into
 // units: where there are more than one of them.
 __device__ __forceinline__ bool in_units(const WinArgs &a, const Unit &u) {
-  return a.sinks > 0 && u.len > a.window && u.len > a.unit;
+  return a.part && u.len > a.window && u.len > a.unit;
 }
 // Sums [2][P] for a first frame of such a sequence: its block's own, and unit j's.
 // Such sequences are longer than a unit, so floor(b / unit) differs, and floor(2 b /
@@ -1353,10 +1356,12 @@ hipError_t launch_window_grads(WinArgs a, int type, void *ws, size_t *need, hipS
   const int D = a.D;
   const size_t delta = ((size_t)a.N * a.H + 3) / 4 * 4;
   // (a sequence has to be longer than the window, and than a unit, for the queries of
-  // its first frames to be cut; units give small calls 256 workgroups)
+  // its first frames to be cut; units give small calls 256 workgroups; many first
+  // frames are workgroups enough)
   const long long unit = a.N * a.G / 256 / 128 * 128;
   a.unit = unit < 128 ? 128 : unit > 512 ? 512 : unit;
-  const bool cut = a.sinks > 0 && a.N > a.window && a.N > a.unit;
+  const bool cut =
+      a.sinks > 0 && a.sinks <= MAX_CUT && a.N > a.window && a.N > a.unit;
   const size_t first = cut ? (size_t)a.G * a.sinks * 2 * padded(D) : 0;
   const size_t own = (a.N / a.unit + 1) * first, part = (2 * a.N / a.unit + 1) * first;
   *need = (4 + delta + own + part) * sizeof(float);
@@ -1366,7 +1371,8 @@ hipError_t launch_window_grads(WinArgs a, int type, void *ws, size_t *need, hipS
   a.delta = p + 4;
   a.own = p + 4 + delta;
   a.part = cut ? a.own + own : nullptr;
-  const bool wide = wide_rows(type_bytes(type), D, {a.qs, a.ks, a.vs, a.ys, a.gys, a.gqs, a.gks, a.gvs},
+  const bool wide = wide_rows(type_bytes(type), D,
+                              {a.qs, a.ks, a.vs, a.ys, a.gys, a.gqs, a.gks, a.gvs},
                               {a.q, a.k, a.v, a.y, a.gy, a.gq, a.gk, a.gv});
   return FOR_FORM(backward_as, a, s);
 }
@@ -1374,7 +1380,7 @@ hipError_t launch_window_grads(WinArgs a, int type, void *ws, size_t *need, hipS
 hipError_t launch_window_step(WinStepArgs a, int type, void *ws, size_t *need, hipStream_t s) {
   const int D = a.D, E = a.H / a.G;
   const long long groups = (long long)a.G * ((E + 15) / 16);
-  if (groups > MAX_ACROSS || a.H > MAX_ACROSS) return hipErrorInvalidValue;
+  if (groups > MAX_ACROSS || a.H > MAX_ACROSS || a.n > MAX_BLOCKS) return hipErrorInvalidValue;
   // enough workgroups for the card, none with less than three tiles a wavefront: the
   // parts' join is a launch of its own (8 query and 2 key heads of 64, bf16, replayed:
   // one stream of 256 frames 7.6 us with parts of one tile, 6.3 in one piece; of 2,000

@@ -943,8 +943,8 @@ class Composer:
         return self._pass.window(n, _array(offset, "offset", self._i32, n + 1), *how, q, k,
                                  v), how[0]
 
-    def window_attention_step(self, q, k, v, pos, k_cache, v_cache, heads, kv_heads=None,
-                              window=1, sinks=0, slot=None, scale=None, stream=None):
+    def window_attention_step(self, q, k, v, pos, k_cache, v_cache, heads, kv_heads=None, *,
+                              window, sinks=0, slot=None, scale=None, stream=None):
         """One step of many streams: row i of q, k and v is the frame of
         position pos[i] (int32 [n]; negative: an idle row) of the stream whose
         keys and values lie in the sinks + window rows from slot[i] * (sinks +

@@ -454,6 +454,69 @@ def test_window_rows_see_no_others(comp, typ, bad):
         same(got, "gv", keys)
 
 
+@pytest.mark.parametrize("typ", ["f32", "f16", "bf16"])
+def test_window_of_many_first_frames(comp, typ):
+    """More of them than are cut into units, and more than there are frames."""
+    q, k, v, gy = _window_inputs([700, 30], 2, 1, 32, typ)
+    for sinks in (257, 300, 256, 2 ** 30):
+        _check_window(comp, q, k, v, gy, [0, 700, 730], 2, 1, 10, sinks)
+
+
+@pytest.mark.parametrize("typ", ["f32", "bf16"])
+def test_all_of_it_no_number(comp, typ):
+    """Every input NaN: every result is, in no time worth speaking of."""
+    q, k, v, gy = (torch.full_like(t, NAN) for t in _window_inputs([3000], 4, 2, 64, typ))
+    off = _i32([0, 3000])
+    how = dict(heads=4, kv_heads=2, window=2000, sinks=4)
+    r = comp.window_attention(q, k, v, off, **how)
+    g = comp.window_attention_grads(q, k, v, off, r["y"], r["lse"], gy, **how)
+    d = torch.full((4,), -0.1, device="cuda")
+    lin = comp.linear_attention(q, q, gy, d, off)
+    for t in (r["y"], g["q"][1:], g["k"], g["v"], lin["y"], lin["last"]):
+        assert t.isnan().all()
+
+
+def test_single_rows_of_any_stride(comp):
+    """One row has no distance to a next one: any is taken for it."""
+    q, k, v, d, st, gy, gl = _linear_inputs([1], 2, 16, 16, "f32")
+    far = torch.empty_strided((1, 32), (1 << 40, 1), device="cuda")
+    far.copy_(q)
+    a = comp.linear_attention(q, k, v, d, _i32([0, 1]), state=st)["y"]
+    assert torch.equal(comp.linear_attention(far, k, v, d, _i32([0, 1]), state=st)["y"], a)
+    a = comp.window_attention(q, q, q, _i32([0, 1]), heads=2)
+    b = comp.window_attention(far, far, far, _i32([0, 1]), heads=2)
+    assert torch.equal(a["y"], b["y"]) and torch.equal(a["lse"], b["lse"])
+    g = [comp.window_attention_grads(t, t, t, _i32([0, 1]), a["y"], a["lse"], t, heads=2)
+         for t in (q, far)]
+    assert all(torch.equal(g[0][c], g[1][c]) for c in "qkv") and not g[0]["q"].any()
+
+
+def test_rows_too_far_apart_are_refused(comp):
+    from paper_2110_02848_amd import gpu
+    wide = torch.zeros(2, (1 << 22) + 1, dtype=torch.float16, device="cuda")
+    x, d = wide[:, :16], torch.zeros(2, device="cuda")
+    near = torch.zeros(2, 16, dtype=torch.float16, device="cuda")
+    off = _i32([0, 2])
+    calls = [lambda: comp.linear_attention(x, near, near, d, off),
+             lambda: comp.linear_attention_grads(near, near, near, d, off, x),
+             lambda: comp.window_attention(near, x, near, off, heads=2),
+             lambda: comp.window_attention_grads(near, near, near, off, near,
+                                                 torch.zeros(2, 2, device="cuda"), x, heads=2)]
+    for call in calls:
+        with pytest.raises(gpu.FstError) as e:
+            call()
+        assert e.value.code == gpu.FST_ERR_TOO_LARGE
+    # as far as may be, and queries of the window attention any way
+    x = torch.zeros(2, 1 << 22, dtype=torch.float16, device="cuda")[:, :16]
+    x.normal_()
+    want = comp.linear_attention(x.contiguous(), near, near + 1, d, off)["y"]
+    assert torch.equal(comp.linear_attention(x, near, near + 1, d, off)["y"], want)
+    q = wide[:, :16]
+    q.normal_()
+    want = comp.window_attention(q.contiguous(), near + 1, near + 2, off, heads=2)["y"]
+    assert torch.equal(comp.window_attention(q, near + 1, near + 2, off, heads=2)["y"], want)
+
+
 def test_window_leaves_rows_of_no_sequence(comp):
     from paper_2110_02848_amd import gpu
     import ctypes
@@ -684,9 +747,10 @@ def test_together_in_float32(comp):
         ref.within(c, got[c], w, 2.0 ** -12 * w.abs().max())
 
 
-def test_together_the_same_again_and_as_a_graph(comp):
+@pytest.mark.parametrize("D,typ", [(64, "bf16"), (128, "f16"), (128, "f32"), (40, "bf16")])
+def test_together_the_same_again_and_as_a_graph(comp, D, typ):
     """Bit for bit: repeats, and replays of a graph between other calls."""
-    L = _Layer(comp, [300, 0, 129, 1], 4, 2, 64, 70, 3, "bf16")
+    L = _Layer(comp, [700, 0, 129, 1], 4, 2, D, 70, 3, typ)
     want = L.run()
     again = L.run()
     for c in want:
@@ -696,7 +760,7 @@ def test_together_the_same_again_and_as_a_graph(comp):
     s.wait_stream(torch.cuda.current_stream())
     with torch.cuda.graph(graph, stream=s):
         out = L.run()
-    bigger = _Layer(comp, [900, 400], 4, 2, 64, 100, 3, "bf16")
+    bigger = _Layer(comp, [1900, 400], 4, 2, D, 100, 3, typ)
     for _ in range(3):
         for t in out.values():
             t.fill_(5.0)
