@@ -150,8 +150,9 @@ __global__ __launch_bounds__(NT) void k_norms_wide(NormArgs a, int rows, int lan
 }
 
 // Any heads, up to 64 E wide.  A wavefront takes one: lane l holds numbers l, l +
-// 64, ..  BACK: gradients;
-// a workgroup's sums for w go to a row of `part`, sides side by side.
+// 64, ..  BACK: gradients; a workgroup's sums for w go to a row of `part`, sides side by
+// side.  Bound by the way from a head's numbers to its results (1,266 rows of 5 + 5
+// heads of 43 f32: 6 us, back 10; 14 where the next head's loads had to wait).
 template <typename T, int E, bool BACK>
 __global__ __launch_bounds__(NT) void k_norms(NormArgs a) {
   extern __shared__ float s_dyn[];
@@ -161,7 +162,25 @@ __global__ __launch_bounds__(NT) void k_norms(NormArgs a) {
   float *s_z = s_dyn + 2 * a.P + w * a.D;                          // a wavefront's [D]
   const int heads = a.side[0].heads + a.side[1].heads;
   float gw[2][E] = {};
+  // a head's numbers, on their way while the one before is worked on
+  T nx[E] = {}, ng[E] = {};
+  const auto fetch = [&](long long row, int hh) {
+    const int o = hh >= a.side[0].heads;
+    const NormSide &sd = a.side[o];
+    const long long at = (long long)(hh - (o ? a.side[0].heads : 0)) * a.D;
+    const T *x = static_cast<const T *>(sd.x) + row * sd.xs + at;
+    const T *g = static_cast<const T *>(sd.g) + row * sd.gs + at;
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const int d = e * WAVE + lane;
+      if (d < a.D) {
+        nx[e] = x[d];
+        if constexpr (BACK) ng[e] = g[d];
+      }
+    }
+  };
   for (long long row = blockIdx.x; row < a.N; row += gridDim.x) {
+    if (w < heads) fetch(row, w);
     __syncthreads();
     for (int i = threadIdx.x; i < a.P; i += NT) s_turn[i] = turn(a.pos[row], a.freq[i]);
     __syncthreads();
@@ -169,16 +188,15 @@ __global__ __launch_bounds__(NT) void k_norms(NormArgs a) {
       const int o = hh >= a.side[0].heads;
       const NormSide &sd = a.side[o];
       const long long at = (long long)(hh - (o ? a.side[0].heads : 0)) * a.D;
-      const T *x = static_cast<const T *>(sd.x) + row * sd.xs + at;
-      const T *g = static_cast<const T *>(sd.g) + row * sd.gs + at;
       T *y = static_cast<T *>(sd.y) + row * sd.ys + at;
-      float xv[E], sum = 0.0f;
+      float xv[E], gv[E], sum = 0.0f;
 #pragma unroll
       for (int e = 0; e < E; ++e) {
-        const int d = e * WAVE + lane;
-        xv[e] = d < a.D ? (float)x[d] : 0.0f;
+        xv[e] = (float)nx[e];
+        gv[e] = (float)ng[e];
         sum = fmaf(xv[e], xv[e], sum);
       }
+      if (hh + NWAVES < heads) fetch(row, hh + NWAVES);
 #pragma unroll
       for (int m = 32; m; m >>= 1) sum += __shfl_xor(sum, m, WAVE);
       const float r = 1.0f / sqrtf(sum / (float)a.D + a.eps);
@@ -186,7 +204,7 @@ __global__ __launch_bounds__(NT) void k_norms(NormArgs a) {
 #pragma unroll
       for (int e = 0; e < E; ++e) {
         const int d = e * WAVE + lane;
-        if (d < a.D) s_z[d] = BACK ? (float)g[d] : xv[e] * r * sd.w[d];
+        if (d < a.D) s_z[d] = BACK ? gv[e] : xv[e] * r * sd.w[d];
       }
       __builtin_amdgcn_wave_barrier();
       float t[E];
@@ -333,11 +351,12 @@ void launch_as(const NormArgs &a, int type, int blocks, hipStream_t s) {
     launch_of<bf16, BACK>(a, blocks, s);
 }
 
-// Workgroups: at most `most`, none without rows.
+// Workgroups: at most `most`, none without rows, no more than their rows' turns ask for.
 int workgroups(const NormArgs &a, int type, bool back, int most) {
   const long long rows = wide(a, type_bytes(type), back) ? rows_at_once(a) : 1;
   const long long n = (a.N + rows - 1) / rows;
-  return (int)(n < most ? n : most);
+  const long long turns = n > most ? (n + most - 1) / most : 1;
+  return (int)((n + turns - 1) / turns);
 }
 
 }  // namespace
@@ -348,8 +367,8 @@ hipError_t launch_norms(const NormArgs &a, int type, hipStream_t s) {
 }
 
 hipError_t launch_norms_grads(NormArgs a, int type, void *ws, size_t *need, hipStream_t s) {
-  // (few: a workgroup's sums for the weights cost as much as some rows)
-  const int blocks = workgroups(a, type, true, 512);
+  // (k_norms_wide: few, a workgroup's sums for the weights cost as much as some rows)
+  const int blocks = workgroups(a, type, true, wide(a, type_bytes(type), true) ? 512 : 1024);
   *need = (size_t)blocks * 2 * a.D * sizeof(float);
   if (!ws) return hipSuccess;
   a.part = static_cast<float *>(ws);
