@@ -79,8 +79,10 @@ __device__ __forceinline__ Frag<T> pack(const float4v &a, const float4v &b) {
   return pack<T>(x);
 }
 
-// Rows of P numbers, 16 bytes between them, so that the reads of 16 lanes a
-// row apart meet different banks.
+// Rows of P numbers, 16 bytes between them: reads of 16 lanes a row apart meet
+// different banks but for one, reads that transpose take twice their time (no bound
+// of the kernels that use them: linear attention, 64 x 2,000 x 8 x 128 x 128 bf16, took
+// as long with rows as Packed below has them).
 template <typename T, int P>
 constexpr int LD = P + PER<T>;
 template <typename T, int P, int R>
@@ -221,14 +223,16 @@ struct Stage {
 };
 
 // Tiles whose rows lie side by side, without room between them: 16-byte group g of
-// row r lies at group g ^ swizzle(r), so that a read of 16 rows, and one that
-// transposes four, meet different banks.  They come from memory straight to LDS.
+// row r lies at group g ^ swizzle(r), so that reads meet different banks: a read of 16
+// rows goes by 16 lanes, rows 0 .. 3 and 12 .. 15 of a group of numbers and the other
+// eight of the next (or the other way round), one that transposes by 32 lanes, eight
+// rows of 32 bytes.  They come from memory straight to LDS.
 template <typename T, int P>
 struct Packed {
   static constexpr int GROUPS = P / PER<T>, ROW = P * (int)sizeof(T);
 
   static __device__ __forceinline__ int swizzle(int r) {
-    return GROUPS == 8 ? ((r >> 1 & 3) << 1) | (r >> 3 & 1) : ((r & 7) << 1) | (r >> 3 & 1);
+    return GROUPS == 8 ? r & 6 : (r & 7) << 1;
   }
   static __device__ __forceinline__ const char *at(const char *t, int r, int g) {
     return t + r * ROW + ((g ^ swizzle(r)) << 4);
