@@ -150,6 +150,11 @@ __device__ __noinline__ float4v exact_row(const T *q, const T *k, long long ks, 
 // way while one is multiplied.  m is the maximum that exponents are taken from: it
 // follows a row's maximum only once that is past it by LATE (powers of 2), so that
 // most tiles leave the sums as they are; p stays below 2^LATE.
+//
+// Bound by the vector units: of a wavefront's 160 or so instructions for a tile, 32 are
+// exponentials, which take four times as long (40,000 x 8 x 64 bf16, window 512: 87 to
+// 98 us as the card's clock goes, 64 % of cycles on the vector units, 24 % on the matrix
+// cores; 16 x 2,000 x 16 x 128, window 1,000: 220 us, 44 and 29 %).
 template <typename T, int P, bool WIDE>
 __global__ __launch_bounds__(WNT, MIN_WAVES<T>) void k_window(WinArgs a) {
   constexpr int QT = QT_OF<T>, DT = P / 16, DS = P / 32, TILE = KEYS * P * (int)sizeof(T);
@@ -337,7 +342,8 @@ __global__ __launch_bounds__(WNT, MIN_WAVES<T>) void k_window(WinArgs a) {
 // ---------------------------------------------------------------------------
 
 // delta = y . dy of each row and head, a lane for 16 bytes of it; float16: the largest
-// lengths of rows of dy and v, whose product bounds dS.  Bound by memory.
+// lengths of rows of dy and v, whose product bounds dS.  Bound by memory (200 MB of y
+// and dy: 31 us).
 template <typename T, int P, bool WIDE>
 __global__ __launch_bounds__(WNT) void k_window_delta(WinArgs a) {
   constexpr int LANES = P / PER<T>, EACH = WNT / LANES;
@@ -959,7 +965,10 @@ __device__ __forceinline__ void sinks_block(const WinArgs &a, const Unit &u, int
 }
 
 // Workgroups of all three: blocks of keys, blocks of queries, units for the first
-// frames.
+// frames.  Nine products where seven are needed: scores and dy v^T are computed for dq
+// and again for dk and dv.  Bound by what a wavefront waits for between them with
+// two a SIMD (16 x 2,000 x 16 heads of 128 bf16, window 1,000: 720 to 740 us, 28 % of
+// cycles on the matrix cores, 28 % on the vector units).
 template <typename T, int P, bool WIDE>
 __global__ __launch_bounds__(WNT, MIN_WAVES<T>) void k_window_back(WinArgs a) {
   extern __shared__ __attribute__((aligned(16))) char s_dyn[];
@@ -990,7 +999,7 @@ __global__ __launch_bounds__(WNT, MIN_WAVES<T>) void k_window_back(WinArgs a) {
 // delta from y as it was rounded is off by half a spacing of y, which is next to
 // nothing beside dS of many frames but as much as the rounding of dS beside few:
 // queries of a sequence's first block, and of windows up to FEW frames, have it
-// summed again from P and dy v^T.
+// summed again from P and dy v^T (the same case: 11 us).
 template <typename T, int P, bool WIDE>
 __global__ __launch_bounds__(WNT, MIN_WAVES<T>) void k_window_sums(WinArgs a, int every) {
   constexpr int BLOCK = BLOCK_OF<T>;
@@ -1001,7 +1010,8 @@ __global__ __launch_bounds__(WNT, MIN_WAVES<T>) void k_window_sums(WinArgs a, in
   if (u.lo < u.hi) dq_block<T, P, WIDE, true>(a, u, blockIdx.y, s_dyn);
 }
 
-// Gradients of first frames whose sums lie in parts: their own, then the units'.
+// Gradients of first frames whose sums lie in parts: their own, then the units' (the
+// same case: 5 us, a launch and a trip to memory).
 template <typename T, int P>
 __global__ __launch_bounds__(P) void k_window_first(WinArgs a) {
   Unit u;
@@ -1035,6 +1045,8 @@ __device__ __forceinline__ int ring(int p, int window, int sinks) {
 // part of its cache, 32 frames a wavefront at a time: k straight from memory as
 // an operand, v through LDS of the wavefront's own.  The row's own frame comes
 // from k and v, and the first part writes it to the cache, where no one reads it.
+// Bound by memory (256 rows of 16 + 4 heads of 128 f16, window 1,000: 83 us for 441 MB,
+// 5.3 TB/s); few rows by a load's way and the parts' join.
 template <typename T, int P, bool WIDE>
 __global__ __launch_bounds__(WNT) void k_window_step(WinStepArgs a) {
   constexpr int DT = P / 16, DS = P / 32, GROUPS = P / PER<T>, LOADS = 32 * GROUPS / WAVE;
