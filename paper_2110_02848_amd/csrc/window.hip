@@ -965,7 +965,7 @@ __device__ __forceinline__ void sinks_block(const WinArgs &a, const Unit &u, int
 }
 
 // Workgroups of all three: blocks of keys, blocks of queries, units for the first
-// frames.  Nine products where seven are needed: scores and dy v^T are computed for dq
+// frames.  Seven products where five are needed: scores and dy v^T are computed for dq
 // and again for dk and dv.  Bound by what a wavefront waits for between them with
 // two a SIMD (16 x 2,000 x 16 heads of 128 bf16, window 1,000: 720 to 740 us, 28 % of
 // cycles on the matrix cores, 28 % on the vector units).
