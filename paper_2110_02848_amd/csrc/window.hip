@@ -255,27 +255,26 @@ __global__ __launch_bounds__(WNT, MIN_WAVES<T>) void k_window(WinArgs a) {
           }
         }
       }
-      float shift[QT];
+      float top[QT];  // a lane's own, until a row is late
       bool late = false;
 #pragma unroll
       for (int i = 0; i < QT; ++i) {
-        float top = fmaxf(fmaxf(x[0][i][0], x[0][i][1]), x[0][i][2]);
-        top = fmaxf(top, x[0][i][3]);
+        top[i] = fmaxf(fmaxf(x[0][i][0], x[0][i][1]), x[0][i][2]);
+        top[i] = fmaxf(top[i], x[0][i][3]);
 #pragma unroll
         for (int kt = 1; kt < 4; ++kt) {
-          top = fmaxf(fmaxf(top, x[kt][i][0]), x[kt][i][1]);
-          top = fmaxf(fmaxf(top, x[kt][i][2]), x[kt][i][3]);
+          top[i] = fmaxf(fmaxf(top[i], x[kt][i][0]), x[kt][i][1]);
+          top[i] = fmaxf(fmaxf(top[i], x[kt][i][2]), x[kt][i][3]);
         }
-        top = column_max(top);
-        shift[i] = fmaxf(m[i], top);
-        late = late || !((shift[i] - m[i]) * c <= LATE);
+        late = late || !((top[i] - m[i]) * c <= LATE);
       }
       if (__any(late)) {
 #pragma unroll
         for (int i = 0; i < QT; ++i) {
           // (while a row has seen nothing, m is -infinity and the sums are 0)
-          const float less = shift[i] == -INFINITY ? 1.0f : exp2_of((m[i] - shift[i]) * c);
-          m[i] = shift[i];
+          const float shift = fmaxf(m[i], column_max(top[i]));
+          const float less = shift == -INFINITY ? 1.0f : exp2_of((m[i] - shift) * c);
+          m[i] = shift;
           l[i] *= less;
 #pragma unroll
           for (int d = 0; d < DT; ++d) o[d][i] *= less;
