@@ -152,9 +152,9 @@ __device__ __noinline__ float4v exact_row(const T *q, const T *k, long long ks, 
 // most tiles leave the sums as they are; p stays below 2^LATE.
 //
 // Bound by the vector units: of a wavefront's 160 or so instructions for a tile, 32 are
-// exponentials, which take four times as long (40,000 x 8 x 64 bf16, window 512: 87 to
-// 98 us as the card's clock goes, 64 % of cycles on the vector units, 24 % on the matrix
-// cores; 16 x 2,000 x 16 x 128, window 1,000: 220 us, 44 and 29 %).
+// exponentials, which take four times as long (40,000 x 8 x 64 bf16, window 512: 85 to
+// 96 us as the card's clock goes, 64 % of cycles on the vector units, 24 % on the matrix
+// cores; 16 x 2,000 x 16 x 128, window 1,000: 214 us, 44 and 29 %).
 template <typename T, int P, bool WIDE>
 __global__ __launch_bounds__(WNT, MIN_WAVES<T>) void k_window(WinArgs a) {
   constexpr int QT = QT_OF<T>, DT = P / 16, DS = P / 32, TILE = KEYS * P * (int)sizeof(T);

@@ -183,6 +183,17 @@ def test_linear_lengths_and_widths(comp, lens, H, K, V, typ, rev):
     _check_linear(comp, q, k, v, d, ref.offsets(lens), st, gy, gl, rev)
 
 
+@pytest.mark.parametrize("typ", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("n,H,K,V", [(37, 3, 64, 128), (16, 8, 41, 33), (1, 9, 8, 100),
+                                     (5, 1, 128, 60)])
+def test_linear_of_many_sequences_and_heads(comp, n, H, K, V, typ):
+    """Every job, head and slice of columns is some workgroup's, whatever is left of
+    the division by the card's eight XCDs."""
+    lens = [(7 * i) % 19 for i in range(n)] if n > 1 else [70]
+    q, k, v, d, st, gy, gl = _linear_inputs(lens, H, K, V, typ)
+    _check_linear(comp, q, k, v, d, ref.offsets(lens), st, gy, gl, False)
+
+
 @pytest.mark.parametrize("rev", [False, True])
 @pytest.mark.parametrize("typ", ["f32", "f16", "bf16"])
 @pytest.mark.parametrize("lens,H,K,V", [([1500], 2, 64, 64), ([700, 0, 403], 1, 33, 65),
