@@ -172,7 +172,8 @@ struct WinArgs {
   float scale;
   // workspace of the gradients
   float *delta;                     // [N, H]
-  uint32_t *most;                   // float16: largest lengths of rows of gy and v
+  float *most;                      // float16: workgroups' largest lengths of rows of gy
+  int mosts;                        // and v; how many
   float *own, *part;                // sums for gk and gv of cut sequences' first frames:
                                     // their blocks' own, and units' (or null)
   long long unit;                   // queries of a unit
