@@ -31,6 +31,7 @@ constexpr int CHUNK = 64;   // rows that are multiplied at once, 16 of them by a
 template <typename T>
 constexpr int SLICE_OF = sizeof(T) == 2 ? 64 : 32;
 constexpr int LNT = 256;    // threads of a step
+constexpr int MANY = 12;    // units of a sequence, from which k_linear_scan has parts
 static_assert(CHUNK == 16 * 4, "a wavefront has 16 rows");
 
 // e^(g n) for 0 <= n <= CHUNK, from 64 bits: chunk after chunk multiplies them.
@@ -404,48 +405,66 @@ __global__ __launch_bounds__(256 * CG, (MIN_WAVES<T, PA, CG>)) void k_linear(Lin
 }
 
 // From the units' own contributions to the states entering them, in place: a lane
-// takes an element of a head's state, its workgroup's wavefronts a part of a
-// sequence's units each.  What each part makes of a zero state meets in LDS; a part's
-// units stay in registers, unless there are more than AHEAD of them.  Bound by two
-// trips to memory (63 units of 8 x 64 x 64: 8 us; 10 with one wavefront for all units).
+// takes an element of a head's state.  PARTS > 1: its workgroup's wavefronts a part of a
+// sequence's units each, and what each part makes of a zero state meets in LDS.  A
+// part's units stay in registers, unless there are more than AHEAD of them.  Bound by
+// two trips to memory (63 units of 8 x 64 x 64: 6 us).  Few units of many sequences
+// take one part, whose lanes have one exponential (4 units of 33 sequences, 5 x 128 x
+// 128: 16 us; four parts, all AHEAD units passed one by one: 132).
+template <int PARTS>
 __global__ __launch_bounds__(NT) void k_linear_scan(LinArgs a) {
-  constexpr int AHEAD = 32;
-  __shared__ float s_sum[NWAVES][WAVE];
+  constexpr int AHEAD = 32, STEP = 8;
+  __shared__ float s_sum[PARTS][WAVE];
   const LinJob &job = a.job[blockIdx.z];
   const int AB = job.A * job.B, all = AB * a.H;
   const int lane = threadIdx.x & (WAVE - 1);
-  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
-  const int at = blockIdx.x * WAVE + lane, e = at < all ? at : all - 1;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE), w = PARTS > 1 ? wave : 0;
+  const int at = (PARTS > 1 ? blockIdx.x : blockIdx.x * NWAVES + wave) * WAVE + lane;
+  const int e = at < all ? at : all - 1;
   const int s = blockIdx.y;
   const long long b = clamped(a.off[s], 0, a.N);
   const long long len = clamped(a.off[s + 1], b, a.N) - b;
   const long long n = len > 0 ? over_steps(len - 1, a.unit) + 1 : 1;
-  const long long share = (n + NWAVES - 1) / NWAVES, u0 = w * share;
+  const long long share = (n + PARTS - 1) / PARTS, u0 = w * share;
   const long long u1 = u0 + share < n ? u0 + share : n;
   float *p = job.units + rows_before(b, s, a.unit) * all + e;
+  float S = job.state ? job.state[(long long)s * all + e] : 0.0f;
   float x[AHEAD];
 #pragma unroll
-  for (int c = 0; c < AHEAD; ++c) x[c] = u0 + c < u1 ? p[(u0 + c) * all] : 0.0f;
+  for (int c0 = 0; c0 < AHEAD; c0 += STEP)
+    if (u0 + c0 < u1) {
+#pragma unroll
+      for (int c = c0; c < c0 + STEP; ++c) x[c] = u0 + c < u1 ? p[(u0 + c) * all] : 0.0f;
+    }
   const float g = a.log_decay[e / AB];
   const double d = (g < -1e4f ? -1e4 : (double)g) * (double)a.unit, whole = exp(d);
   const float kh = (float)whole;
   const float kl = fabsf(kh) < INFINITY ? (float)(whole - (double)kh) : 0.0f;
-  float sum = 0.0f;
+  if constexpr (PARTS > 1) {
+    float sum = 0.0f;
 #pragma unroll
-  for (int c = 0; c < AHEAD; ++c)
-    if (u0 + c < u1) sum = fmaf(kh, sum, fmaf(kl, sum, x[c]));
-  for (long long u = u0 + AHEAD; u < u1; ++u) sum = fmaf(kh, sum, fmaf(kl, sum, p[u * all]));
-  s_sum[w][lane] = sum;
-  __syncthreads();
-  float S = job.state ? job.state[(long long)s * all + e] : 0.0f;
-  const float over = w ? (float)exp(d * (double)share) : 1.0f;
-  for (int q = 0; q < w; ++q) S = fmaf(over, S, s_sum[q][lane]);
+    for (int c0 = 0; c0 < AHEAD; c0 += STEP)
+      if (u0 + c0 < u1) {
+#pragma unroll
+        for (int c = c0; c < c0 + STEP; ++c)
+          if (u0 + c < u1) sum = fmaf(kh, sum, fmaf(kl, sum, x[c]));
+      }
+    for (long long u = u0 + AHEAD; u < u1; ++u) sum = fmaf(kh, sum, fmaf(kl, sum, p[u * all]));
+    s_sum[w][lane] = sum;
+    __syncthreads();
+    const float over = w ? (float)exp(d * (double)share) : 1.0f;
+    for (int q = 0; q < w; ++q) S = fmaf(over, S, s_sum[q][lane]);
+  }
   if (at >= all) return;
 #pragma unroll
-  for (int c = 0; c < AHEAD; ++c)
-    if (u0 + c < u1) {
-      p[(u0 + c) * all] = S;
-      S = fmaf(kh, S, fmaf(kl, S, x[c]));
+  for (int c0 = 0; c0 < AHEAD; c0 += STEP)
+    if (u0 + c0 < u1) {
+#pragma unroll
+      for (int c = c0; c < c0 + STEP; ++c)
+        if (u0 + c < u1) {
+          p[(u0 + c) * all] = S;
+          S = fmaf(kh, S, fmaf(kl, S, x[c]));
+        }
     }
   for (long long u = u0 + AHEAD; u < u1; ++u) {
     const float y = p[u * all];
@@ -581,11 +600,17 @@ bool wide_rows(const LinCall &c, size_t e, std::initializer_list<long long> stri
   return true;
 }
 
-// Steps of a unit, 0: sequences are not cut.
+// Steps of a unit, 0: sequences are not cut.  Uncut, a call takes as long as its longest
+// sequence; cut, as all rows twice and the states, which are worth it where
+// workgroups are few for the sequences' length (on average).  bf16, cut and uncut: 8
+// heads of 64, 8 sequences of 1,200: 35 and 50 us; of 600: 33 and 30; 24 of 1,200: 56 and
+// 50; 8 heads of 128, 4 of 600: 48 and 54; 8 of 600: 69 and 55; 16 of 1,200: 114 and 92;
+// 4 heads of 128, 16 of 1,200: 77 and 91.
 long long unit_steps(const LinCall &c, int type, int jobs) {
   const int slice = slice_of(type, c.V);
   const long long groups = (long long)c.H * ((c.V + slice - 1) / slice);
-  if (c.n * groups * jobs >= 256 || c.N / c.n <= 256) return 0;
+  const long long all = c.n * groups * jobs, length = c.N / c.n;
+  if (all >= 256 || length <= 256 || 14 * all > length) return 0;
   const long long steps = c.N * groups / 512;
   return steps <= CHUNK ? CHUNK : (steps + CHUNK - 1) / CHUNK * CHUNK;
 }
@@ -609,7 +634,10 @@ hipError_t launch_states(const LinArgs &a, const LinJob *all, int jobs, int type
   LinArgs b = a;
   for (int i = 0; i < jobs; ++i) b.job[i] = all[i];
   const long long n = (long long)a.H * all[0].A * all[0].B;
-  k_linear_scan<<<dim3((unsigned)((n + WAVE - 1) / WAVE), a.n, jobs), NT, 0, s>>>(b);
+  if (a.N / a.unit > MANY * (long long)a.n)
+    k_linear_scan<NWAVES><<<dim3((unsigned)((n + WAVE - 1) / WAVE), a.n, jobs), NT, 0, s>>>(b);
+  else
+    k_linear_scan<1><<<dim3((unsigned)((n + NT - 1) / NT), a.n, jobs), NT, 0, s>>>(b);
   return hipGetLastError();
 }
 

@@ -194,6 +194,13 @@ def test_linear_of_many_sequences_and_heads(comp, n, H, K, V, typ):
     _check_linear(comp, q, k, v, d, ref.offsets(lens), st, gy, gl, False)
 
 
+@pytest.mark.parametrize("typ", ["f32", "bf16"])
+@pytest.mark.parametrize("lens", [[9000], [9000] + [1] * 11])
+def test_linear_of_more_units_than_registers(comp, lens, typ):
+    q, k, v, d, st, gy, gl = _linear_inputs(lens, 1, 16, 8, typ)
+    _check_linear(comp, q, k, v, d, ref.offsets(lens), st, gy, gl, False)
+
+
 @pytest.mark.parametrize("rev", [False, True])
 @pytest.mark.parametrize("typ", ["f32", "f16", "bf16"])
 @pytest.mark.parametrize("lens,H,K,V", [([1500], 2, 64, 64), ([700, 0, 403], 1, 33, 65),
