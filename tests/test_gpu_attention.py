@@ -877,3 +877,24 @@ def test_arguments_that_the_binding_refuses(comp):
         comp.window_attention(q, k, v, off, heads=2, window=0)
     with pytest.raises(gpu.FstError):
         comp.linear_attention(q, k[:, :14], v, d, off)
+
+
+# ---------------------------------------------------------------------------
+# sizes, masks and magnitudes at their ends
+# ---------------------------------------------------------------------------
+
+@pytest.mark.parametrize("typ", ["f32", "f16", "bf16"])
+def test_window_of_heads_without_columns(comp, typ):
+    """Every score is 0: lse is the logarithm of how many frames a query sees."""
+    off, H, G, win, sinks = [0, 150, 150, 157], 4, 2, 70, 3
+    q, k = (torch.empty(157, 0, dtype=TYPES[typ], device="cuda") for _ in range(2))
+    how = dict(heads=H, kv_heads=G, window=win, sinks=sinks)
+    print(f"[window] {tuple(q.shape)} strides {q.stride()} {typ}", flush=True)
+    r = comp.window_attention(q, k, k, _i32(off), **how)
+    torch.cuda.synchronize()
+    count = torch.cat([ref.visible(b - a, win, sinks).sum(1) for a, b in zip(off, off[1:])])
+    want = torch.log(count.to(F64))[:, None].expand(-1, H)
+    # (a logarithm of at most 73 in powers of 2, 6.2, and its product with log 2)
+    ref.within("lse", r["lse"], want, torch.full_like(want, 16 * ref.U))
+    g = comp.window_attention_grads(q, k, k, _i32(off), r["y"], r["lse"], q, **how)
+    assert r["y"].shape == (157, 0) and all(g[c].shape == (157, 0) for c in "qkv")
