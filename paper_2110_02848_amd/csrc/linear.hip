@@ -582,6 +582,7 @@ hipError_t launch_range(LinArgs a, const LinJob *all, int lo, int hi, int type, 
     a.job[i - lo] = all[i];
     B = all[i].B > B ? all[i].B : B;
   }
+  if (B == 0) return hipSuccess;  // (no columns of results)
   a.slices = (B + slice_of(type, B) - 1) / slice_of(type, B);
   if (type == FST_F32) return launch_jobs<float, FULL>(a, hi - lo, all[lo].A, B, wide, s);
   if (type == FST_F16) return launch_jobs<f16, FULL>(a, hi - lo, all[lo].A, B, wide, s);
@@ -610,6 +611,7 @@ long long unit_steps(const LinCall &c, int type, int jobs) {
   const int slice = slice_of(type, c.V);
   const long long groups = (long long)c.H * ((c.V + slice - 1) / slice);
   const long long all = c.n * groups * jobs, length = c.N / c.n;
+  if (c.K == 0 || c.V == 0) return 0;  // (no states to cut by)
   if (all >= 256 || length <= 256 || 14 * all > length) return 0;
   const long long steps = c.N * groups / 512;
   return steps <= CHUNK ? CHUNK : (steps + CHUNK - 1) / CHUNK * CHUNK;

@@ -898,3 +898,19 @@ def test_window_of_heads_without_columns(comp, typ):
     ref.within("lse", r["lse"], want, torch.full_like(want, 16 * ref.U))
     g = comp.window_attention_grads(q, k, k, _i32(off), r["y"], r["lse"], q, **how)
     assert r["y"].shape == (157, 0) and all(g[c].shape == (157, 0) for c in "qkv")
+
+
+@pytest.mark.parametrize("typ", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("lens", [[10], [1000]])
+@pytest.mark.parametrize("K,V", [(0, 5), (5, 0), (0, 0), (100, 0), (0, 100)])
+def test_linear_of_heads_without_columns(comp, K, V, lens, typ):
+    """Zeros, whether or not sequences are long enough to be cut into units."""
+    q, k, v, d, st, gy, gl = _linear_inputs(lens, 2, K, V, typ)
+    off = _i32(ref.offsets(lens))
+    print(f"[linear] {tuple(q.shape)} {tuple(v.shape)} {typ} lengths {lens}", flush=True)
+    r = comp.linear_attention(q, k, v, d, off, state=st)
+    g = comp.linear_attention_grads(q, k, v, d, off, gy, state=st, grad_last=gl)
+    torch.cuda.synchronize()
+    for t, like in ((r["y"], v), (g["q"], q), (g["k"], k), (g["v"], v)):
+        assert t.shape == like.shape and not t.any()
+    assert r["last"].shape == g["state"].shape == (len(lens), 2, K, V)
