@@ -170,13 +170,12 @@ struct WinArgs {
   long long N;
   int n, H, G, D, window, sinks;
   float scale;
+  long long unit;                   // queries of a unit.  (Here: beside `scale`, delta would
+                                    // come to k_window_back by way of scratch memory)
   // workspace of the gradients
   float *delta;                     // [N, H]
-  float *most;                      // float16: workgroups' largest lengths of rows of gy
-  int mosts;                        // and v; how many
   float *own, *part;                // sums for gk and gv of cut sequences' first frames:
                                     // their blocks' own, and units' (or null)
-  long long unit;                   // queries of a unit
 };
 hipError_t launch_window(const WinArgs &a, int type, hipStream_t s);
 hipError_t launch_window_grads(WinArgs a, int type, void *ws, size_t *need, hipStream_t s);

@@ -39,7 +39,6 @@ constexpr int QT_OF = sizeof(T) == 2 ? 2 : 1;
 template <typename T>
 constexpr int BLOCK_OF = 16 * QT_OF<T> * WNW;  // queries, or keys, of a workgroup
 constexpr int FEW = 64;              // frames
-constexpr int MOSTS = 512;           // workgroups that look for float16's largest rows
 constexpr int MAX_CUT = 256;         // first frames whose queries are cut into units
 constexpr float LOG2 = 0.69314718055994530942f, LOG2E = 1.44269502162933349609375f;
 
@@ -69,6 +68,27 @@ __device__ __forceinline__ float dot(const T *a, const T *b, int D) {
   float x = 0.0f;
   for (int i = 0; i < D; ++i) x = fmaf((float)a[i], (float)b[i], x);
   return x;
+}
+
+// float16: dS is a number of 16 bits in its products, times a power of two that belongs
+// to the result it is summed into (a query's dq, a key's dk) and goes by what that
+// result sees alone.  It begins as UNMET and falls wherever a dS would be past PAST
+// with it, to one that leaves that dS below 2^12, so that few tiles change it; the sums
+// so far are multiplied by what `lowered` returns.
+template <typename T>
+constexpr bool SCALED = std::is_same<T, f16>::value;
+constexpr float UNMET = 0x1p120f, PAST = 0x1p15f;
+__device__ __forceinline__ float lowered(float &up, float top) {
+  top = column_max(top);
+  const float was = up;
+  if (top * up > PAST) up = fminf(up, power_below(top, 12));
+  return up / was;
+}
+__device__ __forceinline__ float largest(const float4v &a, const float4v &b) {
+  float top = 0.0f;
+#pragma unroll
+  for (int r = 0; r < 4; ++r) top = fmaxf(fmaxf(top, fabsf(a[r])), fabsf(b[r]));
+  return top;
 }
 
 // Whether query t sees no frame but itself: then dS is 0 and no difference of two
@@ -341,9 +361,8 @@ __global__ __launch_bounds__(WNT, MIN_WAVES<T>) void k_window(WinArgs a) {
 // gradients
 // ---------------------------------------------------------------------------
 
-// delta = y . dy of each row and head, a lane for 16 bytes of it; float16: the largest
-// lengths of rows of dy and v, whose product bounds dS.  Bound by memory (200 MB of y
-// and dy: 31 us).
+// delta = y . dy of each row and head, a lane for 16 bytes of it.  Bound by memory (200
+// MB of y and dy: 31 us).
 template <typename T, int P, bool WIDE>
 __global__ __launch_bounds__(WNT) void k_window_delta(WinArgs a) {
   constexpr int LANES = P / PER<T>, EACH = WNT / LANES;
@@ -354,69 +373,26 @@ __global__ __launch_bounds__(WNT) void k_window_delta(WinArgs a) {
     const T *row = static_cast<const T *>(p) + at;
     return __builtin_bit_cast(Group, load_group<T, WIDE>(row, c, a.D, true, row));
   };
-  float top = 0.0f, topv = 0.0f;
   for (long long i = (long long)blockIdx.x * EACH + threadIdx.x / LANES; i < all;
        i += (long long)gridDim.x * EACH) {
     const long long row = (uint64_t)i / (uint32_t)a.H;
     const int h = (int)(i - row * a.H);
     const Group y = read(a.y, row * a.ys + (long long)h * a.D);
     const Group gy = read(a.gy, row * a.gys + (long long)h * a.D);
-    Group v{};
-    if (a.most && h < a.G) v = read(a.v, row * a.vs + (long long)h * a.D);
-    float s = 0.0f, n = 0.0f, nv = 0.0f;
+    float s = 0.0f;
 #pragma unroll
-    for (int j = 0; j < PER<T>; ++j) {
-      const float g = (float)gy.v[j];
-      s = fmaf((float)y.v[j], g, s);
-      n = fmaf(g, g, n);
-      nv = fmaf((float)v.v[j], (float)v.v[j], nv);
-    }
+    for (int j = 0; j < PER<T>; ++j) s = fmaf((float)y.v[j], (float)gy.v[j], s);
 #pragma unroll
-    for (int o = LANES / 2; o; o >>= 1) {
-      s += __shfl_xor(s, o, WAVE);
-      if (a.most) {
-        n += __shfl_xor(n, o, WAVE);
-        nv += __shfl_xor(nv, o, WAVE);
-      }
-    }
+    for (int o = LANES / 2; o; o >>= 1) s += __shfl_xor(s, o, WAVE);
     if (c == 0) a.delta[i] = s;
-    top = n < INFINITY ? fmaxf(top, n) : top;
-    topv = nv < INFINITY ? fmaxf(topv, nv) : topv;
   }
-  if (!a.most) return;
-  __shared__ float s_top[2][WNW];
-  top = wave_max(top), topv = wave_max(topv);
-  if (threadIdx.x % WAVE == 0)
-    s_top[0][threadIdx.x / WAVE] = top, s_top[1][threadIdx.x / WAVE] = topv;
-  __syncthreads();
-  if (threadIdx.x < 2) {
-    float x = s_top[threadIdx.x][0];
-#pragma unroll
-    for (int w = 1; w < WNW; ++w) x = fmaxf(x, s_top[threadIdx.x][w]);
-    a.most[threadIdx.x * MOSTS + blockIdx.x] = sqrtf(x);
-  }
-}
-
-// float16: the power of two that dS is scaled by, from all workgroups' largest lengths
-// (one pair that all of them would raise: 37 us instead of 4 for 4,000 rows of 3 heads).
-template <typename T>
-__device__ __forceinline__ float ds_scale(const WinArgs &a) {
-  if constexpr (std::is_same<T, f16>::value) {
-    float gy = 0.0f, v = 0.0f;
-    for (int i = threadIdx.x % WAVE; i < a.mosts; i += WAVE) {
-      gy = fmaxf(gy, a.most[i]);
-      v = fmaxf(v, a.most[MOSTS + i]);
-    }
-    return power_below(2.0f * wave_max(gy) * wave_max(v), 15);
-  }
-  return 1.0f;
 }
 
 template <typename T>
 __device__ __noinline__ float4v exact_dq(const T *q, const T *gy, const T *k, long long ks,
                                          const T *v, long long vs, int D, long long t,
                                          int window, int sinks, float c, float lse, float delta,
-                                         float up, int d0) {
+                                         int d0) {
   float4v x{};
   for (long long s = 0; s <= t; ++s) {
     if (t - s >= window && s >= sinks) {
@@ -424,7 +400,7 @@ __device__ __noinline__ float4v exact_dq(const T *q, const T *gy, const T *k, lo
       continue;
     }
     const float e = exp2_of(fmaf(dot(q, k + s * ks, D), c, -lse));
-    const float d = e * (dot(gy, v + s * vs, D) - delta) * up;
+    const float d = e * (dot(gy, v + s * vs, D) - delta);
 #pragma unroll
     for (int r = 0; r < 4; ++r)
       x[r] = fmaf(d, d0 + r < D ? (float)k[s * ks + d0 + r] : d, x[r]);
@@ -443,14 +419,14 @@ __device__ __noinline__ TwoFours exact_dkv(const T *q, long long qs, const T *gy
                                            const float *lse, const float *delta, int H, int D,
                                            const T *k, const T *v, long long s, long long t0,
                                            long long t1, int run, int wave, int window,
-                                           int sinks, float c, float up, int d0) {
+                                           int sinks, float c, int d0) {
   TwoFours x{};
   for (long long t = t0; t < t1; ++t) {
     if (run && ((t - t0) % run / 32 != wave || t - s < window)) continue;
     const T *qt = q + t * qs, *gt = gy + t * gys;
     const float e = exp2_of(fmaf(dot(qt, k, D), c, -lse[t * H] * LOG2E));
     const float d =
-        sees_one(t, window, sinks) ? 0.0f : e * (dot(gt, v, D) - delta[t * H]) * up;
+        sees_one(t, window, sinks) ? 0.0f : e * (dot(gt, v, D) - delta[t * H]);
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       x.k[r] = fmaf(d, d0 + r < D ? (float)qt[d0 + r] : d, x.k[r]);
@@ -507,9 +483,11 @@ __device__ __forceinline__ void dq_block(const WinArgs &a, const Unit &u, int h,
                                                       : INFINITY;
     delta[i] = there ? a.delta[(u.b + t) * a.H + h] : 0.0f;
   }
-  const float c = a.scale * LOG2E, up = ds_scale<T>(a);
+  const float c = a.scale * LOG2E;
   float4v o[DT][QT] = {};
-  float sum[QT] = {};
+  float sum[QT] = {}, up[QT];
+#pragma unroll
+  for (int i = 0; i < QT; ++i) up[i] = SCALED<T> ? UNMET : 1.0f;
   for (int tile = 0; tile < sn.tiles; ++tile) {
     char *s_k = s_dyn + (tile & 1) * 2 * TILE, *s_v = s_k + TILE;
     char *s_next = s_dyn + (~tile & 1) * 2 * TILE;
@@ -549,7 +527,7 @@ __device__ __forceinline__ void dq_block(const WinArgs &a, const Unit &u, int h,
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
             const float e = exp2_of(fmaf(x[b][i][r], c, -lse[i]));
-            x[b][i][r] = SUMS ? e * y[b][i][r] : e * (y[b][i][r] - delta[i]) * up;
+            x[b][i][r] = SUMS ? e * y[b][i][r] : e * (y[b][i][r] - delta[i]);
           }
         if (!whole) {
           const Edge e = edge_of(a, sn, sink, s0 + 32 * t2, tw + 16 * i + l16, lg);
@@ -568,9 +546,24 @@ __device__ __forceinline__ void dq_block(const WinArgs &a, const Unit &u, int h,
 #pragma unroll
             for (int r = 0; r < 4; ++r) sum[i] += x[b][i][r];
         }
-        p[i] = pack<T>(x[0][i], x[1][i]);
       }
       if constexpr (SUMS) continue;
+      if constexpr (SCALED<T>) {
+        bool late = false;
+#pragma unroll
+        for (int i = 0; i < QT; ++i) late = late || largest(x[0][i], x[1][i]) * up[i] > PAST;
+        if (__any(late)) {
+#pragma unroll
+          for (int i = 0; i < QT; ++i) {
+            const float less = lowered(up[i], largest(x[0][i], x[1][i]));
+#pragma unroll
+            for (int d = 0; d < DT; ++d) o[d][i] *= less;
+          }
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < QT; ++i)
+        p[i] = SCALED<T> ? pack<T>(x[0][i] * up[i], x[1][i] * up[i]) : pack<T>(x[0][i], x[1][i]);
 #pragma unroll
       for (int d = 0; d < DT; ++d) {
         const Frag<T> f = Packed<T, P>::columns(s_k, 32 * t2, 16 * d, lane);
@@ -593,11 +586,11 @@ __device__ __forceinline__ void dq_block(const WinArgs &a, const Unit &u, int h,
     return;
   }
   const bool fine = finite(o);
-  const float f = a.scale / up;
 #pragma unroll
   for (int i = 0; i < QT; ++i) {
     const long long t = tw + 16 * i + l16;
     if (t >= u.hi) continue;
+    const float f = a.scale / up[i];
     T *gq = static_cast<T *>(a.gq) + (u.b + t) * a.gqs + (long long)h * D;
 #pragma unroll
     for (int d = 0; d < DT; ++d) store_four<T, WIDE>(gq, 16 * d + 4 * lg, D, o[d][i] * f);
@@ -612,7 +605,7 @@ __device__ __forceinline__ void dq_block(const WinArgs &a, const Unit &u, int h,
       if (none_of_four(gq, d, D))
         mend_four(gq, d, D,
                   exact_dq<T>(q + t * a.qs, gy + t * a.gys, k, a.ks, v, a.vs, D, t, a.window,
-                              a.sinks, c, lse[i], delta[i], up, d) * f);
+                              a.sinks, c, lse[i], delta[i], d) * a.scale);
   }
 }
 
@@ -666,8 +659,11 @@ __device__ __forceinline__ void dkv_block(const WinArgs &a, const Unit &u, int g
       }
   }
   cv.finish(s_v);
-  const float c = a.scale * LOG2E, up = ds_scale<T>(a);
+  const float c = a.scale * LOG2E;
   float4v ok[DT][QT] = {}, ov[DT][QT] = {};
+  float up[QT];
+#pragma unroll
+  for (int i = 0; i < QT; ++i) up[i] = SCALED<T> ? UNMET : 1.0f;
   const long long end =
       u.hi - 1 + a.window < u.len && !onward ? u.hi - 1 + a.window : u.len;
   const int tiles = (int)((end - u.lo + QUERIES - 1) / QUERIES), all = tiles * E;
@@ -740,7 +736,7 @@ __device__ __forceinline__ void dkv_block(const WinArgs &a, const Unit &u, int g
           for (int r = 0; r < 4; ++r) {
             const float e = exp2_of(fmaf(x[b][i][r], c, -lse[r]));
             x[b][i][r] = e;
-            y[b][i][r] = e * (y[b][i][r] - delta[r]) * up;
+            y[b][i][r] = e * (y[b][i][r] - delta[r]);
           }
       }
       if (!whole) {
@@ -764,11 +760,25 @@ __device__ __forceinline__ void dkv_block(const WinArgs &a, const Unit &u, int g
             }
         }
       }
+      if constexpr (SCALED<T>) {
+        bool late = false;
+#pragma unroll
+        for (int i = 0; i < QT; ++i) late = late || largest(y[0][i], y[1][i]) * up[i] > PAST;
+        if (__any(late)) {
+#pragma unroll
+          for (int i = 0; i < QT; ++i) {
+            const float less = lowered(up[i], largest(y[0][i], y[1][i]));
+#pragma unroll
+            for (int d = 0; d < DT; ++d) ok[d][i] *= less;
+          }
+        }
+      }
       Frag<T> p[QT], ds[QT];
 #pragma unroll
       for (int i = 0; i < QT; ++i) {
         p[i] = pack<T>(x[0][i], x[1][i]);
-        ds[i] = pack<T>(y[0][i], y[1][i]);
+        ds[i] = SCALED<T> ? pack<T>(y[0][i] * up[i], y[1][i] * up[i])
+                          : pack<T>(y[0][i], y[1][i]);
       }
 #pragma unroll
       for (int d = 0; d < DT; ++d) {
@@ -784,7 +794,6 @@ __device__ __forceinline__ void dkv_block(const WinArgs &a, const Unit &u, int g
     if (more) finish(j + 1);
   }
   const bool fine = finite(ok) && finite(ov);
-  const float f = a.scale / up;
 #pragma unroll
   for (int i = 0; i < QT; ++i) {
     const long long s = sw + 16 * i + l16;
@@ -792,6 +801,7 @@ __device__ __forceinline__ void dkv_block(const WinArgs &a, const Unit &u, int g
     T *gk = static_cast<T *>(a.gk) + (u.b + s) * a.gks + (long long)g * D;
     T *gv = static_cast<T *>(a.gv) + (u.b + s) * a.gvs + (long long)g * D;
     float *own = split && s < a.sinks ? own_part(a, u, g, (int)s, P) : nullptr;
+    const float f = a.scale / up[i];
 #pragma unroll
     for (int d = 0; d < DT; ++d) {
       ok[d][i] *= f;
@@ -824,15 +834,15 @@ __device__ __forceinline__ void dkv_block(const WinArgs &a, const Unit &u, int g
         const T *gh = static_cast<const T *>(a.gy) + u.b * a.gys + (long long)hh * D;
         const TwoFours x = exact_dkv<T>(
             qh, a.qs, gh, a.gys, a.lse + u.b * a.H + hh, a.delta + u.b * a.H + hh, a.H, D,
-            k + s * a.ks, v + s * a.vs, s, s, t1, 0, 0, a.window, a.sinks, c, up, d);
+            k + s * a.ks, v + s * a.vs, s, s, t1, 0, 0, a.window, a.sinks, c, d);
         xk += x.k;
         xv += x.v;
       }
       if (own) {
-        mend_four(own, d, D, xk * f);
+        mend_four(own, d, D, xk * a.scale);
         mend_four(own + P, d, D, xv);
       } else {
-        mend_four(gk, d, D, xk * f);
+        mend_four(gk, d, D, xk * a.scale);
         mend_four(gv, d, D, xv);
       }
     }
@@ -867,7 +877,8 @@ __device__ __forceinline__ void sinks_block(const WinArgs &a, const Unit &u, int
       kf[t].v[e] = load_group<T, WIDE>(k + s * a.ks, at, D, mine, k);
       vf[t].v[e] = load_group<T, WIDE>(v + s * a.vs, at, D, mine, v);
     }
-  const float c = a.scale * LOG2E, up = ds_scale<T>(a);
+  const float c = a.scale * LOG2E;
+  float up = SCALED<T> ? UNMET : 1.0f;
   float4v ok[DT] = {}, ov[DT] = {};
   const long long lo = u.lo > a.window ? u.lo : a.window;
   const int tiles = (int)((u.hi - lo + Q - 1) / Q), all = tiles * E;
@@ -912,12 +923,21 @@ __device__ __forceinline__ void sinks_block(const WinArgs &a, const Unit &u, int
         const long long t = t0 + at + 4 * lg + r;
         const bool sees = mine && t - s >= a.window && t < u.hi;
         const float e = exp2_of(fmaf(x[b][r], c, -lse[r]));
-        const float d = e * (y[b][r] - delta[r]) * up;
+        const float d = e * (y[b][r] - delta[r]);
         x[b][r] = sees ? e : 0.0f;
         y[b][r] = sees ? d : 0.0f;
       }
     }
-    const Frag<T> p = pack<T>(x[0], x[1]), ds = pack<T>(y[0], y[1]);
+    if constexpr (SCALED<T>) {
+      const float top = largest(y[0], y[1]);
+      if (__any(top * up > PAST)) {
+        const float less = lowered(up, top);
+#pragma unroll
+        for (int d = 0; d < DT; ++d) ok[d] *= less;
+      }
+    }
+    const Frag<T> p = pack<T>(x[0], x[1]);
+    const Frag<T> ds = SCALED<T> ? pack<T>(y[0] * up, y[1] * up) : pack<T>(y[0], y[1]);
 #pragma unroll
     for (int d = 0; d < DT; ++d) {
       ov[d] = mac(columns<T, P>(s_g, 32 * w, 16 * d, lane), p, ov[d]);
@@ -925,10 +945,13 @@ __device__ __forceinline__ void sinks_block(const WinArgs &a, const Unit &u, int
     }
   }
   float z = 0.0f;
+  const float f = a.scale / up;
 #pragma unroll
-  for (int d = 0; d < DT; ++d)
+  for (int d = 0; d < DT; ++d) {
+    ok[d] *= f;
 #pragma unroll
     for (int r = 0; r < 4; ++r) z = fmaf(ok[d][r], 0.0f, fmaf(ov[d][r], 0.0f, z));
+  }
   if (!__all(z == 0.0f) && mine) {
 #pragma unroll
     for (int d = 0; d < DT; ++d) {
@@ -939,14 +962,14 @@ __device__ __forceinline__ void sinks_block(const WinArgs &a, const Unit &u, int
         const T *gh = static_cast<const T *>(a.gy) + u.b * a.gys + (long long)h * D;
         const TwoFours x = exact_dkv<T>(
             qh, a.qs, gh, a.gys, a.lse + u.b * a.H + h, a.delta + u.b * a.H + h, a.H, D,
-            k + s * a.ks, v + s * a.vs, s, lo, u.hi, Q, w, a.window, a.sinks, c, up,
+            k + s * a.ks, v + s * a.vs, s, lo, u.hi, Q, w, a.window, a.sinks, c,
             16 * d + 4 * lg);
         xk += x.k;
         xv += x.v;
       }
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        ok[d][r] = fabsf(ok[d][r]) < INFINITY ? ok[d][r] : xk[r];
+        ok[d][r] = fabsf(ok[d][r]) < INFINITY ? ok[d][r] : xk[r] * a.scale;
         ov[d][r] = fabsf(ov[d][r]) < INFINITY ? ov[d][r] : xv[r];
       }
     }
@@ -954,7 +977,6 @@ __device__ __forceinline__ void sinks_block(const WinArgs &a, const Unit &u, int
   // (the sums take as much of LDS as the tiles of a 16-bit type)
   float *s_sum = reinterpret_cast<float *>(s_dyn);
   static_assert(WNW * 16 * P * 4 <= 2 * Q * LD<T, P> * (int)sizeof(T), "room for the sums");
-  const float f = a.scale / up;
 #pragma unroll
   for (int o = 0; o < 2; ++o) {
     __syncthreads();
@@ -969,8 +991,7 @@ __device__ __forceinline__ void sinks_block(const WinArgs &a, const Unit &u, int
       for (int q = 0; q < WNW; ++q) v += s_sum[q * 16 * P + i];
       const int key = first + i / P;
       if (key < a.sinks)
-        unit_part(a, u, u.lo / a.unit, g, key, P)[o * P + i % P] =
-            o ? v : v * f;
+        unit_part(a, u, u.lo / a.unit, g, key, P)[o * P + i % P] = v;
     }
   }
 }
@@ -1307,12 +1328,11 @@ hipError_t forward_as(const WinArgs &a, hipStream_t s) {
 }
 
 template <typename T, int P, bool WIDE>
-hipError_t backward_as(WinArgs a, hipStream_t s) {
+hipError_t backward_as(const WinArgs &a, hipStream_t s) {
   const long long blocks = a.N / BLOCK_OF<T> + a.n;
   constexpr int each = WNT / (P / PER<T>);
-  const long long rows = (a.N * a.H + each - 1) / each, most = a.most ? MOSTS : 8192;
-  a.mosts = (int)(rows < most ? rows : most);
-  k_window_delta<T, P, WIDE><<<a.mosts, WNT, 0, s>>>(a);
+  const long long rows = (a.N * a.H + each - 1) / each;
+  k_window_delta<T, P, WIDE><<<(unsigned)(rows < 8192 ? rows : 8192), WNT, 0, s>>>(a);
   if constexpr (sizeof(T) == 2) {
     constexpr int lds = WALK<T, P>;
     const hipError_t e =
@@ -1389,12 +1409,9 @@ hipError_t launch_window_grads(WinArgs a, int type, void *ws, size_t *need, hipS
       a.sinks > 0 && a.sinks <= MAX_CUT && a.N > a.window && a.N > a.unit;
   const size_t first = cut ? (size_t)a.G * a.sinks * 2 * padded(D) : 0;
   const size_t own = (a.N / a.unit + 1) * first, part = (2 * a.N / a.unit + 1) * first;
-  const size_t most = type == FST_F16 ? 2 * MOSTS : 0;
-  *need = (most + delta + own + part) * sizeof(float);
+  *need = (delta + own + part) * sizeof(float);
   if (!ws) return hipSuccess;
-  float *p = static_cast<float *>(ws);
-  a.most = most ? p : nullptr;
-  a.delta = p + most;
+  a.delta = static_cast<float *>(ws);
   a.own = a.delta + delta;
   a.part = cut ? a.own + own : nullptr;
   const bool wide = wide_rows(type_bytes(type), D,

@@ -914,3 +914,60 @@ def test_linear_of_heads_without_columns(comp, K, V, lens, typ):
     for t, like in ((r["y"], v), (g["q"], q), (g["k"], k), (g["v"], v)):
         assert t.shape == like.shape and not t.any()
     assert r["last"].shape == g["state"].shape == (len(lens), 2, K, V)
+
+
+def _near(out, c, rows):
+    """window_bound of float16 with the spacing of scaled numbers at 0 taken from the
+    row's own largest: dS is scaled to 2^11 or more, so that each of n terms, here at
+    most 400, is off by at most 2^-25 / 2^11 of the largest dS of the row, and this
+    times a number of the other operand, up to 5 where the row's largest has 1 or more
+    in some column: 400 * 5 * 2^-36 < 2^-25 of the row's largest size."""
+    r = out["r" + c]
+    return (out["b" + c] + ref.H16[torch.float16] * r
+            + 2.0 ** -25 * r.amax(1, keepdim=True).expand_as(r))[rows]
+
+
+@pytest.mark.parametrize("where", ["other sequence", "no sequence", "later"])
+@pytest.mark.parametrize("D", [64, 40, 128])
+def test_window_float16_gradients_beside_large_rows(comp, where, D):
+    """A large row takes no digits of the gradients of rows that do not see it."""
+    off, H, G, win, sinks = [0, 200, 260], 2, 1, 90, 3
+    q, k, v, gy = _window_inputs([200, 60, 20], H, G, D, "f16")
+    gy = (gy.float() * 2.0 ** -10).half()
+    how = dict(heads=H, kv_heads=G, window=win, sinks=sinks)
+    o = ref.window(_d(q), _d(k), _d(v), off, H, G, win, sinks, D ** -0.5, _d(gy))
+    at = {"other sequence": 230, "no sequence": 270, "later": 190}[where]
+    queries = range(190 if where == "later" else 200)
+    # (keys that row 190 sees: the first ones and its window)
+    keys = range(sinks, 190 - win + 1) if where == "later" else range(200)
+    print(f"[window] large row {at}, D={D}", flush=True)
+    for big in ((gy,), (v,), (gy, v), (q, gy)):
+        args = []
+        for t in (q, k, v, gy):
+            z = t.clone()
+            if any(t is b for b in big):
+                z[at] = 8000.0
+            args.append(z)
+        r = comp.window_attention(*args[:3], _i32(off), **how)
+        g = comp.window_attention_grads(*args[:3], _i32(off), r["y"], r["lse"], args[3], **how)
+        for c, rows in (("q", queries), ("k", keys), ("v", keys)):
+            rows = list(rows)
+            ref.within("g" + c, g[c][rows], o["g" + c][rows], _near(o, "g" + c, rows))
+
+
+def test_window_float16_gradients_that_grow(comp):
+    """dS that grow, and shrink, by thousands from tile to tile, each row within its
+    own bound."""
+    H, G, D, T, win, sinks = 2, 1, 64, 700, 150, 3
+    q, k, v, gy = _window_inputs([T], H, G, D, "f16")
+    t = torch.arange(T, device="cuda")
+    for e in (10 * torch.sin(t / 40.0), (t - T // 2) / 30.0, (T // 2 - t) / 30.0):
+        size = torch.exp2(e.round().clamp(-10, 10))[:, None]
+        x = [(a.float() * b).half() for a, b in ((v, size), (gy, size.flip(0)))]
+        how = dict(heads=H, kv_heads=G, window=win, sinks=sinks)
+        r = comp.window_attention(q, k, x[0], _i32([0, T]), **how)
+        g = comp.window_attention_grads(q, k, x[0], _i32([0, T]), r["y"], r["lse"], x[1], **how)
+        o = ref.window(_d(q), _d(k), _d(x[0]), [0, T], H, G, win, sinks, D ** -0.5, _d(x[1]))
+        rows = list(range(T))
+        for c in "qk":
+            ref.within("g" + c, g[c], o["g" + c], _near(o, "g" + c, rows))
