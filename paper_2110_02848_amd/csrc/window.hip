@@ -91,6 +91,13 @@ __device__ __forceinline__ float largest(const float4v &a, const float4v &b) {
   return top;
 }
 
+// float16: log 2 of what P is multiplied by for dv, and so dS too.  P of many frames is
+// below 2^-14, where float16 loses digits; it is at most 1 but for lse's rounding.
+template <typename T>
+constexpr float RAISE = SCALED<T> ? 12.0f : 0.0f;
+template <typename T>
+constexpr float RAISED = SCALED<T> ? 0x1p12f : 1.0f;
+
 // Whether query t sees no frame but itself: then dS is 0 and no difference of two
 // sums.
 __device__ __forceinline__ bool sees_one(long long t, int window, int sinks) {
@@ -680,7 +687,7 @@ __device__ __forceinline__ void dkv_block(const WinArgs &a, const Unit &u, int g
     if (threadIdx.x < QUERIES) {
       const bool there = (int)threadIdx.x < count;
       const long long at = (u.b + t0 + threadIdx.x) * a.H + h;
-      r_lse = there ? a.lse[at] * LOG2E : INFINITY;
+      r_lse = there ? a.lse[at] * LOG2E - RAISE<T> : INFINITY;
       r_delta = there ? a.delta[at] : 0.0f;
     }
   };
@@ -801,10 +808,11 @@ __device__ __forceinline__ void dkv_block(const WinArgs &a, const Unit &u, int g
     T *gk = static_cast<T *>(a.gk) + (u.b + s) * a.gks + (long long)g * D;
     T *gv = static_cast<T *>(a.gv) + (u.b + s) * a.gvs + (long long)g * D;
     float *own = split && s < a.sinks ? own_part(a, u, g, (int)s, P) : nullptr;
-    const float f = a.scale / up[i];
+    const float f = a.scale / (up[i] * RAISED<T>);
 #pragma unroll
     for (int d = 0; d < DT; ++d) {
       ok[d][i] *= f;
+      ov[d][i] *= 1.0f / RAISED<T>;
       if (own) {
         *reinterpret_cast<float4v *>(own + 16 * d + 4 * lg) = ok[d][i];
         *reinterpret_cast<float4v *>(own + P + 16 * d + 4 * lg) = ov[d][i];
@@ -894,7 +902,7 @@ __device__ __forceinline__ void sinks_block(const WinArgs &a, const Unit &u, int
     if (threadIdx.x < Q) {
       const bool there = (int)threadIdx.x < count;
       const long long at = (u.b + t0 + threadIdx.x) * a.H + h;
-      r_lse = there ? a.lse[at] * LOG2E : INFINITY;
+      r_lse = there ? a.lse[at] * LOG2E - RAISE<T> : INFINITY;
       r_delta = there ? a.delta[at] : 0.0f;
     }
   };
@@ -945,10 +953,11 @@ __device__ __forceinline__ void sinks_block(const WinArgs &a, const Unit &u, int
     }
   }
   float z = 0.0f;
-  const float f = a.scale / up;
+  const float f = a.scale / (up * RAISED<T>);
 #pragma unroll
   for (int d = 0; d < DT; ++d) {
     ok[d] *= f;
+    ov[d] *= 1.0f / RAISED<T>;
 #pragma unroll
     for (int r = 0; r < 4; ++r) z = fmaf(ok[d][r], 0.0f, fmaf(ov[d][r], 0.0f, z));
   }

@@ -971,3 +971,23 @@ def test_window_float16_gradients_that_grow(comp):
         rows = list(range(T))
         for c in "qk":
             ref.within("g" + c, g[c], o["g" + c], _near(o, "g" + c, rows))
+
+
+@pytest.mark.parametrize("win,sinks", [(1000, 0), (40, 2)])
+def test_window_float16_gradients_of_values_seen_faintly(comp, win, sinks):
+    """A first frame that takes all but 2^-22 of every query's weight: what is left to
+    the others has float16's digits all the same.  (P is scaled to 2^12, and each of at
+    most 300 terms off by 2^-25 2^-12 of a dy, at most 5 * 2^11.)"""
+    T, D = 300, 16
+    q, k, v, gy = _window_inputs([T], 1, 1, D, "f16")
+    q, k = (t.float() / 8 for t in (q, k))
+    q[:, 0], k[:, 0] = 4.0, 0.0
+    k[0, 0] = 15.25
+    q, k, gy = q.half(), k.half(), (gy.float() * 2.0 ** 11).half()
+    how = dict(heads=1, kv_heads=1, window=win, sinks=max(sinks, 1))
+    r = comp.window_attention(q, k, v, _i32([0, T]), **how)
+    g = comp.window_attention_grads(q, k, v, _i32([0, T]), r["y"], r["lse"], gy, **how)
+    o = ref.window(_d(q), _d(k), _d(v), [0, T], 1, 1, win, max(sinks, 1), D ** -0.5, _d(gy))
+    bound = (o["bgv"] + ref.H16[torch.float16] * o["rgv"]
+             + 300 * 2.0 ** -37 * 5 * 2.0 ** 11)
+    ref.within("gv", g["v"], o["gv"], bound)
