@@ -84,7 +84,7 @@ __device__ __noinline__ void exact_rows(T *o, int left, const T *s_q, const T *s
 
 // Over the wavefronts.
 template <int NW>
-__device__ __forceinline__ float largest(const float (&m)[NW][4], int c) {
+__device__ __forceinline__ float largest(const float (&m)[NW][3], int c) {
   float x = m[0][c];
 #pragma unroll
   for (int w = 1; w < NW; ++w) x = fmaxf(x, m[w][c]);
@@ -126,8 +126,9 @@ __device__ __forceinline__ Place place_of(int H, int slices) {
 //
 // Roundings to 16 bits: scores and the state that meets q, once each.  The decayed k
 // that go into the state are as many numbers as hold them: states are float32
-// results.  float16: all three are scaled by a power of two from the
-// chunk's largest numbers, so that they neither overflow nor lose their digits.
+// results.  float16: all three are scaled by powers of two, scores by one of the
+// row's own (tiles.h), the others by the chunk's largest numbers and a bound on the
+// state's, so that they neither overflow nor lose their digits.
 //
 // Bound by memory for heads of 64 (40,000 x 8 x 64 x 64 bf16: 37 us for 164 MB, 4.4 TB/s,
 // the units' states 22 before it), for wider ones by a chunk's steps, each waiting for
@@ -154,7 +155,7 @@ __global__ __launch_bounds__(256 * CG, (MIN_WAVES<T, PA, CG>)) void k_linear(Lin
   T *s_s = s_q + CHUNK * LD<T, PA>;            // FULL: [PB][PA]
   __shared__ float s_pow[CHUNK + 1];
   __shared__ __attribute__((aligned(16))) float s_end[CHUNK];  // rows' powers to the end
-  __shared__ float s_max[NW][4];
+  __shared__ float s_max[NW][3];
 
   const Place at = place_of(a.H, a.slices);
   const LinJob &job = a.job[at.job];
@@ -208,11 +209,11 @@ __global__ __launch_bounds__(256 * CG, (MIN_WAVES<T, PA, CG>)) void k_linear(Lin
           bound = x < INFINITY ? fmaxf(bound, x) : bound;
         }
     bound = wave_max(bound);
-    if (lane == 0) s_max[w][3] = bound;
+    if (lane == 0) s_max[w][2] = bound;
   }
   __syncthreads();
   if constexpr (SCALED && FULL)
-    bound = largest(s_max, 3);
+    bound = largest(s_max, 2);
 
   // powers that every chunk uses: of row i = 16 wr + l16 against rows j = 16 t +
   // 4 lg + r (0 where j is later) and against the state
@@ -263,20 +264,16 @@ __global__ __launch_bounds__(256 * CG, (MIN_WAVES<T, PA, CG>)) void k_linear(Lin
     rv.store(s_v);
     if constexpr (SCALED) {
       const float mk = wave_max(rk.largest()), mv = wave_max(rv.largest());
-      const float mq = FULL ? wave_max(rq.largest()) : 0.0f;
-      if (lane == 0) s_max[w][0] = mq, s_max[w][1] = mk, s_max[w][2] = mv;
+      if (lane == 0) s_max[w][0] = mk, s_max[w][1] = mv;
     }
     __syncthreads();
     if (more) fetch(i0 + CHUNK);
 
-    float p_scale = 1.0f, k_scale = 1.0f;
+    float p_scale = SCALED ? UNMET : 1.0f, k_scale = 1.0f;
     if constexpr (SCALED) {
-      float top[3];
-#pragma unroll
-      for (int c = 0; c < 3; ++c) top[c] = largest(s_max, c);
-      p_scale = power_below(most * (float)A * top[0] * top[1], 15);
-      k_scale = fminf(power_below(most * fabsf(job.sk) * top[1], 12), 0x1p60f);
-      bound = fmaf(keep, bound, most * fabsf(job.sk) * CHUNK * top[1] * top[2]);
+      const float mk = largest(s_max, 0), mv = largest(s_max, 1);
+      k_scale = fminf(power_below(most * fabsf(job.sk) * mk, 12), 0x1p60f);
+      bound = fmaf(keep, bound, most * fabsf(job.sk) * CHUNK * mk * mv);
     }
     if constexpr (FULL) {
       float4v past[NJ] = {}, now[NJ] = {};
@@ -302,8 +299,19 @@ __global__ __launch_bounds__(256 * CG, (MIN_WAVES<T, PA, CG>)) void k_linear(Lin
 #pragma unroll
           for (int r = 0; r < 4; ++r)
             x[c][r] = 32 * t + 16 * c + 4 * lg + r <= i
-                          ? x[c][r] * dec[2 * t + c][r] * p_scale
+                          ? x[c][r] * dec[2 * t + c][r]
                           : 0.0f;
+        }
+        if constexpr (SCALED) {
+          const float top = largest_of(x[0], x[1]);
+          if (__any(top * p_scale > PAST)) {
+            const float less = lowered(p_scale, top);
+            if (t > 0) {
+#pragma unroll
+              for (int j = 0; j < NJ; ++j) now[j] *= less;
+            }
+          }
+          x[0] *= p_scale, x[1] *= p_scale;
         }
         const Frag<T> p = pack<T>(x[0], x[1]);
 #pragma unroll

@@ -434,5 +434,24 @@ __device__ __forceinline__ float power_below(float most, int top) {
   return ldexpf(1.0f, e);
 }
 
+// Numbers that become 16-bit ones with few exponents (float16) before they are multiplied
+// take a power of two of the column of results that they are summed into, by what that
+// column sees alone.  It begins as UNMET and falls wherever a number would be past PAST
+// with it, to one that leaves that number below 2^12, so that few tiles change it; the
+// column's sums are multiplied by what `lowered` returns.  `top`: a lane's largest.
+constexpr float UNMET = 0x1p120f, PAST = 0x1p15f;
+__device__ __forceinline__ float lowered(float &up, float top) {
+  top = column_max(top);
+  const float was = up;
+  if (top * up > PAST) up = fminf(up, power_below(top, 12));
+  return up / was;
+}
+__device__ __forceinline__ float largest_of(const float4v &a, const float4v &b) {
+  float top = 0.0f;
+#pragma unroll
+  for (int r = 0; r < 4; ++r) top = fmaxf(fmaxf(top, fabsf(a[r])), fabsf(b[r]));
+  return top;
+}
+
 }  // namespace tile
 }  // namespace fstc

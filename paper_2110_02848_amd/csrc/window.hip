@@ -70,26 +70,10 @@ __device__ __forceinline__ float dot(const T *a, const T *b, int D) {
   return x;
 }
 
-// float16: dS is a number of 16 bits in its products, times a power of two that belongs
-// to the result it is summed into (a query's dq, a key's dk) and goes by what that
-// result sees alone.  It begins as UNMET and falls wherever a dS would be past PAST
-// with it, to one that leaves that dS below 2^12, so that few tiles change it; the sums
-// so far are multiplied by what `lowered` returns.
+// float16: dS is multiplied times a power of two (tiles.h) of the result that it is
+// summed into, a query's dq or a key's dk.
 template <typename T>
 constexpr bool SCALED = std::is_same<T, f16>::value;
-constexpr float UNMET = 0x1p120f, PAST = 0x1p15f;
-__device__ __forceinline__ float lowered(float &up, float top) {
-  top = column_max(top);
-  const float was = up;
-  if (top * up > PAST) up = fminf(up, power_below(top, 12));
-  return up / was;
-}
-__device__ __forceinline__ float largest(const float4v &a, const float4v &b) {
-  float top = 0.0f;
-#pragma unroll
-  for (int r = 0; r < 4; ++r) top = fmaxf(fmaxf(top, fabsf(a[r])), fabsf(b[r]));
-  return top;
-}
 
 // float16: log 2 of what P is multiplied by for dv, and so dS too.  P of many frames is
 // below 2^-14, where float16 loses digits; it is at most 1 but for lse's rounding.
@@ -558,11 +542,11 @@ __device__ __forceinline__ void dq_block(const WinArgs &a, const Unit &u, int h,
       if constexpr (SCALED<T>) {
         bool late = false;
 #pragma unroll
-        for (int i = 0; i < QT; ++i) late = late || largest(x[0][i], x[1][i]) * up[i] > PAST;
+        for (int i = 0; i < QT; ++i) late = late || largest_of(x[0][i], x[1][i]) * up[i] > PAST;
         if (__any(late)) {
 #pragma unroll
           for (int i = 0; i < QT; ++i) {
-            const float less = lowered(up[i], largest(x[0][i], x[1][i]));
+            const float less = lowered(up[i], largest_of(x[0][i], x[1][i]));
 #pragma unroll
             for (int d = 0; d < DT; ++d) o[d][i] *= less;
           }
@@ -770,11 +754,11 @@ __device__ __forceinline__ void dkv_block(const WinArgs &a, const Unit &u, int g
       if constexpr (SCALED<T>) {
         bool late = false;
 #pragma unroll
-        for (int i = 0; i < QT; ++i) late = late || largest(y[0][i], y[1][i]) * up[i] > PAST;
+        for (int i = 0; i < QT; ++i) late = late || largest_of(y[0][i], y[1][i]) * up[i] > PAST;
         if (__any(late)) {
 #pragma unroll
           for (int i = 0; i < QT; ++i) {
-            const float less = lowered(up[i], largest(y[0][i], y[1][i]));
+            const float less = lowered(up[i], largest_of(y[0][i], y[1][i]));
 #pragma unroll
             for (int d = 0; d < DT; ++d) ok[d][i] *= less;
           }
@@ -937,7 +921,7 @@ __device__ __forceinline__ void sinks_block(const WinArgs &a, const Unit &u, int
       }
     }
     if constexpr (SCALED<T>) {
-      const float top = largest(y[0], y[1]);
+      const float top = largest_of(y[0], y[1]);
       if (__any(top * up > PAST)) {
         const float less = lowered(up, top);
 #pragma unroll

@@ -991,3 +991,38 @@ def test_window_float16_gradients_of_values_seen_faintly(comp, win, sinks):
     bound = (o["bgv"] + ref.H16[torch.float16] * o["rgv"]
              + 300 * 2.0 ** -37 * 5 * 2.0 ** 11)
     ref.within("gv", g["v"], o["gv"], bound)
+
+
+@pytest.mark.parametrize("rev", [False, True])
+@pytest.mark.parametrize("lens,at", [([150], 37), ([150], 149), ([70, 64], 20), ([1100], 700)])
+@pytest.mark.parametrize("K,V", [(64, 64), (33, 20), (128, 128)])
+def test_linear_float16_beside_large_rows(comp, K, V, lens, at, rev):
+    """A large row takes no digits of rows that do not see it."""
+    q, k, v, d, st, gy, gl = _linear_inputs(lens, 2, K, V, "f16")
+    off, n = ref.offsets(lens), sum(lens)
+    args = [_d(t) for t in (q, k, v)]
+    size = [t.abs() for t in args]
+    how = (_d(d), off), (rev, K ** -0.5)
+    y, _ = ref.linear(*args, *how[0], _d(st), *how[1])
+    ay, _ = ref.linear(*size, *how[0], _d(st).abs(), *how[1])
+    want = ref.linear_grads(*args, *how[0], _d(st), *how[1], _d(gy), _d(gl))
+    ag = ref.linear_grads(*size, *how[0], _d(st).abs(), *how[1], _d(gy).abs(), _d(gl).abs())
+    (by, bq, bk, bv), _ = ref.linear_bounds(torch.float16, [ay, *ag[:3]], [], max(lens))
+    print(f"[linear] large row {at} of {lens}, {K} x {V} rev={rev}", flush=True)
+    for t, w in ((q, K), (k, K), (v, V), (gy, V)):
+        t[at, :w] = 6e4
+    r = comp.linear_attention(q, k, v, d, _i32(off), state=st, reverse=rev)
+    g = comp.linear_attention_grads(q, k, v, d, _i32(off), gy, state=st, grad_last=gl,
+                                    reverse=rev)
+    s = max(i for i in range(len(lens)) if off[i] <= at)
+    before, after = range(off[s], at), range(at + 1, off[s + 1])
+    if rev:
+        before, after = after, before
+    others = [t for t in range(n) if not off[s] <= t < off[s + 1]]
+    for c, got, w, b, rows, cols in (("y", r["y"], y, by, before, V),
+                                     ("q", g["q"], want[0], bq, before, K),
+                                     ("k", g["k"], want[1], bk, after, K),
+                                     ("v", g["v"], want[2], bv, after, V)):
+        rows = [*rows, *others]
+        ref.within(c, got[rows], w[rows], b[rows])
+        ref.within(c + ", other head", got[:, cols:], w[:, cols:], b[:, cols:])
