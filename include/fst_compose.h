@@ -537,7 +537,7 @@ FST_API int fst_recurrence_step(fst_ctx *ctx, const fst_matrix *x, const fst_mat
  * No results, gradients or states of rows depend on rows that they do not see:
  * where those hold infinities or NaN, sums that these would make no number of are
  * taken again without them (slowly, and rounded in another order).  Infinities and
- * NaN in rows that they do see make no number of them, as the formulas do. */
+ * NaN in rows that they do see make infinities or NaN of them where the formulas do. */
 #define FST_NORM_MAX_WIDTH 512      /* columns of a head of fst_head_norms     */
 #define FST_ATTENTION_MAX_WIDTH 128 /* of the attentions (FST_ERR_TOO_LARGE,   */
                                     /* which more than 16,383 heads, rows more */

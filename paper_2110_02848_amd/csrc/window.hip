@@ -82,8 +82,8 @@ constexpr float RAISE = SCALED<T> ? 12.0f : 0.0f;
 template <typename T>
 constexpr float RAISED = SCALED<T> ? 0x1p12f : 1.0f;
 
-// Whether query t sees no frame but itself: then dS is 0 and no difference of two
-// sums.
+// Whether query t sees no frame but itself: then dS is 0, or no number where one of its
+// factors is none, and no difference of two sums.
 __device__ __forceinline__ bool sees_one(long long t, int window, int sinks) {
   return t == 0 || (window == 1 && sinks == 0);
 }
@@ -416,8 +416,8 @@ __device__ __noinline__ TwoFours exact_dkv(const T *q, long long qs, const T *gy
     if (run && ((t - t0) % run / 32 != wave || t - s < window)) continue;
     const T *qt = q + t * qs, *gt = gy + t * gys;
     const float e = exp2_of(fmaf(dot(qt, k, D), c, -lse[t * H] * LOG2E));
-    const float d =
-        sees_one(t, window, sinks) ? 0.0f : e * (dot(gt, v, D) - delta[t * H]);
+    float d = e * (dot(gt, v, D) - delta[t * H]);
+    if (sees_one(t, window, sinks)) d *= 0.0f;
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       x.k[r] = fmaf(d, d0 + r < D ? (float)qt[d0 + r] : d, x.k[r]);
@@ -470,8 +470,8 @@ __device__ __forceinline__ void dq_block(const WinArgs &a, const Unit &u, int h,
         qf[i][s].v[e] = load_group<T, WIDE>(q + t * a.qs, at, D, there, q);
         gf[i][s].v[e] = load_group<T, WIDE>(gy + t * a.gys, at, D, there, gy);
       }
-    lse[i] = there && !sees_one(t, a.window, a.sinks) ? a.lse[(u.b + t) * a.H + h] * LOG2E
-                                                      : INFINITY;
+    lse[i] = there ? a.lse[(u.b + t) * a.H + h] * LOG2E : INFINITY;
+    if (sees_one(t, a.window, a.sinks)) lse[i] = fmaf(lse[i], 0.0f, INFINITY);
     delta[i] = there ? a.delta[(u.b + t) * a.H + h] : 0.0f;
   }
   const float c = a.scale * LOG2E;
@@ -783,6 +783,22 @@ __device__ __forceinline__ void dkv_block(const WinArgs &a, const Unit &u, int g
       }
     }
     if (more) finish(j + 1);
+  }
+  // (what the loop leaves out of queries that see only themselves: their lse and delta
+  // tell whether dS is no number)
+  if (sees_one(sw, a.window, a.sinks)) {
+#pragma unroll
+    for (int i = 0; i < QT; ++i) {
+      const long long s = sw + 16 * i + l16;
+      if (s >= u.hi || !sees_one(s, a.window, a.sinks)) continue;
+      float z = 0.0f;
+      for (int hh = g * E; hh < g * E + E; ++hh) {
+        const long long at = (u.b + s) * a.H + hh;
+        z = fmaf(a.lse[at] + a.delta[at], 0.0f, z);
+      }
+#pragma unroll
+      for (int d = 0; d < DT; ++d) ok[d][i] += z;
+    }
   }
   const bool fine = finite(ok) && finite(ov);
 #pragma unroll

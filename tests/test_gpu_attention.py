@@ -1026,3 +1026,42 @@ def test_linear_float16_beside_large_rows(comp, K, V, lens, at, rev):
         rows = [*rows, *others]
         ref.within(c, got[rows], w[rows], b[rows])
         ref.within(c + ", other head", got[:, cols:], w[:, cols:], b[:, cols:])
+
+
+@pytest.mark.parametrize("typ", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("bad", [NAN, INF, -INF])
+def test_window_rows_that_see_only_themselves(comp, typ, bad):
+    """dS = P (dy v^T - delta) is 0 there, and no number where one of its factors is
+    none: the first rows of sequences, and all rows of a window of 1."""
+    H, G, D = 2, 1, 16
+    for lens, win in (([1, 40, 1, 1], 30), ([50, 3], 1)):
+        off = ref.offsets(lens)
+        q, k, v, gy = _window_inputs(lens, H, G, D, typ)
+        how = dict(heads=H, kv_heads=G, window=win, sinks=0)
+        alone = [t for t in range(off[-1]) if win == 1 or t + 1 in off and t in off]
+        for i, at in ((i, at) for i in range(4) for at in alone[:1] + alone[-2:]):
+            args = [t.clone() for t in (q, k, v, gy)]
+            args[i][at, :D] = bad
+            r = comp.window_attention(*args[:3], _i32(off), **how)
+            g = comp.window_attention_grads(*args[:3], _i32(off), r["y"], r["lse"], args[3],
+                                            **how)
+            own = slice(0, 2 * D if i in (1, 2) else D)  # (k and v are both heads')
+            print(f"[window] {typ} window={win} row {at} of input {i}", flush=True)
+            assert g["q"][at, own].isnan().all() and g["k"][at].isnan().all()
+            assert not i == 0 or not g["q"][at, D:].any()
+            assert i == 2 or not g["v"][at].isfinite().any()
+            rest = [t for t in alone if t != at]
+            assert not g["q"][rest].any() and not g["k"][rest].any()
+            assert g["q"].isfinite().sum() == g["q"].numel() - g["q"][at, own].numel()
+
+
+def test_window_rows_that_see_only_themselves_and_no_score(comp):
+    """A score of -infinity alone: its weight e^(z - lse) is no number."""
+    q, k = (torch.full((2, 8), x, device="cuda") for x in (-INF, 1.0))
+    q[1] = 1.0
+    off = _i32([0, 1, 2])
+    r = comp.window_attention(q, k, k, off, heads=1)
+    g = comp.window_attention_grads(q, k, k, off, r["y"], r["lse"], k, heads=1)
+    assert r["y"][0].isnan().all() and torch.equal(r["y"][1], k[1])
+    assert all(g[c][0].isnan().all() for c in "qkv")
+    assert not g["q"][1].any() and not g["k"][1].any() and torch.equal(g["v"][1], k[1])
