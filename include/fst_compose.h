@@ -663,7 +663,8 @@ FST_API int fst_window_attention_grads(fst_ctx *ctx, const fst_window_attention 
  * window.  Row i of q, k and v is the frame of position pos[i] of stream slot[i]
  * (slot NULL: stream i): its k and v are written to the caches, and y is its
  * attention to what the caches then hold, the frames of positions 0 .. pos[i] that
- * it sees.  k_cache and v_cache have num_slots * L rows.  A slot outside
+ * it sees.  k_cache and v_cache have num_slots * L rows (L past 2^31 - 257 gives
+ * FST_ERR_TOO_LARGE).  A slot outside
  * [0, num_slots) or a negative position marks an idle row: its y is 0, no cache is
  * read or written.  Slots of one call must differ. */
 FST_API int fst_window_attention_step(fst_ctx *ctx, const fst_matrix *q, const fst_matrix *k,

@@ -2965,7 +2965,9 @@ int fst_window_attention_step(fst_ctx *c, const fst_matrix *q, const fst_matrix 
   if (!cache_ok(k_cache, *k, num_slots, L) || !cache_ok(v_cache, *v, num_slots, L) ||
       (!slot && num_slots < q->rows) || (q->rows > 0 && !pos))
     return FST_ERR_INVALID_ARG;
-  if (attention_wide(q->cols, heads)) return FST_ERR_TOO_LARGE;
+  // (the kernel counts a ring's rows in 32 bits, past its end by up to 128: a turn of
+  // all wavefronts)
+  if (attention_wide(q->cols, heads) || L > INT32_MAX - 256) return FST_ERR_TOO_LARGE;
   if (q->rows == 0 || q->cols == 0) return FST_OK;
   DeviceGuard g(c->device);
   if (!g.ok) return FST_ERR_HIP;

@@ -255,3 +255,17 @@ def test_window_caches_are_checked(lib):
     assert fill(kc=one, vc=one, slots=1, slot=None) == INVALID
     assert step(pos=None) == INVALID
     assert fill(off=None) == INVALID and fill(seqs=-1) == INVALID and fill(seqs=0) == INVALID
+
+
+def test_window_step_refuses_rings_past_its_row_numbers(lib):
+    """Rows of a ring are counted in 32 bits, a few tiles past its end among them."""
+    q, k, y, r = _m(1, 32), _m(1, 16), _m(1, 32), ctypes.byref
+
+    def step(window, sinks):
+        cache = _m(window + sinks, 16)
+        return lib.fst_window_attention_step(CTX, r(q), r(k), r(k), 4, 2, window, sinks, 1.0,
+                                             SOME, None, 1, r(cache), r(cache), r(y), None)
+
+    most = 2 ** 31 - 257
+    assert step(2 ** 31 - 1, 0) == step(most, 1) == step(1, most) == LARGE
+    assert step(most, 0) not in (INVALID, LARGE)
