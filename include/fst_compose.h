@@ -553,6 +553,7 @@ FST_API int fst_recurrence_step(fst_ctx *ctx, const fst_matrix *x, const fst_mat
  * columns i and num_freq + i, or, with `pairs` not 0, columns 2 i and 2 i + 1.
  * Angles are taken in 64 bits: any position keeps float32's precision.
  *   q, k      q.cols and k.cols are multiples of width; k may be without columns
+ *             (more than 2^31 - 65 heads together give FST_ERR_TOO_LARGE)
  *   freq      device, float32, num_freq <= width / 2; NULL if num_freq is 0
  *   pos       device, q.rows; NULL if num_freq is 0
  * eps is finite and not negative. */

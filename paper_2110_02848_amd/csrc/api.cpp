@@ -2029,6 +2029,11 @@ bool head_norms_ok(const fst_head_norms *A) {
   if (A->num_freq > 0 && (!A->freq || (A->q.rows > 0 && !A->pos))) return false;
   return (A->q.cols == 0 || A->q_weight) && (A->k.cols == 0 || A->k_weight);
 }
+// (a row's heads of both are counted in 32 bits, past their end by a wavefront's turn)
+bool head_norms_large(const fst_head_norms *A) {
+  return A->width > FST_NORM_MAX_WIDTH ||
+         (A->q.cols + A->k.cols) / A->width > INT32_MAX - 64;
+}
 NormArgs norm_args(const fst_head_norms *A) {
   NormArgs a{};
   a.side[0].x = A->q.data, a.side[0].xs = pitch(A->q), a.side[0].w = A->q_weight;
@@ -2802,7 +2807,7 @@ int fst_head_norms_run(fst_ctx *c, const fst_head_norms *A, const fst_matrix *y_
   if (!c || !head_norms_ok(A) || !matrix_is(y_q, A->q, A->q.rows, A->q.cols) ||
       !matrix_is(y_k, A->q, A->k.rows, A->k.cols))
     return FST_ERR_INVALID_ARG;
-  if (A->width > FST_NORM_MAX_WIDTH) return FST_ERR_TOO_LARGE;
+  if (head_norms_large(A)) return FST_ERR_TOO_LARGE;
   if (A->q.rows == 0 || A->q.cols + A->k.cols == 0) return FST_OK;
   DeviceGuard g(c->device);
   if (!g.ok) return FST_ERR_HIP;
@@ -2821,7 +2826,7 @@ int fst_head_norms_grads(fst_ctx *c, const fst_head_norms *A, const fst_matrix *
     if (!matrix_is(m, A->q, A->q.rows, A->q.cols)) return FST_ERR_INVALID_ARG;
   for (const fst_matrix *m : {grad_yk, grad_k})
     if (!matrix_is(m, A->q, A->k.rows, A->k.cols)) return FST_ERR_INVALID_ARG;
-  if (A->width > FST_NORM_MAX_WIDTH) return FST_ERR_TOO_LARGE;
+  if (head_norms_large(A)) return FST_ERR_TOO_LARGE;
   DeviceGuard g(c->device);
   if (!g.ok) return FST_ERR_HIP;
   NormArgs a = norm_args(A);

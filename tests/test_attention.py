@@ -269,3 +269,16 @@ def test_window_step_refuses_rings_past_its_row_numbers(lib):
     most = 2 ** 31 - 257
     assert step(2 ** 31 - 1, 0) == step(most, 1) == step(1, most) == LARGE
     assert step(most, 0) not in (INVALID, LARGE)
+
+
+def test_norms_refuse_more_heads_than_are_counted(lib):
+    """Heads of queries and keys are counted together, in 32 bits."""
+    def calls(nq, nk):
+        q, k, r = _m(1, nq), _m(1, nk), ctypes.byref
+        a = _norms(q=q, k=k, width=1, num_freq=0)
+        return {lib.fst_head_norms_run(CTX, r(a), r(q), r(k), None),
+                lib.fst_head_norms_grads(CTX, r(a), r(q), r(k), r(q), r(k), None, None, None)}
+
+    most = 2 ** 31 - 1
+    assert calls(most, most) == calls(most, 0) == calls(most - 64, 1) == {LARGE}
+    assert not calls(most - 64, 0) & {INVALID, LARGE}
