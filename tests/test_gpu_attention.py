@@ -1065,3 +1065,98 @@ def test_window_rows_that_see_only_themselves_and_no_score(comp):
     assert r["y"][0].isnan().all() and torch.equal(r["y"][1], k[1])
     assert all(g[c][0].isnan().all() for c in "qkv")
     assert not g["q"][1].any() and not g["k"][1].any() and torch.equal(g["v"][1], k[1])
+
+
+@pytest.mark.parametrize("typ", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("H,G,D,win,sinks,lens", [
+    (2, 1, 64, 900, 0, [1]), (2, 1, 64, 900, 0, [20, 900, 901]), (8, 2, 64, 2000, 4, [700, 2003]),
+    (8, 2, 64, 2000, 4, [2004, 2005, 3000]), (20, 1, 32, 800, 64, [100, 864, 1900]),
+    (4, 4, 128, 1600, 1, [1601, 1]), (6, 3, 43, 1500, 10, [1300, 2900]),
+    (3, 1, 128, 30000, 0, [40]),
+])
+def test_window_steps_in_parts(comp, H, G, D, win, sinks, lens, typ):
+    """Few streams with long rings: parts of a ring, and their join.  A new frame in the
+    first part, a later one, and rings that leave later parts without frames."""
+    rows = len(lens) * G * ((H // G + 15) // 16)
+    assert min((512 + rows - 1) // rows, (win + sinks) // 384) > 1  # parts
+    test_window_steps(comp, H, G, D, win, sinks, lens, typ)
+
+
+@pytest.mark.parametrize("typ", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("T", [29000, 30500])
+def test_window_step_of_a_long_ring(comp, T, typ):
+    H, G, D, win, sinks = 2, 1, 64, 30000, 64
+    q, k, v, _ = _window_inputs([T], H, G, D, typ)
+    kc, vc = (torch.full((win + sinks, G * D), NAN, dtype=TYPES[typ], device="cuda")
+              for _ in range(2))
+    print(f"[step] ring {win + sinks}, frame {T} {typ}", flush=True)
+    comp.window_attention_fill(k[:-1], v[:-1], _i32([0, T - 1]), kc, vc, win, sinks)
+    y = comp.window_attention_step(q[-1:], k[-1:], v[-1:], _i32([T - 1]), kc, vc, heads=H,
+                                   kv_heads=G, window=win, sinks=sinks)
+    far = max(T - win, 0)  # the window's first frame
+    sees = list(range(min(sinks, far))) + list(range(far, T))
+    K, V, x = _d(k)[sees], _d(v)[sees], _d(q)[-1].view(H, D)
+    z = D ** -0.5 * x @ K.t()
+    w = torch.softmax(z, 1)
+    size = D ** -0.5 * (x.abs() @ K.abs().t()).max(1, keepdim=True).values
+    off = (2 * D + 24) * ref.U * (size + 1) + 16 * ref.U * (z.abs().max() + 1)
+    r = w @ V.abs()
+    # (as _step_reference has it, for every head)
+    bound = (4 * off + (2 * len(sees) + 64) * ref.U + ref.H16[TYPES[typ]]) * r
+    small = 2.0 ** -24 if typ == "f16" else 0.0
+    ref.within("y", y[0], (w @ V).view(-1), (bound + small * r.max()).view(-1))
+
+
+@pytest.mark.parametrize("typ", ["f32", "bf16"])
+def test_window_steps_in_parts_as_a_graph(comp, typ):
+    """Replays with new frames and positions, other calls of a larger workspace between
+    them, against eager calls bit for bit."""
+    H, G, D, win, sinks, n, T = 8, 2, 64, 1200, 4, 2, 6
+    L = win + sinks
+    g = _gen(5)
+    frames = [[_mat(g, n, w * D, typ) for w in (H, G, G)] for _ in range(T)]
+    begun = _mat(g, n * L, G * D, typ), _mat(g, n * L, G * D, typ)
+    at = [[0, 1203], [400, 1204], [1202, 1205], [1203, 2407], [1204, 2408], [2500, -1]]
+    how = dict(heads=H, kv_heads=G, window=win, sinks=sinks)
+    a, b = ([t.clone() for t in begun] for _ in range(2))
+    want = [comp.window_attention_step(*frames[t], _i32(at[t]), *a, **how) for t in range(T)]
+    x, pos = [t.clone() for t in frames[0]], _i32(at[0])
+    graph = torch.cuda.CUDAGraph()
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.graph(graph, stream=s):
+        y = comp.window_attention_step(*x, pos, *b, **how)
+    big = [_mat(g, 16, w * D, typ) for w in (H, G, G)]
+    ring = [torch.zeros(16 * L, G * D, dtype=TYPES[typ], device="cuda") for _ in range(2)]
+    for t in range(T):
+        for p, f in zip(x, frames[t]):
+            p.copy_(f)
+        pos.copy_(_i32(at[t]))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, want[t]), t
+        comp.window_attention_step(*big, _i32([1500] * 16), *ring, **how)
+        torch.cuda.synchronize()
+    assert all(torch.equal(p, r) for p, r in zip(a, b))
+
+
+@pytest.mark.parametrize("typ", ["f32", "f16", "bf16"])
+def test_linear_sequences_are_their_steps(comp, typ):
+    """The whole sequence's results and states within their bounds of the plain form,
+    that of the steps within theirs of the same."""
+    q, k, v, d, st, _, _ = _linear_inputs([150], 3, 40, 24, typ)
+    r = comp.linear_attention(q, k, v, d, _i32([0, 150]), state=st)
+    args = [_d(t) for t in (q, k, v)]
+    how = _d(d), [0, 150]
+    y, last = ref.linear(*args, *how, _d(st), False, 40 ** -0.5)
+    ay, al = ref.linear(*[t.abs() for t in args], *how, _d(st).abs(), False, 40 ** -0.5)
+    (by,), (bl,) = ref.linear_bounds(TYPES[typ], [ay], [al], 150)
+    ref.within("y", r["y"], y, by)
+    ref.within("last", r["last"], last, bl)
+    state = st.clone()
+    (by,), (bl,) = ref.linear_bounds(torch.float32, [ay], [al], 150 * 64)  # a chunk a step
+    for t in range(150):
+        x, state = comp.linear_attention_step(q[t:t + 1], k[t:t + 1], v[t:t + 1], d, state,
+                                              out=state)
+        ref.within(f"y {t}", x, y[t:t + 1], by[t:t + 1])
+    ref.within("last", state, last, bl)
