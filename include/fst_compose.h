@@ -635,8 +635,8 @@ FST_API int fst_linear_attention_step(fst_ctx *ctx, const fst_matrix *q, const f
  * (one as long as the sequences: all earlier frames), sinks >= 0, their sum at
  * most 2^31 - 1; blocks of 128 rows and sequences together more than 2^23 give
  * FST_ERR_TOO_LARGE.  With 16-bit matrices e^(z - maximum), and for the gradients
- * e^(z - lse) and the gradient of z, are rounded to the matrices' type (float16: those
- * of the gradients scaled by powers of two first) before they are multiplied. */
+ * e^(z - lse) and the gradient of z, are rounded to the matrices' type (float16: scaled
+ * by powers of two first) before they are multiplied. */
 typedef struct {
   int32_t num_seqs;
   const int32_t *offset;

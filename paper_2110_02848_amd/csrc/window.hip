@@ -48,6 +48,21 @@ constexpr float LOG2 = 0.69314718055994530942f, LOG2E = 1.4426950216293334960937
 template <typename T>
 constexpr int MIN_WAVES = sizeof(T) == 2 ? 2 : 1;
 
+// float16: dS is multiplied times a power of two (tiles.h) of the result that it is
+// summed into, a query's dq or a key's dk.
+template <typename T>
+constexpr bool SCALED = std::is_same<T, f16>::value;
+
+// float16: log 2 of what exponentials are multiplied by.  They are at most 1 (P, but for
+// lse's rounding) or 2^LATE (where the sums' maximum lags), and those of frames seen
+// faintly, or among many, below 2^-14, where float16 loses digits.
+template <typename T>
+constexpr float RAISE = SCALED<T> ? 12.0f : 0.0f;
+template <typename T>
+constexpr float RAISED = SCALED<T> ? 0x1p12f : 1.0f;
+template <typename T>
+constexpr float LATE = SCALED<T> ? 3.0f : 8.0f;
+
 __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
 
 template <int N, int M>
@@ -69,18 +84,6 @@ __device__ __forceinline__ float dot(const T *a, const T *b, int D) {
   for (int i = 0; i < D; ++i) x = fmaf((float)a[i], (float)b[i], x);
   return x;
 }
-
-// float16: dS is multiplied times a power of two (tiles.h) of the result that it is
-// summed into, a query's dq or a key's dk.
-template <typename T>
-constexpr bool SCALED = std::is_same<T, f16>::value;
-
-// float16: log 2 of what P is multiplied by for dv, and so dS too.  P of many frames is
-// below 2^-14, where float16 loses digits; it is at most 1 but for lse's rounding.
-template <typename T>
-constexpr float RAISE = SCALED<T> ? 12.0f : 0.0f;
-template <typename T>
-constexpr float RAISED = SCALED<T> ? 0x1p12f : 1.0f;
 
 // Whether query t sees no frame but itself: then dS is 0, or no number where one of its
 // factors is none, and no difference of two sums.
@@ -161,7 +164,7 @@ __device__ __noinline__ float4v exact_row(const T *q, const T *k, long long ks, 
 // Tiles of 64 keys come to two pairs of buffers in turn, the next one's loads under
 // way while one is multiplied.  m is the maximum that exponents are taken from: it
 // follows a row's maximum only once that is past it by LATE (powers of 2), so that
-// most tiles leave the sums as they are; p stays below 2^LATE.
+// most tiles leave the sums as they are; p stays below 2^LATE, times 2^RAISE.
 //
 // Bound by the vector units: of a wavefront's 160 or so instructions for a tile, 32 are
 // exponentials, which take four times as long (40,000 x 8 x 64 bf16, window 512: 85 to
@@ -170,7 +173,6 @@ __device__ __noinline__ float4v exact_row(const T *q, const T *k, long long ks, 
 template <typename T, int P, bool WIDE>
 __global__ __launch_bounds__(WNT, MIN_WAVES<T>) void k_window(WinArgs a) {
   constexpr int QT = QT_OF<T>, DT = P / 16, DS = P / 32, TILE = KEYS * P * (int)sizeof(T);
-  constexpr float LATE = 8.0f;
   extern __shared__ __attribute__((aligned(16))) char s_dyn[];  // [2][k, v][TILE]
   const int lane = threadIdx.x & (WAVE - 1), l16 = lane & 15, lg = lane >> 4;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
@@ -278,7 +280,7 @@ __global__ __launch_bounds__(WNT, MIN_WAVES<T>) void k_window(WinArgs a) {
           top[i] = fmaxf(fmaxf(top[i], x[kt][i][0]), x[kt][i][1]);
           top[i] = fmaxf(fmaxf(top[i], x[kt][i][2]), x[kt][i][3]);
         }
-        late = late || !((top[i] - m[i]) * c <= LATE);
+        late = late || !((top[i] - m[i]) * c <= LATE<T>);
       }
       if (__any(late)) {
 #pragma unroll
@@ -294,7 +296,7 @@ __global__ __launch_bounds__(WNT, MIN_WAVES<T>) void k_window(WinArgs a) {
       }
 #pragma unroll
       for (int i = 0; i < QT; ++i) {
-        const float mc = m[i] == -INFINITY ? 0.0f : m[i] * c;
+        const float mc = (m[i] == -INFINITY ? 0.0f : m[i] * c) - RAISE<T>;
 #pragma unroll
         for (int kt = 0; kt < 4; ++kt)
 #pragma unroll
@@ -331,7 +333,8 @@ __global__ __launch_bounds__(WNT, MIN_WAVES<T>) void k_window(WinArgs a) {
     T *y = static_cast<T *>(a.o) + (u.b + t) * a.os + (long long)h * D;
 #pragma unroll
     for (int d = 0; d < DT; ++d) store_four<T, WIDE>(y, 16 * d + 4 * lg, D, o[d][i] * f);
-    if (lg == 0) a.lse[(u.b + t) * a.H + h] = fmaf(m[i], c, log2f(l[i])) * LOG2;
+    if (lg == 0)
+      a.lse[(u.b + t) * a.H + h] = fmaf(m[i], c, log2f(l[i] * (1.0f / RAISED<T>))) * LOG2;
   }
   if (fine) return;
 #pragma unroll
@@ -343,7 +346,8 @@ __global__ __launch_bounds__(WNT, MIN_WAVES<T>) void k_window(WinArgs a) {
       if (none_of_four(y, d, D))
         mend_four(y, d, D,
                   exact_row<T>(q + t * a.qs, k, a.ks, v, a.vs, D, t, a.window, a.sinks,
-                               a.scale < 0.0f ? -c : c, m[i] == -INFINITY ? 0.0f : m[i] * c, d) *
+                               a.scale < 0.0f ? -c : c,
+                               (m[i] == -INFINITY ? 0.0f : m[i] * c) - RAISE<T>, d) *
                       (1.0f / l[i]));
   }
 }
@@ -1198,7 +1202,7 @@ __global__ __launch_bounds__(WNT) void k_window_step(WinStepArgs a) {
     for (int b = 0; b < 2; ++b)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        x[b][r] = exp2_of(x[b][r] - shift);
+        x[b][r] = exp2_of(x[b][r] - (shift - RAISE<T>));
         l += x[b][r];
       }
     const Frag<T> p = pack<T>(x[0], x[1]);

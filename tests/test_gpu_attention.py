@@ -1160,3 +1160,31 @@ def test_linear_sequences_are_their_steps(comp, typ):
                                               out=state)
         ref.within(f"y {t}", x, y[t:t + 1], by[t:t + 1])
     ref.within("last", state, last, bl)
+
+
+@pytest.mark.parametrize("win,sinks", [(1000, 0), (40, 1)])
+@pytest.mark.parametrize("D", [16, 128])
+def test_window_float16_values_seen_faintly(comp, D, win, sinks):
+    """A first frame without a value that takes all but 2^-20 of every query's weight:
+    what the others give has float16's digits all the same, in whole sequences and in
+    a step.  (Weights are scaled to 2^12, and each of at most 300 off by 2^-25 2^-12 of a v,
+    at most 5 * 2^10.)"""
+    T = 300
+    q, k, v, _ = _window_inputs([T], 1, 1, D, "f16")
+    q, k = (t.float() / 8 for t in (q, k))
+    q[:, 0], k[:, 0] = D ** 0.5, 0.0
+    k[0, 0] = 13.875
+    q, k, v = q.half(), k.half(), (v.float() * 2.0 ** 10).half()
+    v[0] = 0.0
+    how = dict(heads=1, kv_heads=1, window=win, sinks=sinks)
+    r = comp.window_attention(q, k, v, _i32([0, T]), **how)
+    o = ref.window(_d(q), _d(k), _d(v), [0, T], 1, 1, win, sinks, D ** -0.5)
+    bound = (o["by"] + ref.H16[torch.float16] * o["ry"]
+             + 300 * 2.0 ** -37 * 5 * 2.0 ** 10)
+    ref.within("y", r["y"], o["y"], bound)
+    ref.within("lse", r["lse"], o["lse"], o["blse"])
+    L = win + sinks
+    kc, vc = (torch.zeros(L, D, dtype=torch.float16, device="cuda") for _ in range(2))
+    comp.window_attention_fill(k[:-1], v[:-1], _i32([0, T - 1]), kc, vc, win, sinks)
+    y = comp.window_attention_step(q[-1:], k[-1:], v[-1:], _i32([T - 1]), kc, vc, **how)
+    ref.within("step", y, o["y"][-1:], bound[-1:])
