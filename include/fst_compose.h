@@ -551,7 +551,8 @@ FST_API int fst_recurrence_step(fst_ctx *ctx, const fst_matrix *x, const fst_mat
  * then the first 2 * num_freq columns are num_freq pairs, each turned by the
  * angle pos[row] * freq[i]:  (a, b) -> (a cos - b sin, b cos + a sin).  Pair i is
  * columns i and num_freq + i, or, with `pairs` not 0, columns 2 i and 2 i + 1.
- * Angles are taken in 64 bits: any position keeps float32's precision.
+ * Angles are taken in 64 bits: any position keeps float32's precision.  Squares are
+ * float32: a head whose sum of them is past its largest number gives 0.
  *   q, k      q.cols and k.cols are multiples of width; k may be without columns
  *             (more than 2^31 - 65 heads together give FST_ERR_TOO_LARGE)
  *   freq      device, float32, num_freq <= width / 2; NULL if num_freq is 0
@@ -677,9 +678,10 @@ FST_API int fst_window_attention_step(fst_ctx *ctx, const fst_matrix *q, const f
                                       void *stream);
 
 /* Fills the caches of fst_window_attention_step with whole sequences, that of
- * sequence s in stream slot[s] (NULL: s; outside [0, num_slots): left out), so that
- * the next frame's position is its length.  Rows that no frame belongs in are left
- * as they are.  k and v have the caches' columns; window and sinks are theirs. */
+ * sequence s in stream slot[s] (NULL: s; outside [0, num_slots): left out; all others of
+ * a call must differ), so that the next frame's position is its length.  Rows that no
+ * frame belongs in are left as they are.  k and v have the caches' columns; window and
+ * sinks are theirs. */
 FST_API int fst_window_attention_fill(fst_ctx *ctx, int32_t num_seqs, const int32_t *offset,
                                       const fst_matrix *k, const fst_matrix *v, int32_t window,
                                       int32_t sinks, const int32_t *slot, int32_t num_slots,

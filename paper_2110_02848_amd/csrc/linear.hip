@@ -132,12 +132,13 @@ __device__ __forceinline__ Place place_of(int H, int slices) {
 //
 // Bound by memory for heads of 64 (40,000 x 8 x 64 x 64 bf16: 37 us for 164 MB, 4.4 TB/s,
 // the units' states 22 before it), for wider ones by a chunk's steps, each waiting for
-// the one before with two wavefronts a SIMD (64 x 2,000 x 8 x 128 x 128 bf16 with
-// gradients: 920 to 960 us; 40 % of cycles on the vector units, 20 % on the matrix cores).
-// Two workgroups of 64 columns a CU in place of one of 128 took as long.
+// the one before with two wavefronts a SIMD (64 x 2,000 x 8 x 128 x 128 bf16 271 to 290
+// us, its gradients 733 to 786; 40 % of cycles on the vector units, 20 % on the matrix
+// cores).  Two workgroups of 64 columns a CU in place of one of 128 took as long.
 //
 // MIN_WAVES: wavefronts of a SIMD, at least: with one the compiler takes registers
 // that the vector units cannot add in (that case by 64 columns: 1,316 us, with two 960).
+// With three float16 spills 5 of them where heads are 64 wide, 18 number by number.
 template <typename T, int PA, int CG>
 constexpr int MIN_WAVES = CG == 2 ? 2 : sizeof(T) == 4 ? 1 : PA == 64 ? 3 : 2;
 template <typename T, int PA, int CG, bool WIDE, bool FULL>

@@ -39,7 +39,13 @@ constexpr int QT_OF = sizeof(T) == 2 ? 2 : 1;
 template <typename T>
 constexpr int BLOCK_OF = 16 * QT_OF<T> * WNW;  // queries, or keys, of a workgroup
 constexpr int FEW = 64;              // frames
-constexpr int MAX_CUT = 256;         // first frames whose queries are cut into units
+// First frames whose queries are cut into units, at most.  A unit takes workspace and
+// time for each of them, an uncut sequence walks all its queries for a block of them.
+// Gradients, cut and uncut, 64, 256 and 512 of them: 16 x 2,000 x 16 + 4 x 128 bf16, window
+// 1,000: 1,068 and 1,083, 1,366 and 1,116, 1,759 and 1,187 us; 64 x 500 x 8 x 64, window
+// 100: 201 and 190, 286 and 211, 380 and 216; 1 x 20,000 x 8 + 2 x 64, window 256: 186 and
+// 4,925, 280 and 4,867, 409 and 4,836.  (Past it the long sequence would still gain.)
+constexpr int MAX_CUT = 256;
 constexpr float LOG2 = 0.69314718055994530942f, LOG2E = 1.44269502162933349609375f;
 
 // Wavefronts of a SIMD, at least, of the kernels below.  Two have half of its
@@ -166,10 +172,13 @@ __device__ __noinline__ float4v exact_row(const T *q, const T *k, long long ks, 
 // follows a row's maximum only once that is past it by LATE (powers of 2), so that
 // most tiles leave the sums as they are; p stays below 2^LATE, times 2^RAISE.
 //
-// Bound by the vector units: of a wavefront's 160 or so instructions for a tile, 32 are
-// exponentials, which take four times as long (40,000 x 8 x 64 bf16, window 512: 85 to
-// 96 us as the card's clock goes, 64 % of cycles on the vector units, 24 % on the matrix
-// cores; 16 x 2,000 x 16 x 128, window 1,000: 214 us, 44 and 29 %).
+// Bound by the vector units: a wavefront takes 2,910 of their instructions for up to 11
+// tiles, and a tile's 32 exponentials last four times as long as the others (40,000 x 8 x
+// 64 bf16, window 512: 87 to 88 us, 63 % of cycles on the vector units, 25 % on the matrix
+// cores; 16 x 2,000 x 16 x 128, window 1,000: 228 to 243 us, 43 and 30 %).  Rows that are
+// no whole groups of 16 bytes go through registers number by number, for which there is
+// not room enough at widths past 64 (16 x 2,000 x 16 x 100: 1,234 us, back 6,427; of 60
+// 430 and 1,246, of 64 173 and 624).
 template <typename T, int P, bool WIDE>
 __global__ __launch_bounds__(WNT, MIN_WAVES<T>) void k_window(WinArgs a) {
   constexpr int QT = QT_OF<T>, DT = P / 16, DS = P / 32, TILE = KEYS * P * (int)sizeof(T);
@@ -1012,7 +1021,7 @@ __device__ __forceinline__ void sinks_block(const WinArgs &a, const Unit &u, int
 // Workgroups of all three: blocks of keys, blocks of queries, units for the first
 // frames.  Seven products where five are needed: scores and dy v^T are computed for dq
 // and again for dk and dv.  Bound by what a wavefront waits for between them with
-// two a SIMD (16 x 2,000 x 16 heads of 128 bf16, window 1,000: 720 to 740 us, 28 % of
+// two a SIMD (16 x 2,000 x 16 heads of 128 bf16, window 1,000: 770 to 810 us, 28 % of
 // cycles on the matrix cores, 28 % on the vector units).
 template <typename T, int P, bool WIDE>
 __global__ __launch_bounds__(WNT, MIN_WAVES<T>) void k_window_back(WinArgs a) {
@@ -1044,7 +1053,9 @@ __global__ __launch_bounds__(WNT, MIN_WAVES<T>) void k_window_back(WinArgs a) {
 // delta from y as it was rounded is off by half a spacing of y, which is next to
 // nothing beside dS of many frames but as much as the rounding of dS beside few:
 // queries of a sequence's first block, and of windows up to FEW frames, have it
-// summed again from P and dy v^T (the same case: 11 us).
+// summed again from P and dy v^T (the same case: 11 us).  (Where one of many frames takes
+// nearly all the weight, dS keeps of it what y's rounding leaves: to sum it again for
+// all queries would be two of seven products more.)
 template <typename T, int P, bool WIDE>
 __global__ __launch_bounds__(WNT, MIN_WAVES<T>) void k_window_sums(WinArgs a, int every) {
   constexpr int BLOCK = BLOCK_OF<T>;
@@ -1090,8 +1101,8 @@ __device__ __forceinline__ int ring(int p, int window, int sinks) {
 // part of its cache, 32 frames a wavefront at a time: k straight from memory as
 // an operand, v through LDS of the wavefront's own.  The row's own frame comes
 // from k and v, and the first part writes it to the cache, where no one reads it.
-// Bound by memory (256 rows of 16 + 4 heads of 128 f16, window 1,000: 83 us for 441 MB,
-// 5.3 TB/s); few rows by a load's way and the parts' join.
+// Bound by memory (256 rows of 16 + 4 heads of 128 f16, window 1,000: 82 to 86 us for 441
+// MB, 5.1 to 5.4 TB/s); few rows by a load's way and the parts' join.
 template <typename T, int P, bool WIDE>
 __global__ __launch_bounds__(WNT) void k_window_step(WinStepArgs a) {
   constexpr int DT = P / 16, DS = P / 32, GROUPS = P / PER<T>, LOADS = 32 * GROUPS / WAVE;
@@ -1274,7 +1285,8 @@ __global__ __launch_bounds__(P) void k_window_join(WinStepArgs a) {
 }
 
 // Rows of the caches from the frames of whole sequences: entry c holds the last
-// frame that the ring puts there.
+// frame that the ring puts there.  (256 streams of 1,004 frames of 4 heads of 128 f16: 419 us
+// for 1.05 GB, 2.5 TB/s: two bytes a lane.)
 template <typename T>
 __global__ __launch_bounds__(WNT) void k_window_fill(WinFillArgs a) {
   const int s = a.first + blockIdx.y, L = a.sinks + a.window;

@@ -968,7 +968,7 @@ class Composer:
                               stream=None):
         """Fills the caches of ``window_attention_step`` with whole sequences
         (k, v, offset as in ``window_attention``), that of sequence s in stream
-        slot[s] (int32 [n], None: s)."""
+        slot[s] (int32 [n], None: s; no two the same)."""
         n = int(offset.numel()) - 1
         if n < 0:
             raise ValueError("offset: at least one entry is needed")
