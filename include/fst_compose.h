@@ -551,8 +551,8 @@ FST_API int fst_recurrence_step(fst_ctx *ctx, const fst_matrix *x, const fst_mat
  * then the first 2 * num_freq columns are num_freq pairs, each turned by the
  * angle pos[row] * freq[i]:  (a, b) -> (a cos - b sin, b cos + a sin).  Pair i is
  * columns i and num_freq + i, or, with `pairs` not 0, columns 2 i and 2 i + 1.
- * Angles are taken in 64 bits: any position keeps float32's precision.  Squares are
- * float32: a head whose sum of them is past its largest number gives 0.
+ * Angles are taken in 64 bits: any position keeps float32's precision.  So do heads
+ * whose squares are past float32's largest number, or (with such an eps) its smallest.
  *   q, k      q.cols and k.cols are multiples of width; k may be without columns
  *             (more than 2^31 - 65 heads together give FST_ERR_TOO_LARGE)
  *   freq      device, float32, num_freq <= width / 2; NULL if num_freq is 0

@@ -29,6 +29,32 @@ __device__ __forceinline__ float2 turn(int32_t pos, float freq) {
   return make_float2(c, s);
 }
 
+// Whether a head's sum of squares, or numbers below it, may have left float32 (those of
+// float16 numbers do not).
+template <typename T>
+__device__ __forceinline__ bool leaves(float sum, float eps) {
+  if constexpr (std::is_same<T, f16>::value) return false;
+  return !(sum < 0x1p120f) || (sum < 0x1p-100f && eps < 0x1p-100f);
+}
+// Such a head again, with a power of two, which is returned, times its numbers x and the
+// root of eps: `sum` is that of their squares.  The head lies in `lanes` lanes.
+template <int N>
+__device__ __forceinline__ float brought_back(float (&x)[N], float &sum, float eps, int lanes) {
+  float most = sqrtf(eps);
+#pragma unroll
+  for (int j = 0; j < N; ++j) most = fmaxf(most, fabsf(x[j]));
+  for (int m = lanes / 2; m; m /= 2) most = fmaxf(most, __shfl_xor(most, m, WAVE));
+  const float s = power_below(most, 0);
+  sum = 0.0f;
+#pragma unroll
+  for (int j = 0; j < N; ++j) {
+    x[j] *= s;
+    sum = fmaf(x[j], x[j], sum);
+  }
+  for (int m = lanes / 2; m; m /= 2) sum += __shfl_xor(sum, m, WAVE);
+  return s;
+}
+
 // Heads of whole 16-byte groups.  A lane holds V = 16 bytes' pairs of a head, a[j] and
 // b[j], of angle c V + j for lane c of the head's: with `PAIRS` 32 bytes that lie
 // side by side, else two groups P apart (two side by side where nothing turns).
@@ -88,7 +114,9 @@ __global__ __launch_bounds__(NT) void k_norms_wide(NormArgs a, int rows, int lan
         sum = fmaf(z[j], z[j], sum);
       }
       for (int m = lanes / 2; m; m /= 2) sum += __shfl_xor(sum, m, WAVE);
-      const float r = 1.0f / sqrtf(sum / (float)a.D + a.eps);
+      float s = 1.0f;
+      if (leaves<T>(sum, a.eps)) s = brought_back(z, sum, a.eps, lanes);
+      const float r = 1.0f / sqrtf(sum / (float)a.D + a.eps * s * s);
       float y[2 * V];
 #pragma unroll
       for (int j = 0; j < 2 * V; ++j) {
@@ -116,7 +144,7 @@ __global__ __launch_bounds__(NT) void k_norms_wide(NormArgs a, int rows, int lan
         for (int m = lanes / 2; m; m /= 2) dot += __shfl_xor(dot, m, WAVE);
         dot /= (float)a.D;
 #pragma unroll
-        for (int j = 0; j < 2 * V; ++j) y[j] = r * (y[j] - z[j] * dot);
+        for (int j = 0; j < 2 * V; ++j) y[j] = r * s * (y[j] - z[j] * dot);
       }
       if (on) {
         Group y0, y1;
@@ -199,7 +227,9 @@ __global__ __launch_bounds__(NT) void k_norms(NormArgs a) {
       if (hh + NWAVES < heads) fetch(row, hh + NWAVES);
 #pragma unroll
       for (int m = 32; m; m >>= 1) sum += __shfl_xor(sum, m, WAVE);
-      const float r = 1.0f / sqrtf(sum / (float)a.D + a.eps);
+      float s = 1.0f;
+      if (leaves<T>(sum, a.eps)) s = brought_back(xv, sum, a.eps, WAVE);
+      const float r = 1.0f / sqrtf(sum / (float)a.D + a.eps * s * s);
       // what is turned meets its pair in LDS (a wavefront's own, in order)
 #pragma unroll
       for (int e = 0; e < E; ++e) {
@@ -248,7 +278,7 @@ __global__ __launch_bounds__(NT) void k_norms(NormArgs a) {
 #pragma unroll
         for (int e = 0; e < E; ++e) {
           const int d = e * WAVE + lane;
-          if (d < a.D) y[d] = (T)(r * (t[e] - xv[e] * r * dot));
+          if (d < a.D) y[d] = (T)(r * s * (t[e] - xv[e] * r * dot));
         }
       }
     }

@@ -1188,3 +1188,16 @@ def test_window_float16_values_seen_faintly(comp, D, win, sinks):
     comp.window_attention_fill(k[:-1], v[:-1], _i32([0, T - 1]), kc, vc, win, sinks)
     y = comp.window_attention_step(q[-1:], k[-1:], v[-1:], _i32([T - 1]), kc, vc, **how)
     ref.within("step", y, o["y"][-1:], bound[-1:])
+
+
+@pytest.mark.parametrize("typ", ["f32", "bf16"])
+@pytest.mark.parametrize("D,P,pairs", [(64, 32, False), (48, 16, True), (43, 13, False),
+                                       (300, 20, True), (512, 256, False)])
+def test_norms_of_numbers_whose_squares_leave_float32(comp, D, P, pairs, typ):
+    """Results and gradients within the same bounds, beside rows of ordinary size."""
+    for e, eps in ((70, 1e-6), (120, 1e-6), (60, 0.0), (-60, 1e-37), (-70, 0.0), (-110, 0.0)):
+        args = list(_norm_inputs(6, 3, 2, D, P, typ))
+        for i in (0, 1):
+            args[i] = args[i].clone()
+            args[i][1:] *= 2.0 ** e
+        _check_norms(comp, *args, eps, pairs)
