@@ -127,8 +127,8 @@ __device__ __forceinline__ Place place_of(int H, int slices) {
 // Roundings to 16 bits: scores and the state that meets q, once each.  The decayed k
 // that go into the state are as many numbers as hold them: states are float32
 // results.  float16: all three are scaled by powers of two, scores by one of the
-// row's own (tiles.h), the others by the chunk's largest numbers and a bound on the
-// state's, so that they neither overflow nor lose their digits.
+// row's own (tiles.h), the decayed k by the largest of the chunk's, the state by a bound
+// on its numbers, so that they neither overflow nor lose their digits.
 //
 // Bound by memory for heads of 64 (40,000 x 8 x 64 x 64 bf16: 37 us for 164 MB, 4.4 TB/s,
 // the units' states 22 before it), for wider ones by a chunk's steps, each waiting for
@@ -232,7 +232,6 @@ __global__ __launch_bounds__(256 * CG, (MIN_WAVES<T, PA, CG>)) void k_linear(Lin
   const double all = power_of(g, CHUNK);
   float keep = (float)all, keep_lo = (float)(all - (double)keep);
   if (!(fabsf(keep) < INFINITY)) keep_lo = 0.0f;
-  const float most = fmaxf(1.0f, keep);
 
   const T *q = static_cast<const T *>(job.q) + (long long)h * A;
   const T *k = static_cast<const T *>(job.k) + (long long)h * A;
@@ -264,7 +263,8 @@ __global__ __launch_bounds__(256 * CG, (MIN_WAVES<T, PA, CG>)) void k_linear(Lin
     rk.store(s_k);
     rv.store(s_v);
     if constexpr (SCALED) {
-      const float mk = wave_max(rk.largest()), mv = wave_max(rv.largest());
+      const float mk = wave_max(rk.largest(s_end + (CHUNK - count), count));
+      const float mv = wave_max(rv.largest());
       if (lane == 0) s_max[w][0] = mk, s_max[w][1] = mv;
     }
     __syncthreads();
@@ -273,8 +273,8 @@ __global__ __launch_bounds__(256 * CG, (MIN_WAVES<T, PA, CG>)) void k_linear(Lin
     float p_scale = SCALED ? UNMET : 1.0f, k_scale = 1.0f;
     if constexpr (SCALED) {
       const float mk = largest(s_max, 0), mv = largest(s_max, 1);
-      k_scale = fminf(power_below(most * fabsf(job.sk) * mk, 12), 0x1p60f);
-      bound = fmaf(keep, bound, most * fabsf(job.sk) * CHUNK * mk * mv);
+      bound = fmaf(keep, bound, fabsf(job.sk) * CHUNK * mk * mv);
+      k_scale = fminf(power_below(fabsf(job.sk) * mk, 12), power_below(bound, 100));
     }
     if constexpr (FULL) {
       float4v past[NJ] = {}, now[NJ] = {};

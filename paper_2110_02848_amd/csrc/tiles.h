@@ -205,18 +205,22 @@ struct Stage {
       *reinterpret_cast<int4v *>(t + r * LD<T, P> + c) = v[i];
     }
   }
-  // the largest finite magnitude in it
-  __device__ __forceinline__ float largest() const {
+  // the largest finite magnitude in it, or with `weight` that of a row's numbers times
+  // weight[row] (of rows below `count`)
+  __device__ __forceinline__ float largest(const float *weight = nullptr, int count = 0) const {
     float m = 0.0f;
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) {
       struct alignas(16) { T v[PER<T>]; } e;
       __builtin_memcpy(&e, &v[i], 16);
+      float most = 0.0f;
 #pragma unroll
       for (int j = 0; j < PER<T>; ++j) {
         const float x = fabsf((float)e.v[j]);
-        m = x < INFINITY ? fmaxf(m, x) : m;
+        most = x < INFINITY ? fmaxf(most, x) : most;
       }
+      const int r = (i * NTH + (int)threadIdx.x) / GROUPS;
+      m = fmaxf(m, !weight ? most : r < count ? most * weight[r] : 0.0f);
     }
     return m;
   }

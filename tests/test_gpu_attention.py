@@ -1201,3 +1201,40 @@ def test_norms_of_numbers_whose_squares_leave_float32(comp, D, P, pairs, typ):
             args[i] = args[i].clone()
             args[i][1:] *= 2.0 ** e
         _check_norms(comp, *args, eps, pairs)
+
+
+@pytest.mark.parametrize("rev", [False, True])
+@pytest.mark.parametrize("T,V", [(64, 32), (150, 32), (1100, 100)])
+def test_linear_float16_states_after_silence(comp, T, V, rev):
+    """Rows without keys behind a few with them: what is left of those after a fast decay
+    has float32's digits in the last state.  (A decayed k is two numbers of 11 bits, of
+    the chunk's largest decayed k scaled to 2^11 or more: off by 2^-22 of itself and by
+    2^-36 of the largest, a v at most 5 and one of 64 rows.)"""
+    q, k, v, _, _, gy, gl = _linear_inputs([T], 2, 32, V, "f16")
+    d = torch.tensor([-0.5, -0.9]).cuda()
+    at = slice(T - 60, T - 50) if not rev else slice(50, 60)
+    for t in (k, q):
+        keep = t[at].clone()
+        t.zero_()
+        t[at] = keep
+    print(f"[linear] silence, {T} x {V} rev={rev}", flush=True)
+    last = comp.linear_attention(q, k, v, d, _i32([0, T]), reverse=rev)["last"]
+    args = [_d(t) for t in (q, k, v)]
+    _, want = ref.linear(*args, _d(d), [0, T], None, rev, 32 ** -0.5)
+    _, size = ref.linear(*[t.abs() for t in args], _d(d), [0, T], None, rev, 32 ** -0.5)
+    most = size.flatten(2).max(2).values[:, :, None, None]
+    bound = (600 * ref.U + 2.0 ** -22) * size + 64 * 5 * 2.0 ** -36 * most
+    ref.within("last", last, want, bound)
+
+
+def test_linear_float16_with_a_large_state(comp):
+    """Small keys beside a state of 2^100."""
+    q, k, v, d, st, _, _ = _linear_inputs([100], 2, 32, 32, "f16")
+    k = (k.float() * 2.0 ** -20).half()
+    st = st * 2.0 ** 100
+    last = comp.linear_attention(q, k, v, d, _i32([0, 100]), state=st)["last"]
+    args = [_d(t) for t in (q, k, v)]
+    _, want = ref.linear(*args, _d(d), [0, 100], _d(st), False, 32 ** -0.5)
+    _, size = ref.linear(*[t.abs() for t in args], _d(d), [0, 100], _d(st).abs(), False,
+                         32 ** -0.5)
+    ref.within("last", last, want, 600 * ref.U * size)
