@@ -132,8 +132,8 @@ __device__ __forceinline__ Place place_of(int H, int slices) {
 //
 // Bound by memory for heads of 64 (40,000 x 8 x 64 x 64 bf16: 37 us for 164 MB, 4.4 TB/s,
 // the units' states 22 before it), for wider ones by a chunk's steps, each waiting for
-// the one before with two wavefronts a SIMD (64 x 2,000 x 8 x 128 x 128 bf16 270 to 283
-// us, its gradients 733 to 768; 40 % of cycles on the vector units, 20 % on the matrix
+// the one before with two wavefronts a SIMD (64 x 2,000 x 8 x 128 x 128 bf16 270 to 291
+// us, its gradients 733 to 797; 40 % of cycles on the vector units, 20 % on the matrix
 // cores).  Two workgroups of 64 columns a CU in place of one of 128 took as long.
 //
 // MIN_WAVES: wavefronts of a SIMD, at least: with one the compiler takes registers

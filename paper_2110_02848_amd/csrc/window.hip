@@ -174,8 +174,8 @@ __device__ __noinline__ float4v exact_row(const T *q, const T *k, long long ks, 
 //
 // Bound by the vector units: a wavefront takes 2,910 of their instructions for up to 11
 // tiles, and a tile's 32 exponentials last four times as long as the others (40,000 x 8 x
-// 64 bf16, window 512: 87 to 89 us, 62 % of cycles on the vector units, 24 % on the matrix
-// cores; 16 x 2,000 x 16 x 128, window 1,000: 225 to 238 us, 43 and 30 %).  Rows that are
+// 64 bf16, window 512: 87 to 90 us, 63 % of cycles on the vector units, 24 % on the matrix
+// cores; 16 x 2,000 x 16 x 128, window 1,000: 225 to 242 us, 43 and 30 %).  Rows that are
 // no whole groups of 16 bytes go through registers number by number, for which there is
 // not room enough at widths past 64 (16 x 2,000 x 16 x 100: 1,234 us, back 6,427; of 60
 // 430 and 1,246, of 64 173 and 624).
@@ -1021,7 +1021,7 @@ __device__ __forceinline__ void sinks_block(const WinArgs &a, const Unit &u, int
 // Workgroups of all three: blocks of keys, blocks of queries, units for the first
 // frames.  Seven products where five are needed: scores and dy v^T are computed for dq
 // and again for dk and dv.  Bound by what a wavefront waits for between them with
-// two a SIMD (16 x 2,000 x 16 heads of 128 bf16, window 1,000: 764 to 797 us, 28 % of
+// two a SIMD (16 x 2,000 x 16 heads of 128 bf16, window 1,000: 764 to 809 us, 28 % of
 // cycles on the matrix cores, 28 % on the vector units).
 template <typename T, int P, bool WIDE>
 __global__ __launch_bounds__(WNT, MIN_WAVES<T>) void k_window_back(WinArgs a) {
@@ -1101,8 +1101,8 @@ __device__ __forceinline__ int ring(int p, int window, int sinks) {
 // part of its cache, 32 frames a wavefront at a time: k straight from memory as
 // an operand, v through LDS of the wavefront's own.  The row's own frame comes
 // from k and v, and the first part writes it to the cache, where no one reads it.
-// Bound by memory (256 rows of 16 + 4 heads of 128 f16, window 1,000: 82 to 85 us for 441
-// MB, 5.2 to 5.4 TB/s); few rows by a load's way and the parts' join.
+// Bound by memory (256 rows of 16 + 4 heads of 128 f16, window 1,000: 81 to 86 us for 441
+// MB, 5.1 to 5.4 TB/s); few rows by a load's way and the parts' join.
 template <typename T, int P, bool WIDE>
 __global__ __launch_bounds__(WNT) void k_window_step(WinStepArgs a) {
   constexpr int DT = P / 16, DS = P / 32, GROUPS = P / PER<T>, LOADS = 32 * GROUPS / WAVE;
